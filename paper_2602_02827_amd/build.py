@@ -9,17 +9,21 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcolbandit.so")
 SOURCES = ["cb_api.hip", "cb_kernels.hip", "cb_dense.hip", "cb_quant.hip", "cb_baselines.hip"]
-HEADERS = ["cb_device.h", "cb_launch.h", "cb_segments.h", "cb_sample.h", os.path.join("..", "..", "include", "colbandit.h")]
+# the training operators: infinities and NaN have their meaning there
+TRAIN_SOURCES = ["cb_train_api.hip", "cb_attention_bf16.hip", "cb_attention_f32.hip", "cb_contrast.hip", "cb_clip.hip"]
+HEADERS = ["cb_device.h", "cb_launch.h", "cb_segments.h", "cb_sample.h", "cb_train.h", "cb_tile.h", "cb_attention.h",
+           os.path.join("..", "..", "include", "colbandit.h"), os.path.join("..", "..", "include", "colbandit_train.h")]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-Xarch_device", "-fno-honor-nans", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          # packed fp32 VALU forms are kept off for the device code of this library
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
+TRAIN_FLAGS = [f for f in FLAGS if f not in ("-Xarch_device", "-fno-honor-nans")]
 
 
 def _stale() -> bool:
     if not os.path.exists(LIB):
         return True
     t = os.path.getmtime(LIB)
-    return any(os.path.getmtime(os.path.join(CSRC, f)) > t for f in SOURCES + HEADERS)
+    return any(os.path.getmtime(os.path.join(CSRC, f)) > t for f in SOURCES + TRAIN_SOURCES + HEADERS)
 
 
 def build_library(force: bool = False, verbose: bool = False) -> str:
@@ -28,9 +32,9 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     objs = []
     procs = []
-    for src in SOURCES:
+    for src in TRAIN_SOURCES + SOURCES:
         obj = os.path.join(CSRC, src.replace(".hip", ".o"))
-        cmd = [hipcc, *FLAGS, "-c", os.path.join(CSRC, src), "-o", obj]
+        cmd = [hipcc, *(FLAGS if src in SOURCES else TRAIN_FLAGS), "-c", os.path.join(CSRC, src), "-o", obj]
         procs.append((cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT,
                                             text=True)))
         objs.append(obj)
