@@ -48,7 +48,7 @@ extern "C" {
  * anything, infinities and NaN included.
  * Rows of q, k and v lie q_row elements apart and heads q_head apart (likewise k, v); the d
  * values of a row and head are consecutive.  Pointers and strides are whole multiples of 16
- * bytes.  out and all gradients are dense, [rows][heads][d].
+ * bytes; rows lie at most 32 MiB apart.  out and all gradients are dense, [rows][heads][d].
  * Preconditions the host cannot check without a copy: offsets are non-decreasing, from 0 to
  * total_q (total_k).  Kernels clamp them, so a violation gives meaningless results, never an
  * out-of-bounds access; rows that no sequence holds are not written.

@@ -7,87 +7,37 @@
 // Where several query heads share a key head and there is no bias, their rows share tiles: column c is row c / pack of
 // head c % pack, so keys and values are staged once for all of them, and a single token still fills its columns.
 #pragma once
+#include <type_traits>
+
 #include "cb_tile.h"
 #include "cb_train.h"
 
 namespace cb {
 
-// First columns' row, rows and key limits of a tile of query columns.
-struct QueryTile {
-    int seq, row0, Lq, Lk, q0, k0;      // sequence, first local row, lengths, first global rows
-    bool none;
-};
-__device__ __forceinline__ QueryTile query_tile(const AttnArgs& A, int slot, int per, int lane) {
-    QueryTile t;
-    t.seq = find_sequence(A.qoff, A.n_seqs, per, A.total_q, slot, lane);
-    const Range q = sequence_rows(A.qoff, t.seq, A.total_q), k = sequence_rows(A.koff, t.seq, A.total_k);
-    t.row0 = (slot - place_of(A.qoff, t.seq, per, A.total_q)) * per;
-    t.Lq = q.n;
-    t.Lk = k.n;
-    t.q0 = q.lo;
-    t.k0 = k.lo;
-    t.none = t.row0 < 0 || t.row0 >= q.n;
-    return t;
-}
-
-// Bias of a head by distance key - query, -reach .. reach, in powers of two.  Finite values stay finite.
-template <class E>
-__device__ __forceinline__ int bucket_of(const AttnArgs& A, int dist) {
-    const int far = A.causal ? (dist < 0 ? -dist : 0) : (dist < 0 ? -dist : dist);
-    int lo = 0, hi = A.n_dir;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (A.starts[mid] <= far) lo = mid; else hi = mid;
-    }
-    return lo + (!A.causal && dist > 0 ? A.n_dir : 0);
-}
+// Bias of a head by distance key - query, in powers of two; finite values stay finite.  A block of 32 x 32 distances that
+// is not all in one direction's last bucket reaches less than kBlock beyond `reach`: the table is that much longer, so that no
+// distance is clamped when it is looked up, and a lane's sixteen places differ by constants.
+constexpr int kBlock = 62;
+__device__ __host__ __forceinline__ int bias_middle(int reach) { return reach + kBlock; }
+__device__ __host__ __forceinline__ int bias_width(int reach) { return 2 * bias_middle(reach) + 1; }
 template <class E>
 __device__ __forceinline__ void fill_bias(const AttnArgs& A, int head, float* table, int tid, int threads) {
-    for (int i = tid; i <= 2 * A.reach; i += threads) {
-        const float x = (float)((const E*)A.bias)[(int64_t)bucket_of<E>(A, i - A.reach) * A.heads + head];
-        const float y = x * LOG2E;
+    for (int i = tid; i < bias_width(A.reach); i += threads) {
+        const int dist = i - bias_middle(A.reach);
+        const int far = A.causal ? (dist < 0 ? -dist : 0) : (dist < 0 ? -dist : dist);
+        int b = -1;
+        for (int j = 0; j < A.n_dir; ++j) b += A.starts[j] <= far ? 1 : 0;   // the starts are scalar loads
+        if (!A.causal && dist > 0) b += A.n_dir;
+        const float x = (float)((const E*)A.bias)[(int64_t)b * A.heads + head], y = x * LOG2E;
         table[i] = fabsf(x) < INFINITY ? fminf(fmaxf(y, -3.4028235e38f), 3.4028235e38f) : y;
     }
 }
-__device__ __forceinline__ float bias_at(const float* table, int reach, int dist) {
-    const int i = dist < -reach ? -reach : dist > reach ? reach : dist;
-    return table[i + reach];
-}
+// Which way a block of 32 rows and columns lies whose first key and row are d0 apart: -1 or 1: all beyond reach, 0: not.
+__device__ __forceinline__ int block_side(int d0, int reach) { return d0 + 31 <= -reach ? -1 : d0 - 31 >= reach ? 1 : 0; }
 
-// A tile of two matrices' rows on its way from memory to LDS: loads are issued a tile ahead and wait in registers.
-template <class E, int D, int THREADS> struct Staged {
-    using T = Tile<E, D>;
-    static constexpr int N = T::ROWS * T::PIECES / THREADS;
-    u32x4 x[N], y[N];
-    uint8_t keep[N];
-    static __device__ __forceinline__ int row(int i, int tid) { return (i * THREADS + tid) / T::PIECES; }
-    static __device__ __forceinline__ int piece(int i, int tid) { return (i * THREADS + tid) % T::PIECES; }
-    __device__ __forceinline__ void put(char* a, char* b, int tid) const {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int at = T::at(row(i, tid), piece(i, tid));
-            const u32x4 zero = {0u, 0u, 0u, 0u};
-            *(u32x4*)(a + at) = keep[i] ? x[i] : zero;       // what the mask hides may be anything
-            *(u32x4*)(b + at) = keep[i] ? y[i] : zero;
-        }
-    }
-    // rows first .. of the keys and values of a head, zeros from `end` on and where the mask hides them
-    __device__ __forceinline__ void keys(const AttnArgs& A, int kv_head, int k0, int first, int end, int tid) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int r = first + row(i, tid);
-            x[i] = y[i] = u32x4{0u, 0u, 0u, 0u};
-            keep[i] = 1;
-            if (r < end) {
-                const int64_t at = k0 + r;
-                const int p = piece(i, tid) * 16;
-                x[i] = *(const u32x4*)((const char*)A.k + (at * A.k_row + kv_head * A.k_head) * (int64_t)sizeof(E) + p);
-                y[i] = *(const u32x4*)((const char*)A.v + (at * A.v_row + kv_head * A.v_head) * (int64_t)sizeof(E) + p);
-                if (A.keep) keep[i] = A.keep[at];
-            }
-        }
-    }
-};
+// Scores are scaled by |scale| in powers of two, as the exponential takes them; the columns' rows take its sign (exact), and are
+// zeros where it is zero, so that the maximum of the raw products is that of the scores.
+__device__ __forceinline__ float scale_of_scores(float scale) { return scale == 0.f ? 1.f : fabsf(scale) * LOG2E; }
 
 // The eight-value pieces of one column's row (B operand of all steps); zeros for a column that is none.
 template <class E, int D> struct Column {
@@ -99,118 +49,241 @@ template <class E, int D> struct Column {
             if (real) v[c] = Oper<E>::load(row + 16 * c + 8 * h);
         }
     }
+    __device__ __forceinline__ void take_sign(float scale) {
+        if (scale > 0.f) return;
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) v[c] = scale < 0.f ? -v[c] : typename Oper<E>::Frag{};
+    }
 };
 
-// Which of a tile's key rows are seen at all, one bit each.
-__device__ __forceinline__ uint64_t seen_keys(const AttnArgs& A, int k0, int first, int end, int rows, int lane) {
-    bool ok = lane < rows && first + lane < end;
-    if (A.keep && ok) ok = A.keep[(int64_t)k0 + first + lane] != 0;
-    return __ballot(ok);
-}
-
-// ---- forward -------------------------------------------------------------------------------------------------
-// One pass over the keys with the running maximum and sum of the softmax, in 32 bits; probabilities are rounded to the
-// storage type for the second product (their sum is not).
-template <class E, int D, int NW, bool BIAS>
-__global__ __launch_bounds__(64 * NW) void k_attention(const AttnArgs A, int slots, int units, int splits, E* out, float* lse,
-                                                       float* o_part, float2* ml_part) {
-    using O = Oper<E>;
+// Two matrices' rows on their way to a tile in LDS, a tile ahead of its use, by the memory unit itself; rows past the end as the
+// last row again (they meet probabilities of zero).  What a mask hides may be anything: a lane overwrites its own pieces of
+// such rows with zeros when they have arrived.
+template <class E, int D, int THREADS, bool MASKED> struct Staged {
     using T = Tile<E, D>;
-    constexpr int NB = T::ROWS / 32, DB = D / 32, THREADS = 64 * NW;
-    __shared__ __align__(16) char lk[T::BYTES], lv[T::BYTES];
-    extern __shared__ float table[];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5;
-    const int slot = blockIdx.x % slots, unit = blockIdx.x / slots % units, split = blockIdx.x / slots / units;
-    const int G = A.pack, per = 32 * NW / G;
-    const QueryTile t = query_tile(A, slot, per, lane);
-    if (t.none) return;
-    const int head0 = unit * G, kv = head0 / A.group;
-    if constexpr (BIAS) fill_bias<E>(A, head0, table, tid, THREADS);
-
-    const int col = wave * 32 + (lane & 31);
-    const int local = col / G, row = t.row0 + local, head = head0 + col % G;
-    const bool real = local < per && row < t.Lq;
-    const int shift = t.Lk - t.Lq, lim = row + shift;
-    const int last = (t.row0 + per < t.Lq ? t.row0 + per : t.Lq) - 1;
-    int end = A.causal ? last + shift + 1 : t.Lk;                 // keys that any column sees
-    end = end < 0 ? 0 : end > t.Lk ? t.Lk : end;
-    const int tiles = (end + T::ROWS - 1) / T::ROWS, each = (tiles + splits - 1) / splits;
-    const int first_tile = split * each, end_tile = first_tile + each < tiles ? first_tile + each : tiles;
-    // this wavefront's columns: their first and last row
-    const int wrow = t.row0 + wave * 32 / G;
-    const bool busy = wave * 32 / G < per && wrow < t.Lq;
-    const int wlast = t.row0 + (wave * 32 + 31) / G;
-    const int wend = A.causal ? (wlast < last ? wlast : last) + shift + 1 : t.Lk, wlim = wrow + shift;
-
-    Column<E, D> q;
-    q.load((const E*)A.q + (int64_t)(t.q0 + row) * A.q_row + head * A.q_head, real, h);
-    f32x16 acc[DB] = {};
-    float m = -INFINITY, l = 0.f;
-    const float scale2 = A.scale * LOG2E;
-    Staged<E, D, THREADS> next;
-    if (first_tile < end_tile) next.keys(A, kv, t.k0, first_tile * T::ROWS, end, tid);
-    for (int i = first_tile; i < end_tile; ++i) {
-        const int base = i * T::ROWS;
-        const uint64_t seen = seen_keys(A, t.k0, base, end, T::ROWS, lane);
-        __syncthreads();
-        next.put(lk, lv, tid);
-        __syncthreads();
-        if (i + 1 < end_tile) next.keys(A, kv, t.k0, base + T::ROWS, end, tid);
-        if (!busy || base >= wend) continue;
-        f32x16 s[NB];
+    static constexpr int N = T::ROWS * T::PIECES / THREADS;
+    uint8_t keep[MASKED ? N : 1];
+    // a_at(row), b_at(row): byte offsets of the matrices' rows; kept(row): whether the mask leaves it.  rows: how many are left.
+    template <class AtA, class AtB, class Kept>
+    __device__ __forceinline__ void issue(const char* a, const char* b, char* lds, int rows, int tid, AtA&& a_at, AtB&& b_at, Kept&& kept) {
+        const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            s[b] = {};
-#pragma unroll
-            for (int c = 0; c < D / 16; ++c) O::mma(s[b], T::rows(lk, lane, b, c), q.v[c]);
+        for (int i = 0; i < N; ++i) {
+            const int pos = i * THREADS + tid, place = pos / T::PIECES;
+            const uint32_t piece = (uint32_t)((pos % T::PIECES ^ T::turn(place)) * 16);
+            const int row = place < rows ? place : rows - 1;
+            char* to = lds + (i * THREADS + wave * 64) * 16;
+            copy_to_lds(a + (a_at(row) + piece), to);
+            copy_to_lds(b + (b_at(row) + piece), to + T::BYTES);
+            if constexpr (MASKED) keep[i] = kept(row);
         }
-        const uint64_t all = T::ROWS == 64 ? ~0ull : (1ull << (T::ROWS & 63)) - 1ull;
-        const bool part = seen != all || (A.causal && base + T::ROWS - 1 > wlim);
-        const int room = A.causal ? lim - base - 4 * h : 1 << 20;
-        const uint64_t mine = seen >> (4 * h);
-        float top = -INFINITY;
+    }
+    __device__ __forceinline__ void finish(char* lds, int tid) const {
+        wait_for_copies();
+        if constexpr (MASKED) {
+            const u32x4 zero = {0u, 0u, 0u, 0u};
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int k = 32 * b + 8 * (r >> 2) + (r & 3);
-                float x = s[b][r] * scale2;
-                if constexpr (BIAS) x += bias_at(table, A.reach, base + k + 4 * h - lim);
-                if (part && !(k <= room && ((uint32_t)(mine >> (32 * b)) >> (k & 31) & 1u))) x = -INFINITY;
-                s[b][r] = x;
-                top = fmaxf(top, x);
-            }
-        top = fmaxf(top, other_half(top));
-        const float m_new = fmaxf(m, top), m_use = m_new == -INFINITY ? 0.f : m_new;
-        if (__ballot(m_new > m)) {
-            const float down = exp2_fast(m - m_use);
-            l *= down;
-#pragma unroll
-            for (int db = 0; db < DB; ++db) acc[db] *= down;
-            m = m_new;
-        }
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                s[b][r] = exp2_fast(s[b][r] - m_use);
-                l += s[b][r];
-            }
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                const auto x = c ? __builtin_shufflevector(s[b], s[b], 8, 9, 10, 11, 12, 13, 14, 15)
-                                 : __builtin_shufflevector(s[b], s[b], 0, 1, 2, 3, 4, 5, 6, 7);
-                const typename O::Frag p = O::round(x);
-#pragma unroll
-                for (int db = 0; db < DB; ++db) O::mma(acc[db], T::turned(lv, lane, b, c, db), p);
+            for (int i = 0; i < N; ++i) {
+                char* to = lds + (i * THREADS + tid) * 16;
+                if (!keep[i]) {
+                    *(u32x4*)to = zero;
+                    *(u32x4*)(to + T::BYTES) = zero;
+                }
             }
         }
     }
-    l += other_half(l);
-    if (!real) return;
-    const int64_t at = (int64_t)(t.q0 + row);
+};
+
+// A workgroup's tile of query columns, and which keys its rows see.
+struct QueryTile {
+    int row0, Lq, Lk, q0, k0, shift, end;     // first row, lengths, first global rows, Lk - Lq, keys that any row sees
+    bool none;
+    __device__ __forceinline__ QueryTile(const AttnArgs& A, int slot, int per, int lane) {
+        const int seq = find_sequence(A.qoff, A.n_seqs, per, A.total_q, slot, lane);
+        const Range q = sequence_rows(A.qoff, seq, A.total_q, per), k = sequence_rows(A.koff, seq, A.total_k);
+        row0 = (slot - q.place) * per;
+        Lq = q.n;
+        Lk = k.n;
+        q0 = q.lo;
+        k0 = k.lo;
+        shift = Lk - Lq;
+        none = row0 < 0 || row0 >= Lq;
+        const int last = (row0 + per < Lq ? row0 + per : Lq) - 1;
+        end = A.causal ? last + shift + 1 : Lk;
+        end = end < 0 ? 0 : end > Lk ? Lk : end;
+    }
+};
+
+// A wavefront's 32 columns of it.
+struct QueryColumns {
+    int row, head, lim, first_lim, end;       // own row, head and key limit; that of the first column; keys that any sees
+    bool real, busy;
+    __device__ __forceinline__ QueryColumns(const AttnArgs& A, const QueryTile& t, int G, int per, int head0, int wave, int lane) {
+        const int local = (wave * 32 + (lane & 31)) / G;
+        row = t.row0 + local;
+        head = head0 + (wave * 32 + (lane & 31)) % G;
+        real = local < per && row < t.Lq;
+        lim = row + t.shift;
+        const int first = t.row0 + wave * 32 / G, last = t.row0 + (wave * 32 + 31) / G;
+        first_lim = first + t.shift;
+        busy = wave * 32 / G < per && first < t.Lq;
+        const int e = last + t.shift + 1;
+        end = A.causal && e < t.end ? e : t.end;
+    }
+};
+
+template <int LO> __device__ __forceinline__ f32x8 eight(const f32x16& x) {
+    return __builtin_shufflevector(x, x, LO, LO + 1, LO + 2, LO + 3, LO + 4, LO + 5, LO + 6, LO + 7);
+}
+
+// Which of a tile's rows a lane's column sees: by a limit on the row, and with a mask one bit each.
+template <bool MASKED> struct Seen {
+    int room;
+    uint32_t low, high;
+    __device__ __forceinline__ Seen(int room, uint64_t mask, int h) : room(room - 4 * h) {
+        if constexpr (MASKED) {
+            const uint64_t upto = room < 0 ? 0ull : room >= 63 ? ~0ull : (2ull << room) - 1ull;
+            const uint64_t m = (mask & upto) >> (4 * h);
+            low = (uint32_t)m;
+            high = (uint32_t)(m >> 32);
+        }
+    }
+    // row 32b + k (and 4h)
+    __device__ __forceinline__ float otherwise(float x, float y, int b, int k) const {
+        if constexpr (MASKED) {
+            const int m = (int)((b ? high : low) << (31 - k)) >> 31;
+            return __int_as_float((__float_as_int(x) & m) | (__float_as_int(y) & ~m));
+        } else {
+            return 32 * b + k <= room ? x : y;
+        }
+    }
+};
+
+// ---- forward -------------------------------------------------------------------------------------------------
+// One pass over the keys with the running maximum and sum of the softmax, in 32 bits; probabilities are rounded to the
+// storage type for the second product (their sum is not).  The maximum that is subtracted may lag by up to kLag: sums and
+// outputs are rescaled only when it is passed, which few tiles after the first do; probabilities up to 2^kLag are no less exact.
+constexpr float kLag = 8.f;
+template <class E, int D, int NW, bool BIAS, bool MASKED>
+__global__ __launch_bounds__(64 * NW, 2) void k_attention(const AttnArgs A, int slots, int units, int splits, E* out, float* lse,
+                                                          float* o_part, float2* ml_part) {
+    using O = Oper<E>;
+    using T = Tile<E, D>;
+    constexpr int NB = T::ROWS / 32, DB = D / 32, THREADS = 64 * NW;
+    __shared__ __align__(16) char lds[2][2 * T::BYTES];
+    extern __shared__ float table[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
+    const int slot = blockIdx.x % slots, unit = blockIdx.x / slots % units, split = blockIdx.x / slots / units;
+    const int G = A.pack, per = 32 * NW / G;
+    const QueryTile t(A, slot, per, lane);
+    if (t.none) return;
+    const int head0 = unit * G, kv = head0 / A.group;
+    const QueryColumns w(A, t, G, per, head0, wave, lane);
+    const int tiles = (t.end + T::ROWS - 1) / T::ROWS, each = (tiles + splits - 1) / splits;
+    const int first_tile = split * each, end_tile = first_tile + each < tiles ? first_tile + each : tiles;
+
+    const int64_t krow = A.k_row * (int64_t)sizeof(E), vrow = A.v_row * (int64_t)sizeof(E);
+    const char* kp = (const char*)A.k + t.k0 * krow + kv * A.k_head * (int64_t)sizeof(E);
+    const char* vp = (const char*)A.v + t.k0 * vrow + kv * A.v_head * (int64_t)sizeof(E);
+    Staged<E, D, THREADS, MASKED> next;
+    uint8_t next_keep = 0;
+    auto issue = [&](int base, char* to) {
+        next.issue(kp + base * krow, vp + base * vrow, to, t.end - base, tid, [&](int r) { return (uint32_t)r * (uint32_t)krow; },
+                   [&](int r) { return (uint32_t)r * (uint32_t)vrow; }, [&](int r) { return A.keep[(int64_t)t.k0 + base + r]; });
+        if constexpr (MASKED) next_keep = lane < T::ROWS && base + lane < t.end ? A.keep[(int64_t)t.k0 + base + lane] : 0;
+    };
+    if (first_tile < end_tile) issue(first_tile * T::ROWS, lds[0]);
+    if constexpr (BIAS) fill_bias<E>(A, head0, table, tid, THREADS);
+    Column<E, D> q;
+    q.load((const E*)A.q + (int64_t)(t.q0 + w.row) * A.q_row + w.head * A.q_head, w.real, h);
+    q.take_sign(A.scale);
+    f32x16 acc[DB] = {};
+    float m = -INFINITY, l = 0.f;
+    const float scale2 = scale_of_scores(A.scale);
+    const int middle = bias_middle(A.reach);
+    if (first_tile < end_tile) next.finish(lds[0], tid);
+    uint64_t seen = __ballot(next_keep != 0);
+    __syncthreads();
+    for (int i = first_tile; i < end_tile; ++i) {
+        const int base = i * T::ROWS;
+        const char *lk = lds[(i - first_tile) & 1], *lv = lk + T::BYTES;
+        char* other = lds[(i - first_tile + 1) & 1];
+        if (i + 1 < end_tile) issue(base + T::ROWS, other);
+        auto compute = [&](auto part) {
+            f32x16 s[NB];
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                s[b] = {};
+#pragma unroll
+                for (int c = 0; c < D / 16; ++c) O::mma(s[b], T::rows(lk, lane, b, c), q.v[c]);
+            }
+            if constexpr (BIAS) {
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    const int d0 = base + 32 * b - w.first_lim, side = block_side(d0, A.reach);
+                    if (side) {
+                        const float x = table[side < 0 ? 0 : 2 * middle];
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) s[b][r] = fmaf(s[b][r], scale2, x);
+                    } else {
+                        const float* x = table + middle + base + 32 * b + 4 * h - w.lim;
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) s[b][r] = fmaf(s[b][r], scale2, x[8 * (r >> 2) + (r & 3)]);
+                    }
+                }
+            }
+            if constexpr (decltype(part)::value) {
+                const int last = t.end - 1 - base, own = w.lim - base;
+                const Seen<MASKED> see(A.causal && own < last ? own : last, seen, h);
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[b][r] = see.otherwise(s[b][r], -INFINITY, b, 8 * (r >> 2) + (r & 3));
+            }
+            float top = s[0][0];
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) top = __builtin_elementwise_maximum(top, s[b][r]);
+            top = max_of_halves(top);
+            if constexpr (!BIAS) top *= scale2;
+            const bool passed = top > m + kLag;
+            if (__ballot(passed)) {
+                const float to = passed ? top : m;
+                const float down = exp2_fast(m - (to == -INFINITY ? 0.f : to));
+                l *= down;
+#pragma unroll
+                for (int db = 0; db < DB; ++db) acc[db] *= down;
+                m = to;
+            }
+            const float off = m == -INFINITY ? 0.f : -m;
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    s[b][r] = exp2_fast(BIAS ? s[b][r] + off : fmaf(s[b][r], scale2, off));
+                    l += s[b][r];
+                }
+                const typename O::Frag p0 = O::round(eight<0>(s[b])), p1 = O::round(eight<8>(s[b]));
+#pragma unroll
+                for (int db = 0; db < DB; ++db) O::mma(acc[db], T::turned(lv, lane, b, 0, db), p0);
+#pragma unroll
+                for (int db = 0; db < DB; ++db) O::mma(acc[db], T::turned(lv, lane, b, 1, db), p1);
+            }
+        };
+        if (w.busy && base < w.end) {
+            const bool whole = base + T::ROWS <= t.end && !(A.causal && base + T::ROWS - 1 > w.first_lim) && (!MASKED || seen == ~0ull);
+            if (whole) compute(std::false_type{}); else compute(std::true_type{});
+        }
+        if (i + 1 < end_tile) next.finish(other, tid);
+        seen = __ballot(next_keep != 0);
+        __syncthreads();
+    }
+    l = sum_of_halves(l);
+    if (!w.real) return;
+    const int64_t at = (int64_t)(t.q0 + w.row);
     if (splits > 1) {
-        const int64_t place = ((int64_t)split * A.heads + head) * A.total_q + at;
+        const int64_t place = ((int64_t)split * A.heads + w.head) * A.total_q + at;
         if (h == 0) ml_part[place] = make_float2(m, l);
 #pragma unroll
         for (int db = 0; db < DB; ++db)
@@ -221,8 +294,8 @@ __global__ __launch_bounds__(64 * NW) void k_attention(const AttnArgs A, int slo
         return;
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    if (h == 0) lse[(int64_t)head * A.total_q + at] = l == 0.f ? -INFINITY : m * LN2 + logf(l);
-    E* o = out + (at * A.heads + head) * D;
+    if (h == 0) lse[(int64_t)w.head * A.total_q + at] = l == 0.f ? -INFINITY : m * LN2 + logf(l);
+    E* o = out + (at * A.heads + w.head) * D;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -231,7 +304,7 @@ __global__ __launch_bounds__(64 * NW) void k_attention(const AttnArgs A, int slo
                                                           acc[db][4 * j + 2] * inv, acc[db][4 * j + 3] * inv});
 }
 
-// Joins the parts of rows whose keys were split: a quarter of a row's values a thread and row.
+// Joins the parts of rows whose keys were split: four of a row's values a thread.
 template <class E, int D>
 __global__ __launch_bounds__(256) void k_attention_join(const AttnArgs A, int splits, const float* o_part, const float2* ml_part,
                                                         E* out, float* lse) {
@@ -242,8 +315,7 @@ __global__ __launch_bounds__(256) void k_attention_join(const AttnArgs A, int sp
     if (place >= rows) return;
     // rows that no sequence holds have no parts: they are not written by any call, nor is their output
     const int64_t row = place % A.total_q;
-    int64_t lo = A.qoff[0], hi = A.qoff[A.n_seqs];
-    if (row < lo || row >= hi) return;
+    if (row < A.qoff[0] || row >= A.qoff[A.n_seqs]) return;
     float m = -INFINITY;
     for (int s = 0; s < splits; ++s) m = fmaxf(m, ml_part[s * rows + place].x);
     const float m_use = m == -INFINITY ? 0.f : m;
@@ -266,58 +338,88 @@ __global__ __launch_bounds__(256) void k_attention_join(const AttnArgs A, int sp
 // to the storage type as operands of the last products.  Queries' and keys' gradients are made by a kernel each, which
 // recomputes the scores twice (seven products where one kernel would need five) but adds in a fixed order, where one
 // kernel would have to add either side's gradients by atomics.
+// The rounding of O reaches dS through delta, the same for all of a row.  Rows of dS sum to zero, so what a row's sum is
+// instead is the error of its delta: the first kernel adds it to the delta that the second one takes.  In the
+// first, 16-bit dS goes into its product as two values of eight bits each, which leaves O's rounding as the only error beside
+// the result's own (gradients of queries, against 64 bits, 512 passages: 2.6e-3 with one value, DQ_ERROR with two; the result's own
+// rounding is 1.7e-3).
+
+// Sums of a 32 x 32 block along its diagonals, added to a histogram by distance.  The block is in accumulators: a lane has
+// sixteen keys of a column.  Sixteen columns at a time go to LDS, 68 words apart (their writes in different banks) with zeros
+// between them; lane i then adds up the diagonal k - n = i - 15, one word of each column, and the histogram has one place for
+// it.  No atomics, which take 2.5 clocks a lane there, and a fixed order.
+constexpr int kPitch = 68, kDiagonal = 16 * kPitch + 16;
+__device__ __forceinline__ void add_diagonals(const f32x16& x, float* scratch, float* hist, int lane) {
+    const int n = lane & 31, h = lane >> 5;
+    const int i = lane < 47 ? lane : 46;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if ((n >> 4) == half) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                *(f32x4*)(scratch + (n & 15) * kPitch + 32 + 8 * j + 4 * h) = f32x4{x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]};
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        float sum = 0.f;
+#pragma unroll
+        for (int c = 0; c < 16; ++c) sum += scratch[c * kPitch + 32 + c - 15 + i];
+        if (lane < 47) hist[i - 15 - 16 * half] += sum;
+    }
+}
 
 // Gradients of queries, delta, and the bias table's share of each tile.
-// The table's gradient: dS of a 32 x 32 block is added to a histogram by distance in LDS, one of each half wavefront: the 32
-// lanes of a half have as many distances, so no two lanes add to one place at once and the order of the sums is the
-// program's.  Blocks whose distances all lie in a direction's last bucket are summed in a register instead.
-template <class E, int D, int NW, bool BIAS>
-__global__ __launch_bounds__(64 * NW) void k_attention_dq(const AttnArgs A, int slots, int units, const E* out, const E* dout,
-                                                          const float* lse, E* dq, float* delta, float* bias_part) {
+template <class E, int D, int NW, bool BIAS, bool MASKED>
+__global__ __launch_bounds__(64 * NW, D <= 64 ? 2 : 1) void k_attention_dq(const AttnArgs A, int slots, int units, const E* out, const E* dout,
+                                                             const float* lse, E* dq, float* delta, float* bias_part) {
     using O = Oper<E>;
     using T = Tile<E, D>;
     constexpr int NB = T::ROWS / 32, DB = D / 32, THREADS = 64 * NW;
-    __shared__ __align__(16) char lk[T::BYTES], lv[T::BYTES];
+    __shared__ __align__(16) char lds[2][2 * T::BYTES];
+    __shared__ __align__(16) float diagonals[BIAS ? NW * kDiagonal : 1];
     __shared__ float far_sum[NW][2];
-    extern __shared__ float table[];                  // [2 reach + 1], then the histograms
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5;
+    extern __shared__ float table[];                  // the bias by distance, then a histogram of each wavefront
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     const int slot = blockIdx.x % slots, unit = blockIdx.x / slots;
     const int G = A.pack, per = 32 * NW / G;
-    const QueryTile t = query_tile(A, slot, per, lane);
+    const QueryTile t(A, slot, per, lane);
     const int head0 = unit * G, kv = head0 / A.group;
     if (t.none) {
         if constexpr (BIAS)
             for (int b = tid; b < A.n_buckets; b += THREADS) bias_part[((int64_t)slot * A.heads + head0) * A.n_buckets + b] = 0.f;
         return;
     }
-    const int width = 2 * A.reach + 125, mid = A.reach + 62;      // distances of blocks that are not far: below reach + 63
-    float* hist = table + 2 * A.reach + 1;
+    const QueryColumns w(A, t, G, per, head0, wave, lane);
+    const int tiles = (t.end + T::ROWS - 1) / T::ROWS;
+    const int64_t krow = A.k_row * (int64_t)sizeof(E), vrow = A.v_row * (int64_t)sizeof(E);
+    const char* kp = (const char*)A.k + t.k0 * krow + kv * A.k_head * (int64_t)sizeof(E);
+    const char* vp = (const char*)A.v + t.k0 * vrow + kv * A.v_head * (int64_t)sizeof(E);
+    Staged<E, D, THREADS, MASKED> next;
+    uint8_t next_keep = 0;
+    auto issue = [&](int base, char* to) {
+        next.issue(kp + base * krow, vp + base * vrow, to, t.end - base, tid, [&](int r) { return (uint32_t)r * (uint32_t)krow; },
+                   [&](int r) { return (uint32_t)r * (uint32_t)vrow; }, [&](int r) { return A.keep[(int64_t)t.k0 + base + r]; });
+        if constexpr (MASKED) next_keep = lane < T::ROWS && base + lane < t.end ? A.keep[(int64_t)t.k0 + base + lane] : 0;
+    };
+    if (tiles > 0) issue(0, lds[0]);
+    const int middle = bias_middle(A.reach), width = bias_width(A.reach);
+    float* hist = table + width;
+    float* own_hist = hist + wave * width + middle;
+    float* scratch = diagonals + wave * kDiagonal;
     if constexpr (BIAS) {
         fill_bias<E>(A, head0, table, tid, THREADS);
-        for (int i = tid; i < 2 * NW * width; i += THREADS) hist[i] = 0.f;
+        for (int i = tid; i < NW * width; i += THREADS) hist[i] = 0.f;
+        for (int i = tid; i < NW * kDiagonal; i += THREADS) diagonals[i] = 0.f;
     }
-    float* mine_hist = hist + (2 * wave + h) * width + mid;
     float far_lo = 0.f, far_hi = 0.f;
 
-    const int col = wave * 32 + (lane & 31);
-    const int local = col / G, row = t.row0 + local, head = head0 + col % G;
-    const bool real = local < per && row < t.Lq;
-    const int shift = t.Lk - t.Lq, lim = row + shift;
-    const int last = (t.row0 + per < t.Lq ? t.row0 + per : t.Lq) - 1;
-    int end = A.causal ? last + shift + 1 : t.Lk;
-    end = end < 0 ? 0 : end > t.Lk ? t.Lk : end;
-    const int tiles = (end + T::ROWS - 1) / T::ROWS;
-    const int wrow = t.row0 + wave * 32 / G;
-    const bool busy = wave * 32 / G < per && wrow < t.Lq;
-    const int wlast = t.row0 + (wave * 32 + 31) / G;
-    const int wend = A.causal ? (wlast < last ? wlast : last) + shift + 1 : t.Lk, wlim = wrow + shift;
-
-    const int64_t at = (int64_t)(t.q0 + row), place = (int64_t)head * A.total_q + at, dense = (at * A.heads + head) * D;
-    const float row_lse = real ? lse[place] : -INFINITY;
+    const int64_t at = (int64_t)(t.q0 + w.row), place = (int64_t)w.head * A.total_q + at, dense = (at * A.heads + w.head) * D;
+    const float row_lse = w.real ? lse[place] : -INFINITY;
     const bool seeing = row_lse != -INFINITY;         // rows that see nothing take no part, whatever their gradient is
     const float lse2 = row_lse * LOG2E;
     Column<E, D> q, g;
-    q.load((const E*)A.q + at * A.q_row + head * A.q_head, seeing, h);
+    q.load((const E*)A.q + at * A.q_row + w.head * A.q_head, seeing, h);
+    q.take_sign(A.scale);
     g.load(dout + dense, seeing, h);
     float dot = 0.f;
     {
@@ -329,66 +431,91 @@ __global__ __launch_bounds__(64 * NW) void k_attention_dq(const AttnArgs A, int 
 #pragma unroll
             for (int e = 0; e < 8; ++e) dot += x[e] * y[e];
         }
-        dot += other_half(dot);
-        if (real && h == 0) delta[place] = dot;
+        dot = sum_of_halves(dot);
     }
     f32x16 acc[DB] = {};
-    const float scale2 = A.scale * LOG2E;
-    Staged<E, D, THREADS> next;
-    if (tiles > 0) next.keys(A, kv, t.k0, 0, end, tid);
+    float row_sum = 0.f;
+    const float scale2 = scale_of_scores(A.scale);
+    const bool all_seeing = __all(seeing);
+    if (tiles > 0) next.finish(lds[0], tid);
+    uint64_t seen = __ballot(next_keep != 0);
+    __syncthreads();
     for (int i = 0; i < tiles; ++i) {
         const int base = i * T::ROWS;
-        const uint64_t seen = seen_keys(A, t.k0, base, end, T::ROWS, lane);
-        __syncthreads();
-        next.put(lk, lv, tid);
-        __syncthreads();
-        if (i + 1 < tiles) next.keys(A, kv, t.k0, base + T::ROWS, end, tid);
-        if (!busy || base >= wend) continue;
-        const uint64_t all = T::ROWS == 64 ? ~0ull : (1ull << (T::ROWS & 63)) - 1ull;
-        const bool part = seen != all || !__all(seeing) || (A.causal && base + T::ROWS - 1 > wlim);
-        const int room = !seeing ? -1 : A.causal ? lim - base - 4 * h : 1 << 20;
-        const uint64_t mine = seen >> (4 * h);
+        const char *lk = lds[i & 1], *lv = lk + T::BYTES;
+        char* other = lds[(i + 1) & 1];
+        if (i + 1 < tiles) issue(base + T::ROWS, other);
+        auto compute = [&](auto part) {
+            const int last = t.end - 1 - base, own = w.lim - base;
+            const Seen<MASKED> see(!seeing ? -1 : A.causal && own < last ? own : last, seen, h);
+#pragma unroll 1
+            for (int b = 0; b < NB; ++b) {
+                f32x16 s = {}, dp = {};
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            f32x16 s = {}, dp = {};
+                for (int c = 0; c < D / 16; ++c) O::mma(s, T::rows(lk, lane, b, c), q.v[c]);
 #pragma unroll
-            for (int c = 0; c < D / 16; ++c) O::mma(s, T::rows(lk, lane, b, c), q.v[c]);
+                for (int c = 0; c < D / 16; ++c) O::mma(dp, T::rows(lv, lane, b, c), g.v[c]);
+                const int d0 = base + 32 * b - w.first_lim, side = BIAS ? block_side(d0, A.reach) : 0;
+                if (BIAS && !side) {
+                    const float* x = table + middle + base + 32 * b + 4 * h - w.lim;
 #pragma unroll
-            for (int c = 0; c < D / 16; ++c) O::mma(dp, T::rows(lv, lane, b, c), g.v[c]);
-            f32x16 ds;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int k = 32 * b + 8 * (r >> 2) + (r & 3);
-                float x = s[r] * scale2;
-                if constexpr (BIAS) x += bias_at(table, A.reach, base + k + 4 * h - lim);
-                float y = exp2_fast(x - lse2) * (dp[r] - dot);
-                if (part && !(k <= room && ((uint32_t)(mine >> (32 * b)) >> (k & 31) & 1u))) y = 0.f;
-                ds[r] = y;
-            }
-            if constexpr (BIAS) {
-                const int d0 = base + 32 * b - wlim;              // distance of the block's first key and row
-                if (d0 - 31 >= A.reach || d0 + 31 <= -A.reach) {
-                    float sum = 0.f;
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) sum += ds[r];
-                    (d0 > 0 ? far_hi : far_lo) += sum;
+                    for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], scale2, x[8 * (r >> 2) + (r & 3)]) - lse2;
                 } else {
-                    const int d = base + 32 * b + 4 * h - lim;
+                    const float x = BIAS ? table[side < 0 ? 0 : 2 * middle] - lse2 : -lse2;
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) atomicAdd(mine_hist + d + 8 * (r >> 2) + (r & 3), ds[r]);
+                    for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], scale2, x);
+                }
+                float sum = 0.f;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    float y = exp2_fast(s[r]) * (dp[r] - dot);
+                    if constexpr (decltype(part)::value) y = see.otherwise(y, 0.f, b, 8 * (r >> 2) + (r & 3));
+                    s[r] = y;
+                    sum += y;
+                }
+                row_sum += sum;
+                if constexpr (BIAS) {
+                    if (side) {
+                        (side < 0 ? far_lo : far_hi) += sum;
+                    } else {
+                        add_diagonals(s, scratch, own_hist + d0, lane);
+                    }
+                }
+                if constexpr (sizeof(E) == 2) {
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        const f32x8 x = c ? eight<8>(s) : eight<0>(s);
+                        f32x8 most;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) most[e] = __uint_as_float(__float_as_uint(x[e]) & 0xffff0000u);
+                        const typename O::Frag p = O::round(most), rest = O::round(x - most);
+#pragma unroll
+                        for (int db = 0; db < DB; ++db) {
+                            const typename O::Frag k = T::turned(lk, lane, b, c, db);
+                            O::mma(acc[db], k, rest);
+                            O::mma(acc[db], k, p);
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int db = 0; db < DB; ++db) O::mma(acc[db], T::turned(lk, lane, b, 0, db), eight<0>(s));
+#pragma unroll
+                    for (int db = 0; db < DB; ++db) O::mma(acc[db], T::turned(lk, lane, b, 1, db), eight<8>(s));
                 }
             }
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                const auto x = c ? __builtin_shufflevector(ds, ds, 8, 9, 10, 11, 12, 13, 14, 15)
-                                 : __builtin_shufflevector(ds, ds, 0, 1, 2, 3, 4, 5, 6, 7);
-                const typename O::Frag p = O::round(x);
-#pragma unroll
-                for (int db = 0; db < DB; ++db) O::mma(acc[db], T::turned(lk, lane, b, c, db), p);
-            }
+        };
+        if (w.busy && base < w.end) {
+            const bool whole = base + T::ROWS <= t.end && all_seeing && !(A.causal && base + T::ROWS - 1 > w.first_lim) &&
+                               (!MASKED || seen == ~0ull);
+            if (whole) compute(std::false_type{}); else compute(std::true_type{});
         }
+        if (i + 1 < tiles) next.finish(other, tid);
+        seen = __ballot(next_keep != 0);
+        __syncthreads();
     }
-    if (real) {
+    row_sum = sum_of_halves(row_sum);
+    if (w.real) {
+        if (h == 0) delta[place] = dot + row_sum;
         E* o = dq + dense;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
@@ -409,37 +536,49 @@ __global__ __launch_bounds__(64 * NW) void k_attention_dq(const AttnArgs A, int 
             far_sum[wave][1] = far_hi;
         }
         __syncthreads();
-        for (int b = tid; b < A.n_buckets; b += THREADS) {
-            const bool behind = b >= A.n_dir;                     // keys behind the query
-            const int i = behind ? b - A.n_dir : b;
-            const bool open = i == A.n_dir - 1;                   // the last one of its direction
-            const int lo = A.starts[i], hi = open ? mid : A.starts[i + 1] - 1;
+        for (int i = tid; i < width; i += THREADS) {
+            float x = hist[i];
+#pragma unroll
+            for (int v = 1; v < NW; ++v) x += hist[v * width + i];
+            hist[i] = x;
+        }
+        __syncthreads();
+        const float* x = hist + middle;
+        for (int b0 = 0; b0 < A.n_buckets; b0 += THREADS / 8) {
+            const int b = b0 + tid / 8;
+            const bool one = b < A.n_buckets, behind = b >= A.n_dir;      // buckets of keys behind the query
+            const int j0 = behind ? b - A.n_dir : b;
+            const bool open = j0 == A.n_dir - 1;                          // the last one of its direction
             float sum = 0.f;
-            for (int w = 0; w < 2 * NW; ++w) {
-                const float* x = hist + w * width + mid;
-                // distance 0 belongs to the keys before; with a causal limit so do all keys behind, of which none is seen
-                for (int j = lo; j <= hi; ++j) sum += behind ? (j > 0 ? x[j] : 0.f) : x[-j];
+            if (one) {
+                // distance 0 belongs to the keys before
+                const int hi = open ? middle : A.starts[j0 + 1] - 1;
+                for (int j = A.starts[j0] + tid % 8; j <= hi; j += 8) sum += behind ? (j > 0 ? x[j] : 0.f) : x[-j];
             }
-            if (open)
-                for (int w = 0; w < NW; ++w) sum += far_sum[w][behind ? 1 : 0];
-            bias_part[((int64_t)slot * A.heads + head0) * A.n_buckets + b] = sum;
+#pragma unroll
+            for (int m = 1; m < 8; m <<= 1) sum += __shfl_xor(sum, m);
+            if (one && tid % 8 == 0) {
+                if (open)
+#pragma unroll
+                    for (int v = 0; v < NW; ++v) sum += far_sum[v][behind ? 1 : 0];
+                bias_part[((int64_t)slot * A.heads + head0) * A.n_buckets + b] = sum;
+            }
         }
     }
 }
 
 // Gradients of keys and values; workgroups from `main` on add up the bias table's shares of all tiles.
-template <class E, int D, int NW, bool BIAS>
-__global__ __launch_bounds__(64 * NW) void k_attention_dkv(const AttnArgs A, int slots, int main, int q_slots, const E* dout,
+template <class E, int D, int NW, bool BIAS, bool MASKED>
+__global__ __launch_bounds__(64 * NW, D <= 64 ? 2 : 1) void k_attention_dkv(const AttnArgs A, int slots, int main, int q_slots, const E* dout,
                                                            const float* lse, const float* delta, const float* bias_part, E* dk, E* dv,
                                                            E* dbias) {
     using O = Oper<E>;
     using T = Tile<E, D>;
     constexpr int NB = T::ROWS / 32, DB = D / 32, THREADS = 64 * NW, COLS = 32 * NW;
-    __shared__ __align__(16) char lq[T::BYTES], lg[T::BYTES];
-    __shared__ __align__(16) float row_lse[T::ROWS], row_delta[T::ROWS];
-    __shared__ __align__(16) int row_lim[T::ROWS];
+    __shared__ __align__(16) char lds[2][2 * T::BYTES];
+    __shared__ __align__(16) float row_lse[2][T::ROWS], row_delta[2][T::ROWS];
     extern __shared__ float table[];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     if constexpr (BIAS) {
         if ((int)blockIdx.x >= main) {                // one entry of the table each wavefront
             const int e = ((int)blockIdx.x - main) * NW + wave;
@@ -455,107 +594,129 @@ __global__ __launch_bounds__(64 * NW) void k_attention_dkv(const AttnArgs A, int
     }
     const int slot = blockIdx.x % slots, kv = blockIdx.x / slots;
     const int seq = find_sequence(A.koff, A.n_seqs, COLS, A.total_k, slot, lane);
-    const Range ks = sequence_rows(A.koff, seq, A.total_k), qs = sequence_rows(A.qoff, seq, A.total_q);
-    const int key0 = (slot - place_of(A.koff, seq, COLS, A.total_k)) * COLS;
+    const Range ks = sequence_rows(A.koff, seq, A.total_k, COLS), qs = sequence_rows(A.qoff, seq, A.total_q);
+    const int key0 = (slot - ks.place) * COLS;
     if (key0 < 0 || key0 >= ks.n) return;
-    const int key = key0 + wave * 32 + (lane & 31), shift = ks.n - qs.n;
+    const int wkey = key0 + wave * 32, key = wkey + (lane & 31), shift = ks.n - qs.n;
     const bool real = key < ks.n;
     const int64_t at = ks.lo + key;
-    const bool seen = real && (!A.keep || A.keep[at]);
+    const bool seen = real && (!MASKED || A.keep[at]);
+    const int G = A.pack, cols = qs.n * G;
+    // first row that sees a key of the tile (below zero: all do); a row before it sees nothing at all only at the sequence's start
+    const int first = A.causal && key0 > shift ? key0 - shift : 0;
+    const int col0 = first * G;
+
+    const int64_t qrow = A.q_row * (int64_t)sizeof(E), qhead = A.q_head * (int64_t)sizeof(E);
+    const int64_t grow = (int64_t)A.heads * D * (int64_t)sizeof(E), ghead = D * (int64_t)sizeof(E);
+    const char* qp = (const char*)A.q + qs.lo * qrow;
+    const char* gp = (const char*)dout + qs.lo * grow;
+    Staged<E, D, THREADS, MASKED> next;
+    float n_lse = 0.f, n_delta = 0.f;
+    auto issue = [&](int head0, int c0, char* to) {
+        const int row0 = c0 / G, c1 = c0 - row0 * G;              // the tile's first row, and its first column's place in it
+        const int64_t place0 = (int64_t)head0 * A.total_q + qs.lo + row0;
+        auto row_of = [&](int r) { return G == 1 ? r : (int)((uint32_t)(c1 + r) / (uint32_t)G); };
+        auto offset = [&](int r, uint32_t per_row, uint32_t per_head) {
+            const int row = row_of(r);
+            return G == 1 ? (uint32_t)row * per_row : (uint32_t)row * per_row + (uint32_t)(c1 + r - row * G) * per_head;
+        };
+        auto place = [&](int r) { return place0 + row_of(r) + (int64_t)(c1 + r - row_of(r) * G) * A.total_q; };
+        next.issue(qp + row0 * qrow + head0 * qhead, gp + row0 * grow + head0 * ghead, to, cols - c0, tid,
+                   [&](int r) { return offset(r, (uint32_t)qrow, (uint32_t)qhead); },
+                   [&](int r) { return offset(r, (uint32_t)grow, (uint32_t)ghead); },
+                   [&](int r) { return (uint8_t)(lse[place(r)] != -INFINITY); });
+        if (tid < T::ROWS) {
+            n_lse = -INFINITY;
+            n_delta = 0.f;
+            if (c0 + tid < cols) {
+                n_lse = lse[place(tid)];
+                n_delta = delta[place(tid)];
+            }
+        }
+    };
+    auto finish = [&](int buf) {
+        next.finish(lds[buf], tid);
+        if (tid < T::ROWS) {
+            row_lse[buf][tid] = n_lse == -INFINITY ? -INFINITY : -n_lse * LOG2E;      // exp2(x - inf) = 0
+            row_delta[buf][tid] = n_delta;
+        }
+    };
+    int head0 = kv * A.group, c0 = col0;
+    const int head_end = head0 + A.group;
+    if (col0 < cols) issue(head0, c0, lds[0]);
     Column<E, D> k, v;
     k.load((const E*)A.k + at * A.k_row + kv * A.k_head, seen, h);
+    k.take_sign(A.scale);
     v.load((const E*)A.v + at * A.v_row + kv * A.v_head, seen, h);
     f32x16 ak[DB] = {}, av[DB] = {};
-    const float scale2 = A.scale * LOG2E;
-    const int G = A.pack;
-    const int first = A.causal && key0 > shift ? key0 - shift : 0;       // first row that sees a key of the tile
-    const int wfirst = A.causal && key0 + wave * 32 > shift ? key0 + wave * 32 - shift : 0;
-    const bool busy = key0 + wave * 32 < ks.n;
-    const int cols = qs.n * G, col0 = (int)((int64_t)first * G / T::ROWS * T::ROWS);
-    for (int head0 = kv * A.group; head0 < (kv + 1) * A.group; head0 += G) {
-        if constexpr (BIAS) {
-            __syncthreads();
-            fill_bias<E>(A, head0, table, tid, THREADS);
-        }
-        Staged<E, D, THREADS> next;
-        float n_lse = 0.f, n_delta = 0.f;
-        auto fetch = [&](int c0) {
-#pragma unroll
-            for (int i = 0; i < next.N; ++i) {
-                const int c = c0 + next.row(i, tid);
-                next.x[i] = next.y[i] = u32x4{0u, 0u, 0u, 0u};
-                next.keep[i] = 1;
-                if (c < cols) {
-                    const int64_t r = qs.lo + c / G;
-                    const int head = head0 + c % G, p = next.piece(i, tid) * 16;
-                    next.x[i] = *(const u32x4*)((const char*)A.q + (r * A.q_row + head * A.q_head) * (int64_t)sizeof(E) + p);
-                    next.y[i] = *(const u32x4*)((const char*)dout + (r * A.heads + head) * (int64_t)(D * sizeof(E)) + p);
-                    next.keep[i] = lse[(int64_t)head * A.total_q + r] != -INFINITY;
-                }
-            }
-            if (tid < T::ROWS) {
-                const int c = c0 + tid;
-                n_lse = -INFINITY;
-                n_delta = 0.f;
-                if (c < cols) {
-                    const int64_t place = (int64_t)(head0 + c % G) * A.total_q + qs.lo + c / G;
-                    n_lse = lse[place];
-                    n_delta = delta[place];
-                }
-            }
-        };
-        if (col0 < cols) fetch(col0);
-        for (int c0 = col0; c0 < cols; c0 += T::ROWS) {
-            __syncthreads();
-            next.put(lq, lg, tid);
-            if (tid < T::ROWS) {
-                row_lse[tid] = n_lse == -INFINITY ? INFINITY : n_lse * LOG2E;     // exp2(x - inf) = 0
-                row_delta[tid] = n_delta;
-                row_lim[tid] = (c0 + tid) / G + shift;
-            }
-            __syncthreads();
-            if (c0 + T::ROWS < cols) fetch(c0 + T::ROWS);
-            if (!busy || (c0 + T::ROWS - 1) / G < wfirst) continue;
-            const bool part = A.causal && key0 + wave * 32 + 31 > c0 / G + shift;
-#pragma unroll
+    const float scale2 = scale_of_scores(A.scale);
+    const int middle = bias_middle(A.reach);
+    const bool busy = wkey < ks.n;
+    const int wfirst = A.causal && wkey > shift ? (wkey - shift) * G : 0;             // first column that sees a key of the wavefront
+    if constexpr (BIAS) fill_bias<E>(A, head0, table, tid, THREADS);
+    if (col0 < cols) finish(0);
+    __syncthreads();
+    int buf = 0;
+    while (col0 < cols && head0 < head_end) {
+        const bool last_tile = c0 + T::ROWS >= cols;
+        const int n_head = last_tile ? head0 + G : head0, n_c = last_tile ? col0 : c0 + T::ROWS;
+        if (n_head < head_end) issue(n_head, n_c, lds[buf ^ 1]);
+        const char *lq = lds[buf], *lg = lq + T::BYTES;
+        auto compute = [&](auto part) {
+            // a lane's key is seen by columns from (key - shift) G on
+            const int need = (key - shift) * G - c0 - 4 * h;
+#pragma unroll 1
             for (int b = 0; b < NB; ++b) {
                 f32x16 s = {}, dp = {};
 #pragma unroll
                 for (int c = 0; c < D / 16; ++c) O::mma(s, T::rows(lq, lane, b, c), k.v[c]);
 #pragma unroll
                 for (int c = 0; c < D / 16; ++c) O::mma(dp, T::rows(lg, lane, b, c), v.v[c]);
+                const int d0 = wkey - (c0 + 32 * b + shift), side = BIAS ? block_side(d0, A.reach) : 0;
+                const float* tab = table + middle + key - (c0 + 32 * b + shift) - 4 * h - 27;    // of the lane's last row
+                const float far = BIAS && side ? table[side < 0 ? 0 : 2 * middle] : 0.f;
                 f32x16 ds;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int r0 = 32 * b + 8 * j + 4 * h;
-                    const f32x4 e = *(const f32x4*)(row_lse + r0), dl = *(const f32x4*)(row_delta + r0);
-                    const int4 lm = *(const int4*)(row_lim + r0);
-                    const int lims[4] = {lm.x, lm.y, lm.z, lm.w};
+                    const f32x4 e = *(const f32x4*)(row_lse[buf] + r0), dl = *(const f32x4*)(row_delta[buf] + r0);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int r = 4 * j + i;
-                        float x = s[r] * scale2;
-                        if constexpr (BIAS) x += bias_at(table, A.reach, key - lims[i]);
-                        float p = exp2_fast(x - e[i]);
-                        if (part && key > lims[i]) p = 0.f;
+                        float x = fmaf(s[r], scale2, e[i]);
+                        if constexpr (BIAS) x += side ? far : tab[27 - 8 * j - i];
+                        float p = exp2_fast(x);
+                        if constexpr (decltype(part)::value) p = 32 * b + 8 * j + i >= need ? p : 0.f;
                         s[r] = p;
                         ds[r] = p * (dp[r] - dl[i]);
                     }
                 }
+                const typename O::Frag p0 = O::round(eight<0>(s)), p1 = O::round(eight<8>(s));
+                const typename O::Frag d0f = O::round(eight<0>(ds)), d1f = O::round(eight<8>(ds));
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const auto x = c ? __builtin_shufflevector(s, s, 8, 9, 10, 11, 12, 13, 14, 15)
-                                     : __builtin_shufflevector(s, s, 0, 1, 2, 3, 4, 5, 6, 7);
-                    const auto y = c ? __builtin_shufflevector(ds, ds, 8, 9, 10, 11, 12, 13, 14, 15)
-                                     : __builtin_shufflevector(ds, ds, 0, 1, 2, 3, 4, 5, 6, 7);
-                    const typename O::Frag p = O::round(x), q = O::round(y);
+                for (int db = 0; db < DB; ++db) O::mma(av[db], T::turned(lg, lane, b, 0, db), p0);
 #pragma unroll
-                    for (int db = 0; db < DB; ++db) O::mma(av[db], T::turned(lg, lane, b, c, db), p);
+                for (int db = 0; db < DB; ++db) O::mma(av[db], T::turned(lg, lane, b, 1, db), p1);
 #pragma unroll
-                    for (int db = 0; db < DB; ++db) O::mma(ak[db], T::turned(lq, lane, b, c, db), q);
-                }
+                for (int db = 0; db < DB; ++db) O::mma(ak[db], T::turned(lq, lane, b, 0, db), d0f);
+#pragma unroll
+                for (int db = 0; db < DB; ++db) O::mma(ak[db], T::turned(lq, lane, b, 1, db), d1f);
+            }
+        };
+        if (busy && c0 + T::ROWS > wfirst) {
+            if (A.causal && (wkey + 31 - shift) * G > c0) compute(std::true_type{}); else compute(std::false_type{});
+        }
+        if (n_head < head_end) finish(buf ^ 1);
+        __syncthreads();
+        if constexpr (BIAS) {
+            if (n_head != head0 && n_head < head_end) {
+                fill_bias<E>(A, n_head, table, tid, THREADS);
+                __syncthreads();
             }
         }
+        head0 = n_head;
+        c0 = n_c;
+        buf ^= 1;
     }
     if (!real) return;
     const int64_t dense = (at * A.kv_heads + kv) * D;
@@ -580,25 +741,26 @@ template <class F> hipError_t by_width(int d, F&& f) {
         default: return f(std::integral_constant<int, 128>{});
     }
 }
-template <class F> hipError_t by_waves(int waves, bool bias, F&& f) {
-    using One = std::integral_constant<int, 1>;
-    using Four = std::integral_constant<int, 4>;
-    if (bias) return waves == 1 ? f(One{}, std::true_type{}) : f(Four{}, std::true_type{});
-    return waves == 1 ? f(One{}, std::false_type{}) : f(Four{}, std::false_type{});
+template <class F> hipError_t by_form(int waves, bool bias, bool masked, F&& f) {
+    auto w = [&](auto b, auto m) {
+        return waves == 1 ? f(std::integral_constant<int, 1>{}, b, m) : f(std::integral_constant<int, 4>{}, b, m);
+    };
+    if (bias) return masked ? w(std::true_type{}, std::true_type{}) : w(std::true_type{}, std::false_type{});
+    return masked ? w(std::false_type{}, std::true_type{}) : w(std::false_type{}, std::false_type{});
 }
 
 template <class E>
 hipError_t launch_attention(const AttnArgs& A, const AttnPlan& P, E* out, float* lse, char* ws, hipStream_t st) {
-    if (P.q_slots == 0 || A.total_q == 0) return hipSuccess;
+    if (A.total_q == 0) return hipSuccess;
     return by_width(P.d, [&](auto dc) {
         constexpr int D = decltype(dc)::value;
         float* o_part = (float*)(ws + P.o_part);
         float2* ml_part = (float2*)(ws + P.ml_part);
-        const hipError_t e = by_waves(P.q_waves, A.bias != nullptr, [&](auto nw, auto bias) {
+        const hipError_t e = by_form(P.q_waves, A.bias != nullptr, A.keep != nullptr, [&](auto nw, auto bias, auto masked) {
             constexpr int NW = decltype(nw)::value;
-            constexpr bool BIAS = decltype(bias)::value;
-            const size_t lds = BIAS ? 4 * (size_t)(2 * A.reach + 1) : 0;
-            k_attention<E, D, NW, BIAS><<<dim3((unsigned)(P.q_slots * P.units * P.splits)), 64 * NW, lds, st>>>(
+            constexpr bool BIAS = decltype(bias)::value, MASKED = decltype(masked)::value;
+            const size_t lds = BIAS ? 4 * (size_t)bias_width(A.reach) : 0;
+            k_attention<E, D, NW, BIAS, MASKED><<<dim3((unsigned)(P.q_slots * P.units * P.splits)), 64 * NW, lds, st>>>(
                 A, (int)P.q_slots, P.units, P.splits, out, lse, o_part, ml_part);
             return hipGetLastError();
         });
@@ -617,25 +779,25 @@ hipError_t launch_attention_backward(const AttnArgs& A, const AttnPlan& P, const
         constexpr int D = decltype(dc)::value;
         hipError_t e = hipSuccess;
         if (A.total_q > 0) {
-            e = by_waves(P.q_waves, A.bias != nullptr, [&](auto nw, auto bias) {
+            e = by_form(P.q_waves, A.bias != nullptr, A.keep != nullptr, [&](auto nw, auto bias, auto masked) {
                 constexpr int NW = decltype(nw)::value;
-                constexpr bool BIAS = decltype(bias)::value;
-                const size_t lds = BIAS ? 4 * (size_t)(2 * A.reach + 1 + 2 * NW * (2 * A.reach + 125)) : 0;
-                k_attention_dq<E, D, NW, BIAS><<<dim3((unsigned)(P.q_slots * P.units)), 64 * NW, lds, st>>>(
+                constexpr bool BIAS = decltype(bias)::value, MASKED = decltype(masked)::value;
+                const size_t lds = BIAS ? 4 * (size_t)((NW + 1) * bias_width(A.reach)) : 0;
+                k_attention_dq<E, D, NW, BIAS, MASKED><<<dim3((unsigned)(P.q_slots * P.units)), 64 * NW, lds, st>>>(
                     A, (int)P.q_slots, P.units, (const E*)G.out, (const E*)G.dout, G.lse, (E*)G.dq, delta, bias_part);
                 return hipGetLastError();
             });
             if (e != hipSuccess) return e;
         }
         const int q_slots = A.total_q > 0 ? (int)P.q_slots : 0;
-        return by_waves(P.k_waves, A.bias != nullptr, [&](auto nw, auto bias) {
+        return by_form(P.k_waves, A.bias != nullptr, A.keep != nullptr, [&](auto nw, auto bias, auto masked) {
             constexpr int NW = decltype(nw)::value;
-            constexpr bool BIAS = decltype(bias)::value;
-            const size_t lds = BIAS ? 4 * (size_t)(2 * A.reach + 1) : 0;
+            constexpr bool BIAS = decltype(bias)::value, MASKED = decltype(masked)::value;
+            const size_t lds = BIAS ? 4 * (size_t)bias_width(A.reach) : 0;
             const int main = A.total_k > 0 ? (int)(P.k_slots * A.kv_heads) : 0;
             const int more = BIAS ? (A.n_buckets * A.heads + NW - 1) / NW : 0;
             if (main + more == 0) return hipSuccess;
-            k_attention_dkv<E, D, NW, BIAS><<<dim3((unsigned)(main + more)), 64 * NW, lds, st>>>(
+            k_attention_dkv<E, D, NW, BIAS, MASKED><<<dim3((unsigned)(main + more)), 64 * NW, lds, st>>>(
                 A, (int)P.k_slots, main, q_slots, (const E*)G.dout, G.lse, delta, bias_part, (E*)G.dk, (E*)G.dv, (E*)G.dbias);
             return hipGetLastError();
         });

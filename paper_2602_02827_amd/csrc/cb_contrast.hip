@@ -243,8 +243,8 @@ __global__ __launch_bounds__(256) void k_maxsim_ddocs(const float* dscores, cons
     __shared__ int next[4][kTokens], begin[kTokens + 1];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int doc = find_sequence(off, N, kTokens, total, blockIdx.x, lane);
-    const Range r = sequence_rows(off, doc, total);
-    const int first = ((int)blockIdx.x - place_of(off, doc, kTokens, total)) * kTokens;
+    const Range r = sequence_rows(off, doc, total, kTokens);
+    const int first = ((int)blockIdx.x - r.place) * kTokens;
     if (first < 0 || first >= r.n) return;
     const int piece = tid % R::LANES, group = tid / R::LANES;
     const int entries = nq * T;

@@ -55,14 +55,20 @@ template <> struct Oper<float> {
     static __device__ __forceinline__ void store4(float* p, const f32x4& x) { *(f32x4*)p = x; }
 };
 
-// ROWS rows of D values in LDS, as 16-byte pieces.  A piece's place in its row is turned by the row's low bits, so that
-// eight rows' pieces of one column lie in different banks (row operands: eight lanes a clock), and so do the rows that a
-// turned operand takes.
+// ROWS rows of D values in LDS, as 16-byte pieces.  A piece's place in its row is turned by the row's low bits.  256 bytes are
+// read a clock: sixteen rows' pieces of one column (row operands) lie in different banks, and so do the four rows of 64 bytes
+// that half a wavefront takes of a turned operand in 16 bits (128-byte and 256-byte rows: by the turn's upper bits; the others
+// by their pitch).
 template <class E, int D> struct Tile {
     using Frag = typename Oper<E>::Frag;
     static constexpr int ROWS = Oper<E>::ROWS, PITCH = D * (int)sizeof(E), PIECES = PITCH / 16;
     static constexpr int BYTES = ROWS * PITCH;
-    static __device__ __forceinline__ int turn(int row) { return PIECES % 8 == 0 ? row & 7 : (row >> 1) & 3; }
+    static __device__ __forceinline__ int turn(int row) {
+        if constexpr (sizeof(E) == 4 && PIECES % 16 == 0) return (row & 3) | ((row >> 1) & 4) | ((row << 1) & 8);
+        if constexpr (PIECES % 16 == 0) return ((row & 3) << 2) | ((row >> 2) & 3);
+        if constexpr (PIECES % 8 == 0) return ((row & 2) << 1) | ((row >> 2) & 3);
+        return (row >> 2) & 3;
+    }
     static __device__ __forceinline__ int at(int row, int piece) { return row * PITCH + ((piece ^ turn(row)) << 4); }
     // rows 32b .. 32b+31, elements 16c .. 16c+15 of each
     static __device__ __forceinline__ Frag rows(const char* t, int lane, int b, int c) {
@@ -85,7 +91,8 @@ template <class E, int D> struct Tile {
             const char* p = t + at(row, piece) + (lane & 1) * 8;
             using L = __attribute__((address_space(3))) i16x4;
             const i16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)p);
-            const i16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)(p + 8 * PITCH));   // eight rows on: the same turn
+            const char* p8 = t + at(row + 8, piece) + (lane & 1) * 8;
+            const i16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)p8);
             const auto both = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
             return __builtin_bit_cast(bf16x8, both);
         } else {
@@ -101,13 +108,31 @@ template <class E, int D> struct Tile {
     }
 };
 
-// value of the lane that holds the other half of the accumulator's rows
-__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+// The two halves of a column's rows are in lanes n and n + 32.
+__device__ __forceinline__ float max_of_halves(float x) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const auto s = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const uint32_t a = s[0], b = s[1];
+    return fmaxf(__uint_as_float(a), __uint_as_float(b));
+}
+__device__ __forceinline__ float sum_of_halves(float x) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const auto s = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const uint32_t a = s[0], b = s[1];
+    return __uint_as_float(a) + __uint_as_float(b);
+}
+
+// Sixteen bytes a lane from memory to LDS without registers: lane i's go to dst + 16 i (dst: the same for the wavefront).
+__device__ __forceinline__ void copy_to_lds(const void* src, char* dst) {
+    using G = const __attribute__((address_space(1))) void;
+    using L = __attribute__((address_space(3))) void;
+    __builtin_amdgcn_global_load_lds((G*)src, (L*)dst, 16, 0, 0);
+}
+__device__ __forceinline__ void wait_for_copies() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // Tiles of ragged sequences: sequence i begins at place off[i] / per + i, which leaves room for all its tiles of `per` rows
 // and needs no table.  Finds the sequence of a place (all lanes of a wavefront together), 64 offsets at a time.
-__device__ __forceinline__ int place_of(const int64_t* off, int i, int per, int total) {
-    int64_t x = off[i];
+__device__ __forceinline__ int place_of(int64_t x, int i, int per, int total) {
     x = x < 0 ? 0 : x > total ? total : x;
     return (int)((uint32_t)x / (uint32_t)per) + i;
 }
@@ -116,20 +141,21 @@ __device__ __forceinline__ int find_sequence(const int64_t* off, int n, int per,
     while (hi - lo > 1) {
         const int step = (hi - lo + 63) / 64;
         const int i = lo + lane * step;
-        const unsigned long long le = __ballot(i < hi && place_of(off, i, per, total) <= place);
+        const unsigned long long le = __ballot(i < hi && place_of(off[i], i, per, total) <= place);
         const int c = le == ~0ull ? 64 : __builtin_ctzll(~le);   // of the first ones: also for offsets that are out of order
-        if (c == 0) return lo;
+        if (c == 0) break;
         lo += (c - 1) * step;
         hi = lo + step < hi ? lo + step : hi;
     }
-    return lo;
+    return __builtin_amdgcn_readfirstlane(lo);
 }
-struct Range { int lo, n; };
-__device__ __forceinline__ Range sequence_rows(const int64_t* off, int i, int total) {
+// Rows of sequence i (the same in all lanes), and the place of its first tile.
+struct Range { int lo, n, place; };
+__device__ __forceinline__ Range sequence_rows(const int64_t* off, int i, int total, int per = 1) {
     int64_t a = off[i], b = off[i + 1];
     a = a < 0 ? 0 : a > total ? total : a;
     b = b < a ? a : b > total ? total : b;
-    return {(int)a, (int)(b - a)};
+    return {(int)a, (int)(b - a), place_of(a, i, per, total)};
 }
 
 }  // namespace cb

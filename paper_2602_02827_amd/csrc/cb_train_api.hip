@@ -56,7 +56,7 @@ using namespace cb;
 
 namespace {
 
-constexpr int64_t kMostRows = 0x7fffffff - (1 << 16);
+constexpr int64_t kMostRows = 0x7fffffff - (1 << 16), kMostRowBytes = 1 << 25;
 
 bool misaligned(const void* p, size_t to = 16) { return ((uintptr_t)p & (to - 1)) != 0; }
 
@@ -100,8 +100,14 @@ int attn_args(const colbandit_attn* a, AttnArgs& A) {
     if (!a->q_offsets || !a->k_offsets || (a->total_q && !a->q) || (a->total_k && (!a->k || !a->v))) return COLBANDIT_ERR_NULL;
     const int64_t eb = a->dt == COLBANDIT_BF16 ? 2 : 4;
     const int64_t strides[] = {a->q_row, a->q_head, a->k_row, a->k_head, a->v_row, a->v_head};
-    for (int64_t s : strides)
+    for (int64_t s : strides) {
+        if (s < 0) return COLBANDIT_ERR_SHAPE;
         if (s * eb % 16) return COLBANDIT_ERR_ALIGNMENT;
+    }
+    // a tile's rows are addressed in 32 bits from its first one
+    if (a->k_row * eb > kMostRowBytes || a->v_row * eb > kMostRowBytes || a->q_row * eb > kMostRowBytes ||
+        (int64_t)a->heads * a->d * eb > kMostRowBytes)
+        return COLBANDIT_ERR_UNSUPPORTED;
     if (misaligned(a->q) || misaligned(a->k) || misaligned(a->v) || misaligned(a->q_offsets, 8) || misaligned(a->k_offsets, 8))
         return COLBANDIT_ERR_ALIGNMENT;
     A = AttnArgs{};
@@ -132,7 +138,7 @@ int attn_args(const colbandit_attn* a, AttnArgs& A) {
     A.heads = a->heads;
     A.kv_heads = a->kv_heads;
     A.group = a->heads / a->kv_heads;
-    A.pack = !a->bias && A.group <= 16 ? A.group : 1;
+    A.pack = !a->bias && A.group <= 16 && a->q_head * eb <= kMostRowBytes ? A.group : 1;
     A.total_q = (int)a->total_q;
     A.total_k = (int)a->total_k;
     A.causal = a->causal != 0;
