@@ -20,17 +20,34 @@ namespace cb {
 constexpr int kBlock = 62;
 __device__ __host__ __forceinline__ int bias_middle(int reach) { return reach + kBlock; }
 __device__ __host__ __forceinline__ int bias_width(int reach) { return 2 * bias_middle(reach) + 1; }
+// Eight threads write a bucket's distances (its first one is in `starts`, in LDS).
+__device__ __forceinline__ void load_starts(const AttnArgs& A, int16_t* starts, int tid, int threads) {
+    for (int i = tid; i <= A.n_dir; i += threads) starts[i] = i < A.n_dir ? A.starts[i] : (int16_t)(bias_middle(A.reach) + 1);
+}
 template <class E>
-__device__ __forceinline__ void fill_bias(const AttnArgs& A, int head, float* table, int tid, int threads) {
-    for (int i = tid; i < bias_width(A.reach); i += threads) {
-        const int dist = i - bias_middle(A.reach);
-        const int far = A.causal ? (dist < 0 ? -dist : 0) : (dist < 0 ? -dist : dist);
-        int b = -1;
-        for (int j = 0; j < A.n_dir; ++j) b += A.starts[j] <= far ? 1 : 0;   // the starts are scalar loads
-        if (!A.causal && dist > 0) b += A.n_dir;
+__device__ __forceinline__ void fill_bias(const AttnArgs& A, int head, const int16_t* starts, float* table, int tid, int threads) {
+    const int middle = bias_middle(A.reach);
+    for (int b = tid >> 3; b < A.n_buckets; b += threads >> 3) {
+        const bool behind = b >= A.n_dir;             // keys behind the query
+        const int i = behind ? b - A.n_dir : b;
         const float x = (float)((const E*)A.bias)[(int64_t)b * A.heads + head], y = x * LOG2E;
-        table[i] = fabsf(x) < INFINITY ? fminf(fmaxf(y, -3.4028235e38f), 3.4028235e38f) : y;
+        const float z = fabsf(x) < INFINITY ? fminf(fmaxf(y, -3.4028235e38f), 3.4028235e38f) : y;
+        const int end = starts[i + 1];
+        for (int j = starts[i] + (tid & 7); j < end; j += 8)
+            if (!behind) table[middle - j] = z; else if (j > 0) table[middle + j] = z;
+        if (A.causal && b == 0)                       // no row sees a key behind it: as distance 0
+            for (int j = 1 + (tid & 7); j <= middle; j += 8) table[middle + j] = z;
     }
+}
+// LDS of the starts and of `tables` tables.
+constexpr int kStartsBytes = 272;                     // of up to 129
+__host__ __forceinline__ size_t bias_bytes(int reach, int tables) { return kStartsBytes + 4 * (size_t)(tables * bias_width(reach)); }
+
+// Workgroups are dealt to the eight XCDs in turn; numbered so that each XCD has consecutive ones, the tiles that share keys
+// read them through one L2.
+__device__ __forceinline__ int in_order(int block, int blocks) {
+    const int each = blocks >> 3, more = blocks & 7, xcd = block & 7;
+    return xcd * each + (xcd < more ? xcd : more) + (block >> 3);
 }
 // Which way a block of 32 rows and columns lies whose first key and row are d0 apart: -1 or 1: all beyond reach, 0: not.
 __device__ __forceinline__ int block_side(int d0, int reach) { return d0 + 31 <= -reach ? -1 : d0 - 31 >= reach ? 1 : 0; }
@@ -65,8 +82,8 @@ template <class E, int D, int THREADS, bool MASKED> struct Staged {
     uint8_t keep[MASKED ? N : 1];
     // a_at(row), b_at(row): byte offsets of the matrices' rows; kept(row): whether the mask leaves it.  rows: how many are left.
     template <class AtA, class AtB, class Kept>
-    __device__ __forceinline__ void issue(const char* a, const char* b, char* lds, int rows, int tid, AtA&& a_at, AtB&& b_at, Kept&& kept) {
-        const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    __device__ __forceinline__ void issue(const char* a, const char* b, char* lds, int rows, int tid0, AtA&& a_at, AtB&& b_at, Kept&& kept) {
+        const int tid = here(tid0), wave = __builtin_amdgcn_readfirstlane(tid0 >> 6);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int pos = i * THREADS + tid, place = pos / T::PIECES;
@@ -116,12 +133,12 @@ struct QueryTile {
 
 // A wavefront's 32 columns of it.
 struct QueryColumns {
-    int row, head, lim, first_lim, end;       // own row, head and key limit; that of the first column; keys that any sees
+    int row, head, lim, first_lim, end;       // own row, head in its unit, key limit; that of the first column; keys that any sees
     bool real, busy;
-    __device__ __forceinline__ QueryColumns(const AttnArgs& A, const QueryTile& t, int G, int per, int head0, int wave, int lane) {
+    __device__ __forceinline__ QueryColumns(const AttnArgs& A, const QueryTile& t, int G, int per, int wave, int lane) {
         const int local = (wave * 32 + (lane & 31)) / G;
         row = t.row0 + local;
-        head = head0 + (wave * 32 + (lane & 31)) % G;
+        head = (wave * 32 + (lane & 31)) % G;
         real = local < per && row < t.Lq;
         lim = row + t.shift;
         const int first = t.row0 + wave * 32 / G, last = t.row0 + (wave * 32 + 31) / G;
@@ -136,90 +153,104 @@ template <int LO> __device__ __forceinline__ f32x8 eight(const f32x16& x) {
     return __builtin_shufflevector(x, x, LO, LO + 1, LO + 2, LO + 3, LO + 4, LO + 5, LO + 6, LO + 7);
 }
 
-// Which of a tile's rows a lane's column sees: by a limit on the row, and with a mask one bit each.
-template <bool MASKED> struct Seen {
-    int room;
-    uint32_t low, high;
-    __device__ __forceinline__ Seen(int room, uint64_t mask, int h) : room(room - 4 * h) {
-        if constexpr (MASKED) {
-            const uint64_t upto = room < 0 ? 0ull : room >= 63 ? ~0ull : (2ull << room) - 1ull;
-            const uint64_t m = (mask & upto) >> (4 * h);
-            low = (uint32_t)m;
-            high = (uint32_t)(m >> 32);
-        }
-    }
-    // row 32b + k (and 4h)
-    __device__ __forceinline__ float otherwise(float x, float y, int b, int k) const {
-        if constexpr (MASKED) {
-            const int m = (int)((b ? high : low) << (31 - k)) >> 31;
-            return __int_as_float((__float_as_int(x) & m) | (__float_as_int(y) & ~m));
-        } else {
-            return 32 * b + k <= room ? x : y;
-        }
-    }
-};
+// Tiles are seen whole, or some of their rows by no column (past the end, or hidden by the mask: minus infinity is added to
+// their scores, a value of each row in LDS), or by some columns only (causal: a limit on the row as well).
+struct Whole { static constexpr bool part = false, diagonal = false; };
+struct Part { static constexpr bool part = true, diagonal = false; };
+struct Diagonal { static constexpr bool part = true, diagonal = true; };
 
 // ---- forward -------------------------------------------------------------------------------------------------
 // One pass over the keys with the running maximum and sum of the softmax, in 32 bits; probabilities are rounded to the
 // storage type for the second product (their sum is not).  The maximum that is subtracted may lag by up to kLag: sums and
 // outputs are rescaled only when it is passed, which few tiles after the first do; probabilities up to 2^kLag are no less exact.
 constexpr float kLag = 8.f;
+// A workgroup takes its tile for `run` head units one after the other, the first keys of the next on their way while it
+// computes: short sequences have one to three tiles of keys, whose latency would otherwise be most of the time.
 template <class E, int D, int NW, bool BIAS, bool MASKED>
-__global__ __launch_bounds__(64 * NW, 2) void k_attention(const AttnArgs A, int slots, int units, int splits, E* out, float* lse,
+__global__ __launch_bounds__(64 * NW, D <= 64 ? 3 : 2) void k_attention(const AttnArgs A, int slots, int units, int run, int splits, E* out, float* lse,
                                                           float* o_part, float2* ml_part) {
     using O = Oper<E>;
     using T = Tile<E, D>;
     constexpr int NB = T::ROWS / 32, DB = D / 32, THREADS = 64 * NW;
     __shared__ __align__(16) char lds[2][2 * T::BYTES];
-    extern __shared__ float table[];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
-    const int slot = blockIdx.x % slots, unit = blockIdx.x / slots % units, split = blockIdx.x / slots / units;
+    __shared__ __align__(16) float hidden[2][T::ROWS];           // 0, or minus infinity for rows that no column sees
+    extern __shared__ __align__(16) char dyn[];
+    const int tid = threadIdx.x, lane0 = tid & 63, lane = lane0, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
+    const int work = in_order(blockIdx.x, gridDim.x), runs = (units + run - 1) / run;
+    const int split = work % splits, slot = work / splits / runs;
+    int unit = work / splits % runs * run;
+    const int end_unit = unit + run < units ? unit + run : units;
     const int G = A.pack, per = 32 * NW / G;
     const QueryTile t(A, slot, per, lane);
     if (t.none) return;
-    const int head0 = unit * G, kv = head0 / A.group;
-    const QueryColumns w(A, t, G, per, head0, wave, lane);
+    const QueryColumns w(A, t, G, per, wave, lane);
     const int tiles = (t.end + T::ROWS - 1) / T::ROWS, each = (tiles + splits - 1) / splits;
     const int first_tile = split * each, end_tile = first_tile + each < tiles ? first_tile + each : tiles;
 
     const int64_t krow = A.k_row * (int64_t)sizeof(E), vrow = A.v_row * (int64_t)sizeof(E);
-    const char* kp = (const char*)A.k + t.k0 * krow + kv * A.k_head * (int64_t)sizeof(E);
-    const char* vp = (const char*)A.v + t.k0 * vrow + kv * A.v_head * (int64_t)sizeof(E);
     Staged<E, D, THREADS, MASKED> next;
     uint8_t next_keep = 0;
-    auto issue = [&](int base, char* to) {
-        next.issue(kp + base * krow, vp + base * vrow, to, t.end - base, tid, [&](int r) { return (uint32_t)r * (uint32_t)krow; },
-                   [&](int r) { return (uint32_t)r * (uint32_t)vrow; }, [&](int r) { return A.keep[(int64_t)t.k0 + base + r]; });
+    auto issue = [&](int u, int base, char* to) {
+        const int kv = u * G / A.group;
+        next.issue((const char*)A.k + (t.k0 + base) * krow + kv * A.k_head * (int64_t)sizeof(E),
+                   (const char*)A.v + (t.k0 + base) * vrow + kv * A.v_head * (int64_t)sizeof(E), to, t.end - base, tid,
+                   [&](int r) { return (uint32_t)r * (uint32_t)krow; }, [&](int r) { return (uint32_t)r * (uint32_t)vrow; },
+                   [&](int r) { return A.keep[(int64_t)t.k0 + base + r]; });
+        next_keep = base + lane < t.end;
         if constexpr (MASKED) next_keep = lane < T::ROWS && base + lane < t.end ? A.keep[(int64_t)t.k0 + base + lane] : 0;
     };
-    if (first_tile < end_tile) issue(first_tile * T::ROWS, lds[0]);
-    if constexpr (BIAS) fill_bias<E>(A, head0, table, tid, THREADS);
+    constexpr uint64_t kAllRows = T::ROWS == 64 ? ~0ull : (1ull << (T::ROWS & 63)) - 1ull;
+    uint64_t seen = 0;                                           // rows of the tile that some column sees
+    auto finish = [&](int buf) {
+        next.finish(lds[buf], tid);
+        if (tid < T::ROWS) hidden[buf][tid] = next_keep ? 0.f : -INFINITY;
+        seen = __ballot(next_keep != 0) & kAllRows;
+    };
     Column<E, D> q;
-    q.load((const E*)A.q + (int64_t)(t.q0 + w.row) * A.q_row + w.head * A.q_head, w.real, h);
-    q.take_sign(A.scale);
+    auto load_q = [&](int u) {
+        const int h = here(lane0) >> 5;
+        q.load((const E*)A.q + (int64_t)(t.q0 + w.row) * A.q_row + (u * G + w.head) * A.q_head, w.real, h);
+        q.take_sign(A.scale);
+    };
+    const bool any = first_tile < end_tile;
+    if (any) issue(unit, first_tile * T::ROWS, lds[0]);
+    load_q(unit);
+    int16_t* starts = (int16_t*)dyn;
+    float* table = (float*)(dyn + kStartsBytes);
+    const int middle = bias_middle(A.reach), width = bias_width(A.reach);
+    if constexpr (BIAS) {
+        load_starts(A, starts, tid, THREADS);
+        __syncthreads();
+        fill_bias<E>(A, unit, starts, table, tid, THREADS);
+    }
     f32x16 acc[DB] = {};
     float m = -INFINITY, l = 0.f;
+    bool sees = !MASKED;                                         // the mask leaves the row some key
     const float scale2 = scale_of_scores(A.scale);
-    const int middle = bias_middle(A.reach);
-    if (first_tile < end_tile) next.finish(lds[0], tid);
-    uint64_t seen = __ballot(next_keep != 0);
+    if (any) finish(0);
     __syncthreads();
-    for (int i = first_tile; i < end_tile; ++i) {
+    int i = first_tile, buf = 0;
+    while (true) {
         const int base = i * T::ROWS;
-        const char *lk = lds[(i - first_tile) & 1], *lv = lk + T::BYTES;
-        char* other = lds[(i - first_tile + 1) & 1];
-        if (i + 1 < end_tile) issue(base + T::ROWS, other);
-        auto compute = [&](auto part) {
-            f32x16 s[NB];
+        const char *lk = lds[buf], *lv = lk + T::BYTES;
+        const bool last = i + 1 >= end_tile;                     // of the unit
+        const int n_unit = last ? unit + 1 : unit, n_i = last ? first_tile : i + 1;
+        const bool more = n_unit < end_unit;
+        if (more && any) issue(n_unit, n_i * T::ROWS, lds[buf ^ 1]);
+        auto compute = [&](auto how, auto blocks) {
+            using How = decltype(how);
+            const int lane = here(lane0), h = lane >> 5;
+            constexpr int N = decltype(blocks)::value;           // blocks of 32 keys
+            f32x16 s[N];
 #pragma unroll
-            for (int b = 0; b < NB; ++b) {
+            for (int b = 0; b < N; ++b) {
                 s[b] = {};
 #pragma unroll
                 for (int c = 0; c < D / 16; ++c) O::mma(s[b], T::rows(lk, lane, b, c), q.v[c]);
             }
             if constexpr (BIAS) {
 #pragma unroll
-                for (int b = 0; b < NB; ++b) {
+                for (int b = 0; b < N; ++b) {
                     const int d0 = base + 32 * b - w.first_lim, side = block_side(d0, A.reach);
                     if (side) {
                         const float x = table[side < 0 ? 0 : 2 * middle];
@@ -232,21 +263,29 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attention(const AttnArgs A, int 
                     }
                 }
             }
-            if constexpr (decltype(part)::value) {
-                const int last = t.end - 1 - base, own = w.lim - base;
-                const Seen<MASKED> see(A.causal && own < last ? own : last, seen, h);
+            constexpr bool SCALED = BIAS || How::part;           // s is in powers of two
+            if constexpr (How::part) {
+                const int room = w.lim - base - 4 * h;
 #pragma unroll
-                for (int b = 0; b < NB; ++b)
+                for (int b = 0; b < N; ++b)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s[b][r] = see.otherwise(s[b][r], -INFINITY, b, 8 * (r >> 2) + (r & 3));
+                    for (int j = 0; j < 4; ++j) {
+                        const f32x4 no = *(const f32x4*)(hidden[buf] + 32 * b + 8 * j + 4 * h);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            float& x = ((float*)&s[b])[4 * j + e];
+                            x = BIAS ? x + no[e] : fmaf(x, scale2, no[e]);
+                            if constexpr (How::diagonal) x = 32 * b + 8 * j + e <= room ? x : -INFINITY;
+                        }
+                    }
             }
             float top = s[0][0];
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
+            for (int b = 0; b < N; ++b)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) top = __builtin_elementwise_maximum(top, s[b][r]);
             top = max_of_halves(top);
-            if constexpr (!BIAS) top *= scale2;
+            if constexpr (!SCALED) top *= scale2;
             const bool passed = top > m + kLag;
             if (__ballot(passed)) {
                 const float to = passed ? top : m;
@@ -258,10 +297,10 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attention(const AttnArgs A, int 
             }
             const float off = m == -INFINITY ? 0.f : -m;
 #pragma unroll
-            for (int b = 0; b < NB; ++b) {
+            for (int b = 0; b < N; ++b) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    s[b][r] = exp2_fast(BIAS ? s[b][r] + off : fmaf(s[b][r], scale2, off));
+                    s[b][r] = exp2_fast(SCALED ? s[b][r] + off : fmaf(s[b][r], scale2, off));
                     l += s[b][r];
                 }
                 const typename O::Frag p0 = O::round(eight<0>(s[b])), p1 = O::round(eight<8>(s[b]));
@@ -271,37 +310,70 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attention(const AttnArgs A, int 
                 for (int db = 0; db < DB; ++db) O::mma(acc[db], T::turned(lv, lane, b, 1, db), p1);
             }
         };
-        if (w.busy && base < w.end) {
-            const bool whole = base + T::ROWS <= t.end && !(A.causal && base + T::ROWS - 1 > w.first_lim) && (!MASKED || seen == ~0ull);
-            if (whole) compute(std::false_type{}); else compute(std::true_type{});
+        if (any && w.busy && base < w.end) {
+            using All = std::integral_constant<int, NB>;
+            using One = std::integral_constant<int, 1>;
+            const bool one = NB > 1 && base + 32 >= w.end;
+            if constexpr (MASKED) {
+                const int room = A.causal ? w.lim - base : 63;
+                sees |= (seen & (room < 0 ? 0ull : room >= 63 ? ~0ull : (2ull << room) - 1ull)) != 0;
+            }
+            if (A.causal && base + T::ROWS - 1 > w.first_lim) {
+                if (one) compute(Diagonal{}, One{}); else compute(Diagonal{}, All{});
+            } else if (seen != kAllRows) {
+                if (one) compute(Part{}, One{}); else compute(Part{}, All{});
+            } else {
+                compute(Whole{}, All{});
+            }
         }
-        if (i + 1 < end_tile) next.finish(other, tid);
-        seen = __ballot(next_keep != 0);
+        if (last) {
+            if (more) load_q(n_unit);
+            l = sum_of_halves(l);
+            if (MASKED && !sees) {                               // whatever its row held
+                m = -INFINITY;
+                l = 0.f;
+#pragma unroll
+                for (int db = 0; db < DB; ++db) acc[db] = {};
+            }
+            const int head = unit * G + w.head;
+            const int64_t at = (int64_t)(t.q0 + w.row);
+            if (w.real && splits > 1) {
+                const int64_t place = ((int64_t)split * A.heads + head) * A.total_q + at;
+                if (h == 0) ml_part[place] = make_float2(m, l);
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        *(f32x4*)(o_part + place * D + 32 * db + 8 * j + 4 * h) =
+                            f32x4{acc[db][4 * j], acc[db][4 * j + 1], acc[db][4 * j + 2], acc[db][4 * j + 3]};
+            } else if (w.real) {
+                const float inv = l == 0.f ? 0.f : 1.f / l;
+                if (h == 0) lse[(int64_t)head * A.total_q + at] = l == 0.f ? -INFINITY : m * LN2 + logf(l);
+                E* o = out + (at * A.heads + head) * D;
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        O::store4(o + 32 * db + 8 * j + 4 * h, f32x4{acc[db][4 * j] * inv, acc[db][4 * j + 1] * inv,
+                                                                      acc[db][4 * j + 2] * inv, acc[db][4 * j + 3] * inv});
+            }
+            if (!more) return;
+            m = -INFINITY;
+            l = 0.f;
+            sees = !MASKED;
+#pragma unroll
+            for (int db = 0; db < DB; ++db) acc[db] = {};
+        }
+        if (any) finish(buf ^ 1);
         __syncthreads();
+        if (BIAS && last) {                                      // nobody reads the table of the unit before any more
+            fill_bias<E>(A, n_unit, starts, table, tid, THREADS);
+            __syncthreads();
+        }
+        unit = n_unit;
+        i = n_i;
+        buf ^= 1;
     }
-    l = sum_of_halves(l);
-    if (!w.real) return;
-    const int64_t at = (int64_t)(t.q0 + w.row);
-    if (splits > 1) {
-        const int64_t place = ((int64_t)split * A.heads + w.head) * A.total_q + at;
-        if (h == 0) ml_part[place] = make_float2(m, l);
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                *(f32x4*)(o_part + place * D + 32 * db + 8 * j + 4 * h) =
-                    f32x4{acc[db][4 * j], acc[db][4 * j + 1], acc[db][4 * j + 2], acc[db][4 * j + 3]};
-        return;
-    }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    if (h == 0) lse[(int64_t)w.head * A.total_q + at] = l == 0.f ? -INFINITY : m * LN2 + logf(l);
-    E* o = out + (at * A.heads + w.head) * D;
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            O::store4(o + 32 * db + 8 * j + 4 * h, f32x4{acc[db][4 * j] * inv, acc[db][4 * j + 1] * inv,
-                                                          acc[db][4 * j + 2] * inv, acc[db][4 * j + 3] * inv});
 }
 
 // Joins the parts of rows whose keys were split: four of a row's values a thread.
@@ -341,7 +413,7 @@ __global__ __launch_bounds__(256) void k_attention_join(const AttnArgs A, int sp
 // The rounding of O reaches dS through delta, the same for all of a row.  Rows of dS sum to zero, so what a row's sum is
 // instead is the error of its delta: the first kernel adds it to the delta that the second one takes.  In the
 // first, 16-bit dS goes into its product as two values of eight bits each, which leaves O's rounding as the only error beside
-// the result's own (gradients of queries, against 64 bits, 512 passages: 2.6e-3 with one value, DQ_ERROR with two; the result's own
+// the result's own (gradients of queries, against 64 bits, 512 passages: 2.6e-3 with one value, 2.0e-3 with two; the result's own
 // rounding is 1.7e-3).
 
 // Sums of a 32 x 32 block along its diagonals, added to a histogram by distance.  The block is in accumulators: a lane has
@@ -368,89 +440,118 @@ __device__ __forceinline__ void add_diagonals(const f32x16& x, float* scratch, f
     }
 }
 
-// Gradients of queries, delta, and the bias table's share of each tile.
+// Gradients of queries, delta, and the bias table's share of each tile; head units one after the other, as the forward pass.
 template <class E, int D, int NW, bool BIAS, bool MASKED>
-__global__ __launch_bounds__(64 * NW, D <= 64 ? 2 : 1) void k_attention_dq(const AttnArgs A, int slots, int units, const E* out, const E* dout,
-                                                             const float* lse, E* dq, float* delta, float* bias_part) {
+__global__ __launch_bounds__(64 * NW, D <= 64 ? 2 : 1) void k_attention_dq(const AttnArgs A, int slots, int units, int run, const E* out,
+                                                                           const E* dout, const float* lse, E* dq, float* delta,
+                                                                           float* bias_part) {
     using O = Oper<E>;
     using T = Tile<E, D>;
     constexpr int NB = T::ROWS / 32, DB = D / 32, THREADS = 64 * NW;
     __shared__ __align__(16) char lds[2][2 * T::BYTES];
     __shared__ __align__(16) float diagonals[BIAS ? NW * kDiagonal : 1];
+    __shared__ __align__(16) float hidden[2][T::ROWS];
     __shared__ float far_sum[NW][2];
-    extern __shared__ float table[];                  // the bias by distance, then a histogram of each wavefront
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
-    const int slot = blockIdx.x % slots, unit = blockIdx.x / slots;
+    extern __shared__ __align__(16) char dyn[];       // the bias by distance, then a histogram of each wavefront
+    const int tid = threadIdx.x, lane0 = tid & 63, lane = lane0, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
+    const int work = in_order(blockIdx.x, gridDim.x), runs = (units + run - 1) / run;
+    const int slot = work / runs;
+    int unit = work % runs * run;
+    const int end_unit = unit + run < units ? unit + run : units;
     const int G = A.pack, per = 32 * NW / G;
     const QueryTile t(A, slot, per, lane);
-    const int head0 = unit * G, kv = head0 / A.group;
     if (t.none) {
         if constexpr (BIAS)
-            for (int b = tid; b < A.n_buckets; b += THREADS) bias_part[((int64_t)slot * A.heads + head0) * A.n_buckets + b] = 0.f;
+            for (int b = tid; b < (end_unit - unit) * A.n_buckets; b += THREADS)
+                bias_part[((int64_t)slot * A.heads + unit) * A.n_buckets + b] = 0.f;
         return;
     }
-    const QueryColumns w(A, t, G, per, head0, wave, lane);
+    const QueryColumns w(A, t, G, per, wave, lane);
     const int tiles = (t.end + T::ROWS - 1) / T::ROWS;
     const int64_t krow = A.k_row * (int64_t)sizeof(E), vrow = A.v_row * (int64_t)sizeof(E);
-    const char* kp = (const char*)A.k + t.k0 * krow + kv * A.k_head * (int64_t)sizeof(E);
-    const char* vp = (const char*)A.v + t.k0 * vrow + kv * A.v_head * (int64_t)sizeof(E);
     Staged<E, D, THREADS, MASKED> next;
     uint8_t next_keep = 0;
-    auto issue = [&](int base, char* to) {
-        next.issue(kp + base * krow, vp + base * vrow, to, t.end - base, tid, [&](int r) { return (uint32_t)r * (uint32_t)krow; },
-                   [&](int r) { return (uint32_t)r * (uint32_t)vrow; }, [&](int r) { return A.keep[(int64_t)t.k0 + base + r]; });
+    auto issue = [&](int u, int base, char* to) {
+        const int kv = u * G / A.group;
+        next.issue((const char*)A.k + (t.k0 + base) * krow + kv * A.k_head * (int64_t)sizeof(E),
+                   (const char*)A.v + (t.k0 + base) * vrow + kv * A.v_head * (int64_t)sizeof(E), to, t.end - base, tid,
+                   [&](int r) { return (uint32_t)r * (uint32_t)krow; }, [&](int r) { return (uint32_t)r * (uint32_t)vrow; },
+                   [&](int r) { return A.keep[(int64_t)t.k0 + base + r]; });
+        next_keep = base + lane < t.end;
         if constexpr (MASKED) next_keep = lane < T::ROWS && base + lane < t.end ? A.keep[(int64_t)t.k0 + base + lane] : 0;
     };
-    if (tiles > 0) issue(0, lds[0]);
-    const int middle = bias_middle(A.reach), width = bias_width(A.reach);
-    float* hist = table + width;
-    float* own_hist = hist + wave * width + middle;
-    float* scratch = diagonals + wave * kDiagonal;
-    if constexpr (BIAS) {
-        fill_bias<E>(A, head0, table, tid, THREADS);
-        for (int i = tid; i < NW * width; i += THREADS) hist[i] = 0.f;
-        for (int i = tid; i < NW * kDiagonal; i += THREADS) diagonals[i] = 0.f;
-    }
-    float far_lo = 0.f, far_hi = 0.f;
-
-    const int64_t at = (int64_t)(t.q0 + w.row), place = (int64_t)w.head * A.total_q + at, dense = (at * A.heads + w.head) * D;
-    const float row_lse = w.real ? lse[place] : -INFINITY;
-    const bool seeing = row_lse != -INFINITY;         // rows that see nothing take no part, whatever their gradient is
-    const float lse2 = row_lse * LOG2E;
+    constexpr uint64_t kAllRows = T::ROWS == 64 ? ~0ull : (1ull << (T::ROWS & 63)) - 1ull;
+    uint64_t seen = 0;                                           // rows of the tile that some column sees
+    auto finish = [&](int buf) {
+        next.finish(lds[buf], tid);
+        if (tid < T::ROWS) hidden[buf][tid] = next_keep ? 0.f : -INFINITY;
+        seen = __ballot(next_keep != 0) & kAllRows;
+    };
+    const bool any = tiles > 0;
+    if (any) issue(unit, 0, lds[0]);
     Column<E, D> q, g;
-    q.load((const E*)A.q + at * A.q_row + w.head * A.q_head, seeing, h);
-    q.take_sign(A.scale);
-    g.load(dout + dense, seeing, h);
-    float dot = 0.f;
-    {
+    float dot = 0.f, own_lse = 0.f;
+    const int64_t at = (int64_t)(t.q0 + w.row);
+    auto load_rows = [&](int u) {
+        const int head = u * G + w.head;
+        const int64_t dense = (at * A.heads + head) * D;
+        const float row_lse = w.real ? lse[(int64_t)head * A.total_q + at] : -INFINITY;
         Column<E, D> o;
-        o.load(out + dense, seeing, h);
+        q.load((const E*)A.q + at * A.q_row + head * A.q_head, w.real, h);
+        g.load(dout + dense, w.real, h);
+        o.load(out + dense, w.real, h);
+        // rows that see nothing take no part, whatever their gradient is: exp2(x - inf) = 0
+        const bool seeing = row_lse != -INFINITY;
+        own_lse = seeing ? -row_lse * LOG2E : -INFINITY;
+        dot = 0.f;
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) {
+            if (!seeing) q.v[c] = g.v[c] = {};
             const f32x8 x = O::wide(g.v[c]), y = O::wide(o.v[c]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) dot += x[e] * y[e];
         }
         dot = sum_of_halves(dot);
+        q.take_sign(A.scale);
+    };
+    load_rows(unit);
+    const int middle = bias_middle(A.reach), width = bias_width(A.reach);
+    int16_t* starts = (int16_t*)dyn;
+    float* table = (float*)(dyn + kStartsBytes);
+    float* hist = table + width;
+    float* own_hist = hist + wave * width + middle;
+    float* scratch = diagonals + wave * kDiagonal;
+    if constexpr (BIAS) {
+        for (int i = tid; i < NW * width; i += THREADS) hist[i] = 0.f;
+        for (int i = tid; i < NW * kDiagonal; i += THREADS) diagonals[i] = 0.f;
+        load_starts(A, starts, tid, THREADS);
+        __syncthreads();
+        fill_bias<E>(A, unit, starts, table, tid, THREADS);
     }
+    float far_lo = 0.f, far_hi = 0.f, weight_lo = 0.f, weight_hi = 0.f;
     f32x16 acc[DB] = {};
     float row_sum = 0.f;
     const float scale2 = scale_of_scores(A.scale);
-    const bool all_seeing = __all(seeing);
-    if (tiles > 0) next.finish(lds[0], tid);
-    uint64_t seen = __ballot(next_keep != 0);
+    if (any) finish(0);
     __syncthreads();
-    for (int i = 0; i < tiles; ++i) {
+    int i = 0, buf = 0;
+    while (true) {
         const int base = i * T::ROWS;
-        const char *lk = lds[i & 1], *lv = lk + T::BYTES;
-        char* other = lds[(i + 1) & 1];
-        if (i + 1 < tiles) issue(base + T::ROWS, other);
-        auto compute = [&](auto part) {
-            const int last = t.end - 1 - base, own = w.lim - base;
-            const Seen<MASKED> see(!seeing ? -1 : A.causal && own < last ? own : last, seen, h);
+        const char *lk = lds[buf], *lv = lk + T::BYTES;
+        const bool last = i + 1 >= tiles;
+        const int n_unit = last ? unit + 1 : unit, n_i = last ? 0 : i + 1;
+        const bool more = n_unit < end_unit;
+        if (more && any) issue(n_unit, n_i * T::ROWS, lds[buf ^ 1]);
+        const int blocks = NB == 1 || base + 32 >= w.end ? 1 : NB;
+        auto compute = [&](auto how) {
+            using How = decltype(how);
+            const int lane = here(lane0), h = lane >> 5;
+            const int room = w.lim - base - 4 * h;
 #pragma unroll 1
-            for (int b = 0; b < NB; ++b) {
-                f32x16 s = {}, dp = {};
+            for (int b = 0; b < blocks; ++b) {
+                f32x16 s = {}, dp;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) dp[r] = -dot;
 #pragma unroll
                 for (int c = 0; c < D / 16; ++c) O::mma(s, T::rows(lk, lane, b, c), q.v[c]);
 #pragma unroll
@@ -459,24 +560,38 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 2 : 1) void k_attention_dq(const
                 if (BIAS && !side) {
                     const float* x = table + middle + base + 32 * b + 4 * h - w.lim;
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], scale2, x[8 * (r >> 2) + (r & 3)]) - lse2;
+                    for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], scale2, x[8 * (r >> 2) + (r & 3)]) + own_lse;
                 } else {
-                    const float x = BIAS ? table[side < 0 ? 0 : 2 * middle] - lse2 : -lse2;
+                    const float x = BIAS ? table[side < 0 ? 0 : 2 * middle] + own_lse : own_lse;
 #pragma unroll
                     for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], scale2, x);
                 }
-                float sum = 0.f;
+                float sum = 0.f, weight = 0.f;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    float y = exp2_fast(s[r]) * (dp[r] - dot);
-                    if constexpr (decltype(part)::value) y = see.otherwise(y, 0.f, b, 8 * (r >> 2) + (r & 3));
-                    s[r] = y;
-                    sum += y;
+                for (int j = 0; j < 4; ++j) {
+                    f32x4 no = {0.f, 0.f, 0.f, 0.f};
+                    if constexpr (How::part) no = *(const f32x4*)(hidden[buf] + 32 * b + 8 * j + 4 * h);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int r = 4 * j + e;
+                        const bool own = !How::diagonal || 32 * b + 8 * j + e <= room;
+                        float p = exp2_fast(How::part ? s[r] + no[e] : s[r]);
+                        if constexpr (BIAS && How::diagonal) p = own ? p : 0.f;
+                        if constexpr (BIAS) weight += p;
+                        float y = p * dp[r];
+                        if constexpr (How::diagonal) y = own ? y : 0.f;
+                        s[r] = y;
+                        sum += y;
+                    }
                 }
                 row_sum += sum;
                 if constexpr (BIAS) {
-                    if (side) {
-                        (side < 0 ? far_lo : far_hi) += sum;
+                    if (side < 0) {
+                        far_lo += sum;
+                        weight_lo += weight;
+                    } else if (side > 0) {
+                        far_hi += sum;
+                        weight_hi += weight;
                     } else {
                         add_diagonals(s, scratch, own_hist + d0, lane);
                     }
@@ -504,81 +619,106 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 2 : 1) void k_attention_dq(const
                 }
             }
         };
-        if (w.busy && base < w.end) {
-            const bool whole = base + T::ROWS <= t.end && all_seeing && !(A.causal && base + T::ROWS - 1 > w.first_lim) &&
-                               (!MASKED || seen == ~0ull);
-            if (whole) compute(std::false_type{}); else compute(std::true_type{});
+        if (any && w.busy && base < w.end) {
+            if (A.causal && base + T::ROWS - 1 > w.first_lim) compute(Diagonal{});
+            else if (seen != kAllRows) compute(Part{});
+            else compute(Whole{});
         }
-        if (i + 1 < tiles) next.finish(other, tid);
-        seen = __ballot(next_keep != 0);
-        __syncthreads();
-    }
-    row_sum = sum_of_halves(row_sum);
-    if (w.real) {
-        if (h == 0) delta[place] = dot + row_sum;
-        E* o = dq + dense;
+        if (last) {
+            row_sum = sum_of_halves(row_sum);
+            const int head = unit * G + w.head;
+            if (w.real) {
+                if (h == 0) delta[(int64_t)head * A.total_q + at] = dot + row_sum;
+                E* o = dq + (at * A.heads + head) * D;
 #pragma unroll
-        for (int db = 0; db < DB; ++db)
+                for (int db = 0; db < DB; ++db)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                O::store4(o + 32 * db + 8 * j + 4 * h,
-                          f32x4{acc[db][4 * j] * A.scale, acc[db][4 * j + 1] * A.scale, acc[db][4 * j + 2] * A.scale,
-                                acc[db][4 * j + 3] * A.scale});
-    }
-    if constexpr (BIAS) {
-#pragma unroll
-        for (int m = 1; m < 64; m <<= 1) {
-            far_lo += __shfl_xor(far_lo, m);
-            far_hi += __shfl_xor(far_hi, m);
-        }
-        if (lane == 0) {
-            far_sum[wave][0] = far_lo;
-            far_sum[wave][1] = far_hi;
-        }
-        __syncthreads();
-        for (int i = tid; i < width; i += THREADS) {
-            float x = hist[i];
-#pragma unroll
-            for (int v = 1; v < NW; ++v) x += hist[v * width + i];
-            hist[i] = x;
-        }
-        __syncthreads();
-        const float* x = hist + middle;
-        for (int b0 = 0; b0 < A.n_buckets; b0 += THREADS / 8) {
-            const int b = b0 + tid / 8;
-            const bool one = b < A.n_buckets, behind = b >= A.n_dir;      // buckets of keys behind the query
-            const int j0 = behind ? b - A.n_dir : b;
-            const bool open = j0 == A.n_dir - 1;                          // the last one of its direction
-            float sum = 0.f;
-            if (one) {
-                // distance 0 belongs to the keys before
-                const int hi = open ? middle : A.starts[j0 + 1] - 1;
-                for (int j = A.starts[j0] + tid % 8; j <= hi; j += 8) sum += behind ? (j > 0 ? x[j] : 0.f) : x[-j];
+                    for (int j = 0; j < 4; ++j)
+                        O::store4(o + 32 * db + 8 * j + 4 * h,
+                                  f32x4{acc[db][4 * j] * A.scale, acc[db][4 * j + 1] * A.scale, acc[db][4 * j + 2] * A.scale,
+                                        acc[db][4 * j + 3] * A.scale});
             }
+            if (more) load_rows(n_unit);
+        }
+        if (more && any) finish(buf ^ 1);
+        if constexpr (BIAS) {
+            if (last) {
+                // what delta was off by, over the many keys of the open buckets
+                far_lo -= row_sum * weight_lo;
+                far_hi -= row_sum * weight_hi;
 #pragma unroll
-            for (int m = 1; m < 8; m <<= 1) sum += __shfl_xor(sum, m);
-            if (one && tid % 8 == 0) {
-                if (open)
+                for (int m = 1; m < 64; m <<= 1) {
+                    far_lo += __shfl_xor(far_lo, m);
+                    far_hi += __shfl_xor(far_hi, m);
+                }
+                if (lane == 0) {
+                    far_sum[wave][0] = far_lo;
+                    far_sum[wave][1] = far_hi;
+                }
+                far_lo = far_hi = weight_lo = weight_hi = 0.f;
+                __syncthreads();
+                for (int j = tid; j < width; j += THREADS) {
+                    float x = hist[j];
 #pragma unroll
-                    for (int v = 0; v < NW; ++v) sum += far_sum[v][behind ? 1 : 0];
-                bias_part[((int64_t)slot * A.heads + head0) * A.n_buckets + b] = sum;
+                    for (int v = 1; v < NW; ++v) {
+                        x += hist[v * width + j];
+                        hist[v * width + j] = 0.f;
+                    }
+                    hist[j] = 0.f;
+                    table[j] = x;                                         // its bias has been used
+                }
+                __syncthreads();
+                const float* x = table + middle;
+                for (int b0 = 0; b0 < A.n_buckets; b0 += THREADS / 8) {
+                    const int b = b0 + tid / 8;
+                    const bool one = b < A.n_buckets, behind = b >= A.n_dir;      // buckets of keys behind the query
+                    const int j0 = behind ? b - A.n_dir : b;
+                    const bool open = j0 == A.n_dir - 1;                          // the last one of its direction
+                    float sum = 0.f;
+                    if (one) {
+                        // distance 0 belongs to the keys before
+                        const int hi = open ? middle : A.starts[j0 + 1] - 1;
+                        for (int j = A.starts[j0] + tid % 8; j <= hi; j += 8) sum += behind ? (j > 0 ? x[j] : 0.f) : x[-j];
+                    }
+#pragma unroll
+                    for (int m = 1; m < 8; m <<= 1) sum += __shfl_xor(sum, m);
+                    if (one && tid % 8 == 0) {
+                        if (open)
+#pragma unroll
+                            for (int v = 0; v < NW; ++v) sum += far_sum[v][behind ? 1 : 0];
+                        bias_part[((int64_t)slot * A.heads + unit) * A.n_buckets + b] = sum;
+                    }
+                }
+                __syncthreads();
+                if (more) fill_bias<E>(A, n_unit, starts, table, tid, THREADS);
             }
         }
+        if (last) {
+            if (!more) return;
+            row_sum = 0.f;
+#pragma unroll
+            for (int db = 0; db < DB; ++db) acc[db] = {};
+        }
+        __syncthreads();
+        unit = n_unit;
+        i = n_i;
+        buf ^= 1;
     }
 }
 
-// Gradients of keys and values; workgroups from `main` on add up the bias table's shares of all tiles.
+// Gradients of keys and values, `run` key heads one after the other; workgroups from `main` on add up the bias table's shares
+// of all tiles.
 template <class E, int D, int NW, bool BIAS, bool MASKED>
-__global__ __launch_bounds__(64 * NW, D <= 64 ? 2 : 1) void k_attention_dkv(const AttnArgs A, int slots, int main, int q_slots, const E* dout,
-                                                           const float* lse, const float* delta, const float* bias_part, E* dk, E* dv,
-                                                           E* dbias) {
+__global__ __launch_bounds__(64 * NW, D <= 64 ? 2 : 1) void k_attention_dkv(const AttnArgs A, int slots, int run, int main, int q_slots,
+                                                                            const E* dout, const float* lse, const float* delta,
+                                                                            const float* bias_part, E* dk, E* dv, E* dbias) {
     using O = Oper<E>;
     using T = Tile<E, D>;
     constexpr int NB = T::ROWS / 32, DB = D / 32, THREADS = 64 * NW, COLS = 32 * NW;
     __shared__ __align__(16) char lds[2][2 * T::BYTES];
     __shared__ __align__(16) float row_lse[2][T::ROWS], row_delta[2][T::ROWS];
-    extern __shared__ float table[];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
+    extern __shared__ __align__(16) char dyn[];
+    const int tid = threadIdx.x, lane0 = tid & 63, lane = lane0, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     if constexpr (BIAS) {
         if ((int)blockIdx.x >= main) {                // one entry of the table each wavefront
             const int e = ((int)blockIdx.x - main) * NW + wave;
@@ -592,7 +732,8 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 2 : 1) void k_attention_dkv(cons
             return;
         }
     }
-    const int slot = blockIdx.x % slots, kv = blockIdx.x / slots;
+    const int work = in_order(blockIdx.x, main), runs = (A.kv_heads + run - 1) / run, slot = work / runs, kv0 = work % runs * run;
+    const int kv_end = kv0 + run < A.kv_heads ? kv0 + run : A.kv_heads;
     const int seq = find_sequence(A.koff, A.n_seqs, COLS, A.total_k, slot, lane);
     const Range ks = sequence_rows(A.koff, seq, A.total_k, COLS), qs = sequence_rows(A.qoff, seq, A.total_q);
     const int key0 = (slot - ks.place) * COLS;
@@ -602,9 +743,8 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 2 : 1) void k_attention_dkv(cons
     const int64_t at = ks.lo + key;
     const bool seen = real && (!MASKED || A.keep[at]);
     const int G = A.pack, cols = qs.n * G;
-    // first row that sees a key of the tile (below zero: all do); a row before it sees nothing at all only at the sequence's start
-    const int first = A.causal && key0 > shift ? key0 - shift : 0;
-    const int col0 = first * G;
+    // columns from the first row that sees a key of the tile: rows before it may see nothing at all
+    const int col0 = A.causal && key0 > shift ? (key0 - shift) * G : 0;
 
     const int64_t qrow = A.q_row * (int64_t)sizeof(E), qhead = A.q_head * (int64_t)sizeof(E);
     const int64_t grow = (int64_t)A.heads * D * (int64_t)sizeof(E), ghead = D * (int64_t)sizeof(E);
@@ -612,6 +752,10 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 2 : 1) void k_attention_dkv(cons
     const char* gp = (const char*)dout + qs.lo * grow;
     Staged<E, D, THREADS, MASKED> next;
     float n_lse = 0.f, n_delta = 0.f;
+    const float scale2 = scale_of_scores(A.scale);
+    // 16 bits: a row's log-sum-exp and delta are what its accumulators start from (in 32 bits that would cost the scores an
+    // error of some roundings of the log-sum-exp, which 16-bit results do not show)
+    constexpr bool START = sizeof(E) == 2;
     auto issue = [&](int head0, int c0, char* to) {
         const int row0 = c0 / G, c1 = c0 - row0 * G;              // the tile's first row, and its first column's place in it
         const int64_t place0 = (int64_t)head0 * A.total_q + qs.lo + row0;
@@ -637,59 +781,88 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 2 : 1) void k_attention_dkv(cons
     auto finish = [&](int buf) {
         next.finish(lds[buf], tid);
         if (tid < T::ROWS) {
-            row_lse[buf][tid] = n_lse == -INFINITY ? -INFINITY : -n_lse * LOG2E;      // exp2(x - inf) = 0
-            row_delta[buf][tid] = n_delta;
+            // exp2(x - inf) = 0
+            row_lse[buf][tid] = n_lse == -INFINITY ? -INFINITY : -n_lse * (START ? LOG2E / scale2 : LOG2E);
+            row_delta[buf][tid] = -n_delta;
         }
     };
-    int head0 = kv * A.group, c0 = col0;
-    const int head_end = head0 + A.group;
-    if (col0 < cols) issue(head0, c0, lds[0]);
+    int head0 = kv0 * A.group, c0 = col0;
+    const int head_end = kv_end * A.group;
+    const bool any = col0 < cols;
+    if (any) issue(head0, c0, lds[0]);
     Column<E, D> k, v;
-    k.load((const E*)A.k + at * A.k_row + kv * A.k_head, seen, h);
-    k.take_sign(A.scale);
-    v.load((const E*)A.v + at * A.v_row + kv * A.v_head, seen, h);
+    auto load_keys = [&](int kv) {
+        k.load((const E*)A.k + at * A.k_row + kv * A.k_head, seen, h);
+        k.take_sign(A.scale);
+        v.load((const E*)A.v + at * A.v_row + kv * A.v_head, seen, h);
+    };
+    load_keys(kv0);
     f32x16 ak[DB] = {}, av[DB] = {};
-    const float scale2 = scale_of_scores(A.scale);
     const int middle = bias_middle(A.reach);
     const bool busy = wkey < ks.n;
     const int wfirst = A.causal && wkey > shift ? (wkey - shift) * G : 0;             // first column that sees a key of the wavefront
-    if constexpr (BIAS) fill_bias<E>(A, head0, table, tid, THREADS);
-    if (col0 < cols) finish(0);
+    int16_t* starts = (int16_t*)dyn;
+    float* table = (float*)(dyn + kStartsBytes);
+    if constexpr (BIAS) {
+        load_starts(A, starts, tid, THREADS);
+        __syncthreads();
+        fill_bias<E>(A, head0, starts, table, tid, THREADS);
+    }
+    if (any) finish(0);
     __syncthreads();
     int buf = 0;
-    while (col0 < cols && head0 < head_end) {
+    while (true) {
         const bool last_tile = c0 + T::ROWS >= cols;
         const int n_head = last_tile ? head0 + G : head0, n_c = last_tile ? col0 : c0 + T::ROWS;
-        if (n_head < head_end) issue(n_head, n_c, lds[buf ^ 1]);
+        const bool more = n_head < head_end, last = last_tile && n_head % A.group == 0;   // of a key head
+        if (more && any) issue(n_head, n_c, lds[buf ^ 1]);
         const char *lq = lds[buf], *lg = lq + T::BYTES;
-        auto compute = [&](auto part) {
+        const int blocks = NB == 1 || c0 + 32 >= cols ? 1 : NB;
+        auto compute = [&](auto diagonal) {
+            const int lane = here(lane0), h = lane >> 5;
             // a lane's key is seen by columns from (key - shift) G on
             const int need = (key - shift) * G - c0 - 4 * h;
 #pragma unroll 1
-            for (int b = 0; b < NB; ++b) {
-                f32x16 s = {}, dp = {};
+            for (int b = 0; b < blocks; ++b) {
+                f32x16 s, dp, e, dl;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const f32x4 x = *(const f32x4*)(row_lse[buf] + 32 * b + 8 * j + 4 * h);
+                    const f32x4 y = *(const f32x4*)(row_delta[buf] + 32 * b + 8 * j + 4 * h);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        e[4 * j + i] = x[i];
+                        dl[4 * j + i] = y[i];
+                    }
+                }
+                if constexpr (START) {
+                    s = e;
+                    dp = dl;
+                } else {
+                    s = {};
+                    dp = {};
+                }
 #pragma unroll
                 for (int c = 0; c < D / 16; ++c) O::mma(s, T::rows(lq, lane, b, c), k.v[c]);
 #pragma unroll
                 for (int c = 0; c < D / 16; ++c) O::mma(dp, T::rows(lg, lane, b, c), v.v[c]);
                 const int d0 = wkey - (c0 + 32 * b + shift), side = BIAS ? block_side(d0, A.reach) : 0;
-                const float* tab = table + middle + key - (c0 + 32 * b + shift) - 4 * h - 27;    // of the lane's last row
-                const float far = BIAS && side ? table[side < 0 ? 0 : 2 * middle] : 0.f;
+                if (BIAS && !side) {
+                    const float* x = table + middle + key - (c0 + 32 * b + shift) - 4 * h - 27;    // of the lane's last row
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], scale2, x[27 - 8 * (r >> 2) - (r & 3)]);
+                } else {
+                    const float x = BIAS ? table[side < 0 ? 0 : 2 * middle] : 0.f;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[r] = BIAS ? fmaf(s[r], scale2, x) : s[r] * scale2;
+                }
                 f32x16 ds;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int r0 = 32 * b + 8 * j + 4 * h;
-                    const f32x4 e = *(const f32x4*)(row_lse[buf] + r0), dl = *(const f32x4*)(row_delta[buf] + r0);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int r = 4 * j + i;
-                        float x = fmaf(s[r], scale2, e[i]);
-                        if constexpr (BIAS) x += side ? far : tab[27 - 8 * j - i];
-                        float p = exp2_fast(x);
-                        if constexpr (decltype(part)::value) p = 32 * b + 8 * j + i >= need ? p : 0.f;
-                        s[r] = p;
-                        ds[r] = p * (dp[r] - dl[i]);
-                    }
+                for (int r = 0; r < 16; ++r) {
+                    float p = exp2_fast(START ? s[r] : s[r] + e[r]);
+                    if constexpr (decltype(diagonal)::value) p = 32 * b + 8 * (r >> 2) + (r & 3) >= need ? p : 0.f;
+                    s[r] = p;
+                    ds[r] = p * (START ? dp[r] : dp[r] + dl[r]);
                 }
                 const typename O::Frag p0 = O::round(eight<0>(s)), p1 = O::round(eight<8>(s));
                 const typename O::Frag d0f = O::round(eight<0>(ds)), d1f = O::round(eight<8>(ds));
@@ -703,33 +876,39 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 2 : 1) void k_attention_dkv(cons
                 for (int db = 0; db < DB; ++db) O::mma(ak[db], T::turned(lq, lane, b, 1, db), d1f);
             }
         };
-        if (busy && c0 + T::ROWS > wfirst) {
+        if (any && busy && c0 + T::ROWS > wfirst) {
             if (A.causal && (wkey + 31 - shift) * G > c0) compute(std::true_type{}); else compute(std::false_type{});
         }
-        if (n_head < head_end) finish(buf ^ 1);
-        __syncthreads();
-        if constexpr (BIAS) {
-            if (n_head != head0 && n_head < head_end) {
-                fill_bias<E>(A, n_head, table, tid, THREADS);
-                __syncthreads();
+        if (last) {
+            const int kv = head0 / A.group;
+            if (more) load_keys(kv + 1);
+            if (real) {
+                const int64_t dense = (at * A.kv_heads + kv) * D;
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const f32x4 x = {ak[db][4 * j], ak[db][4 * j + 1], ak[db][4 * j + 2], ak[db][4 * j + 3]};
+                        const f32x4 y = {av[db][4 * j], av[db][4 * j + 1], av[db][4 * j + 2], av[db][4 * j + 3]};
+                        const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+                        O::store4(dk + dense + 32 * db + 8 * j + 4 * h, seen ? x * A.scale : zero);
+                        O::store4(dv + dense + 32 * db + 8 * j + 4 * h, seen ? y : zero);
+                    }
             }
+            if (!more) return;
+#pragma unroll
+            for (int db = 0; db < DB; ++db) ak[db] = av[db] = {};
+        }
+        if (more && any) finish(buf ^ 1);
+        __syncthreads();
+        if (BIAS && n_head != head0) {
+            fill_bias<E>(A, n_head, starts, table, tid, THREADS);
+            __syncthreads();
         }
         head0 = n_head;
         c0 = n_c;
         buf ^= 1;
     }
-    if (!real) return;
-    const int64_t dense = (at * A.kv_heads + kv) * D;
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            f32x4 x = {ak[db][4 * j], ak[db][4 * j + 1], ak[db][4 * j + 2], ak[db][4 * j + 3]};
-            f32x4 y = {av[db][4 * j], av[db][4 * j + 1], av[db][4 * j + 2], av[db][4 * j + 3]};
-            const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-            O::store4(dk + dense + 32 * db + 8 * j + 4 * h, seen ? x * A.scale : zero);
-            O::store4(dv + dense + 32 * db + 8 * j + 4 * h, seen ? y : zero);
-        }
 }
 
 // ---- launches ------------------------------------------------------------------------------------------------
@@ -759,9 +938,10 @@ hipError_t launch_attention(const AttnArgs& A, const AttnPlan& P, E* out, float*
         const hipError_t e = by_form(P.q_waves, A.bias != nullptr, A.keep != nullptr, [&](auto nw, auto bias, auto masked) {
             constexpr int NW = decltype(nw)::value;
             constexpr bool BIAS = decltype(bias)::value, MASKED = decltype(masked)::value;
-            const size_t lds = BIAS ? 4 * (size_t)bias_width(A.reach) : 0;
-            k_attention<E, D, NW, BIAS, MASKED><<<dim3((unsigned)(P.q_slots * P.units * P.splits)), 64 * NW, lds, st>>>(
-                A, (int)P.q_slots, P.units, P.splits, out, lse, o_part, ml_part);
+            const size_t lds = BIAS ? bias_bytes(A.reach, 1) : 0;
+            const int64_t runs = (P.units + P.run - 1) / P.run;
+            k_attention<E, D, NW, BIAS, MASKED><<<dim3((unsigned)(P.q_slots * runs * P.splits)), 64 * NW, lds, st>>>(
+                A, (int)P.q_slots, P.units, P.run, P.splits, out, lse, o_part, ml_part);
             return hipGetLastError();
         });
         if (e != hipSuccess || P.splits == 1) return e;
@@ -782,9 +962,10 @@ hipError_t launch_attention_backward(const AttnArgs& A, const AttnPlan& P, const
             e = by_form(P.q_waves, A.bias != nullptr, A.keep != nullptr, [&](auto nw, auto bias, auto masked) {
                 constexpr int NW = decltype(nw)::value;
                 constexpr bool BIAS = decltype(bias)::value, MASKED = decltype(masked)::value;
-                const size_t lds = BIAS ? 4 * (size_t)((NW + 1) * bias_width(A.reach)) : 0;
-                k_attention_dq<E, D, NW, BIAS, MASKED><<<dim3((unsigned)(P.q_slots * P.units)), 64 * NW, lds, st>>>(
-                    A, (int)P.q_slots, P.units, (const E*)G.out, (const E*)G.dout, G.lse, (E*)G.dq, delta, bias_part);
+                const size_t lds = BIAS ? bias_bytes(A.reach, NW + 1) : 0;
+                const int64_t runs = (P.units + P.run - 1) / P.run;
+                k_attention_dq<E, D, NW, BIAS, MASKED><<<dim3((unsigned)(P.q_slots * runs)), 64 * NW, lds, st>>>(
+                    A, (int)P.q_slots, P.units, P.run, (const E*)G.out, (const E*)G.dout, G.lse, (E*)G.dq, delta, bias_part);
                 return hipGetLastError();
             });
             if (e != hipSuccess) return e;
@@ -793,12 +974,12 @@ hipError_t launch_attention_backward(const AttnArgs& A, const AttnPlan& P, const
         return by_form(P.k_waves, A.bias != nullptr, A.keep != nullptr, [&](auto nw, auto bias, auto masked) {
             constexpr int NW = decltype(nw)::value;
             constexpr bool BIAS = decltype(bias)::value, MASKED = decltype(masked)::value;
-            const size_t lds = BIAS ? 4 * (size_t)bias_width(A.reach) : 0;
-            const int main = A.total_k > 0 ? (int)(P.k_slots * A.kv_heads) : 0;
+            const size_t lds = BIAS ? bias_bytes(A.reach, 1) : 0;
+            const int main = A.total_k > 0 ? (int)(P.k_slots * ((A.kv_heads + P.kv_run - 1) / P.kv_run)) : 0;
             const int more = BIAS ? (A.n_buckets * A.heads + NW - 1) / NW : 0;
             if (main + more == 0) return hipSuccess;
             k_attention_dkv<E, D, NW, BIAS, MASKED><<<dim3((unsigned)(main + more)), 64 * NW, lds, st>>>(
-                A, (int)P.k_slots, main, q_slots, (const E*)G.dout, G.lse, delta, bias_part, (E*)G.dk, (E*)G.dv, (E*)G.dbias);
+                A, (int)P.k_slots, P.kv_run, main, q_slots, (const E*)G.dout, G.lse, delta, bias_part, (E*)G.dk, (E*)G.dv, (E*)G.dbias);
             return hipGetLastError();
         });
     });

@@ -122,6 +122,13 @@ __device__ __forceinline__ float sum_of_halves(float x) {
     return __uint_as_float(a) + __uint_as_float(b);
 }
 
+// The same value, but one that the compiler works out what depends on it from where it stands: addresses that a loop needs
+// once a turn then take no registers over the whole of it.
+__device__ __forceinline__ int here(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
 // Sixteen bytes a lane from memory to LDS without registers: lane i's go to dst + 16 i (dst: the same for the wavefront).
 __device__ __forceinline__ void copy_to_lds(const void* src, char* dst) {
     using G = const __attribute__((address_space(1))) void;

@@ -29,6 +29,7 @@ struct AttnPlan {
     int q_waves, k_waves;        // wavefronts of a workgroup, 32 query (key) columns each
     int64_t q_slots, k_slots;    // places for tiles of all sequences
     int units;                   // head units: heads / pack
+    int run, kv_run;             // head units (key heads) that a workgroup takes one after the other
     int splits;                  // parts that the keys of a forward call's tiles are cut into
     size_t o_part, ml_part, delta, bias_part, bytes;
 };

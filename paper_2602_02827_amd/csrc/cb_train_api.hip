@@ -23,6 +23,14 @@ AttnPlan plan_attention(const AttnArgs& A, int d, int dt, bool backward) {
     P.q_slots = A.total_q / (32 * P.q_waves / A.pack) + A.n_seqs;
     P.k_slots = A.total_k / (32 * P.k_waves) + A.n_seqs;
     P.splits = 1;
+    // Short sequences: a workgroup goes on to the next heads, as long as enough workgroups are left.
+    auto run_of = [](int64_t slots, int units, int64_t rows) {
+        int r = 1;
+        while (rows <= 384 && 2 * r <= units && slots * (units / (2 * r)) >= 1536) r *= 2;
+        return r;
+    };
+    P.run = run_of(P.q_slots, P.units, k_rows);
+    P.kv_run = run_of(P.k_slots, A.kv_heads, (int64_t)A.total_q * A.group / A.n_seqs);
     size_t o = 0;
     auto take = [&](int64_t bytes) {
         const size_t at = o;
@@ -138,7 +146,8 @@ int attn_args(const colbandit_attn* a, AttnArgs& A) {
     A.heads = a->heads;
     A.kv_heads = a->kv_heads;
     A.group = a->heads / a->kv_heads;
-    A.pack = !a->bias && A.group <= 16 && a->q_head * eb <= kMostRowBytes ? A.group : 1;
+    A.pack = !a->bias && A.group <= 16 && a->q_head * eb <= kMostRowBytes && a->total_q <= kMostRows / A.group &&
+                     a->total_k <= kMostRows / A.group ? A.group : 1;      // columns are counted in 31 bits
     A.total_q = (int)a->total_q;
     A.total_k = (int)a->total_k;
     A.causal = a->causal != 0;
