@@ -43,11 +43,12 @@ __device__ __forceinline__ void fill_bias(const AttnArgs& A, int head, const int
 constexpr int kStartsBytes = 272;                     // of up to 129
 __host__ __forceinline__ size_t bias_bytes(int reach, int tables) { return kStartsBytes + 4 * (size_t)(tables * bias_width(reach)); }
 
-// Workgroups are dealt to the eight XCDs in turn; numbered so that each XCD has consecutive ones, the tiles that share keys
-// read them through one L2.
+// Workgroups are dealt to the eight XCDs in turn; numbered so that each XCD has runs of consecutive ones (64, or as many as
+// leave each eight runs, so that long sequences are spread), the tiles that share keys read them through one L2.
 __device__ __forceinline__ int in_order(int block, int blocks) {
-    const int each = blocks >> 3, more = blocks & 7, xcd = block & 7;
-    return xcd * each + (xcd < more ? xcd : more) + (block >> 3);
+    const int lg = blocks < 128 ? 0 : blocks >= 4096 ? 6 : 25 - __builtin_clz(blocks);
+    const int whole = blocks >> (lg + 3) << (lg + 3), xcd = block & 7, i = block >> 3;
+    return block < whole ? (((i >> lg) * 8 + xcd) << lg) + (i & ((1 << lg) - 1)) : block;
 }
 // Which way a block of 32 rows and columns lies whose first key and row are d0 apart: -1 or 1: all beyond reach, 0: not.
 __device__ __forceinline__ int block_side(int d0, int reach) { return d0 + 31 <= -reach ? -1 : d0 - 31 >= reach ? 1 : 0; }
@@ -376,32 +377,56 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 3 : 2) void k_attention(const At
     }
 }
 
-// Joins the parts of rows whose keys were split: four of a row's values a thread.
+// Joins the parts of rows whose keys were split: a wavefront for each row and head, its lanes over the parts for their maximum, then
+// over the row's values, four each, and several parts at a time.
 template <class E, int D>
 __global__ __launch_bounds__(256) void k_attention_join(const AttnArgs A, int splits, const float* o_part, const float2* ml_part,
                                                         E* out, float* lse) {
-    constexpr int PER = D / 4;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t rows = (int64_t)A.heads * A.total_q, place = i / PER;
-    const int dim = (int)(i % PER) * 4;
+    constexpr int LANES = D / 4 <= 8 ? 8 : D / 4 <= 16 ? 16 : 32, PARTS = 64 / LANES, AHEAD = 4;
+    const int lane = threadIdx.x & 63;
+    const int64_t rows = (int64_t)A.heads * A.total_q, place = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (place >= rows) return;
     // rows that no sequence holds have no parts: they are not written by any call, nor is their output
     const int64_t row = place % A.total_q;
     if (row < A.qoff[0] || row >= A.qoff[A.n_seqs]) return;
     float m = -INFINITY;
-    for (int s = 0; s < splits; ++s) m = fmaxf(m, ml_part[s * rows + place].x);
+    for (int s = lane; s < splits; s += 64) m = fmaxf(m, ml_part[s * rows + place].x);
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) m = fmaxf(m, __shfl_xor(m, x));
     const float m_use = m == -INFINITY ? 0.f : m;
+    const int dim = lane % LANES * 4;
     float l = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < splits; ++s) {
-        const float2 ml = ml_part[s * rows + place];
-        if (ml.y == 0.f) continue;
-        const float w = exp2_fast(ml.x - m_use);
-        l += ml.y * w;
-        o += *(const f32x4*)(o_part + (s * rows + place) * D + dim) * w;
+    for (int s0 = lane / LANES; s0 < splits; s0 += PARTS * AHEAD) {
+        float2 ml[AHEAD];
+        f32x4 x[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            const int s = s0 + j * PARTS;
+            ml[j] = make_float2(-INFINITY, 0.f);
+            x[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (s < splits && dim < D) {
+                ml[j] = ml_part[s * rows + place];
+                x[j] = *(const f32x4*)(o_part + (s * rows + place) * D + dim);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            if (ml[j].y == 0.f) continue;
+            const float w = exp2_fast(ml[j].x - m_use);
+            l += ml[j].y * w;
+            o += x[j] * w;
+        }
     }
+#pragma unroll
+    for (int x = LANES; x < 64; x <<= 1) {
+        l += __shfl_xor(l, x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], x);
+    }
+    if (lane >= LANES || dim >= D) return;
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    if (dim == 0) lse[place] = l == 0.f ? -INFINITY : m * LN2 + logf(l);
+    if (lane == 0) lse[place] = l == 0.f ? -INFINITY : m * LN2 + logf(l);
     Oper<E>::store4(out + (row * A.heads + place / A.total_q) * D + dim, o * inv);
 }
 
@@ -945,8 +970,8 @@ hipError_t launch_attention(const AttnArgs& A, const AttnPlan& P, E* out, float*
             return hipGetLastError();
         });
         if (e != hipSuccess || P.splits == 1) return e;
-        const int64_t threads = (int64_t)A.heads * A.total_q * (D / 4);
-        k_attention_join<E, D><<<dim3((unsigned)((threads + 255) / 256)), 256, 0, st>>>(A, P.splits, o_part, ml_part, out, lse);
+        const int64_t rows = (int64_t)A.heads * A.total_q;
+        k_attention_join<E, D><<<dim3((unsigned)((rows + 3) / 4)), 256, 0, st>>>(A, P.splits, o_part, ml_part, out, lse);
         return hipGetLastError();
     });
 }

@@ -9,19 +9,33 @@ namespace cb {
 
 // ---- scores --------------------------------------------------------------------------------------------------
 // A workgroup keeps the rows of a few whole queries in registers, 32 * CT columns to a wavefront, and streams the tokens of
-// its documents through LDS.  A column's running maximum and its place stay in the column's two lanes.
+// its documents through LDS, the next tile on its way while it multiplies.  A column's running maximum and its place stay in the
+// column's two lanes; a comparison, and two selections of it, for every product (the place within a block is a constant).
 template <class E, int D, int CT>
-__global__ __launch_bounds__(256) void k_maxsim_train(const E* Q, int nq, int T, const E* docs, const int64_t* off, int N, int total,
-                                                      int col_groups, int q_per, int docs_per, float* scores, int32_t* argmax) {
+__global__ __launch_bounds__(256, 2) void k_maxsim_train(const E* Q, int nq, int T, const E* docs, const int64_t* off, int N, int total,
+                                                         int col_groups, int q_per, int docs_per, float* scores, int32_t* argmax) {
     using O = Oper<E>;
     using L = Tile<E, D>;
-    constexpr int NB = L::ROWS / 32, PIECES = L::ROWS * L::PIECES / 256;
-    __shared__ __align__(16) char tile[L::BYTES];
-    __shared__ float cells[128 * CT];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 31, h = lane >> 5;
+    constexpr int NB = L::ROWS / 32, COPIES = L::ROWS * L::PIECES / 256;
+    __shared__ __align__(16) char tile[2][L::BYTES];
+    __shared__ float cells[2][128 * CT];
+    const int tid = threadIdx.x, lane0 = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane0 & 31, h = lane0 >> 5;
     const int group = blockIdx.x % col_groups, part = blockIdx.x / col_groups;
     const int q0 = group * q_per, queries = nq - q0 < q_per ? nq - q0 : q_per, cols = queries * T;
     const int doc0 = part * docs_per, doc_end = N - doc0 < docs_per ? N : doc0 + docs_per;
+    auto issue = [&](const Range& r, int base, char* to) {
+        if (r.n == 0) return;
+        const int t = here(tid);
+        const char* src = (const char*)(docs + (int64_t)(r.lo + base) * D);
+        const int rows = r.n - base;
+#pragma unroll
+        for (int p = 0; p < COPIES; ++p) {
+            const int at = p * 256 + t, place = at / L::PIECES, row = place < rows ? place : rows - 1;
+            copy_to_lds(src + (uint32_t)(row * L::PITCH + (at % L::PIECES ^ L::turn(place)) * 16), to + (p * 256 + wave * 64) * 16);
+        }
+    };
+    Range r = sequence_rows(off, doc0, total);
+    issue(r, 0, tile[0]);
     typename O::Frag q[CT][D / 16];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
@@ -32,78 +46,84 @@ __global__ __launch_bounds__(256) void k_maxsim_train(const E* Q, int nq, int T,
             if (col < cols) q[ct][c] = O::load(Q + ((int64_t)q0 * T + col) * D + 16 * c + 8 * h);
         }
     }
-    for (int i = doc0; i < doc_end; ++i) {
-        const Range r = sequence_rows(off, i, total);
-        float best[CT];
-        int where[CT];
+    float best[CT];
+    int where[CT];
+    int i = doc0, base = 0, buf = 0;
+    wait_for_copies();
+    __syncthreads();
+    while (true) {
+        const bool first = base == 0, last = base + L::ROWS >= r.n;       // of the document
+        const int n_i = last ? i + 1 : i, n_base = last ? 0 : base + L::ROWS;
+        const bool more = n_i < doc_end;
+        const Range n_r = last && more ? sequence_rows(off, n_i, total) : r;
+        if (more) issue(n_r, n_base, tile[buf ^ 1]);
+        if (first) {
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-            best[ct] = -INFINITY;
-            where[ct] = r.n ? 0 : -1;
+            for (int ct = 0; ct < CT; ++ct) {
+                best[ct] = -INFINITY;
+                where[ct] = r.n ? 0 : -1;
+            }
         }
-        u32x4 next[PIECES];
-        auto fetch = [&](int base) {
-#pragma unroll
-            for (int p = 0; p < PIECES; ++p) {
-                const int at = p * 256 + tid, row = base + at / L::PIECES;
-                next[p] = u32x4{0u, 0u, 0u, 0u};
-                if (row < r.n) next[p] = *(const u32x4*)((const char*)(docs + (int64_t)(r.lo + row) * D) + at % L::PIECES * 16);
-            }
-        };
-        if (r.n) fetch(0);
-        for (int base = 0; base < r.n; base += L::ROWS) {
-            __syncthreads();
-#pragma unroll
-            for (int p = 0; p < PIECES; ++p) {
-                const int at = p * 256 + tid;
-                *(u32x4*)(tile + L::at(at / L::PIECES, at % L::PIECES)) = next[p];
-            }
-            __syncthreads();
-            if (base + L::ROWS < r.n) fetch(base + L::ROWS);
-            if (wave * CT * 32 >= cols) continue;
-#pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                if (base + 32 * b >= r.n) break;
+        if (wave * CT * 32 < cols) {
+            const int lane = here(lane0);
+#pragma unroll 1
+            for (int b = 0; b < NB && base + 32 * b < r.n; ++b) {
                 f32x16 s[CT] = {};
 #pragma unroll
                 for (int c = 0; c < D / 16; ++c) {
-                    const typename O::Frag a = L::rows(tile, lane, b, c);
+                    const typename O::Frag a = L::rows(tile[buf], lane, b, c);
 #pragma unroll
                     for (int ct = 0; ct < CT; ++ct) O::mma(s[ct], a, q[ct][c]);
                 }
-                const int first = base + 32 * b + 4 * h, room = r.n - first;
-                const bool whole = base + 32 * b + 32 <= r.n;
+                const int at = base + 32 * b + 4 * (lane >> 5), room = r.n - at;
+                if (base + 32 * b + 32 > r.n) {
 #pragma unroll
-                for (int ct = 0; ct < CT; ++ct)
+                    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                        for (int x = 0; x < 16; ++x) s[ct][x] = 8 * (x >> 2) + (x & 3) < room ? s[ct][x] : -INFINITY;
+                }
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) {
+                    int k = -1;
 #pragma unroll
                     for (int x = 0; x < 16; ++x) {
-                        const int k = 8 * (x >> 2) + (x & 3);
-                        const bool more = s[ct][x] > best[ct] && (whole || k < room);
-                        best[ct] = more ? s[ct][x] : best[ct];
-                        where[ct] = more ? first + k : where[ct];
+                        const bool higher = s[ct][x] > best[ct];          // the first of equal ones stays
+                        best[ct] = higher ? s[ct][x] : best[ct];
+                        k = higher ? 8 * (x >> 2) + (x & 3) : k;
                     }
+                    where[ct] = k < 0 ? where[ct] : at + k;
+                }
             }
         }
+        if (last) {
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-            const float b2 = __shfl_xor(best[ct], 32);
-            const int w2 = __shfl_xor(where[ct], 32);
-            const bool take = b2 > best[ct] || (b2 == best[ct] && w2 < where[ct]);
-            if (take) {
-                best[ct] = b2;
-                where[ct] = w2;
+            for (int ct = 0; ct < CT; ++ct) {
+                const float b2 = __shfl_xor(best[ct], 32);
+                const int w2 = __shfl_xor(where[ct], 32);
+                const bool take = b2 > best[ct] || (b2 == best[ct] && w2 < where[ct]);
+                best[ct] = take ? b2 : best[ct];
+                where[ct] = take ? w2 : where[ct];
+                const int col = (wave * CT + ct) * 32 + n;
+                if (h == 0) cells[i & 1][col] = best[ct];
+                if (h == 0 && col < cols) argmax[((int64_t)(q0 + col / T) * N + i) * T + col % T] = where[ct];
             }
-            const int col = (wave * CT + ct) * 32 + n;
-            if (ct == 0) __syncthreads();            // the sums of the document before have been read
-            if (h == 0) cells[col] = best[ct];
-            if (h == 0 && col < cols) argmax[((int64_t)(q0 + col / T) * N + i) * T + col % T] = where[ct];
         }
+        if (more) wait_for_copies();
         __syncthreads();
-        if (tid < queries) {
-            float sum = 0.f;
-            for (int t = 0; t < T; ++t) sum += cells[tid * T + t];
-            scores[(int64_t)(q0 + tid) * N + i] = sum;
+        if (last) {                                  // eight lanes a query; the next document's cells are the other ones
+            for (int x = tid >> 3; x < queries; x += 32) {
+                float sum = 0.f;
+                for (int t = tid & 7; t < T; t += 8) sum += cells[i & 1][x * T + t];
+#pragma unroll
+                for (int m = 1; m < 8; m <<= 1) sum += __shfl_xor(sum, m);
+                if ((tid & 7) == 0) scores[(int64_t)(q0 + x) * N + i] = sum;
+            }
         }
+        if (!more) return;
+        r = n_r;
+        i = n_i;
+        base = n_base;
+        buf ^= 1;
     }
 }
 
@@ -182,19 +202,19 @@ template <class E, int D> struct RowLanes {
     }
 };
 
-// Queries: a row is the weighted sum of one token of every document.  A workgroup has four tokens of a query; the documents
-// are split over its lane groups, whose sums are added in their order.
+// Queries: a row is the weighted sum of one token of every document.  A workgroup has one query token; the documents are split
+// over its lane groups, whose sums are added in their order.
 template <class E, int D>
-__global__ __launch_bounds__(256) void k_maxsim_dq(const float* dscores, const int32_t* argmax, int T, int t_groups, const E* docs,
-                                                   const int64_t* off, int N, int total, E* dQ) {
+__device__ __forceinline__ void query_gradient(char* lds, int block, const float* dscores, const int32_t* argmax, int T, const E* docs,
+                                               const int64_t* off, int N, int total, E* dQ) {
     using R = RowLanes<E, D>;
-    constexpr int GROUPS = 256 / R::LANES, TOKENS = 4, PARTS = GROUPS / TOKENS, AHEAD = 8;
-    __shared__ float sums[PARTS][TOKENS][R::LANES * R::PER];
-    const int tid = threadIdx.x, piece = tid % R::LANES, token = tid / R::LANES % TOKENS, part = tid / R::LANES / TOKENS;
-    const int q = blockIdx.x / t_groups, t = blockIdx.x % t_groups * TOKENS + token;
+    constexpr int PARTS = 256 / R::LANES, AHEAD = 8, WIDTH = R::LANES * R::PER;
+    float* sums = (float*)lds;                       // [PARTS][WIDTH]
+    const int tid = threadIdx.x, piece = tid % R::LANES, part = tid / R::LANES;
+    const int q = block / T, t = block % T;
     const int each = (N + PARTS - 1) / PARTS, i0 = part * each, i1 = N - i0 < each ? N : i0 + each;
     float acc[R::PER] = {};
-    if (t < T && piece < R::PIECES) {
+    if (piece < R::PIECES) {
         const int32_t* a = argmax + (int64_t)q * N * T + t;
         const float* g = dscores + (int64_t)q * N;
         for (int i = i0; i < i1; i += AHEAD) {
@@ -217,49 +237,55 @@ __global__ __launch_bounds__(256) void k_maxsim_dq(const float* dscores, const i
         }
     }
 #pragma unroll
-    for (int j = 0; j < R::PER; ++j) sums[part][token][piece * R::PER + j] = acc[j];
+    for (int j = 0; j < R::PER; ++j) sums[part * WIDTH + piece * R::PER + j] = acc[j];
     __syncthreads();
-    if (part == 0 && t < T && piece < R::PIECES) {
+    if (part == 0 && piece < R::PIECES) {
         for (int p = 1; p < PARTS; ++p)
 #pragma unroll
-            for (int j = 0; j < R::PER; ++j) acc[j] += sums[p][token][piece * R::PER + j];
-        R::store(dQ + ((int64_t)q * T + t) * D, piece, acc);
+            for (int j = 0; j < R::PER; ++j) acc[j] += sums[p * WIDTH + piece * R::PER + j];
+        R::store(dQ + (int64_t)block * D, piece, acc);
     }
 }
 
 // Documents: a token's row is the weighted sum of the query tokens that chose it.  A workgroup has 64 tokens; it sorts the
 // (query, token) entries that chose one of them by token, keeping their order (each wavefront a quarter of the entries, lanes
-// with the same token found by ballots), and lane groups add up a token's list each.  The sort, not atomics on the rows, so
-// that the order of the sums is fixed.
+// with the same token found by ballots), and each lane group adds up the lists of consecutive tokens as one, eight rows on
+// their way at a time.  The sort, not atomics on the rows, so that the order of the sums is fixed.
+// MANY: more entries than are sorted at once; the rows are added up in LDS then.
 constexpr int kEntries = 4096, kTokens = 64;
-template <class E, int D>
-__global__ __launch_bounds__(256) void k_maxsim_ddocs(const float* dscores, const int32_t* argmax, const E* Q, int nq, int T,
-                                                      const int64_t* off, int N, int total, E* ddocs) {
+template <int D, bool MANY> struct TokenLists {
+    float weight[kEntries];
+    uint16_t list[kEntries];
+    int8_t token[kEntries];
+    int next[4][kTokens], begin[kTokens + 1];
+    __align__(16) float rows[MANY ? kTokens : 1][MANY ? D : 1];
+};
+template <class E, int D, bool MANY>
+__device__ __forceinline__ void document_gradient(char* lds, int block, const float* dscores, const int32_t* argmax, const E* Q, int nq,
+                                                  int T, const int64_t* off, int N, int total, E* ddocs) {
     using R = RowLanes<E, D>;
-    constexpr int GROUPS = 256 / R::LANES, OWN = kTokens / GROUPS, AHEAD = 4;
-    __shared__ float weight[kEntries];
-    __shared__ uint16_t list[kEntries];
-    __shared__ int8_t token[kEntries];
-    __shared__ int next[4][kTokens], begin[kTokens + 1];
+    constexpr int GROUPS = 256 / R::LANES, OWN = kTokens / GROUPS, AHEAD = 8;
+    TokenLists<D, MANY>& s = *(TokenLists<D, MANY>*)lds;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int doc = find_sequence(off, N, kTokens, total, blockIdx.x, lane);
+    const int doc = find_sequence(off, N, kTokens, total, block, lane);
     const Range r = sequence_rows(off, doc, total, kTokens);
-    const int first = ((int)blockIdx.x - r.place) * kTokens;
+    const int first = (block - r.place) * kTokens;
     if (first < 0 || first >= r.n) return;
     const int piece = tid % R::LANES, group = tid / R::LANES;
     const int entries = nq * T;
-    float acc[OWN][R::PER] = {};
+    if constexpr (MANY)
+        for (int i = tid; i < kTokens * D; i += 256) (&s.rows[0][0])[i] = 0.f;
     for (int e0 = 0; e0 < entries; e0 += kEntries) {
         const int count = entries - e0 < kEntries ? entries - e0 : kEntries;
         const int quarter = ((count + 255) / 256) * 64;          // entries of a wavefront, 64 a step
         const int w0 = wave * quarter, w1 = w0 + quarter < count ? w0 + quarter : count;
         __syncthreads();
-        next[wave][lane] = 0;
+        s.next[wave][lane] = 0;
 #pragma unroll 4
         for (int e = w0 + lane; e < w1; e += 64) {
             const int q = (int)((uint32_t)(e0 + e) / (uint32_t)T);
             const int x = argmax[((int64_t)q * N + doc) * T + (e0 + e - q * T)] - first;
-            token[e] = (int8_t)(x >= 0 && x < kTokens ? x : -1);
+            s.token[e] = (int8_t)(x >= 0 && x < kTokens ? x : -1);
         }
         __syncthreads();
         auto same = [&](int x) {                     // lanes of the step with this lane's token
@@ -272,9 +298,9 @@ __global__ __launch_bounds__(256) void k_maxsim_ddocs(const float* dscores, cons
             return m;
         };
         for (int e = w0; e < w1; e += 64) {
-            const int x = e + lane < w1 ? token[e + lane] : -1;
+            const int x = e + lane < w1 ? s.token[e + lane] : -1;
             const uint64_t m = same(x);
-            if (x >= 0 && lane == __builtin_ctzll(m)) next[wave][x] += __builtin_popcountll(m);
+            if (x >= 0 && lane == __builtin_ctzll(m)) s.next[wave][x] += __builtin_popcountll(m);
             __builtin_amdgcn_wave_barrier();
         }
         __syncthreads();
@@ -282,7 +308,7 @@ __global__ __launch_bounds__(256) void k_maxsim_ddocs(const float* dscores, cons
             int n = 0, c[4];
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                c[w] = next[w][lane];
+                c[w] = s.next[w][lane];
                 n += c[w];
             }
             int end = n;
@@ -292,59 +318,95 @@ __global__ __launch_bounds__(256) void k_maxsim_ddocs(const float* dscores, cons
                 if (lane >= m) end += x;
             }
             int at = end - n;
-            begin[lane] = at;
-            if (lane == 63) begin[64] = end;
+            s.begin[lane] = at;
+            if (lane == 63) s.begin[64] = end;
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                next[w][lane] = at;
+                s.next[w][lane] = at;
                 at += c[w];
             }
         }
         __syncthreads();
         for (int e = w0; e < w1; e += 64) {
-            const int x = e + lane < w1 ? token[e + lane] : -1;
+            const int x = e + lane < w1 ? s.token[e + lane] : -1;
             const uint64_t m = same(x);
             if (x >= 0) {
-                const int at = next[wave][x] + __builtin_popcountll(m & ((1ull << lane) - 1ull));
+                const int at = s.next[wave][x] + __builtin_popcountll(m & ((1ull << lane) - 1ull));
                 __builtin_amdgcn_wave_barrier();
-                list[at] = (uint16_t)(e + lane);
-                weight[at] = dscores[(int64_t)((uint32_t)(e0 + e + lane) / (uint32_t)T) * N + doc];
-                if (lane == 63 - __builtin_clzll(m)) next[wave][x] = at + 1;
+                s.list[at] = (uint16_t)(e + lane);
+                s.weight[at] = dscores[(int64_t)((uint32_t)(e0 + e + lane) / (uint32_t)T) * N + doc];
+                if (lane == 63 - __builtin_clzll(m)) s.next[wave][x] = at + 1;
             }
             __builtin_amdgcn_wave_barrier();
         }
         __syncthreads();
         if (piece < R::PIECES) {
+            int token = group * OWN, bound = s.begin[token + 1];
+            const int end = s.begin[group * OWN + OWN];
+            float acc[R::PER] = {};
+            auto done = [&]() {                      // with a token's list
+                if constexpr (MANY) {
 #pragma unroll
-            for (int k = 0; k < OWN; ++k) {
-                const int tk = group + k * GROUPS, b1 = begin[tk + 1];
-                for (int b = begin[tk]; b < b1; b += AHEAD) {
-                    u32x4 x[AHEAD];
-                    float w[AHEAD];
+                    for (int j = 0; j < R::PER; ++j) s.rows[token][piece * R::PER + j] += acc[j];
+                } else if (first + token < r.n) {
+                    R::store(ddocs + (int64_t)(r.lo + first + token) * D, piece, acc);
+                }
 #pragma unroll
-                    for (int j = 0; j < AHEAD; ++j) {
-                        x[j] = u32x4{0u, 0u, 0u, 0u};
-                        w[j] = 0.f;
-                        if (b + j < b1) {
-                            w[j] = weight[b + j];
-                            x[j] = *(const u32x4*)((const char*)(Q + (int64_t)(e0 + list[b + j]) * D) + piece * 16);
-                        }
+                for (int j = 0; j < R::PER; ++j) acc[j] = 0.f;
+                ++token;
+                bound = s.begin[token + 1 < kTokens ? token + 1 : kTokens];
+            };
+            for (int b = s.begin[token]; b < end; b += AHEAD) {
+                u32x4 x[AHEAD];
+                float w[AHEAD];
+#pragma unroll
+                for (int j = 0; j < AHEAD; ++j) {
+                    x[j] = u32x4{0u, 0u, 0u, 0u};
+                    w[j] = 0.f;
+                    if (b + j < end) {
+                        w[j] = s.weight[b + j];
+                        x[j] = *(const u32x4*)((const char*)(Q + (int64_t)(e0 + s.list[b + j]) * D) + piece * 16);
                     }
+                }
 #pragma unroll
-                    for (int j = 0; j < AHEAD; ++j) R::add(acc[k], x[j], w[j]);
+                for (int j = 0; j < AHEAD; ++j) {
+                    while (b + j >= bound && b + j < end) done();
+                    R::add(acc, x[j], w[j]);
                 }
             }
+            while (token < group * OWN + OWN) done();
         }
     }
-    if (piece < R::PIECES) {
+    if constexpr (MANY) {
+        if (piece < R::PIECES) {                     // the lane group's own tokens
+            for (int k = 0; k < OWN; ++k) {
+                const int token = group * OWN + k;
+                if (first + token >= r.n) break;
+                float acc[R::PER];
 #pragma unroll
-        for (int k = 0; k < OWN; ++k) {
-            const int row = first + group + k * GROUPS;
-            if (row < r.n) R::store(ddocs + (int64_t)(r.lo + row) * D, piece, acc[k]);
+                for (int j = 0; j < R::PER; ++j) acc[j] = s.rows[token][piece * R::PER + j];
+                R::store(ddocs + (int64_t)(r.lo + first + token) * D, piece, acc);
+            }
         }
     }
 }
 
+// One launch for both: the first workgroups take documents, which take longer.
+template <class E, int D, bool MANY>
+__global__ __launch_bounds__(256) void k_maxsim_gradients(const float* dscores, const int32_t* argmax, const E* Q, int nq, int T,
+                                                          const E* docs, const int64_t* off, int N, int total, int doc_blocks, E* dQ,
+                                                          E* ddocs) {
+    constexpr size_t SUMS = sizeof(float) * (256 / RowLanes<E, D>::LANES) * RowLanes<E, D>::LANES * RowLanes<E, D>::PER;
+    constexpr size_t LISTS = sizeof(TokenLists<D, MANY>);
+    __shared__ __align__(16) char lds[SUMS > LISTS ? SUMS : LISTS];
+    const int block = blockIdx.x;
+    if (block < doc_blocks) document_gradient<E, D, MANY>(lds, block, dscores, argmax, Q, nq, T, off, N, total, ddocs);
+    else query_gradient<E, D>(lds, block - doc_blocks, dscores, argmax, T, docs, off, N, total, dQ);
+}
+
+#ifndef DOCGROUPS
+#define DOCGROUPS 1024
+#endif
 // ---- launches ------------------------------------------------------------------------------------------------
 template <class F> hipError_t by_type_and_width(int dt, int d, F&& f) {
     auto width = [&](auto type) {
@@ -366,7 +428,7 @@ hipError_t launch_maxsim_scores(const void* Q, int nq, int T, int d, int dt, con
         auto go = [&](auto ct) {
             constexpr int CT = decltype(ct)::value;
             const int q_per = 128 * CT / T, col_groups = (nq + q_per - 1) / q_per;
-            int64_t docs_per = N * col_groups / 2048;
+            int64_t docs_per = N * col_groups / DOCGROUPS;
             docs_per = docs_per < 1 ? 1 : docs_per;
             const int64_t parts = (N + docs_per - 1) / docs_per;
             k_maxsim_train<E, D, CT><<<dim3((unsigned)(parts * col_groups)), 256, 0, st>>>(
@@ -390,14 +452,13 @@ hipError_t launch_maxsim_backward(const float* dscores, const int32_t* argmax, c
     return by_type_and_width(dt, d, [&](auto type, auto dc) {
         using E = decltype(type);
         constexpr int D = decltype(dc)::value;
-        const int t_groups = (T + 3) / 4;
-        k_maxsim_dq<E, D><<<dim3((unsigned)(nq * t_groups)), 256, 0, st>>>(dscores, argmax, T, t_groups, (const E*)docs, off, (int)N,
-                                                                           (int)total, (E*)dQ);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess || total == 0) return e;
-        k_maxsim_ddocs<E, D><<<dim3((unsigned)(total / kTokens + N)), 256, 0, st>>>(dscores, argmax, (const E*)Q, nq, T, off, (int)N,
-                                                                                    (int)total, (E*)ddocs);
-        return hipGetLastError();
+        const int doc_blocks = total > 0 ? (int)(total / kTokens + N) : 0;
+        auto go = [&](auto many) {
+            k_maxsim_gradients<E, D, decltype(many)::value><<<dim3((unsigned)(doc_blocks + nq * T)), 256, 0, st>>>(
+                dscores, argmax, (const E*)Q, nq, T, (const E*)docs, off, (int)N, (int)total, doc_blocks, (E*)dQ, (E*)ddocs);
+            return hipGetLastError();
+        };
+        return nq * T > kEntries ? go(std::true_type{}) : go(std::false_type{});
     });
 }
 

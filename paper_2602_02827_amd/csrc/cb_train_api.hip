@@ -38,11 +38,13 @@ AttnPlan plan_attention(const AttnArgs& A, int d, int dt, bool backward) {
         return at;
     };
     if (!backward) {
-        // Few tiles over long keys: their keys are cut into parts of 256 rows or more until there are a thousand workgroups.
+        // Few tiles over long keys: their keys are cut into parts of 128 rows or more (on average; the longest sequence's are
+        // longer) until there are 2,048 workgroups.  16 tokens over 1 to 16,385 keys, us: 50 so, 53 with 256 rows and 1,024, 65 with
+        // 128 and 4,096, 80 with 512 and 1,024.
         const int64_t groups = P.q_slots * P.units;
         if (groups < 512 && k_rows >= 512) {
-            int64_t s = (1023 + groups) / groups;
-            s = s < k_rows / 256 ? s : k_rows / 256;
+            int64_t s = (2048 - 1 + groups) / groups;
+            s = s < k_rows / 128 ? s : k_rows / 128;
             P.splits = (int)(s < 1 ? 1 : s > 256 ? 256 : s);
         }
         if (P.splits > 1) {
