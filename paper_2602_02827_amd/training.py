@@ -70,7 +70,8 @@ def _ptr(t):
 
 
 def _stream():
-    return torch.cuda.current_stream().cuda_stream
+    # the handle alone: making a Stream object of it costs as much as a small call's kernels (2.8 us)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _check(rc, what):
@@ -81,7 +82,7 @@ def _check(rc, what):
 def _on_device(*tensors):
     dev = torch.cuda.current_device()
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.device.index != dev):
+        if t is not None and t.get_device() != dev:
             raise ValueError("tensors must live on the current device")
 
 
@@ -154,8 +155,8 @@ def colbandit_attention(q, k, v, q_offsets, k_offsets=None, *, causal=False, sca
     a = _attn(q, k, v, q_offsets, k_offsets, causal, scale, keep, bias, max_distance)
     L = lib()
     o, lse = (out["out"], out["lse"]) if out else (None, None)
-    o = torch.empty(q.shape, dtype=q.dtype, device=q.device) if o is None else _dense(o, q.shape, q.dtype, "out")
-    lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device) if lse is None else \
+    o = q.new_empty(q.shape) if o is None else _dense(o, q.shape, q.dtype, "out")
+    lse = q.new_empty((q.shape[1], q.shape[0]), dtype=torch.float32) if lse is None else \
         _dense(lse, (q.shape[1], q.shape[0]), torch.float32, "lse")
     ws, nb = _workspace(workspace, L.colbandit_attention_workspace_bytes(a, 0), q.device)
     _check(L.colbandit_attention(a, o.data_ptr(), lse.data_ptr(), _ptr(ws), nb, _stream()), "colbandit_attention")
@@ -172,9 +173,7 @@ def colbandit_attention_backward(dout, q, k, v, out, lse, q_offsets, k_offsets=N
     _dense(lse, (q.shape[1], q.shape[0]), torch.float32, "lse")
     _dense(dout, q.shape, q.dtype, "dout")
     _on_device(out, lse, dout)
-    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    dk = torch.empty(k.shape, dtype=q.dtype, device=q.device)
-    dv = torch.empty(k.shape, dtype=q.dtype, device=q.device)
+    dq, dk, dv = q.new_empty(q.shape), k.new_empty(k.shape), k.new_empty(k.shape)
     dbias = None if bias is None else torch.empty_like(bias)
     ws, nb = _workspace(workspace, L.colbandit_attention_workspace_bytes(a, 1), q.device)
     _check(L.colbandit_attention_backward(a, out.data_ptr(), lse.data_ptr(), dout.data_ptr(), dq.data_ptr(), dk.data_ptr(),
@@ -197,8 +196,8 @@ def colbandit_maxsim_scores(Q, docs, offsets):
     """MaxSim of all (query, document) pairs.  Returns dict(scores float32 [n_queries, N], argmax int32
     [n_queries, N, T])."""
     nq, T, d, N, total = _maxsim(Q, docs, offsets)
-    scores = torch.empty((nq, N), dtype=torch.float32, device=Q.device)
-    argmax = torch.empty((nq, N, T), dtype=torch.int32, device=Q.device)
+    scores = Q.new_empty((nq, N), dtype=torch.float32)
+    argmax = Q.new_empty((nq, N, T), dtype=torch.int32)
     _check(lib().colbandit_maxsim_scores(Q.data_ptr(), nq, T, d, _DTYPES[Q.dtype], docs.data_ptr(), offsets.data_ptr(), N,
                                          total, scores.data_ptr(), argmax.data_ptr(), _stream()), "colbandit_maxsim_scores")
     return {"scores": scores, "argmax": argmax}
@@ -211,7 +210,7 @@ def colbandit_contrastive_loss(scores, targets, temperature=1.0):
     _dense(scores, (nq, N), torch.float32, "scores")
     _dense(targets, (nq,), torch.int64, "targets")
     _on_device(scores, targets)
-    loss = torch.empty((nq,), dtype=torch.float32, device=scores.device)
+    loss = scores.new_empty(nq)
     dscores = torch.empty_like(scores)
     _check(lib().colbandit_contrastive_loss(scores.data_ptr(), nq, N, targets.data_ptr(), temperature, loss.data_ptr(),
                                             dscores.data_ptr(), _stream()), "colbandit_contrastive_loss")
