@@ -79,7 +79,7 @@ template <class E, int D> struct Column {
 // such rows with zeros when they have arrived.
 template <class E, int D, int THREADS, bool MASKED> struct Staged {
     using T = Tile<E, D>;
-    static constexpr int N = T::ROWS * T::PIECES / THREADS;
+    static constexpr int ALL = T::ROWS * T::PIECES, N = (ALL + THREADS - 1) / THREADS;
     uint8_t keep[MASKED ? N : 1];
     // a_at(row), b_at(row): byte offsets of the matrices' rows; kept(row): whether the mask leaves it.  rows: how many are left.
     template <class AtA, class AtB, class Kept>
@@ -88,6 +88,7 @@ template <class E, int D, int THREADS, bool MASKED> struct Staged {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int pos = i * THREADS + tid, place = pos / T::PIECES;
+            if (ALL % THREADS && i * THREADS + wave * 64 >= ALL) break;          // of the wavefront
             const uint32_t piece = (uint32_t)((pos % T::PIECES ^ T::turn(place)) * 16);
             const int row = place < rows ? place : rows - 1;
             char* to = lds + (i * THREADS + wave * 64) * 16;
@@ -103,6 +104,7 @@ template <class E, int D, int THREADS, bool MASKED> struct Staged {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 char* to = lds + (i * THREADS + tid) * 16;
+                if (ALL % THREADS && i * THREADS + tid >= ALL) break;
                 if (!keep[i]) {
                     *(u32x4*)to = zero;
                     *(u32x4*)(to + T::BYTES) = zero;
@@ -154,11 +156,23 @@ template <int LO> __device__ __forceinline__ f32x8 eight(const f32x16& x) {
     return __builtin_shufflevector(x, x, LO, LO + 1, LO + 2, LO + 3, LO + 4, LO + 5, LO + 6, LO + 7);
 }
 
-// Tiles are seen whole, or some of their rows by no column (past the end, or hidden by the mask: minus infinity is added to
-// their scores, a value of each row in LDS), or by some columns only (causal: a limit on the row as well).
-struct Whole { static constexpr bool part = false, diagonal = false; };
-struct Part { static constexpr bool part = true, diagonal = false; };
-struct Diagonal { static constexpr bool part = true, diagonal = true; };
+// Values of a block's rows, as its accumulators have them (LDS).  Tiles whose rows are not all seen by every column get minus
+// infinity added to the scores of rows that none sees (past the end, or hidden by the mask), and causal ones a limit on the row as
+// well.  These, and all that not every tile needs, are branches around a few instructions: a copy of the whole tile's code for each
+// case costs some sixty registers, since the accumulators are in other places in each.
+__device__ __forceinline__ f32x16 of_rows(const float* v, int b, int h) {
+    f32x16 x;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const f32x4 y = *(const f32x4*)(v + 32 * b + 8 * j + 4 * h);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[4 * j + i] = y[i];
+    }
+    return x;
+}
+
+// Wide heads take all registers: their workgroups do not go on to the next one.
+template <int D> constexpr bool kRuns = D <= 64;
 
 // ---- forward -------------------------------------------------------------------------------------------------
 // One pass over the keys with the running maximum and sum of the softmax, in 32 bits; probabilities are rounded to the
@@ -236,22 +250,25 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 3 : 2) void k_attention(const At
         const char *lk = lds[buf], *lv = lk + T::BYTES;
         const bool last = i + 1 >= end_tile;                     // of the unit
         const int n_unit = last ? unit + 1 : unit, n_i = last ? first_tile : i + 1;
-        const bool more = n_unit < end_unit;
+        const bool more = kRuns<D> ? n_unit < end_unit : !last;
         if (more && any) issue(n_unit, n_i * T::ROWS, lds[buf ^ 1]);
-        auto compute = [&](auto how, auto blocks) {
-            using How = decltype(how);
+        if (any && w.busy && base < w.end) {
             const int lane = here(lane0), h = lane >> 5;
-            constexpr int N = decltype(blocks)::value;           // blocks of 32 keys
-            f32x16 s[N];
+            const bool one = NB > 1 && base + 32 >= w.end;       // its second block has no keys
+            const bool diagonal = A.causal && base + T::ROWS - 1 > w.first_lim, part = seen != kAllRows;
+            if constexpr (MASKED) {
+                const int room = A.causal ? w.lim - base : 63;
+                sees |= (seen & (room < 0 ? 0ull : room >= 63 ? ~0ull : (2ull << room) - 1ull)) != 0;
+            }
+            f32x16 s[NB];
+            float top = -INFINITY;
 #pragma unroll
-            for (int b = 0; b < N; ++b) {
+            for (int b = 0; b < NB; ++b) {
+                if (b && one) break;
                 s[b] = {};
 #pragma unroll
                 for (int c = 0; c < D / 16; ++c) O::mma(s[b], T::rows(lk, lane, b, c), q.v[c]);
-            }
-            if constexpr (BIAS) {
-#pragma unroll
-                for (int b = 0; b < N; ++b) {
+                if constexpr (BIAS) {
                     const int d0 = base + 32 * b - w.first_lim, side = block_side(d0, A.reach);
                     if (side) {
                         const float x = table[side < 0 ? 0 : 2 * middle];
@@ -263,30 +280,17 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 3 : 2) void k_attention(const At
                         for (int r = 0; r < 16; ++r) s[b][r] = fmaf(s[b][r], scale2, x[8 * (r >> 2) + (r & 3)]);
                     }
                 }
-            }
-            constexpr bool SCALED = BIAS || How::part;           // s is in powers of two
-            if constexpr (How::part) {
-                const int room = w.lim - base - 4 * h;
+                if (part) s[b] += of_rows(hidden[buf], b, h);
+                if (diagonal) {
+                    const int room = w.lim - base - 32 * b - 4 * h;
 #pragma unroll
-                for (int b = 0; b < N; ++b)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const f32x4 no = *(const f32x4*)(hidden[buf] + 32 * b + 8 * j + 4 * h);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            float& x = ((float*)&s[b])[4 * j + e];
-                            x = BIAS ? x + no[e] : fmaf(x, scale2, no[e]);
-                            if constexpr (How::diagonal) x = 32 * b + 8 * j + e <= room ? x : -INFINITY;
-                        }
-                    }
-            }
-            float top = s[0][0];
-#pragma unroll
-            for (int b = 0; b < N; ++b)
+                    for (int r = 0; r < 16; ++r) s[b][r] = 8 * (r >> 2) + (r & 3) <= room ? s[b][r] : -INFINITY;
+                }
 #pragma unroll
                 for (int r = 0; r < 16; ++r) top = __builtin_elementwise_maximum(top, s[b][r]);
+            }
             top = max_of_halves(top);
-            if constexpr (!SCALED) top *= scale2;
+            if constexpr (!BIAS) top *= scale2;
             const bool passed = top > m + kLag;
             if (__ballot(passed)) {
                 const float to = passed ? top : m;
@@ -298,10 +302,11 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 3 : 2) void k_attention(const At
             }
             const float off = m == -INFINITY ? 0.f : -m;
 #pragma unroll
-            for (int b = 0; b < N; ++b) {
+            for (int b = 0; b < NB; ++b) {
+                if (b && one) break;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    s[b][r] = exp2_fast(SCALED ? s[b][r] + off : fmaf(s[b][r], scale2, off));
+                    s[b][r] = exp2_fast(BIAS ? s[b][r] + off : fmaf(s[b][r], scale2, off));
                     l += s[b][r];
                 }
                 const typename O::Frag p0 = O::round(eight<0>(s[b])), p1 = O::round(eight<8>(s[b]));
@@ -310,25 +315,9 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 3 : 2) void k_attention(const At
 #pragma unroll
                 for (int db = 0; db < DB; ++db) O::mma(acc[db], T::turned(lv, lane, b, 1, db), p1);
             }
-        };
-        if (any && w.busy && base < w.end) {
-            using All = std::integral_constant<int, NB>;
-            using One = std::integral_constant<int, 1>;
-            const bool one = NB > 1 && base + 32 >= w.end;
-            if constexpr (MASKED) {
-                const int room = A.causal ? w.lim - base : 63;
-                sees |= (seen & (room < 0 ? 0ull : room >= 63 ? ~0ull : (2ull << room) - 1ull)) != 0;
-            }
-            if (A.causal && base + T::ROWS - 1 > w.first_lim) {
-                if (one) compute(Diagonal{}, One{}); else compute(Diagonal{}, All{});
-            } else if (seen != kAllRows) {
-                if (one) compute(Part{}, One{}); else compute(Part{}, All{});
-            } else {
-                compute(Whole{}, All{});
-            }
         }
         if (last) {
-            if (more) load_q(n_unit);
+            if (kRuns<D> && more) load_q(n_unit);
             l = sum_of_halves(l);
             if (MASKED && !sees) {                               // whatever its row held
                 m = -INFINITY;
@@ -467,7 +456,7 @@ __device__ __forceinline__ void add_diagonals(const f32x16& x, float* scratch, f
 
 // Gradients of queries, delta, and the bias table's share of each tile; head units one after the other, as the forward pass.
 template <class E, int D, int NW, bool BIAS, bool MASKED>
-__global__ __launch_bounds__(64 * NW, D <= 64 ? 2 : 1) void k_attention_dq(const AttnArgs A, int slots, int units, int run, const E* out,
+__global__ __launch_bounds__(64 * NW, D <= 64 || sizeof(E) == 2 ? 2 : 1) void k_attention_dq(const AttnArgs A, int slots, int units, int run, const E* out,
                                                                            const E* dout, const float* lse, E* dq, float* delta,
                                                                            float* bias_part) {
     using O = Oper<E>;
@@ -565,22 +554,22 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 2 : 1) void k_attention_dq(const
         const char *lk = lds[buf], *lv = lk + T::BYTES;
         const bool last = i + 1 >= tiles;
         const int n_unit = last ? unit + 1 : unit, n_i = last ? 0 : i + 1;
-        const bool more = n_unit < end_unit;
+        const bool more = kRuns<D> ? n_unit < end_unit : !last;
         if (more && any) issue(n_unit, n_i * T::ROWS, lds[buf ^ 1]);
-        const int blocks = NB == 1 || base + 32 >= w.end ? 1 : NB;
-        auto compute = [&](auto how) {
-            using How = decltype(how);
+        if (any && w.busy && base < w.end) {
             const int lane = here(lane0), h = lane >> 5;
-            const int room = w.lim - base - 4 * h;
+            const bool diagonal = A.causal && base + T::ROWS - 1 > w.first_lim, part = seen != kAllRows;
 #pragma unroll 1
-            for (int b = 0; b < blocks; ++b) {
+            for (int b = 0; b < NB && base + 32 * b < w.end; ++b) {
                 f32x16 s = {}, dp;
+#pragma unroll
+                for (int c = 0; c < D / 16; ++c) O::mma(s, T::rows(lk, lane, b, c), q.v[c]);
+                phase();
 #pragma unroll
                 for (int r = 0; r < 16; ++r) dp[r] = -dot;
 #pragma unroll
-                for (int c = 0; c < D / 16; ++c) O::mma(s, T::rows(lk, lane, b, c), q.v[c]);
-#pragma unroll
                 for (int c = 0; c < D / 16; ++c) O::mma(dp, T::rows(lv, lane, b, c), g.v[c]);
+                phase();
                 const int d0 = base + 32 * b - w.first_lim, side = BIAS ? block_side(d0, A.reach) : 0;
                 if (BIAS && !side) {
                     const float* x = table + middle + base + 32 * b + 4 * h - w.lim;
@@ -591,23 +580,23 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 2 : 1) void k_attention_dq(const
 #pragma unroll
                     for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], scale2, x);
                 }
+                if (part) s += of_rows(hidden[buf], b, h);
+                if (diagonal) {                       // (dp as well: what the row does not see may be anything)
+                    const int room = w.lim - base - 32 * b - 4 * h;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const bool own = 8 * (r >> 2) + (r & 3) <= room;
+                        s[r] = own ? s[r] : -INFINITY;
+                        dp[r] = own ? dp[r] : 0.f;
+                    }
+                }
                 float sum = 0.f, weight = 0.f;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    f32x4 no = {0.f, 0.f, 0.f, 0.f};
-                    if constexpr (How::part) no = *(const f32x4*)(hidden[buf] + 32 * b + 8 * j + 4 * h);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int r = 4 * j + e;
-                        const bool own = !How::diagonal || 32 * b + 8 * j + e <= room;
-                        float p = exp2_fast(How::part ? s[r] + no[e] : s[r]);
-                        if constexpr (BIAS && How::diagonal) p = own ? p : 0.f;
-                        if constexpr (BIAS) weight += p;
-                        float y = p * dp[r];
-                        if constexpr (How::diagonal) y = own ? y : 0.f;
-                        s[r] = y;
-                        sum += y;
-                    }
+                for (int r = 0; r < 16; ++r) {
+                    const float p = exp2_fast(s[r]);
+                    if constexpr (BIAS) weight += p;
+                    s[r] = p * dp[r];
+                    sum += s[r];
                 }
                 row_sum += sum;
                 if constexpr (BIAS) {
@@ -621,6 +610,7 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 2 : 1) void k_attention_dq(const
                         add_diagonals(s, scratch, own_hist + d0, lane);
                     }
                 }
+                phase();
                 if constexpr (sizeof(E) == 2) {
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
@@ -643,11 +633,6 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 2 : 1) void k_attention_dq(const
                     for (int db = 0; db < DB; ++db) O::mma(acc[db], T::turned(lk, lane, b, 1, db), eight<8>(s));
                 }
             }
-        };
-        if (any && w.busy && base < w.end) {
-            if (A.causal && base + T::ROWS - 1 > w.first_lim) compute(Diagonal{});
-            else if (seen != kAllRows) compute(Part{});
-            else compute(Whole{});
         }
         if (last) {
             row_sum = sum_of_halves(row_sum);
@@ -663,7 +648,7 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 2 : 1) void k_attention_dq(const
                                   f32x4{acc[db][4 * j] * A.scale, acc[db][4 * j + 1] * A.scale, acc[db][4 * j + 2] * A.scale,
                                         acc[db][4 * j + 3] * A.scale});
             }
-            if (more) load_rows(n_unit);
+            if (kRuns<D> && more) load_rows(n_unit);
         }
         if (more && any) finish(buf ^ 1);
         if constexpr (BIAS) {
@@ -733,20 +718,30 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 2 : 1) void k_attention_dq(const
 
 // Gradients of keys and values, `run` key heads one after the other; workgroups from `main` on add up the bias table's shares
 // of all tiles.
+// A wavefront with both gradients of 32 wide rows takes more than half of the registers, so nothing runs beside its waits.
+// In 16 bits wide heads have two wavefronts for the same rows, one for either gradient: the scores are made twice (five products
+// where there were four), but two wavefronts share a SIMD.
+template <class E, int D> constexpr bool kApart = sizeof(E) == 2 && D >= 96;
+template <class E, int D, int NW> constexpr int dkv_threads() { return (kApart<E, D> ? 128 : 64) * NW; }
+template <class E, int D> constexpr int dkv_waves() { return D <= 64 || kApart<E, D> ? 2 : 1; }
+#define DKV_BOUNDS (dkv_threads<E, D, NW>()), (dkv_waves<E, D>())
 template <class E, int D, int NW, bool BIAS, bool MASKED>
-__global__ __launch_bounds__(64 * NW, D <= 64 ? 2 : 1) void k_attention_dkv(const AttnArgs A, int slots, int run, int main, int q_slots,
+__global__ __launch_bounds__(DKV_BOUNDS) void k_attention_dkv(const AttnArgs A, int slots, int run, int main, int q_slots,
                                                                             const E* dout, const float* lse, const float* delta,
                                                                             const float* bias_part, E* dk, E* dv, E* dbias) {
     using O = Oper<E>;
     using T = Tile<E, D>;
-    constexpr int NB = T::ROWS / 32, DB = D / 32, THREADS = 64 * NW, COLS = 32 * NW;
+    constexpr int NB = T::ROWS / 32, DB = D / 32, COLS = 32 * NW;
+    constexpr bool APART = kApart<E, D>;
+    constexpr int WAVES = APART ? 2 * NW : NW, THREADS = 64 * WAVES;
+    const bool keys = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) >= NW;        // (APART) this wavefront has the keys' gradient
     __shared__ __align__(16) char lds[2][2 * T::BYTES];
     __shared__ __align__(16) float row_lse[2][T::ROWS], row_delta[2][T::ROWS];
     extern __shared__ __align__(16) char dyn[];
     const int tid = threadIdx.x, lane0 = tid & 63, lane = lane0, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     if constexpr (BIAS) {
         if ((int)blockIdx.x >= main) {                // one entry of the table each wavefront
-            const int e = ((int)blockIdx.x - main) * NW + wave;
+            const int e = ((int)blockIdx.x - main) * WAVES + wave;
             if (e >= A.n_buckets * A.heads) return;
             const int head = e / A.n_buckets, b = e % A.n_buckets;
             float sum = 0.f;
@@ -763,7 +758,7 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 2 : 1) void k_attention_dkv(cons
     const Range ks = sequence_rows(A.koff, seq, A.total_k, COLS), qs = sequence_rows(A.qoff, seq, A.total_q);
     const int key0 = (slot - ks.place) * COLS;
     if (key0 < 0 || key0 >= ks.n) return;
-    const int wkey = key0 + wave * 32, key = wkey + (lane & 31), shift = ks.n - qs.n;
+    const int wkey = key0 + wave % NW * 32, key = wkey + (lane & 31), shift = ks.n - qs.n;
     const bool real = key < ks.n;
     const int64_t at = ks.lo + key;
     const bool seen = real && (!MASKED || A.keep[at]);
@@ -819,10 +814,10 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 2 : 1) void k_attention_dkv(cons
     auto load_keys = [&](int kv) {
         k.load((const E*)A.k + at * A.k_row + kv * A.k_head, seen, h);
         k.take_sign(A.scale);
-        v.load((const E*)A.v + at * A.v_row + kv * A.v_head, seen, h);
+        if (!APART || keys) v.load((const E*)A.v + at * A.v_row + kv * A.v_head, seen, h);
     };
     load_keys(kv0);
-    f32x16 ak[DB] = {}, av[DB] = {};
+    f32x16 acc[DB] = {}, acc2[APART ? 1 : DB] = {};              // of keys and of values, or of the wavefront's own
     const int middle = bias_middle(A.reach);
     const bool busy = wkey < ks.n;
     const int wfirst = A.causal && wkey > shift ? (wkey - shift) * G : 0;             // first column that sees a key of the wavefront
@@ -839,90 +834,94 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 2 : 1) void k_attention_dkv(cons
     while (true) {
         const bool last_tile = c0 + T::ROWS >= cols;
         const int n_head = last_tile ? head0 + G : head0, n_c = last_tile ? col0 : c0 + T::ROWS;
-        const bool more = n_head < head_end, last = last_tile && n_head % A.group == 0;   // of a key head
+        const bool last = last_tile && n_head % A.group == 0;                           // of a key head
+        const bool more = kRuns<D> ? n_head < head_end : !last;
         if (more && any) issue(n_head, n_c, lds[buf ^ 1]);
         const char *lq = lds[buf], *lg = lq + T::BYTES;
-        const int blocks = NB == 1 || c0 + 32 >= cols ? 1 : NB;
-        auto compute = [&](auto diagonal) {
+        if (any && busy && c0 + T::ROWS > wfirst) {
             const int lane = here(lane0), h = lane >> 5;
-            // a lane's key is seen by columns from (key - shift) G on
-            const int need = (key - shift) * G - c0 - 4 * h;
+            const bool diagonal = A.causal && (wkey + 31 - shift) * G > c0;
+            const char* own = APART && !keys ? lg : lq;           // (own gradient's other operand)
 #pragma unroll 1
-            for (int b = 0; b < blocks; ++b) {
-                f32x16 s, dp, e, dl;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const f32x4 x = *(const f32x4*)(row_lse[buf] + 32 * b + 8 * j + 4 * h);
-                    const f32x4 y = *(const f32x4*)(row_delta[buf] + 32 * b + 8 * j + 4 * h);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        e[4 * j + i] = x[i];
-                        dl[4 * j + i] = y[i];
-                    }
-                }
-                if constexpr (START) {
-                    s = e;
-                    dp = dl;
-                } else {
-                    s = {};
-                    dp = {};
-                }
+            for (int b = 0; b < NB && c0 + 32 * b < cols; ++b) {
+                f32x16 s = {}, dp = {};
+                if constexpr (START) s = of_rows(row_lse[buf], b, h);
 #pragma unroll
                 for (int c = 0; c < D / 16; ++c) O::mma(s, T::rows(lq, lane, b, c), k.v[c]);
+                phase();
+                if (!APART || keys) {
+                    if constexpr (START) dp = of_rows(row_delta[buf], b, h);
 #pragma unroll
-                for (int c = 0; c < D / 16; ++c) O::mma(dp, T::rows(lg, lane, b, c), v.v[c]);
+                    for (int c = 0; c < D / 16; ++c) O::mma(dp, T::rows(lg, lane, b, c), v.v[c]);
+                    phase();
+                }
+                if constexpr (!START) {
+                    s = s * scale2 + of_rows(row_lse[buf], b, h);
+                    dp += of_rows(row_delta[buf], b, h);
+                }
                 const int d0 = wkey - (c0 + 32 * b + shift), side = BIAS ? block_side(d0, A.reach) : 0;
+                const float by = START ? scale2 : 1.f;
                 if (BIAS && !side) {
                     const float* x = table + middle + key - (c0 + 32 * b + shift) - 4 * h - 27;    // of the lane's last row
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], scale2, x[27 - 8 * (r >> 2) - (r & 3)]);
-                } else {
+                    for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], by, x[27 - 8 * (r >> 2) - (r & 3)]);
+                } else if constexpr (BIAS || START) {
                     const float x = BIAS ? table[side < 0 ? 0 : 2 * middle] : 0.f;
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s[r] = BIAS ? fmaf(s[r], scale2, x) : s[r] * scale2;
+                    for (int r = 0; r < 16; ++r) s[r] = BIAS ? fmaf(s[r], by, x) : s[r] * by;
                 }
-                f32x16 ds;
+                if (diagonal) {                       // a lane's key is seen by columns from (key - shift) G on
+                    const int need = (key - shift) * G - c0 - 32 * b - 4 * h;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    float p = exp2_fast(START ? s[r] : s[r] + e[r]);
-                    if constexpr (decltype(diagonal)::value) p = 32 * b + 8 * (r >> 2) + (r & 3) >= need ? p : 0.f;
-                    s[r] = p;
-                    ds[r] = p * (START ? dp[r] : dp[r] + dl[r]);
+                    for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + (r & 3) >= need ? s[r] : -INFINITY;
                 }
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = exp2_fast(s[r]);
+                if constexpr (!APART) {
+                    const typename O::Frag p0 = O::round(eight<0>(s)), p1 = O::round(eight<8>(s));
+                    phase();
+#pragma unroll
+                    for (int db = 0; db < DB; ++db) O::mma(acc2[db], T::turned(lg, lane, b, 0, db), p0);
+#pragma unroll
+                    for (int db = 0; db < DB; ++db) O::mma(acc2[db], T::turned(lg, lane, b, 1, db), p1);
+                    phase();
+                }
+                if (!APART || keys) s *= dp;
                 const typename O::Frag p0 = O::round(eight<0>(s)), p1 = O::round(eight<8>(s));
-                const typename O::Frag d0f = O::round(eight<0>(ds)), d1f = O::round(eight<8>(ds));
+                phase();
 #pragma unroll
-                for (int db = 0; db < DB; ++db) O::mma(av[db], T::turned(lg, lane, b, 0, db), p0);
+                for (int db = 0; db < DB; ++db) O::mma(acc[db], T::turned(own, lane, b, 0, db), p0);
 #pragma unroll
-                for (int db = 0; db < DB; ++db) O::mma(av[db], T::turned(lg, lane, b, 1, db), p1);
-#pragma unroll
-                for (int db = 0; db < DB; ++db) O::mma(ak[db], T::turned(lq, lane, b, 0, db), d0f);
-#pragma unroll
-                for (int db = 0; db < DB; ++db) O::mma(ak[db], T::turned(lq, lane, b, 1, db), d1f);
+                for (int db = 0; db < DB; ++db) O::mma(acc[db], T::turned(own, lane, b, 1, db), p1);
             }
-        };
-        if (any && busy && c0 + T::ROWS > wfirst) {
-            if (A.causal && (wkey + 31 - shift) * G > c0) compute(std::true_type{}); else compute(std::false_type{});
         }
         if (last) {
             const int kv = head0 / A.group;
-            if (more) load_keys(kv + 1);
+            if (kRuns<D> && more) load_keys(kv + 1);
             if (real) {
                 const int64_t dense = (at * A.kv_heads + kv) * D;
+                auto store = [&](E* to, const f32x16(&a)[DB], float by) {
 #pragma unroll
-                for (int db = 0; db < DB; ++db)
+                    for (int db = 0; db < DB; ++db)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const f32x4 x = {ak[db][4 * j], ak[db][4 * j + 1], ak[db][4 * j + 2], ak[db][4 * j + 3]};
-                        const f32x4 y = {av[db][4 * j], av[db][4 * j + 1], av[db][4 * j + 2], av[db][4 * j + 3]};
-                        const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-                        O::store4(dk + dense + 32 * db + 8 * j + 4 * h, seen ? x * A.scale : zero);
-                        O::store4(dv + dense + 32 * db + 8 * j + 4 * h, seen ? y : zero);
-                    }
+                        for (int j = 0; j < 4; ++j) {
+                            const f32x4 x = {a[db][4 * j] * by, a[db][4 * j + 1] * by, a[db][4 * j + 2] * by, a[db][4 * j + 3] * by};
+                            O::store4(to + dense + 32 * db + 8 * j + 4 * h, seen ? x : f32x4{0.f, 0.f, 0.f, 0.f});
+                        }
+                };
+                if constexpr (!APART) {
+                    store(dk, acc, A.scale);
+                    store(dv, acc2, 1.f);
+                } else {
+                    store(keys ? dk : dv, acc, keys ? A.scale : 1.f);
+                }
             }
             if (!more) return;
 #pragma unroll
-            for (int db = 0; db < DB; ++db) ak[db] = av[db] = {};
+            for (int db = 0; db < DB; ++db) {
+                acc[db] = {};
+                if constexpr (!APART) acc2[db] = {};
+            }
         }
         if (more && any) finish(buf ^ 1);
         __syncthreads();
@@ -1001,9 +1000,10 @@ hipError_t launch_attention_backward(const AttnArgs& A, const AttnPlan& P, const
             constexpr bool BIAS = decltype(bias)::value, MASKED = decltype(masked)::value;
             const size_t lds = BIAS ? bias_bytes(A.reach, 1) : 0;
             const int main = A.total_k > 0 ? (int)(P.k_slots * ((A.kv_heads + P.kv_run - 1) / P.kv_run)) : 0;
-            const int more = BIAS ? (A.n_buckets * A.heads + NW - 1) / NW : 0;
+            constexpr int WAVES = kApart<E, D> ? 2 * NW : NW;
+            const int more = BIAS ? (A.n_buckets * A.heads + WAVES - 1) / WAVES : 0;
             if (main + more == 0) return hipSuccess;
-            k_attention_dkv<E, D, NW, BIAS, MASKED><<<dim3((unsigned)(main + more)), 64 * NW, lds, st>>>(
+            k_attention_dkv<E, D, NW, BIAS, MASKED><<<dim3((unsigned)(main + more)), 64 * WAVES, lds, st>>>(
                 A, (int)P.k_slots, P.kv_run, main, q_slots, (const E*)G.dout, G.lse, delta, bias_part, (E*)G.dk, (E*)G.dv, (E*)G.dbias);
             return hipGetLastError();
         });

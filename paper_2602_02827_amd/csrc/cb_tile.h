@@ -129,6 +129,9 @@ __device__ __forceinline__ int here(int x) {
     return x;
 }
 
+// The compiler moves nothing across: operands of the next products are not read while the registers are needed for these.
+__device__ __forceinline__ void phase() { __builtin_amdgcn_sched_barrier(0); }
+
 // Sixteen bytes a lane from memory to LDS without registers: lane i's go to dst + 16 i (dst: the same for the wavefront).
 __device__ __forceinline__ void copy_to_lds(const void* src, char* dst) {
     using G = const __attribute__((address_space(1))) void;

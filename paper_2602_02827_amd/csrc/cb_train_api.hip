@@ -23,14 +23,14 @@ AttnPlan plan_attention(const AttnArgs& A, int d, int dt, bool backward) {
     P.q_slots = A.total_q / (32 * P.q_waves / A.pack) + A.n_seqs;
     P.k_slots = A.total_k / (32 * P.k_waves) + A.n_seqs;
     P.splits = 1;
-    // Short sequences: a workgroup goes on to the next heads, as long as enough workgroups are left.
+    // Short sequences: a workgroup goes on to the next heads, as long as enough workgroups are left (wide heads: kRuns).
     auto run_of = [](int64_t slots, int units, int64_t rows) {
         int r = 1;
         while (rows <= 384 && 2 * r <= units && slots * (units / (2 * r)) >= 1536) r *= 2;
         return r;
     };
-    P.run = run_of(P.q_slots, P.units, k_rows);
-    P.kv_run = run_of(P.k_slots, A.kv_heads, (int64_t)A.total_q * A.group / A.n_seqs);
+    P.run = d <= 64 ? run_of(P.q_slots, P.units, k_rows) : 1;
+    P.kv_run = d <= 64 ? run_of(P.k_slots, A.kv_heads, (int64_t)A.total_q * A.group / A.n_seqs) : 1;
     size_t o = 0;
     auto take = [&](int64_t bytes) {
         const size_t at = o;
