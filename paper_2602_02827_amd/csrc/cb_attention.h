@@ -20,9 +20,17 @@ namespace cb {
 constexpr int kBlock = 62;
 __device__ __host__ __forceinline__ int bias_middle(int reach) { return reach + kBlock; }
 __device__ __host__ __forceinline__ int bias_width(int reach) { return 2 * bias_middle(reach) + 1; }
-// Eight threads write a bucket's distances (its first one is in `starts`, in LDS).
+// Eight threads write a bucket's distances; its first one is in `starts`, in LDS.  They are put there by way of scalar registers:
+// vector loads of a kernel's arguments take microseconds.
 __device__ __forceinline__ void load_starts(const AttnArgs& A, int16_t* starts, int tid, int threads) {
-    for (int i = tid; i <= A.n_dir; i += threads) starts[i] = i < A.n_dir ? A.starts[i] : (int16_t)(bias_middle(A.reach) + 1);
+    for (int first = 0; first <= A.n_dir; first += threads) {
+        const int own = first + tid;
+        int x = bias_middle(A.reach) + 1;             // behind the last one
+        const int end = A.n_dir < first + threads ? A.n_dir : first + threads;
+#pragma unroll 8
+        for (int j = first; j < end; ++j) x = j == own ? A.starts[j] : x;
+        if (own <= A.n_dir) starts[own] = (int16_t)x;
+    }
 }
 template <class E>
 __device__ __forceinline__ void fill_bias(const AttnArgs& A, int head, const int16_t* starts, float* table, int tid, int threads) {
@@ -431,27 +439,25 @@ __global__ __launch_bounds__(256) void k_attention_join(const AttnArgs A, int sp
 // rounding is 1.7e-3).
 
 // Sums of a 32 x 32 block along its diagonals, added to a histogram by distance.  The block is in accumulators: a lane has
-// sixteen keys of a column.  Sixteen columns at a time go to LDS, 68 words apart (their writes in different banks) with zeros
-// between them; lane i then adds up the diagonal k - n = i - 15, one word of each column, and the histogram has one place for
-// it.  No atomics, which take 2.5 clocks a lane there, and a fixed order.
-constexpr int kPitch = 68, kDiagonal = 16 * kPitch + 16;
+// sixteen keys of a column.  The columns go to LDS, 68 words apart (sixteen lanes' writes in different banks) with zeros between
+// them; lane i then adds up the diagonal k - n = i - 31, one word of each column, and the histogram has one place for it.
+// No atomics, which take 2.5 clocks a lane there, and a fixed order.
+constexpr int kPitch = 68, kDiagonal = 32 * kPitch + 32;
 __device__ __forceinline__ void add_diagonals(const f32x16& x, float* scratch, float* hist, int lane) {
     const int n = lane & 31, h = lane >> 5;
-    const int i = lane < 47 ? lane : 46;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        if ((n >> 4) == half) {
+    for (int j = 0; j < 4; ++j)
+        *(f32x4*)(scratch + n * kPitch + 32 + 8 * j + 4 * h) = f32x4{x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]};
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const float* own = scratch + 32 - 31 + (lane < 63 ? lane : 62);
+    float sum = 0.f, more = 0.f;
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                *(f32x4*)(scratch + (n & 15) * kPitch + 32 + 8 * j + 4 * h) = f32x4{x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]};
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        float sum = 0.f;
-#pragma unroll
-        for (int c = 0; c < 16; ++c) sum += scratch[c * kPitch + 32 + c - 15 + i];
-        if (lane < 47) hist[i - 15 - 16 * half] += sum;
+    for (int c = 0; c < 32; c += 2) {
+        sum += own[c * kPitch + c];
+        more += own[(c + 1) * kPitch + c + 1];
     }
+    if (lane < 63) hist[lane - 31] += sum + more;
 }
 
 // Gradients of queries, delta, and the bias table's share of each tile; head units one after the other, as the forward pass.
@@ -465,12 +471,12 @@ __global__ __launch_bounds__(64 * NW, D <= 64 || sizeof(E) == 2 ? 2 : 1) void k_
     __shared__ __align__(16) char lds[2][2 * T::BYTES];
     __shared__ __align__(16) float diagonals[BIAS ? NW * kDiagonal : 1];
     __shared__ __align__(16) float hidden[2][T::ROWS];
-    __shared__ float far_sum[NW][2];
-    extern __shared__ __align__(16) char dyn[];       // the bias by distance, then a histogram of each wavefront
+    __shared__ float far_sum[kMostRun][NW][2];
+    extern __shared__ __align__(16) char dyn[];       // the bias by distance, then histograms of each head and wavefront
     const int tid = threadIdx.x, lane0 = tid & 63, lane = lane0, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     const int work = in_order(blockIdx.x, gridDim.x), runs = (units + run - 1) / run;
-    const int slot = work / runs;
-    int unit = work % runs * run;
+    const int slot = work / runs, first_unit = work % runs * run;
+    int unit = first_unit;
     const int end_unit = unit + run < units ? unit + run : units;
     const int G = A.pack, per = 32 * NW / G;
     const QueryTile t(A, slot, per, lane);
@@ -536,7 +542,7 @@ __global__ __launch_bounds__(64 * NW, D <= 64 || sizeof(E) == 2 ? 2 : 1) void k_
     float* own_hist = hist + wave * width + middle;
     float* scratch = diagonals + wave * kDiagonal;
     if constexpr (BIAS) {
-        for (int i = tid; i < NW * width; i += THREADS) hist[i] = 0.f;
+        for (int i = tid; i < (end_unit - unit) * NW * width; i += THREADS) hist[i] = 0.f;
         for (int i = tid; i < NW * kDiagonal; i += THREADS) diagonals[i] = 0.f;
         load_starts(A, starts, tid, THREADS);
         __syncthreads();
@@ -590,25 +596,24 @@ __global__ __launch_bounds__(64 * NW, D <= 64 || sizeof(E) == 2 ? 2 : 1) void k_
                         dp[r] = own ? dp[r] : 0.f;
                     }
                 }
-                float sum = 0.f, weight = 0.f;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = exp2_fast(s[r]);
+                if (BIAS && side) {
+                    float weight = 0.f;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) weight += s[r];
+                    (side < 0 ? weight_lo : weight_hi) += weight;
+                }
+                float sum = 0.f;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const float p = exp2_fast(s[r]);
-                    if constexpr (BIAS) weight += p;
-                    s[r] = p * dp[r];
+                    s[r] *= dp[r];
                     sum += s[r];
                 }
                 row_sum += sum;
                 if constexpr (BIAS) {
-                    if (side < 0) {
-                        far_lo += sum;
-                        weight_lo += weight;
-                    } else if (side > 0) {
-                        far_hi += sum;
-                        weight_hi += weight;
-                    } else {
-                        add_diagonals(s, scratch, own_hist + d0, lane);
-                    }
+                    if (side) (side < 0 ? far_lo : far_hi) += sum;
+                    else add_diagonals(s, scratch, own_hist + d0, lane);
                 }
                 phase();
                 if constexpr (sizeof(E) == 2) {
@@ -662,49 +667,17 @@ __global__ __launch_bounds__(64 * NW, D <= 64 || sizeof(E) == 2 ? 2 : 1) void k_
                     far_hi += __shfl_xor(far_hi, m);
                 }
                 if (lane == 0) {
-                    far_sum[wave][0] = far_lo;
-                    far_sum[wave][1] = far_hi;
+                    far_sum[unit - first_unit][wave][0] = far_lo;
+                    far_sum[unit - first_unit][wave][1] = far_hi;
                 }
                 far_lo = far_hi = weight_lo = weight_hi = 0.f;
-                __syncthreads();
-                for (int j = tid; j < width; j += THREADS) {
-                    float x = hist[j];
-#pragma unroll
-                    for (int v = 1; v < NW; ++v) {
-                        x += hist[v * width + j];
-                        hist[v * width + j] = 0.f;
-                    }
-                    hist[j] = 0.f;
-                    table[j] = x;                                         // its bias has been used
-                }
-                __syncthreads();
-                const float* x = table + middle;
-                for (int b0 = 0; b0 < A.n_buckets; b0 += THREADS / 8) {
-                    const int b = b0 + tid / 8;
-                    const bool one = b < A.n_buckets, behind = b >= A.n_dir;      // buckets of keys behind the query
-                    const int j0 = behind ? b - A.n_dir : b;
-                    const bool open = j0 == A.n_dir - 1;                          // the last one of its direction
-                    float sum = 0.f;
-                    if (one) {
-                        // distance 0 belongs to the keys before
-                        const int hi = open ? middle : A.starts[j0 + 1] - 1;
-                        for (int j = A.starts[j0] + tid % 8; j <= hi; j += 8) sum += behind ? (j > 0 ? x[j] : 0.f) : x[-j];
-                    }
-#pragma unroll
-                    for (int m = 1; m < 8; m <<= 1) sum += __shfl_xor(sum, m);
-                    if (one && tid % 8 == 0) {
-                        if (open)
-#pragma unroll
-                            for (int v = 0; v < NW; ++v) sum += far_sum[v][behind ? 1 : 0];
-                        bias_part[((int64_t)slot * A.heads + unit) * A.n_buckets + b] = sum;
-                    }
-                }
+                own_hist += NW * width;
                 __syncthreads();
                 if (more) fill_bias<E>(A, n_unit, starts, table, tid, THREADS);
             }
         }
         if (last) {
-            if (!more) return;
+            if (!more) break;
             row_sum = 0.f;
 #pragma unroll
             for (int db = 0; db < DB; ++db) acc[db] = {};
@@ -713,6 +686,31 @@ __global__ __launch_bounds__(64 * NW, D <= 64 || sizeof(E) == 2 ? 2 : 1) void k_
         unit = n_unit;
         i = n_i;
         buf ^= 1;
+    }
+    if constexpr (BIAS) {                             // the histograms of all heads: by wavefront, by bucket
+        const int heads = end_unit - first_unit;
+        for (int i = tid; i < heads * width; i += THREADS) {
+            float* x = hist + i / width * NW * width + i % width;
+#pragma unroll
+            for (int v = 1; v < NW; ++v) x[0] += x[v * width];
+        }
+        __syncthreads();
+        for (int i = tid >> 3; i < heads * A.n_buckets; i += THREADS / 8) {
+            const int u = i / A.n_buckets, b = i % A.n_buckets;
+            const float* x = hist + u * NW * width + middle;
+            const bool behind = b >= A.n_dir;                             // buckets of keys behind the query
+            const int j0 = behind ? b - A.n_dir : b, end = starts[j0 + 1];
+            float sum = 0.f;
+            for (int j = starts[j0] + (tid & 7); j < end; j += 8) sum += behind ? (j > 0 ? x[j] : 0.f) : x[-j];
+#pragma unroll
+            for (int m = 1; m < 8; m <<= 1) sum += __shfl_xor(sum, m);
+            if ((tid & 7) == 0) {
+                if (j0 == A.n_dir - 1)                                    // the open one of its direction
+#pragma unroll
+                    for (int v = 0; v < NW; ++v) sum += far_sum[u][v][behind ? 1 : 0];
+                bias_part[((int64_t)slot * A.heads + first_unit + u) * A.n_buckets + b] = sum;
+            }
+        }
     }
 }
 
@@ -986,7 +984,7 @@ hipError_t launch_attention_backward(const AttnArgs& A, const AttnPlan& P, const
             e = by_form(P.q_waves, A.bias != nullptr, A.keep != nullptr, [&](auto nw, auto bias, auto masked) {
                 constexpr int NW = decltype(nw)::value;
                 constexpr bool BIAS = decltype(bias)::value, MASKED = decltype(masked)::value;
-                const size_t lds = BIAS ? bias_bytes(A.reach, NW + 1) : 0;
+                const size_t lds = BIAS ? bias_bytes(A.reach, 1 + P.run * NW) : 0;
                 const int64_t runs = (P.units + P.run - 1) / P.run;
                 k_attention_dq<E, D, NW, BIAS, MASKED><<<dim3((unsigned)(P.q_slots * runs)), 64 * NW, lds, st>>>(
                     A, (int)P.q_slots, P.units, P.run, (const E*)G.out, (const E*)G.dout, G.lse, (E*)G.dq, delta, bias_part);

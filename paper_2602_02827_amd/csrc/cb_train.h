@@ -24,6 +24,8 @@ struct AttnArgs {
     int16_t starts[128];         // first distance of each bucket of one direction
 };
 
+constexpr int kMostRun = 2;      // heads that a workgroup takes one after the other (four: the histograms leave half the workgroups no LDS)
+
 struct AttnPlan {
     int d, dt;
     int q_waves, k_waves;        // wavefronts of a workgroup, 32 query (key) columns each

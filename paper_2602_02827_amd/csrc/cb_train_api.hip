@@ -26,11 +26,12 @@ AttnPlan plan_attention(const AttnArgs& A, int d, int dt, bool backward) {
     // Short sequences: a workgroup goes on to the next heads, as long as enough workgroups are left (wide heads: kRuns).
     auto run_of = [](int64_t slots, int units, int64_t rows) {
         int r = 1;
-        while (rows <= 384 && 2 * r <= units && slots * (units / (2 * r)) >= 1536) r *= 2;
+        while (rows <= 384 && 2 * r <= kMostRun && 2 * r <= units && slots * (units / (2 * r)) >= 1536) r *= 2;
         return r;
     };
     P.run = d <= 64 ? run_of(P.q_slots, P.units, k_rows) : 1;
     P.kv_run = d <= 64 ? run_of(P.k_slots, A.kv_heads, (int64_t)A.total_q * A.group / A.n_seqs) : 1;
+    if (A.bias && A.reach > 128) P.run = 1;          // (histograms of all its heads are in LDS)
     size_t o = 0;
     auto take = [&](int64_t bytes) {
         const size_t at = o;
