@@ -82,43 +82,30 @@ template <class E, int D> struct Column {
     }
 };
 
-// Two matrices' rows on their way to a tile in LDS, a tile ahead of its use, by the memory unit itself; rows past the end as the
-// last row again (they meet probabilities of zero).  What a mask hides may be anything: a lane overwrites its own pieces of
-// such rows with zeros when they have arrived.
+// Two matrices' rows on their way to tiles in LDS.  What a mask hides may be anything: zeros are written in its place.
 template <class E, int D, int THREADS, bool MASKED> struct Staged {
     using T = Tile<E, D>;
-    static constexpr int ALL = T::ROWS * T::PIECES, N = (ALL + THREADS - 1) / THREADS;
-    uint8_t keep[MASKED ? N : 1];
+    using R = Rows<E, D, THREADS>;
+    R x, y;
+    uint8_t keep[MASKED ? R::N : 1];
     // a_at(row), b_at(row): byte offsets of the matrices' rows; kept(row): whether the mask leaves it.  rows: how many are left.
     template <class AtA, class AtB, class Kept>
     __device__ __forceinline__ void issue(const char* a, const char* b, char* lds, int rows, int tid0, AtA&& a_at, AtB&& b_at, Kept&& kept) {
         const int tid = here(tid0), wave = __builtin_amdgcn_readfirstlane(tid0 >> 6);
+        x.issue(a, lds, rows, tid, wave, a_at);
+        y.issue(b, lds + T::BYTES, rows, tid, wave, b_at);
+        if constexpr (MASKED) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int pos = i * THREADS + tid, place = pos / T::PIECES;
-            if (ALL % THREADS && i * THREADS + wave * 64 >= ALL) break;          // of the wavefront
-            const uint32_t piece = (uint32_t)((pos % T::PIECES ^ T::turn(place)) * 16);
-            const int row = place < rows ? place : rows - 1;
-            char* to = lds + (i * THREADS + wave * 64) * 16;
-            copy_to_lds(a + (a_at(row) + piece), to);
-            copy_to_lds(b + (b_at(row) + piece), to + T::BYTES);
-            if constexpr (MASKED) keep[i] = kept(row);
+            for (int i = 0; i < R::N; ++i) {
+                const int r = R::row(i, tid);
+                keep[i] = kept(r < rows ? r : rows - 1);
+            }
         }
     }
     __device__ __forceinline__ void finish(char* lds, int tid) const {
-        wait_for_copies();
-        if constexpr (MASKED) {
-            const u32x4 zero = {0u, 0u, 0u, 0u};
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                char* to = lds + (i * THREADS + tid) * 16;
-                if (ALL % THREADS && i * THREADS + tid >= ALL) break;
-                if (!keep[i]) {
-                    *(u32x4*)to = zero;
-                    *(u32x4*)(to + T::BYTES) = zero;
-                }
-            }
-        }
+        auto whole = [&](int i) { return !MASKED || keep[MASKED ? i : 0]; };
+        x.finish(lds, tid, whole);
+        y.finish(lds + T::BYTES, tid, whole);
     }
 };
 
@@ -179,8 +166,14 @@ __device__ __forceinline__ f32x16 of_rows(const float* v, int b, int h) {
     return x;
 }
 
-// Wide heads take all registers: their workgroups do not go on to the next one.
+// Wavefronts per SIMD that the registers are shared out for (one more each makes the compiler spill, and is slower; forward
+// pass, 512 passages, three and four: 152 and 176 us; gradients, two and three: 764 and 851 us).
+template <class E, int D> constexpr int kWaves = sizeof(E) == 2 ? (D <= 64 ? 3 : 2) : D <= 32 ? 3 : D <= 96 ? 2 : 1;
+template <class E, int D> constexpr int kGradientWaves = sizeof(E) == 2 || D <= 32 ? 2 : 1;
+// Wide heads take all registers: their workgroups do not go on to the next one, and their gradients in 32 bits are not made by
+// single wavefronts, which would hold a whole tile on its way in registers as well.
 template <int D> constexpr bool kRuns = D <= 64;
+template <class E, int D> constexpr bool kSingle = sizeof(E) == 2 || D <= 64;
 
 // ---- forward -------------------------------------------------------------------------------------------------
 // One pass over the keys with the running maximum and sum of the softmax, in 32 bits; probabilities are rounded to the
@@ -190,7 +183,7 @@ constexpr float kLag = 8.f;
 // A workgroup takes its tile for `run` head units one after the other, the first keys of the next on their way while it
 // computes: short sequences have one to three tiles of keys, whose latency would otherwise be most of the time.
 template <class E, int D, int NW, bool BIAS, bool MASKED>
-__global__ __launch_bounds__(64 * NW, D <= 64 ? 3 : 2) void k_attention(const AttnArgs A, int slots, int units, int run, int splits, E* out, float* lse,
+__global__ __launch_bounds__(64 * NW, (kWaves<E, D>)) void k_attention(const AttnArgs A, int slots, int units, int run, int splits, E* out, float* lse,
                                                           float* o_part, float2* ml_part) {
     using O = Oper<E>;
     using T = Tile<E, D>;
@@ -462,7 +455,7 @@ __device__ __forceinline__ void add_diagonals(const f32x16& x, float* scratch, f
 
 // Gradients of queries, delta, and the bias table's share of each tile; head units one after the other, as the forward pass.
 template <class E, int D, int NW, bool BIAS, bool MASKED>
-__global__ __launch_bounds__(64 * NW, D <= 64 || sizeof(E) == 2 ? 2 : 1) void k_attention_dq(const AttnArgs A, int slots, int units, int run, const E* out,
+__global__ __launch_bounds__(64 * NW, (kGradientWaves<E, D>)) void k_attention_dq(const AttnArgs A, int slots, int units, int run, const E* out,
                                                                            const E* dout, const float* lse, E* dq, float* delta,
                                                                            float* bias_part) {
     using O = Oper<E>;
@@ -526,7 +519,10 @@ __global__ __launch_bounds__(64 * NW, D <= 64 || sizeof(E) == 2 ? 2 : 1) void k_
         dot = 0.f;
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) {
-            if (!seeing) q.v[c] = g.v[c] = {};
+            if (!seeing) {
+                q.v[c] = {};
+                g.v[c] = {};
+            }
             const f32x8 x = O::wide(g.v[c]), y = O::wide(o.v[c]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) dot += x[e] * y[e];
@@ -633,9 +629,9 @@ __global__ __launch_bounds__(64 * NW, D <= 64 || sizeof(E) == 2 ? 2 : 1) void k_
                     }
                 } else {
 #pragma unroll
-                    for (int db = 0; db < DB; ++db) O::mma(acc[db], T::turned(lk, lane, b, 0, db), eight<0>(s));
+                    for (int db = 0; db < DB; ++db) O::mma(acc[db], T::turned(lk, lane, b, 0, db), O::round(eight<0>(s)));
 #pragma unroll
-                    for (int db = 0; db < DB; ++db) O::mma(acc[db], T::turned(lk, lane, b, 1, db), eight<8>(s));
+                    for (int db = 0; db < DB; ++db) O::mma(acc[db], T::turned(lk, lane, b, 1, db), O::round(eight<8>(s)));
                 }
             }
         }
@@ -720,11 +716,8 @@ __global__ __launch_bounds__(64 * NW, D <= 64 || sizeof(E) == 2 ? 2 : 1) void k_
 // In 16 bits wide heads have two wavefronts for the same rows, one for either gradient: the scores are made twice (five products
 // where there were four), but two wavefronts share a SIMD.
 template <class E, int D> constexpr bool kApart = sizeof(E) == 2 && D >= 96;
-template <class E, int D, int NW> constexpr int dkv_threads() { return (kApart<E, D> ? 128 : 64) * NW; }
-template <class E, int D> constexpr int dkv_waves() { return D <= 64 || kApart<E, D> ? 2 : 1; }
-#define DKV_BOUNDS (dkv_threads<E, D, NW>()), (dkv_waves<E, D>())
 template <class E, int D, int NW, bool BIAS, bool MASKED>
-__global__ __launch_bounds__(DKV_BOUNDS) void k_attention_dkv(const AttnArgs A, int slots, int run, int main, int q_slots,
+__global__ __launch_bounds__((kApart<E, D> ? 128 : 64) * NW, (kGradientWaves<E, D>)) void k_attention_dkv(const AttnArgs A, int slots, int run, int main, int q_slots,
                                                                             const E* dout, const float* lse, const float* delta,
                                                                             const float* bias_part, E* dk, E* dv, E* dbias) {
     using O = Oper<E>;
@@ -942,9 +935,11 @@ template <class F> hipError_t by_width(int d, F&& f) {
         default: return f(std::integral_constant<int, 128>{});
     }
 }
-template <class F> hipError_t by_form(int waves, bool bias, bool masked, F&& f) {
+template <bool SINGLE, class F> hipError_t by_form(int waves, bool bias, bool masked, F&& f) {
     auto w = [&](auto b, auto m) {
-        return waves == 1 ? f(std::integral_constant<int, 1>{}, b, m) : f(std::integral_constant<int, 4>{}, b, m);
+        if constexpr (SINGLE)
+            if (waves == 1) return f(std::integral_constant<int, 1>{}, b, m);
+        return f(std::integral_constant<int, 4>{}, b, m);
     };
     if (bias) return masked ? w(std::true_type{}, std::true_type{}) : w(std::true_type{}, std::false_type{});
     return masked ? w(std::false_type{}, std::true_type{}) : w(std::false_type{}, std::false_type{});
@@ -957,7 +952,7 @@ hipError_t launch_attention(const AttnArgs& A, const AttnPlan& P, E* out, float*
         constexpr int D = decltype(dc)::value;
         float* o_part = (float*)(ws + P.o_part);
         float2* ml_part = (float2*)(ws + P.ml_part);
-        const hipError_t e = by_form(P.q_waves, A.bias != nullptr, A.keep != nullptr, [&](auto nw, auto bias, auto masked) {
+        const hipError_t e = by_form<true>(P.q_waves, A.bias != nullptr, A.keep != nullptr, [&](auto nw, auto bias, auto masked) {
             constexpr int NW = decltype(nw)::value;
             constexpr bool BIAS = decltype(bias)::value, MASKED = decltype(masked)::value;
             const size_t lds = BIAS ? bias_bytes(A.reach, 1) : 0;
@@ -981,7 +976,7 @@ hipError_t launch_attention_backward(const AttnArgs& A, const AttnPlan& P, const
         constexpr int D = decltype(dc)::value;
         hipError_t e = hipSuccess;
         if (A.total_q > 0) {
-            e = by_form(P.q_waves, A.bias != nullptr, A.keep != nullptr, [&](auto nw, auto bias, auto masked) {
+            e = by_form<kSingle<E, D>>(P.q_waves, A.bias != nullptr, A.keep != nullptr, [&](auto nw, auto bias, auto masked) {
                 constexpr int NW = decltype(nw)::value;
                 constexpr bool BIAS = decltype(bias)::value, MASKED = decltype(masked)::value;
                 const size_t lds = BIAS ? bias_bytes(A.reach, 1 + P.run * NW) : 0;
@@ -993,7 +988,7 @@ hipError_t launch_attention_backward(const AttnArgs& A, const AttnPlan& P, const
             if (e != hipSuccess) return e;
         }
         const int q_slots = A.total_q > 0 ? (int)P.q_slots : 0;
-        return by_form(P.k_waves, A.bias != nullptr, A.keep != nullptr, [&](auto nw, auto bias, auto masked) {
+        return by_form<kSingle<E, D>>(P.k_waves, A.bias != nullptr, A.keep != nullptr, [&](auto nw, auto bias, auto masked) {
             constexpr int NW = decltype(nw)::value;
             constexpr bool BIAS = decltype(bias)::value, MASKED = decltype(masked)::value;
             const size_t lds = BIAS ? bias_bytes(A.reach, 1) : 0;

@@ -12,28 +12,24 @@ namespace cb {
 // its documents through LDS, the next tile on its way while it multiplies.  A column's running maximum and its place stay in the
 // column's two lanes; a comparison, and two selections of it, for every product (the place within a block is a constant).
 template <class E, int D, int CT>
-__global__ __launch_bounds__(256, 2) void k_maxsim_train(const E* Q, int nq, int T, const E* docs, const int64_t* off, int N, int total,
+__global__ __launch_bounds__(256, (sizeof(E) == 4 && D == 128 ? 1 : 2)) void k_maxsim_train(const E* Q, int nq, int T, const E* docs, const int64_t* off, int N, int total,
                                                          int col_groups, int q_per, int docs_per, float* scores, int32_t* argmax) {
     using O = Oper<E>;
     using L = Tile<E, D>;
-    constexpr int NB = L::ROWS / 32, COPIES = L::ROWS * L::PIECES / 256;
+    constexpr int NB = L::ROWS / 32;
     __shared__ __align__(16) char tile[2][L::BYTES];
     __shared__ float cells[2][128 * CT];
     const int tid = threadIdx.x, lane0 = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane0 & 31, h = lane0 >> 5;
     const int group = blockIdx.x % col_groups, part = blockIdx.x / col_groups;
     const int q0 = group * q_per, queries = nq - q0 < q_per ? nq - q0 : q_per, cols = queries * T;
     const int doc0 = part * docs_per, doc_end = N - doc0 < docs_per ? N : doc0 + docs_per;
+    Rows<E, D, 256> next;
     auto issue = [&](const Range& r, int base, char* to) {
         if (r.n == 0) return;
-        const int t = here(tid);
-        const char* src = (const char*)(docs + (int64_t)(r.lo + base) * D);
-        const int rows = r.n - base;
-#pragma unroll
-        for (int p = 0; p < COPIES; ++p) {
-            const int at = p * 256 + t, place = at / L::PIECES, row = place < rows ? place : rows - 1;
-            copy_to_lds(src + (uint32_t)(row * L::PITCH + (at % L::PIECES ^ L::turn(place)) * 16), to + (p * 256 + wave * 64) * 16);
-        }
+        next.issue((const char*)(docs + (int64_t)(r.lo + base) * D), to, r.n - base, here(tid), wave,
+                   [&](int row) { return (uint32_t)(row * D * (int)sizeof(E)); });
     };
+    auto finish = [&](char* to) { next.finish(to, tid, [](int) { return true; }); };
     Range r = sequence_rows(off, doc0, total);
     issue(r, 0, tile[0]);
     typename O::Frag q[CT][D / 16];
@@ -49,7 +45,7 @@ __global__ __launch_bounds__(256, 2) void k_maxsim_train(const E* Q, int nq, int
     float best[CT];
     int where[CT];
     int i = doc0, base = 0, buf = 0;
-    wait_for_copies();
+    if (r.n) finish(tile[0]);
     __syncthreads();
     while (true) {
         const bool first = base == 0, last = base + L::ROWS >= r.n;       // of the document
@@ -108,7 +104,7 @@ __global__ __launch_bounds__(256, 2) void k_maxsim_train(const E* Q, int nq, int
                 if (h == 0 && col < cols) argmax[((int64_t)(q0 + col / T) * N + i) * T + col % T] = where[ct];
             }
         }
-        if (more) wait_for_copies();
+        if (more && n_r.n) finish(tile[buf ^ 1]);
         __syncthreads();
         if (last) {                                  // eight lanes a query; the next document's cells are the other ones
             for (int x = tid >> 3; x < queries; x += 32) {

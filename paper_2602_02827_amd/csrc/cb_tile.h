@@ -8,7 +8,8 @@
 // then are the B operand of step c as they are, if the A operand takes its eight elements in the same order: 16c + 4h
 // .. +3 and 16c + 8 + 4h .. +3 (turned operand).  So probabilities never leave the registers they were computed in.
 //   bf16   one v_mfma_f32_32x32x16_bf16 a step; turned operands by two transposing LDS reads of four rows each
-//   fp32   eight v_mfma_f32_32x32x2_f32 a step, element e of both operands in the e-th
+//   fp32   the same instruction, whose rate is sixteen times that of the 32-bit ones, on three bf16 pieces of eight bits of every
+//          value: six products of pieces a step, the three smallest (2^-23 of a product together) left out
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -40,71 +41,79 @@ template <> struct Oper<__bf16> {
     static __device__ __forceinline__ void store4(__bf16* p, const f32x4& x) { *(bf16x4*)p = __builtin_convertvector(x, bf16x4); }
 };
 template <> struct Oper<float> {
-    using Frag = f32x8;
+    // The first piece is cut off, so that it never overflows, the others are rounded; their sum is the value.
+    struct Frag {
+        bf16x8 p[3];
+        __device__ __forceinline__ Frag operator-() const { return {{-p[0], -p[1], -p[2]}}; }
+    };
     static constexpr int ROWS = 32;
     static __device__ __forceinline__ void mma(f32x16& acc, const Frag& a, const Frag& b) {
+        constexpr int A[6] = {2, 0, 1, 1, 0, 0}, B[6] = {0, 2, 1, 0, 1, 0};       // the smallest first
 #pragma unroll
-        for (int e = 0; e < 8; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], acc, 0, 0, 0);
+        for (int i = 0; i < 6; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.p[A[i]], b.p[B[i]], acc, 0, 0, 0);
     }
-    static __device__ __forceinline__ Frag round(const f32x8& x) { return x; }
-    static __device__ __forceinline__ f32x8 wide(const Frag& x) { return x; }
+    static __device__ __forceinline__ Frag round(const f32x8& x) {
+        f32x8 first;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) first[i] = __uint_as_float(__float_as_uint(x[i]) & 0xffff0000u);
+        Frag f;
+        f.p[0] = __builtin_convertvector(first, bf16x8);
+        const f32x8 rest = x - first;
+        f.p[1] = __builtin_convertvector(rest, bf16x8);
+        f.p[2] = __builtin_convertvector(rest - __builtin_convertvector(f.p[1], f32x8), bf16x8);
+        return f;
+    }
+    static __device__ __forceinline__ f32x8 wide(const Frag& x) {
+        return __builtin_convertvector(x.p[0], f32x8) + (__builtin_convertvector(x.p[1], f32x8) + __builtin_convertvector(x.p[2], f32x8));
+    }
     static __device__ __forceinline__ Frag load(const void* p) {
         const f32x4 a = *(const f32x4*)p, b = *((const f32x4*)p + 1);
-        return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+        return round(__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
     }
     static __device__ __forceinline__ void store4(float* p, const f32x4& x) { *(f32x4*)p = x; }
 };
 
-// ROWS rows of D values in LDS, as 16-byte pieces.  A piece's place in its row is turned by the row's low bits.  256 bytes are
-// read a clock: sixteen rows' pieces of one column (row operands) lie in different banks, and so do the four rows of 64 bytes
-// that half a wavefront takes of a turned operand in 16 bits (128-byte and 256-byte rows: by the turn's upper bits; the others
-// by their pitch).
-template <class E, int D> struct Tile {
-    using Frag = typename Oper<E>::Frag;
-    static constexpr int ROWS = Oper<E>::ROWS, PITCH = D * (int)sizeof(E), PIECES = PITCH / 16;
-    static constexpr int BYTES = ROWS * PITCH;
+// ROWS rows of D values in LDS, as 16-byte pieces of bf16.  A piece's place in its row is turned by the row's low bits.  256 bytes
+// are read a clock: sixteen rows' pieces of one column (row operands) lie in different banks, and so do the four rows of 64 bytes
+// that half a wavefront takes of a turned operand (128-byte and 256-byte rows: by the turn's upper bits; the others by their pitch).
+template <int ROWS, int D> struct Plane {
+    static constexpr int PITCH = 2 * D, PIECES = PITCH / 16, BYTES = ROWS * PITCH;
     static __device__ __forceinline__ int turn(int row) {
-        if constexpr (sizeof(E) == 4 && PIECES % 16 == 0) return (row & 3) | ((row >> 1) & 4) | ((row << 1) & 8);
         if constexpr (PIECES % 16 == 0) return ((row & 3) << 2) | ((row >> 2) & 3);
         if constexpr (PIECES % 8 == 0) return ((row & 2) << 1) | ((row >> 2) & 3);
         return (row >> 2) & 3;
     }
     static __device__ __forceinline__ int at(int row, int piece) { return row * PITCH + ((piece ^ turn(row)) << 4); }
+    static __device__ __forceinline__ int row_place(int lane, int b, int c) { return at(32 * b + (lane & 31), 2 * c + (lane >> 5)); }
+    // (sixteen lanes read four rows of sixteen values and get a column of four each; eight rows on for the other four)
+    static __device__ __forceinline__ int turned_place(int lane, int b, int c, int db, int half) {
+        const int row = 32 * b + 16 * c + 8 * half + 4 * (lane >> 5) + ((lane & 15) >> 2);
+        return at(row, 4 * db + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) + (lane & 1) * 8;
+    }
+    static __device__ __forceinline__ bf16x8 turned(const char* t, int x, int y) {
+        using L = __attribute__((address_space(3))) i16x4;
+        const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)(t + x)), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)(t + y));
+        const auto both = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+        return __builtin_bit_cast(bf16x8, both);
+    }
+};
+// A tile: one plane, or one of each piece.
+template <class E, int D> struct Tile {
+    using Frag = typename Oper<E>::Frag;
+    static constexpr int ROWS = Oper<E>::ROWS, PLANES = sizeof(E) == 2 ? 1 : 3;
+    using P = Plane<ROWS, D>;
+    static constexpr int PIECES = P::PIECES, BYTES = PLANES * P::BYTES;
     // rows 32b .. 32b+31, elements 16c .. 16c+15 of each
     static __device__ __forceinline__ Frag rows(const char* t, int lane, int b, int c) {
-        const int n = lane & 31, h = lane >> 5;
-        if constexpr (sizeof(E) == 2) {
-            return *(const bf16x8*)(t + at(32 * b + n, 2 * c + h));
-        } else {
-            const f32x4 x = *(const f32x4*)(t + at(32 * b + n, 4 * c + 2 * h));
-            const f32x4 y = *(const f32x4*)(t + at(32 * b + n, 4 * c + 2 * h + 1));
-            return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
-        }
+        const char* p = t + P::row_place(lane, b, c);
+        if constexpr (PLANES == 1) return *(const bf16x8*)p;
+        else return {{*(const bf16x8*)p, *(const bf16x8*)(p + P::BYTES), *(const bf16x8*)(p + 2 * P::BYTES)}};
     }
     // columns 32db .. 32db+31 of the rows 32b + 16c .. +15, in the accumulators' order
     static __device__ __forceinline__ Frag turned(const char* t, int lane, int b, int c, int db) {
-        const int h = lane >> 5;
-        if constexpr (sizeof(E) == 2) {
-            // sixteen lanes read four rows of sixteen values and get a column of four each
-            const int row = 32 * b + 16 * c + 4 * h + ((lane & 15) >> 2);
-            const int piece = 4 * db + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
-            const char* p = t + at(row, piece) + (lane & 1) * 8;
-            using L = __attribute__((address_space(3))) i16x4;
-            const i16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)p);
-            const char* p8 = t + at(row + 8, piece) + (lane & 1) * 8;
-            const i16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)p8);
-            const auto both = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
-            return __builtin_bit_cast(bf16x8, both);
-        } else {
-            const int col = 32 * db + (lane & 31);
-            f32x8 r;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int row = 32 * b + 16 * c + 8 * (e >> 2) + 4 * h + (e & 3);
-                r[e] = *(const float*)(t + at(row, col >> 2) + (col & 3) * 4);
-            }
-            return r;
-        }
+        const int x = P::turned_place(lane, b, c, db, 0), y = P::turned_place(lane, b, c, db, 1);
+        if constexpr (PLANES == 1) return P::turned(t, x, y);
+        else return {{P::turned(t, x, y), P::turned(t + P::BYTES, x, y), P::turned(t + 2 * P::BYTES, x, y)}};
     }
 };
 
@@ -139,6 +148,48 @@ __device__ __forceinline__ void copy_to_lds(const void* src, char* dst) {
     __builtin_amdgcn_global_load_lds((G*)src, (L*)dst, 16, 0, 0);
 }
 __device__ __forceinline__ void wait_for_copies() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// A matrix's rows on their way to a tile in LDS, a tile ahead of its use, rows past the end as the last row again.  16 bits: by the
+// memory unit itself.  32 bits: they wait in registers, and are cut into their pieces as they are written.
+// at(row): byte offset of a row; whole(i): whether the i-th piece of this thread is kept (zeros otherwise).
+template <class E, int D, int THREADS> struct Rows {
+    using T = Tile<E, D>;
+    static constexpr int ALL = T::ROWS * T::PIECES, N = (ALL + THREADS - 1) / THREADS;
+    static constexpr bool DIRECT = sizeof(E) == 2;
+    f32x4 x[DIRECT ? 1 : N][2];
+    static __device__ __forceinline__ int row(int i, int tid) { return (i * THREADS + tid) / T::PIECES; }
+    template <class At> __device__ __forceinline__ void issue(const char* a, char* lds, int rows, int tid, int wave, At&& at) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (ALL % THREADS && i * THREADS + wave * 64 >= ALL) break;          // of the wavefront
+            const int pos = i * THREADS + tid, place = row(i, tid);
+            const char* src = a + (at(place < rows ? place : rows - 1) +
+                                   (uint32_t)((pos % T::PIECES ^ T::P::turn(place)) * 8 * (int)sizeof(E)));
+            if constexpr (DIRECT) {
+                copy_to_lds(src, lds + (i * THREADS + wave * 64) * 16);
+            } else {
+                x[i][0] = *(const f32x4*)src;
+                x[i][1] = *((const f32x4*)src + 1);
+            }
+        }
+    }
+    template <class Whole> __device__ __forceinline__ void finish(char* lds, int tid, Whole&& whole) const {
+        if constexpr (DIRECT) wait_for_copies();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (ALL % THREADS && i * THREADS + tid >= ALL) break;
+            char* to = lds + (i * THREADS + tid) * 16;
+            if constexpr (DIRECT) {
+                if (!whole(i)) *(u32x4*)to = u32x4{0u, 0u, 0u, 0u};      // its own pieces have arrived
+            } else {
+                const f32x8 v = __builtin_shufflevector(x[i][0], x[i][1], 0, 1, 2, 3, 4, 5, 6, 7);
+                const auto f = Oper<E>::round(whole(i) ? v : f32x8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                for (int p = 0; p < 3; ++p) *(bf16x8*)(to + p * T::P::BYTES) = f.p[p];
+            }
+        }
+    }
+};
 
 // Tiles of ragged sequences: sequence i begins at place off[i] / per + i, which leaves room for all its tiles of `per` rows
 // and needs no table.  Finds the sequence of a place (all lanes of a wavefront together), 64 offsets at a time.

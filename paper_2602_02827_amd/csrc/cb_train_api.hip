@@ -18,8 +18,9 @@ AttnPlan plan_attention(const AttnArgs& A, int d, int dt, bool backward) {
     P.units = A.heads / A.pack;
     // Columns of a mean sequence: short ones get workgroups of one wavefront.
     const int64_t q_cols = (int64_t)A.total_q * A.pack / A.n_seqs, k_rows = A.total_k / A.n_seqs;
-    P.q_waves = q_cols <= 32 ? 1 : 4;
-    P.k_waves = k_rows <= 32 ? 1 : 4;
+    const bool single = !backward || dt == TR_BF16 || d <= 64;       // (kSingle)
+    P.q_waves = q_cols <= 32 && single ? 1 : 4;
+    P.k_waves = k_rows <= 32 && single ? 1 : 4;
     P.q_slots = A.total_q / (32 * P.q_waves / A.pack) + A.n_seqs;
     P.k_slots = A.total_k / (32 * P.k_waves) + A.n_seqs;
     P.splits = 1;
