@@ -83,9 +83,9 @@ template <class E, int D> struct Column {
 };
 
 // Two matrices' rows on their way to tiles in LDS.  What a mask hides may be anything: zeros are written in its place.
-template <class E, int D, int THREADS, bool MASKED> struct Staged {
-    using T = Tile<E, D>;
-    using R = Rows<E, D, THREADS>;
+template <class E, int D, int THREADS, bool MASKED, int ROWS> struct Staged {
+    using T = Tile<E, D, ROWS>;
+    using R = Rows<E, D, THREADS, ROWS>;
     R x, y;
     uint8_t keep[MASKED ? R::N : 1];
     // a_at(row), b_at(row): byte offsets of the matrices' rows; kept(row): whether the mask leaves it.  rows: how many are left.
@@ -168,8 +168,11 @@ __device__ __forceinline__ f32x16 of_rows(const float* v, int b, int h) {
 
 // Wavefronts per SIMD that the registers are shared out for (one more each makes the compiler spill, and is slower; forward
 // pass, 512 passages, three and four: 152 and 176 us; gradients, two and three: 764 and 851 us).
-template <class E, int D> constexpr int kWaves = sizeof(E) == 2 ? (D <= 64 ? 3 : 2) : D <= 32 ? 3 : D <= 96 ? 2 : 1;
+template <class E, int D> constexpr int kWaves = sizeof(E) == 2 || D <= 32 ? 3 : D <= 96 ? 2 : 1;
 template <class E, int D> constexpr int kGradientWaves = sizeof(E) == 2 || D <= 32 ? 2 : 1;
+// Key rows of the forward pass's tiles: of wide heads 32, so that LDS holds three workgroups (48 pages of 1,030 rows, d = 128: 608
+// us, with 64 rows and two 640; the gradients' kernels, which have registers for two, lose by it).
+template <class E, int D> constexpr int kForwardRows = D >= 96 ? 32 : Oper<E>::ROWS;
 // Wide heads take all registers: their workgroups do not go on to the next one, and their gradients in 32 bits are not made by
 // single wavefronts, which would hold a whole tile on its way in registers as well.
 template <int D> constexpr bool kRuns = D <= 64;
@@ -186,9 +189,9 @@ template <class E, int D, int NW, bool BIAS, bool MASKED>
 __global__ __launch_bounds__(64 * NW, (kWaves<E, D>)) void k_attention(const AttnArgs A, int slots, int units, int run, int splits, E* out, float* lse,
                                                           float* o_part, float2* ml_part) {
     using O = Oper<E>;
-    using T = Tile<E, D>;
+    using T = Tile<E, D, kForwardRows<E, D>>;
     constexpr int NB = T::ROWS / 32, DB = D / 32, THREADS = 64 * NW;
-    __shared__ __align__(16) char lds[2][2 * T::BYTES];
+    __shared__ __align__(256) char lds[2][2 * T::BYTES];
     __shared__ __align__(16) float hidden[2][T::ROWS];           // 0, or minus infinity for rows that no column sees
     extern __shared__ __align__(16) char dyn[];
     const int tid = threadIdx.x, lane0 = tid & 63, lane = lane0, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
@@ -204,7 +207,7 @@ __global__ __launch_bounds__(64 * NW, (kWaves<E, D>)) void k_attention(const Att
     const int first_tile = split * each, end_tile = first_tile + each < tiles ? first_tile + each : tiles;
 
     const int64_t krow = A.k_row * (int64_t)sizeof(E), vrow = A.v_row * (int64_t)sizeof(E);
-    Staged<E, D, THREADS, MASKED> next;
+    Staged<E, D, THREADS, MASKED, T::ROWS> next;
     uint8_t next_keep = 0;
     auto issue = [&](int u, int base, char* to) {
         const int kv = u * G / A.group;
@@ -245,16 +248,16 @@ __global__ __launch_bounds__(64 * NW, (kWaves<E, D>)) void k_attention(const Att
     const float scale2 = scale_of_scores(A.scale);
     if (any) finish(0);
     __syncthreads();
+    const typename T::At at_tiles(lds[0], lane);
     int i = first_tile, buf = 0;
     while (true) {
         const int base = i * T::ROWS;
-        const char *lk = lds[buf], *lv = lk + T::BYTES;
+        const typename T::At lk = at_tiles + buf * 2 * T::BYTES, lv = lk + T::BYTES;
         const bool last = i + 1 >= end_tile;                     // of the unit
         const int n_unit = last ? unit + 1 : unit, n_i = last ? first_tile : i + 1;
         const bool more = kRuns<D> ? n_unit < end_unit : !last;
         if (more && any) issue(n_unit, n_i * T::ROWS, lds[buf ^ 1]);
         if (any && w.busy && base < w.end) {
-            const int lane = here(lane0), h = lane >> 5;
             const bool one = NB > 1 && base + 32 >= w.end;       // its second block has no keys
             const bool diagonal = A.causal && base + T::ROWS - 1 > w.first_lim, part = seen != kAllRows;
             if constexpr (MASKED) {
@@ -268,7 +271,7 @@ __global__ __launch_bounds__(64 * NW, (kWaves<E, D>)) void k_attention(const Att
                 if (b && one) break;
                 s[b] = {};
 #pragma unroll
-                for (int c = 0; c < D / 16; ++c) O::mma(s[b], T::rows(lk, lane, b, c), q.v[c]);
+                for (int c = 0; c < D / 16; ++c) O::mma(s[b], T::rows(lk, b, c), q.v[c]);
                 if constexpr (BIAS) {
                     const int d0 = base + 32 * b - w.first_lim, side = block_side(d0, A.reach);
                     if (side) {
@@ -312,9 +315,9 @@ __global__ __launch_bounds__(64 * NW, (kWaves<E, D>)) void k_attention(const Att
                 }
                 const typename O::Frag p0 = O::round(eight<0>(s[b])), p1 = O::round(eight<8>(s[b]));
 #pragma unroll
-                for (int db = 0; db < DB; ++db) O::mma(acc[db], T::turned(lv, lane, b, 0, db), p0);
+                for (int db = 0; db < DB; ++db) O::mma(acc[db], T::turned(lv, b, 0, db), p0);
 #pragma unroll
-                for (int db = 0; db < DB; ++db) O::mma(acc[db], T::turned(lv, lane, b, 1, db), p1);
+                for (int db = 0; db < DB; ++db) O::mma(acc[db], T::turned(lv, b, 1, db), p1);
             }
         }
         if (last) {
@@ -461,7 +464,7 @@ __global__ __launch_bounds__(64 * NW, (kGradientWaves<E, D>)) void k_attention_d
     using O = Oper<E>;
     using T = Tile<E, D>;
     constexpr int NB = T::ROWS / 32, DB = D / 32, THREADS = 64 * NW;
-    __shared__ __align__(16) char lds[2][2 * T::BYTES];
+    __shared__ __align__(256) char lds[2][2 * T::BYTES];
     __shared__ __align__(16) float diagonals[BIAS ? NW * kDiagonal : 1];
     __shared__ __align__(16) float hidden[2][T::ROWS];
     __shared__ float far_sum[kMostRun][NW][2];
@@ -482,7 +485,7 @@ __global__ __launch_bounds__(64 * NW, (kGradientWaves<E, D>)) void k_attention_d
     const QueryColumns w(A, t, G, per, wave, lane);
     const int tiles = (t.end + T::ROWS - 1) / T::ROWS;
     const int64_t krow = A.k_row * (int64_t)sizeof(E), vrow = A.v_row * (int64_t)sizeof(E);
-    Staged<E, D, THREADS, MASKED> next;
+    Staged<E, D, THREADS, MASKED, T::ROWS> next;
     uint8_t next_keep = 0;
     auto issue = [&](int u, int base, char* to) {
         const int kv = u * G / A.group;
@@ -550,27 +553,27 @@ __global__ __launch_bounds__(64 * NW, (kGradientWaves<E, D>)) void k_attention_d
     const float scale2 = scale_of_scores(A.scale);
     if (any) finish(0);
     __syncthreads();
+    const typename T::At at_tiles(lds[0], lane);
     int i = 0, buf = 0;
     while (true) {
         const int base = i * T::ROWS;
-        const char *lk = lds[buf], *lv = lk + T::BYTES;
+        const typename T::At lk = at_tiles + buf * 2 * T::BYTES, lv = lk + T::BYTES;
         const bool last = i + 1 >= tiles;
         const int n_unit = last ? unit + 1 : unit, n_i = last ? 0 : i + 1;
         const bool more = kRuns<D> ? n_unit < end_unit : !last;
         if (more && any) issue(n_unit, n_i * T::ROWS, lds[buf ^ 1]);
         if (any && w.busy && base < w.end) {
-            const int lane = here(lane0), h = lane >> 5;
             const bool diagonal = A.causal && base + T::ROWS - 1 > w.first_lim, part = seen != kAllRows;
 #pragma unroll 1
             for (int b = 0; b < NB && base + 32 * b < w.end; ++b) {
                 f32x16 s = {}, dp;
 #pragma unroll
-                for (int c = 0; c < D / 16; ++c) O::mma(s, T::rows(lk, lane, b, c), q.v[c]);
+                for (int c = 0; c < D / 16; ++c) O::mma(s, T::rows(lk, b, c), q.v[c]);
                 phase();
 #pragma unroll
                 for (int r = 0; r < 16; ++r) dp[r] = -dot;
 #pragma unroll
-                for (int c = 0; c < D / 16; ++c) O::mma(dp, T::rows(lv, lane, b, c), g.v[c]);
+                for (int c = 0; c < D / 16; ++c) O::mma(dp, T::rows(lv, b, c), g.v[c]);
                 phase();
                 const int d0 = base + 32 * b - w.first_lim, side = BIAS ? block_side(d0, A.reach) : 0;
                 if (BIAS && !side) {
@@ -622,16 +625,16 @@ __global__ __launch_bounds__(64 * NW, (kGradientWaves<E, D>)) void k_attention_d
                         const typename O::Frag p = O::round(most), rest = O::round(x - most);
 #pragma unroll
                         for (int db = 0; db < DB; ++db) {
-                            const typename O::Frag k = T::turned(lk, lane, b, c, db);
+                            const typename O::Frag k = T::turned(lk, b, c, db);
                             O::mma(acc[db], k, rest);
                             O::mma(acc[db], k, p);
                         }
                     }
                 } else {
 #pragma unroll
-                    for (int db = 0; db < DB; ++db) O::mma(acc[db], T::turned(lk, lane, b, 0, db), O::round(eight<0>(s)));
+                    for (int db = 0; db < DB; ++db) O::mma(acc[db], T::turned(lk, b, 0, db), O::round(eight<0>(s)));
 #pragma unroll
-                    for (int db = 0; db < DB; ++db) O::mma(acc[db], T::turned(lk, lane, b, 1, db), O::round(eight<8>(s)));
+                    for (int db = 0; db < DB; ++db) O::mma(acc[db], T::turned(lk, b, 1, db), O::round(eight<8>(s)));
                 }
             }
         }
@@ -726,7 +729,7 @@ __global__ __launch_bounds__((kApart<E, D> ? 128 : 64) * NW, (kGradientWaves<E, 
     constexpr bool APART = kApart<E, D>;
     constexpr int WAVES = APART ? 2 * NW : NW, THREADS = 64 * WAVES;
     const bool keys = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) >= NW;        // (APART) this wavefront has the keys' gradient
-    __shared__ __align__(16) char lds[2][2 * T::BYTES];
+    __shared__ __align__(256) char lds[2][2 * T::BYTES];
     __shared__ __align__(16) float row_lse[2][T::ROWS], row_delta[2][T::ROWS];
     extern __shared__ __align__(16) char dyn[];
     const int tid = threadIdx.x, lane0 = tid & 63, lane = lane0, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
@@ -761,7 +764,7 @@ __global__ __launch_bounds__((kApart<E, D> ? 128 : 64) * NW, (kGradientWaves<E, 
     const int64_t grow = (int64_t)A.heads * D * (int64_t)sizeof(E), ghead = D * (int64_t)sizeof(E);
     const char* qp = (const char*)A.q + qs.lo * qrow;
     const char* gp = (const char*)dout + qs.lo * grow;
-    Staged<E, D, THREADS, MASKED> next;
+    Staged<E, D, THREADS, MASKED, T::ROWS> next;
     float n_lse = 0.f, n_delta = 0.f;
     const float scale2 = scale_of_scores(A.scale);
     // 16 bits: a row's log-sum-exp and delta are what its accumulators start from (in 32 bits that would cost the scores an
@@ -821,6 +824,7 @@ __global__ __launch_bounds__((kApart<E, D> ? 128 : 64) * NW, (kGradientWaves<E, 
     }
     if (any) finish(0);
     __syncthreads();
+    const typename T::At at_tiles(lds[0], lane);
     int buf = 0;
     while (true) {
         const bool last_tile = c0 + T::ROWS >= cols;
@@ -828,22 +832,21 @@ __global__ __launch_bounds__((kApart<E, D> ? 128 : 64) * NW, (kGradientWaves<E, 
         const bool last = last_tile && n_head % A.group == 0;                           // of a key head
         const bool more = kRuns<D> ? n_head < head_end : !last;
         if (more && any) issue(n_head, n_c, lds[buf ^ 1]);
-        const char *lq = lds[buf], *lg = lq + T::BYTES;
+        const typename T::At lq = at_tiles + buf * 2 * T::BYTES, lg = lq + T::BYTES;
         if (any && busy && c0 + T::ROWS > wfirst) {
-            const int lane = here(lane0), h = lane >> 5;
             const bool diagonal = A.causal && (wkey + 31 - shift) * G > c0;
-            const char* own = APART && !keys ? lg : lq;           // (own gradient's other operand)
+            const typename T::At own = APART && !keys ? lg : lq;           // (own gradient's other operand)
 #pragma unroll 1
             for (int b = 0; b < NB && c0 + 32 * b < cols; ++b) {
                 f32x16 s = {}, dp = {};
                 if constexpr (START) s = of_rows(row_lse[buf], b, h);
 #pragma unroll
-                for (int c = 0; c < D / 16; ++c) O::mma(s, T::rows(lq, lane, b, c), k.v[c]);
+                for (int c = 0; c < D / 16; ++c) O::mma(s, T::rows(lq, b, c), k.v[c]);
                 phase();
                 if (!APART || keys) {
                     if constexpr (START) dp = of_rows(row_delta[buf], b, h);
 #pragma unroll
-                    for (int c = 0; c < D / 16; ++c) O::mma(dp, T::rows(lg, lane, b, c), v.v[c]);
+                    for (int c = 0; c < D / 16; ++c) O::mma(dp, T::rows(lg, b, c), v.v[c]);
                     phase();
                 }
                 if constexpr (!START) {
@@ -872,18 +875,18 @@ __global__ __launch_bounds__((kApart<E, D> ? 128 : 64) * NW, (kGradientWaves<E, 
                     const typename O::Frag p0 = O::round(eight<0>(s)), p1 = O::round(eight<8>(s));
                     phase();
 #pragma unroll
-                    for (int db = 0; db < DB; ++db) O::mma(acc2[db], T::turned(lg, lane, b, 0, db), p0);
+                    for (int db = 0; db < DB; ++db) O::mma(acc2[db], T::turned(lg, b, 0, db), p0);
 #pragma unroll
-                    for (int db = 0; db < DB; ++db) O::mma(acc2[db], T::turned(lg, lane, b, 1, db), p1);
+                    for (int db = 0; db < DB; ++db) O::mma(acc2[db], T::turned(lg, b, 1, db), p1);
                     phase();
                 }
                 if (!APART || keys) s *= dp;
                 const typename O::Frag p0 = O::round(eight<0>(s)), p1 = O::round(eight<8>(s));
                 phase();
 #pragma unroll
-                for (int db = 0; db < DB; ++db) O::mma(acc[db], T::turned(own, lane, b, 0, db), p0);
+                for (int db = 0; db < DB; ++db) O::mma(acc[db], T::turned(own, b, 0, db), p0);
 #pragma unroll
-                for (int db = 0; db < DB; ++db) O::mma(acc[db], T::turned(own, lane, b, 1, db), p1);
+                for (int db = 0; db < DB; ++db) O::mma(acc[db], T::turned(own, b, 1, db), p1);
             }
         }
         if (last) {

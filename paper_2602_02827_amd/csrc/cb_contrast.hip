@@ -17,7 +17,7 @@ __global__ __launch_bounds__(256, (sizeof(E) == 4 && D == 128 ? 1 : 2)) void k_m
     using O = Oper<E>;
     using L = Tile<E, D>;
     constexpr int NB = L::ROWS / 32;
-    __shared__ __align__(16) char tile[2][L::BYTES];
+    __shared__ __align__(256) char tile[2][L::BYTES];
     __shared__ float cells[2][128 * CT];
     const int tid = threadIdx.x, lane0 = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane0 & 31, h = lane0 >> 5;
     const int group = blockIdx.x % col_groups, part = blockIdx.x / col_groups;
@@ -44,6 +44,7 @@ __global__ __launch_bounds__(256, (sizeof(E) == 4 && D == 128 ? 1 : 2)) void k_m
     }
     float best[CT];
     int where[CT];
+    const typename L::At at_tile(tile[0], lane0);
     int i = doc0, base = 0, buf = 0;
     if (r.n) finish(tile[0]);
     __syncthreads();
@@ -61,17 +62,17 @@ __global__ __launch_bounds__(256, (sizeof(E) == 4 && D == 128 ? 1 : 2)) void k_m
             }
         }
         if (wave * CT * 32 < cols) {
-            const int lane = here(lane0);
+            const typename L::At t = at_tile + buf * L::BYTES;
 #pragma unroll 1
             for (int b = 0; b < NB && base + 32 * b < r.n; ++b) {
                 f32x16 s[CT] = {};
 #pragma unroll
                 for (int c = 0; c < D / 16; ++c) {
-                    const typename O::Frag a = L::rows(tile[buf], lane, b, c);
+                    const typename O::Frag a = L::rows(t, b, c);
 #pragma unroll
                     for (int ct = 0; ct < CT; ++ct) O::mma(s[ct], a, q[ct][c]);
                 }
-                const int at = base + 32 * b + 4 * (lane >> 5), room = r.n - at;
+                const int at = base + 32 * b + 4 * h, room = r.n - at;
                 if (base + 32 * b + 32 > r.n) {
 #pragma unroll
                     for (int ct = 0; ct < CT; ++ct)

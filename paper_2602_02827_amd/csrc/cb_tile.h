@@ -76,44 +76,63 @@ template <> struct Oper<float> {
 // ROWS rows of D values in LDS, as 16-byte pieces of bf16.  A piece's place in its row is turned by the row's low bits.  256 bytes
 // are read a clock: sixteen rows' pieces of one column (row operands) lie in different banks, and so do the four rows of 64 bytes
 // that half a wavefront takes of a turned operand (128-byte and 256-byte rows: by the turn's upper bits; the others by their pitch).
+// All that a lane's places differ by is then a constant, added or (below 256, tiles are aligned to that) toggled.
 template <int ROWS, int D> struct Plane {
     static constexpr int PITCH = 2 * D, PIECES = PITCH / 16, BYTES = ROWS * PITCH;
+    static constexpr bool POWER = (PIECES & (PIECES - 1)) == 0;
     static __device__ __forceinline__ int turn(int row) {
         if constexpr (PIECES % 16 == 0) return ((row & 3) << 2) | ((row >> 2) & 3);
         if constexpr (PIECES % 8 == 0) return ((row & 2) << 1) | ((row >> 2) & 3);
         return (row >> 2) & 3;
     }
     static __device__ __forceinline__ int at(int row, int piece) { return row * PITCH + ((piece ^ turn(row)) << 4); }
-    static __device__ __forceinline__ int row_place(int lane, int b, int c) { return at(32 * b + (lane & 31), 2 * c + (lane >> 5)); }
-    // (sixteen lanes read four rows of sixteen values and get a column of four each; eight rows on for the other four)
-    static __device__ __forceinline__ int turned_place(int lane, int b, int c, int db, int half) {
-        const int row = 32 * b + 16 * c + 8 * half + 4 * (lane >> 5) + ((lane & 15) >> 2);
-        return at(row, 4 * db + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) + (lane & 1) * 8;
+    // row operands: row n, piece 2c + h
+    static __device__ __forceinline__ uint32_t row_place(int lane) { return (uint32_t)at(lane & 31, lane >> 5); }
+    static __device__ __forceinline__ uint32_t row_place(uint32_t p, int b, int c) {
+        return (p ^ (uint32_t)((POWER ? c : c & 1) << 5)) + (uint32_t)(32 * b * PITCH + (POWER ? 0 : (c >> 1) * 64));
     }
-    static __device__ __forceinline__ bf16x8 turned(const char* t, int x, int y) {
-        using L = __attribute__((address_space(3))) i16x4;
-        const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)(t + x)), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)(t + y));
-        const auto both = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-        return __builtin_bit_cast(bf16x8, both);
+    // turned operands: sixteen lanes read four rows of sixteen values and get a column of four each; eight rows on for the other four
+    static __device__ __forceinline__ uint32_t turned_place(int lane) {
+        return (uint32_t)(at(4 * (lane >> 5) + ((lane & 15) >> 2), ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) + (lane & 1) * 8);
+    }
+    static __device__ __forceinline__ uint32_t turned_place(uint32_t p, int b, int c, int db, int half) {
+        return (p ^ (uint32_t)((half << 5) | (POWER ? db << 6 : 0))) + (uint32_t)((32 * b + 16 * c + 8 * half) * PITCH + (POWER ? 0 : db * 64));
     }
 };
-// A tile: one plane, or one of each piece.
-template <class E, int D> struct Tile {
+using lds_ptr = uint32_t;                             // an address in LDS
+__device__ __forceinline__ lds_ptr in_lds(const void* p) { return (lds_ptr)(uintptr_t)(const __attribute__((address_space(3))) char*)p; }
+__device__ __forceinline__ bf16x8 read_row(lds_ptr p) { return *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)p; }
+__device__ __forceinline__ bf16x8 read_turned(lds_ptr p, lds_ptr q) {
+    using L = __attribute__((address_space(3))) i16x4;
+    const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)(uintptr_t)p), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)(uintptr_t)q);
+    const auto both = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    return __builtin_bit_cast(bf16x8, both);
+}
+
+// A tile: one plane, or one of each piece.  R rows of it.
+template <class E, int D, int R = Oper<E>::ROWS> struct Tile {
     using Frag = typename Oper<E>::Frag;
-    static constexpr int ROWS = Oper<E>::ROWS, PLANES = sizeof(E) == 2 ? 1 : 3;
+    static constexpr int ROWS = R, PLANES = sizeof(E) == 2 ? 1 : 3;
     using P = Plane<ROWS, D>;
     static constexpr int PIECES = P::PIECES, BYTES = PLANES * P::BYTES;
+    // a lane's places in a tile
+    struct At {
+        lds_ptr row, turned;
+        __device__ __forceinline__ At(const char* t, int lane) : row(in_lds(t) + P::row_place(lane)), turned(in_lds(t) + P::turned_place(lane)) {}
+        __device__ __forceinline__ At(lds_ptr r, lds_ptr u) : row(r), turned(u) {}
+        __device__ __forceinline__ At operator+(int bytes) const { return At(row + bytes, turned + bytes); }
+    };
     // rows 32b .. 32b+31, elements 16c .. 16c+15 of each
-    static __device__ __forceinline__ Frag rows(const char* t, int lane, int b, int c) {
-        const char* p = t + P::row_place(lane, b, c);
-        if constexpr (PLANES == 1) return *(const bf16x8*)p;
-        else return {{*(const bf16x8*)p, *(const bf16x8*)(p + P::BYTES), *(const bf16x8*)(p + 2 * P::BYTES)}};
+    static __device__ __forceinline__ Frag rows(const At& t, int b, int c) {
+        const lds_ptr p = P::row_place(t.row, b, c);
+        if constexpr (PLANES == 1) return read_row(p);
+        else return {{read_row(p), read_row(p + P::BYTES), read_row(p + 2 * P::BYTES)}};
     }
     // columns 32db .. 32db+31 of the rows 32b + 16c .. +15, in the accumulators' order
-    static __device__ __forceinline__ Frag turned(const char* t, int lane, int b, int c, int db) {
-        const int x = P::turned_place(lane, b, c, db, 0), y = P::turned_place(lane, b, c, db, 1);
-        if constexpr (PLANES == 1) return P::turned(t, x, y);
-        else return {{P::turned(t, x, y), P::turned(t + P::BYTES, x, y), P::turned(t + 2 * P::BYTES, x, y)}};
+    static __device__ __forceinline__ Frag turned(const At& t, int b, int c, int db) {
+        const lds_ptr x = P::turned_place(t.turned, b, c, db, 0), y = P::turned_place(t.turned, b, c, db, 1);
+        if constexpr (PLANES == 1) return read_turned(x, y);
+        else return {{read_turned(x, y), read_turned(x + P::BYTES, y + P::BYTES), read_turned(x + 2 * P::BYTES, y + 2 * P::BYTES)}};
     }
 };
 
@@ -152,19 +171,21 @@ __device__ __forceinline__ void wait_for_copies() { asm volatile("s_waitcnt vmcn
 // A matrix's rows on their way to a tile in LDS, a tile ahead of its use, rows past the end as the last row again.  16 bits: by the
 // memory unit itself.  32 bits: they wait in registers, and are cut into their pieces as they are written.
 // at(row): byte offset of a row; whole(i): whether the i-th piece of this thread is kept (zeros otherwise).
-template <class E, int D, int THREADS> struct Rows {
-    using T = Tile<E, D>;
+template <class E, int D, int THREADS, int R = Oper<E>::ROWS> struct Rows {
+    using T = Tile<E, D, R>;
     static constexpr int ALL = T::ROWS * T::PIECES, N = (ALL + THREADS - 1) / THREADS;
     static constexpr bool DIRECT = sizeof(E) == 2;
     f32x4 x[DIRECT ? 1 : N][2];
     static __device__ __forceinline__ int row(int i, int tid) { return (i * THREADS + tid) / T::PIECES; }
+    static __device__ __forceinline__ uint32_t piece(int i, int tid) {
+        return (uint32_t)(((i * THREADS + tid) % T::PIECES ^ T::P::turn(row(i, tid))) * 8 * (int)sizeof(E));
+    }
     template <class At> __device__ __forceinline__ void issue(const char* a, char* lds, int rows, int tid, int wave, At&& at) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             if (ALL % THREADS && i * THREADS + wave * 64 >= ALL) break;          // of the wavefront
-            const int pos = i * THREADS + tid, place = row(i, tid);
-            const char* src = a + (at(place < rows ? place : rows - 1) +
-                                   (uint32_t)((pos % T::PIECES ^ T::P::turn(place)) * 8 * (int)sizeof(E)));
+            const int place = row(i, tid);
+            const char* src = a + (at(place < rows ? place : rows - 1) + piece(i, tid));
             if constexpr (DIRECT) {
                 copy_to_lds(src, lds + (i * THREADS + wave * 64) * 16);
             } else {
