@@ -12,7 +12,7 @@ namespace cb {
 // its documents through LDS, the next tile on its way while it multiplies.  A column's running maximum and its place stay in the
 // column's two lanes; a comparison, and two selections of it, for every product (the place within a block is a constant).
 template <class E, int D, int CT>
-__global__ __launch_bounds__(256, (sizeof(E) == 4 && D == 128 ? 1 : 2)) void k_maxsim_train(const E* Q, int nq, int T, const E* docs, const int64_t* off, int N, int total,
+__global__ __launch_bounds__(256, (sizeof(E) == 4 ? (D == 128 ? 1 : 2) : 4)) void k_maxsim_train(const E* Q, int nq, int T, const E* docs, const int64_t* off, int N, int total,
                                                          int col_groups, int q_per, int docs_per, float* scores, int32_t* argmax) {
     using O = Oper<E>;
     using L = Tile<E, D>;
@@ -199,8 +199,9 @@ template <class E, int D> struct RowLanes {
     }
 };
 
-// Queries: a row is the weighted sum of one token of every document.  A workgroup has one query token; the documents are split
-// over its lane groups, whose sums are added in their order.
+// Queries: a row is the weighted sum of one token of every document.  A workgroup has one query token; its lane groups take the
+// documents in turn (all workgroups go through the corpus together, so its rows are found in L2), and their sums are added in
+// order.
 template <class E, int D>
 __device__ __forceinline__ void query_gradient(char* lds, int block, const float* dscores, const int32_t* argmax, int T, const E* docs,
                                                const int64_t* off, int N, int total, E* dQ) {
@@ -209,22 +210,22 @@ __device__ __forceinline__ void query_gradient(char* lds, int block, const float
     float* sums = (float*)lds;                       // [PARTS][WIDTH]
     const int tid = threadIdx.x, piece = tid % R::LANES, part = tid / R::LANES;
     const int q = block / T, t = block % T;
-    const int each = (N + PARTS - 1) / PARTS, i0 = part * each, i1 = N - i0 < each ? N : i0 + each;
     float acc[R::PER] = {};
     if (piece < R::PIECES) {
         const int32_t* a = argmax + (int64_t)q * N * T + t;
         const float* g = dscores + (int64_t)q * N;
-        for (int i = i0; i < i1; i += AHEAD) {
+        for (int first = part; first < N; first += PARTS * AHEAD) {
             u32x4 x[AHEAD];
             float w[AHEAD];
 #pragma unroll
             for (int j = 0; j < AHEAD; ++j) {
                 x[j] = u32x4{0u, 0u, 0u, 0u};
                 w[j] = 0.f;
-                if (i + j < i1) {
-                    const int64_t at = a[(int64_t)(i + j) * T], row = off[i + j] + at;
+                const int i = first + j * PARTS;
+                if (i < N) {
+                    const int64_t at = a[(int64_t)i * T], row = off[i] + at;
                     if (at >= 0 && row >= 0 && row < total) {
-                        w[j] = g[i + j];
+                        w[j] = g[i];
                         x[j] = *(const u32x4*)((const char*)(docs + row * D) + piece * 16);
                     }
                 }
@@ -390,7 +391,7 @@ __device__ __forceinline__ void document_gradient(char* lds, int block, const fl
 
 // One launch for both: the first workgroups take documents, which take longer.
 template <class E, int D, bool MANY>
-__global__ __launch_bounds__(256) void k_maxsim_gradients(const float* dscores, const int32_t* argmax, const E* Q, int nq, int T,
+__global__ __launch_bounds__(256, 4) void k_maxsim_gradients(const float* dscores, const int32_t* argmax, const E* Q, int nq, int T,
                                                           const E* docs, const int64_t* off, int N, int total, int doc_blocks, E* dQ,
                                                           E* ddocs) {
     constexpr size_t SUMS = sizeof(float) * (256 / RowLanes<E, D>::LANES) * RowLanes<E, D>::LANES * RowLanes<E, D>::PER;
