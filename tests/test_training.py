@@ -280,6 +280,59 @@ def test_strides_of_a_packed_projection_and_of_heads_first(tr, dev, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("heads", [4, 2])
+def test_rows_and_heads_beyond_32_bits(tr, dev, heads):
+    """Rows 16 MiB apart and heads 3 GiB apart (packed heads' rows are addressed from their tile's first one in 32 bits: these are
+    too far apart for that), so that offsets pass 2^32 bytes."""
+    ql, H, Hk, d = [140, 60], heads, 2, 64
+    n = sum(ql)
+    p = problem(dev, "bf16", ql, ql, H, Hk, d, seed=16)
+    want, want_grads = attend(tr, p, ql, ql, causal=True)
+    room = torch.empty(H * (n << 23), dtype=torch.bfloat16, device=dev)
+    for order in ("rows", "heads"):
+        row, head = (1 << 23, d) if order == "rows" else (H * d, n << 23)
+        for x in "qkv":
+            far = dict(p)
+            far[x] = torch.as_strided(room, p[x].shape, (row, head, 1))
+            far[x].copy_(p[x])
+            f, b = attend(tr, far, ql, ql, causal=True)
+            for name in ("out", "lse"):
+                assert torch.equal(f[name], want[name]), (order, x, name)
+            if order == "rows" or x != "q" or H == Hk:          # (else other tiles, which add in another order)
+                for name in ("dq", "dk", "dv"):
+                    assert torch.equal(b[name], want_grads[name]), (order, x, name)
+
+
+@gpu
+@pytest.mark.parametrize("wild", [[0, 1 << 40, 90], [-7, 50, 1 << 40], [80, 20, 60], [0, 0, 0]])
+def test_offsets_that_are_none_stay_in_bounds(tr, dev, wild):
+    """The kernels clamp them to the tensors; results mean nothing, neighbours in memory stay as they are."""
+    ql = [40, 50]
+    p = problem(dev, "bf16", ql, ql, 2, 2, 32, seed=17, bias=8, keep=True)
+    off, how = torch.tensor(wild, device=dev), dict(keep=p["keep"], bias=p["bias"])
+    guard = torch.full((3, 90, 2, 32), 7.0, dtype=torch.bfloat16, device=dev)
+    lse = torch.zeros(2, 90, device=dev)
+    tr.colbandit_attention(p["q"], p["k"], p["v"], off, out={"out": guard[1], "lse": lse}, **how)
+    b = tr.colbandit_attention_backward(p["dout"], p["q"], p["k"], p["v"], guard[1], lse, off, **how)
+    Q, D, _ = embeddings(dev, "f32", 3, 7, [90], 32)
+    f = tr.colbandit_maxsim_scores(Q, D, off)
+    g = tr.colbandit_maxsim_backward(f["scores"].nan_to_num(), f["argmax"], Q, D, off)
+    torch.cuda.synchronize()
+    assert bool((guard[0] == 7).all()) and bool((guard[2] == 7).all()) and b["dq"].shape == p["q"].shape and g["dQ"].shape == Q.shape
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [0.0, -0.3, 1e-20, 5.0])
+def test_scales_of_any_sign_and_size(tr, dev, dtype, scale):
+    """The products' sign is the columns', a scale of zero leaves only the bias; 5 makes rows that are nearly one key (scores up to
+    80, whose 32-bit rounding is 2.5 times that of the bound's 32)."""
+    ql = [70, 33]
+    p = problem(dev, dtype, ql, ql, 2, 2, 32, seed=18, bias=8, size=0.4 if scale == 5.0 else 1.0)
+    check_attention(tr, p, ql, ql, dtype, scale=scale)
+
+
+@gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("wild", [math.nan, math.inf, -math.inf, "lowest"])
 def test_masked_keys_may_hold_anything(tr, dev, dtype, wild):
@@ -632,6 +685,20 @@ def test_loss_and_clipping_in_graphs(tr, dev):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+# ---- together --------------------------------------------------------------------------------------------
+
+@gpu
+def test_fine_tuning_an_encoder(tr, dev):
+    """The operators as a program uses them: the loss falls to less than half, more queries find their document, and the same
+    seed gives the same losses."""
+    from paper_2602_02827_amd import finetune
+    r = finetune.train(steps=40, n_docs=128)
+    assert all(math.isfinite(x) for x in r["losses"] + r["norms"])
+    assert sum(r["losses"][-5:]) < 0.5 * sum(r["losses"][:5]), r["losses"]
+    assert r["after"] > r["before"]
+    assert finetune.train(steps=3, n_docs=128)["losses"] == r["losses"][:3]
 
 
 # ---- boundary --------------------------------------------------------------------------------------------
