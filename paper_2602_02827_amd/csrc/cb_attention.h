@@ -51,12 +51,27 @@ __device__ __forceinline__ void fill_bias(const AttnArgs& A, int head, const int
 constexpr int kStartsBytes = 272;                     // of up to 129
 __host__ __forceinline__ size_t bias_bytes(int reach, int tables) { return kStartsBytes + 4 * (size_t)(tables * bias_width(reach)); }
 
-// Workgroups are dealt to the eight XCDs in turn; numbered so that each XCD has runs of consecutive ones (64, or as many as
-// leave each eight runs, so that long sequences are spread), the tiles that share keys read them through one L2.
+// Places of tiles, in the order in which workgroups (and what each has several of: `inner`) take them.
+// BY_XCD: workgroups are dealt to the eight XCDs in turn; numbered so that each XCD has runs of consecutive ones (64, or as many as
+// leave each eight runs), the heads of a short sequence, whose values lie side by side, are read through one L2.
+// LONGEST_FIRST: under a causal limit the later rows see more keys (earlier keys are seen by more rows): places go round the
+// sequences, each one's longest tiles first (`down`: its last ones), so that short ones are left for the end.  Sequences are taken
+// to be of one length; others are only in another order.
 __device__ __forceinline__ int in_order(int block, int blocks) {
     const int lg = blocks < 128 ? 0 : blocks >= 4096 ? 6 : 25 - __builtin_clz(blocks);
     const int whole = blocks >> (lg + 3) << (lg + 3), xcd = block & 7, i = block >> 3;
     return block < whole ? (((i >> lg) * 8 + xcd) << lg) + (i & ((1 << lg) - 1)) : block;
+}
+__device__ __forceinline__ int longest_first(int x, int slots, int n, bool down) {
+    const int f = slots / n, rest = slots - f * n, j = x / n;      // sequence i has the places from i f + floor(i rest / n)
+    int i = x - j * n;
+    if (j >= f) i = (int)(((int64_t)(x - f * n + 1) * n + rest - 1) / rest) - 1;      // of those with one more
+    return i * f + (int)((int64_t)i * rest / n) + (down && j < f ? f - 1 - j : j);
+}
+struct Work { int slot, inner; };
+__device__ __forceinline__ Work work_of(int block, int slots, int inner, int n, int order, bool down) {
+    const int x = order == BY_XCD ? in_order(block, slots * inner) : block, slot = x / inner;
+    return {order == LONGEST_FIRST ? longest_first(slot, slots, n, down) : slot, x - slot * inner};
 }
 // Which way a block of 32 rows and columns lies whose first key and row are d0 apart: -1 or 1: all beyond reach, 0: not.
 __device__ __forceinline__ int block_side(int d0, int reach) { return d0 + 31 <= -reach ? -1 : d0 - 31 >= reach ? 1 : 0; }
@@ -167,9 +182,10 @@ __device__ __forceinline__ f32x16 of_rows(const float* v, int b, int h) {
 }
 
 // Wavefronts per SIMD that the registers are shared out for (one more each makes the compiler spill, and is slower; forward
-// pass, 512 passages, three and four: 152 and 176 us; gradients, two and three: 764 and 851 us).
-template <class E, int D> constexpr int kWaves = sizeof(E) == 2 || D <= 32 ? 3 : D <= 96 ? 2 : 1;
-template <class E, int D> constexpr int kGradientWaves = sizeof(E) == 2 || D <= 32 ? 2 : 1;
+// pass, 512 passages, three and four: 152 and 176 us; gradients, two and three: 764 and 851 us).  Of workgroups of one wavefront
+// LDS holds about one a SIMD, and of wide heads with a bias one workgroup for the queries' gradients.
+template <class E, int D, int NW> constexpr int kWaves = NW == 1 ? 1 : sizeof(E) == 2 || D <= 32 ? 3 : D <= 96 ? 2 : 1;
+template <class E, int D, int NW> constexpr int kGradientWaves = NW > 1 && (sizeof(E) == 2 || D <= 32) ? 2 : 1;
 // Key rows of the forward pass's tiles: of wide heads 32, so that LDS holds three workgroups (48 pages of 1,030 rows, d = 128: 608
 // us, with 64 rows and two 640; the gradients' kernels, which have registers for two, lose by it).
 template <class E, int D> constexpr int kForwardRows = D >= 96 ? 32 : Oper<E>::ROWS;
@@ -186,7 +202,7 @@ constexpr float kLag = 8.f;
 // A workgroup takes its tile for `run` head units one after the other, the first keys of the next on their way while it
 // computes: short sequences have one to three tiles of keys, whose latency would otherwise be most of the time.
 template <class E, int D, int NW, bool BIAS, bool MASKED>
-__global__ __launch_bounds__(64 * NW, (kWaves<E, D>)) void k_attention(const AttnArgs A, int slots, int units, int run, int splits, E* out, float* lse,
+__global__ __launch_bounds__(64 * NW, (kWaves<E, D, NW>)) void k_attention(const AttnArgs A, int slots, int order, int units, int run, int splits, E* out, float* lse,
                                                           float* o_part, float2* ml_part) {
     using O = Oper<E>;
     using T = Tile<E, D, kForwardRows<E, D>>;
@@ -195,9 +211,9 @@ __global__ __launch_bounds__(64 * NW, (kWaves<E, D>)) void k_attention(const Att
     __shared__ __align__(16) float hidden[2][T::ROWS];           // 0, or minus infinity for rows that no column sees
     extern __shared__ __align__(16) char dyn[];
     const int tid = threadIdx.x, lane0 = tid & 63, lane = lane0, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
-    const int work = in_order(blockIdx.x, gridDim.x), runs = (units + run - 1) / run;
-    const int split = work % splits, slot = work / splits / runs;
-    int unit = work / splits % runs * run;
+    const Work work = work_of(blockIdx.x, slots, (units + run - 1) / run * splits, A.n_seqs, order, true);
+    const int split = work.inner % splits, slot = work.slot;
+    int unit = work.inner / splits * run;
     const int end_unit = unit + run < units ? unit + run : units;
     const int G = A.pack, per = 32 * NW / G;
     const QueryTile t(A, slot, per, lane);
@@ -236,7 +252,7 @@ __global__ __launch_bounds__(64 * NW, (kWaves<E, D>)) void k_attention(const Att
     load_q(unit);
     int16_t* starts = (int16_t*)dyn;
     float* table = (float*)(dyn + kStartsBytes);
-    const int middle = bias_middle(A.reach), width = bias_width(A.reach);
+    const int middle = bias_middle(A.reach);
     if constexpr (BIAS) {
         load_starts(A, starts, tid, THREADS);
         __syncthreads();
@@ -458,7 +474,7 @@ __device__ __forceinline__ void add_diagonals(const f32x16& x, float* scratch, f
 
 // Gradients of queries, delta, and the bias table's share of each tile; head units one after the other, as the forward pass.
 template <class E, int D, int NW, bool BIAS, bool MASKED>
-__global__ __launch_bounds__(64 * NW, (kGradientWaves<E, D>)) void k_attention_dq(const AttnArgs A, int slots, int units, int run, const E* out,
+__global__ __launch_bounds__(64 * NW, (BIAS && D >= 96 ? 1 : kGradientWaves<E, D, NW>)) void k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const E* out,
                                                                            const E* dout, const float* lse, E* dq, float* delta,
                                                                            float* bias_part) {
     using O = Oper<E>;
@@ -470,8 +486,8 @@ __global__ __launch_bounds__(64 * NW, (kGradientWaves<E, D>)) void k_attention_d
     __shared__ float far_sum[kMostRun][NW][2];
     extern __shared__ __align__(16) char dyn[];       // the bias by distance, then histograms of each head and wavefront
     const int tid = threadIdx.x, lane0 = tid & 63, lane = lane0, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
-    const int work = in_order(blockIdx.x, gridDim.x), runs = (units + run - 1) / run;
-    const int slot = work / runs, first_unit = work % runs * run;
+    const Work work = work_of(blockIdx.x, slots, (units + run - 1) / run, A.n_seqs, order, true);
+    const int slot = work.slot, first_unit = work.inner * run;
     int unit = first_unit;
     const int end_unit = unit + run < units ? unit + run : units;
     const int G = A.pack, per = 32 * NW / G;
@@ -720,7 +736,7 @@ __global__ __launch_bounds__(64 * NW, (kGradientWaves<E, D>)) void k_attention_d
 // where there were four), but two wavefronts share a SIMD.
 template <class E, int D> constexpr bool kApart = sizeof(E) == 2 && D >= 96;
 template <class E, int D, int NW, bool BIAS, bool MASKED>
-__global__ __launch_bounds__((kApart<E, D> ? 128 : 64) * NW, (kGradientWaves<E, D>)) void k_attention_dkv(const AttnArgs A, int slots, int run, int main, int q_slots,
+__global__ __launch_bounds__((kApart<E, D> ? 128 : 64) * NW, (kGradientWaves<E, D, NW>)) void k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int q_slots,
                                                                             const E* dout, const float* lse, const float* delta,
                                                                             const float* bias_part, E* dk, E* dv, E* dbias) {
     using O = Oper<E>;
@@ -746,7 +762,8 @@ __global__ __launch_bounds__((kApart<E, D> ? 128 : 64) * NW, (kGradientWaves<E, 
             return;
         }
     }
-    const int work = in_order(blockIdx.x, main), runs = (A.kv_heads + run - 1) / run, slot = work / runs, kv0 = work % runs * run;
+    const Work work = work_of(blockIdx.x, slots, (A.kv_heads + run - 1) / run, A.n_seqs, order, false);
+    const int slot = work.slot, kv0 = work.inner * run;
     const int kv_end = kv0 + run < A.kv_heads ? kv0 + run : A.kv_heads;
     const int seq = find_sequence(A.koff, A.n_seqs, COLS, A.total_k, slot, lane);
     const Range ks = sequence_rows(A.koff, seq, A.total_k, COLS), qs = sequence_rows(A.qoff, seq, A.total_q);
@@ -961,7 +978,7 @@ hipError_t launch_attention(const AttnArgs& A, const AttnPlan& P, E* out, float*
             const size_t lds = BIAS ? bias_bytes(A.reach, 1) : 0;
             const int64_t runs = (P.units + P.run - 1) / P.run;
             k_attention<E, D, NW, BIAS, MASKED><<<dim3((unsigned)(P.q_slots * runs * P.splits)), 64 * NW, lds, st>>>(
-                A, (int)P.q_slots, P.units, P.run, P.splits, out, lse, o_part, ml_part);
+                A, (int)P.q_slots, P.q_order, P.units, P.run, P.splits, out, lse, o_part, ml_part);
             return hipGetLastError();
         });
         if (e != hipSuccess || P.splits == 1) return e;
@@ -985,7 +1002,7 @@ hipError_t launch_attention_backward(const AttnArgs& A, const AttnPlan& P, const
                 const size_t lds = BIAS ? bias_bytes(A.reach, 1 + P.run * NW) : 0;
                 const int64_t runs = (P.units + P.run - 1) / P.run;
                 k_attention_dq<E, D, NW, BIAS, MASKED><<<dim3((unsigned)(P.q_slots * runs)), 64 * NW, lds, st>>>(
-                    A, (int)P.q_slots, P.units, P.run, (const E*)G.out, (const E*)G.dout, G.lse, (E*)G.dq, delta, bias_part);
+                    A, (int)P.q_slots, P.q_order, P.units, P.run, (const E*)G.out, (const E*)G.dout, G.lse, (E*)G.dq, delta, bias_part);
                 return hipGetLastError();
             });
             if (e != hipSuccess) return e;
@@ -1000,7 +1017,7 @@ hipError_t launch_attention_backward(const AttnArgs& A, const AttnPlan& P, const
             const int more = BIAS ? (A.n_buckets * A.heads + WAVES - 1) / WAVES : 0;
             if (main + more == 0) return hipSuccess;
             k_attention_dkv<E, D, NW, BIAS, MASKED><<<dim3((unsigned)(main + more)), 64 * WAVES, lds, st>>>(
-                A, (int)P.k_slots, P.kv_run, main, q_slots, (const E*)G.dout, G.lse, delta, bias_part, (E*)G.dk, (E*)G.dv, (E*)G.dbias);
+                A, (int)P.k_slots, P.k_order, P.kv_run, main, q_slots, (const E*)G.dout, G.lse, delta, bias_part, (E*)G.dk, (E*)G.dv, (E*)G.dbias);
             return hipGetLastError();
         });
     });

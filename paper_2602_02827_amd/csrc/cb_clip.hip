@@ -6,7 +6,7 @@ namespace cb {
 // Two launches for up to kTable tensors: squares into one partial sum a workgroup, then every workgroup of the second adds up the
 // partial sums itself, in their order (they are few and in L2), and scales its share.  What is read last by the first is read
 // first by the second, from the last-level cache where it fits.
-constexpr int kTable = 128, kThreads = 256, kMostParts = 1024;
+constexpr int kTable = 128, kThreads = 256, kMostParts = 2048;
 constexpr int64_t kChunk = 8192;                     // values of a chunk; a chunk has one tensor
 
 struct ClipTable {
@@ -162,7 +162,7 @@ hipError_t launch_clip(int64_t n, const void* const* grads, void* const* out, co
     each([&](const ClipTable& t, uint32_t chunks, bool first) {
         const uint32_t work = out ? chunks : 0;
         if (work || first)
-            k_clip_scale<<<dim3(work < 1 ? 1 : work < 2048 ? work : 2048), kThreads, 0, st>>>(t, work, (const double*)ws, (int)parts,
+            k_clip_scale<<<dim3(work < 1 ? 1 : work < kMostParts ? work : kMostParts), kThreads, 0, st>>>(t, work, (const double*)ws, (int)parts,
                                                                                                max_norm, first ? norm : nullptr);
     });
     return e;

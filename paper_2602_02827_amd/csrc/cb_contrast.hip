@@ -391,7 +391,7 @@ __device__ __forceinline__ void document_gradient(char* lds, int block, const fl
 
 // One launch for both: the first workgroups take documents, which take longer.
 template <class E, int D, bool MANY>
-__global__ __launch_bounds__(256, 4) void k_maxsim_gradients(const float* dscores, const int32_t* argmax, const E* Q, int nq, int T,
+__global__ __launch_bounds__(256, MANY ? 2 : 4) void k_maxsim_gradients(const float* dscores, const int32_t* argmax, const E* Q, int nq, int T,
                                                           const E* docs, const int64_t* off, int N, int total, int doc_blocks, E* dQ,
                                                           E* ddocs) {
     constexpr size_t SUMS = sizeof(float) * (256 / RowLanes<E, D>::LANES) * RowLanes<E, D>::LANES * RowLanes<E, D>::PER;
@@ -402,9 +402,6 @@ __global__ __launch_bounds__(256, 4) void k_maxsim_gradients(const float* dscore
     else query_gradient<E, D>(lds, block - doc_blocks, dscores, argmax, T, docs, off, N, total, dQ);
 }
 
-#ifndef DOCGROUPS
-#define DOCGROUPS 1024
-#endif
 // ---- launches ------------------------------------------------------------------------------------------------
 template <class F> hipError_t by_type_and_width(int dt, int d, F&& f) {
     auto width = [&](auto type) {
@@ -423,17 +420,22 @@ hipError_t launch_maxsim_scores(const void* Q, int nq, int T, int d, int dt, con
     return by_type_and_width(dt, d, [&](auto type, auto dc) {
         using E = decltype(type);
         constexpr int D = decltype(dc)::value;
+        // About as many workgroups as run at once (four a CU; 512, 768 and 2,048 measured alike), of consecutive documents each.
+        // Two columns a lane read a tile's operands half as often (64 x 32 tokens against 512 passages, both kernels: 139 us, one
+        // column 145), where there are enough workgroups of them (16 x 24 tokens against 128 pages: 63 us, one column 57).
+        constexpr int64_t kGroups = 1024;
         auto go = [&](auto ct) {
             constexpr int CT = decltype(ct)::value;
             const int q_per = 128 * CT / T, col_groups = (nq + q_per - 1) / q_per;
-            int64_t docs_per = N * col_groups / DOCGROUPS;
+            int64_t docs_per = N * col_groups / kGroups;
             docs_per = docs_per < 1 ? 1 : docs_per;
             const int64_t parts = (N + docs_per - 1) / docs_per;
             k_maxsim_train<E, D, CT><<<dim3((unsigned)(parts * col_groups)), 256, 0, st>>>(
                 (const E*)Q, nq, T, (const E*)docs, off, (int)N, (int)total, col_groups, q_per, (int)docs_per, scores, argmax);
             return hipGetLastError();
         };
-        if ((int64_t)nq * T <= 128) return go(std::integral_constant<int, 1>{});
+        const int two = 256 / T;
+        if ((nq + two - 1) / two * N < kGroups) return go(std::integral_constant<int, 1>{});
         return go(std::integral_constant<int, 2>{});
     });
 }

@@ -26,10 +26,13 @@ struct AttnArgs {
 
 constexpr int kMostRun = 2;      // heads that a workgroup takes one after the other (four: the histograms leave half the workgroups no LDS)
 
+enum { AS_THEY_COME, BY_XCD, LONGEST_FIRST };         // order of workgroups
+
 struct AttnPlan {
     int d, dt;
     int q_waves, k_waves;        // wavefronts of a workgroup, 32 query (key) columns each
     int64_t q_slots, k_slots;    // places for tiles of all sequences
+    int q_order, k_order;
     int units;                   // head units: heads / pack
     int run, kv_run;             // head units (key heads) that a workgroup takes one after the other
     int splits;                  // parts that the keys of a forward call's tiles are cut into

@@ -8,6 +8,7 @@
 namespace cb {
 
 namespace {
+constexpr int64_t kShortRows = 384;
 int64_t round_up(int64_t x) { return (x + 255) / 256 * 256; }
 }
 
@@ -23,11 +24,16 @@ AttnPlan plan_attention(const AttnArgs& A, int d, int dt, bool backward) {
     P.k_waves = k_rows <= 32 && single ? 1 : 4;
     P.q_slots = A.total_q / (32 * P.q_waves / A.pack) + A.n_seqs;
     P.k_slots = A.total_k / (32 * P.k_waves) + A.n_seqs;
+    auto order_of = [&](int64_t slots, int64_t rows) {
+        return rows <= kShortRows ? BY_XCD : A.causal && slots >= 4 * (int64_t)A.n_seqs ? LONGEST_FIRST : AS_THEY_COME;
+    };
+    P.q_order = order_of(P.q_slots, k_rows);
+    P.k_order = order_of(P.k_slots, (int64_t)A.total_q * A.group / A.n_seqs);
     P.splits = 1;
     // Short sequences: a workgroup goes on to the next heads, as long as enough workgroups are left (wide heads: kRuns).
     auto run_of = [](int64_t slots, int units, int64_t rows) {
         int r = 1;
-        while (rows <= 384 && 2 * r <= kMostRun && 2 * r <= units && slots * (units / (2 * r)) >= 1536) r *= 2;
+        while (rows <= kShortRows && 2 * r <= kMostRun && 2 * r <= units && slots * (units / (2 * r)) >= 1536) r *= 2;
         return r;
     };
     P.run = d <= 64 ? run_of(P.q_slots, P.units, k_rows) : 1;
