@@ -46,6 +46,9 @@ extern "C" {
  * A row that sees nothing has out = 0 and lse = -inf, and takes no part in any gradient.
  * Query head h reads key head h / (heads / kv_heads).  Keys that the mask hides may hold
  * anything, infinities and NaN included.
+ * Products are summed in 32 bits.  fp32 values are multiplied as three bf16 pieces each, whose
+ * sum is the value; the three smallest of the nine products of pieces, 2^-23 of a product
+ * together, are left out.  fp32 values that are seen must be finite.
  * Rows of q, k and v lie q_row elements apart and heads q_head apart (likewise k, v); the d
  * values of a row and head are consecutive.  Pointers and strides are whole multiples of 16
  * bytes; rows lie at most 32 MiB apart.  out and all gradients are dense, [rows][heads][d].
@@ -111,8 +114,8 @@ int colbandit_attention_backward(const colbandit_attn *a, const void *out, const
  *   scores   DEVICE float [n_queries][N]
  *   argmax   DEVICE int32 [n_queries][N][T]: the j that token t chose, the lowest of equal
  *            ones; -1 in an empty document
- * Products are summed in 32 bits (fp32 inputs: by the fp32 matrix instructions).  Embeddings
- * are finite.
+ * Products are summed in 32 bits; precision is that of the attention calls' products.
+ * Embeddings are finite.
  */
 int colbandit_maxsim_scores(const void *Q, int n_queries, int T, int d, colbandit_dtype dt,
                             const void *docs, const int64_t *offsets, int64_t N,

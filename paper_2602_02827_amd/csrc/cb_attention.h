@@ -53,10 +53,11 @@ __host__ __forceinline__ size_t bias_bytes(int reach, int tables) { return kStar
 
 // Places of tiles, in the order in which workgroups (and what each has several of: `inner`) take them.
 // BY_XCD: workgroups are dealt to the eight XCDs in turn; numbered so that each XCD has runs of consecutive ones (64, or as many as
-// leave each eight runs), the heads of a short sequence, whose values lie side by side, are read through one L2.
+// leave each eight runs), the heads of a short sequence, whose values lie side by side, are read through one L2 (512 passages,
+// forward and backward: 700 us, as they come 722; 48 pages, where a head's tiles are kept together as they come: 588 and 578).
 // LONGEST_FIRST: under a causal limit the later rows see more keys (earlier keys are seen by more rows): places go round the
 // sequences, each one's longest tiles first (`down`: its last ones), so that short ones are left for the end.  Sequences are taken
-// to be of one length; others are only in another order.
+// to be of one length; others are only in another order (24 causal pages, forward and backward: 492 us, as they come 561).
 __device__ __forceinline__ int in_order(int block, int blocks) {
     const int lg = blocks < 128 ? 0 : blocks >= 4096 ? 6 : 25 - __builtin_clz(blocks);
     const int whole = blocks >> (lg + 3) << (lg + 3), xcd = block & 7, i = block >> 3;
@@ -181,11 +182,13 @@ __device__ __forceinline__ f32x16 of_rows(const float* v, int b, int h) {
     return x;
 }
 
-// Wavefronts per SIMD that the registers are shared out for (one more each makes the compiler spill, and is slower; forward
-// pass, 512 passages, three and four: 152 and 176 us; gradients, two and three: 764 and 851 us).  Of workgroups of one wavefront
-// LDS holds about one a SIMD, and of wide heads with a bias one workgroup for the queries' gradients.
+// Wavefronts per SIMD that the registers are shared out for: forward pass, gradients of queries, of keys and values (one more each
+// makes the compiler spill, and is slower; 512 passages: forward pass with three and four 152 and 176 us, forward and backward with
+// two and three for the queries 705 and 642, with two and three for the keys 642 and 752).  Of workgroups of one wavefront LDS
+// holds about one a SIMD.
 template <class E, int D, int NW> constexpr int kWaves = NW == 1 ? 1 : sizeof(E) == 2 || D <= 32 ? 3 : D <= 96 ? 2 : 1;
 template <class E, int D, int NW> constexpr int kGradientWaves = NW > 1 && (sizeof(E) == 2 || D <= 32) ? 2 : 1;
+template <class E, int D, int NW> constexpr int kQueryWaves = NW > 1 && sizeof(E) == 2 && D <= 64 ? 3 : kGradientWaves<E, D, NW>;
 // Key rows of the forward pass's tiles: of wide heads 32, so that LDS holds three workgroups (48 pages of 1,030 rows, d = 128: 608
 // us, with 64 rows and two 640; the gradients' kernels, which have registers for two, lose by it).
 template <class E, int D> constexpr int kForwardRows = D >= 96 ? 32 : Oper<E>::ROWS;
@@ -197,13 +200,19 @@ template <class E, int D> constexpr bool kSingle = sizeof(E) == 2 || D <= 64;
 // ---- forward -------------------------------------------------------------------------------------------------
 // One pass over the keys with the running maximum and sum of the softmax, in 32 bits; probabilities are rounded to the
 // storage type for the second product (their sum is not).  The maximum that is subtracted may lag by up to kLag: sums and
-// outputs are rescaled only when it is passed, which few tiles after the first do; probabilities up to 2^kLag are no less exact.
+// outputs are rescaled only when it is passed, which few tiles after the first do; probabilities up to 2^kLag are no less exact
+// (48 pages of 1,030 rows, 16 heads of 128 over 8: 588 us, without a lag 633).
 constexpr float kLag = 8.f;
 // A workgroup takes its tile for `run` head units one after the other, the first keys of the next on their way while it
 // computes: short sequences have one to three tiles of keys, whose latency would otherwise be most of the time.
+// Long sequences are bound by the matrix and vector units' turns (an exponential, a maximum, a sum and half a conversion for every
+// score: as many clocks as the products): the pages above 564 us, 740 TFLOP/s where a large product reaches 1,189.  Short ones by
+// latency and what a workgroup does before its first product: 512 passages, 12 heads of 64 with bias and mask, 148 us.  Single
+// tokens by memory: 16 over 1 to 16,385 keys, two key heads of 128, 134 MB in 30 us and 7.5 us to join their parts.
 template <class E, int D, int NW, bool BIAS, bool MASKED>
-__global__ __launch_bounds__(64 * NW, (kWaves<E, D, NW>)) void k_attention(const AttnArgs A, int slots, int order, int units, int run, int splits, E* out, float* lse,
-                                                          float* o_part, float2* ml_part) {
+__global__ __launch_bounds__(64 * NW, (kWaves<E, D, NW>)) void k_attention(const AttnArgs A, int slots, int order, int units, int run,
+                                                                           int splits, E* out, float* lse, float* o_part,
+                                                                           float2* ml_part) {
     using O = Oper<E>;
     using T = Tile<E, D, kForwardRows<E, D>>;
     constexpr int NB = T::ROWS / 32, DB = D / 32, THREADS = 64 * NW;
@@ -449,39 +458,40 @@ __global__ __launch_bounds__(256) void k_attention_join(const AttnArgs A, int sp
 // first, 16-bit dS goes into its product as two values of eight bits each, which leaves O's rounding as the only error beside
 // the result's own (gradients of queries, against 64 bits, 512 passages: 2.6e-3 with one value, 2.0e-3 with two; the result's own
 // rounding is 1.7e-3).
+// Bound by the matrix and vector units' turns where sequences are long (24 causal pages, 8 heads of 128 over 2: 174 and 231 us, 450
+// TFLOP/s of the three and four products that each cannot do without), by latency and by what surrounds the products where they are
+// short (the 512 passages: 322 us, a third of them the bias table's sums, and 252).
 
-// Sums of a 32 x 32 block along its diagonals, added to a histogram by distance.  The block is in accumulators: a lane has
-// sixteen keys of a column.  The columns go to LDS, 68 words apart (sixteen lanes' writes in different banks) with zeros between
-// them; lane i then adds up the diagonal k - n = i - 31, one word of each column, and the histogram has one place for it.
+// Sums of a 32 x 32 block along its diagonals, added to a histogram by distance.  The block is in accumulators: a lane has sixteen
+// keys of a column.  Lane p of a half takes key k's value from column (p + k) mod 32: it lies on diagonal -p, or 32 - p where that
+// wraps.  Both sums of a lane are complete with those of the other half's keys; the lower half has the first, the upper the second.
 // No atomics, which take 2.5 clocks a lane there, and a fixed order.
-constexpr int kPitch = 68, kDiagonal = 32 * kPitch + 32;
-__device__ __forceinline__ void add_diagonals(const f32x16& x, float* scratch, float* hist, int lane) {
-    const int n = lane & 31, h = lane >> 5;
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+__device__ __forceinline__ void add_diagonals(const f32x16& x, float* hist, int lane) {
+    const int own = here(lane), p = own & 31, h = own >> 5, from = p + 4 * h;
+    float a = 0.f, w = 0.f;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-        *(f32x4*)(scratch + n * kPitch + 32 + 8 * j + 4 * h) = f32x4{x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]};
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    const float* own = scratch + 32 - 31 + (lane < 63 ? lane : 62);
-    float sum = 0.f, more = 0.f;
-#pragma unroll
-    for (int c = 0; c < 32; c += 2) {
-        sum += own[c * kPitch + c];
-        more += own[(c + 1) * kPitch + c + 1];
+    for (int r = 0; r < 16; ++r) {
+        const int n = from + 8 * (r >> 2) + (r & 3);
+        const float y = __int_as_float(__builtin_amdgcn_ds_bpermute((n & 31) << 2 | h << 7, __float_as_int(x[r])));
+        a += n < 32 ? y : 0.f;
+        w += n < 32 ? 0.f : y;
     }
-    if (lane < 63) hist[lane - 31] += sum + more;
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(w), false, false);
+    const uint32_t lo = s[0], hi = s[1];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    hist[32 * h - p] += __uint_as_float(lo) + __uint_as_float(hi);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
 // Gradients of queries, delta, and the bias table's share of each tile; head units one after the other, as the forward pass.
 template <class E, int D, int NW, bool BIAS, bool MASKED>
-__global__ __launch_bounds__(64 * NW, (BIAS && D >= 96 ? 1 : kGradientWaves<E, D, NW>)) void k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const E* out,
-                                                                           const E* dout, const float* lse, E* dq, float* delta,
-                                                                           float* bias_part) {
+__global__ __launch_bounds__(64 * NW, (kQueryWaves<E, D, NW>)) void
+k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const E* out, const E* dout, const float* lse, E* dq,
+               float* delta, float* bias_part) {
     using O = Oper<E>;
     using T = Tile<E, D>;
     constexpr int NB = T::ROWS / 32, DB = D / 32, THREADS = 64 * NW;
     __shared__ __align__(256) char lds[2][2 * T::BYTES];
-    __shared__ __align__(16) float diagonals[BIAS ? NW * kDiagonal : 1];
     __shared__ __align__(16) float hidden[2][T::ROWS];
     __shared__ float far_sum[kMostRun][NW][2];
     extern __shared__ __align__(16) char dyn[];       // the bias by distance, then histograms of each head and wavefront
@@ -523,9 +533,9 @@ __global__ __launch_bounds__(64 * NW, (BIAS && D >= 96 ? 1 : kGradientWaves<E, D
     if (any) issue(unit, 0, lds[0]);
     Column<E, D> q, g;
     float dot = 0.f, own_lse = 0.f;
-    const int64_t at = (int64_t)(t.q0 + w.row);
     auto load_rows = [&](int u) {
-        const int head = u * G + w.head;
+        const int64_t at = t.q0 + here(w.row);
+        const int h = here(lane0) >> 5, head = u * G + w.head;
         const int64_t dense = (at * A.heads + head) * D;
         const float row_lse = w.real ? lse[(int64_t)head * A.total_q + at] : -INFINITY;
         Column<E, D> o;
@@ -555,10 +565,8 @@ __global__ __launch_bounds__(64 * NW, (BIAS && D >= 96 ? 1 : kGradientWaves<E, D
     float* table = (float*)(dyn + kStartsBytes);
     float* hist = table + width;
     float* own_hist = hist + wave * width + middle;
-    float* scratch = diagonals + wave * kDiagonal;
     if constexpr (BIAS) {
         for (int i = tid; i < (end_unit - unit) * NW * width; i += THREADS) hist[i] = 0.f;
-        for (int i = tid; i < NW * kDiagonal; i += THREADS) diagonals[i] = 0.f;
         load_starts(A, starts, tid, THREADS);
         __syncthreads();
         fill_bias<E>(A, unit, starts, table, tid, THREADS);
@@ -628,7 +636,7 @@ __global__ __launch_bounds__(64 * NW, (BIAS && D >= 96 ? 1 : kGradientWaves<E, D
                 row_sum += sum;
                 if constexpr (BIAS) {
                     if (side) (side < 0 ? far_lo : far_hi) += sum;
-                    else add_diagonals(s, scratch, own_hist + d0, lane);
+                    else add_diagonals(s, own_hist + d0, lane);
                 }
                 phase();
                 if constexpr (sizeof(E) == 2) {
@@ -656,6 +664,7 @@ __global__ __launch_bounds__(64 * NW, (BIAS && D >= 96 ? 1 : kGradientWaves<E, D
         }
         if (last) {
             row_sum = sum_of_halves(row_sum);
+            const int64_t at = t.q0 + here(w.row);
             const int head = unit * G + w.head;
             if (w.real) {
                 if (h == 0) delta[(int64_t)head * A.total_q + at] = dot + row_sum;
@@ -733,12 +742,12 @@ __global__ __launch_bounds__(64 * NW, (BIAS && D >= 96 ? 1 : kGradientWaves<E, D
 // of all tiles.
 // A wavefront with both gradients of 32 wide rows takes more than half of the registers, so nothing runs beside its waits.
 // In 16 bits wide heads have two wavefronts for the same rows, one for either gradient: the scores are made twice (five products
-// where there were four), but two wavefronts share a SIMD.
+// where there were four), but two wavefronts share a SIMD (24 causal pages, forward and backward: 574 us, with one 865).
 template <class E, int D> constexpr bool kApart = sizeof(E) == 2 && D >= 96;
 template <class E, int D, int NW, bool BIAS, bool MASKED>
-__global__ __launch_bounds__((kApart<E, D> ? 128 : 64) * NW, (kGradientWaves<E, D, NW>)) void k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int q_slots,
-                                                                            const E* dout, const float* lse, const float* delta,
-                                                                            const float* bias_part, E* dk, E* dv, E* dbias) {
+__global__ __launch_bounds__((kApart<E, D> ? 128 : 64) * NW, (kGradientWaves<E, D, NW>)) void
+k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int q_slots, const E* dout, const float* lse,
+                const float* delta, const float* bias_part, E* dk, E* dv, E* dbias) {
     using O = Oper<E>;
     using T = Tile<E, D>;
     constexpr int NB = T::ROWS / 32, DB = D / 32, COLS = 32 * NW;

@@ -8,7 +8,7 @@
 namespace cb {
 
 namespace {
-constexpr int64_t kShortRows = 384;
+constexpr int64_t kShortRows = 384;                   // up to six tiles of the other side's rows
 int64_t round_up(int64_t x) { return (x + 255) / 256 * 256; }
 }
 
@@ -17,7 +17,8 @@ AttnPlan plan_attention(const AttnArgs& A, int d, int dt, bool backward) {
     P.d = d;
     P.dt = dt;
     P.units = A.heads / A.pack;
-    // Columns of a mean sequence: short ones get workgroups of one wavefront.
+    // Columns of a mean sequence: up to 32 get workgroups of one wavefront, which leave no wavefront without rows and join no
+    // others (61 short fp32 candidates: 22.3 us, with four 23.2; one query of 32 tokens 16.7 and 17.7).
     const int64_t q_cols = (int64_t)A.total_q * A.pack / A.n_seqs, k_rows = A.total_k / A.n_seqs;
     const bool single = !backward || dt == TR_BF16 || d <= 64;       // (kSingle)
     P.q_waves = q_cols <= 32 && single ? 1 : 4;
@@ -30,7 +31,8 @@ AttnPlan plan_attention(const AttnArgs& A, int d, int dt, bool backward) {
     P.q_order = order_of(P.q_slots, k_rows);
     P.k_order = order_of(P.k_slots, (int64_t)A.total_q * A.group / A.n_seqs);
     P.splits = 1;
-    // Short sequences: a workgroup goes on to the next heads, as long as enough workgroups are left (wide heads: kRuns).
+    // Short sequences: a workgroup goes on to the next heads, as long as enough workgroups are left (six a CU; wide heads: kRuns).
+    // 512 passages, forward and backward: 701 us, one head each 724.
     auto run_of = [](int64_t slots, int units, int64_t rows) {
         int r = 1;
         while (rows <= kShortRows && 2 * r <= kMostRun && 2 * r <= units && slots * (units / (2 * r)) >= 1536) r *= 2;
@@ -156,6 +158,7 @@ int attn_args(const colbandit_attn* a, AttnArgs& A) {
     A.heads = a->heads;
     A.kv_heads = a->kv_heads;
     A.group = a->heads / a->kv_heads;
+    // (16 single tokens, four heads to a key head: 42 us, a tile for each head 98; 48 pages, two heads to one: 588 and 612)
     A.pack = !a->bias && A.group <= 16 && a->q_head * eb <= kMostRowBytes && a->total_q <= kMostRows / A.group &&
                      a->total_k <= kMostRows / A.group ? A.group : 1;      // columns are counted in 31 bits
     A.total_q = (int)a->total_q;
