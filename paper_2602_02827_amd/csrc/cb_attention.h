@@ -184,7 +184,7 @@ __device__ __forceinline__ f32x16 of_rows(const float* v, int b, int h) {
 
 // Wavefronts per SIMD that the registers are shared out for: forward pass, gradients of queries, of keys and values (one more each
 // makes the compiler spill, and is slower; 512 passages: forward pass with three and four 152 and 176 us, forward and backward with
-// two and three for the queries 705 and 642, with two and three for the keys 642 and 752).  Of workgroups of one wavefront LDS
+// two and three for the queries 705 and 642, with three for the keys 706 where it was 642).  Of workgroups of one wavefront LDS
 // holds about one a SIMD.
 template <class E, int D, int NW> constexpr int kWaves = NW == 1 ? 1 : sizeof(E) == 2 || D <= 32 ? 3 : D <= 96 ? 2 : 1;
 template <class E, int D, int NW> constexpr int kGradientWaves = NW > 1 && (sizeof(E) == 2 || D <= 32) ? 2 : 1;
@@ -207,7 +207,7 @@ constexpr float kLag = 8.f;
 // computes: short sequences have one to three tiles of keys, whose latency would otherwise be most of the time.
 // Long sequences are bound by the matrix and vector units' turns (an exponential, a maximum, a sum and half a conversion for every
 // score: as many clocks as the products): the pages above 564 us, 740 TFLOP/s where a large product reaches 1,189.  Short ones by
-// latency and what a workgroup does before its first product: 512 passages, 12 heads of 64 with bias and mask, 148 us.  Single
+// latency and what a workgroup does before its first product: 512 passages, 12 heads of 64 with bias and mask, 145 us.  Single
 // tokens by memory: 16 over 1 to 16,385 keys, two key heads of 128, 134 MB in 30 us and 7.5 us to join their parts.
 template <class E, int D, int NW, bool BIAS, bool MASKED>
 __global__ __launch_bounds__(64 * NW, (kWaves<E, D, NW>)) void k_attention(const AttnArgs A, int slots, int order, int units, int run,
@@ -454,13 +454,16 @@ __global__ __launch_bounds__(256) void k_attention_join(const AttnArgs A, int sp
 // recomputes the scores twice (seven products where one kernel would need five) but adds in a fixed order, where one
 // kernel would have to add either side's gradients by atomics.
 // The rounding of O reaches dS through delta, the same for all of a row.  Rows of dS sum to zero, so what a row's sum is
-// instead is the error of its delta: the first kernel adds it to the delta that the second one takes.  In the
-// first, 16-bit dS goes into its product as two values of eight bits each, which leaves O's rounding as the only error beside
-// the result's own (gradients of queries, against 64 bits, 512 passages: 2.6e-3 with one value, 2.0e-3 with two; the result's own
-// rounding is 1.7e-3).
-// Bound by the matrix and vector units' turns where sequences are long (24 causal pages, 8 heads of 128 over 2: 174 and 231 us, 450
+// instead is the error of its delta: the first kernel adds it to the delta that the second one takes.  In the first, 16-bit dS goes
+// into its product as two values of eight bits each, which leaves O's rounding as the only error beside the result's own (gradients
+// of queries, against 64 bits, 512 passages: 2.6e-3 with one value, 2.0e-3 with two; the result's own rounding is 1.7e-3).  Rows that
+// see few keys have small gradients and a large O, so that its rounding counts most there: tiles that see up to kTwice keys go over
+// them twice, first for delta in 32 bits (60 causal sequences of 1 to 17 tokens: 2.8e-3, so 1.7e-3; of 1 to 301: 2.2e-3 and 1.7e-3.
+// It costs the 512 passages 25 us of 671, with 64 keys 4 us, which leaves 2.1e-3 for sequences of up to 131 tokens).
+constexpr int kTwice = 128;
+// Bound by the matrix and vector units' turns where sequences are long (24 causal pages, 8 heads of 128 over 2: 172 and 228 us, 455
 // TFLOP/s of the three and four products that each cannot do without), by latency and by what surrounds the products where they are
-// short (the 512 passages: 322 us, a third of them the bias table's sums, and 252).
+// short (the 512 passages: 289 and 250 us).
 
 // Sums of a 32 x 32 block along its diagonals, added to a histogram by distance.  The block is in accumulators: a lane has sixteen
 // keys of a column.  Lane p of a half takes key k's value from column (p + k) mod 32: it lies on diagonal -p, or 32 - p where that
@@ -510,6 +513,8 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
     }
     const QueryColumns w(A, t, G, per, wave, lane);
     const int tiles = (t.end + T::ROWS - 1) / T::ROWS;
+    const bool twice = sizeof(E) == 2 && t.end <= kTwice;        // first for delta
+    const int steps = twice ? 2 * tiles : tiles;
     const int64_t krow = A.k_row * (int64_t)sizeof(E), vrow = A.v_row * (int64_t)sizeof(E);
     Staged<E, D, THREADS, MASKED, T::ROWS> next;
     uint8_t next_keep = 0;
@@ -556,7 +561,7 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
 #pragma unroll
             for (int e = 0; e < 8; ++e) dot += x[e] * y[e];
         }
-        dot = sum_of_halves(dot);
+        dot = twice ? 0.f : sum_of_halves(dot);
         q.take_sign(A.scale);
     };
     load_rows(unit);
@@ -580,12 +585,13 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
     const typename T::At at_tiles(lds[0], lane);
     int i = 0, buf = 0;
     while (true) {
-        const int base = i * T::ROWS;
+        const bool before = twice && i < tiles;
+        const int base = (i < tiles ? i : i - tiles) * T::ROWS;
         const typename T::At lk = at_tiles + buf * 2 * T::BYTES, lv = lk + T::BYTES;
-        const bool last = i + 1 >= tiles;
+        const bool last = i + 1 >= steps;
         const int n_unit = last ? unit + 1 : unit, n_i = last ? 0 : i + 1;
         const bool more = kRuns<D> ? n_unit < end_unit : !last;
-        if (more && any) issue(n_unit, n_i * T::ROWS, lds[buf ^ 1]);
+        if (more && any) issue(n_unit, (n_i < tiles ? n_i : n_i - tiles) * T::ROWS, lds[buf ^ 1]);
         if (any && w.busy && base < w.end) {
             const bool diagonal = A.causal && base + T::ROWS - 1 > w.first_lim, part = seen != kAllRows;
 #pragma unroll 1
@@ -621,7 +627,7 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
                 }
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[r] = exp2_fast(s[r]);
-                if (BIAS && side) {
+                if (BIAS && side && !before) {
                     float weight = 0.f;
 #pragma unroll
                     for (int r = 0; r < 16; ++r) weight += s[r];
@@ -634,6 +640,7 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
                     sum += s[r];
                 }
                 row_sum += sum;
+                if (before) continue;
                 if constexpr (BIAS) {
                     if (side) (side < 0 ? far_lo : far_hi) += sum;
                     else add_diagonals(s, own_hist + d0, lane);
@@ -661,6 +668,10 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
                     for (int db = 0; db < DB; ++db) O::mma(acc[db], T::turned(lk, b, 1, db), O::round(eight<8>(s)));
                 }
             }
+        }
+        if (before && i + 1 == tiles) {
+            dot = sum_of_halves(row_sum);
+            row_sum = 0.f;
         }
         if (last) {
             row_sum = sum_of_halves(row_sum);

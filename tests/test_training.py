@@ -280,6 +280,23 @@ def test_strides_of_a_packed_projection_and_of_heads_first(tr, dev, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("ql", [list(range(1, 18)), [128, 97, 65], [1, 2, 3, 40]])
+@pytest.mark.parametrize("d,H,Hk", [(64, 3, 3), (128, 4, 2)])
+@pytest.mark.parametrize("bias", [None, 32])
+def test_short_rows_lose_nothing_but_the_results_rounding(tr, dev, ql, d, H, Hk, bias):
+    """Rows that see up to 128 keys: delta in 32 bits and dS in two values of eight bits, 2^-17 of it, which over 128 keys is some
+    2^-13.5 of the sum.  A stored value is the exact one's nearest, or off by no more than that and twice the error before it is
+    rounded: the norm of the error is that of the exact gradients' own rounding and at most 2^-12 of their norm."""
+    p = problem(dev, "bf16", ql, ql, H, Hk, d, seed=19, bias=bias)
+    want = Attention(p["q"], p["k"], p["v"], ql, ql, "bf16", causal=True, bias=p["bias"], dout=p["dout"])
+    _, b = attend(tr, p, ql, ql, causal=True)
+    for name in ("dq",) if bias is None else ("dq", "dbias"):
+        exact = getattr(want, name)
+        error, own = float((b[name].double().cpu() - exact).norm()), float((exact.bfloat16().double() - exact).norm())
+        assert error <= own + 2.0 ** -12 * float(exact.norm()), (name, error, own)
+
+
+@gpu
 @pytest.mark.parametrize("heads", [4, 2])
 def test_rows_and_heads_beyond_32_bits(tr, dev, heads):
     """Rows 16 MiB apart and heads 3 GiB apart (packed heads' rows are addressed from their tile's first one in 32 bits: these are
