@@ -17,12 +17,14 @@ AttnPlan plan_attention(const AttnArgs& A, int d, int dt, bool backward) {
     P.d = d;
     P.dt = dt;
     P.units = A.heads / A.pack;
-    // Columns of a mean sequence: up to 32 get workgroups of one wavefront, which leave no wavefront without rows and join no
-    // others (61 short fp32 candidates: 22.3 us, with four 23.2; one query of 32 tokens 16.7 and 17.7).
+    // Up to 32 columns of a mean sequence get workgroups of one wavefront, which wait for no other, as long as all run at once (LDS
+    // holds about one a SIMD).  One query of 32 tokens, 12 heads: 16.7 us, with four wavefronts 17.7; 128 fp32 sequences of 32, 6
+    // heads, with gradients 39.5 and 40.6; but 512 sequences of 8 to 32, 12 heads, with gradients 233 and 219.
     const int64_t q_cols = (int64_t)A.total_q * A.pack / A.n_seqs, k_rows = A.total_k / A.n_seqs;
     const bool single = !backward || dt == TR_BF16 || d <= 64;       // (kSingle)
-    P.q_waves = q_cols <= 32 && single ? 1 : 4;
-    P.k_waves = k_rows <= 32 && single ? 1 : 4;
+    auto waves_of = [&](int64_t cols, int64_t groups) { return cols <= 32 && groups <= 1024 && single ? 1 : 4; };
+    P.q_waves = waves_of(q_cols, ((int64_t)A.total_q * A.pack / 32 + A.n_seqs) * P.units);
+    P.k_waves = waves_of(k_rows, (A.total_k / 32 + A.n_seqs) * A.kv_heads);
     P.q_slots = A.total_q / (32 * P.q_waves / A.pack) + A.n_seqs;
     P.k_slots = A.total_k / (32 * P.k_waves) + A.n_seqs;
     auto order_of = [&](int64_t slots, int64_t rows) {
