@@ -46,6 +46,9 @@ extern "C" {
  * A row that sees nothing has out = 0 and lse = -inf, and takes no part in any gradient.
  * Query head h reads key head h / (heads / kv_heads).  Keys that the mask hides may hold
  * anything, infinities and NaN included.
+ * Scores are held in 32 bits: of a bias of 1e9 in size a row's products leave nothing.  Rows whose
+ * scores are all that far from zero (a table may hide distances by any finite value, down to the
+ * type's lowest) have outputs and gradients like any other; lse has a 32-bit value's rounding.
  * Products are summed in 32 bits.  fp32 values are multiplied as three bf16 pieces each, whose
  * sum is the value; the three smallest of the nine products of pieces, 2^-23 of a product
  * together, are left out.  fp32 values that are seen must be finite.

@@ -14,7 +14,7 @@
 
 namespace cb {
 
-// Bias of a head by distance key - query, in powers of two; finite values stay finite.  A block of 32 x 32 distances that
+// Bias of a head by distance key - query, as it is in the table.  A block of 32 x 32 distances that
 // is not all in one direction's last bucket reaches less than kBlock beyond `reach`: the table is that much longer, so that no
 // distance is clamped when it is looked up, and a lane's sixteen places differ by constants.
 constexpr int kBlock = 62;
@@ -38,8 +38,7 @@ __device__ __forceinline__ void fill_bias(const AttnArgs& A, int head, const int
     for (int b = tid >> 3; b < A.n_buckets; b += threads >> 3) {
         const bool behind = b >= A.n_dir;             // keys behind the query
         const int i = behind ? b - A.n_dir : b;
-        const float x = (float)((const E*)A.bias)[(int64_t)b * A.heads + head], y = x * LOG2E;
-        const float z = fabsf(x) < INFINITY ? fminf(fmaxf(y, -3.4028235e38f), 3.4028235e38f) : y;
+        const float z = (float)((const E*)A.bias)[(int64_t)b * A.heads + head];
         const int end = starts[i + 1];
         for (int j = starts[i] + (tid & 7); j < end; j += 8)
             if (!behind) table[middle - j] = z; else if (j > 0) table[middle + j] = z;
@@ -77,9 +76,33 @@ __device__ __forceinline__ Work work_of(int block, int slots, int inner, int n, 
 // Which way a block of 32 rows and columns lies whose first key and row are d0 apart: -1 or 1: all beyond reach, 0: not.
 __device__ __forceinline__ int block_side(int d0, int reach) { return d0 + 31 <= -reach ? -1 : d0 - 31 >= reach ? 1 : 0; }
 
-// Scores are scaled by |scale| in powers of two, as the exponential takes them; the columns' rows take its sign (exact), and are
-// zeros where it is zero, so that the maximum of the raw products is that of the scores.
-__device__ __forceinline__ float scale_of_scores(float scale) { return scale == 0.f ? 1.f : fabsf(scale) * LOG2E; }
+// The columns' rows take the scale's sign (exact), and are zeros where it is zero, so that the maximum of the raw products is that
+// of the scores.  Without a bias scores stay raw products; with one they are scaled by |scale| and natural, as the table is.
+// The exponential takes powers of two, and is given fma(score, k, -(maximum * k)), one instruction.  Where the maximum is far from
+// zero (a table that hides distances by values down to the type's lowest, in rows that see no other distance; scores of millions) the
+// rounding of that product, or its overflow, is larger than the differences that matter: there it is (score - maximum) * k, which is
+// 0 for the maximum itself.  kFar is where that begins, in powers of two: up to it the product's rounding is 2^-18.
+constexpr float kFar = 128.f;
+__device__ __forceinline__ float unit_of_scores(float scale) { return scale == 0.f ? 1.f : fabsf(scale); }
+// A product that is rounded before anything is added to it.
+__device__ __forceinline__ float rounded_product(float a, float b) {
+#pragma clang fp contract(off)
+    return a * b;
+}
+// Exponent of a probability's share whose own maximum is m, from where the maximum is `to` (both finite).
+__device__ __forceinline__ float exponent_between(float m, float to, float k) {
+    const float a = m * k, b = to * k;
+    return fabsf(a) > kFar || fabsf(b) > kFar ? (m - to) * k : a - b;
+}
+// From here on a sum's logarithm is taken to be the maximum: the sum of up to 2^31 exponentials adds less than three of its last
+// places, and the backward pass finds the maximum in it, to the bit.
+constexpr float kLostLog = 134217728.f;
+// Natural logarithm of a sum l of exponentials from the maximum m on, a score's unit being `unit`.
+__device__ __forceinline__ float log_of_sum(float m, float l, float k, float unit) {
+    if (l == 0.f) return -INFINITY;
+    const float a = m * k, b = rounded_product(m, unit);
+    return fabsf(a) <= kFar ? fmaf(a, LN2, logf(l)) : fabsf(b) < kLostLog ? b + logf(l) : b;
+}
 
 // The eight-value pieces of one column's row (B operand of all steps); zeros for a column that is none.
 template <class E, int D> struct Column {
@@ -182,6 +205,14 @@ __device__ __forceinline__ f32x16 of_rows(const float* v, int b, int h) {
     return x;
 }
 
+// Rows of a block that a lane's column sees under a limit, as bits: a lane's rows lie at 8 (r / 4) + r % 4 from its first one.  One
+// register instead of sixteen comparisons' masks, which take scalar registers that other values are then moved out of.
+__device__ __forceinline__ uint32_t bits_up_to(int room) { return room < 0 ? 0u : room >= 31 ? ~0u : (2u << room) - 1u; }
+__device__ __forceinline__ uint32_t all_if(uint32_t bits, int r) { return (uint32_t)((int)(bits << (31 - 8 * (r >> 2) - (r & 3))) >> 31); }
+__device__ __forceinline__ float hidden_unless(float x, uint32_t all) {
+    return __uint_as_float((__float_as_uint(x) & all) | (0xff800000u & ~all));
+}
+
 // Wavefronts per SIMD that the registers are shared out for: forward pass, gradients of queries, of keys and values (one more each
 // makes the compiler spill, and is slower; 512 passages: forward pass with three and four 152 and 176 us, forward and backward with
 // two and three for the queries 705 and 642, with three for the keys 706 where it was 642).  Of workgroups of one wavefront LDS
@@ -268,9 +299,10 @@ __global__ __launch_bounds__(64 * NW, (kWaves<E, D, NW>)) void k_attention(const
         fill_bias<E>(A, unit, starts, table, tid, THREADS);
     }
     f32x16 acc[DB] = {};
-    float m = -INFINITY, l = 0.f;
+    float m = -INFINITY, l = 0.f, off = 0.f;                     // off: -m k, of a row with a maximum
+    bool far = false;                                            // of some row of the wavefront
     bool sees = !MASKED;                                         // the mask leaves the row some key
-    const float scale2 = scale_of_scores(A.scale);
+    const float unit_scale = unit_of_scores(A.scale), k = BIAS ? LOG2E : unit_scale * LOG2E, lag = fminf(kLag / k, 1e38f);
     if (any) finish(0);
     __syncthreads();
     const typename T::At at_tiles(lds[0], lane);
@@ -302,40 +334,48 @@ __global__ __launch_bounds__(64 * NW, (kWaves<E, D, NW>)) void k_attention(const
                     if (side) {
                         const float x = table[side < 0 ? 0 : 2 * middle];
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) s[b][r] = fmaf(s[b][r], scale2, x);
+                        for (int r = 0; r < 16; ++r) s[b][r] = fmaf(s[b][r], unit_scale, x);
                     } else {
                         const float* x = table + middle + base + 32 * b + 4 * h - w.lim;
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) s[b][r] = fmaf(s[b][r], scale2, x[8 * (r >> 2) + (r & 3)]);
+                        for (int r = 0; r < 16; ++r) s[b][r] = fmaf(s[b][r], unit_scale, x[8 * (r >> 2) + (r & 3)]);
                     }
                 }
                 if (part) s[b] += of_rows(hidden[buf], b, h);
                 if (diagonal) {
-                    const int room = w.lim - base - 32 * b - 4 * h;
+                    const uint32_t own = bits_up_to(w.lim - base - 32 * b - 4 * h);
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s[b][r] = 8 * (r >> 2) + (r & 3) <= room ? s[b][r] : -INFINITY;
+                    for (int r = 0; r < 16; ++r) s[b][r] = hidden_unless(s[b][r], all_if(own, r));
                 }
 #pragma unroll
                 for (int r = 0; r < 16; ++r) top = __builtin_elementwise_maximum(top, s[b][r]);
             }
             top = max_of_halves(top);
-            if constexpr (!BIAS) top *= scale2;
-            const bool passed = top > m + kLag;
+            const bool passed = top > m + lag;
             if (__ballot(passed)) {
                 const float to = passed ? top : m;
-                const float down = exp2_fast(m - (to == -INFINITY ? 0.f : to));
+                const float down = m == -INFINITY ? 0.f : exp2_fast(exponent_between(m, to, k));
+                off = to == -INFINITY ? 0.f : -(to * k);
+                far = __ballot(fabsf(off) > kFar) != 0;
                 l *= down;
 #pragma unroll
                 for (int db = 0; db < DB; ++db) acc[db] *= down;
                 m = to;
             }
-            const float off = m == -INFINITY ? 0.f : -m;
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 if (b && one) break;
+                if (far) {
+                    const float from = m == -INFINITY ? 0.f : m;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[b][r] = (s[b][r] - from) * k;
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[b][r] = fmaf(s[b][r], k, off);
+                }
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    s[b][r] = exp2_fast(BIAS ? s[b][r] + off : fmaf(s[b][r], scale2, off));
+                    s[b][r] = exp2_fast(s[b][r]);
                     l += s[b][r];
                 }
                 const typename O::Frag p0 = O::round(eight<0>(s[b])), p1 = O::round(eight<8>(s[b]));
@@ -367,7 +407,7 @@ __global__ __launch_bounds__(64 * NW, (kWaves<E, D, NW>)) void k_attention(const
                             f32x4{acc[db][4 * j], acc[db][4 * j + 1], acc[db][4 * j + 2], acc[db][4 * j + 3]};
             } else if (w.real) {
                 const float inv = l == 0.f ? 0.f : 1.f / l;
-                if (h == 0) lse[(int64_t)head * A.total_q + at] = l == 0.f ? -INFINITY : m * LN2 + logf(l);
+                if (h == 0) lse[(int64_t)head * A.total_q + at] = log_of_sum(m, l, k, BIAS ? 1.f : unit_scale);
                 E* o = out + (at * A.heads + head) * D;
 #pragma unroll
                 for (int db = 0; db < DB; ++db)
@@ -378,7 +418,8 @@ __global__ __launch_bounds__(64 * NW, (kWaves<E, D, NW>)) void k_attention(const
             }
             if (!more) return;
             m = -INFINITY;
-            l = 0.f;
+            l = off = 0.f;
+            far = false;
             sees = !MASKED;
 #pragma unroll
             for (int db = 0; db < DB; ++db) acc[db] = {};
@@ -400,6 +441,7 @@ __global__ __launch_bounds__(64 * NW, (kWaves<E, D, NW>)) void k_attention(const
 template <class E, int D>
 __global__ __launch_bounds__(256) void k_attention_join(const AttnArgs A, int splits, const float* o_part, const float2* ml_part,
                                                         E* out, float* lse) {
+    const float unit = A.bias ? 1.f : unit_of_scores(A.scale), k = unit * LOG2E;
     constexpr int LANES = D / 4 <= 8 ? 8 : D / 4 <= 16 ? 16 : 32, PARTS = 64 / LANES, AHEAD = 4;
     const int lane = threadIdx.x & 63;
     const int64_t rows = (int64_t)A.heads * A.total_q, place = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -411,7 +453,6 @@ __global__ __launch_bounds__(256) void k_attention_join(const AttnArgs A, int sp
     for (int s = lane; s < splits; s += 64) m = fmaxf(m, ml_part[s * rows + place].x);
 #pragma unroll
     for (int x = 1; x < 64; x <<= 1) m = fmaxf(m, __shfl_xor(m, x));
-    const float m_use = m == -INFINITY ? 0.f : m;
     const int dim = lane % LANES * 4;
     float l = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
@@ -431,7 +472,7 @@ __global__ __launch_bounds__(256) void k_attention_join(const AttnArgs A, int sp
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) {
             if (ml[j].y == 0.f) continue;
-            const float w = exp2_fast(ml[j].x - m_use);
+            const float w = exp2_fast(exponent_between(ml[j].x, m, k));
             l += ml[j].y * w;
             o += x[j] * w;
         }
@@ -444,7 +485,7 @@ __global__ __launch_bounds__(256) void k_attention_join(const AttnArgs A, int sp
     }
     if (lane >= LANES || dim >= D) return;
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    if (lane == 0) lse[place] = l == 0.f ? -INFINITY : m * LN2 + logf(l);
+    if (lane == 0) lse[place] = log_of_sum(m, l, k, unit);
     Oper<E>::store4(out + (row * A.heads + place / A.total_q) * D + dim, o * inv);
 }
 
@@ -461,6 +502,15 @@ __global__ __launch_bounds__(256) void k_attention_join(const AttnArgs A, int sp
 // them twice, first for delta in 32 bits (60 causal sequences of 1 to 17 tokens: 2.8e-3, so 1.7e-3; of 1 to 301: 2.2e-3 and 1.7e-3.
 // It costs the 512 passages 25 us of 671, with 64 keys 4 us, which leaves 2.1e-3 for sequences of up to 131 tokens).
 constexpr int kTwice = 128;
+// P's error is the rounding of a log-sum-exp in 32 bits, 2^-24 of its size.  Rows where that would show (is_far: from 2^-16 on) are
+// normalised again: exponents are score - lse, which is exact or nearly so, and the first kernel goes over the keys of their tiles
+// twice, first for the sum of what they give, by whose logarithm it and the second kernel correct them, and for delta.
+constexpr float kFarRow = 256.f;
+// (A log-sum-exp is also divided by the scale, where accumulators start from it: that must not overflow.)
+__device__ __forceinline__ bool is_far(float lse, float scale2) {
+    const float a = fabsf(lse);
+    return a < INFINITY && (a > kFarRow || a * LOG2E > 1e30f * scale2);
+}
 // Bound by the matrix and vector units' turns where sequences are long (24 causal pages, 8 heads of 128 over 2: 172 and 228 us, 455
 // TFLOP/s of the three and four products that each cannot do without), by latency and by what surrounds the products where they are
 // short (the 512 passages: 289 and 250 us).
@@ -497,6 +547,8 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
     __shared__ __align__(256) char lds[2][2 * T::BYTES];
     __shared__ __align__(16) float hidden[2][T::ROWS];
     __shared__ float far_sum[kMostRun][NW][2];
+    __shared__ float far_lse[THREADS];                // own log-sum-exp, for far tiles
+    __shared__ int any_row_far[2][NW];                // of a wavefront's rows, for this head unit and the next
     extern __shared__ __align__(16) char dyn[];       // the bias by distance, then histograms of each head and wavefront
     const int tid = threadIdx.x, lane0 = tid & 63, lane = lane0, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     const Work work = work_of(blockIdx.x, slots, (units + run - 1) / run, A.n_seqs, order, true);
@@ -513,8 +565,8 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
     }
     const QueryColumns w(A, t, G, per, wave, lane);
     const int tiles = (t.end + T::ROWS - 1) / T::ROWS;
-    const bool twice = sizeof(E) == 2 && t.end <= kTwice;        // first for delta
-    const int steps = twice ? 2 * tiles : tiles;
+    const bool few = sizeof(E) == 2 && t.end <= kTwice;
+    bool far = false, twice = few;                               // some row of the tile is far; twice: first for delta and sums
     const int64_t krow = A.k_row * (int64_t)sizeof(E), vrow = A.v_row * (int64_t)sizeof(E);
     Staged<E, D, THREADS, MASKED, T::ROWS> next;
     uint8_t next_keep = 0;
@@ -537,7 +589,8 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
     const bool any = tiles > 0;
     if (any) issue(unit, 0, lds[0]);
     Column<E, D> q, g;
-    float dot = 0.f, own_lse = 0.f;
+    float dot = 0.f, own_lse = 0.f;                              // own_lse: what is added to the exponent
+    const float unit_scale = unit_of_scores(A.scale), scale2 = unit_scale * LOG2E;
     auto load_rows = [&](int u) {
         const int64_t at = t.q0 + here(w.row);
         const int h = here(lane0) >> 5, head = u * G + w.head;
@@ -550,6 +603,9 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
         // rows that see nothing take no part, whatever their gradient is: exp2(x - inf) = 0
         const bool seeing = row_lse != -INFINITY;
         own_lse = seeing ? -row_lse * LOG2E : -INFINITY;
+        far_lse[tid] = seeing ? row_lse : INFINITY;
+        const bool is = __ballot(is_far(row_lse, scale2)) != 0;
+        if (lane0 == 0) any_row_far[u & 1][wave] = is;
         dot = 0.f;
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) {
@@ -561,7 +617,7 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
 #pragma unroll
             for (int e = 0; e < 8; ++e) dot += x[e] * y[e];
         }
-        dot = twice ? 0.f : sum_of_halves(dot);
+        dot = few ? 0.f : sum_of_halves(dot);
         q.take_sign(A.scale);
     };
     load_rows(unit);
@@ -579,16 +635,27 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
     float far_lo = 0.f, far_hi = 0.f, weight_lo = 0.f, weight_hi = 0.f;
     f32x16 acc[DB] = {};
     float row_sum = 0.f;
-    const float scale2 = scale_of_scores(A.scale);
     if (any) finish(0);
     __syncthreads();
     const typename T::At at_tiles(lds[0], lane);
+    float weight = 0.f;                                          // sum of a row's probabilities, in a far tile's first pass
     int i = 0, buf = 0;
     while (true) {
+        if (i == 0) {                                            // a head unit begins
+            int is = 0;
+#pragma unroll
+            for (int v = 0; v < NW; ++v) is |= any_row_far[unit & 1][v];
+            far = __builtin_amdgcn_readfirstlane(is) != 0;
+            twice = few || far;
+            if (far) {
+                own_lse = dot = weight = 0.f;
+            }
+        }
         const bool before = twice && i < tiles;
+        const float k = BIAS || far ? LOG2E : scale2;
         const int base = (i < tiles ? i : i - tiles) * T::ROWS;
         const typename T::At lk = at_tiles + buf * 2 * T::BYTES, lv = lk + T::BYTES;
-        const bool last = i + 1 >= steps;
+        const bool last = i + 1 >= (twice ? 2 * tiles : tiles);
         const int n_unit = last ? unit + 1 : unit, n_i = last ? 0 : i + 1;
         const bool more = kRuns<D> ? n_unit < end_unit : !last;
         if (more && any) issue(n_unit, (n_i < tiles ? n_i : n_i - tiles) * T::ROWS, lds[buf ^ 1]);
@@ -609,24 +676,31 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
                 if (BIAS && !side) {
                     const float* x = table + middle + base + 32 * b + 4 * h - w.lim;
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], scale2, x[8 * (r >> 2) + (r & 3)]) + own_lse;
-                } else {
-                    const float x = BIAS ? table[side < 0 ? 0 : 2 * middle] + own_lse : own_lse;
+                    for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], unit_scale, x[8 * (r >> 2) + (r & 3)]);
+                } else if constexpr (BIAS) {
+                    const float x = table[side < 0 ? 0 : 2 * middle];
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], scale2, x);
+                    for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], unit_scale, x);
                 }
                 if (part) s += of_rows(hidden[buf], b, h);
                 if (diagonal) {                       // (dp as well: what the row does not see may be anything)
-                    const int room = w.lim - base - 32 * b - 4 * h;
+                    const uint32_t own = bits_up_to(w.lim - base - 32 * b - 4 * h);
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
-                        const bool own = 8 * (r >> 2) + (r & 3) <= room;
-                        s[r] = own ? s[r] : -INFINITY;
-                        dp[r] = own ? dp[r] : 0.f;
+                        s[r] = hidden_unless(s[r], all_if(own, r));
+                        dp[r] = __uint_as_float(__float_as_uint(dp[r]) & all_if(own, r));
                     }
                 }
+                if (far) {
+                    const float from = far_lse[tid];
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = exp2_fast(s[r]);
+                    for (int r = 0; r < 16; ++r) s[r] = (BIAS ? s[r] : rounded_product(s[r], unit_scale)) - from;
+                    if (before)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) weight += exp2_fast(s[r] * LOG2E);
+                }
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = exp2_fast(fmaf(s[r], k, own_lse));
                 if (BIAS && side && !before) {
                     float weight = 0.f;
 #pragma unroll
@@ -656,9 +730,9 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
                         const typename O::Frag p = O::round(most), rest = O::round(x - most);
 #pragma unroll
                         for (int db = 0; db < DB; ++db) {
-                            const typename O::Frag k = T::turned(lk, b, c, db);
-                            O::mma(acc[db], k, rest);
-                            O::mma(acc[db], k, p);
+                            const typename O::Frag x = T::turned(lk, b, c, db);
+                            O::mma(acc[db], x, rest);
+                            O::mma(acc[db], x, p);
                         }
                     }
                 } else {
@@ -672,6 +746,11 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
         if (before && i + 1 == tiles) {
             dot = sum_of_halves(row_sum);
             row_sum = 0.f;
+            if (far) {
+                weight = sum_of_halves(weight);
+                dot = weight == 0.f ? 0.f : dot / weight;
+                own_lse = weight == 0.f ? 0.f : -log2f(weight);
+            }
         }
         if (last) {
             row_sum = sum_of_halves(row_sum);
@@ -679,6 +758,7 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
             const int head = unit * G + w.head;
             if (w.real) {
                 if (h == 0) delta[(int64_t)head * A.total_q + at] = dot + row_sum;
+                if (far && h == 0) delta[((int64_t)A.heads + head) * A.total_q + at] = own_lse;
                 E* o = dq + (at * A.heads + head) * D;
 #pragma unroll
                 for (int db = 0; db < DB; ++db)
@@ -766,7 +846,8 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int q
     constexpr int WAVES = APART ? 2 * NW : NW, THREADS = 64 * WAVES;
     const bool keys = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) >= NW;        // (APART) this wavefront has the keys' gradient
     __shared__ __align__(256) char lds[2][2 * T::BYTES];
-    __shared__ __align__(16) float row_lse[2][T::ROWS], row_delta[2][T::ROWS];
+    __shared__ __align__(16) float row_lse[2][T::ROWS], row_delta[2][T::ROWS], row_far[2][2][T::ROWS];
+    __shared__ int tile_far[2];                       // some row is far: row_far has log-sum-exps, and what is added to far rows' exponents
     extern __shared__ __align__(16) char dyn[];
     const int tid = threadIdx.x, lane0 = tid & 63, lane = lane0, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     if constexpr (BIAS) {
@@ -803,19 +884,22 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int q
     const char* gp = (const char*)dout + qs.lo * grow;
     Staged<E, D, THREADS, MASKED, T::ROWS> next;
     float n_lse = 0.f, n_delta = 0.f;
-    const float scale2 = scale_of_scores(A.scale);
+    const float unit_scale = unit_of_scores(A.scale), scale2 = unit_scale * LOG2E, per_unit = BIAS ? LOG2E : scale2;
     // 16 bits: a row's log-sum-exp and delta are what its accumulators start from (in 32 bits that would cost the scores an
-    // error of some roundings of the log-sum-exp, which 16-bit results do not show)
+    // error of some roundings of the log-sum-exp, which 16-bit results do not show: it is at most kFarRow there)
     constexpr bool START = sizeof(E) == 2;
+    auto place_of_row = [&](int head0, int c0, int r) {           // of a tile's row among all heads'
+        const int row0 = c0 / G, c1 = c0 - row0 * G, row = G == 1 ? r : (int)((uint32_t)(c1 + r) / (uint32_t)G);
+        return (int64_t)head0 * A.total_q + qs.lo + row0 + row + (int64_t)(c1 + r - row * G) * A.total_q;
+    };
     auto issue = [&](int head0, int c0, char* to) {
         const int row0 = c0 / G, c1 = c0 - row0 * G;              // the tile's first row, and its first column's place in it
-        const int64_t place0 = (int64_t)head0 * A.total_q + qs.lo + row0;
         auto row_of = [&](int r) { return G == 1 ? r : (int)((uint32_t)(c1 + r) / (uint32_t)G); };
         auto offset = [&](int r, uint32_t per_row, uint32_t per_head) {
             const int row = row_of(r);
             return G == 1 ? (uint32_t)row * per_row : (uint32_t)row * per_row + (uint32_t)(c1 + r - row * G) * per_head;
         };
-        auto place = [&](int r) { return place0 + row_of(r) + (int64_t)(c1 + r - row_of(r) * G) * A.total_q; };
+        auto place = [&](int r) { return place_of_row(head0, c0, r); };
         next.issue(qp + row0 * qrow + head0 * qhead, gp + row0 * grow + head0 * ghead, to, cols - c0, tid,
                    [&](int r) { return offset(r, (uint32_t)qrow, (uint32_t)qhead); },
                    [&](int r) { return offset(r, (uint32_t)grow, (uint32_t)ghead); },
@@ -829,12 +913,19 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int q
             }
         }
     };
-    auto finish = [&](int buf) {
+    auto finish = [&](int buf, int head0, int c0) {
         next.finish(lds[buf], tid);
         if (tid < T::ROWS) {
+            const bool own = is_far(n_lse, scale2), far = __ballot(own) != 0;
             // exp2(x - inf) = 0
-            row_lse[buf][tid] = n_lse == -INFINITY ? -INFINITY : -n_lse * (START ? LOG2E / scale2 : LOG2E);
+            const float add = n_lse == -INFINITY ? -INFINITY : -n_lse * (START ? LOG2E / scale2 : LOG2E);
+            if (far) {
+                row_far[buf][0][tid] = n_lse == -INFINITY ? INFINITY : n_lse;
+                row_far[buf][1][tid] = own ? delta[(int64_t)A.heads * A.total_q + place_of_row(head0, c0, tid)] : 0.f;
+            }
+            row_lse[buf][tid] = far ? 0.f : add;
             row_delta[buf][tid] = -n_delta;
+            if (tid == 0) tile_far[buf] = far;
         }
     };
     int head0 = kv0 * A.group, c0 = col0;
@@ -859,7 +950,7 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int q
         __syncthreads();
         fill_bias<E>(A, head0, starts, table, tid, THREADS);
     }
-    if (any) finish(0);
+    if (any) finish(0, head0, c0);
     __syncthreads();
     const typename T::At at_tiles(lds[0], lane);
     int buf = 0;
@@ -873,12 +964,13 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int q
         if (any && busy && c0 + T::ROWS > wfirst) {
             const bool diagonal = A.causal && (wkey + 31 - shift) * G > c0;
             const typename T::At own = APART && !keys ? lg : lq;           // (own gradient's other operand)
+            const bool far = __builtin_amdgcn_readfirstlane(tile_far[buf]) != 0;
 #pragma unroll 1
             for (int b = 0; b < NB && c0 + 32 * b < cols; ++b) {
                 f32x16 s = {}, dp = {};
                 if constexpr (START) s = of_rows(row_lse[buf], b, h);
 #pragma unroll
-                for (int c = 0; c < D / 16; ++c) O::mma(s, T::rows(lq, b, c), k.v[c]);
+                for (int c = 0; c < D / 16; ++c) O::template mma<true>(s, T::rows(lq, b, c), k.v[c]);
                 phase();
                 if (!APART || keys) {
                     if constexpr (START) dp = of_rows(row_delta[buf], b, h);
@@ -886,25 +978,34 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int q
                     for (int c = 0; c < D / 16; ++c) O::mma(dp, T::rows(lg, b, c), v.v[c]);
                     phase();
                 }
-                if constexpr (!START) {
-                    s = s * scale2 + of_rows(row_lse[buf], b, h);
-                    dp += of_rows(row_delta[buf], b, h);
+                if constexpr (!START) dp += of_rows(row_delta[buf], b, h);
+                if constexpr (BIAS) {
+                    const int d0 = wkey - (c0 + 32 * b + shift), side = block_side(d0, A.reach);
+                    if (!side) {
+                        const float* x = table + middle + key - (c0 + 32 * b + shift) - 4 * h - 27;    // of the lane's last row
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], unit_scale, x[27 - 8 * (r >> 2) - (r & 3)]);
+                    } else {
+                        const float x = table[side < 0 ? 0 : 2 * middle];
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], unit_scale, x);
+                    }
                 }
-                const int d0 = wkey - (c0 + 32 * b + shift), side = BIAS ? block_side(d0, A.reach) : 0;
-                const float by = START ? scale2 : 1.f;
-                if (BIAS && !side) {
-                    const float* x = table + middle + key - (c0 + 32 * b + shift) - 4 * h - 27;    // of the lane's last row
+                if (far) {
+                    const f32x16 from = of_rows(row_far[buf][0], b, h), x = of_rows(row_far[buf][1], b, h);
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], by, x[27 - 8 * (r >> 2) - (r & 3)]);
-                } else if constexpr (BIAS || START) {
-                    const float x = BIAS ? table[side < 0 ? 0 : 2 * middle] : 0.f;
+                    for (int r = 0; r < 16; ++r) s[r] = fmaf((BIAS ? s[r] : rounded_product(s[r], unit_scale)) - from[r], LOG2E, x[r]);
+                } else if constexpr (START) {
+                    s *= per_unit;
+                } else {
+                    const f32x16 x = of_rows(row_lse[buf], b, h);
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s[r] = BIAS ? fmaf(s[r], by, x) : s[r] * by;
+                    for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], per_unit, x[r]);
                 }
                 if (diagonal) {                       // a lane's key is seen by columns from (key - shift) G on
-                    const int need = (key - shift) * G - c0 - 32 * b - 4 * h;
+                    const uint32_t own = ~bits_up_to((key - shift) * G - c0 - 32 * b - 4 * h - 1);
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + (r & 3) >= need ? s[r] : -INFINITY;
+                    for (int r = 0; r < 16; ++r) s[r] = hidden_unless(s[r], all_if(own, r));
                 }
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[r] = exp2_fast(s[r]);
@@ -954,7 +1055,7 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int q
                 if constexpr (!APART) acc2[db] = {};
             }
         }
-        if (more && any) finish(buf ^ 1);
+        if (more && any) finish(buf ^ 1, n_head, n_c);
         __syncthreads();
         if (BIAS && n_head != head0) {
             fill_bias<E>(A, n_head, starts, table, tid, THREADS);

@@ -32,7 +32,7 @@ template <class E> struct Oper;
 template <> struct Oper<__bf16> {
     using Frag = bf16x8;
     static constexpr int ROWS = 64;                  // of a staged tile
-    static __device__ __forceinline__ void mma(f32x16& acc, const Frag& a, const Frag& b) {
+    template <bool TURNED = false> static __device__ __forceinline__ void mma(f32x16& acc, const Frag& a, const Frag& b) {
         acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, acc, 0, 0, 0);
     }
     static __device__ __forceinline__ Frag round(const f32x8& x) { return __builtin_convertvector(x, bf16x8); }
@@ -47,10 +47,12 @@ template <> struct Oper<float> {
         __device__ __forceinline__ Frag operator-() const { return {{-p[0], -p[1], -p[2]}}; }
     };
     static constexpr int ROWS = 32;
-    static __device__ __forceinline__ void mma(f32x16& acc, const Frag& a, const Frag& b) {
-        constexpr int A[6] = {2, 0, 1, 1, 0, 0}, B[6] = {0, 2, 1, 0, 1, 0};       // the smallest first
+    // TURNED: the operands are in each other's place; the result is the same to the last bit.
+    template <bool TURNED = false> static __device__ __forceinline__ void mma(f32x16& acc, const Frag& a, const Frag& b) {
+        constexpr int X[6] = {2, 0, 1, 1, 0, 0}, Y[6] = {0, 2, 1, 0, 1, 0};       // the smallest first
 #pragma unroll
-        for (int i = 0; i < 6; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.p[A[i]], b.p[B[i]], acc, 0, 0, 0);
+        for (int i = 0; i < 6; ++i)
+            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.p[TURNED ? Y[i] : X[i]], b.p[TURNED ? X[i] : Y[i]], acc, 0, 0, 0);
     }
     static __device__ __forceinline__ Frag round(const f32x8& x) {
         f32x8 first;

@@ -65,7 +65,7 @@ AttnPlan plan_attention(const AttnArgs& A, int d, int dt, bool backward) {
             P.ml_part = take(rows * 8);
         }
     } else {
-        P.delta = take((int64_t)A.heads * A.total_q * 4);
+        P.delta = take((int64_t)A.heads * A.total_q * 8);        // and a value of rows that are far (is_far)
         if (A.bias) P.bias_part = take(P.q_slots * A.heads * A.n_buckets * 4);
     }
     P.bytes = o;

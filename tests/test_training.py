@@ -382,6 +382,113 @@ def test_a_bias_of_the_lowest_value_hides_a_distance(tr, dev):
         within(b[x][:50], getattr(r, x)[:50], getattr(r, x + "_tol")[:50], x)
 
 
+def check_far(tr, p, ql, kl, dtype, causal=False, scale=None, like=None, by=1.0, lse_of=lambda x: x):
+    """All results of rows whose log-sum-exp may be of any size: it has a 32-bit value's own rounding, and as much again for the
+    product that it is the sum of.  The reference's probabilities are exp(S - lse), which in 64 bits lose a sum's logarithm too
+    where lse is that large: it is then given a problem of the same probabilities (`like`: other inputs, q divided by `by`, a power
+    of two, which is what the keys' gradient differs by), and `lse_of` its log-sum-exp."""
+    f, b = attend(tr, p, ql, kl, causal, scale)
+    a = dict(p, **(like or {}))
+    r = Attention(a["q"], a["k"], a["v"], ql, kl, dtype, causal, scale, a["keep"], a["bias"], 128, a["dout"])
+    r.dk, r.dk_tol, r.lse = r.dk * by, r.dk_tol * by, torch.where(r.lse == -math.inf, r.lse, lse_of(r.lse))
+    lse = f["lse"].double().cpu()
+    assert torch.equal(lse == -math.inf, r.lse == -math.inf)
+    fine = r.lse > -math.inf
+    assert bool(((lse - r.lse).abs() <= F * 2 + 2.0 ** -22 * r.lse.abs())[fine].all())
+    within(f["out"], r.out, r.out_tol, "out")
+    for x in ("dq", "dk", "dv") + (() if p["bias"] is None else ("dbias",)):
+        within(b[x], getattr(r, x), getattr(r, x + "_tol"), x)
+
+
+def extreme(value, dtype):
+    return {"lowest": torch.finfo(DT[dtype]).min, "highest": torch.finfo(DT[dtype]).max}.get(value, value)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [32, 64, 96, 128])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("low", [-1e4, -1e7, -1e9, -1e30, -1e38, "lowest"])
+def test_rows_that_see_nothing_but_a_hidden_distance(tr, dev, dtype, d, causal, low):
+    """A bucket of the table hides distance 0.  Rows that see other keys give it no weight; those that see only this one (the first
+    of a causal sequence, sequences of one token) have all of it there, and all gradients."""
+    lengths = [50, 1, 133, 1]
+    p = problem(dev, dtype, lengths, lengths, 2, 2, d, seed=20, bias=8)
+    p["bias"][0] = extreme(low, dtype)
+    check_far(tr, p, lengths, lengths, dtype, causal)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("ql,kl", [([150, 1, 70], [150, 1, 70]), ([1, 3], [5000, 700])])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("value", ["lowest", -1e30, 1e30, "highest"])
+def test_a_table_that_is_far_from_zero_everywhere(tr, dev, dtype, ql, kl, causal, value):
+    """Products are below such a bias' rounding in 64 bits as well: all keys that are seen weigh the same, in one part or several."""
+    p = problem(dev, dtype, ql, kl, 2, 2, 64, seed=21, bias=32, keep=True)
+    p["bias"][:] = extreme(value, dtype)
+    at, tiny = float(p["bias"][0, 0].double()), 2.0 ** -40
+    check_far(tr, p, ql, kl, dtype, causal, like=dict(q=p["q"].double() * tiny, bias=torch.zeros_like(p["bias"])), by=1 / tiny,
+              lse_of=lambda x: x + at)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_biases_beyond_the_powers_of_two_keep_their_order(tr, dev, dtype):
+    """Values whose product with log2(e) is beyond 32 bits: a row that sees two of them has its weight at the higher one."""
+    lengths = [2, 1, 2]
+    p = problem(dev, dtype, lengths, lengths, 2, 2, 32, seed=22, bias=8)
+    p["bias"][:] = extreme("lowest", dtype)
+    p["bias"][1] = -2.5e38                           # the key before
+    check_far(tr, p, lengths, lengths, dtype, True)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bias", [None, 32])
+@pytest.mark.parametrize("exponent", [10, 20, 30, 60])
+@pytest.mark.parametrize("ql,kl", [([150, 1, 70], [150, 1, 70]), ([1, 3], [5000, 700])])
+def test_scores_of_any_size(tr, dev, dtype, bias, exponent, ql, kl):
+    """Whole numbers times a power of two: products are exact in 32 bits, and a row has one key, or equal ones that share it."""
+    p = problem(dev, dtype, ql, kl, 4, 2, 64, seed=23, bias=bias)
+    g = torch.Generator().manual_seed(24)
+    for x, by in (("q", 2.0 ** exponent), ("k", 1.0)):
+        p[x] = (torch.randint(-8, 9, p[x].shape, generator=g) * by).to(DT[dtype]).to(dev)
+    if bias:
+        p["bias"].zero_()
+    by = 2.0 ** (exponent - 10)                      # (at 2^10 scores are multiples of 128: the next one has nothing)
+    check_far(tr, p, ql, kl, dtype, like=dict(q=p["q"].double() / by), by=by, lse_of=lambda x: (x / 128).round() * 128 * by + (x - (x / 128).round() * 128))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bias", [None, 32])
+@pytest.mark.parametrize("d", [64, 128])
+def test_scores_of_any_size_that_are_rounded(tr, dev, dtype, bias, d):
+    """Scores of some 2^30, whose rounding in 32 bits is 2^7: a row has one key, the gradients' kernels have to find the very scores
+    of the forward pass.  Rows whose first two scores are closer than 2^-16 of their size take no part."""
+    lengths = [150, 1, 70]
+    p = problem(dev, dtype, lengths, lengths, 4, 2, d, seed=26, bias=bias, size=2.0 ** 30)
+    S = torch.einsum("qhd,khd->hqk", p["q"].double().cpu(), p["k"].double().cpu().repeat_interleave(2, 1))
+    own = torch.block_diag(*[torch.ones(n, n) for n in lengths]).bool()
+    top = S.masked_fill(~own, -math.inf).topk(2, -1).values
+    p["dout"][((top[..., 0] - top[..., 1]) < 2.0 ** -16 * top[..., 0].abs()).T.to(dev)] = 0
+    f, b = attend(tr, p, lengths, lengths)
+    r = Attention(p["q"], p["k"], p["v"], lengths, lengths, dtype, bias=p["bias"], dout=p["dout"])
+    for x in ("dq", "dk", "dv") + (() if bias is None else ("dbias",)):
+        within(b[x], getattr(r, x), getattr(r, x + "_tol"), x)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bias", [None, 8])
+def test_a_scale_near_zero(tr, dev, dtype, bias):
+    """A log-sum-exp divided by it is beyond 32 bits."""
+    lengths = [200, 33]
+    p = problem(dev, dtype, lengths, lengths, 2, 1, 64, seed=25, bias=bias)
+    check_far(tr, p, lengths, lengths, dtype, scale=1.2e-38)
+
+
 @gpu
 @pytest.mark.parametrize("size", [30.0, 1e-3])
 def test_sharp_and_flat_rows(tr, dev, size):
