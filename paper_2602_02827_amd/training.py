@@ -97,8 +97,10 @@ def _workspace(ws, need, device):
         return None, 0
     if ws is None:
         ws = torch.empty(need, dtype=torch.uint8, device=device)
-    elif not ws.is_contiguous():
-        raise ValueError("the workspace must be contiguous")
+    else:
+        _on_device(ws)
+        if not ws.is_contiguous():
+            raise ValueError("the workspace must be contiguous")
     return ws, ws.numel() * ws.element_size()
 
 
@@ -158,6 +160,7 @@ def colbandit_attention(q, k, v, q_offsets, k_offsets=None, *, causal=False, sca
     o = q.new_empty(q.shape) if o is None else _dense(o, q.shape, q.dtype, "out")
     lse = q.new_empty((q.shape[1], q.shape[0]), dtype=torch.float32) if lse is None else \
         _dense(lse, (q.shape[1], q.shape[0]), torch.float32, "lse")
+    _on_device(o, lse)
     ws, nb = _workspace(workspace, L.colbandit_attention_workspace_bytes(a, 0), q.device)
     _check(L.colbandit_attention(a, o.data_ptr(), lse.data_ptr(), _ptr(ws), nb, _stream()), "colbandit_attention")
     return {"out": o, "lse": lse}
@@ -243,7 +246,7 @@ def colbandit_clip_gradients(grads, max_norm, out=None, workspace=None):
             raise TypeError("gradients must be float32 or bfloat16, and outputs of their types")
         if not g.is_contiguous() or not o.is_contiguous() or o.shape != g.shape:
             raise ValueError("gradients and outputs must be contiguous, and outputs of their shapes")
-    _on_device(*grads)
+    _on_device(*grads, *to)
     n = len(grads)
     pointers = ctypes.c_void_p * n
     sizes = (ctypes.c_int64 * n)(*[g.numel() for g in grads])

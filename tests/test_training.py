@@ -946,3 +946,31 @@ def test_python_refusals(tr):
             continue                                 # the last: tensors that are not on the device
         with pytest.raises((TypeError, ValueError, RuntimeError, AssertionError)):
             tr.colbandit_attention(a["q"], a["k"], a["v"], a["off"], a["k_off"], keep=a["keep"], bias=a["bias"])
+
+
+def test_what_a_call_writes_must_be_on_the_device(tr, monkeypatch):
+    """Outputs and workspaces that lie elsewhere are refused before the library is called (here by a stand-in of it, with the tensors'
+    places made up, so that nothing is launched)."""
+    class Library:
+        def __getattr__(self, name):
+            return (lambda *a: 256) if name.endswith("workspace_bytes") else lambda *a: pytest.fail(name + " was called")
+    elsewhere = []
+    monkeypatch.setattr(tr, "lib", Library)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda t: -1 if any(t is x for x in elsewhere) else 0)
+    q, off = torch.zeros(10, 2, 64), torch.tensor([0, 10])
+    g, out, lse, ws = [torch.zeros(5), torch.zeros(3)], torch.zeros_like(q), torch.zeros(2, 10), torch.zeros(256, dtype=torch.uint8)
+    to = [torch.zeros(5), torch.zeros(3)]
+    calls = {
+        "out": (out, lambda: tr.colbandit_attention(q, q, q, off, out={"out": out, "lse": lse}, workspace=ws)),
+        "lse": (lse, lambda: tr.colbandit_attention(q, q, q, off, out={"out": out, "lse": lse}, workspace=ws)),
+        "workspace": (ws, lambda: tr.colbandit_attention(q, q, q, off, workspace=ws)),
+        "backward workspace": (ws, lambda: tr.colbandit_attention_backward(q, q, q, q, out, lse, off, workspace=ws)),
+        "clipped": (to[1], lambda: tr.colbandit_clip_gradients(g, 1.0, out=to, workspace=ws)),
+        "clip workspace": (ws, lambda: tr.colbandit_clip_gradients(g, 1.0, workspace=ws)),
+    }
+    for name, (tensor, call) in calls.items():
+        elsewhere[:] = [tensor]
+        with pytest.raises(ValueError, match="current device"):
+            call()
+            pytest.fail(name)
