@@ -262,6 +262,26 @@ def colbandit_clip_gradients(grads, max_norm, out=None, workspace=None):
 # ---- as parts of a torch program ---------------------------------------------------------------------
 
 
+class _FirstOrderOnly(torch.autograd.Function):
+    """Gradients as they are; whatever is differentiated through them is an error and not left out."""
+    @staticmethod
+    def forward(ctx, n, *tensors):
+        return tensors[:n]
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("second-order gradients of the training operators are not available")
+
+
+def _first_order(grads, *inputs):
+    """`grads` of a backward pass; where they are themselves to be differentiated (create_graph), tied to its inputs."""
+    if not torch.is_grad_enabled() or not any(t is not None and t.requires_grad for t in inputs):
+        return grads
+    there = [g for g in grads if g is not None]
+    tied = iter(_FirstOrderOnly.apply(len(there), *there, *(t for t in inputs if t is not None)))
+    return tuple(None if g is None else next(tied) for g in grads)
+
+
 class _Attention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, bias, q_offsets, k_offsets, keep, how):
@@ -275,11 +295,11 @@ class _Attention(torch.autograd.Function):
         q, k, v, bias, q_offsets, k_offsets, keep, out, lse = ctx.saved_tensors
         g = colbandit_attention_backward(dout.contiguous(), q, k, v, out, lse, q_offsets, k_offsets, keep=keep, bias=bias,
                                          **ctx.how)
-        return g["dq"], g["dk"], g["dv"], g["dbias"], None, None, None, None
+        return *_first_order((g["dq"], g["dk"], g["dv"], g["dbias"]), q, k, v, bias, dout), None, None, None, None
 
 
 def attention(q, k, v, q_offsets, k_offsets=None, *, causal=False, scale=None, keep=None, bias=None, max_distance=128):
-    """colbandit_attention's output, differentiable in q, k, v and bias."""
+    """colbandit_attention's output, differentiable in q, k, v and bias (once: second-order gradients are an error)."""
     return _Attention.apply(q, k, v, bias, q_offsets, k_offsets, keep,
                             dict(causal=causal, scale=scale, max_distance=max_distance))
 
@@ -297,12 +317,12 @@ class _ContrastiveMaxSim(torch.autograd.Function):
     def backward(ctx, dloss):
         dscores, argmax, Q, docs, offsets = ctx.saved_tensors
         g = colbandit_maxsim_backward(dscores * dloss, argmax, Q, docs, offsets)
-        return g["dQ"], g["ddocs"], None, None, None
+        return *_first_order((g["dQ"], g["ddocs"]), Q, docs, dloss), None, None, None
 
 
 def contrastive_maxsim(Q, docs, offsets, targets, temperature=1.0):
     """Mean contrastive loss of queries Q [n_queries, T, d] against packed documents, differentiable in
-    Q and docs; targets int64 [n_queries], -1 leaves a query out."""
+    Q and docs (once: second-order gradients are an error); targets int64 [n_queries], -1 leaves a query out."""
     return _ContrastiveMaxSim.apply(Q, docs, offsets, targets, float(temperature))
 
 

@@ -974,3 +974,39 @@ def test_what_a_call_writes_must_be_on_the_device(tr, monkeypatch):
         with pytest.raises(ValueError, match="current device"):
             call()
             pytest.fail(name)
+
+
+def second_order_is_an_error(value, x):
+    """First-order gradients as ever; a penalty on them is no term that is left out."""
+    (value() * 2).backward()
+    first, x.grad = x.grad, None
+    g, = torch.autograd.grad(value(), x, create_graph=True)
+    assert torch.equal(g * 2, first)
+    with pytest.raises(RuntimeError, match="second-order"):
+        (g.square().sum() + x.square().sum()).backward()
+
+
+def test_second_order_gradients_are_refused(tr, monkeypatch):
+    """The autograd forms over stand-ins of the library's calls."""
+    monkeypatch.setattr(tr, "colbandit_attention", lambda q, *a, **k: {"out": q.detach() * 3, "lse": q.new_zeros(2, 10)})
+    monkeypatch.setattr(tr, "colbandit_attention_backward", lambda dout, q, k, v, *a, bias=None, **h: {
+        "dq": dout * 3, "dk": torch.zeros_like(k), "dv": torch.zeros_like(v), "dbias": None if bias is None else torch.zeros_like(bias)})
+    monkeypatch.setattr(tr, "colbandit_maxsim_scores", lambda Q, docs, off: {"scores": Q.detach().sum((1, 2))[:, None], "argmax": off})
+    monkeypatch.setattr(tr, "colbandit_contrastive_loss", lambda s, t, temp: {"loss": s[:, 0], "dscores": torch.ones_like(s) / len(s)})
+    monkeypatch.setattr(tr, "colbandit_maxsim_backward", lambda d, a, Q, docs, off: {
+        "dQ": d[:, :, None].expand(Q.shape).clone(), "ddocs": torch.zeros_like(docs)})
+    q, off = torch.randn(10, 2, 64, requires_grad=True), torch.tensor([0, 10])
+    for bias in (None, torch.zeros(32, 2, requires_grad=True)):
+        q.grad = None
+        second_order_is_an_error(lambda: tr.attention(q, q.detach(), q.detach(), off, bias=bias).sum(), q)
+    Q, docs = torch.randn(3, 4, 32, requires_grad=True), torch.randn(7, 32)
+    second_order_is_an_error(lambda: tr.contrastive_maxsim(Q, docs, torch.tensor([0, 7]), torch.zeros(3, dtype=torch.int64)), Q)
+
+
+@gpu
+def test_second_order_gradients_are_refused_on_the_device(tr, dev):
+    q, off = torch.randn(10, 2, 64, device=dev, requires_grad=True), torch.tensor([0, 4, 10], device=dev)
+    second_order_is_an_error(lambda: tr.attention(q, q.detach() * 0.5, q.detach(), off).sum(), q)
+    Q, D, docs = embeddings(dev, "f32", 3, 7, [5, 6], 32)
+    Q.requires_grad_()
+    second_order_is_an_error(lambda: tr.contrastive_maxsim(Q, D, docs, torch.tensor([0, 1, 0], device=dev)), Q)
