@@ -55,9 +55,11 @@ extern "C" {
  * Rows of q, k and v lie q_row elements apart and heads q_head apart (likewise k, v); the d
  * values of a row and head are consecutive.  Pointers and strides are whole multiples of 16
  * bytes; rows lie at most 32 MiB apart.  out and all gradients are dense, [rows][heads][d].
- * Preconditions the host cannot check without a copy: offsets are non-decreasing, from 0 to
- * total_q (total_k).  Kernels clamp them, so a violation gives meaningless results, never an
- * out-of-bounds access; rows that no sequence holds are not written.
+ * Rows behind the last sequence (a batch padded to a round size) belong to none: out 0, lse -inf,
+ * all gradients 0, whatever they hold.
+ * Preconditions the host cannot check without a copy: offsets are non-decreasing, from 0 to at
+ * most total_q (total_k).  Kernels clamp them, so a violation gives meaningless results and rows
+ * that are not written, never an out-of-bounds access.
  */
 typedef struct {
     int dt;                        /* colbandit_dtype of q, k, v, bias, out, gradients   */
@@ -140,7 +142,8 @@ int colbandit_contrastive_loss(const float *scores, int n_queries, int64_t N,
  * dQ[q][t]       = sum_i dscores[q][i] * docs[offsets[i] + argmax[q][i][t]]
  * ddocs[row]     = sum of dscores[q][i] * Q[q][t] over the (q, t) that chose the row
  * Sums in 32 bits, in a fixed order.  dQ [n_queries][T][d] and ddocs [total_tokens][d] have the
- * storage type and are 16-byte aligned; tokens that nobody chose get zeros.
+ * storage type and are 16-byte aligned; tokens that nobody chose get zeros, and so do those
+ * behind the last document.
  */
 int colbandit_maxsim_backward(const float *dscores, const int32_t *argmax, const void *Q,
                               int n_queries, int T, int d, colbandit_dtype dt, const void *docs,

@@ -56,7 +56,7 @@ __host__ __forceinline__ size_t bias_bytes(int reach, int tables) { return kStar
 // forward and backward: 700 us, as they come 722; 48 pages, where a head's tiles are kept together as they come: 588 and 578).
 // LONGEST_FIRST: under a causal limit the later rows see more keys (earlier keys are seen by more rows): places go round the
 // sequences, each one's longest tiles first (`down`: its last ones), so that short ones are left for the end.  Sequences are taken
-// to be of one length; others are only in another order (24 causal pages, forward and backward: 492 us, as they come 561).
+// to be of one length; others are only in another order; the last place, which only rows behind the last sequence can have, stays (24 causal pages, forward and backward: 492 us, as they come 561).
 __device__ __forceinline__ int in_order(int block, int blocks) {
     const int lg = blocks < 128 ? 0 : blocks >= 4096 ? 6 : 25 - __builtin_clz(blocks);
     const int whole = blocks >> (lg + 3) << (lg + 3), xcd = block & 7, i = block >> 3;
@@ -71,7 +71,7 @@ __device__ __forceinline__ int longest_first(int x, int slots, int n, bool down)
 struct Work { int slot, inner; };
 __device__ __forceinline__ Work work_of(int block, int slots, int inner, int n, int order, bool down) {
     const int x = order == BY_XCD ? in_order(block, slots * inner) : block, slot = x / inner;
-    return {order == LONGEST_FIRST ? longest_first(slot, slots, n, down) : slot, x - slot * inner};
+    return {order == LONGEST_FIRST && slot < slots - 1 ? longest_first(slot, slots - 1, n, down) : slot, x - slot * inner};
 }
 // Which way a block of 32 rows and columns lies whose first key and row are d0 apart: -1 or 1: all beyond reach, 0: not.
 __device__ __forceinline__ int block_side(int d0, int reach) { return d0 + 31 <= -reach ? -1 : d0 - 31 >= reach ? 1 : 0; }
@@ -154,7 +154,9 @@ struct QueryTile {
     bool none;
     __device__ __forceinline__ QueryTile(const AttnArgs& A, int slot, int per, int lane) {
         const int seq = find_sequence(A.qoff, A.n_seqs, per, A.total_q, slot, lane);
-        const Range q = sequence_rows(A.qoff, seq, A.total_q, per), k = sequence_rows(A.koff, seq, A.total_k);
+        bool rest;
+        const Range q = rows_of_place(A.qoff, seq, A.n_seqs, A.total_q, per, slot, rest);
+        const Range k = rest ? Range{0, 0, 0} : sequence_rows(A.koff, seq, A.total_k);
         row0 = (slot - q.place) * per;
         Lq = q.n;
         Lk = k.n;
@@ -446,9 +448,8 @@ __global__ __launch_bounds__(256) void k_attention_join(const AttnArgs A, int sp
     const int lane = threadIdx.x & 63;
     const int64_t rows = (int64_t)A.heads * A.total_q, place = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (place >= rows) return;
-    // rows that no sequence holds have no parts: they are not written by any call, nor is their output
     const int64_t row = place % A.total_q;
-    if (row < A.qoff[0] || row >= A.qoff[A.n_seqs]) return;
+    if (row < A.qoff[0]) return;                     // no sequence's, and no parts either
     float m = -INFINITY;
     for (int s = lane; s < splits; s += 64) m = fmaxf(m, ml_part[s * rows + place].x);
 #pragma unroll
@@ -867,7 +868,9 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int q
     const int slot = work.slot, kv0 = work.inner * run;
     const int kv_end = kv0 + run < A.kv_heads ? kv0 + run : A.kv_heads;
     const int seq = find_sequence(A.koff, A.n_seqs, COLS, A.total_k, slot, lane);
-    const Range ks = sequence_rows(A.koff, seq, A.total_k, COLS), qs = sequence_rows(A.qoff, seq, A.total_q);
+    bool rest;
+    const Range ks = rows_of_place(A.koff, seq, A.n_seqs, A.total_k, COLS, slot, rest);
+    const Range qs = rest ? Range{0, 0, 0} : sequence_rows(A.qoff, seq, A.total_q);
     const int key0 = (slot - ks.place) * COLS;
     if (key0 < 0 || key0 >= ks.n) return;
     const int wkey = key0 + wave % NW * 32, key = wkey + (lane & 31), shift = ks.n - qs.n;

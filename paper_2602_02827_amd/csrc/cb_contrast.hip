@@ -271,10 +271,17 @@ __device__ __forceinline__ void document_gradient(char* lds, int block, const fl
     TokenLists<D, MANY>& s = *(TokenLists<D, MANY>*)lds;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int doc = find_sequence(off, N, kTokens, total, block, lane);
-    const Range r = sequence_rows(off, doc, total, kTokens);
+    bool rest;
+    const Range r = rows_of_place(off, doc, N, total, kTokens, block, rest);
     const int first = (block - r.place) * kTokens;
     if (first < 0 || first >= r.n) return;
     const int piece = tid % R::LANES, group = tid / R::LANES;
+    if (rest) {                                      // tokens of no document
+        const float none[R::PER] = {};
+        for (int token = first + group; token < r.n && token < first + kTokens; token += GROUPS)
+            if (piece < R::PIECES) R::store(ddocs + (int64_t)(r.lo + token) * D, piece, none);
+        return;
+    }
     const int entries = nq * T;
     if constexpr (MANY)
         for (int i = tid; i < kTokens * D; i += 256) (&s.rows[0][0])[i] = 0.f;
@@ -457,7 +464,7 @@ hipError_t launch_maxsim_backward(const float* dscores, const int32_t* argmax, c
     return by_type_and_width(dt, d, [&](auto type, auto dc) {
         using E = decltype(type);
         constexpr int D = decltype(dc)::value;
-        const int doc_blocks = total > 0 ? (int)(total / kTokens + N) : 0;
+        const int doc_blocks = total > 0 ? (int)(total / kTokens + N + 1) : 0;
         auto go = [&](auto many) {
             k_maxsim_gradients<E, D, decltype(many)::value><<<dim3((unsigned)(doc_blocks + nq * T)), 256, 0, st>>>(
                 dscores, argmax, (const E*)Q, nq, T, (const E*)docs, off, (int)N, (int)total, doc_blocks, (E*)dQ, (E*)ddocs);

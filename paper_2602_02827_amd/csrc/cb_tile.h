@@ -215,7 +215,7 @@ template <class E, int D, int THREADS, int R = Oper<E>::ROWS> struct Rows {
 };
 
 // Tiles of ragged sequences: sequence i begins at place off[i] / per + i, which leaves room for all its tiles of `per` rows
-// and needs no table.  Finds the sequence of a place (all lanes of a wavefront together), 64 offsets at a time.
+// and needs no table.  Rows behind the last sequence follow as one more.  Finds the sequence of a place (all lanes of a wavefront together), 64 offsets at a time.
 __device__ __forceinline__ int place_of(int64_t x, int i, int per, int total) {
     x = x < 0 ? 0 : x > total ? total : x;
     return (int)((uint32_t)x / (uint32_t)per) + i;
@@ -240,6 +240,13 @@ __device__ __forceinline__ Range sequence_rows(const int64_t* off, int i, int to
     a = a < 0 ? 0 : a > total ? total : a;
     b = b < a ? a : b > total ? total : b;
     return {(int)a, (int)(b - a), place_of(a, i, per, total)};
+}
+// The same for the sequence of a place, of n; rest: the place is one of the rows behind the last sequence, and these are meant.
+__device__ __forceinline__ Range rows_of_place(const int64_t* off, int i, int n, int total, int per, int place, bool& rest) {
+    const Range r = sequence_rows(off, i, total, per);
+    const int end = r.lo + r.n, after = place_of(end, n, per, total);
+    rest = i == n - 1 && place >= after;
+    return rest ? Range{end, total - end, after} : r;
 }
 
 }  // namespace cb

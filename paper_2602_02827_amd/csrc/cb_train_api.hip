@@ -43,6 +43,9 @@ AttnPlan plan_attention(const AttnArgs& A, int d, int dt, bool backward) {
     P.run = d <= 64 ? run_of(P.q_slots, P.units, k_rows) : 1;
     P.kv_run = d <= 64 ? run_of(P.k_slots, A.kv_heads, (int64_t)A.total_q * A.group / A.n_seqs) : 1;
     if (A.bias && A.reach > 128) P.run = 1;          // (histograms of all its heads are in LDS)
+    const int64_t groups = P.q_slots * P.units;
+    ++P.q_slots;                                     // the rows behind the last sequence may end in a tile of their own
+    ++P.k_slots;
     size_t o = 0;
     auto take = [&](int64_t bytes) {
         const size_t at = o;
@@ -53,7 +56,6 @@ AttnPlan plan_attention(const AttnArgs& A, int d, int dt, bool backward) {
         // Few tiles over long keys: their keys are cut into parts of 128 rows or more (on average; the longest sequence's are
         // longer) until there are 2,048 workgroups.  16 tokens over 1 to 16,385 keys, us: 50 so, 53 with 256 rows and 1,024, 65 with
         // 128 and 4,096, 80 with 512 and 1,024.
-        const int64_t groups = P.q_slots * P.units;
         if (groups < 512 && k_rows >= 512) {
             int64_t s = (2048 - 1 + groups) / groups;
             s = s < k_rows / 128 ? s : k_rows / 128;

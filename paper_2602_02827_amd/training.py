@@ -151,8 +151,8 @@ def _dense(t, shape, dtype, what):
 def colbandit_attention(q, k, v, q_offsets, k_offsets=None, *, causal=False, scale=None, keep=None, bias=None,
                         max_distance=128, workspace=None, out=None):
     """Attention over packed sequences.  q [total_q, heads, d], k and v [total_k, kv_heads, d] (any
-    row and head strides), offsets int64 [n+1]; `k_offsets` None: the queries' own.  `out`: tensors
-    to write, as this returns them.  Returns dict(out [total_q, heads, d], lse float32
+    row and head strides), offsets int64 [n+1]; `k_offsets` None: the queries' own; rows behind the last
+    sequence get zeros.  `out`: tensors to write, as this returns them.  Returns dict(out [total_q, heads, d], lse float32
     [heads, total_q])."""
     a = _attn(q, k, v, q_offsets, k_offsets, causal, scale, keep, bias, max_distance)
     L = lib()

@@ -1010,3 +1010,48 @@ def test_second_order_gradients_are_refused_on_the_device(tr, dev):
     Q, D, docs = embeddings(dev, "f32", 3, 7, [5, 6], 32)
     Q.requires_grad_()
     second_order_is_an_error(lambda: tr.contrastive_maxsim(Q, D, docs, torch.tensor([0, 1, 0], device=dev)), Q)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("ql,kl,H,Hk,d,bias", [([40, 3], [40, 3], 2, 2, 64, 8), ([1, 1, 1], [2000, 7, 900], 4, 1, 128, None),
+                                               ([130, 0, 300, 64], [130, 0, 300, 64], 6, 2, 32, None), ([5], [5], 1, 1, 96, 32)])
+@pytest.mark.parametrize("more", [1, 31, 64, 128, 333])
+def test_rows_behind_the_last_sequence_get_zeros(tr, dev, dtype, ql, kl, H, Hk, d, bias, more):
+    """A batch padded to a round size, with NaN: the sequences' results are those without it (the plan may be another), the other
+    rows' are zeros, and minus infinity for the log-sum-exp."""
+    p = problem(dev, dtype, ql, kl, H, Hk, d, seed=27, bias=bias, keep=True)
+    r = Attention(p["q"], p["k"], p["v"], ql, kl, dtype, keep=p["keep"], bias=p["bias"], dout=p["dout"])
+    nq, nk = sum(ql), sum(kl)
+    far = {x: torch.full((p[x].shape[0] + more, *p[x].shape[1:]), math.nan, dtype=DT[dtype], device=dev) for x in ("q", "k", "v", "dout")}
+    for x in far:
+        far[x][:len(p[x])] = p[x]
+    far["keep"] = torch.ones(nk + more, dtype=torch.bool, device=dev)
+    far["keep"][:nk] = p["keep"]
+    for x in ("q", "k", "v"):                        # what the allocator gives next held other values
+        torch.full_like(far[x], 7.0)
+    f, b = attend(tr, dict(far, bias=p["bias"]), ql, kl)
+    within(f["out"][:nq], r.out, r.out_tol, "out")
+    assert not f["out"][nq:].any() and bool((f["lse"][:, nq:] == -math.inf).all())
+    for x, n in (("dq", nq), ("dk", nk), ("dv", nk)):
+        within(b[x][:n], getattr(r, x), getattr(r, x + "_tol"), x)
+        assert not b[x][n:].any(), x
+    if bias is not None:
+        within(b["dbias"], r.dbias, r.dbias_tol, "dbias")
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nq,T", [(3, 7), (150, 32)])
+@pytest.mark.parametrize("lengths", [[50, 0, 64, 3], [1]])
+@pytest.mark.parametrize("more", [1, 64, 200])
+def test_tokens_behind_the_last_document_get_zeros(tr, dev, dtype, nq, T, lengths, more):
+    Q, D, off = embeddings(dev, dtype, nq, T, lengths, 96, seed=28)
+    padded = torch.cat([D, torch.full((more, 96), math.nan, dtype=D.dtype, device=dev)])
+    f, g = tr.colbandit_maxsim_scores(Q, D, off), tr.colbandit_maxsim_scores(Q, padded, off)
+    assert torch.equal(f["scores"], g["scores"]) and torch.equal(f["argmax"], g["argmax"])
+    dscores = torch.randn(nq, len(lengths), generator=torch.Generator().manual_seed(1)).to(dev)
+    want = tr.colbandit_maxsim_backward(dscores, f["argmax"], Q, D, off)
+    torch.full_like(padded, 7.0)
+    got = tr.colbandit_maxsim_backward(dscores, f["argmax"], Q, padded, off)
+    assert torch.equal(got["dQ"], want["dQ"]) and torch.equal(got["ddocs"][:len(D)], want["ddocs"]) and not got["ddocs"][len(D):].any()
