@@ -32,7 +32,10 @@ extern "C" {
 #endif
 
 /* Limits (requests beyond them return COLBANDIT_ERR_UNSUPPORTED).
- * Head width and embedding width: 32, 64, 96 or 128.  Rows: below 2^31 - 2^16. */
+ * Head width and embedding width: 32, 64, 96 or 128.  Rows: below 2^31 - 2^16.  Heads: 4,096.
+ * A launch has less than 2^32 threads, which bounds attention at some 2^31 query rows (key rows)
+ * times heads, and at 2^24 sequences times heads (one head a workgroup of 256 threads), and the
+ * gradients of MaxSim at 2^24 documents, 64-token tiles and query tokens together. */
 #define COLBANDIT_MAX_DISTANCE 256   /* last distance with a bucket of its own range     */
 #define COLBANDIT_MAX_BUCKETS 128    /* rows of the bias table                           */
 

@@ -458,13 +458,16 @@ hipError_t launch_contrastive_loss(const float* scores, int nq, int64_t N, const
     return hipGetLastError();
 }
 
+static int64_t document_groups(int64_t N, int64_t total) { return total > 0 ? total / kTokens + N + 1 : 0; }
+int64_t maxsim_backward_groups(int nq, int T, int64_t N, int64_t total) { return document_groups(N, total) + (int64_t)nq * T; }
+
 hipError_t launch_maxsim_backward(const float* dscores, const int32_t* argmax, const void* Q, int nq, int T, int d, int dt,
                                   const void* docs, const int64_t* off, int64_t N, int64_t total, void* dQ, void* ddocs,
                                   hipStream_t st) {
     return by_type_and_width(dt, d, [&](auto type, auto dc) {
         using E = decltype(type);
         constexpr int D = decltype(dc)::value;
-        const int doc_blocks = total > 0 ? (int)(total / kTokens + N + 1) : 0;
+        const int doc_blocks = (int)document_groups(N, total);
         auto go = [&](auto many) {
             k_maxsim_gradients<E, D, decltype(many)::value><<<dim3((unsigned)(doc_blocks + nq * T)), 256, 0, st>>>(
                 dscores, argmax, (const E*)Q, nq, T, (const E*)docs, off, (int)N, (int)total, doc_blocks, (E*)dQ, (E*)ddocs);

@@ -54,6 +54,7 @@ hipError_t launch_maxsim_scores(const void* Q, int nq, int T, int d, int dt, con
                                 int64_t total, float* scores, int32_t* argmax, hipStream_t st);
 hipError_t launch_contrastive_loss(const float* scores, int nq, int64_t N, const int64_t* targets, float temperature,
                                    float* loss, float* dscores, hipStream_t st);
+int64_t maxsim_backward_groups(int nq, int T, int64_t N, int64_t total);     // of 256 threads
 hipError_t launch_maxsim_backward(const float* dscores, const int32_t* argmax, const void* Q, int nq, int T, int d, int dt,
                                   const void* docs, const int64_t* off, int64_t N, int64_t total, void* dQ, void* ddocs,
                                   hipStream_t st);

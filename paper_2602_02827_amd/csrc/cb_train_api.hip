@@ -172,11 +172,16 @@ int attn_args(const colbandit_attn* a, AttnArgs& A) {
     return COLBANDIT_OK;
 }
 
-// Workgroups of any launch of the plan fit a grid.
+// Threads of one launch, below 2^32.
+bool fits_a_grid(int64_t groups, int64_t threads) { return groups <= 0xffffffffll / threads; }
+
+// Every launch of the plan can be made.
 bool launchable(const AttnArgs& A, const AttnPlan& P) {
-    const int64_t most = 0x7fffffff;
-    return P.q_slots <= most / P.units / P.splits && P.k_slots <= (most - (1 << 20)) / A.kv_heads && A.heads <= 1 << 12 &&
-           (int64_t)A.heads * A.total_q <= most * 32 && P.bytes < (1ull << 46);
+    if (A.heads > 1 << 12 || P.bytes >= (1ull << 46)) return false;
+    const int64_t rows = (int64_t)A.heads * A.total_q, entries = A.bias ? (int64_t)A.n_buckets * A.heads : 0;
+    return fits_a_grid(P.q_slots * ((P.units + P.run - 1) / P.run) * P.splits, 64 * P.q_waves) &&
+           fits_a_grid(P.k_slots * ((A.kv_heads + P.kv_run - 1) / P.kv_run) + entries, 128 * P.k_waves) &&      // (some have twice as many)
+           (P.splits == 1 || fits_a_grid((rows + 3) / 4, 256));
 }
 
 int check_maxsim(const void* Q, int nq, int T, int d, int dt, const void* docs, const int64_t* off, int64_t N, int64_t total) {
@@ -184,7 +189,7 @@ int check_maxsim(const void* Q, int nq, int T, int d, int dt, const void* docs, 
     if (nq < 1 || T < 1 || d < 1 || N < 1 || total < 0) return COLBANDIT_ERR_SHAPE;
     if (dt != COLBANDIT_F32 && dt != COLBANDIT_BF16) return COLBANDIT_ERR_SHAPE;
     if (d != 32 && d != 64 && d != 96 && d != 128) return COLBANDIT_ERR_UNSUPPORTED;
-    // N: places of documents' tiles and entries are counted in 31 bits
+    // places of documents' tiles and entries are counted in 31 bits
     if (T > COLBANDIT_MAX_T || nq > 65535 || total > kMostRows || N > (1 << 28)) return COLBANDIT_ERR_UNSUPPORTED;
     if (misaligned(Q) || misaligned(docs) || misaligned(off, 8)) return COLBANDIT_ERR_ALIGNMENT;
     return COLBANDIT_OK;
@@ -273,6 +278,7 @@ int colbandit_maxsim_backward(const float* dscores, const int32_t* argmax, const
                               void* ddocs, void* stream) {
     const int rc = check_maxsim(Q, n_queries, T, d, dt, docs, offsets, N, total_tokens);
     if (rc) return rc;
+    if (!fits_a_grid(maxsim_backward_groups(n_queries, T, N, total_tokens), 256)) return COLBANDIT_ERR_UNSUPPORTED;
     if (!dscores || !argmax || !dQ || (total_tokens && !ddocs)) return COLBANDIT_ERR_NULL;
     if (misaligned(dscores, 4) || misaligned(argmax, 4) || misaligned(dQ) || misaligned(ddocs)) return COLBANDIT_ERR_ALIGNMENT;
     return hip(launch_maxsim_backward(dscores, argmax, Q, n_queries, T, d, dt, docs, offsets, N, total_tokens, dQ, ddocs,

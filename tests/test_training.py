@@ -1055,3 +1055,22 @@ def test_tokens_behind_the_last_document_get_zeros(tr, dev, dtype, nq, T, length
     torch.full_like(padded, 7.0)
     got = tr.colbandit_maxsim_backward(dscores, f["argmax"], Q, padded, off)
     assert torch.equal(got["dQ"], want["dQ"]) and torch.equal(got["ddocs"][:len(D)], want["ddocs"]) and not got["ddocs"][len(D):].any()
+
+
+def test_what_no_launch_can_hold_is_refused(tr):
+    """Launches of 2^32 threads and more are refused as what they are before anything is enqueued (the device would refuse them one
+    by one, the second after the first has run)."""
+    L = tr.lib()
+    def both(**kw):
+        a = _attn_struct(tr, **kw)
+        return (L.colbandit_attention(a, 0x10000, 0x20000, 0x100000, 1 << 45, None),
+                L.colbandit_attention_backward(a, 0x10000, 0x20000, 0x30000, 0x40000, 0x50000, 0x60000, None, 0x100000, 1 << 45, None))
+
+    assert both(n_seqs=6_000_000, total_q=6_000_000, total_k=6_000_000, heads=12, kv_heads=12) == (-4, -4)
+    assert both(n_seqs=1, total_q=(1 << 31) - (1 << 17), total_k=64, heads=64, kv_heads=64) == (-4, -4)
+    assert both(n_seqs=1, total_q=10, total_k=12, heads=8192, kv_heads=8192, q_row=64, k_row=64, v_row=64, d=32) == (-4, -4)
+
+    def grads(nq=2, T=8, N=3, total=20):
+        return L.colbandit_maxsim_backward(0x4000, 0x5000, 0x1000, nq, T, 64, 1, 0x2000, 0x3000, N, total, 0x6000, 0x7000, None)
+
+    assert grads(N=1 << 24) == -4 and grads(total=1 << 30, N=3) == -4 and grads(nq=65535, T=128, N=9_000_000) == -4
