@@ -327,6 +327,10 @@ def contrastive_maxsim(Q, docs, offsets, targets, temperature=1.0):
 
 
 def clip_gradients_(parameters, max_norm):
-    """Clips the parameters' gradients in place to a global norm of max_norm; returns the norm before."""
+    """Clips the parameters' gradients in place to a global norm of max_norm; returns the norm before (0 where no parameter
+    has a gradient)."""
+    parameters = list(parameters)
     grads = [p.grad for p in parameters if p.grad is not None]
+    if not grads:
+        return torch.zeros((), device=parameters[0].device if parameters else None)
     return colbandit_clip_gradients(grads, float(max_norm))["norm"]

@@ -1074,3 +1074,7 @@ def test_what_no_launch_can_hold_is_refused(tr):
         return L.colbandit_maxsim_backward(0x4000, 0x5000, 0x1000, nq, T, 64, 1, 0x2000, 0x3000, N, total, 0x6000, 0x7000, None)
 
     assert grads(N=1 << 24) == -4 and grads(total=1 << 30, N=3) == -4 and grads(nq=65535, T=128, N=9_000_000) == -4
+
+
+def test_clipping_where_nothing_has_a_gradient(tr):
+    assert float(tr.clip_gradients_([], 1.0)) == 0 and float(tr.clip_gradients_(iter([torch.nn.Parameter(torch.ones(3))]), 1.0)) == 0
