@@ -158,7 +158,8 @@ int colbandit_maxsim_backward(const float *dscores, const int32_t *argmax, const
  * input times min(1, max_norm / (norm + 1e-6)), rounded once.
  *   n_tensors  >= 1
  *   grads, out HOST arrays of DEVICE pointers (out[i] may be grads[i]: clipped in place, and
- *              not written where nothing has to change); each aligned to its type
+ *              not written where nothing has to change); each aligned to its type; no other two
+ *              of all these tensors overlap
  *   sizes      HOST [n_tensors]: values of each tensor, >= 0
  *   dts        HOST [n_tensors]: colbandit_dtype of each tensor and its output
  *   max_norm   > 0, may be +inf

@@ -329,7 +329,7 @@ def contrastive_maxsim(Q, docs, offsets, targets, temperature=1.0):
 def clip_gradients_(parameters, max_norm):
     """Clips the parameters' gradients in place to a global norm of max_norm; returns the norm before (0 where no parameter
     has a gradient)."""
-    parameters = list(parameters)
+    parameters = list(dict.fromkeys(parameters))     # one that is listed twice has one gradient
     grads = [p.grad for p in parameters if p.grad is not None]
     if not grads:
         return torch.zeros((), device=parameters[0].device if parameters else None)

@@ -1078,3 +1078,11 @@ def test_what_no_launch_can_hold_is_refused(tr):
 
 def test_clipping_where_nothing_has_a_gradient(tr):
     assert float(tr.clip_gradients_([], 1.0)) == 0 and float(tr.clip_gradients_(iter([torch.nn.Parameter(torch.ones(3))]), 1.0)) == 0
+
+
+def test_a_parameter_that_is_listed_twice_is_clipped_once(tr, monkeypatch):
+    """Two entries of one tensor would be scaled in place by two workgroups at once."""
+    monkeypatch.setattr(tr, "colbandit_clip_gradients", lambda grads, most: {"norm": len(grads)})
+    p, q = (torch.nn.Parameter(torch.ones(3)) for _ in range(2))
+    p.grad, q.grad = torch.ones(3), torch.ones(3)
+    assert tr.clip_gradients_([p, q, p], 1.0) == 2
