@@ -91,6 +91,7 @@ def train(steps=60, n_docs=256, batch=32, temperature=1.0, max_norm=1.0, rate=2.
     before = accuracy(encoder, tokens, offsets, queries)
     losses, norms = [], []
     parameters = list(encoder.parameters())
+    batch = min(batch, n_docs)
     targets = torch.arange(batch, device=device)
     for step in range(steps):
         ids = torch.randperm(n_docs, generator=g)[:batch].to(device)

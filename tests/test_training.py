@@ -1086,3 +1086,10 @@ def test_a_parameter_that_is_listed_twice_is_clipped_once(tr, monkeypatch):
     p, q = (torch.nn.Parameter(torch.ones(3)) for _ in range(2))
     p.grad, q.grad = torch.ones(3), torch.ones(3)
     assert tr.clip_gradients_([p, q, p], 1.0) == 2
+
+
+@gpu
+def test_fine_tuning_on_fewer_documents_than_a_batch(tr, dev):
+    from paper_2602_02827_amd import finetune
+    r = finetune.train(steps=2, n_docs=5)
+    assert all(math.isfinite(x) for x in r["losses"] + r["norms"])
