@@ -1093,3 +1093,195 @@ def test_fine_tuning_on_fewer_documents_than_a_batch(tr, dev):
     from paper_2602_02827_amd import finetune
     r = finetune.train(steps=2, n_docs=5)
     assert all(math.isfinite(x) for x in r["losses"] + r["norms"])
+
+
+# ---- forms that large calls take -------------------------------------------------------------------------
+
+def heads_in_a_row(ql, kl, heads, kv_heads, bias):
+    """Whether the plan's workgroups go on to a second head: units (key heads) in pairs leave 1,536 workgroups or more, of short
+    sequences and four wavefronts; for the queries' tiles and for the keys'."""
+    n, group = len(ql), heads // kv_heads
+    pack = 1 if bias or group > 16 else group
+    units, q_slots, k_slots = heads // pack, sum(ql) // (128 // pack) + n, sum(kl) // 128 + n
+    many = (sum(ql) * pack // 32 + n) * units > 1024 and (sum(kl) // 32 + n) * kv_heads > 1024
+    short = sum(kl) // n <= 384 and sum(ql) * group // n <= 384
+    return many and short and units > 1 and q_slots * (units // 2) >= 1536, many and short and kv_heads > 1 and k_slots * (kv_heads // 2) >= 1536
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [32, 64])
+@pytest.mark.parametrize("bias,keep,causal", [(None, False, False), (32, True, False), (8, False, True)])
+def test_two_heads_a_workgroup_of_many_sequences(tr, dev, dtype, d, bias, keep, causal):
+    """Three heads: the last workgroup of a tile has one."""
+    lengths = np.random.default_rng(30).integers(0, 10, 1600).tolist()
+    assert heads_in_a_row(lengths, lengths, 3, 3, bias) == (True, True)
+    p = problem(dev, dtype, lengths, lengths, 3, 3, d, seed=30, bias=bias, keep=keep)
+    check_attention(tr, p, lengths, lengths, dtype, causal)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,d,bias,keep,causal", [("bf16", 64, 32, True, False), ("bf16", 32, None, True, True), ("f32", 32, 32, False, True)])
+def test_two_heads_a_workgroup_of_several_tiles(tr, dev, dtype, d, bias, keep, causal):
+    lengths = [1 + i * 179 // 127 for i in range(128)]
+    assert heads_in_a_row(lengths, lengths, 25, 25, bias) == (True, True)
+    p = problem(dev, dtype, lengths, lengths, 25, 25, d, seed=31, bias=bias, keep=keep)
+    check_attention(tr, p, lengths, lengths, dtype, causal)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bias,keep,causal", [(None, True, True), (None, False, False), (32, True, False)])
+def test_two_heads_a_workgroup_that_share_keys(tr, dev, dtype, bias, keep, causal):
+    g = np.random.default_rng(32)
+    kl = g.integers(0, 21, 800).tolist()
+    ql = [int(x) for x in np.minimum(g.integers(0, 30, 800), 25)]
+    assert heads_in_a_row(ql, kl, 10, 5, bias) == (True, True)
+    p = problem(dev, dtype, ql, kl, 10, 5, 64, seed=32, bias=bias, keep=keep)
+    check_attention(tr, p, ql, kl, dtype, causal)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 96, 128])
+@pytest.mark.parametrize("n_buckets,causal", [(64, False), (128, False), (31, True)])
+def test_tables_that_reach_beyond_128(tr, dev, dtype, d, n_buckets, causal):
+    """Their histograms leave a workgroup one head, where there are many sequences too."""
+    lengths = [9, 0, 4] * 60 + [600]
+    p = problem(dev, dtype, lengths, lengths, 3, 3, d, seed=33, bias=n_buckets, keep=True)
+    starts = tr.colbandit_bias_buckets(n_buckets, 256, causal)
+    assert starts[-1] > 128
+    check_attention(tr, p, lengths, lengths, dtype, causal, max_distance=256)
+
+
+@gpu
+def test_tables_that_reach_beyond_128_over_many_sequences(tr, dev):
+    lengths = [9, 0, 4] * 533 + [500]
+    assert heads_in_a_row(lengths, lengths, 3, 3, 128) == (True, True)
+    p = problem(dev, "bf16", lengths, lengths, 3, 3, 64, seed=34, bias=128)
+    check_attention(tr, p, lengths, lengths, "bf16", max_distance=256)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [32, 64, 96, 128])
+@pytest.mark.parametrize("nq,T", [(24, 32), (11, 24), (3, 128)])
+def test_maxsim_of_many_documents(tr, dev, dtype, d, nq, T):
+    """Two columns a lane: groups of queries times documents are 1,024 or more."""
+    lengths = np.random.default_rng(35).integers(0, 80, 700).tolist()
+    assert -(-nq // (256 // T)) * len(lengths) >= 1024
+    Q, D, off = embeddings(dev, dtype, nq, T, lengths, d, seed=35)
+    f = tr.colbandit_maxsim_scores(Q, D, off)
+    scores, arg = maxsim_reference(Q, D, off)
+    np.testing.assert_array_equal(f["argmax"].cpu().numpy(), arg)
+    np.testing.assert_array_equal(f["scores"].double().cpu().numpy(), scores)
+    g = torch.randn(nq, len(lengths), generator=torch.Generator().manual_seed(2)).to(dev)
+    b = tr.colbandit_maxsim_backward(g, f["argmax"], Q, D, off)
+    dQ, dQ_abs, dD, dD_abs = gradient_reference(g, arg, Q, D, off)
+    within(b["dQ"], dQ, U[dtype] * dQ.abs() + F * dQ_abs, "dQ")
+    within(b["ddocs"], dD, U[dtype] * dD.abs() + F * dD_abs, "ddocs")
+
+
+@gpu
+@pytest.mark.parametrize("d", [32, 64, 96, 128])
+@pytest.mark.parametrize("nq,T,n", [(5, 24, 40), (24, 32, 400)])
+@pytest.mark.parametrize("spread", [0, 3])
+def test_maxsim_scores_of_full_width_numbers(tr, dev, d, nq, T, n, spread):
+    """fp32 values of 24 significant bits, of sizes up to 10^spread apart.  A product's pieces that are left out are 2^-22 of it; six
+    products of pieces for sixteen elements are added one after the other, each sum off by at most 2^-23 of the absolute terms.  The
+    chosen token is one whose cell is within both cells' bounds of the best."""
+    g = torch.Generator().manual_seed(36 + d)
+    lengths = np.random.default_rng(36).integers(1, 60, n).tolist()
+    size = 10.0 ** (torch.rand(d, generator=g) * spread)
+    Q = (torch.randn(nq, T, d, generator=g) * size / d ** 0.5).to(dev)
+    D = (torch.randn(sum(lengths), d, generator=g) / size).to(dev)
+    off = offsets(lengths).to(dev)
+    f = tr.colbandit_maxsim_scores(Q, D, off)
+    q, x, arg = Q.double().cpu().reshape(nq * T, d), D.double().cpu(), f["argmax"].cpu().long()
+    rate = 2.0 ** -22 + 6 * d / 16 * 2.0 ** -23
+    o = off.tolist()
+    for i in range(n):
+        S, A = q @ x[o[i]:o[i + 1]].T, rate * (q.abs() @ x[o[i]:o[i + 1]].abs().T)
+        at = arg[:, i].reshape(-1, 1)
+        best = S.max(1, keepdim=True)
+        assert bool((S.gather(1, at) >= best.values - A.gather(1, at) - A.gather(1, best.indices)).all())
+        want, tol = best.values.view(nq, T).sum(1), A.max(1).values.view(nq, T).sum(1)
+        tol = tol + T * 2.0 ** -24 * best.values.abs().view(nq, T).sum(1)
+        assert bool(((f["scores"][:, i].double().cpu() - want).abs() <= tol).all()), i
+
+
+# ---- refusals of the binding on tensors that are on the device -----------------------------------------------
+
+def refused(call, base, bad):
+    """The call takes `base`, and refuses each change of it by its own error and words."""
+    call(**base)
+    for change, error, words in bad:
+        with pytest.raises(error, match=words):
+            call(**dict(base, **change))
+            pytest.fail(str(change))
+
+
+@gpu
+def test_attention_refusals_on_the_device(tr, dev):
+    q, off = torch.zeros(10, 2, 64, device=dev), torch.tensor([0, 10], device=dev)
+    cpu = q.cpu()
+    base = dict(q=q, k=q, v=q, q_offsets=off, k_offsets=None, keep=torch.ones(10, dtype=torch.bool, device=dev),
+                bias=torch.zeros(32, 2, device=dev), max_distance=128, scale=None)
+    E = tr.ColbanditError
+    bad = [
+        (dict(q=q.half()), TypeError, "float32 or bfloat16"), (dict(k=q.bfloat16()), TypeError, "one type"),
+        (dict(v=q.double()), TypeError, "one type"), (dict(q=q[0]), ValueError, "total_q, heads, d"),
+        (dict(v=q[:, :1]), ValueError, "total_k, kv_heads, d"), (dict(k=q[:, :, :32], v=q[:, :, :32]), ValueError, "total_k, kv_heads, d"),
+        (dict(q=torch.zeros(10, 64, 2, device=dev).transpose(1, 2)), ValueError, "consecutive"),
+        (dict(q_offsets=off.int()), ValueError, "offsets"), (dict(q_offsets=off[:1]), ValueError, "offsets"),
+        (dict(q_offsets=torch.tensor([0, 1, 10, 1], device=dev)[::2]), ValueError, "offsets"),
+        (dict(k_offsets=torch.tensor([0, 5, 10], device=dev)), ValueError, "equally many"),
+        (dict(keep=torch.ones(9, dtype=torch.bool, device=dev)), ValueError, "keep"), (dict(keep=torch.ones(10, device=dev)), ValueError, "keep"),
+        (dict(bias=torch.zeros(32, 3, device=dev)), ValueError, "n_buckets, heads"),
+        (dict(bias=torch.zeros(2, 32, device=dev).t()), ValueError, "n_buckets, heads"),
+        (dict(bias=torch.zeros(32, 2, device=dev).bfloat16()), TypeError, "type of q"),
+        (dict(q=cpu), ValueError, "current device"), (dict(k=cpu), ValueError, "current device"), (dict(v=cpu), ValueError, "current device"),
+        (dict(q_offsets=off.cpu()), ValueError, "current device"), (dict(k_offsets=off.cpu()), ValueError, "current device"),
+        (dict(keep=torch.ones(10, dtype=torch.bool)), ValueError, "current device"), (dict(bias=torch.zeros(32, 2)), ValueError, "current device"),
+        (dict(scale=math.nan), E, "knob"), (dict(bias=torch.zeros(31, 2, device=dev)), E, "invalid size"), (dict(max_distance=300), E, "kernels cover"),
+    ]
+    refused(tr.colbandit_attention, base, bad)
+    f = tr.colbandit_attention(q, q, q, off)
+    back = dict(base, dout=torch.zeros_like(q), out=f["out"], lse=f["lse"])
+    more = [(dict(dout=q[:9]), ValueError, "dout"), (dict(out=q.bfloat16()), ValueError, "out"), (dict(lse=f["lse"].t().contiguous()), ValueError, "lse"),
+            (dict(dout=cpu), ValueError, "current device"), (dict(out=cpu), ValueError, "current device"), (dict(lse=f["lse"].cpu()), ValueError, "current device")]
+    refused(tr.colbandit_attention_backward, back, bad + more)
+    for out, words in ((dict(out=q.clone(), lse=f["lse"].cpu()), "current device"), (dict(out=cpu, lse=f["lse"]), "current device"),
+                       (dict(out=q[:9].clone(), lse=f["lse"]), "out"), (dict(out=q.clone(), lse=f["lse"].double()), "lse")):
+        with pytest.raises(ValueError, match=words):
+            tr.colbandit_attention(q, q, q, off, out=out)
+
+
+@gpu
+def test_loss_and_clip_refusals_on_the_device(tr, dev):
+    Q, D, off = embeddings(dev, "f32", 3, 7, [5, 6], 64)
+    base = dict(Q=Q, docs=D, offsets=off)
+    bad = [(dict(Q=Q.half()), TypeError, "float32 or bfloat16"), (dict(docs=D.bfloat16()), TypeError, "one type"),
+           (dict(Q=Q[0]), ValueError, "n_queries"), (dict(docs=D[:, :32]), ValueError, "n_queries"), (dict(Q=Q[:, ::2]), ValueError, "contiguous"),
+           (dict(docs=D[::2]), ValueError, "contiguous"), (dict(offsets=off.int()), ValueError, "offsets"), (dict(offsets=off[:1]), ValueError, "offsets"),
+           (dict(Q=Q.cpu()), ValueError, "current device"), (dict(docs=D.cpu()), ValueError, "current device"),
+           (dict(offsets=off.cpu()), ValueError, "current device"),
+           (dict(Q=Q[:, :, :48].contiguous(), docs=D[:, :48].contiguous()), tr.ColbanditError, "kernels cover")]
+    refused(tr.colbandit_maxsim_scores, base, bad)
+    f = tr.colbandit_maxsim_scores(Q, D, off)
+    g = torch.zeros_like(f["scores"])
+    more = [(dict(dscores=g[:2]), ValueError, "dscores"), (dict(dscores=g.double()), ValueError, "dscores"), (dict(argmax=f["argmax"].long()), ValueError, "argmax"),
+            (dict(dscores=g.cpu()), ValueError, "current device"), (dict(argmax=f["argmax"].cpu()), ValueError, "current device")]
+    refused(tr.colbandit_maxsim_backward, dict(base, dscores=g, argmax=f["argmax"]), bad + more)
+    t = torch.tensor([0, 1, 0], device=dev)
+    refused(tr.colbandit_contrastive_loss, dict(scores=g, targets=t, temperature=1.0), [
+        (dict(scores=g.double()), ValueError, "scores"), (dict(scores=g.t()), ValueError, "scores"), (dict(targets=t.int()), ValueError, "targets"),
+        (dict(targets=t[:2]), ValueError, "targets"), (dict(scores=g.cpu()), ValueError, "current device"),
+        (dict(targets=t.cpu()), ValueError, "current device"), (dict(temperature=0.0), tr.ColbanditError, "knob")])
+    x = [torch.ones(5, device=dev), torch.ones(3, device=dev).bfloat16()]
+    to = [torch.empty_like(a) for a in x]
+    refused(tr.colbandit_clip_gradients, dict(grads=x, max_norm=1.0, out=to), [
+        (dict(grads=[]), ValueError, "list of tensors"), (dict(out=to[:1]), ValueError, "as many"), (dict(grads=[x[0].half(), x[1]]), TypeError, "float32 or bfloat16"),
+        (dict(out=[to[1], to[0]]), TypeError, "of their types"), (dict(out=[to[0][:4], to[1]]), ValueError, "of their shapes"),
+        (dict(grads=[torch.ones(10, device=dev)[::2], x[1]]), ValueError, "contiguous"), (dict(grads=[x[0].cpu(), x[1]]), ValueError, "current device"),
+        (dict(out=[to[0].cpu(), to[1]]), ValueError, "current device"), (dict(max_norm=0.0), tr.ColbanditError, "knob")])
