@@ -53,7 +53,7 @@ extern "C" {
  * scores are all that far from zero (a table may hide distances by any finite value, down to the
  * type's lowest) have outputs and gradients like any other; lse has a 32-bit value's rounding.
  * Products are summed in 32 bits.  fp32 values are multiplied as three bf16 pieces each, whose
- * sum is the value; the three smallest of the nine products of pieces, 2^-23 of a product
+ * sum is the value; the three smallest of the nine products of pieces, 2^-22 of a product
  * together, are left out.  fp32 values that are seen must be finite.
  * Rows of q, k and v lie q_row elements apart and heads q_head apart (likewise k, v); the d
  * values of a row and head are consecutive.  Pointers and strides are whole multiples of 16
@@ -133,7 +133,8 @@ int colbandit_maxsim_scores(const void *Q, int n_queries, int T, int d, colbandi
  * loss[q] = log sum_i exp(scores[q][i] / temperature) - scores[q][targets[q]] / temperature
  * dscores[q][i] = d(mean of loss) / d(scores[q][i])
  * A target outside 0 .. N-1 takes its query out of the mean: loss 0, dscores 0.  Scores of
- * -inf have no weight.
+ * -inf have no weight; a target's makes a loss of +inf, and if all are -inf the loss and its
+ * gradient are NaN, as the formula has it.
  *   targets  DEVICE int64 [n_queries];  loss DEVICE float [n_queries]
  *   dscores  DEVICE float [n_queries][N]
  */
@@ -155,7 +156,8 @@ int colbandit_maxsim_backward(const float *dscores, const int32_t *argmax, const
 
 /*
  * norm = sqrt of the sum of the squares of all values of all tensors; every output is its
- * input times min(1, max_norm / (norm + 1e-6)), rounded once.
+ * input times min(1, max_norm / (norm + 1e-6)): the factor is rounded to 32 bits, the product
+ * as well, and to 16 bits after that where the tensor has them.
  *   n_tensors  >= 1
  *   grads, out HOST arrays of DEVICE pointers (out[i] may be grads[i]: clipped in place, and
  *              not written where nothing has to change); each aligned to its type; no other two

@@ -225,10 +225,8 @@ template <class E, int D, int NW> constexpr int kQueryWaves = NW > 1 && sizeof(E
 // Key rows of the forward pass's tiles: of wide heads 32, so that LDS holds three workgroups (48 pages of 1,030 rows, d = 128: 608
 // us, with 64 rows and two 640; the gradients' kernels, which have registers for two, lose by it).
 template <class E, int D> constexpr int kForwardRows = D >= 96 ? 32 : Oper<E>::ROWS;
-// Wide heads take all registers: their workgroups do not go on to the next one, and their gradients in 32 bits are not made by
-// single wavefronts, which would hold a whole tile on its way in registers as well.
-template <int D> constexpr bool kRuns = D <= 64;
-template <class E, int D> constexpr bool kSingle = sizeof(E) == 2 || D <= 64;
+template <int D> constexpr bool kRuns = goes_on_to_next_head(D);
+template <class E, int D> constexpr bool kSingle = single_wavefronts_make_gradients(sizeof(E) == 2 ? TR_BF16 : TR_F32, D);
 
 // ---- forward -------------------------------------------------------------------------------------------------
 // One pass over the keys with the running maximum and sum of the softmax, in 32 bits; probabilities are rounded to the

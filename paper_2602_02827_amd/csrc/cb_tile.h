@@ -9,7 +9,7 @@
 // .. +3 and 16c + 8 + 4h .. +3 (turned operand).  So probabilities never leave the registers they were computed in.
 //   bf16   one v_mfma_f32_32x32x16_bf16 a step; turned operands by two transposing LDS reads of four rows each
 //   fp32   the same instruction, whose rate is sixteen times that of the 32-bit ones, on three bf16 pieces of eight bits of every
-//          value: six products of pieces a step, the three smallest (2^-23 of a product together) left out
+//          value: six products of pieces a step, the three smallest (2^-22 of a product together) left out
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>

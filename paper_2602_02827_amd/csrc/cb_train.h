@@ -24,6 +24,10 @@ struct AttnArgs {
     int16_t starts[128];         // first distance of each bucket of one direction
 };
 
+// Wide heads take all registers: their workgroups do not go on to the next one, and their gradients in 32 bits are not made by
+// single wavefronts, which would hold a whole tile on its way in registers as well.  (For the plan and for the kernels.)
+constexpr bool goes_on_to_next_head(int d) { return d <= 64; }
+constexpr bool single_wavefronts_make_gradients(int dt, int d) { return dt == TR_BF16 || d <= 64; }
 constexpr int kMostRun = 2;      // heads that a workgroup takes one after the other (four: the histograms leave half the workgroups no LDS)
 
 enum { AS_THEY_COME, BY_XCD, LONGEST_FIRST };         // order of workgroups

@@ -21,7 +21,7 @@ AttnPlan plan_attention(const AttnArgs& A, int d, int dt, bool backward) {
     // holds about one a SIMD).  One query of 32 tokens, 12 heads: 16.7 us, with four wavefronts 17.7; 128 fp32 sequences of 32, 6
     // heads, with gradients 39.5 and 40.6; but 512 sequences of 8 to 32, 12 heads, with gradients 233 and 219.
     const int64_t q_cols = (int64_t)A.total_q * A.pack / A.n_seqs, k_rows = A.total_k / A.n_seqs;
-    const bool single = !backward || dt == TR_BF16 || d <= 64;       // (kSingle)
+    const bool single = !backward || single_wavefronts_make_gradients(dt, d);
     auto waves_of = [&](int64_t cols, int64_t groups) { return cols <= 32 && groups <= 1024 && single ? 1 : 4; };
     P.q_waves = waves_of(q_cols, ((int64_t)A.total_q * A.pack / 32 + A.n_seqs) * P.units);
     P.k_waves = waves_of(k_rows, (A.total_k / 32 + A.n_seqs) * A.kv_heads);
@@ -33,15 +33,15 @@ AttnPlan plan_attention(const AttnArgs& A, int d, int dt, bool backward) {
     P.q_order = order_of(P.q_slots, k_rows);
     P.k_order = order_of(P.k_slots, (int64_t)A.total_q * A.group / A.n_seqs);
     P.splits = 1;
-    // Short sequences: a workgroup goes on to the next heads, as long as enough workgroups are left (six a CU; wide heads: kRuns).
+    // Short sequences: a workgroup goes on to the next heads, as long as enough workgroups are left (six a CU).
     // 512 passages, forward and backward: 701 us, one head each 724.
     auto run_of = [](int64_t slots, int units, int64_t rows) {
         int r = 1;
         while (rows <= kShortRows && 2 * r <= kMostRun && 2 * r <= units && slots * (units / (2 * r)) >= 1536) r *= 2;
         return r;
     };
-    P.run = d <= 64 ? run_of(P.q_slots, P.units, k_rows) : 1;
-    P.kv_run = d <= 64 ? run_of(P.k_slots, A.kv_heads, (int64_t)A.total_q * A.group / A.n_seqs) : 1;
+    P.run = goes_on_to_next_head(d) ? run_of(P.q_slots, P.units, k_rows) : 1;
+    P.kv_run = goes_on_to_next_head(d) ? run_of(P.k_slots, A.kv_heads, (int64_t)A.total_q * A.group / A.n_seqs) : 1;
     if (A.bias && A.reach > 128) P.run = 1;          // (histograms of all its heads are in LDS)
     const int64_t groups = P.q_slots * P.units;
     ++P.q_slots;                                     // the rows behind the last sequence may end in a tile of their own
