@@ -100,6 +100,7 @@ constexpr float kLostLog = 134217728.f;
 // Natural logarithm of a sum l of exponentials from the maximum m on, a score's unit being `unit`.
 __device__ __forceinline__ float log_of_sum(float m, float l, float k, float unit) {
     if (l == 0.f) return -INFINITY;
+    if (l != l) return l;                            // the row saw a NaN
     const float a = m * k, b = rounded_product(m, unit);
     return fabsf(a) <= kFar ? fmaf(a, LN2, logf(l)) : fabsf(b) < kLostLog ? b + logf(l) : b;
 }

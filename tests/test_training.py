@@ -1285,3 +1285,33 @@ def test_loss_and_clip_refusals_on_the_device(tr, dev):
         (dict(out=[to[1], to[0]]), TypeError, "of their types"), (dict(out=[to[0][:4], to[1]]), ValueError, "of their shapes"),
         (dict(grads=[torch.ones(10, device=dev)[::2], x[1]]), ValueError, "contiguous"), (dict(grads=[x[0].cpu(), x[1]]), ValueError, "current device"),
         (dict(out=[to[0].cpu(), to[1]]), ValueError, "current device"), (dict(max_norm=0.0), tr.ColbanditError, "knob")])
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("ql,kl", [([40, 200], [40, 200]), ([1, 1], [700, 3000])])
+@pytest.mark.parametrize("bias", [None, 8])
+def test_a_nan_that_is_seen_is_in_every_result(tr, dev, dtype, ql, kl, bias):
+    """A key of the second sequence is NaN: so are all results of its rows, and the first sequence's are as they were."""
+    p = problem(dev, dtype, ql, kl, 2, 2, 64, seed=40, bias=bias)
+    f, b = attend(tr, p, ql, kl)
+    p["k"] = p["k"].clone()
+    p["k"][kl[0] + 2] = math.nan
+    g, c = attend(tr, p, ql, kl)
+    for x, y, rows in ((f["out"], g["out"], ql[0]), (f["lse"].t(), g["lse"].t(), ql[0]), (b["dq"], c["dq"], ql[0]), (b["dk"], c["dk"], kl[0]), (b["dv"], c["dv"], kl[0])):
+        assert torch.equal(x[:rows], y[:rows]) and bool(torch.isnan(y[rows:]).all())
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("ql,kl", [([40, 200], [40, 200]), ([1, 1], [700, 3000])])
+@pytest.mark.parametrize("bias", [None, 8])
+def test_a_query_that_is_nan_is_in_every_result(tr, dev, dtype, ql, kl, bias):
+    """The last row of the second sequence: all its scores are NaN, so it is no row that sees nothing."""
+    p = problem(dev, dtype, ql, kl, 2, 2, 64, seed=41, bias=bias)
+    p["q"][-1] = math.nan
+    f, b = attend(tr, p, ql, kl)
+    for x in (f["out"][-1], f["lse"][:, -1], b["dq"][-1], b["dk"][kl[0]:], b["dv"][kl[0]:]):
+        assert bool(torch.isnan(x).all())
+    for x in (f["out"][:-1], f["lse"][:, :-1], b["dq"][:-1], b["dk"][:kl[0]], b["dv"][:kl[0]]):
+        assert bool(torch.isfinite(x).all())
