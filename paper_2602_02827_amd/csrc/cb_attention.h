@@ -217,17 +217,15 @@ __device__ __forceinline__ float hidden_unless(float x, uint32_t all) {
 }
 
 // Wavefronts per SIMD that the registers are shared out for: forward pass, gradients of queries, of keys and values (one more each
-// makes the compiler spill, and is slower; 512 passages: forward pass with three and four 152 and 176 us, forward and backward with
-// two and three for the queries 705 and 642, with three for the keys 706 where it was 642).  Of workgroups of one wavefront LDS
-// holds about one a SIMD.
-template <class E, int D, int NW> constexpr int kWaves = NW == 1 ? 1 : sizeof(E) == 2 || D <= 32 ? 3 : D <= 96 ? 2 : 1;
-template <class E, int D, int NW> constexpr int kGradientWaves = NW > 1 && (sizeof(E) == 2 || D <= 32) ? 2 : 1;
-template <class E, int D, int NW> constexpr int kQueryWaves = NW > 1 && sizeof(E) == 2 && D <= 64 ? 3 : kGradientWaves<E, D, NW>;
+// makes the compiler spill, and is slower; 512 passages: forward pass with three and four 150 and 227 us, forward and backward with
+// two and three for the queries 765 and 691, with two and three for the keys 691 and 850).
+template <class E, int D> constexpr int kWaves = sizeof(E) == 2 || D <= 32 ? 3 : D <= 96 ? 2 : 1;
+template <class E, int D> constexpr int kGradientWaves = sizeof(E) == 2 || D <= 32 ? 2 : 1;
+template <class E, int D> constexpr int kQueryWaves = sizeof(E) == 2 && D <= 64 ? 3 : kGradientWaves<E, D>;
 // Key rows of the forward pass's tiles: of wide heads 32, so that LDS holds three workgroups (48 pages of 1,030 rows, d = 128: 608
 // us, with 64 rows and two 640; the gradients' kernels, which have registers for two, lose by it).
 template <class E, int D> constexpr int kForwardRows = D >= 96 ? 32 : Oper<E>::ROWS;
 template <int D> constexpr bool kRuns = goes_on_to_next_head(D);
-template <class E, int D> constexpr bool kSingle = single_wavefronts_make_gradients(sizeof(E) == 2 ? TR_BF16 : TR_F32, D);
 
 // ---- forward -------------------------------------------------------------------------------------------------
 // One pass over the keys with the running maximum and sum of the softmax, in 32 bits; probabilities are rounded to the
@@ -241,13 +239,13 @@ constexpr float kLag = 8.f;
 // score: as many clocks as the products): the pages above 564 us, 740 TFLOP/s where a large product reaches 1,189.  Short ones by
 // latency and what a workgroup does before its first product: 512 passages, 12 heads of 64 with bias and mask, 145 us.  Single
 // tokens by memory: 16 over 1 to 16,385 keys, two key heads of 128, 134 MB in 30 us and 7.5 us to join their parts.
-template <class E, int D, int NW, bool BIAS, bool MASKED>
-__global__ __launch_bounds__(64 * NW, (kWaves<E, D, NW>)) void k_attention(const AttnArgs A, int slots, int order, int units, int run,
+template <class E, int D, bool BIAS, bool MASKED>
+__global__ __launch_bounds__(64 * kWavefronts, (kWaves<E, D>)) void k_attention(const AttnArgs A, int slots, int order, int units, int run,
                                                                            int splits, E* out, float* lse, float* o_part,
                                                                            float2* ml_part) {
     using O = Oper<E>;
     using T = Tile<E, D, kForwardRows<E, D>>;
-    constexpr int NB = T::ROWS / 32, DB = D / 32, THREADS = 64 * NW;
+    constexpr int NB = T::ROWS / 32, DB = D / 32, THREADS = 64 * kWavefronts;
     __shared__ __align__(256) char lds[2][2 * T::BYTES];
     __shared__ __align__(16) float hidden[2][T::ROWS];           // 0, or minus infinity for rows that no column sees
     extern __shared__ __align__(16) char dyn[];
@@ -256,7 +254,7 @@ __global__ __launch_bounds__(64 * NW, (kWaves<E, D, NW>)) void k_attention(const
     const int split = work.inner % splits, slot = work.slot;
     int unit = work.inner / splits * run;
     const int end_unit = unit + run < units ? unit + run : units;
-    const int G = A.pack, per = 32 * NW / G;
+    const int G = A.pack, per = 32 * kWavefronts / G;
     const QueryTile t(A, slot, per, lane);
     if (t.none) return;
     const QueryColumns w(A, t, G, per, wave, lane);
@@ -537,25 +535,25 @@ __device__ __forceinline__ void add_diagonals(const f32x16& x, float* hist, int 
 }
 
 // Gradients of queries, delta, and the bias table's share of each tile; head units one after the other, as the forward pass.
-template <class E, int D, int NW, bool BIAS, bool MASKED>
-__global__ __launch_bounds__(64 * NW, (kQueryWaves<E, D, NW>)) void
+template <class E, int D, bool BIAS, bool MASKED>
+__global__ __launch_bounds__(64 * kWavefronts, (kQueryWaves<E, D>)) void
 k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const E* out, const E* dout, const float* lse, E* dq,
                float* delta, float* bias_part) {
     using O = Oper<E>;
     using T = Tile<E, D>;
-    constexpr int NB = T::ROWS / 32, DB = D / 32, THREADS = 64 * NW;
+    constexpr int NB = T::ROWS / 32, DB = D / 32, THREADS = 64 * kWavefronts;
     __shared__ __align__(256) char lds[2][2 * T::BYTES];
     __shared__ __align__(16) float hidden[2][T::ROWS];
-    __shared__ float far_sum[kMostRun][NW][2];
+    __shared__ float far_sum[kMostRun][kWavefronts][2];
     __shared__ float far_lse[THREADS];                // own log-sum-exp, for far tiles
-    __shared__ int any_row_far[2][NW];                // of a wavefront's rows, for this head unit and the next
+    __shared__ int any_row_far[2][kWavefronts];                // of a wavefront's rows, for this head unit and the next
     extern __shared__ __align__(16) char dyn[];       // the bias by distance, then histograms of each head and wavefront
     const int tid = threadIdx.x, lane0 = tid & 63, lane = lane0, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     const Work work = work_of(blockIdx.x, slots, (units + run - 1) / run, A.n_seqs, order, true);
     const int slot = work.slot, first_unit = work.inner * run;
     int unit = first_unit;
     const int end_unit = unit + run < units ? unit + run : units;
-    const int G = A.pack, per = 32 * NW / G;
+    const int G = A.pack, per = 32 * kWavefronts / G;
     const QueryTile t(A, slot, per, lane);
     if (t.none) {
         if constexpr (BIAS)
@@ -627,7 +625,7 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
     float* hist = table + width;
     float* own_hist = hist + wave * width + middle;
     if constexpr (BIAS) {
-        for (int i = tid; i < (end_unit - unit) * NW * width; i += THREADS) hist[i] = 0.f;
+        for (int i = tid; i < (end_unit - unit) * kWavefronts * width; i += THREADS) hist[i] = 0.f;
         load_starts(A, starts, tid, THREADS);
         __syncthreads();
         fill_bias<E>(A, unit, starts, table, tid, THREADS);
@@ -644,7 +642,7 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
         if (i == 0) {                                            // a head unit begins
             int is = 0;
 #pragma unroll
-            for (int v = 0; v < NW; ++v) is |= any_row_far[unit & 1][v];
+            for (int v = 0; v < kWavefronts; ++v) is |= any_row_far[unit & 1][v];
             far = __builtin_amdgcn_readfirstlane(is) != 0;
             twice = few || far;
             if (far) {
@@ -786,7 +784,7 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
                     far_sum[unit - first_unit][wave][1] = far_hi;
                 }
                 far_lo = far_hi = weight_lo = weight_hi = 0.f;
-                own_hist += NW * width;
+                own_hist += kWavefronts * width;
                 __syncthreads();
                 if (more) fill_bias<E>(A, n_unit, starts, table, tid, THREADS);
             }
@@ -805,14 +803,14 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
     if constexpr (BIAS) {                             // the histograms of all heads: by wavefront, by bucket
         const int heads = end_unit - first_unit;
         for (int i = tid; i < heads * width; i += THREADS) {
-            float* x = hist + i / width * NW * width + i % width;
+            float* x = hist + i / width * kWavefronts * width + i % width;
 #pragma unroll
-            for (int v = 1; v < NW; ++v) x[0] += x[v * width];
+            for (int v = 1; v < kWavefronts; ++v) x[0] += x[v * width];
         }
         __syncthreads();
         for (int i = tid >> 3; i < heads * A.n_buckets; i += THREADS / 8) {
             const int u = i / A.n_buckets, b = i % A.n_buckets;
-            const float* x = hist + u * NW * width + middle;
+            const float* x = hist + u * kWavefronts * width + middle;
             const bool behind = b >= A.n_dir;                             // buckets of keys behind the query
             const int j0 = behind ? b - A.n_dir : b, end = starts[j0 + 1];
             float sum = 0.f;
@@ -822,7 +820,7 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
             if ((tid & 7) == 0) {
                 if (j0 == A.n_dir - 1)                                    // the open one of its direction
 #pragma unroll
-                    for (int v = 0; v < NW; ++v) sum += far_sum[u][v][behind ? 1 : 0];
+                    for (int v = 0; v < kWavefronts; ++v) sum += far_sum[u][v][behind ? 1 : 0];
                 bias_part[((int64_t)slot * A.heads + first_unit + u) * A.n_buckets + b] = sum;
             }
         }
@@ -835,16 +833,16 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
 // In 16 bits wide heads have two wavefronts for the same rows, one for either gradient: the scores are made twice (five products
 // where there were four), but two wavefronts share a SIMD (24 causal pages, forward and backward: 574 us, with one 865).
 template <class E, int D> constexpr bool kApart = sizeof(E) == 2 && D >= 96;
-template <class E, int D, int NW, bool BIAS, bool MASKED>
-__global__ __launch_bounds__((kApart<E, D> ? 128 : 64) * NW, (kGradientWaves<E, D, NW>)) void
+template <class E, int D, bool BIAS, bool MASKED>
+__global__ __launch_bounds__((kApart<E, D> ? 128 : 64) * kWavefronts, (kGradientWaves<E, D>)) void
 k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int q_slots, const E* dout, const float* lse,
                 const float* delta, const float* bias_part, E* dk, E* dv, E* dbias) {
     using O = Oper<E>;
     using T = Tile<E, D>;
-    constexpr int NB = T::ROWS / 32, DB = D / 32, COLS = 32 * NW;
+    constexpr int NB = T::ROWS / 32, DB = D / 32, COLS = 32 * kWavefronts;
     constexpr bool APART = kApart<E, D>;
-    constexpr int WAVES = APART ? 2 * NW : NW, THREADS = 64 * WAVES;
-    const bool keys = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) >= NW;        // (APART) this wavefront has the keys' gradient
+    constexpr int WAVES = APART ? 2 * kWavefronts : kWavefronts, THREADS = 64 * WAVES;
+    const bool keys = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) >= kWavefronts;        // (APART) this wavefront has the keys' gradient
     __shared__ __align__(256) char lds[2][2 * T::BYTES];
     __shared__ __align__(16) float row_lse[2][T::ROWS], row_delta[2][T::ROWS], row_far[2][2][T::ROWS];
     __shared__ int tile_far[2];                       // some row is far: row_far has log-sum-exps, and what is added to far rows' exponents
@@ -872,7 +870,7 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int q
     const Range qs = rest ? Range{0, 0, 0} : sequence_rows(A.qoff, seq, A.total_q);
     const int key0 = (slot - ks.place) * COLS;
     if (key0 < 0 || key0 >= ks.n) return;
-    const int wkey = key0 + wave % NW * 32, key = wkey + (lane & 31), shift = ks.n - qs.n;
+    const int wkey = key0 + wave % kWavefronts * 32, key = wkey + (lane & 31), shift = ks.n - qs.n;
     const bool real = key < ks.n;
     const int64_t at = ks.lo + key;
     const bool seen = real && (!MASKED || A.keep[at]);
@@ -1078,14 +1076,9 @@ template <class F> hipError_t by_width(int d, F&& f) {
         default: return f(std::integral_constant<int, 128>{});
     }
 }
-template <bool SINGLE, class F> hipError_t by_form(int waves, bool bias, bool masked, F&& f) {
-    auto w = [&](auto b, auto m) {
-        if constexpr (SINGLE)
-            if (waves == 1) return f(std::integral_constant<int, 1>{}, b, m);
-        return f(std::integral_constant<int, 4>{}, b, m);
-    };
-    if (bias) return masked ? w(std::true_type{}, std::true_type{}) : w(std::true_type{}, std::false_type{});
-    return masked ? w(std::false_type{}, std::true_type{}) : w(std::false_type{}, std::false_type{});
+template <class F> hipError_t by_form(bool bias, bool masked, F&& f) {
+    if (bias) return masked ? f(std::true_type{}, std::true_type{}) : f(std::true_type{}, std::false_type{});
+    return masked ? f(std::false_type{}, std::true_type{}) : f(std::false_type{}, std::false_type{});
 }
 
 template <class E>
@@ -1095,12 +1088,11 @@ hipError_t launch_attention(const AttnArgs& A, const AttnPlan& P, E* out, float*
         constexpr int D = decltype(dc)::value;
         float* o_part = (float*)(ws + P.o_part);
         float2* ml_part = (float2*)(ws + P.ml_part);
-        const hipError_t e = by_form<true>(P.q_waves, A.bias != nullptr, A.keep != nullptr, [&](auto nw, auto bias, auto masked) {
-            constexpr int NW = decltype(nw)::value;
+        const hipError_t e = by_form(A.bias != nullptr, A.keep != nullptr, [&](auto bias, auto masked) {
             constexpr bool BIAS = decltype(bias)::value, MASKED = decltype(masked)::value;
             const size_t lds = BIAS ? bias_bytes(A.reach, 1) : 0;
             const int64_t runs = (P.units + P.run - 1) / P.run;
-            k_attention<E, D, NW, BIAS, MASKED><<<dim3((unsigned)(P.q_slots * runs * P.splits)), 64 * NW, lds, st>>>(
+            k_attention<E, D, BIAS, MASKED><<<dim3((unsigned)(P.q_slots * runs * P.splits)), 64 * kWavefronts, lds, st>>>(
                 A, (int)P.q_slots, P.q_order, P.units, P.run, P.splits, out, lse, o_part, ml_part);
             return hipGetLastError();
         });
@@ -1119,27 +1111,25 @@ hipError_t launch_attention_backward(const AttnArgs& A, const AttnPlan& P, const
         constexpr int D = decltype(dc)::value;
         hipError_t e = hipSuccess;
         if (A.total_q > 0) {
-            e = by_form<kSingle<E, D>>(P.q_waves, A.bias != nullptr, A.keep != nullptr, [&](auto nw, auto bias, auto masked) {
-                constexpr int NW = decltype(nw)::value;
+            e = by_form(A.bias != nullptr, A.keep != nullptr, [&](auto bias, auto masked) {
                 constexpr bool BIAS = decltype(bias)::value, MASKED = decltype(masked)::value;
-                const size_t lds = BIAS ? bias_bytes(A.reach, 1 + P.run * NW) : 0;
+                const size_t lds = BIAS ? bias_bytes(A.reach, 1 + P.run * kWavefronts) : 0;
                 const int64_t runs = (P.units + P.run - 1) / P.run;
-                k_attention_dq<E, D, NW, BIAS, MASKED><<<dim3((unsigned)(P.q_slots * runs)), 64 * NW, lds, st>>>(
+                k_attention_dq<E, D, BIAS, MASKED><<<dim3((unsigned)(P.q_slots * runs)), 64 * kWavefronts, lds, st>>>(
                     A, (int)P.q_slots, P.q_order, P.units, P.run, (const E*)G.out, (const E*)G.dout, G.lse, (E*)G.dq, delta, bias_part);
                 return hipGetLastError();
             });
             if (e != hipSuccess) return e;
         }
         const int q_slots = A.total_q > 0 ? (int)P.q_slots : 0;
-        return by_form<kSingle<E, D>>(P.k_waves, A.bias != nullptr, A.keep != nullptr, [&](auto nw, auto bias, auto masked) {
-            constexpr int NW = decltype(nw)::value;
+        return by_form(A.bias != nullptr, A.keep != nullptr, [&](auto bias, auto masked) {
             constexpr bool BIAS = decltype(bias)::value, MASKED = decltype(masked)::value;
             const size_t lds = BIAS ? bias_bytes(A.reach, 1) : 0;
             const int main = A.total_k > 0 ? (int)(P.k_slots * ((A.kv_heads + P.kv_run - 1) / P.kv_run)) : 0;
-            constexpr int WAVES = kApart<E, D> ? 2 * NW : NW;
+            constexpr int WAVES = kApart<E, D> ? 2 * kWavefronts : kWavefronts;
             const int more = BIAS ? (A.n_buckets * A.heads + WAVES - 1) / WAVES : 0;
             if (main + more == 0) return hipSuccess;
-            k_attention_dkv<E, D, NW, BIAS, MASKED><<<dim3((unsigned)(main + more)), 64 * WAVES, lds, st>>>(
+            k_attention_dkv<E, D, BIAS, MASKED><<<dim3((unsigned)(main + more)), 64 * WAVES, lds, st>>>(
                 A, (int)P.k_slots, P.k_order, P.kv_run, main, q_slots, (const E*)G.dout, G.lse, delta, bias_part, (E*)G.dk, (E*)G.dv, (E*)G.dbias);
             return hipGetLastError();
         });

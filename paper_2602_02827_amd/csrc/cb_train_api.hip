@@ -17,16 +17,9 @@ AttnPlan plan_attention(const AttnArgs& A, int d, int dt, bool backward) {
     P.d = d;
     P.dt = dt;
     P.units = A.heads / A.pack;
-    // Up to 32 columns of a mean sequence get workgroups of one wavefront, which wait for no other, as long as all run at once (LDS
-    // holds about one a SIMD).  One query of 32 tokens, 12 heads: 16.7 us, with four wavefronts 17.7; 128 fp32 sequences of 32, 6
-    // heads, with gradients 39.5 and 40.6; but 512 sequences of 8 to 32, 12 heads, with gradients 233 and 219.
-    const int64_t q_cols = (int64_t)A.total_q * A.pack / A.n_seqs, k_rows = A.total_k / A.n_seqs;
-    const bool single = !backward || single_wavefronts_make_gradients(dt, d);
-    auto waves_of = [&](int64_t cols, int64_t groups) { return cols <= 32 && groups <= 1024 && single ? 1 : 4; };
-    P.q_waves = waves_of(q_cols, ((int64_t)A.total_q * A.pack / 32 + A.n_seqs) * P.units);
-    P.k_waves = waves_of(k_rows, (A.total_k / 32 + A.n_seqs) * A.kv_heads);
-    P.q_slots = A.total_q / (32 * P.q_waves / A.pack) + A.n_seqs;
-    P.k_slots = A.total_k / (32 * P.k_waves) + A.n_seqs;
+    const int64_t k_rows = A.total_k / A.n_seqs;
+    P.q_slots = A.total_q / (32 * kWavefronts / A.pack) + A.n_seqs;
+    P.k_slots = A.total_k / (32 * kWavefronts) + A.n_seqs;
     auto order_of = [&](int64_t slots, int64_t rows) {
         return rows <= kShortRows ? BY_XCD : A.causal && slots >= 4 * (int64_t)A.n_seqs ? LONGEST_FIRST : AS_THEY_COME;
     };
@@ -179,8 +172,8 @@ bool fits_a_grid(int64_t groups, int64_t threads) { return groups <= 0xffffffffl
 bool launchable(const AttnArgs& A, const AttnPlan& P) {
     if (A.heads > 1 << 12 || P.bytes >= (1ull << 46)) return false;
     const int64_t rows = (int64_t)A.heads * A.total_q, entries = A.bias ? (int64_t)A.n_buckets * A.heads : 0;
-    return fits_a_grid(P.q_slots * ((P.units + P.run - 1) / P.run) * P.splits, 64 * P.q_waves) &&
-           fits_a_grid(P.k_slots * ((A.kv_heads + P.kv_run - 1) / P.kv_run) + entries, 128 * P.k_waves) &&      // (some have twice as many)
+    return fits_a_grid(P.q_slots * ((P.units + P.run - 1) / P.run) * P.splits, 64 * kWavefronts) &&
+           fits_a_grid(P.k_slots * ((A.kv_heads + P.kv_run - 1) / P.kv_run) + entries, 128 * kWavefronts) &&      // (some have twice as many)
            (P.splits == 1 || fits_a_grid((rows + 3) / 4, 256));
 }
 

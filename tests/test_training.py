@@ -1099,13 +1099,12 @@ def test_fine_tuning_on_fewer_documents_than_a_batch(tr, dev):
 
 def heads_in_a_row(ql, kl, heads, kv_heads, bias):
     """Whether the plan's workgroups go on to a second head: units (key heads) in pairs leave 1,536 workgroups or more, of short
-    sequences and four wavefronts; for the queries' tiles and for the keys'."""
+    sequences; for the queries' tiles and for the keys'."""
     n, group = len(ql), heads // kv_heads
     pack = 1 if bias or group > 16 else group
     units, q_slots, k_slots = heads // pack, sum(ql) // (128 // pack) + n, sum(kl) // 128 + n
-    many = (sum(ql) * pack // 32 + n) * units > 1024 and (sum(kl) // 32 + n) * kv_heads > 1024
     short = sum(kl) // n <= 384 and sum(ql) * group // n <= 384
-    return many and short and units > 1 and q_slots * (units // 2) >= 1536, many and short and kv_heads > 1 and k_slots * (kv_heads // 2) >= 1536
+    return short and units > 1 and q_slots * (units // 2) >= 1536, short and kv_heads > 1 and k_slots * (kv_heads // 2) >= 1536
 
 
 @gpu
