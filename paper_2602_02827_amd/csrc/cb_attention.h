@@ -955,6 +955,7 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int q
     const typename T::At at_tiles(lds[0], lane);
     int buf = 0;
     while (true) {
+        const int far_now = tile_far[buf];
         const bool last_tile = c0 + T::ROWS >= cols;
         const int n_head = last_tile ? head0 + G : head0, n_c = last_tile ? col0 : c0 + T::ROWS;
         const bool last = last_tile && n_head % A.group == 0;                           // of a key head
@@ -964,10 +965,10 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int q
         if (any && busy && c0 + T::ROWS > wfirst) {
             const bool diagonal = A.causal && (wkey + 31 - shift) * G > c0;
             const typename T::At own = APART && !keys ? lg : lq;           // (own gradient's other operand)
-            const bool far = __builtin_amdgcn_readfirstlane(tile_far[buf]) != 0;
 #pragma unroll 1
             for (int b = 0; b < NB && c0 + 32 * b < cols; ++b) {
                 f32x16 s = {}, dp = {};
+                const bool far = __builtin_amdgcn_readfirstlane(far_now) != 0;
                 if constexpr (START) s = of_rows(row_lse[buf], b, h);
 #pragma unroll
                 for (int c = 0; c < D / 16; ++c) O::template mma<true>(s, T::rows(lq, b, c), k.v[c]);
