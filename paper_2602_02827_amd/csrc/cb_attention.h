@@ -53,10 +53,10 @@ __host__ __forceinline__ size_t bias_bytes(int reach, int tables) { return kStar
 // Places of tiles, in the order in which workgroups (and what each has several of: `inner`) take them.
 // BY_XCD: workgroups are dealt to the eight XCDs in turn; numbered so that each XCD has runs of consecutive ones (64, or as many as
 // leave each eight runs), the heads of a short sequence, whose values lie side by side, are read through one L2 (512 passages,
-// forward and backward: 700 us, as they come 722; 48 pages, where a head's tiles are kept together as they come: 588 and 578).
+// forward and backward: 691 us, as they come 709; 48 pages, where a head's tiles are kept together as they come: 576 and 563).
 // LONGEST_FIRST: under a causal limit the later rows see more keys (earlier keys are seen by more rows): places go round the
 // sequences, each one's longest tiles first (`down`: its last ones), so that short ones are left for the end.  Sequences are taken
-// to be of one length; others are only in another order; the last place, which only rows behind the last sequence can have, stays (24 causal pages, forward and backward: 492 us, as they come 561).
+// to be of one length; others are only in another order; the last place, which only rows behind the last sequence can have, stays (24 causal pages, forward and backward: 508 us, as they come 585).
 __device__ __forceinline__ int in_order(int block, int blocks) {
     const int lg = blocks < 128 ? 0 : blocks >= 4096 ? 6 : 25 - __builtin_clz(blocks);
     const int whole = blocks >> (lg + 3) << (lg + 3), xcd = block & 7, i = block >> 3;
@@ -222,23 +222,25 @@ __device__ __forceinline__ float hidden_unless(float x, uint32_t all) {
 template <class E, int D> constexpr int kWaves = sizeof(E) == 2 || D <= 32 ? 3 : D <= 96 ? 2 : 1;
 template <class E, int D> constexpr int kGradientWaves = sizeof(E) == 2 || D <= 32 ? 2 : 1;
 template <class E, int D> constexpr int kQueryWaves = sizeof(E) == 2 && D <= 64 ? 3 : kGradientWaves<E, D>;
-// Key rows of the forward pass's tiles: of wide heads 32, so that LDS holds three workgroups (48 pages of 1,030 rows, d = 128: 608
-// us, with 64 rows and two 640; the gradients' kernels, which have registers for two, lose by it).
+// Key rows of the forward pass's tiles: of wide heads 32, so that LDS and registers hold three workgroups (48 pages of 1,030 rows,
+// d = 128: 563 us; with 64 rows the compiler spills, 1,215; the gradients' kernels, which have registers for two, lose by 32).
 template <class E, int D> constexpr int kForwardRows = D >= 96 ? 32 : Oper<E>::ROWS;
 template <int D> constexpr bool kRuns = goes_on_to_next_head(D);
 
 // ---- forward -------------------------------------------------------------------------------------------------
 // One pass over the keys with the running maximum and sum of the softmax, in 32 bits; probabilities are rounded to the
-// storage type for the second product (their sum is not).  The maximum that is subtracted may lag by up to kLag: sums and
+// storage type for the second product (their sum is not; outputs in 16 bits are off by 2.3e-3 of their norm, their own rounding
+// is 1.7e-3; probabilities in two values would make three products of two).  The maximum that is subtracted may lag by up to kLag: sums and
 // outputs are rescaled only when it is passed, which few tiles after the first do; probabilities up to 2^kLag are no less exact
-// (48 pages of 1,030 rows, 16 heads of 128 over 8: 588 us, without a lag 633).
+// (48 pages of 1,030 rows, 16 heads of 128 over 8: 563 us, without a lag 613).
 constexpr float kLag = 8.f;
 // A workgroup takes its tile for `run` head units one after the other, the first keys of the next on their way while it
 // computes: short sequences have one to three tiles of keys, whose latency would otherwise be most of the time.
 // Long sequences are bound by the matrix and vector units' turns (an exponential, a maximum, a sum and half a conversion for every
-// score: as many clocks as the products): the pages above 564 us, 740 TFLOP/s where a large product reaches 1,189.  Short ones by
-// latency and what a workgroup does before its first product: 512 passages, 12 heads of 64 with bias and mask, 145 us.  Single
-// tokens by memory: 16 over 1 to 16,385 keys, two key heads of 128, 134 MB in 30 us and 7.5 us to join their parts.
+// score: as many clocks as the products): the pages above 552 to 565 us, 750 TFLOP/s where this library's scoring of all documents
+// reaches 1,504.  Short ones by latency and what a workgroup does before its first product: 512 passages, 12 heads of 64 with bias and
+// mask, 151 us.  Single tokens by memory: 16 over 1 to 16,385 keys, two key heads of 128, 134 MB in 30 us and 7.3 us to join their
+// parts.
 template <class E, int D, bool BIAS, bool MASKED>
 __global__ __launch_bounds__(64 * kWavefronts, (kWaves<E, D>)) void k_attention(const AttnArgs A, int slots, int order, int units, int run,
                                                                            int splits, E* out, float* lse, float* o_part,
@@ -495,10 +497,11 @@ __global__ __launch_bounds__(256) void k_attention_join(const AttnArgs A, int sp
 // The rounding of O reaches dS through delta, the same for all of a row.  Rows of dS sum to zero, so what a row's sum is
 // instead is the error of its delta: the first kernel adds it to the delta that the second one takes.  In the first, 16-bit dS goes
 // into its product as two values of eight bits each, which leaves O's rounding as the only error beside the result's own (gradients
-// of queries, against 64 bits, 512 passages: 2.6e-3 with one value, 2.0e-3 with two; the result's own rounding is 1.7e-3).  Rows that
+// of queries, against 64 bits, 512 passages: 2.6e-3 with one value, 2.0e-3 with two; the result's own rounding is 1.7e-3).  Those of
+// keys and values are made from dS and P in one value each: 2.35e-3, as a second one would be two more products of four.  Rows that
 // see few keys have small gradients and a large O, so that its rounding counts most there: tiles that see up to kTwice keys go over
 // them twice, first for delta in 32 bits (60 causal sequences of 1 to 17 tokens: 2.8e-3, so 1.7e-3; of 1 to 301: 2.2e-3 and 1.7e-3.
-// It costs the 512 passages 25 us of 671, with 64 keys 4 us, which leaves 2.1e-3 for sequences of up to 131 tokens).
+// It costs the 512 passages 22 us of 691, with 64 keys 2 us, which leaves 2.1e-3 for sequences of up to 131 tokens).
 constexpr int kTwice = 128;
 // P's error is the rounding of a log-sum-exp in 32 bits, 2^-24 of its size.  Rows where that would show (is_far: from 2^-16 on) are
 // normalised again: exponents are score - lse, which is exact or nearly so, and the first kernel goes over the keys of their tiles
@@ -509,9 +512,9 @@ __device__ __forceinline__ bool is_far(float lse, float scale2) {
     const float a = fabsf(lse);
     return a < INFINITY && (a > kFarRow || a * LOG2E > 1e30f * scale2);
 }
-// Bound by the matrix and vector units' turns where sequences are long (24 causal pages, 8 heads of 128 over 2: 172 and 228 us, 455
+// Bound by the matrix and vector units' turns where sequences are long (24 causal pages, 8 heads of 128 over 2: 178 and 227 us, 451
 // TFLOP/s of the three and four products that each cannot do without), by latency and by what surrounds the products where they are
-// short (the 512 passages: 289 and 250 us).
+// short (the 512 passages: 289 and 265 us).
 
 // Sums of a 32 x 32 block along its diagonals, added to a histogram by distance.  The block is in accumulators: a lane has sixteen
 // keys of a column.  Lane p of a half takes key k's value from column (p + k) mod 32: it lies on diagonal -p, or 32 - p where that
@@ -831,7 +834,7 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
 // of all tiles.
 // A wavefront with both gradients of 32 wide rows takes more than half of the registers, so nothing runs beside its waits.
 // In 16 bits wide heads have two wavefronts for the same rows, one for either gradient: the scores are made twice (five products
-// where there were four), but two wavefronts share a SIMD (24 causal pages, forward and backward: 574 us, with one 865).
+// where there were four), but two wavefronts share a SIMD (24 causal pages, forward and backward: 508 us, with one 828).
 template <class E, int D> constexpr bool kApart = sizeof(E) == 2 && D >= 96;
 template <class E, int D, bool BIAS, bool MASKED>
 __global__ __launch_bounds__((kApart<E, D> ? 128 : 64) * kWavefronts, (kGradientWaves<E, D>)) void

@@ -5,10 +5,10 @@ namespace cb {
 
 // Two launches for up to kTable tensors: squares into one partial sum a workgroup, then every workgroup of the second adds up the
 // partial sums itself, in their order (they are few and in L2), and scales its share.  What is read last by the first is read
-// first by the second, from the last-level cache where it fits.  Bound by memory: 57 million fp32 values, 46 us for the norm (4.9
-// TB/s) and 79 us for the scaling (226 MB in and out, 5.7 TB/s); a single small matrix by its two launches (5 us each).
-// Four workgroups a CU: 133 us in a row and 135 with cold caches, with eight 131 and 139, with two 153; chunks of half and twice the
-// size 132 and 134.
+// first by the second, from the last-level cache where it fits.  Bound by memory: 57 million fp32 values, 48 us for the norm (4.7
+// TB/s) and 78 us for the scaling (226 MB in and out, 5.8 TB/s); a single small matrix by its two launches (5 us each).
+// Four workgroups a CU: 133 us in a row and 135 with cold caches, with eight 132 and 139, with two 169; chunks of half and twice the
+// size 134 and 137.
 constexpr int kTable = 128, kThreads = 256, kMostParts = 1024;
 constexpr int64_t kChunk = 8192;                     // values of a chunk; a chunk has one tensor
 

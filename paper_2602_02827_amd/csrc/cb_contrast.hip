@@ -10,9 +10,11 @@ namespace cb {
 // ---- scores --------------------------------------------------------------------------------------------------
 // A workgroup keeps the rows of a few whole queries in registers, 32 * CT columns to a wavefront, and streams the tokens of
 // its documents through LDS, the next tile on its way while it multiplies.  A column's running maximum and its place stay in the
-// column's two lanes; a comparison, and two selections of it, for every product (the place within a block is a constant): these
-// three, not the matrix instructions, are what it is bound by.  64 x 32 tokens against 512 passages, d = 128: 50 us, 570 TFLOP/s;
-// 16 x 24 against 128 pages: 34 us.
+// column's two lanes; a comparison, and two selections of it, for every product (the place within a block is a constant).
+// 64 x 32 tokens against 512 passages, d = 128: 50 us, 570 TFLOP/s.  Vector instructions take 56 % of the SIMDs' clocks there, half of
+// them the three above, and the matrix units 35 %, with little of the one beside the other: four wavefronts a SIMD wait for the same
+// tile at the same barrier, and at a document's end for its shuffles, its stores and the next one's offsets.  16 x 24 against 128
+// pages: 34 us.
 template <class E, int D, int CT>
 __global__ __launch_bounds__(256, (sizeof(E) == 4 ? (D == 128 ? 1 : 2) : 4)) void
 k_maxsim_train(const E* Q, int nq, int T, const E* docs, const int64_t* off, int N, int total, int col_groups, int q_per, int docs_per,
@@ -205,8 +207,7 @@ template <class E, int D> struct RowLanes {
 // Queries: a row is the weighted sum of one token of every document.  A workgroup has one query token; its lane groups take the
 // documents in turn (all workgroups go through the corpus together, so its rows are found in L2), and their sums are added in
 // order.
-// Bound by the gathers from L2 and the last-level cache, as the documents' gradient is: 64 x 32 tokens and 512 passages, both 88 us
-// for 1.05 million rows of 256 bytes each, 6.1 TB/s.
+// 64 x 32 tokens and 512 passages: 37 us by themselves, 1.05 million rows of 256 bytes, 7.2 TB/s from L2 and the last-level cache.
 template <class E, int D>
 __device__ __forceinline__ void query_gradient(char* lds, int block, const float* dscores, const int32_t* argmax, int T, const E* docs,
                                                const int64_t* off, int N, int total, E* dQ) {
@@ -254,6 +255,9 @@ __device__ __forceinline__ void query_gradient(char* lds, int block, const float
 // (query, token) entries that chose one of them by token, keeping their order (each wavefront a quarter of the entries, lanes
 // with the same token found by ballots), and each lane group adds up the lists of consecutive tokens as one, eight rows on
 // their way at a time.  The sort, not atomics on the rows, so that the order of the sums is fixed.
+// 64 x 32 tokens and 512 passages: 74 us by themselves, 87 together with the queries' workgroups.  Over that launch vector
+// instructions take 70 % of the SIMDs' clocks (the sort's ballots and places; a multiply-add and half an unpacking for every value),
+// and the wavefronts wait 61 % of theirs; the queries that are gathered, 0.5 MB, lie in every L2.
 // MANY: more entries than are sorted at once; the rows are added up in LDS then.
 constexpr int kEntries = 4096, kTokens = 64;
 template <int D, bool MANY> struct TokenLists {
@@ -433,7 +437,7 @@ hipError_t launch_maxsim_scores(const void* Q, int nq, int T, int d, int dt, con
         using E = decltype(type);
         constexpr int D = decltype(dc)::value;
         // About as many workgroups as run at once (four a CU; 512, 768 and 2,048 measured alike), of consecutive documents each.
-        // Two columns a lane read a tile's operands half as often (64 x 32 tokens against 512 passages, both kernels: 139 us, one
+        // Two columns a lane read a tile's operands half as often (64 x 32 tokens against 512 passages, the whole loss: 140 us, one
         // column 145), where there are enough workgroups of them (16 x 24 tokens against 128 pages: 63 us, one column 57).
         constexpr int64_t kGroups = 1024;
         auto go = [&](auto ct) {

@@ -27,7 +27,7 @@ AttnPlan plan_attention(const AttnArgs& A, int d, int dt, bool backward) {
     P.k_order = order_of(P.k_slots, (int64_t)A.total_q * A.group / A.n_seqs);
     P.splits = 1;
     // Short sequences: a workgroup goes on to the next heads, as long as enough workgroups are left (six a CU).
-    // 512 passages, forward and backward: 701 us, one head each 724.
+    // 512 passages, forward and backward: 691 us, one head each 706.
     auto run_of = [](int64_t slots, int units, int64_t rows) {
         int r = 1;
         while (rows <= kShortRows && 2 * r <= kMostRun && 2 * r <= units && slots * (units / (2 * r)) >= 1536) r *= 2;
@@ -47,8 +47,8 @@ AttnPlan plan_attention(const AttnArgs& A, int d, int dt, bool backward) {
     };
     if (!backward) {
         // Few tiles over long keys: their keys are cut into parts of 128 rows or more (on average; the longest sequence's are
-        // longer) until there are 2,048 workgroups.  16 tokens over 1 to 16,385 keys, us: 50 so, 53 with 256 rows and 1,024, 65 with
-        // 128 and 4,096, 80 with 512 and 1,024.
+        // longer) until there are 2,048 workgroups.  16 tokens over 1 to 16,385 keys, us: 40 so, 46 with 256 rows and 1,024, 42 with
+        // 128 and 4,096, 66 with 512 and 1,024.
         if (groups < 512 && k_rows >= 512) {
             int64_t s = (2048 - 1 + groups) / groups;
             s = s < k_rows / 128 ? s : k_rows / 128;
@@ -155,7 +155,7 @@ int attn_args(const colbandit_attn* a, AttnArgs& A) {
     A.heads = a->heads;
     A.kv_heads = a->kv_heads;
     A.group = a->heads / a->kv_heads;
-    // (16 single tokens, four heads to a key head: 42 us, a tile for each head 98; 48 pages, two heads to one: 588 and 612)
+    // (16 single tokens, four heads to a key head: 40 us, a tile for each head 85; 24 causal pages, with gradients: 507 and 541)
     A.pack = !a->bias && A.group <= 16 && a->q_head * eb <= kMostRowBytes && a->total_q <= kMostRows / A.group &&
                      a->total_k <= kMostRows / A.group ? A.group : 1;      // columns are counted in 31 bits
     A.total_q = (int)a->total_q;
