@@ -1314,3 +1314,43 @@ def test_a_query_that_is_nan_is_in_every_result(tr, dev, dtype, ql, kl, bias):
         assert bool(torch.isnan(x).all())
     for x in (f["out"][:-1], f["lse"][:, :-1], b["dq"][:-1], b["dk"][:kl[0]], b["dv"][:kl[0]]):
         assert bool(torch.isfinite(x).all())
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [32, 64])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("head", [0, 1, 2])
+def test_one_head_of_several_in_a_row_is_far_from_zero(tr, dev, dtype, d, causal, head):
+    """Workgroups that go on from a head whose rows see nothing but a hidden distance to one whose do not, and the other way."""
+    lengths = np.random.default_rng(43).integers(0, 4, 1600).tolist()
+    assert heads_in_a_row(lengths, lengths, 3, 3, 8) == (True, True)
+    p = problem(dev, dtype, lengths, lengths, 3, 3, d, seed=43, bias=8)
+    p["bias"][0, head] = torch.finfo(DT[dtype]).min
+    check_far(tr, p, lengths, lengths, dtype, causal)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,heads,kv_heads", [(64, 4, 4), (128, 4, 2), (96, 3, 1)])
+@pytest.mark.parametrize("ql,kl", [([150, 3, 70], [150, 3, 70]), ([40, 1], [1100, 900])])
+@pytest.mark.parametrize("causal", [False, True])
+def test_rows_on_both_sides_of_where_they_are_normalised_again(tr, dev, monkeypatch, dtype, d, heads, kv_heads, ql, kl, causal):
+    """Ordinary rows with biases that move them to 240 and to 280: log-sum-exps below and above 256 in one call.  Scores of up to 290
+    carry nine times the error of the file's bound, which is for up to 32."""
+    monkeypatch.setitem(globals(), "F", F * 290 / 32)
+    p = problem(dev, dtype, ql, kl, heads, kv_heads, d, seed=44, bias=32, keep=True)
+    p["bias"] += torch.tensor([240.0, 280.0], device=dev).repeat(2)[:heads].to(DT[dtype])
+    check_attention(tr, p, ql, kl, dtype, causal)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+def test_a_table_of_minus_infinity_hides_a_distance(tr, dev, dtype, d, causal):
+    """Rows that see nothing else see nothing."""
+    lengths = [50, 1, 133, 1]
+    p = problem(dev, dtype, lengths, lengths, 2, 2, d, seed=45, bias=8)
+    p["bias"][0] = -math.inf
+    check_attention(tr, p, lengths, lengths, dtype, causal)
