@@ -135,6 +135,7 @@ int colbandit_maxsim_scores(const void *Q, int n_queries, int T, int d, colbandi
  * A target outside 0 .. N-1 takes its query out of the mean: loss 0, dscores 0.  Scores of
  * -inf have no weight; a target's makes a loss of +inf, and if all are -inf the loss and its
  * gradient are NaN, as the formula has it.
+ *   temperature  > 0, finite, and so is its inverse in 32 bits
  *   targets  DEVICE int64 [n_queries];  loss DEVICE float [n_queries]
  *   dscores  DEVICE float [n_queries][N]
  */

@@ -260,7 +260,7 @@ int colbandit_contrastive_loss(const float* scores, int n_queries, int64_t N, co
                                float* dscores, void* stream) {
     if (!scores || !targets || !loss || !dscores) return COLBANDIT_ERR_NULL;
     if (n_queries < 1 || N < 1) return COLBANDIT_ERR_SHAPE;
-    if (!(temperature > 0.f && temperature < INFINITY)) return COLBANDIT_ERR_KNOB;
+    if (!(temperature > 0.f && temperature < INFINITY && 1.f / temperature < INFINITY)) return COLBANDIT_ERR_KNOB;
     if (n_queries > 65535) return COLBANDIT_ERR_UNSUPPORTED;
     if (misaligned(scores, 4) || misaligned(targets, 8) || misaligned(loss, 4) || misaligned(dscores, 4)) return COLBANDIT_ERR_ALIGNMENT;
     return hip(launch_contrastive_loss(scores, n_queries, N, targets, temperature, loss, dscores, (hipStream_t)stream));

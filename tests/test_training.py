@@ -1354,3 +1354,9 @@ def test_a_table_of_minus_infinity_hides_a_distance(tr, dev, dtype, d, causal):
     p = problem(dev, dtype, lengths, lengths, 2, 2, d, seed=45, bias=8)
     p["bias"][0] = -math.inf
     check_attention(tr, p, lengths, lengths, dtype, causal)
+
+
+def test_a_temperature_whose_inverse_is_infinite_is_refused(tr):
+    L = tr.lib()
+    for temperature in (1e-39, 1e-45):
+        assert L.colbandit_contrastive_loss(0x1000, 2, 3, 0x2000, temperature, 0x3000, 0x4000, None) == -3
