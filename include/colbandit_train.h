@@ -46,7 +46,9 @@ extern "C" {
  *   S_ij   = scale * <q_i, k_j> + bias[bucket(j - p_i)][head]
  *   seen   : keep == NULL or keep[key row j] != 0, and not causal or j <= p_i
  *   out_i  = sum_j exp(S_ij - lse_i) v_j,   lse_i = log sum_j exp(S_ij)   over the seen j
- * A row that sees nothing has out = 0 and lse = -inf, and takes no part in any gradient.
+ * A row that sees nothing has out = 0 and lse = -inf, and takes no part in any gradient (its q
+ * and dout may hold anything where the mask, the causal limit or lengths hide its keys, and are
+ * finite where biases of -inf do).
  * Query head h reads key head h / (heads / kv_heads).  Keys that the mask hides may hold
  * anything, infinities and NaN included.
  * Scores are held in 32 bits: of a bias of 1e9 in size a row's products leave nothing.  Rows whose
