@@ -1360,3 +1360,23 @@ def test_a_temperature_whose_inverse_is_infinite_is_refused(tr):
     L = tr.lib()
     for temperature in (1e-39, 1e-45):
         assert L.colbandit_contrastive_loss(0x1000, 2, 3, 0x2000, temperature, 0x3000, 0x4000, None) == -3
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,H,Hk,bias", [(64, 2, 2, 8), (64, 6, 2, None), (128, 4, 2, None), (96, 2, 2, 32)])
+def test_rows_before_all_keys_may_hold_anything(tr, dev, dtype, d, H, Hk, bias):
+    """More queries than keys under a causal limit, and none at all: rows that see nothing, without a mask."""
+    ql, kl = [140, 40, 7, 300], [9, 39, 0, 150]
+    p = problem(dev, dtype, ql, kl, H, Hk, d, seed=46, bias=bias)
+    f, b = check_attention(tr, p, ql, kl, dtype, True)
+    wild = dict(p, q=p["q"].clone(), dout=p["dout"].clone())
+    a = 0
+    for lq, lk in zip(ql, kl):
+        wild["q"][a:a + lq - lk] = math.nan
+        wild["dout"][a:a + lq - lk] = math.inf
+        a += lq
+    f2, b2 = attend(tr, wild, ql, kl, True)
+    for x, y in ((f, f2), (b, b2)):
+        for name in x:
+            assert x[name] is None or torch.equal(x[name], y[name]), name
