@@ -14,6 +14,12 @@
  *   colbandit_contrastive_loss     cross-entropy over each query's scores, and its gradient
  *   colbandit_maxsim_backward      gradients of the embeddings from those of the scores
  *   colbandit_clip_gradients       global norm of many tensors, and the tensors clipped to it
+ *   colbandit_embedding            rows of a token table, scaled; its gradient by sorted tokens
+ *   colbandit_norm_rotate          queries and keys, each head normalised, weighted and rotated by
+ *                                  its row's position; its gradients
+ *   colbandit_attention_window     attention through a window around each row, and to the first
+ *                                  keys of its sequence; its gradients
+ *   colbandit_orthogonalise        matrices (updates of weights) made nearly orthogonal
  *
  * Conventions are those of colbandit.h: DEVICE pointers are the caller's memory on the
  * current HIP device, HOST pointers are plain memory that is read before the call returns;
@@ -115,6 +121,118 @@ int colbandit_attention(const colbandit_attn *a, void *out, float *lse, void *wo
 int colbandit_attention_backward(const colbandit_attn *a, const void *out, const float *lse,
                                  const void *dout, void *dq, void *dk, void *dv, void *dbias,
                                  void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The same attention, of rows that see less of their sequence:
+ *   seen   : as above, and (p_i - before <= j <= p_i + after or j < sinks)
+ * Under a causal limit `after` says nothing.  Keys and values that the mask leaves are finite
+ * (also those that no row's window reaches).  Rows: at most 2^28.  The gradients' workgroups for
+ * the first keys count towards a launch's, one for 512 rows of a sequence and each key head.
+ */
+#define COLBANDIT_MAX_SINKS 1024
+typedef struct {
+    int64_t before, after;         /* >= 0; of any size                                   */
+    int64_t sinks;                 /* 0 .. COLBANDIT_MAX_SINKS                            */
+} colbandit_window;
+size_t colbandit_sizeof_window(void);
+
+size_t colbandit_attention_window_workspace_bytes(const colbandit_attn *a, const colbandit_window *w,
+                                                  int backward);
+int colbandit_attention_window(const colbandit_attn *a, const colbandit_window *w, void *out,
+                               float *lse, void *workspace, size_t workspace_bytes, void *stream);
+int colbandit_attention_window_backward(const colbandit_attn *a, const colbandit_window *w,
+                                        const void *out, const float *lse, const void *dout,
+                                        void *dq, void *dk, void *dv, void *dbias, void *workspace,
+                                        size_t workspace_bytes, void *stream);
+
+/*
+ * out[i] = scale * table[tokens[i]], zeros where the token is none of 0 .. vocab-1 (padding)
+ *   table    DEVICE [vocab][width], rows table_row elements apart
+ *   tokens   DEVICE int64 [n];  out DEVICE [n][width]
+ * Products in 32 bits, rounded once; table and out may differ in type.
+ * n below 2^31 - 2^16, vocab at most 2^24, width at most 2^16.  Values looked up below 2^34 (2^37
+ * where rows begin at whole multiples of 16 bytes and width is one of 8), of the gradient, n / 64
+ * rows more than the table's, below 2^32 (2^35).
+ */
+int colbandit_embedding(const void *table, colbandit_dtype table_dt, int64_t table_row,
+                        const int64_t *tokens, int64_t n, int64_t vocab, int64_t width, float scale,
+                        void *out, colbandit_dtype out_dt, void *stream);
+/*
+ * dtable[v] = scale * sum of dout[i] over the i whose token is v; zeros for tokens that do not occur
+ *   dout     DEVICE [n][width], rows dout_row elements apart;  dtable DEVICE [vocab][width]
+ * Sums in 32 bits, in the order of i (of more than 64 in groups of 64 of the sorted tokens).  What
+ * stands in rows of padding tokens is not read.
+ */
+size_t colbandit_embedding_workspace_bytes(int64_t n, int64_t vocab, int64_t width);
+int colbandit_embedding_backward(const void *dout, colbandit_dtype dout_dt, int64_t dout_row,
+                                 const int64_t *tokens, int64_t n, int64_t vocab, int64_t width,
+                                 float scale, void *dtable, colbandit_dtype table_dt,
+                                 void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Norms and rotation of queries and keys.  Of a head's d values x
+ *   y = x / sqrt(mean of x^2 + eps) * weight
+ * and of each pair (y_a, y_b), whose cosine c and sine s are the table's at the row's position,
+ *   out_a = y_a c - y_b s,  out_b = y_b c + y_a s
+ * Pair i is values 2i and 2i + 1 (interleaved) or i and i + d/2.  Arithmetic in 32 bits, rounded
+ * once; squares must not overflow there (|x| below 2^60).
+ * Rows whose position is none of the table's (padding) get zeros, and take no part in any gradient.
+ * Rows of q and k lie q_row elements apart and heads q_head apart (likewise k); the d values are
+ * consecutive.  Pointers to q, k, the table, outputs and gradients, and strides, are whole multiples
+ * of 16 bytes.  Outputs and their gradients are dense, [rows][heads][d].  Heads: at most 4,096.
+ */
+typedef struct {
+    int dt;                        /* colbandit_dtype of q, k, outputs, their gradients   */
+    int heads, kv_heads, d;        /* d: 32, 64, 96 or 128                                */
+    int interleaved;
+    float eps;                     /* >= 0                                                */
+    int64_t rows, n_positions;
+    const void *q, *k;             /* DEVICE                                              */
+    int64_t q_row, q_head, k_row, k_head;
+    const float *q_weight, *k_weight;          /* DEVICE [d], or NULL: ones               */
+    const float *table;            /* DEVICE [n_positions][d/2][2], or NULL: no rotation  */
+    const int64_t *positions;      /* DEVICE [rows]; not read without a table             */
+} colbandit_rotation;
+size_t colbandit_sizeof_rotation(void);
+
+/*
+ * The usual table, in HOST memory [n_positions][d/2][2]: cosine and sine of position * base^(-2i/d),
+ * computed in 64 bits.  Pure host code.
+ */
+int colbandit_rotary_table(int64_t n_positions, int d, double base, float *table);
+
+int colbandit_norm_rotate(const colbandit_rotation *r, void *q_out, void *k_out, void *stream);
+/*
+ * dq, dk from the gradients of the outputs; dq_weight, dk_weight DEVICE float [d], either may be
+ * NULL.  Sums in 32 bits, in a fixed order.
+ */
+size_t colbandit_norm_rotate_workspace_bytes(const colbandit_rotation *r);
+int colbandit_norm_rotate_backward(const colbandit_rotation *r, const void *dq_out, const void *dk_out,
+                                   void *dq, void *dk, float *dq_weight, float *dk_weight,
+                                   void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Each matrix G, in the singular value decomposition U S V^T of it divided by its Frobenius norm,
+ * becomes U p(..p(S)) V^T with p(s) = a s + b s^3 + c s^5, `steps` times: with the usual
+ * coefficients singular values come near to one.  Computed by matrix products,
+ *   X <- a X + (b A + c A^2) X,  A = X X^T
+ * whose sums are 32 bits; X, A and the bracket are held as two 16-bit pieces each, 22 bits of a
+ * value.  A matrix of zeros stays zeros, one that holds an infinity or NaN is NaN everywhere.
+ *   n_matrices    >= 1
+ *   in, out       HOST arrays of DEVICE pointers [rows][cols], dense, each aligned to its type
+ *                 (out[i] may be in[i]; no other two overlap)
+ *   rows, cols    HOST, >= 0; the smaller of the two at most 2^14, the other 2^26
+ *   dts           HOST: colbandit_dtype of each matrix and its output
+ *   steps         1 .. 64
+ *   coefficients  HOST float [3]: a, b, c.  Refused (COLBANDIT_ERR_KNOB) where singular values from
+ *                 0 to 1 would pass 4 in size in some step, or b s^2 + c s^4 would pass 32.
+ */
+size_t colbandit_orthogonalise_workspace_bytes(int64_t n_matrices, const int64_t *rows,
+                                               const int64_t *cols);
+int colbandit_orthogonalise(int64_t n_matrices, const void *const *in, void *const *out,
+                            const int64_t *rows, const int64_t *cols, const int32_t *dts, int steps,
+                            const float *coefficients, void *workspace, size_t workspace_bytes,
+                            void *stream);
 
 /*
  * MaxSim of all pairs, for training: scores[q][i] = sum_t max_j <Q[q][t], docs[offsets[i]+j]>.

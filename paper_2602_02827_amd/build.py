@@ -10,8 +10,9 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcolbandit.so")
 SOURCES = ["cb_api.hip", "cb_kernels.hip", "cb_dense.hip", "cb_quant.hip", "cb_baselines.hip"]
 # the training operators: infinities and NaN have their meaning there
-TRAIN_SOURCES = ["cb_train_api.hip", "cb_attention_bf16.hip", "cb_attention_f32.hip", "cb_contrast.hip", "cb_clip.hip"]
-HEADERS = ["cb_device.h", "cb_launch.h", "cb_segments.h", "cb_sample.h", "cb_train.h", "cb_tile.h", "cb_attention.h",
+TRAIN_SOURCES = ["cb_train_api.hip", "cb_attention_bf16.hip", "cb_attention_f32.hip", "cb_attention_window_bf16.hip",
+                 "cb_attention_window_f32.hip", "cb_contrast.hip", "cb_clip.hip", "cb_embed.hip", "cb_rotate.hip", "cb_ortho.hip"]
+HEADERS = ["cb_device.h", "cb_launch.h", "cb_segments.h", "cb_sample.h", "cb_train.h", "cb_tile.h", "cb_attention.h", "cb_ortho.h",
            os.path.join("..", "..", "include", "colbandit.h"), os.path.join("..", "..", "include", "colbandit_train.h")]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-Xarch_device", "-fno-honor-nans", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          # packed fp32 VALU forms are kept off for the device code of this library

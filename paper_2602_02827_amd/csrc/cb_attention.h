@@ -171,6 +171,35 @@ struct QueryTile {
     }
 };
 
+// Tiles of the keys that a workgroup's rows see: all of them from the first one on or, with a window, those of the first keys
+// that all rows see (`first` of them) and then the ones from the first row's first key to the last row's last.  Where they meet they are
+// one run.
+template <bool WIN, int ROWS> struct KeyTiles {
+    int count;
+    __device__ __forceinline__ KeyTiles(const AttnArgs&, QueryTile& t, int) : count((t.end + ROWS - 1) / ROWS) {}
+    __device__ __forceinline__ int base(int i) const { return i * ROWS; }
+};
+template <int ROWS> struct KeyTiles<true, ROWS> {
+    int count, first, lo;
+    __device__ __forceinline__ KeyTiles(const AttnArgs& A, QueryTile& t, int per) {
+        const int last = (t.row0 + per < t.Lq ? t.row0 + per : t.Lq) - 1 + t.shift;
+        int sinks = A.sinks < t.Lk ? A.sinks : t.Lk;
+        if (A.causal && last + 1 < sinks) sinks = last + 1 < 0 ? 0 : last + 1;
+        int hi = last + A.after + 1;
+        hi = hi < 0 ? 0 : hi > t.Lk ? t.Lk : hi;
+        lo = t.row0 + t.shift - A.before;
+        lo = lo < 0 ? 0 : lo > hi ? hi : lo;
+        first = (sinks + ROWS - 1) / ROWS;
+        if (lo < first * ROWS) {
+            first = lo = 0;
+            hi = hi > sinks ? hi : sinks;
+        }
+        t.end = hi;
+        count = first + (hi - lo + ROWS - 1) / ROWS;
+    }
+    __device__ __forceinline__ int base(int i) const { return i < first ? i * ROWS : lo + (i - first) * ROWS; }
+};
+
 // A wavefront's 32 columns of it.
 struct QueryColumns {
     int row, head, lim, first_lim, end;       // own row, head in its unit, key limit; that of the first column; keys that any sees
@@ -187,6 +216,42 @@ struct QueryColumns {
         const int e = last + t.shift + 1;
         end = A.causal && e < t.end ? e : t.end;
     }
+};
+
+// What a wavefront's columns, and a lane's, see of the keys through a window.  The first keys of a sequence are seen by all rows (under
+// a causal limit, by those that are not before them).
+__device__ __forceinline__ uint32_t bits_up_to(int room);
+struct ColumnWindow {
+    int lo, hi, sink;                         // of the lane's column: first and last key, last of the first keys
+    int any_lo, any_hi, any_sink;             // of all columns: from the first key of any to the last of any
+    int all_lo, all_hi, all_sink;             // from the last one's first key to the first one's last
+    __device__ __forceinline__ ColumnWindow(const AttnArgs& A, const QueryTile& t, const QueryColumns& w, int G, int wave) {
+        const int first = w.first_lim, last = t.row0 + (wave * 32 + 31) / G + t.shift;
+        lo = w.lim - A.before;
+        hi = w.lim + A.after;
+        any_lo = first - A.before;
+        all_lo = last - A.before;
+        all_hi = first + A.after;
+        any_hi = last + A.after < t.end ? last + A.after : t.end - 1;
+        auto limit = [&](int p) { return A.causal && p < A.sinks - 1 ? p : A.sinks - 1; };
+        sink = limit(w.lim);
+        any_sink = limit(last);
+        all_sink = limit(first);
+    }
+    // whether some column sees some of the n keys from `base` on; whether every one sees all of them
+    __device__ __forceinline__ bool some(int base, int n) const { return (base <= any_hi && base + n > any_lo) || base <= any_sink; }
+    __device__ __forceinline__ bool every(int base, int n) const { return (base >= all_lo && base + n - 1 <= all_hi) || base + n - 1 <= all_sink; }
+    // keys that the column sees, of those that a lane has (from `base` on), as bits
+    __device__ __forceinline__ uint32_t bits(int base) const {
+        return (bits_up_to(hi - base) & ~bits_up_to(lo - 1 - base)) | bits_up_to(sink - base);
+    }
+    static __device__ __forceinline__ uint64_t up_to(int room) { return room < 0 ? 0ull : room >= 63 ? ~0ull : (2ull << room) - 1ull; }
+    __device__ __forceinline__ uint64_t wide_bits(int base) const {
+        return (up_to(hi - base) & ~up_to(lo - 1 - base)) | up_to(sink - base);
+    }
+};
+struct NoWindow {
+    __device__ __forceinline__ NoWindow(const AttnArgs&, const QueryTile&, const QueryColumns&, int, int) {}
 };
 
 template <int LO> __device__ __forceinline__ f32x8 eight(const f32x16& x) {
@@ -241,7 +306,7 @@ constexpr float kLag = 8.f;
 // reaches 1,504.  Short ones by latency and what a workgroup does before its first product: 512 passages, 12 heads of 64 with bias and
 // mask, 151 us.  Single tokens by memory: 16 over 1 to 16,385 keys, two key heads of 128, 134 MB in 30 us and 7.3 us to join their
 // parts.
-template <class E, int D, bool BIAS, bool MASKED>
+template <class E, int D, bool BIAS, bool MASKED, bool WIN>
 __global__ __launch_bounds__(64 * kWavefronts, (kWaves<E, D>)) void k_attention(const AttnArgs A, int slots, int order, int units, int run,
                                                                            int splits, E* out, float* lse, float* o_part,
                                                                            float2* ml_part) {
@@ -257,10 +322,12 @@ __global__ __launch_bounds__(64 * kWavefronts, (kWaves<E, D>)) void k_attention(
     int unit = work.inner / splits * run;
     const int end_unit = unit + run < units ? unit + run : units;
     const int G = A.pack, per = 32 * kWavefronts / G;
-    const QueryTile t(A, slot, per, lane);
+    QueryTile t(A, slot, per, lane);
     if (t.none) return;
+    const KeyTiles<WIN, T::ROWS> at_key(A, t, per);
     const QueryColumns w(A, t, G, per, wave, lane);
-    const int tiles = (t.end + T::ROWS - 1) / T::ROWS, each = (tiles + splits - 1) / splits;
+    const std::conditional_t<WIN, ColumnWindow, NoWindow> win(A, t, w, G, wave);
+    const int tiles = at_key.count, each = (tiles + splits - 1) / splits;
     const int first_tile = split * each, end_tile = first_tile + each < tiles ? first_tile + each : tiles;
 
     const int64_t krow = A.k_row * (int64_t)sizeof(E), vrow = A.v_row * (int64_t)sizeof(E);
@@ -289,7 +356,7 @@ __global__ __launch_bounds__(64 * kWavefronts, (kWaves<E, D>)) void k_attention(
         q.take_sign(A.scale);
     };
     const bool any = first_tile < end_tile;
-    if (any) issue(unit, first_tile * T::ROWS, lds[0]);
+    if (any) issue(unit, at_key.base(first_tile), lds[0]);
     load_q(unit);
     int16_t* starts = (int16_t*)dyn;
     float* table = (float*)(dyn + kStartsBytes);
@@ -309,16 +376,27 @@ __global__ __launch_bounds__(64 * kWavefronts, (kWaves<E, D>)) void k_attention(
     const typename T::At at_tiles(lds[0], lane);
     int i = first_tile, buf = 0;
     while (true) {
-        const int base = i * T::ROWS;
+        const int base = at_key.base(i);
         const typename T::At lk = at_tiles + buf * 2 * T::BYTES, lv = lk + T::BYTES;
         const bool last = i + 1 >= end_tile;                     // of the unit
         const int n_unit = last ? unit + 1 : unit, n_i = last ? first_tile : i + 1;
         const bool more = kRuns<D> ? n_unit < end_unit : !last;
-        if (more && any) issue(n_unit, n_i * T::ROWS, lds[buf ^ 1]);
-        if (any && w.busy && base < w.end) {
-            const bool one = NB > 1 && base + 32 >= w.end;       // its second block has no keys
-            const bool diagonal = A.causal && base + T::ROWS - 1 > w.first_lim, part = seen != kAllRows;
-            if constexpr (MASKED) {
+        if (more && any) issue(n_unit, at_key.base(n_i), lds[buf ^ 1]);
+        bool visit = any && w.busy, one, diagonal;               // one: its second block has no keys
+        const bool part = seen != kAllRows;
+        if constexpr (WIN) {
+            visit = visit && win.some(base, T::ROWS);
+            one = NB > 1 && !win.some(base + 32, 32);
+            diagonal = !win.every(base, T::ROWS);
+        } else {
+            visit = visit && base < w.end;
+            one = NB > 1 && base + 32 >= w.end;
+            diagonal = A.causal && base + T::ROWS - 1 > w.first_lim;
+        }
+        if (visit) {
+            if constexpr (MASKED && WIN) {
+                sees |= (seen & win.wide_bits(base)) != 0;
+            } else if constexpr (MASKED) {
                 const int room = A.causal ? w.lim - base : 63;
                 sees |= (seen & (room < 0 ? 0ull : room >= 63 ? ~0ull : (2ull << room) - 1ull)) != 0;
             }
@@ -344,7 +422,9 @@ __global__ __launch_bounds__(64 * kWavefronts, (kWaves<E, D>)) void k_attention(
                 }
                 if (part) s[b] += of_rows(hidden[buf], b, h);
                 if (diagonal) {
-                    const uint32_t own = bits_up_to(w.lim - base - 32 * b - 4 * h);
+                    uint32_t own;
+                    if constexpr (WIN) own = win.bits(base + 32 * b + 4 * h);
+                    else own = bits_up_to(w.lim - base - 32 * b - 4 * h);
 #pragma unroll
                     for (int r = 0; r < 16; ++r) s[b][r] = hidden_unless(s[b][r], all_if(own, r));
                 }
@@ -538,7 +618,7 @@ __device__ __forceinline__ void add_diagonals(const f32x16& x, float* hist, int 
 }
 
 // Gradients of queries, delta, and the bias table's share of each tile; head units one after the other, as the forward pass.
-template <class E, int D, bool BIAS, bool MASKED>
+template <class E, int D, bool BIAS, bool MASKED, bool WIN>
 __global__ __launch_bounds__(64 * kWavefronts, (kQueryWaves<E, D>)) void
 k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const E* out, const E* dout, const float* lse, E* dq,
                float* delta, float* bias_part) {
@@ -557,16 +637,18 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
     int unit = first_unit;
     const int end_unit = unit + run < units ? unit + run : units;
     const int G = A.pack, per = 32 * kWavefronts / G;
-    const QueryTile t(A, slot, per, lane);
+    QueryTile t(A, slot, per, lane);
     if (t.none) {
         if constexpr (BIAS)
             for (int b = tid; b < (end_unit - unit) * A.n_buckets; b += THREADS)
                 bias_part[((int64_t)slot * A.heads + unit) * A.n_buckets + b] = 0.f;
         return;
     }
+    const KeyTiles<WIN, T::ROWS> at_key(A, t, per);
     const QueryColumns w(A, t, G, per, wave, lane);
-    const int tiles = (t.end + T::ROWS - 1) / T::ROWS;
-    const bool few = sizeof(E) == 2 && t.end <= kTwice;
+    const std::conditional_t<WIN, ColumnWindow, NoWindow> win(A, t, w, G, wave);
+    const int tiles = at_key.count;
+    const bool few = sizeof(E) == 2 && (WIN ? tiles * T::ROWS <= kTwice || A.before + A.after + A.sinks < kTwice : t.end <= kTwice);
     bool far = false, twice = few;                               // some row of the tile is far; twice: first for delta and sums
     const int64_t krow = A.k_row * (int64_t)sizeof(E), vrow = A.v_row * (int64_t)sizeof(E);
     Staged<E, D, THREADS, MASKED, T::ROWS> next;
@@ -588,7 +670,7 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
         seen = __ballot(next_keep != 0) & kAllRows;
     };
     const bool any = tiles > 0;
-    if (any) issue(unit, 0, lds[0]);
+    if (any) issue(unit, at_key.base(0), lds[0]);
     Column<E, D> q, g;
     float dot = 0.f, own_lse = 0.f;                              // own_lse: what is added to the exponent
     const float unit_scale = unit_of_scores(A.scale), scale2 = unit_scale * LOG2E;
@@ -654,16 +736,26 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
         }
         const bool before = twice && i < tiles;
         const float k = BIAS || far ? LOG2E : scale2;
-        const int base = (i < tiles ? i : i - tiles) * T::ROWS;
+        const int base = at_key.base(i < tiles ? i : i - tiles);
         const typename T::At lk = at_tiles + buf * 2 * T::BYTES, lv = lk + T::BYTES;
         const bool last = i + 1 >= (twice ? 2 * tiles : tiles);
         const int n_unit = last ? unit + 1 : unit, n_i = last ? 0 : i + 1;
         const bool more = kRuns<D> ? n_unit < end_unit : !last;
-        if (more && any) issue(n_unit, (n_i < tiles ? n_i : n_i - tiles) * T::ROWS, lds[buf ^ 1]);
-        if (any && w.busy && base < w.end) {
-            const bool diagonal = A.causal && base + T::ROWS - 1 > w.first_lim, part = seen != kAllRows;
+        if (more && any) issue(n_unit, at_key.base(n_i < tiles ? n_i : n_i - tiles), lds[buf ^ 1]);
+        bool visit = any && w.busy, diagonal;
+        const bool part = seen != kAllRows;
+        if constexpr (WIN) {
+            visit = visit && win.some(base, T::ROWS);
+            diagonal = !win.every(base, T::ROWS);
+        } else {
+            visit = visit && base < w.end;
+            diagonal = A.causal && base + T::ROWS - 1 > w.first_lim;
+        }
+        if (visit) {
 #pragma unroll 1
-            for (int b = 0; b < NB && base + 32 * b < w.end; ++b) {
+            for (int b = 0; b < NB && (WIN || base + 32 * b < w.end); ++b) {
+                if constexpr (WIN)
+                    if (!win.some(base + 32 * b, 32)) continue;
                 f32x16 s = {}, dp;
 #pragma unroll
                 for (int c = 0; c < D / 16; ++c) O::mma(s, T::rows(lk, b, c), q.v[c]);
@@ -685,7 +777,9 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
                 }
                 if (part) s += of_rows(hidden[buf], b, h);
                 if (diagonal) {                       // (dp as well: what the row does not see may be anything)
-                    const uint32_t own = bits_up_to(w.lim - base - 32 * b - 4 * h);
+                    uint32_t own;
+                    if constexpr (WIN) own = win.bits(base + 32 * b + 4 * h);
+                    else own = bits_up_to(w.lim - base - 32 * b - 4 * h);
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         s[r] = hidden_unless(s[r], all_if(own, r));
@@ -836,10 +930,13 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
 // In 16 bits wide heads have two wavefronts for the same rows, one for either gradient: the scores are made twice (five products
 // where there were four), but two wavefronts share a SIMD (24 causal pages, forward and backward: 508 us, with one 828).
 template <class E, int D> constexpr bool kApart = sizeof(E) == 2 && D >= 96;
-template <class E, int D, bool BIAS, bool MASKED>
+// With a window the first keys are left to workgroups of their own (from `main` on, `sink_groups` of them), since all of a sequence's
+// rows see them: a key tile's others see some rows only.  Such a workgroup takes kSinkRows rows of a sequence, and leaves its shares of
+// the first keys' gradients to k_attention_join_sinks.
+template <class E, int D, bool BIAS, bool MASKED, bool WIN>
 __global__ __launch_bounds__((kApart<E, D> ? 128 : 64) * kWavefronts, (kGradientWaves<E, D>)) void
-k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int q_slots, const E* dout, const float* lse,
-                const float* delta, const float* bias_part, E* dk, E* dv, E* dbias) {
+k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int sink_groups, int q_slots, const E* dout, const float* lse,
+                const float* delta, const float* bias_part, E* dk, E* dv, E* dbias, float* sink_part) {
     using O = Oper<E>;
     using T = Tile<E, D>;
     constexpr int NB = T::ROWS / 32, DB = D / 32, COLS = 32 * kWavefronts;
@@ -852,8 +949,8 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int q
     extern __shared__ __align__(16) char dyn[];
     const int tid = threadIdx.x, lane0 = tid & 63, lane = lane0, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     if constexpr (BIAS) {
-        if ((int)blockIdx.x >= main) {                // one entry of the table each wavefront
-            const int e = ((int)blockIdx.x - main) * WAVES + wave;
+        if ((int)blockIdx.x >= main + (WIN ? sink_groups : 0)) {      // one entry of the table each wavefront
+            const int e = ((int)blockIdx.x - main - (WIN ? sink_groups : 0)) * WAVES + wave;
             if (e >= A.n_buckets * A.heads) return;
             const int head = e / A.n_buckets, b = e % A.n_buckets;
             float sum = 0.f;
@@ -864,22 +961,69 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int q
             return;
         }
     }
-    const Work work = work_of(blockIdx.x, slots, (A.kv_heads + run - 1) / run, A.n_seqs, order, false);
-    const int slot = work.slot, kv0 = work.inner * run;
-    const int kv_end = kv0 + run < A.kv_heads ? kv0 + run : A.kv_heads;
-    const int seq = find_sequence(A.koff, A.n_seqs, COLS, A.total_k, slot, lane);
-    bool rest;
-    const Range ks = rows_of_place(A.koff, seq, A.n_seqs, A.total_k, COLS, slot, rest);
-    const Range qs = rest ? Range{0, 0, 0} : sequence_rows(A.qoff, seq, A.total_q);
-    const int key0 = (slot - ks.place) * COLS;
-    if (key0 < 0 || key0 >= ks.n) return;
+    const bool sinks = WIN && (int)blockIdx.x >= main;
+    int slot, kv0, kv_end, seq, key0;
+    bool rest = false;
+    Range ks, qs;
+    if (!sinks) {
+        const Work work = work_of(blockIdx.x, slots, (A.kv_heads + run - 1) / run, A.n_seqs, order, false);
+        slot = work.slot;
+        kv0 = work.inner * run;
+        kv_end = kv0 + run < A.kv_heads ? kv0 + run : A.kv_heads;
+        seq = find_sequence(A.koff, A.n_seqs, COLS, A.total_k, slot, lane);
+        ks = rows_of_place(A.koff, seq, A.n_seqs, A.total_k, COLS, slot, rest);
+        qs = rest ? Range{0, 0, 0} : sequence_rows(A.qoff, seq, A.total_q);
+        key0 = (slot - ks.place) * COLS;
+        if (key0 < 0 || key0 >= ks.n) return;
+    } else {
+        const int x = (int)blockIdx.x - main, inner = A.kv_heads * ((A.sinks + COLS - 1) / COLS);
+        slot = x / inner;
+        kv0 = x % inner % A.kv_heads;
+        kv_end = kv0 + 1;
+        key0 = x % inner / A.kv_heads * COLS;
+        seq = find_sequence(A.qoff, A.n_seqs, kSinkRows, A.total_q, slot, lane);
+        qs = rows_of_place(A.qoff, seq, A.n_seqs, A.total_q, kSinkRows, slot, rest);
+        if (rest) return;
+        ks = sequence_rows(A.koff, seq, A.total_k);
+    }
     const int wkey = key0 + wave % kWavefronts * 32, key = wkey + (lane & 31), shift = ks.n - qs.n;
-    const bool real = key < ks.n;
+    const int G = A.pack;
+    int key_from = 0, key_to = ks.n;                              // keys that are this workgroup's
+    int cols = qs.n * G;
+    // columns from the first row that sees a key of the tile: rows before it may see nothing at all
+    int col0 = A.causal && key0 > shift ? (key0 - shift) * G : 0;
+    int wfirst = A.causal && wkey > shift ? (wkey - shift) * G : 0;             // first column that sees a key of the wavefront
+    int wend = cols, see_from = 0, see_to = 0, all_from = 0, all_to = 0;        // (WIN) columns that see the lane's key; all of the wavefront's
+    if constexpr (WIN) {
+        auto row = [&](int r) { return r < 0 ? 0 : r > qs.n ? qs.n : r; };      // ends of ranges of rows
+        if (sinks) {
+            const int begin = (slot - qs.place) * kSinkRows, end = row(begin + kSinkRows);
+            key_to = A.sinks < ks.n ? A.sinks : ks.n;
+            if (begin < 0 || begin >= qs.n || key0 >= key_to) return;
+            const int from = A.causal ? row(key0 - shift) : 0;
+            col0 = (from > begin ? from : begin) * G;
+            cols = wend = end * G;
+            see_from = A.causal ? row(key - shift) * G : 0;
+            see_to = cols;
+            all_from = A.causal ? row(wkey + 31 - shift) * G : 0;
+            all_to = cols;
+        } else {
+            key_from = rest ? 0 : A.sinks;
+            if (key0 + COLS <= key_from) return;
+            const int last = key0 + COLS < ks.n ? key0 + COLS : ks.n, wlast = wkey + 32 < ks.n ? wkey + 32 : ks.n;
+            col0 = row((key0 > key_from ? key0 : key_from) - A.after - shift) * G;
+            cols = row(last + A.before - shift) * G;
+            wfirst = row((wkey > key_from ? wkey : key_from) - A.after - shift) * G;
+            wend = row(wlast + A.before - shift) * G;
+            see_from = row(key - A.after - shift) * G;
+            see_to = row(key + 1 + A.before - shift) * G;
+            all_from = row(wkey + 31 - A.after - shift) * G;
+            all_to = row(wkey + 1 + A.before - shift) * G;
+        }
+    }
+    const bool real = key < key_to && key >= key_from;
     const int64_t at = ks.lo + key;
     const bool seen = real && (!MASKED || A.keep[at]);
-    const int G = A.pack, cols = qs.n * G;
-    // columns from the first row that sees a key of the tile: rows before it may see nothing at all
-    const int col0 = A.causal && key0 > shift ? (key0 - shift) * G : 0;
 
     const int64_t qrow = A.q_row * (int64_t)sizeof(E), qhead = A.q_head * (int64_t)sizeof(E);
     const int64_t grow = (int64_t)A.heads * D * (int64_t)sizeof(E), ghead = D * (int64_t)sizeof(E);
@@ -944,8 +1088,7 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int q
     load_keys(kv0);
     f32x16 acc[DB] = {}, acc2[APART ? 1 : DB] = {};              // of keys and of values, or of the wavefront's own
     const int middle = bias_middle(A.reach);
-    const bool busy = wkey < ks.n;
-    const int wfirst = A.causal && wkey > shift ? (wkey - shift) * G : 0;             // first column that sees a key of the wavefront
+    const bool busy = wkey < key_to && wkey + 32 > key_from;
     int16_t* starts = (int16_t*)dyn;
     float* table = (float*)(dyn + kStartsBytes);
     if constexpr (BIAS) {
@@ -965,11 +1108,15 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int q
         const bool more = kRuns<D> ? n_head < head_end : !last;
         if (more && any) issue(n_head, n_c, lds[buf ^ 1]);
         const typename T::At lq = at_tiles + buf * 2 * T::BYTES, lg = lq + T::BYTES;
-        if (any && busy && c0 + T::ROWS > wfirst) {
-            const bool diagonal = A.causal && (wkey + 31 - shift) * G > c0;
+        if (any && busy && c0 + T::ROWS > wfirst && (!WIN || c0 < wend)) {
+            bool diagonal;
+            if constexpr (WIN) diagonal = c0 < all_from || c0 + T::ROWS > all_to;
+            else diagonal = A.causal && (wkey + 31 - shift) * G > c0;
             const typename T::At own = APART && !keys ? lg : lq;           // (own gradient's other operand)
 #pragma unroll 1
-            for (int b = 0; b < NB && c0 + 32 * b < cols; ++b) {
+            for (int b = 0; b < NB && c0 + 32 * b < (WIN ? wend : cols); ++b) {
+                if constexpr (WIN)
+                    if (c0 + 32 * b + 32 <= wfirst) continue;
                 f32x16 s = {}, dp = {};
                 const bool far = __builtin_amdgcn_readfirstlane(far_now) != 0;
                 if constexpr (START) s = of_rows(row_lse[buf], b, h);
@@ -1007,7 +1154,13 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int q
                     for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], per_unit, x[r]);
                 }
                 if (diagonal) {                       // a lane's key is seen by columns from (key - shift) G on
-                    const uint32_t own = ~bits_up_to((key - shift) * G - c0 - 32 * b - 4 * h - 1);
+                    uint32_t own;
+                    if constexpr (WIN) {
+                        const int from = c0 + 32 * b + 4 * h;
+                        own = bits_up_to(see_to - 1 - from) & ~bits_up_to(see_from - 1 - from);
+                    } else {
+                        own = ~bits_up_to((key - shift) * G - c0 - 32 * b - 4 * h - 1);
+                    }
 #pragma unroll
                     for (int r = 0; r < 16; ++r) s[r] = hidden_unless(s[r], all_if(own, r));
                 }
@@ -1045,7 +1198,24 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int q
                             O::store4(to + dense + 32 * db + 8 * j + 4 * h, seen ? x : f32x4{0.f, 0.f, 0.f, 0.f});
                         }
                 };
-                if constexpr (!APART) {
+                if (WIN && sinks) {
+                    float* to = sink_part + (((int64_t)slot * A.kv_heads + kv) * A.sinks + key) * 2 * D;
+                    auto leave = [&](int which, const f32x16(&a)[DB], float by) {
+#pragma unroll
+                        for (int db = 0; db < DB; ++db)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const f32x4 x = {a[db][4 * j] * by, a[db][4 * j + 1] * by, a[db][4 * j + 2] * by, a[db][4 * j + 3] * by};
+                                *(f32x4*)(to + which * D + 32 * db + 8 * j + 4 * h) = seen ? x : f32x4{0.f, 0.f, 0.f, 0.f};
+                            }
+                    };
+                    if constexpr (!APART) {
+                        leave(0, acc, A.scale);
+                        leave(1, acc2, 1.f);
+                    } else {
+                        leave(keys ? 0 : 1, acc, keys ? A.scale : 1.f);
+                    }
+                } else if constexpr (!APART) {
                     store(dk, acc, A.scale);
                     store(dv, acc2, 1.f);
                 } else {
@@ -1071,6 +1241,25 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int q
     }
 }
 
+// Adds up the shares of the first keys' gradients: a wavefront for each of them and key head.
+template <class E, int D>
+__global__ __launch_bounds__(256) void k_attention_join_sinks(const AttnArgs A, const float* part, E* dk, E* dv) {
+    const int lane = threadIdx.x & 63;
+    const int64_t place = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t of = place / A.sinks;
+    const int key = (int)(place - of * A.sinks), seq = (int)(of / A.kv_heads), kv = (int)(of % A.kv_heads);
+    if (seq >= A.n_seqs || lane >= D / 2) return;
+    const Range ks = sequence_rows(A.koff, seq, A.total_k), qs = sequence_rows(A.qoff, seq, A.total_q, kSinkRows);
+    if (key >= ks.n) return;
+    const int parts = (qs.n + kSinkRows - 1) / kSinkRows;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int p = 0; p < parts; ++p)
+        sum += *(const f32x4*)(part + (((int64_t)(qs.place + p) * A.kv_heads + kv) * A.sinks + key) * 2 * D + 4 * lane);
+    E* to = lane < D / 4 ? dk : dv;
+    Oper<E>::store4(to + ((int64_t)(ks.lo + key) * A.kv_heads + kv) * D + 4 * (lane % (D / 4)), sum);
+}
+
 // ---- launches ------------------------------------------------------------------------------------------------
 template <class F> hipError_t by_width(int d, F&& f) {
     switch (d) {
@@ -1085,7 +1274,7 @@ template <class F> hipError_t by_form(bool bias, bool masked, F&& f) {
     return masked ? f(std::false_type{}, std::true_type{}) : f(std::false_type{}, std::false_type{});
 }
 
-template <class E>
+template <class E, bool WIN>
 hipError_t launch_attention(const AttnArgs& A, const AttnPlan& P, E* out, float* lse, char* ws, hipStream_t st) {
     if (A.total_q == 0) return hipSuccess;
     return by_width(P.d, [&](auto dc) {
@@ -1096,7 +1285,7 @@ hipError_t launch_attention(const AttnArgs& A, const AttnPlan& P, E* out, float*
             constexpr bool BIAS = decltype(bias)::value, MASKED = decltype(masked)::value;
             const size_t lds = BIAS ? bias_bytes(A.reach, 1) : 0;
             const int64_t runs = (P.units + P.run - 1) / P.run;
-            k_attention<E, D, BIAS, MASKED><<<dim3((unsigned)(P.q_slots * runs * P.splits)), 64 * kWavefronts, lds, st>>>(
+            k_attention<E, D, BIAS, MASKED, WIN><<<dim3((unsigned)(P.q_slots * runs * P.splits)), 64 * kWavefronts, lds, st>>>(
                 A, (int)P.q_slots, P.q_order, P.units, P.run, P.splits, out, lse, o_part, ml_part);
             return hipGetLastError();
         });
@@ -1107,7 +1296,7 @@ hipError_t launch_attention(const AttnArgs& A, const AttnPlan& P, E* out, float*
     });
 }
 
-template <class E>
+template <class E, bool WIN>
 hipError_t launch_attention_backward(const AttnArgs& A, const AttnPlan& P, const AttnGrads& G, char* ws, hipStream_t st) {
     float* delta = (float*)(ws + P.delta);
     float* bias_part = (float*)(ws + P.bias_part);
@@ -1119,24 +1308,33 @@ hipError_t launch_attention_backward(const AttnArgs& A, const AttnPlan& P, const
                 constexpr bool BIAS = decltype(bias)::value, MASKED = decltype(masked)::value;
                 const size_t lds = BIAS ? bias_bytes(A.reach, 1 + P.run * kWavefronts) : 0;
                 const int64_t runs = (P.units + P.run - 1) / P.run;
-                k_attention_dq<E, D, BIAS, MASKED><<<dim3((unsigned)(P.q_slots * runs)), 64 * kWavefronts, lds, st>>>(
+                k_attention_dq<E, D, BIAS, MASKED, WIN><<<dim3((unsigned)(P.q_slots * runs)), 64 * kWavefronts, lds, st>>>(
                     A, (int)P.q_slots, P.q_order, P.units, P.run, (const E*)G.out, (const E*)G.dout, G.lse, (E*)G.dq, delta, bias_part);
                 return hipGetLastError();
             });
             if (e != hipSuccess) return e;
         }
         const int q_slots = A.total_q > 0 ? (int)P.q_slots : 0;
-        return by_form(A.bias != nullptr, A.keep != nullptr, [&](auto bias, auto masked) {
+        e = by_form(A.bias != nullptr, A.keep != nullptr, [&](auto bias, auto masked) {
             constexpr bool BIAS = decltype(bias)::value, MASKED = decltype(masked)::value;
             const size_t lds = BIAS ? bias_bytes(A.reach, 1) : 0;
             const int main = A.total_k > 0 ? (int)(P.k_slots * ((A.kv_heads + P.kv_run - 1) / P.kv_run)) : 0;
             constexpr int WAVES = kApart<E, D> ? 2 * kWavefronts : kWavefronts;
             const int more = BIAS ? (A.n_buckets * A.heads + WAVES - 1) / WAVES : 0;
+            const int sinks = WIN && main ? (int)P.sink_groups : 0;
             if (main + more == 0) return hipSuccess;
-            k_attention_dkv<E, D, BIAS, MASKED><<<dim3((unsigned)(main + more)), 64 * WAVES, lds, st>>>(
-                A, (int)P.k_slots, P.k_order, P.kv_run, main, q_slots, (const E*)G.dout, G.lse, delta, bias_part, (E*)G.dk, (E*)G.dv, (E*)G.dbias);
+            k_attention_dkv<E, D, BIAS, MASKED, WIN><<<dim3((unsigned)(main + sinks + more)), 64 * WAVES, lds, st>>>(
+                A, (int)P.k_slots, P.k_order, P.kv_run, main, sinks, q_slots, (const E*)G.dout, G.lse, delta, bias_part, (E*)G.dk, (E*)G.dv,
+                (E*)G.dbias, (float*)(ws + P.sink_part));
             return hipGetLastError();
         });
+        if constexpr (WIN) {
+            if (e != hipSuccess || !A.sinks || !A.total_k) return e;
+            const int64_t places = (int64_t)A.n_seqs * A.kv_heads * A.sinks;
+            k_attention_join_sinks<E, D><<<dim3((unsigned)((places + 3) / 4)), 256, 0, st>>>(A, (const float*)(ws + P.sink_part), (E*)G.dk, (E*)G.dv);
+            e = hipGetLastError();
+        }
+        return e;
     });
 }
 

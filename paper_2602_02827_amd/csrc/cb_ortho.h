@@ -1,0 +1,24 @@
+// What the kernels that orthogonalise matrices are told about them (by value).
+#pragma once
+#include <stddef.h>
+#include <stdint.h>
+
+namespace cb {
+
+constexpr int kOrthoTable = 40;
+
+struct OrthoMatrix {
+    const void* in;
+    void* out;
+    size_t x, y, a, b;                               // places in the workspace: X of even and of odd steps, A, B
+    int m, n, mp, np;                                // m <= n, and both rounded up to whole tiles
+    uint32_t chunk0, side0, square0, apply0;         // its first workgroups
+    uint8_t bf16, tall;                              // tall: in and out are n x m
+};
+struct OrthoTable {
+    OrthoMatrix of[kOrthoTable];
+    int n;
+};
+static_assert(sizeof(OrthoTable) <= 3800, "kernel arguments");
+
+}  // namespace cb

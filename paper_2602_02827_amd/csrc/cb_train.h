@@ -22,6 +22,8 @@ struct AttnArgs {
     int n_buckets, n_dir;        // buckets in all, and of one direction
     int reach;                   // first distance of a direction's last bucket
     int16_t starts[128];         // first distance of each bucket of one direction
+    int windowed;                // rows see `before` keys before them, `after` behind them, and the first `sinks`
+    int before, after, sinks;
 };
 
 // Wavefronts of a workgroup, 32 columns each.  (Of one, for sequences of up to 32 columns: one query of 32 tokens, forward pass and both
@@ -30,6 +32,9 @@ constexpr int kWavefronts = 4;
 // Wide heads take all registers: their workgroups do not go on to the next one.
 constexpr bool goes_on_to_next_head(int d) { return d <= 64; }
 constexpr int kMostRun = 2;      // heads that a workgroup takes one after the other (four: the histograms leave half the workgroups no LDS)
+
+// Rows of a sequence that one workgroup adds up for the gradients of its first keys, where all rows see them.
+constexpr int kSinkRows = 512;
 
 enum { AS_THEY_COME, BY_XCD, LONGEST_FIRST };         // order of workgroups
 
@@ -40,7 +45,8 @@ struct AttnPlan {
     int units;                   // head units: heads / pack
     int run, kv_run;             // head units (key heads) that a workgroup takes one after the other
     int splits;                  // parts that the keys of a forward call's tiles are cut into
-    size_t o_part, ml_part, delta, bias_part, bytes;
+    int64_t sink_groups;         // workgroups for the first keys' gradients
+    size_t o_part, ml_part, delta, bias_part, sink_part, bytes;
 };
 AttnPlan plan_attention(const AttnArgs& A, int d, int dt, bool backward);
 
@@ -54,6 +60,11 @@ struct AttnGrads {
 hipError_t launch_attention_backward_bf16(const AttnArgs& A, const AttnPlan& P, const AttnGrads& G, char* ws, hipStream_t st);
 hipError_t launch_attention_backward_f32(const AttnArgs& A, const AttnPlan& P, const AttnGrads& G, char* ws, hipStream_t st);
 
+hipError_t launch_attention_window_bf16(const AttnArgs& A, const AttnPlan& P, void* out, float* lse, char* ws, hipStream_t st);
+hipError_t launch_attention_window_f32(const AttnArgs& A, const AttnPlan& P, void* out, float* lse, char* ws, hipStream_t st);
+hipError_t launch_attention_window_backward_bf16(const AttnArgs& A, const AttnPlan& P, const AttnGrads& G, char* ws, hipStream_t st);
+hipError_t launch_attention_window_backward_f32(const AttnArgs& A, const AttnPlan& P, const AttnGrads& G, char* ws, hipStream_t st);
+
 hipError_t launch_maxsim_scores(const void* Q, int nq, int T, int d, int dt, const void* docs, const int64_t* off, int64_t N,
                                 int64_t total, float* scores, int32_t* argmax, hipStream_t st);
 hipError_t launch_contrastive_loss(const float* scores, int nq, int64_t N, const int64_t* targets, float temperature,
@@ -66,5 +77,36 @@ hipError_t launch_maxsim_backward(const float* dscores, const int32_t* argmax, c
 size_t clip_workspace_bytes(int64_t n, const int64_t* sizes);
 hipError_t launch_clip(int64_t n, const void* const* grads, void* const* out, const int64_t* sizes, const int32_t* dts,
                        float max_norm, float* norm, void* ws, hipStream_t st);
+
+bool embedding_is_wide(const void* rows, int rows_dt, int64_t row, const void* dense, int dense_dt, int64_t width);
+bool embedding_launchable(int64_t n, int64_t vocab, int64_t width, bool wide, bool backward);
+hipError_t launch_embedding(const void* table, int table_dt, int64_t table_row, const int64_t* tokens, int64_t n, int64_t vocab, int64_t width,
+                            float scale, void* out, int out_dt, hipStream_t st);
+size_t embedding_workspace_bytes(int64_t n, int64_t vocab, int64_t width);
+hipError_t launch_embedding_backward(const void* dout, int dout_dt, int64_t dout_row, const int64_t* tokens, int64_t n, int64_t vocab,
+                                     int64_t width, float scale, void* dtable, int table_dt, char* ws, hipStream_t st);
+
+// Norms of queries and keys with rotation, as the kernels take them (by value).
+struct RotateArgs {
+    const void *q, *k;
+    int64_t q_row, q_head, k_row, k_head;
+    const float *q_weight, *k_weight, *table;        // table [n_positions][d / 2][2]: cosine, sine
+    const int64_t* positions;
+    int64_t rows, n_positions;
+    int heads, kv_heads, near;
+    float eps;
+    const void *dq_out, *dk_out;                     // (backward pass) gradients of the outputs
+    void *q_to, *k_to;                               // outputs, or gradients of the inputs
+    float* part;                                     // the workgroups' sums for the weights' gradients
+};
+int64_t rotate_groups(const RotateArgs& A, int d, bool back);
+size_t rotate_workspace_bytes(const RotateArgs& A, int d);
+hipError_t launch_rotate(const RotateArgs& A, int d, int dt, hipStream_t st);
+hipError_t launch_rotate_backward(const RotateArgs& A, int d, int dt, float* dq_weight, float* dk_weight, hipStream_t st);
+
+size_t ortho_workspace_bytes(int64_t n, const int64_t* rows, const int64_t* cols);
+bool ortho_launchable(int64_t n, const int64_t* rows, const int64_t* cols);
+hipError_t launch_ortho(int64_t n, const void* const* in, void* const* out, const int64_t* rows, const int64_t* cols, const int32_t* dts,
+                        int steps, const float* coefficients, char* ws, hipStream_t st);
 
 }  // namespace cb

@@ -17,14 +17,19 @@ AttnPlan plan_attention(const AttnArgs& A, int d, int dt, bool backward) {
     P.d = d;
     P.dt = dt;
     P.units = A.heads / A.pack;
-    const int64_t k_rows = A.total_k / A.n_seqs;
+    int64_t k_rows = A.total_k / A.n_seqs, q_rows = (int64_t)A.total_q * A.group / A.n_seqs;
+    if (A.windowed) {                                // what a tile sees of them
+        const int64_t tile = 32 * kWavefronts, span = (int64_t)A.before + A.after + tile;
+        k_rows = span + A.sinks < k_rows ? span + A.sinks : k_rows;
+        q_rows = span * A.group < q_rows ? span * A.group : q_rows;
+    }
     P.q_slots = A.total_q / (32 * kWavefronts / A.pack) + A.n_seqs;
     P.k_slots = A.total_k / (32 * kWavefronts) + A.n_seqs;
     auto order_of = [&](int64_t slots, int64_t rows) {
         return rows <= kShortRows ? BY_XCD : A.causal && slots >= 4 * (int64_t)A.n_seqs ? LONGEST_FIRST : AS_THEY_COME;
     };
     P.q_order = order_of(P.q_slots, k_rows);
-    P.k_order = order_of(P.k_slots, (int64_t)A.total_q * A.group / A.n_seqs);
+    P.k_order = order_of(P.k_slots, q_rows);
     P.splits = 1;
     // Short sequences: a workgroup goes on to the next heads, as long as enough workgroups are left (six a CU).
     // 512 passages, forward and backward: 691 us, one head each 706.
@@ -34,7 +39,7 @@ AttnPlan plan_attention(const AttnArgs& A, int d, int dt, bool backward) {
         return r;
     };
     P.run = goes_on_to_next_head(d) ? run_of(P.q_slots, P.units, k_rows) : 1;
-    P.kv_run = goes_on_to_next_head(d) ? run_of(P.k_slots, A.kv_heads, (int64_t)A.total_q * A.group / A.n_seqs) : 1;
+    P.kv_run = goes_on_to_next_head(d) ? run_of(P.k_slots, A.kv_heads, q_rows) : 1;
     if (A.bias && A.reach > 128) P.run = 1;          // (histograms of all its heads are in LDS)
     const int64_t groups = P.q_slots * P.units;
     ++P.q_slots;                                     // the rows behind the last sequence may end in a tile of their own
@@ -62,6 +67,11 @@ AttnPlan plan_attention(const AttnArgs& A, int d, int dt, bool backward) {
     } else {
         P.delta = take((int64_t)A.heads * A.total_q * 8);        // and a value of rows that are far (is_far)
         if (A.bias) P.bias_part = take(P.q_slots * A.heads * A.n_buckets * 4);
+        if (A.windowed && A.sinks) {
+            const int64_t slots = A.total_q / kSinkRows + A.n_seqs, tile = 32 * kWavefronts;
+            P.sink_groups = slots * A.kv_heads * ((A.sinks + tile - 1) / tile);
+            P.sink_part = take(slots * A.kv_heads * A.sinks * 2 * d * 4);
+        }
     }
     P.bytes = o;
     return P;
@@ -165,6 +175,21 @@ int attn_args(const colbandit_attn* a, AttnArgs& A) {
     return COLBANDIT_OK;
 }
 
+// Distances and their sums with rows are counted in 31 bits.
+constexpr int64_t kMostWindowRows = 1 << 28;
+constexpr int kWholeWindow = 1 << 29;
+
+int window_args(const colbandit_window* w, AttnArgs& A) {
+    if (!w) return COLBANDIT_ERR_NULL;
+    if (w->before < 0 || w->after < 0 || w->sinks < 0) return COLBANDIT_ERR_SHAPE;
+    if (w->sinks > COLBANDIT_MAX_SINKS || A.total_q > kMostWindowRows || A.total_k > kMostWindowRows) return COLBANDIT_ERR_UNSUPPORTED;
+    A.windowed = 1;
+    A.before = w->before < kWholeWindow ? (int)w->before : kWholeWindow;
+    A.after = A.causal ? 0 : w->after < kWholeWindow ? (int)w->after : kWholeWindow;
+    A.sinks = (int)w->sinks;
+    return COLBANDIT_OK;
+}
+
 // Threads of one launch, below 2^32.
 bool fits_a_grid(int64_t groups, int64_t threads) { return groups <= 0xffffffffll / threads; }
 
@@ -173,7 +198,8 @@ bool launchable(const AttnArgs& A, const AttnPlan& P) {
     if (A.heads > 1 << 12 || P.bytes >= (1ull << 46)) return false;
     const int64_t rows = (int64_t)A.heads * A.total_q, entries = A.bias ? (int64_t)A.n_buckets * A.heads : 0;
     return fits_a_grid(P.q_slots * ((P.units + P.run - 1) / P.run) * P.splits, 64 * kWavefronts) &&
-           fits_a_grid(P.k_slots * ((A.kv_heads + P.kv_run - 1) / P.kv_run) + entries, 128 * kWavefronts) &&      // (some have twice as many)
+           fits_a_grid(P.k_slots * ((A.kv_heads + P.kv_run - 1) / P.kv_run) + P.sink_groups + entries, 128 * kWavefronts) &&      // (some have twice as many)
+           fits_a_grid(((int64_t)A.n_seqs * A.kv_heads * A.sinks + 3) / 4, 256) &&
            (P.splits == 1 || fits_a_grid((rows + 3) / 4, 256));
 }
 
@@ -189,6 +215,130 @@ int check_maxsim(const void* Q, int nq, int T, int d, int dt, const void* docs, 
 }
 
 int hip(hipError_t e) { return e == hipSuccess ? COLBANDIT_OK : COLBANDIT_ERR_HIP; }
+
+int attention(const colbandit_attn* a, AttnArgs& A, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    if (A.total_q && (!out || !lse)) return COLBANDIT_ERR_NULL;
+    if (misaligned(out) || misaligned(lse, 4)) return COLBANDIT_ERR_ALIGNMENT;
+    const AttnPlan P = plan_attention(A, a->d, a->dt, false);
+    if (!launchable(A, P)) return COLBANDIT_ERR_UNSUPPORTED;
+    const int rc = workspace_ok(workspace, workspace_bytes, P.bytes);
+    if (rc) return rc;
+    const auto launch = A.windowed ? (a->dt == COLBANDIT_BF16 ? launch_attention_window_bf16 : launch_attention_window_f32)
+                                   : (a->dt == COLBANDIT_BF16 ? launch_attention_bf16 : launch_attention_f32);
+    return hip(launch(A, P, out, lse, (char*)workspace, (hipStream_t)stream));
+}
+
+int attention_backward(const colbandit_attn* a, AttnArgs& A, const AttnGrads& G, void* workspace, size_t workspace_bytes, void* stream) {
+    if (A.total_q && (!G.out || !G.lse || !G.dout || !G.dq)) return COLBANDIT_ERR_NULL;
+    if (A.total_k && (!G.dk || !G.dv)) return COLBANDIT_ERR_NULL;
+    if (A.bias && !G.dbias) return COLBANDIT_ERR_NULL;
+    if (misaligned(G.out) || misaligned(G.dout) || misaligned(G.dq) || misaligned(G.dk) || misaligned(G.dv) || misaligned(G.lse, 4) ||
+        misaligned(G.dbias, a->dt == COLBANDIT_BF16 ? 2 : 4))
+        return COLBANDIT_ERR_ALIGNMENT;
+    const AttnPlan P = plan_attention(A, a->d, a->dt, true);
+    if (!launchable(A, P)) return COLBANDIT_ERR_UNSUPPORTED;
+    const int rc = workspace_ok(workspace, workspace_bytes, P.bytes);
+    if (rc) return rc;
+    const auto launch = A.windowed ? (a->dt == COLBANDIT_BF16 ? launch_attention_window_backward_bf16 : launch_attention_window_backward_f32)
+                                   : (a->dt == COLBANDIT_BF16 ? launch_attention_backward_bf16 : launch_attention_backward_f32);
+    return hip(launch(A, P, G, (char*)workspace, (hipStream_t)stream));
+}
+
+bool is_type(int dt) { return dt == COLBANDIT_F32 || dt == COLBANDIT_BF16; }
+int64_t size_of(int dt) { return dt == COLBANDIT_BF16 ? 2 : 4; }
+
+constexpr int64_t kMostVocab = 1 << 24, kMostWidth = 1 << 16;
+int check_embedding(int64_t n, int64_t vocab, int64_t width, int64_t row, int dt, int other) {
+    if (n < 0 || vocab < 1 || width < 1 || !is_type(dt) || !is_type(other)) return COLBANDIT_ERR_SHAPE;
+    if (row < width) return COLBANDIT_ERR_SHAPE;
+    if (n > kMostRows || vocab > kMostVocab || width > kMostWidth || row > ((int64_t)1 << 32)) return COLBANDIT_ERR_UNSUPPORTED;
+    return COLBANDIT_OK;
+}
+
+int rotate_args(const colbandit_rotation* r, bool back, RotateArgs& A) {
+    if (!r) return COLBANDIT_ERR_NULL;
+    if (!is_type(r->dt) || r->rows < 0 || r->heads < 1 || r->kv_heads < 1 || r->d < 1) return COLBANDIT_ERR_SHAPE;
+    if (!(r->eps >= 0.f && r->eps < INFINITY)) return COLBANDIT_ERR_KNOB;
+    if (r->d != 32 && r->d != 64 && r->d != 96 && r->d != 128) return COLBANDIT_ERR_UNSUPPORTED;
+    if (r->rows > kMostRows || r->heads > 1 << 12) return COLBANDIT_ERR_UNSUPPORTED;
+    if (r->kv_heads > 1 << 12 || r->n_positions > ((int64_t)1 << 40)) return COLBANDIT_ERR_UNSUPPORTED;
+    if (r->table && r->n_positions < 1) return COLBANDIT_ERR_SHAPE;
+    if (r->rows && (!r->q || !r->k || (r->table && !r->positions))) return COLBANDIT_ERR_NULL;
+    const int64_t strides[] = {r->q_row, r->q_head, r->k_row, r->k_head};
+    for (int64_t s : strides) {
+        if (s < 0) return COLBANDIT_ERR_SHAPE;
+        if (s * size_of(r->dt) % 16) return COLBANDIT_ERR_ALIGNMENT;
+    }
+    if (misaligned(r->q) || misaligned(r->k) || misaligned(r->table) || misaligned(r->positions, 8) || misaligned(r->q_weight, 4) ||
+        misaligned(r->k_weight, 4))
+        return COLBANDIT_ERR_ALIGNMENT;
+    A = RotateArgs{};
+    A.q = r->q;
+    A.k = r->k;
+    A.q_row = r->q_row;
+    A.q_head = r->q_head;
+    A.k_row = r->k_row;
+    A.k_head = r->k_head;
+    A.q_weight = r->q_weight;
+    A.k_weight = r->k_weight;
+    A.table = r->table;
+    A.positions = r->positions;
+    A.rows = r->rows;
+    A.n_positions = r->n_positions;
+    A.heads = r->heads;
+    A.kv_heads = r->kv_heads;
+    A.near = r->interleaved != 0;
+    A.eps = r->eps;
+    return fits_a_grid(rotate_groups(A, r->d, back), 256) ? COLBANDIT_OK : COLBANDIT_ERR_UNSUPPORTED;
+}
+
+// Whether singular values from 0 to 1 stay within what the pieces of X, A and B can hold (4, 16 and 32 in size) over all steps of
+// s <- a s + b s^3 + c s^5.  A polynomial's extremes are where its derivative is zero, and at the ends.
+bool polynomial_holds(const float* k, int steps) {
+    const double a = k[0], b = k[1], c = k[2];
+    if (!isfinite(a) || !isfinite(b) || !isfinite(c)) return false;
+    double most = 1.0;
+    for (int s = 0; s < steps; ++s) {
+        most *= 1.0001;                              // (roundings)
+        if (most > 4.0) return false;
+        const double u1 = most * most;
+        auto square = [&](double u) { return fabs(b * u + c * u * u); };
+        double side = square(u1);
+        if (c != 0.0 && -b / (2 * c) > 0.0 && -b / (2 * c) < u1) side = fmax(side, square(-b / (2 * c)));
+        if (side > 32.0) return false;
+        auto value = [&](double u) { return fabs(sqrt(u) * (a + b * u + c * u * u)); };
+        double next = value(u1);
+        const double q[3] = {5 * c, 3 * b, a};       // of u = s^2
+        double roots[2];
+        int n = 0;
+        if (q[0] == 0.0) {
+            if (q[1] != 0.0) roots[n++] = -q[2] / q[1];
+        } else {
+            const double under = q[1] * q[1] - 4 * q[0] * q[2];
+            if (under >= 0.0) {
+                roots[n++] = (-q[1] + sqrt(under)) / (2 * q[0]);
+                roots[n++] = (-q[1] - sqrt(under)) / (2 * q[0]);
+            }
+        }
+        for (int i = 0; i < n; ++i)
+            if (roots[i] > 0.0 && roots[i] < u1) next = fmax(next, value(roots[i]));
+        most = next;
+    }
+    return most <= 4.0;
+}
+
+constexpr int64_t kMostSide = 1 << 14, kMostLength = 1 << 26;
+int check_matrices(int64_t n, const int64_t* rows, const int64_t* cols) {
+    if (!rows || !cols) return COLBANDIT_ERR_NULL;
+    if (n < 1) return COLBANDIT_ERR_SHAPE;
+    for (int64_t i = 0; i < n; ++i)
+        if (rows[i] < 0 || cols[i] < 0) return COLBANDIT_ERR_SHAPE;
+    for (int64_t i = 0; i < n; ++i) {
+        const int64_t m = rows[i] < cols[i] ? rows[i] : cols[i], longer = rows[i] < cols[i] ? cols[i] : rows[i];
+        if (m > kMostSide || longer > kMostLength) return COLBANDIT_ERR_UNSUPPORTED;
+    }
+    return ortho_launchable(n, rows, cols) ? COLBANDIT_OK : COLBANDIT_ERR_UNSUPPORTED;
+}
 
 }  // namespace
 
@@ -213,38 +363,140 @@ size_t colbandit_attention_workspace_bytes(const colbandit_attn* a, int backward
 
 int colbandit_attention(const colbandit_attn* a, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
     AttnArgs A;
-    int rc = attn_args(a, A);
-    if (rc) return rc;
-    if (A.total_q && (!out || !lse)) return COLBANDIT_ERR_NULL;
-    if (misaligned(out) || misaligned(lse, 4)) return COLBANDIT_ERR_ALIGNMENT;
-    const AttnPlan P = plan_attention(A, a->d, a->dt, false);
-    if (!launchable(A, P)) return COLBANDIT_ERR_UNSUPPORTED;
-    rc = workspace_ok(workspace, workspace_bytes, P.bytes);
-    if (rc) return rc;
-    const hipStream_t st = (hipStream_t)stream;
-    return hip(a->dt == COLBANDIT_BF16 ? launch_attention_bf16(A, P, out, lse, (char*)workspace, st)
-                                       : launch_attention_f32(A, P, out, lse, (char*)workspace, st));
+    const int rc = attn_args(a, A);
+    return rc ? rc : attention(a, A, out, lse, workspace, workspace_bytes, stream);
 }
 
 int colbandit_attention_backward(const colbandit_attn* a, const void* out, const float* lse, const void* dout, void* dq, void* dk,
                                  void* dv, void* dbias, void* workspace, size_t workspace_bytes, void* stream) {
     AttnArgs A;
+    const int rc = attn_args(a, A);
+    return rc ? rc : attention_backward(a, A, {out, dout, lse, dq, dk, dv, dbias}, workspace, workspace_bytes, stream);
+}
+
+size_t colbandit_sizeof_window(void) { return sizeof(colbandit_window); }
+
+size_t colbandit_attention_window_workspace_bytes(const colbandit_attn* a, const colbandit_window* w, int backward) {
+    AttnArgs A;
+    if (attn_args(a, A) || window_args(w, A)) return 0;
+    return plan_attention(A, a->d, a->dt, backward != 0).bytes;
+}
+
+int colbandit_attention_window(const colbandit_attn* a, const colbandit_window* w, void* out, float* lse, void* workspace,
+                               size_t workspace_bytes, void* stream) {
+    AttnArgs A;
     int rc = attn_args(a, A);
+    if (!rc) rc = window_args(w, A);
+    return rc ? rc : attention(a, A, out, lse, workspace, workspace_bytes, stream);
+}
+
+int colbandit_attention_window_backward(const colbandit_attn* a, const colbandit_window* w, const void* out, const float* lse, const void* dout,
+                                        void* dq, void* dk, void* dv, void* dbias, void* workspace, size_t workspace_bytes, void* stream) {
+    AttnArgs A;
+    int rc = attn_args(a, A);
+    if (!rc) rc = window_args(w, A);
+    return rc ? rc : attention_backward(a, A, {out, dout, lse, dq, dk, dv, dbias}, workspace, workspace_bytes, stream);
+}
+
+int colbandit_embedding(const void* table, colbandit_dtype table_dt, int64_t table_row, const int64_t* tokens, int64_t n, int64_t vocab,
+                        int64_t width, float scale, void* out, colbandit_dtype out_dt, void* stream) {
+    const int rc = check_embedding(n, vocab, width, table_row, table_dt, out_dt);
     if (rc) return rc;
-    if (A.total_q && (!out || !lse || !dout || !dq)) return COLBANDIT_ERR_NULL;
-    if (A.total_k && (!dk || !dv)) return COLBANDIT_ERR_NULL;
-    if (A.bias && !dbias) return COLBANDIT_ERR_NULL;
-    if (misaligned(out) || misaligned(dout) || misaligned(dq) || misaligned(dk) || misaligned(dv) || misaligned(lse, 4) ||
-        misaligned(dbias, a->dt == COLBANDIT_BF16 ? 2 : 4))
+    if (!table || (n && (!tokens || !out))) return COLBANDIT_ERR_NULL;
+    if (!embedding_launchable(n, vocab, width, embedding_is_wide(table, table_dt, table_row, out, out_dt, width), false)) return COLBANDIT_ERR_UNSUPPORTED;
+    if (misaligned(table, size_of(table_dt)) || misaligned(out, size_of(out_dt)) || misaligned(tokens, 8)) return COLBANDIT_ERR_ALIGNMENT;
+    return hip(launch_embedding(table, table_dt, table_row, tokens, n, vocab, width, scale, out, out_dt, (hipStream_t)stream));
+}
+
+size_t colbandit_embedding_workspace_bytes(int64_t n, int64_t vocab, int64_t width) {
+    return check_embedding(n, vocab, width, width, COLBANDIT_F32, COLBANDIT_F32) ? 0 : embedding_workspace_bytes(n, vocab, width);
+}
+
+int colbandit_embedding_backward(const void* dout, colbandit_dtype dout_dt, int64_t dout_row, const int64_t* tokens, int64_t n, int64_t vocab,
+                                 int64_t width, float scale, void* dtable, colbandit_dtype table_dt, void* workspace, size_t workspace_bytes,
+                                 void* stream) {
+    int rc = check_embedding(n, vocab, width, dout_row, table_dt, dout_dt);
+    if (rc) return rc;
+    if (!dtable || (n && (!tokens || !dout))) return COLBANDIT_ERR_NULL;
+    if (!embedding_launchable(n, vocab, width, embedding_is_wide(dout, dout_dt, dout_row, dtable, table_dt, width), true))
+        return COLBANDIT_ERR_UNSUPPORTED;
+    if (misaligned(dtable, size_of(table_dt)) || misaligned(dout, size_of(dout_dt)) || misaligned(tokens, 8)) return COLBANDIT_ERR_ALIGNMENT;
+    rc = workspace_ok(workspace, workspace_bytes, embedding_workspace_bytes(n, vocab, width));
+    if (rc) return rc;
+    return hip(launch_embedding_backward(dout, dout_dt, dout_row, tokens, n, vocab, width, scale, dtable, table_dt, (char*)workspace,
+                                         (hipStream_t)stream));
+}
+
+int colbandit_rotary_table(int64_t n_positions, int d, double base, float* table) {
+    if (!table) return COLBANDIT_ERR_NULL;
+    if (n_positions < 1 || d < 2 || d % 2) return COLBANDIT_ERR_SHAPE;
+    if (!(base > 0.0 && base < INFINITY)) return COLBANDIT_ERR_KNOB;
+    for (int i = 0; i < d / 2; ++i) {
+        const double frequency = pow(base, -2.0 * i / d);
+        for (int64_t p = 0; p < n_positions; ++p) {
+            float* to = table + (p * (d / 2) + i) * 2;
+            to[0] = (float)cos((double)p * frequency);
+            to[1] = (float)sin((double)p * frequency);
+        }
+    }
+    return COLBANDIT_OK;
+}
+
+size_t colbandit_sizeof_rotation(void) { return sizeof(colbandit_rotation); }
+
+int colbandit_norm_rotate(const colbandit_rotation* r, void* q_out, void* k_out, void* stream) {
+    RotateArgs A;
+    const int rc = rotate_args(r, false, A);
+    if (rc) return rc;
+    if (A.rows && (!q_out || !k_out)) return COLBANDIT_ERR_NULL;
+    if (misaligned(q_out) || misaligned(k_out)) return COLBANDIT_ERR_ALIGNMENT;
+    A.q_to = q_out;
+    A.k_to = k_out;
+    return hip(launch_rotate(A, r->d, r->dt, (hipStream_t)stream));
+}
+
+size_t colbandit_norm_rotate_workspace_bytes(const colbandit_rotation* r) {
+    RotateArgs A;
+    return rotate_args(r, true, A) ? 0 : rotate_workspace_bytes(A, r->d);
+}
+
+int colbandit_norm_rotate_backward(const colbandit_rotation* r, const void* dq_out, const void* dk_out, void* dq, void* dk, float* dq_weight,
+                                   float* dk_weight, void* workspace, size_t workspace_bytes, void* stream) {
+    RotateArgs A;
+    int rc = rotate_args(r, true, A);
+    if (rc) return rc;
+    if (A.rows && (!dq_out || !dk_out || !dq || !dk)) return COLBANDIT_ERR_NULL;
+    if (misaligned(dq_out) || misaligned(dk_out) || misaligned(dq) || misaligned(dk) || misaligned(dq_weight, 4) || misaligned(dk_weight, 4))
         return COLBANDIT_ERR_ALIGNMENT;
-    const AttnPlan P = plan_attention(A, a->d, a->dt, true);
-    if (!launchable(A, P)) return COLBANDIT_ERR_UNSUPPORTED;
-    rc = workspace_ok(workspace, workspace_bytes, P.bytes);
+    rc = workspace_ok(workspace, workspace_bytes, rotate_workspace_bytes(A, r->d));
     if (rc) return rc;
-    const AttnGrads G = {out, dout, lse, dq, dk, dv, dbias};
-    const hipStream_t st = (hipStream_t)stream;
-    return hip(a->dt == COLBANDIT_BF16 ? launch_attention_backward_bf16(A, P, G, (char*)workspace, st)
-                                       : launch_attention_backward_f32(A, P, G, (char*)workspace, st));
+    A.dq_out = dq_out;
+    A.dk_out = dk_out;
+    A.q_to = dq;
+    A.k_to = dk;
+    A.part = (float*)workspace;
+    return hip(launch_rotate_backward(A, r->d, r->dt, dq_weight, dk_weight, (hipStream_t)stream));
+}
+
+size_t colbandit_orthogonalise_workspace_bytes(int64_t n_matrices, const int64_t* rows, const int64_t* cols) {
+    return check_matrices(n_matrices, rows, cols) ? 0 : ortho_workspace_bytes(n_matrices, rows, cols);
+}
+
+int colbandit_orthogonalise(int64_t n_matrices, const void* const* in, void* const* out, const int64_t* rows, const int64_t* cols,
+                            const int32_t* dts, int steps, const float* coefficients, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!in || !out || !dts || !coefficients) return COLBANDIT_ERR_NULL;
+    int rc = check_matrices(n_matrices, rows, cols);
+    if (rc) return rc;
+    if (steps < 1) return COLBANDIT_ERR_SHAPE;
+    if (steps > 64 || !polynomial_holds(coefficients, steps)) return COLBANDIT_ERR_KNOB;
+    for (int64_t i = 0; i < n_matrices; ++i) {
+        if (!is_type(dts[i])) return COLBANDIT_ERR_SHAPE;
+        if (rows[i] && cols[i] && (!in[i] || !out[i])) return COLBANDIT_ERR_NULL;
+        if (misaligned(in[i], size_of(dts[i])) || misaligned(out[i], size_of(dts[i]))) return COLBANDIT_ERR_ALIGNMENT;
+    }
+    rc = workspace_ok(workspace, workspace_bytes, ortho_workspace_bytes(n_matrices, rows, cols));
+    if (rc) return rc;
+    return hip(launch_ortho(n_matrices, in, out, rows, cols, dts, steps, coefficients, (char*)workspace, (hipStream_t)stream));
 }
 
 int colbandit_maxsim_scores(const void* Q, int n_queries, int T, int d, colbandit_dtype dt, const void* docs, const int64_t* offsets,

@@ -2,8 +2,8 @@
 
 The `colbandit_*` functions marshal arguments only, as those of `binding` do: torch supplies device
 memory and the current stream, every step runs in the library's HIP kernels, and there is no
-fallback.  Tensors must live on the current device.  `attention`, `contrastive_maxsim` and
-`clip_gradients_` are the same operators as parts of a torch program.
+fallback.  Tensors must live on the current device.  `embedding`, `norm_rotate`, `attention`, `contrastive_maxsim`,
+`clip_gradients_` and `orthogonal_step_` are the same operators as parts of a torch program.
 """
 from __future__ import annotations
 
@@ -20,6 +20,11 @@ EXPORTS = [
     "colbandit_sizeof_attn", "colbandit_bias_buckets", "colbandit_attention_workspace_bytes", "colbandit_attention",
     "colbandit_attention_backward", "colbandit_maxsim_scores", "colbandit_contrastive_loss", "colbandit_maxsim_backward",
     "colbandit_clip_workspace_bytes", "colbandit_clip_gradients",
+    "colbandit_sizeof_window", "colbandit_attention_window_workspace_bytes", "colbandit_attention_window",
+    "colbandit_attention_window_backward", "colbandit_embedding", "colbandit_embedding_workspace_bytes",
+    "colbandit_embedding_backward", "colbandit_sizeof_rotation", "colbandit_rotary_table", "colbandit_norm_rotate",
+    "colbandit_norm_rotate_workspace_bytes", "colbandit_norm_rotate_backward", "colbandit_orthogonalise_workspace_bytes",
+    "colbandit_orthogonalise",
 ]
 
 _DTYPES = {torch.bfloat16: BF16, torch.float32: F32}
@@ -36,6 +41,18 @@ class ColbanditAttn(ctypes.Structure):
                 ("keep", ctypes.c_void_p), ("bias", ctypes.c_void_p)]
 
 
+class ColbanditWindow(ctypes.Structure):
+    _fields_ = [("before", ctypes.c_int64), ("after", ctypes.c_int64), ("sinks", ctypes.c_int64)]
+
+
+class ColbanditRotation(ctypes.Structure):
+    _fields_ = [("dt", ctypes.c_int), ("heads", ctypes.c_int), ("kv_heads", ctypes.c_int), ("d", ctypes.c_int),
+                ("interleaved", ctypes.c_int), ("eps", ctypes.c_float), ("rows", ctypes.c_int64), ("n_positions", ctypes.c_int64),
+                ("q", ctypes.c_void_p), ("k", ctypes.c_void_p),
+                ("q_row", ctypes.c_int64), ("q_head", ctypes.c_int64), ("k_row", ctypes.c_int64), ("k_head", ctypes.c_int64),
+                ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("table", ctypes.c_void_p), ("positions", ctypes.c_void_p)]
+
+
 _lib = None
 
 
@@ -45,7 +62,8 @@ def lib():
     if _lib is None:
         L = binding.lib()
         vp, i, i64, sz, f = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_size_t, ctypes.c_float
-        attn = ctypes.POINTER(ColbanditAttn)
+        d = ctypes.c_double
+        attn, window, rotation = (ctypes.POINTER(t) for t in (ColbanditAttn, ColbanditWindow, ColbanditRotation))
         for name, res, args in [
                 ("colbandit_sizeof_attn", sz, []),
                 ("colbandit_bias_buckets", i, [i, i, i, vp]),
@@ -56,10 +74,25 @@ def lib():
                 ("colbandit_contrastive_loss", i, [vp, i, i64, vp, f, vp, vp, vp]),
                 ("colbandit_maxsim_backward", i, [vp, vp, vp, i, i, i, i, vp, vp, i64, i64, vp, vp, vp]),
                 ("colbandit_clip_workspace_bytes", sz, [i64, vp]),
-                ("colbandit_clip_gradients", i, [i64, vp, vp, vp, vp, f, vp, vp, sz, vp])]:
+                ("colbandit_clip_gradients", i, [i64, vp, vp, vp, vp, f, vp, vp, sz, vp]),
+                ("colbandit_sizeof_window", sz, []),
+                ("colbandit_attention_window_workspace_bytes", sz, [attn, window, i]),
+                ("colbandit_attention_window", i, [attn, window, vp, vp, vp, sz, vp]),
+                ("colbandit_attention_window_backward", i, [attn, window, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
+                ("colbandit_embedding", i, [vp, i, i64, vp, i64, i64, i64, f, vp, i, vp]),
+                ("colbandit_embedding_workspace_bytes", sz, [i64, i64, i64]),
+                ("colbandit_embedding_backward", i, [vp, i, i64, vp, i64, i64, i64, f, vp, i, vp, sz, vp]),
+                ("colbandit_sizeof_rotation", sz, []),
+                ("colbandit_rotary_table", i, [i64, i, d, vp]),
+                ("colbandit_norm_rotate", i, [rotation, vp, vp, vp]),
+                ("colbandit_norm_rotate_workspace_bytes", sz, [rotation]),
+                ("colbandit_norm_rotate_backward", i, [rotation, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
+                ("colbandit_orthogonalise_workspace_bytes", sz, [i64, vp, vp]),
+                ("colbandit_orthogonalise", i, [i64, vp, vp, vp, vp, vp, i, vp, vp, sz, vp])]:
             fn = getattr(L, name)
             fn.restype, fn.argtypes = res, args
-        if L.colbandit_sizeof_attn() != ctypes.sizeof(ColbanditAttn):
+        if (L.colbandit_sizeof_attn(), L.colbandit_sizeof_window(), L.colbandit_sizeof_rotation()) != tuple(
+                ctypes.sizeof(t) for t in (ColbanditAttn, ColbanditWindow, ColbanditRotation)):
             raise ImportError("libcolbandit.so was built from a different colbandit_train.h: rebuild it")
         _lib = L
     return _lib
@@ -142,6 +175,16 @@ def _attn(q, k, v, q_offsets, k_offsets, causal, scale, keep, bias, max_distance
         q.stride(0), q.stride(1), k.stride(0), k.stride(1), v.stride(0), v.stride(1), _ptr(keep), _ptr(bias))
 
 
+def _window(window, sinks):
+    """(before, after) and a number of first keys as the library takes them; None: all keys."""
+    if window is None:
+        if sinks:
+            raise ValueError("sinks come with a window")
+        return None
+    before, after = window
+    return ColbanditWindow(before, after, sinks)
+
+
 def _dense(t, shape, dtype, what):
     if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
         raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
@@ -149,11 +192,13 @@ def _dense(t, shape, dtype, what):
 
 
 def colbandit_attention(q, k, v, q_offsets, k_offsets=None, *, causal=False, scale=None, keep=None, bias=None,
-                        max_distance=128, workspace=None, out=None):
-    """Attention over packed sequences.  q [total_q, heads, d], k and v [total_k, kv_heads, d] (any
+                        max_distance=128, window=None, sinks=0, workspace=None, out=None):
+    """Attention over packed sequences, of all keys or, with window=(before, after), of those up to so far from a row's
+    position and the first `sinks` of its sequence.  q [total_q, heads, d], k and v [total_k, kv_heads, d] (any
     row and head strides), offsets int64 [n+1]; `k_offsets` None: the queries' own; rows behind the last
     sequence get zeros.  `out`: tensors to write, as this returns them.  Returns dict(out [total_q, heads, d], lse float32
     [heads, total_q])."""
+    w = _window(window, sinks)
     a = _attn(q, k, v, q_offsets, k_offsets, causal, scale, keep, bias, max_distance)
     L = lib()
     o, lse = (out["out"], out["lse"]) if out else (None, None)
@@ -161,15 +206,20 @@ def colbandit_attention(q, k, v, q_offsets, k_offsets=None, *, causal=False, sca
     lse = q.new_empty((q.shape[1], q.shape[0]), dtype=torch.float32) if lse is None else \
         _dense(lse, (q.shape[1], q.shape[0]), torch.float32, "lse")
     _on_device(o, lse)
+    if w is not None:
+        ws, nb = _workspace(workspace, L.colbandit_attention_window_workspace_bytes(a, w, 0), q.device)
+        _check(L.colbandit_attention_window(a, w, o.data_ptr(), lse.data_ptr(), _ptr(ws), nb, _stream()), "colbandit_attention_window")
+        return {"out": o, "lse": lse}
     ws, nb = _workspace(workspace, L.colbandit_attention_workspace_bytes(a, 0), q.device)
     _check(L.colbandit_attention(a, o.data_ptr(), lse.data_ptr(), _ptr(ws), nb, _stream()), "colbandit_attention")
     return {"out": o, "lse": lse}
 
 
 def colbandit_attention_backward(dout, q, k, v, out, lse, q_offsets, k_offsets=None, *, causal=False, scale=None,
-                                 keep=None, bias=None, max_distance=128, workspace=None):
+                                 keep=None, bias=None, max_distance=128, window=None, sinks=0, workspace=None):
     """Gradients of colbandit_attention's inputs from that of its output.  Returns dict(dq, dk, dv,
     dbias), dense, `dbias` None without a bias."""
+    w = _window(window, sinks)
     a = _attn(q, k, v, q_offsets, k_offsets, causal, scale, keep, bias, max_distance)
     L = lib()
     _dense(out, q.shape, q.dtype, "out")
@@ -178,11 +228,126 @@ def colbandit_attention_backward(dout, q, k, v, out, lse, q_offsets, k_offsets=N
     _on_device(out, lse, dout)
     dq, dk, dv = q.new_empty(q.shape), k.new_empty(k.shape), k.new_empty(k.shape)
     dbias = None if bias is None else torch.empty_like(bias)
+    if w is not None:
+        ws, nb = _workspace(workspace, L.colbandit_attention_window_workspace_bytes(a, w, 1), q.device)
+        _check(L.colbandit_attention_window_backward(a, w, out.data_ptr(), lse.data_ptr(), dout.data_ptr(), dq.data_ptr(), dk.data_ptr(),
+                                                     dv.data_ptr(), _ptr(dbias), _ptr(ws), nb, _stream()),
+               "colbandit_attention_window_backward")
+        return {"dq": dq, "dk": dk, "dv": dv, "dbias": dbias}
     ws, nb = _workspace(workspace, L.colbandit_attention_workspace_bytes(a, 1), q.device)
     _check(L.colbandit_attention_backward(a, out.data_ptr(), lse.data_ptr(), dout.data_ptr(), dq.data_ptr(), dk.data_ptr(),
                                           dv.data_ptr(), _ptr(dbias), _ptr(ws), nb, _stream()),
            "colbandit_attention_backward")
     return {"dq": dq, "dk": dk, "dv": dv, "dbias": dbias}
+
+
+def _rows_of(t, what):
+    if t.dtype not in _DTYPES:
+        raise TypeError(f"{what} must be float32 or bfloat16")
+    if t.dim() != 2 or t.shape[1] < 1 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        raise ValueError(f"{what} is [rows, width] with consecutive values in rows that do not overlap")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _tokens(tokens):
+    if tokens.dtype != torch.int64 or tokens.dim() != 1 or not tokens.is_contiguous():
+        raise ValueError("tokens must be a contiguous int64 vector")
+
+
+def colbandit_embedding(table, tokens, *, scale=1.0, dtype=None, out=None):
+    """Rows of `table` [vocab, width] for `tokens` int64 [n], times scale; zeros for tokens outside of the table (padding).  `dtype`: of
+    the rows, where it is not the table's; `out`: a tensor to write.  Returns dict(out [n, width])."""
+    row = _rows_of(table, "table")
+    _tokens(tokens)
+    n, (vocab, width) = tokens.shape[0], table.shape
+    dtype = table.dtype if dtype is None else dtype
+    if dtype not in _DTYPES:
+        raise TypeError("rows must be float32 or bfloat16")
+    out = table.new_empty((n, width), dtype=dtype) if out is None else _dense(out, (n, width), dtype, "out")
+    _on_device(table, tokens, out)
+    _check(lib().colbandit_embedding(table.data_ptr(), _DTYPES[table.dtype], row, tokens.data_ptr(), n, vocab, width, scale,
+                                     out.data_ptr(), _DTYPES[dtype], _stream()), "colbandit_embedding")
+    return {"out": out}
+
+
+def colbandit_embedding_backward(dout, tokens, vocab, *, scale=1.0, dtype=None, out=None, workspace=None):
+    """Gradient of a table of `vocab` rows from that of the rows that were looked up, in the order of the tokens.  `dtype`: of the
+    table; `out`: a tensor to write.  Returns dict(dtable [vocab, width])."""
+    row = _rows_of(dout, "dout")
+    _tokens(tokens)
+    n, width = dout.shape
+    if tokens.shape[0] != n:
+        raise ValueError("dout has a row for each token")
+    dtype = dout.dtype if dtype is None else dtype
+    if dtype not in _DTYPES:
+        raise TypeError("a table is float32 or bfloat16")
+    L = lib()
+    out = dout.new_empty((vocab, width), dtype=dtype) if out is None else _dense(out, (vocab, width), dtype, "dtable")
+    _on_device(dout, tokens, out)
+    ws, nb = _workspace(workspace, L.colbandit_embedding_workspace_bytes(n, vocab, width), dout.device)
+    _check(L.colbandit_embedding_backward(dout.data_ptr(), _DTYPES[dout.dtype], row, tokens.data_ptr(), n, vocab, width, scale,
+                                          out.data_ptr(), _DTYPES[dtype], _ptr(ws), nb, _stream()), "colbandit_embedding_backward")
+    return {"dtable": out}
+
+
+def colbandit_rotary_table(n_positions, d, base=10000.0, device=None) -> torch.Tensor:
+    """Cosine and sine of position * base^(-2i/d), float32 [n_positions, d/2, 2] (computed by the library on the host, in 64
+    bits), on the current device or `device`."""
+    table = torch.empty((n_positions, d // 2, 2), dtype=torch.float32)
+    _check(lib().colbandit_rotary_table(n_positions, d, base, table.data_ptr()), "colbandit_rotary_table")
+    return table.to(torch.device("cuda", torch.cuda.current_device()) if device is None else device)
+
+
+def _rotation(q, k, positions, table, q_weight, k_weight, eps, interleaved):
+    if q.dtype not in _DTYPES or k.dtype != q.dtype:
+        raise TypeError("q and k must be float32 or bfloat16, both of one type")
+    if q.dim() != 3 or k.dim() != 3 or q.shape[0] != k.shape[0] or q.shape[2] != k.shape[2]:
+        raise ValueError("q is [rows, heads, d], k [rows, kv_heads, d]")
+    if q.stride(2) != 1 or k.stride(2) != 1:
+        raise ValueError("the values of a row and head must be consecutive")
+    d = q.shape[2]
+    for w in (q_weight, k_weight):
+        if w is not None:
+            _dense(w, (d,), torch.float32, "a weight")
+    if table is not None:
+        if positions is None:
+            raise ValueError("a rotation needs positions")
+        _dense(table, (table.shape[0], d // 2, 2), torch.float32, "the table")
+        _dense(positions, q.shape[:1], torch.int64, "positions")
+    _on_device(q, k, positions, table, q_weight, k_weight)
+    return ColbanditRotation(_DTYPES[q.dtype], q.shape[1], k.shape[1], d, 1 if interleaved else 0, eps, q.shape[0],
+                             0 if table is None else table.shape[0], q.data_ptr(), k.data_ptr(), q.stride(0), q.stride(1),
+                             k.stride(0), k.stride(1), _ptr(q_weight), _ptr(k_weight), _ptr(table),
+                             None if table is None else positions.data_ptr())
+
+
+def colbandit_norm_rotate(q, k, *, positions=None, table=None, q_weight=None, k_weight=None, eps=1e-6, interleaved=False, out=None):
+    """q [rows, heads, d] and k [rows, kv_heads, d] (any row and head strides), each head divided by its root mean square, times
+    the weights float32 [d], and rotated by `table` (colbandit_rotary_table) at `positions` int64 [rows]; rows whose position is none
+    of the table's get zeros.  `table` None: no rotation.  `out`: tensors to write, as this returns them.  Returns dict(q, k), dense."""
+    r = _rotation(q, k, positions, table, q_weight, k_weight, eps, interleaved)
+    q_out, k_out = (q.new_empty(q.shape), k.new_empty(k.shape)) if out is None else (
+        _dense(out["q"], q.shape, q.dtype, "q"), _dense(out["k"], k.shape, k.dtype, "k"))
+    _on_device(q_out, k_out)
+    _check(lib().colbandit_norm_rotate(r, q_out.data_ptr(), k_out.data_ptr(), _stream()), "colbandit_norm_rotate")
+    return {"q": q_out, "k": k_out}
+
+
+def colbandit_norm_rotate_backward(dq_out, dk_out, q, k, *, positions=None, table=None, q_weight=None, k_weight=None, eps=1e-6,
+                                   interleaved=False, workspace=None):
+    """Gradients of colbandit_norm_rotate's inputs from those of its outputs.  Returns dict(dq, dk, dq_weight, dk_weight), the last two
+    also where there are no weights."""
+    _dense(dq_out, q.shape, q.dtype, "dq_out")
+    _dense(dk_out, k.shape, k.dtype, "dk_out")
+    r = _rotation(q, k, positions, table, q_weight, k_weight, eps, interleaved)
+    _on_device(dq_out, dk_out)
+    L = lib()
+    dq, dk = q.new_empty(q.shape), k.new_empty(k.shape)
+    dw = q.new_empty((2, q.shape[2]), dtype=torch.float32)
+    ws, nb = _workspace(workspace, L.colbandit_norm_rotate_workspace_bytes(r), q.device)
+    _check(L.colbandit_norm_rotate_backward(r, dq_out.data_ptr(), dk_out.data_ptr(), dq.data_ptr(), dk.data_ptr(), dw[0].data_ptr(),
+                                            dw[1].data_ptr(), _ptr(ws), nb, _stream()), "colbandit_norm_rotate_backward")
+    return {"dq": dq, "dk": dk, "dq_weight": dw[0], "dk_weight": dw[1]}
 
 
 def _maxsim(Q, docs, offsets):
@@ -259,6 +424,34 @@ def colbandit_clip_gradients(grads, max_norm, out=None, workspace=None):
     return {"norm": norm, "grads": to}
 
 
+POLYNOMIAL = (3.4445, -4.7750, 2.0315)               # takes singular values of any size to between 0.7 and 1.2 in five steps
+
+
+def colbandit_orthogonalise(matrices, *, steps=5, coefficients=POLYNOMIAL, out=None, workspace=None):
+    """Each of `matrices` (a list of contiguous 2-d float32 or bfloat16 tensors) with its singular values brought near to one by
+    `steps` of s <- a s + b s^3 + c s^5, after a division by its Frobenius norm.  Into `out` (a list alike; it may be `matrices`), or
+    new tensors.  Returns dict(out)."""
+    matrices = list(matrices)
+    to = [torch.empty_like(m) for m in matrices] if out is None else list(out)
+    if not matrices or len(to) != len(matrices):
+        raise ValueError("matrices must be a list of tensors, and out one of as many")
+    for m, o in zip(matrices, to):
+        if m.dtype not in _DTYPES or o.dtype != m.dtype:
+            raise TypeError("matrices must be float32 or bfloat16, and outputs of their types")
+        if m.dim() != 2 or not m.is_contiguous() or not o.is_contiguous() or o.shape != m.shape:
+            raise ValueError("matrices and outputs must be contiguous and two-dimensional, and outputs of their shapes")
+    _on_device(*matrices, *to)
+    n = len(matrices)
+    pointers, sizes = ctypes.c_void_p * n, ctypes.c_int64 * n
+    rows, cols = sizes(*[m.shape[0] for m in matrices]), sizes(*[m.shape[1] for m in matrices])
+    L = lib()
+    ws, nb = _workspace(workspace, L.colbandit_orthogonalise_workspace_bytes(n, rows, cols), matrices[0].device)
+    _check(L.colbandit_orthogonalise(n, pointers(*[m.data_ptr() for m in matrices]), pointers(*[o.data_ptr() for o in to]), rows, cols,
+                                     (ctypes.c_int32 * n)(*[_DTYPES[m.dtype] for m in matrices]), steps,
+                                     (ctypes.c_float * 3)(*coefficients), _ptr(ws), nb, _stream()), "colbandit_orthogonalise")
+    return {"out": to}
+
+
 # ---- as parts of a torch program ---------------------------------------------------------------------
 
 
@@ -298,10 +491,59 @@ class _Attention(torch.autograd.Function):
         return *_first_order((g["dq"], g["dk"], g["dv"], g["dbias"]), q, k, v, bias, dout), None, None, None, None
 
 
-def attention(q, k, v, q_offsets, k_offsets=None, *, causal=False, scale=None, keep=None, bias=None, max_distance=128):
+def attention(q, k, v, q_offsets, k_offsets=None, *, causal=False, scale=None, keep=None, bias=None, max_distance=128, window=None,
+              sinks=0):
     """colbandit_attention's output, differentiable in q, k, v and bias (once: second-order gradients are an error)."""
-    return _Attention.apply(q, k, v, bias, q_offsets, k_offsets, keep,
-                            dict(causal=causal, scale=scale, max_distance=max_distance))
+    how = dict(causal=causal, scale=scale, max_distance=max_distance)
+    if window is not None or sinks:
+        how.update(window=window, sinks=sinks)
+    return _Attention.apply(q, k, v, bias, q_offsets, k_offsets, keep, how)
+
+
+class _Embedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, table, tokens, scale, dtype):
+        ctx.save_for_backward(tokens)
+        ctx.how = (table.shape[0], scale, table.dtype)
+        return colbandit_embedding(table, tokens, scale=scale, dtype=dtype)["out"]
+
+    @staticmethod
+    def backward(ctx, dout):
+        tokens, = ctx.saved_tensors
+        vocab, scale, dtype = ctx.how
+        if dout.dim() != 2 or dout.stride(1) != 1 or dout.stride(0) < dout.shape[1]:
+            dout = dout.contiguous()
+        g = colbandit_embedding_backward(dout, tokens, vocab, scale=scale, dtype=dtype)["dtable"]
+        return *_first_order((g,), dout), None, None, None
+
+
+def embedding(table, tokens, *, scale=1.0, dtype=None):
+    """colbandit_embedding's rows, differentiable in the table (once: second-order gradients are an error).  `tokens` of any shape:
+    the rows have it, and the width as one more dimension."""
+    out = _Embedding.apply(table, tokens.reshape(-1).contiguous(), float(scale), dtype)
+    return out if tokens.dim() == 1 else out.view(*tokens.shape, table.shape[1])
+
+
+class _NormRotate(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, q_weight, k_weight, positions, table, how):
+        r = colbandit_norm_rotate(q, k, positions=positions, table=table, q_weight=q_weight, k_weight=k_weight, **how)
+        ctx.save_for_backward(q, k, q_weight, k_weight, positions, table)
+        ctx.how = how
+        return r["q"], r["k"]
+
+    @staticmethod
+    def backward(ctx, dq, dk):
+        q, k, q_weight, k_weight, positions, table = ctx.saved_tensors
+        g = colbandit_norm_rotate_backward(dq.contiguous(), dk.contiguous(), q, k, positions=positions, table=table, q_weight=q_weight,
+                                           k_weight=k_weight, **ctx.how)
+        return *_first_order((g["dq"], g["dk"], None if q_weight is None else g["dq_weight"],
+                              None if k_weight is None else g["dk_weight"]), q, k, q_weight, k_weight, dq, dk), None, None, None
+
+
+def norm_rotate(q, k, *, positions=None, table=None, q_weight=None, k_weight=None, eps=1e-6, interleaved=False):
+    """colbandit_norm_rotate's (q, k), differentiable in q, k and the weights (once: second-order gradients are an error)."""
+    return _NormRotate.apply(q, k, q_weight, k_weight, positions, table, dict(eps=eps, interleaved=interleaved))
 
 
 class _ContrastiveMaxSim(torch.autograd.Function):
@@ -334,3 +576,23 @@ def clip_gradients_(parameters, max_norm):
     if not grads:
         return torch.zeros((), device=parameters[0].device if parameters else None)
     return colbandit_clip_gradients(grads, float(max_norm))["norm"]
+
+
+def orthogonal_step_(parameters, momenta, rate, momentum=0.95, steps=5, coefficients=POLYNOMIAL):
+    """One step of descent along orthogonalised momenta, for 2-d parameters: of each that has a gradient the momentum becomes
+    momentum * itself + gradient, and the parameter goes down `rate` times sqrt(max(1, rows / columns)) times
+    colbandit_orthogonalise of gradient + momentum * itself.  `momenta`: a dict of the parameters' momenta, which this fills."""
+    parameters = [p for p in dict.fromkeys(parameters) if p.grad is not None]
+    if not parameters:
+        return
+    updates = []
+    with torch.no_grad():
+        for p in parameters:
+            m = momenta.get(p)
+            if m is None:
+                m = momenta[p] = torch.zeros_like(p, memory_format=torch.contiguous_format)
+            m.mul_(momentum).add_(p.grad)
+            updates.append(torch.add(p.grad, m, alpha=momentum).contiguous())
+        colbandit_orthogonalise(updates, steps=steps, coefficients=coefficients, out=updates)
+        for p, u in zip(parameters, updates):
+            p.sub_(u, alpha=rate * math.sqrt(max(1.0, p.shape[0] / p.shape[1])))
