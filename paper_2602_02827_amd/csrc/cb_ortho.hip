@@ -21,13 +21,15 @@ constexpr float kScaleX = 8192.f, kScaleA = 2048.f, kScaleB = 1024.f;
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
-// Pieces lie in lines of 128 bytes: 32 consecutive values of a row, all first pieces and then all second ones.
+// Pieces lie in lines of 128 bytes: 32 consecutive values of a row, all first pieces and then all second ones.  The lines of a block
+// of 32 columns follow one another, so that what a tile reads at once lies side by side (with a row's lines side by side the rows of a
+// tile lie a few KB apart, in a quarter of the L2's channels).
 constexpr int kLine = 128;
-__device__ __forceinline__ char* line_at(char* base, int row, int blocks, int block) {
-    return base + ((int64_t)row * blocks + block) * kLine;
+__device__ __forceinline__ char* line_at(char* base, int row, int rows, int block) {
+    return base + ((int64_t)block * rows + row) * kLine;
 }
-__device__ __forceinline__ const char* line_at(const char* base, int row, int blocks, int block) {
-    return base + ((int64_t)row * blocks + block) * kLine;
+__device__ __forceinline__ const char* line_at(const char* base, int row, int rows, int block) {
+    return base + ((int64_t)block * rows + row) * kLine;
 }
 __device__ __forceinline__ void split(const f32x4& x, f16x4& first, f16x4& second) {
     first = __builtin_convertvector(x, f16x4);
@@ -39,8 +41,9 @@ __device__ __forceinline__ void store_line(char* line, int at, const f32x4& x) {
     *(f16x4*)(line + 2 * at) = first;
     *(f16x4*)(line + 64 + 2 * at) = second;
 }
-__device__ __forceinline__ f32x4 load_line(const char* line, int at) {
-    return __builtin_convertvector(*(const f16x4*)(line + 2 * at), f32x4) + __builtin_convertvector(*(const f16x4*)(line + 64 + 2 * at), f32x4);
+__device__ __forceinline__ void split(const f32x8& x, f16x8& first, f16x8& second) {
+    first = __builtin_convertvector(x, f16x8);
+    second = __builtin_convertvector(x - __builtin_convertvector(first, f32x8), f16x8);
 }
 
 template <class F> __device__ __forceinline__ int find_matrix(const OrthoTable& t, uint32_t block, F&& first) {
@@ -57,13 +60,28 @@ constexpr int kThreads = 256;
 // ---- in -------------------------------------------------------------------------------------------------------
 constexpr int64_t kNormChunk = 8192;
 
+// Eight values at a time where they lie at a whole multiple of sixteen bytes.
+__device__ __forceinline__ f32x8 load_eight(const float* p) {
+    return __builtin_shufflevector(*(const f32x4*)p, *(const f32x4*)(p + 4), 0, 1, 2, 3, 4, 5, 6, 7);
+}
+__device__ __forceinline__ f32x8 load_eight(const __bf16* p) { return __builtin_convertvector(*(const bf16x8*)p, f32x8); }
 template <class E> __device__ __forceinline__ double squares_of(const E* p, int count) {
-    double sum = 0.0;
-    for (int i = threadIdx.x; i < count; i += kThreads) {
+    double sum = 0.0, more = 0.0;
+    const int eights = ((uintptr_t)p & 15) ? 0 : count / 8;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < eights; i += kThreads) {
+        const f32x8 x = load_eight(p + 8 * i);
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+            sum = fma((double)x[e], (double)x[e], sum);
+            more = fma((double)x[e + 1], (double)x[e + 1], more);
+        }
+    }
+    for (int i = 8 * eights + threadIdx.x; i < count; i += kThreads) {
         const double x = (double)(float)p[i];
         sum = fma(x, x, sum);
     }
-    return sum;
+    return sum + more;
 }
 __device__ __forceinline__ double block_total(double x) {
     __shared__ double s[kThreads / 64];
@@ -88,6 +106,21 @@ __global__ __launch_bounds__(kThreads) void k_ortho_norm(const OrthoTable t, dou
 // Pieces of 64 x 64 values of X: of a row that is none, zeros.
 constexpr int kSide = 64;
 template <class E> __device__ __forceinline__ void load_side(const E* p, const OrthoMatrix& M, int i0, int j0, double by, float (*to)[kSide + 1]) {
+    const int across = M.tall ? M.m : M.n, r0 = M.tall ? j0 : i0, c0 = M.tall ? i0 : j0;
+    if (across % 8 == 0 && ((uintptr_t)p & 15) == 0) {
+#pragma unroll
+        for (int y = 0; y < kSide * kSide / 8 / kThreads; ++y) {
+            const int x = y * kThreads + threadIdx.x, r = x / (kSide / 8), c = x % (kSide / 8) * 8;
+            f32x8 v = {};
+            if (r0 + r < (M.tall ? M.n : M.m) && c0 + c < across) v = load_eight(p + (int64_t)(r0 + r) * across + c0 + c);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float z = (float)((double)v[e] * by);
+                if (M.tall) to[c + e][r] = z; else to[r][c + e] = z;
+            }
+        }
+        return;
+    }
     for (int x = threadIdx.x; x < kSide * kSide; x += kThreads) {
         const int r = x / kSide, c = x % kSide;
         if (!M.tall) {
@@ -107,13 +140,13 @@ __global__ __launch_bounds__(kThreads) void k_ortho_in(const OrthoTable t, const
     sum = block_total(sum);
     // a matrix of zeros stays one; one that is not finite is NaN everywhere, as its products would be
     const double by = sum == 0.0 ? 0.0 : sum < (double)INFINITY ? (double)kScaleX / sqrt(sum) : (double)NAN;
-    const int blocks = M.np / 32, across = M.np / kSide, at = blockIdx.x - M.side0;
+    const int across = M.np / kSide, at = blockIdx.x - M.side0;
     const int i0 = at / across * kSide, j0 = at % across * kSide;
     if (M.bf16) load_side((const __bf16*)M.in, M, i0, j0, by, side);
     else load_side((const float*)M.in, M, i0, j0, by, side);
     __syncthreads();
     const int r = threadIdx.x / 4, c = threadIdx.x % 4 * 16;
-    char* line = line_at(ws + M.x, i0 + r, blocks, (j0 + c) / 32);
+    char* line = line_at(ws + M.x, i0 + r, M.mp, (j0 + c) / 32);
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         const float* x = &side[r][c + 4 * q];
@@ -130,6 +163,8 @@ __global__ __launch_bounds__(kThreads) void k_ortho_in(const OrthoTable t, const
 // Symmetric products are made for tiles on and below the diagonal and stored twice.
 // Tiles of 32 k of both operands pass through LDS, two of them, copied there by the memory unit.  A line's 16-byte pieces are turned
 // by its row, so that sixteen rows' pieces (256 bytes, what LDS reads a clock) lie in different banks, and so do four rows' halves.
+// Each XCD has tiles that follow one another, of as much work as any other's: a matrix is then read into one L2 and not into eight.
+// Launches go through the matrices there and back: what one wrote last, the next reads first, from the last-level cache.
 enum { GRAM, SQUARE, APPLY };
 
 __device__ __forceinline__ int turn_of(int row) {
@@ -139,15 +174,66 @@ __device__ __forceinline__ int turn_of(int row) {
 __device__ __forceinline__ f16x8 read_piece(lds_ptr p) { return *(const __attribute__((address_space(3))) f16x8*)(uintptr_t)p; }
 __device__ __forceinline__ void mma(f32x16& acc, const f16x8& a, const f16x8& b) { acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, acc, 0, 0, 0); }
 
-template <int T, int STEP, bool LAST>
-__global__ __launch_bounds__(kThreads, 2) void k_ortho_product(const OrthoTable t, char* ws, int odd, float a, float b, float c) {
-    constexpr int NB = T / 64, BYTES = T * kLine;    // blocks of 32 of a wavefront's side; one operand's tile
-    __shared__ __align__(256) char lds[2][2 * BYTES];
+// Sixteen bytes a lane from memory to LDS without registers: lane i's, from base + offset, go to dst + 16 i (base, dst: the same for
+// the wavefront).  The instruction is written out because the compiler, for its own builtin, waits for all copies under way before the
+// next read of any LDS, which it cannot tell from theirs (updates of an encoder's matrices: the third product 186 us so, 160).  Every
+// copy is waited for, and followed by a barrier, before its bytes are read and before the wavefront ends.
+__device__ __forceinline__ void copy_ahead(const char* base, uint32_t offset, char* dst) {
+    const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)dst);      // (LDS begins at a whole multiple of 4 GiB)
+    const uint64_t at = (uint64_t)(uintptr_t)base;
+    const uint64_t from = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32)) << 32 |
+                          (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at);
+    uint32_t before;                                 // m0 is left as it was
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
+                 : "=&s"(before) : "s"(to), "v"(offset), "s"(from) : "memory");
+}
+// All but the last N of the wavefront's copies have arrived.
+template <int N> __device__ __forceinline__ void wait_but() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
+
+// Eight values of a row of the output, which has the input's shape.
+__device__ __forceinline__ void store_row(const OrthoMatrix& M, int row, int col, const f32x8& z) {
+    const int rows = M.tall ? M.n : M.m, cols = M.tall ? M.m : M.n;
+    if (row >= rows || col >= cols) return;
+    const int64_t at = (int64_t)row * cols + col;
+    if (cols % 8 == 0 && ((uintptr_t)M.out & 15) == 0) {
+        if (M.bf16) {
+            *(bf16x8*)((__bf16*)M.out + at) = __builtin_convertvector(z, bf16x8);
+        } else {
+            *(f32x4*)((float*)M.out + at) = __builtin_shufflevector(z, z, 0, 1, 2, 3);
+            *(f32x4*)((float*)M.out + at + 4) = __builtin_shufflevector(z, z, 4, 5, 6, 7);
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        if (col + e >= cols) continue;
+        if (M.bf16) ((__bf16*)M.out)[at + e] = (__bf16)z[e]; else ((float*)M.out)[at + e] = z[e];
+    }
+}
+
+struct Piece { int row, col; };                      // of a tile: eight values from here on
+__device__ __forceinline__ void store_piece(char* line, const Piece& p, const f32x8& z) {
+    f16x8 first, second;
+    split(z, first, second);
+    *(f16x8*)(line + p.col % 32 * 2) = first;
+    *(f16x8*)(line + 64 + p.col % 32 * 2) = second;
+}
+
+template <int T, int AHEAD, int STEP, bool LAST>
+__global__ __launch_bounds__(kThreads, 2) void k_ortho_product(const OrthoTable t, char* ws, int odd, int back, float a, float b, float c) {
+    constexpr int NB = T / 64;                       // blocks of 32 of a wavefront's side
+    constexpr int BYTES = 2 * T * kLine, COPIES = T / 16;
+    __shared__ __align__(256) char lds[AHEAD + 1][BYTES];
+    static_assert(T * T * 4 <= (AHEAD + 1) * BYTES, "the tile goes through the same LDS");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
-    const int which = find_matrix(t, blockIdx.x, [&](int j) { return STEP == APPLY ? t.of[j].apply0 : t.of[j].square0; });
+    const OrthoEnds& ends = STEP == GRAM ? t.gram : STEP == SQUARE ? t.square : t.apply;
+    const uint32_t first = ends.of[blockIdx.x % kXcds], behind = ends.of[blockIdx.x % kXcds + 1];
+    if (blockIdx.x / kXcds >= behind - first) return;
+    const uint32_t tile = back ? behind - 1 - blockIdx.x / kXcds : first + blockIdx.x / kXcds;
+    const int which = find_matrix(t, tile, [&](int j) { return STEP == APPLY ? t.of[j].apply0 : t.of[j].square0; });
     const OrthoMatrix& M = t.of[which];
     const char* X = ws + (odd ? M.y : M.x);
-    const int at = blockIdx.x - (STEP == APPLY ? M.apply0 : M.square0);
+    const int at = tile - (STEP == APPLY ? M.apply0 : M.square0);
     int ti, tj;
     if constexpr (STEP == APPLY) {
         const int across = M.np / T;
@@ -159,114 +245,150 @@ __global__ __launch_bounds__(kThreads, 2) void k_ortho_product(const OrthoTable 
         while (ti * (ti + 1) / 2 > at) --ti;
         tj = at - ti * (ti + 1) / 2;
     }
-    const int i0 = ti * T, j0 = tj * T;
-    const int x_blocks = M.np / 32, a_blocks = M.mp / 32;
+    const int i0 = ti * T, j0 = tj * T, rows = M.mp;
     const char* P = STEP == GRAM ? X : ws + (STEP == SQUARE ? M.a : M.b);
-    const int p_blocks = STEP == GRAM ? x_blocks : a_blocks, steps = p_blocks;
-    auto issue = [&](int kb, int buf) {
+    const int steps = (STEP == GRAM ? M.np : M.mp) / 32;
+    auto issue = [&](int kb) {
+        char* to = lds[kb % (AHEAD + 1)] + wave * 8 * kLine;      // eight lines a wavefront
+        const char *p = line_at(P, i0, rows, kb), *q = STEP == APPLY ? line_at(X, kb * 32, rows, j0 / 32) : line_at(P, j0, rows, kb);
 #pragma unroll
-        for (int x = 0; x < T / 32; ++x) {           // eight lines a wavefront
-            const int line = x * 32 + wave * 8 + (lane >> 3), piece = (lane & 7) ^ turn_of(line);
-            char* to = lds[buf] + (x * 32 + wave * 8) * kLine;
-            copy_to_lds(line_at(P, i0 + line, p_blocks, kb) + piece * 16, to);
-            const char* q = STEP == APPLY ? line_at(X, kb * 32 + (line & 31), x_blocks, j0 / 32 + (line >> 5)) : line_at(P, j0 + line, p_blocks, kb);
-            copy_to_lds(q + piece * 16, to + BYTES);
+        for (int x = 0; x < COPIES / 2; ++x) {
+            const int line = x * 32 + wave * 8 + (lane >> 3);
+            const uint32_t piece = (uint32_t)((lane & 7) ^ turn_of(line)) * 16;
+            copy_ahead(p, (uint32_t)line * kLine + piece, to + x * 32 * kLine);
+            copy_ahead(q, (STEP == APPLY ? (uint32_t)(line >> 5) * (uint32_t)rows + (uint32_t)(line & 31) : (uint32_t)line) * kLine + piece,
+                       to + (T + x * 32) * kLine);
         }
     };
     const int wi = (wave & 1) * (T / 2), wj = (wave >> 1) * (T / 2);
     const lds_ptr base = in_lds(lds[0]);
     // row operand: line `row`, eight values from 16 c + 8 h on; turned: sixteen lanes read four rows of sixteen values
-    const lds_ptr p_place = base + (uint32_t)((wi + n) * kLine), q_place = base + (uint32_t)(BYTES + (wj + n) * kLine);
+    const lds_ptr p_place = base + (uint32_t)((wi + n) * kLine), q_place = base + (uint32_t)((T + wj + n) * kLine);
     const int t_row = 8 * h + ((lane & 15) >> 2), t_piece = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+    // what the product is added to: a thread's pieces of eight values, a block's lines one after the other
+    constexpr int PIECES = T * T / 8 / kThreads;
+    auto piece_of = [&](int x) {
+        const int p = x * kThreads + tid;
+        return Piece{(p >> 2) % T, (p >> 2) / T * 32 + (p & 3) * 8};
+    };
+    f16x8 add[STEP == GRAM ? 1 : PIECES][2];
+    if constexpr (STEP != GRAM)
+#pragma unroll
+        for (int x = 0; x < PIECES; ++x) {
+            const Piece p = piece_of(x);
+            const char* line = line_at(STEP == SQUARE ? P : X, i0 + p.row, rows, (j0 + p.col) / 32) + p.col % 32 * 2;
+            add[x][0] = *(const f16x8*)line;
+            add[x][1] = *(const f16x8*)(line + 64);
+        }
     f32x16 acc[NB][NB] = {};                         // [j][i]
-    issue(0, 0);
-    wait_for_copies();
-    __syncthreads();
+    for (int kb = 0; kb < AHEAD && kb < steps; ++kb) issue(kb);
     for (int kb = 0; kb < steps; ++kb) {
-        const int buf = kb & 1;
-        if (kb + 1 < steps) issue(kb + 1, buf ^ 1);
-        const uint32_t from = (uint32_t)(buf * 2 * BYTES);
+        // this tile's copies have arrived: those of AHEAD - 1 later ones may be under way
+        if (kb + AHEAD - 1 < steps) wait_but<(AHEAD - 1) * COPIES>(); else wait_but<0>();
+        __syncthreads();                             // everyone's, and nobody reads the one before any more
+        if (kb + AHEAD < steps) issue(kb + AHEAD);
+        const uint32_t from = (uint32_t)(kb % (AHEAD + 1) * BYTES);
+        // all operands are asked for first: the products begin with the first ones while the others arrive
+        f16x8 p[2][NB][2], q[2][NB][2];
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            f16x8 p[NB][2], q[NB][2];
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
-            for (int x = 0; x < NB; ++x)
+            for (int y = 1; y >= 0; --y) {
+                const uint32_t piece = (uint32_t)(((2 * s + h + 4 * y) ^ turn_of(n)) << 4);
 #pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    const uint32_t piece = (uint32_t)(((2 * s + h + 4 * y) ^ turn_of(n)) << 4);
-                    p[x][y] = read_piece(p_place + from + (uint32_t)(x * 32 * kLine) + piece);
+                for (int x = 0; x < NB; ++x) {
                     if constexpr (STEP != APPLY) {
-                        q[x][y] = read_piece(q_place + from + (uint32_t)(x * 32 * kLine) + piece);
+                        q[s][x][y] = read_piece(q_place + from + (uint32_t)(x * 32 * kLine) + piece);
                     } else {
                         auto place = [&](int row) {
-                            return base + from + (uint32_t)(BYTES + (wj + 32 * x + row) * kLine + (((t_piece + 4 * y) ^ turn_of(row)) << 4) + (lane & 1) * 8);
+                            return base + from + (uint32_t)((T + wj + 32 * x + row) * kLine + (((t_piece + 4 * y) ^ turn_of(row)) << 4) + (lane & 1) * 8);
                         };
-                        q[x][y] = __builtin_bit_cast(f16x8, read_turned(place(16 * s + t_row), place(16 * s + t_row + 4)));
+                        q[s][x][y] = __builtin_bit_cast(f16x8, read_turned(place(16 * s + t_row), place(16 * s + t_row + 4)));
                     }
                 }
 #pragma unroll
-            for (int x = 0; x < NB; ++x)
+                for (int x = 0; x < NB; ++x) p[s][x][1 - y] = read_piece(p_place + from + (uint32_t)(x * 32 * kLine) + (piece ^ 64));
+            }
+        phase();
 #pragma unroll
-                for (int y = 0; y < NB; ++y) {       // the smallest first
-                    mma(acc[x][y], q[x][1], p[y][0]);
-                    mma(acc[x][y], q[x][0], p[y][1]);
-                    mma(acc[x][y], q[x][0], p[y][0]);
-                }
-        }
-        wait_for_copies();
-        __syncthreads();
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int z = 0; z < 3; ++z)              // the smallest first
+#pragma unroll
+                for (int x = 0; x < NB; ++x)
+#pragma unroll
+                    for (int y = 0; y < NB; ++y) mma(acc[x][y], q[s][x][z == 0], p[s][y][z == 1]);
     }
+    __syncthreads();
+    // The tile goes through LDS once more, in 32 bits, so that lines are read and written whole (from the accumulators a lane would
+    // have eight bytes of each: twice as many requests to L2 as the products' operands).  Four values' places are turned by the row.
+    float* tile_of = (float*)lds[0];
+    auto place = [&](int i, int j) { return i * T + (((j >> 2) ^ (i & (T / 4 - 1))) << 2 | (j & 3)); };
 #pragma unroll
     for (int x = 0; x < NB; ++x)
 #pragma unroll
-        for (int y = 0; y < NB; ++y) {
-            const int i = i0 + wi + 32 * y + n, jb = j0 + wj + 32 * x;
-            f32x16& v = acc[x][y];
-            if constexpr (STEP != APPLY) {
-                char* to = ws + (STEP == GRAM ? M.a : M.b);
-                if constexpr (STEP == GRAM) v *= kScaleA / (kScaleX * kScaleX);
+        for (int y = 0; y < NB; ++y)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int j = 8 * r + 4 * h;
-                    f32x4 z = {v[4 * r], v[4 * r + 1], v[4 * r + 2], v[4 * r + 3]};
-                    if constexpr (STEP == SQUARE) {
-                        z = z * (c * (kScaleB / (kScaleA * kScaleA))) + load_line(line_at(P, i, a_blocks, jb / 32), j) * (b * (kScaleB / kScaleA));
-                    }
-                    store_line(line_at(to, i, a_blocks, jb / 32), j, z);
-                    if (ti != tj) {                  // its other half
-                        f16x4 first, second;
-                        split(z, first, second);
+            for (int r = 0; r < 4; ++r)
+                *(f32x4*)(tile_of + place(wi + 32 * y + n, wj + 32 * x + 8 * r + 4 * h)) =
+                    f32x4{acc[x][y][4 * r], acc[x][y][4 * r + 1], acc[x][y][4 * r + 2], acc[x][y][4 * r + 3]};
+    char* to = ws + (STEP == GRAM ? M.a : STEP == SQUARE ? M.b : odd ? M.x : M.y);
+    const float by = STEP == GRAM ? kScaleA / (kScaleX * kScaleX) : STEP == SQUARE ? c * (kScaleB / (kScaleA * kScaleA)) : 1.f / kScaleB;
+    const float more = STEP == SQUARE ? b * (kScaleB / kScaleA) : a;
+    const bool mirrored = STEP != APPLY && ti != tj, again = STEP == APPLY ? LAST && M.tall : mirrored;
+    __syncthreads();
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            char* line = line_at(to, jb + j + e, a_blocks, i / 32);
-                            *(_Float16*)(line + 2 * n) = first[e];
-                            *(_Float16*)(line + 64 + 2 * n) = second[e];
-                        }
-                    }
-                }
-            } else {
-                const float by = kScaleX / (kScaleB * kScaleX);
+    for (int x = 0; x < PIECES; ++x) {
+        const Piece p = piece_of(x);
+        f32x8 z;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int j = 8 * r + 4 * h;
-                    f32x4 z = f32x4{v[4 * r], v[4 * r + 1], v[4 * r + 2], v[4 * r + 3]} * by + load_line(line_at(X, i, x_blocks, jb / 32), j) * a;
-                    if constexpr (!LAST) {
-                        store_line(line_at(ws + (odd ? M.x : M.y), i, x_blocks, jb / 32), j, z);
-                    } else {
-                        z *= 1.f / kScaleX;
+        for (int q = 0; q < 2; ++q) {
+            const f32x4 v = *(const f32x4*)(tile_of + place(p.row, p.col + 4 * q));
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            if (i >= M.m || jb + j + e >= M.n) continue;
-                            const int64_t place = M.tall ? (int64_t)(jb + j + e) * M.m + i : (int64_t)i * M.n + jb + j + e;
-                            if (M.bf16) ((__bf16*)M.out)[place] = (__bf16)z[e]; else ((float*)M.out)[place] = z[e];
-                        }
-                    }
-                }
-            }
+            for (int e = 0; e < 4; ++e) z[4 * q + e] = v[e] * by;
         }
+        if constexpr (STEP != GRAM) z += (__builtin_convertvector(add[x][0], f32x8) + __builtin_convertvector(add[x][1], f32x8)) * more;
+        if constexpr (LAST) z *= 1.f / kScaleX;
+        if constexpr (!LAST) store_piece(line_at(to, i0 + p.row, rows, (j0 + p.col) / 32), p, z);
+        else if (!M.tall) store_row(M, i0 + p.row, j0 + p.col, z);
+        if constexpr (STEP != GRAM) {
+            if (again)                               // each thread's own places
+#pragma unroll
+                for (int q = 0; q < 2; ++q)
+                    *(f32x4*)(tile_of + place(p.row, p.col + 4 * q)) = f32x4{z[4 * q], z[4 * q + 1], z[4 * q + 2], z[4 * q + 3]};
+        }
+    }
+    if (!again) return;                              // the tile is also, or only, stored as its transpose
+    if constexpr (STEP != GRAM) __syncthreads();
+#pragma unroll 2
+    for (int x = 0; x < PIECES; ++x) {
+        const Piece p = piece_of(x);                 // of the transpose
+        f32x8 z;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[e] = tile_of[place(p.col + e, p.row)] * (STEP == GRAM ? by : 1.f);
+        if constexpr (STEP == APPLY) store_row(M, j0 + p.row, i0 + p.col, z);
+        else store_piece(line_at(to, j0 + p.row, rows, (i0 + p.col) / 32), p, z);
+    }
 }
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+// Tiles of all matrices in eight runs of about the same work, a matrix's being tiles of `depth`.
+template <class Depth> void share_out(const OrthoTable& t, OrthoEnds& ends, int64_t tiles, uint32_t OrthoMatrix::*first, Depth&& depth) {
+    auto tiles_of = [&](int i) { return (i + 1 < t.n ? (int64_t)(t.of[i + 1].*first) : tiles) - (int64_t)(t.of[i].*first); };
+    double all = 0.0, before = 0.0;
+    for (int i = 0; i < t.n; ++i) all += (double)tiles_of(i) * depth(t.of[i]);
+    int x = 1;
+    for (int i = 0; i < t.n; ++i) {
+        const double own = (double)tiles_of(i) * depth(t.of[i]);
+        while (x < kXcds && before + own >= all * x / kXcds) {
+            const int64_t at = (int64_t)((all * x / kXcds - before) / depth(t.of[i]) + 0.5);
+            ends.of[x++] = (uint32_t)((int64_t)(t.of[i].*first) + (at < tiles_of(i) ? at : tiles_of(i)));
+        }
+        before += own;
+    }
+    while (x <= kXcds) ends.of[x++] = (uint32_t)tiles;
+}
 
 // The matrices from `first` on that one series of launches takes, and what it needs.
 struct OrthoGroup { OrthoTable t; int64_t end, chunks, sides, squares, applies; size_t parts, bytes; int tile; };
@@ -274,12 +396,12 @@ OrthoGroup group_from(int64_t first, int64_t n, const int64_t* rows, const int64
                       const int32_t* dts) {
     OrthoGroup G = {};
     G.end = first + kOrthoTable < n ? first + kOrthoTable : n;
-    int64_t wide_tiles = 0;                          // of 128, in the products that have fewest
+    int64_t half = 0;                                // tiles of 128, in the products that have fewest
     for (int64_t i = first; i < G.end; ++i) {
         const int64_t m = rows[i] < cols[i] ? rows[i] : cols[i], across = (m + 127) / 128;
-        wide_tiles += across * (across + 1) / 2;
+        half += across * (across + 1) / 2;
     }
-    G.tile = wide_tiles >= 256 ? 128 : 64;
+    G.tile = half >= 256 ? 128 : 64;
     size_t at = 0;
     auto take = [&](int64_t bytes) {
         const size_t x = at;
@@ -314,10 +436,29 @@ OrthoGroup group_from(int64_t first, int64_t n, const int64_t* rows, const int64
     }
     G.parts = take(G.chunks * 8);
     G.bytes = at;
+    share_out(G.t, G.t.gram, G.squares, &OrthoMatrix::square0, [](const OrthoMatrix& M) { return M.np; });
+    share_out(G.t, G.t.square, G.squares, &OrthoMatrix::square0, [](const OrthoMatrix& M) { return M.mp; });
+    share_out(G.t, G.t.apply, G.applies, &OrthoMatrix::apply0, [](const OrthoMatrix& M) { return M.mp; });
     return G;
 }
 
-template <int T> hipError_t launch_group(const OrthoGroup& G, char* ws, int steps, const float* k, hipStream_t st) {
+unsigned groups_of(const OrthoEnds& ends) {
+    uint32_t most = 0;
+    for (int x = 0; x < kXcds; ++x) most = ends.of[x + 1] - ends.of[x] > most ? ends.of[x + 1] - ends.of[x] : most;
+    return most * kXcds;
+}
+
+// Tiles of 128 x 128 leave room for two workgroups a CU, one storing while the other multiplies, with copies one k tile ahead; of
+// small matrices, in tiles of 64 x 64, the copies' latency is all there is: three ahead.
+template <int STEP, bool LAST = false>
+hipError_t launch_product(const OrthoGroup& G, const OrthoEnds& ends, char* ws, int odd, int back, const float* k, hipStream_t st) {
+    const dim3 grid(groups_of(ends));
+    if (G.tile == 128) k_ortho_product<128, 1, STEP, LAST><<<grid, kThreads, 0, st>>>(G.t, ws, odd, back, k[0], k[1], k[2]);
+    else k_ortho_product<64, 3, STEP, LAST><<<grid, kThreads, 0, st>>>(G.t, ws, odd, back, k[0], k[1], k[2]);
+    return hipGetLastError();
+}
+
+hipError_t launch_group(const OrthoGroup& G, char* ws, int steps, const float* k, hipStream_t st) {
     double* parts = (double*)(ws + G.parts);
     k_ortho_norm<<<dim3((unsigned)G.chunks), kThreads, 0, st>>>(G.t, parts);
     hipError_t e = hipGetLastError();
@@ -326,13 +467,10 @@ template <int T> hipError_t launch_group(const OrthoGroup& G, char* ws, int step
     e = hipGetLastError();
     for (int s = 0; s < steps && e == hipSuccess; ++s) {
         const int odd = s & 1;
-        k_ortho_product<T, GRAM, false><<<dim3((unsigned)G.squares), kThreads, 0, st>>>(G.t, ws, odd, k[0], k[1], k[2]);
-        if ((e = hipGetLastError()) != hipSuccess) break;
-        k_ortho_product<T, SQUARE, false><<<dim3((unsigned)G.squares), kThreads, 0, st>>>(G.t, ws, odd, k[0], k[1], k[2]);
-        if ((e = hipGetLastError()) != hipSuccess) break;
-        if (s + 1 < steps) k_ortho_product<T, APPLY, false><<<dim3((unsigned)G.applies), kThreads, 0, st>>>(G.t, ws, odd, k[0], k[1], k[2]);
-        else k_ortho_product<T, APPLY, true><<<dim3((unsigned)G.applies), kThreads, 0, st>>>(G.t, ws, odd, k[0], k[1], k[2]);
-        e = hipGetLastError();
+        if ((e = launch_product<GRAM>(G, G.t.gram, ws, odd, s & 1, k, st)) != hipSuccess) break;
+        if ((e = launch_product<SQUARE>(G, G.t.square, ws, odd, ~s & 1, k, st)) != hipSuccess) break;
+        e = s + 1 < steps ? launch_product<APPLY>(G, G.t.apply, ws, odd, s & 1, k, st)
+                          : launch_product<APPLY, true>(G, G.t.apply, ws, odd, s & 1, k, st);
     }
     return e;
 }
@@ -353,7 +491,7 @@ bool ortho_launchable(int64_t n, const int64_t* rows, const int64_t* cols) {
     constexpr int64_t most = 0xffffffffll / kThreads;
     for (int64_t i = 0; i < n;) {
         const OrthoGroup G = group_from(i, n, rows, cols, nullptr, nullptr, nullptr);
-        if (G.chunks > most || G.sides > most || G.squares > most || G.applies > most) return false;
+        if (G.chunks > most || G.sides > most || 8 * G.squares > most || 8 * G.applies > most) return false;
         i = G.end;
     }
     return true;
@@ -366,7 +504,7 @@ hipError_t launch_ortho(int64_t n, const void* const* in, void* const* out, cons
         const OrthoGroup G = group_from(i, n, rows, cols, in, out, dts);
         i = G.end;
         if (!G.t.n) continue;
-        const hipError_t e = G.tile == 128 ? launch_group<128>(G, ws, steps, coefficients, st) : launch_group<64>(G, ws, steps, coefficients, st);
+        const hipError_t e = launch_group(G, ws, steps, coefficients, st);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;

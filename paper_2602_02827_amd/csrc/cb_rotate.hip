@@ -214,7 +214,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_rotate_join(const float* part,
 int parts_of(const RotateArgs& A, int lanes) {
     const int heads = A.heads + A.kv_heads;
     int parts = 1;
-    while (parts < heads && A.rows * parts * lanes < 65536) parts *= 2;
+    while (parts < heads && A.rows * parts * lanes < 1 << 19) parts *= 2;
     return parts < heads ? parts : heads;
 }
 constexpr int64_t kMostGroups = 1024;                // of the backward pass
