@@ -150,9 +150,9 @@ int colbandit_attention_window_backward(const colbandit_attn *a, const colbandit
  *   table    DEVICE [vocab][width], rows table_row elements apart
  *   tokens   DEVICE int64 [n];  out DEVICE [n][width]
  * Products in 32 bits, rounded once; table and out may differ in type.
- * n below 2^31 - 2^16, vocab at most 2^24, width at most 2^16.  Values looked up below 2^34 (2^37
+ * n below 2^31 - 2^16, vocab at most 2^24, width at most 2^16.  Values looked up below 2^34 (2^36
  * where rows begin at whole multiples of 16 bytes and width is one of 8), of the gradient, n / 64
- * rows more than the table's, below 2^32 (2^35).
+ * rows more than the table's, below 2^32 (2^34).
  */
 int colbandit_embedding(const void *table, colbandit_dtype table_dt, int64_t table_row,
                         const int64_t *tokens, int64_t n, int64_t vocab, int64_t width, float scale,

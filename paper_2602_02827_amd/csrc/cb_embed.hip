@@ -11,14 +11,19 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-// V consecutive values in 32 bits: eight where rows are whole multiples of 16 bytes, or one.
+// V consecutive values in 32 bits: eight where one side has 16 bits, four where both have 32 (sixteen bytes a lane), and one where rows
+// do not lie so.  (54 thousand rows of 768, a 32-bit table of 32,000 under 16-bit rows, with the gradient: pieces of eight 108 us, of four
+// 115; 2,700 rows of 256 in 32 bits: 14.4 and 13.7.)
 template <int V> struct Piece { float v[V]; };
 template <int V> __device__ __forceinline__ Piece<V> load_piece(const float* p) {
     Piece<V> x;
-    if constexpr (V == 8) {
-        const f32x4 a = *(const f32x4*)p, b = *((const f32x4*)p + 1);
+    if constexpr (V > 1) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x.v[i] = a[i], x.v[4 + i] = b[i];
+        for (int q = 0; q < V / 4; ++q) {
+            const f32x4 a = *((const f32x4*)p + q);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x.v[4 * q + i] = a[i];
+        }
     } else {
         x.v[0] = *p;
     }
@@ -39,6 +44,8 @@ template <int V> __device__ __forceinline__ void store_piece(float* p, const Pie
     if constexpr (V == 8) {
         *(f32x4*)p = f32x4{x.v[0], x.v[1], x.v[2], x.v[3]};
         *((f32x4*)p + 1) = f32x4{x.v[4], x.v[5], x.v[6], x.v[7]};
+    } else if constexpr (V == 4) {
+        *(f32x4*)p = f32x4{x.v[0], x.v[1], x.v[2], x.v[3]};
     } else {
         *p = x.v[0];
     }
@@ -53,6 +60,7 @@ template <int V> __device__ __forceinline__ void store_piece(__bf16* p, const Pi
         *p = (__bf16)x.v[0];
     }
 }
+template <class W, class O> constexpr int kMostPiece = sizeof(W) + sizeof(O) == 8 ? 4 : 8;
 
 // Pieces of all rows are dealt to threads one after the other, so that no lane is left over whatever a row's width is.
 struct Place { uint64_t row; uint32_t piece; };
@@ -94,12 +102,15 @@ __global__ __launch_bounds__(kThreads) void k_embed(const W* table, int64_t tabl
 // dtable[v] = scale * sum of dout[i] over the i whose token is v, in the order of i: the same inputs give the same bits.
 // First tokens are sorted, each workgroup having a range of the table's rows: it goes over all tokens, counts those below its range
 // (which is where its part of the sorted list begins) and those of each row, and then puts its own into their places.  A wavefront
-// has a run of consecutive tokens, so that the order of equal ones is that of the list.
-constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kMostRange = 960;
+// has a run of consecutive tokens, so that the order of equal ones is that of the list.  It notes its own tokens as it comes by, and
+// only goes over its run again where there are more of them than it has room for.
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kMostRange = 960, kNoted = 512;
 
 __global__ __launch_bounds__(kSortThreads) void k_embed_sort(const int64_t* tokens, int n, int vocab, int range, int* starts, int* order) {
     extern __shared__ int place[];                   // [wavefront][row of the range]: counts, then next places
     __shared__ int below_of[kSortWaves], sums[kSortWaves];
+    __shared__ int noted[kSortWaves][kNoted];
+    __shared__ uint16_t noted_row[kSortWaves][kNoted];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int lo = blockIdx.x * range, rows = vocab - lo < range ? vocab - lo : range;
     int* own = place + wave * range;
@@ -108,12 +119,29 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(const int64_t* toke
     const int each = ((n + kSortWaves - 1) / kSortWaves + 63) / 64 * 64;
     const int64_t run = (int64_t)wave * each;        // (n is below 2^31, a run's end may not be)
     const int begin = run < n ? (int)run : n, end = run + each < n ? (int)(run + each) : n;
-    int below = 0;
-#pragma unroll 4
-    for (int i = begin; i < end; i += 64) {
-        const int64_t t = end - i > lane ? tokens[i + lane] : -1;
-        below += t >= 0 && t < lo;
-        if (t >= lo && t < lo + rows) atomicAdd(own + (int)(t - lo), 1);
+    const uint64_t before_me = (1ull << lane) - 1ull;
+    int below = 0, notes = 0;
+    constexpr int AHEAD = 8;
+    for (int i0 = begin; i0 < end; i0 += 64 * AHEAD) {
+        int64_t t[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) t[j] = end - i0 > 64 * j + lane ? tokens[(int64_t)i0 + 64 * j + lane] : -1;
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            below += t[j] >= 0 && t[j] < lo;
+            const bool mine = t[j] >= lo && t[j] < lo + rows;
+            const uint64_t all = __ballot(mine);
+            if (!all) continue;
+            const int at = notes + __popcll(all & before_me);
+            if (mine) {
+                atomicAdd(own + (int)(t[j] - lo), 1);
+                if (at < kNoted) {
+                    noted[wave][at] = i0 + 64 * j + lane;
+                    noted_row[wave][at] = (uint16_t)(t[j] - lo);
+                }
+            }
+            notes += __popcll(all);
+        }
     }
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) below += __shfl_xor(below, m);
@@ -143,23 +171,29 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(const int64_t* toke
         for (int w = 0; w < kSortWaves; ++w) place[w * range + tid] += first;
     }
     __syncthreads();
-    for (int i = begin; i < end; i += 64) {
-        const int64_t t = end - i > lane ? tokens[i + lane] : -1;
-        const bool mine = t >= lo && t < lo + rows;
-        const int r = mine ? (int)(t - lo) : -1;
-        uint64_t left = __ballot(mine);
-        while (left) {                               // one row after the other, its lanes in their order
+    // sixty-four of its tokens: row by row, a row's lanes in their order (r: -1 in lanes that have none)
+    auto put = [&](int r, int position) {
+        uint64_t left = __ballot(r >= 0);
+        while (left) {
             const int row = __shfl(r, __builtin_ctzll(left));
             const uint64_t same = __ballot(r == row);
             if (r == row) {
-                const int before = __popcll(same & ((1ull << lane) - 1ull));
+                const int before = __popcll(same & before_me);
                 const int at = own[row];
-                order[at + before] = i + lane;
+                order[at + before] = position;
                 if (before == 0) own[row] = at + __popcll(same);
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             left &= ~same;
         }
+    };
+    if (notes <= kNoted) {
+        for (int i = lane; i - lane < notes; i += 64) put(i < notes ? (int)noted_row[wave][i] : -1, i < notes ? noted[wave][i] : 0);
+        return;
+    }
+    for (int i = begin; i < end; i += 64) {
+        const int64_t t = end - i > lane ? tokens[i + lane] : -1;
+        put(t >= lo && t < lo + rows ? (int)(t - lo) : -1, i + lane);
     }
 }
 
@@ -168,24 +202,34 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(const int64_t* toke
 // own, joined by a second launch.
 constexpr int kLong = 64;
 
+// A piece as it is stored, so that many are under way in few registers.
+template <class O, int V> struct Raw;
+template <> struct Raw<__bf16, 8> { bf16x8 x; };
+template <> struct Raw<float, 4> { f32x4 x; };
+template <> struct Raw<float, 8> { f32x4 x[2]; };
+template <class O> struct Raw<O, 1> { O x[1]; };
+
 template <class O, int V>
 __device__ __forceinline__ Piece<V> sum_of_tokens(const O* dout, int64_t dout_row, uint32_t piece, const int* order, int begin, int end) {
     constexpr int AHEAD = 8;
     Piece<V> sum = {};
+#pragma unroll 1
     for (int i = begin; i < end; i += AHEAD) {
-        Piece<V> x[AHEAD];
+        Raw<O, V> x[AHEAD];
         int at[AHEAD];
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) at[j] = i + j < end ? order[i + j] : -1;
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) {
             x[j] = {};
-            if (at[j] >= 0) x[j] = load_piece<V>(dout + at[j] * dout_row + (int64_t)piece * V);
+            if (at[j] >= 0) x[j] = *(const Raw<O, V>*)(dout + at[j] * dout_row + (int64_t)piece * V);
         }
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j)
+        for (int j = 0; j < AHEAD; ++j) {
+            const Piece<V> y = load_piece<V>((const O*)&x[j]);
 #pragma unroll
-            for (int e = 0; e < V; ++e) sum.v[e] += x[j].v[e];
+            for (int e = 0; e < V; ++e) sum.v[e] += y.v[e];
+        }
     }
     return sum;
 }
@@ -239,9 +283,9 @@ __global__ __launch_bounds__(kThreads) void k_embed_join(const int64_t* tokens, 
     if (piece < pieces) {
 #pragma unroll 4
         for (int c = chunk + mine; c <= last; c += kJoinParts) {
-            const Piece<V> x = load_piece<V>(part + ((int64_t)(2 * (int64_t)c + (c == chunk && from > begin)) * pieces + piece) * V);
+            const Raw<float, V> x = *(const Raw<float, V>*)(part + ((int64_t)(2 * (int64_t)c + (c == chunk && from > begin)) * pieces + piece) * V);
 #pragma unroll
-            for (int e = 0; e < V; ++e) sum.v[e] += x.v[e];
+            for (int e = 0; e < V; ++e) sum.v[e] += ((const float*)&x)[e];
         }
     }
     sums[mine][threadIdx.x % kJoinPieces] = sum;
@@ -273,17 +317,17 @@ template <class F> hipError_t by_types(int w, int o, F&& f) {
     if (w == TR_F32) return o == TR_F32 ? f((float*)nullptr, (float*)nullptr) : f((float*)nullptr, (__bf16*)nullptr);
     return o == TR_F32 ? f((__bf16*)nullptr, (float*)nullptr) : f((__bf16*)nullptr, (__bf16*)nullptr);
 }
-bool whole(const void* p, int64_t row, int eb) { return ((uintptr_t)p | (uintptr_t)(row * eb)) % 16 == 0; }
 int size_of(int dt) { return dt == TR_BF16 ? 2 : 4; }
-
 }  // namespace
 
-// Whether a row's pieces are of eight values: `rows` and `dense` are the two sides.
-bool embedding_is_wide(const void* rows, int rows_dt, int64_t row, const void* dense, int dense_dt, int64_t width) {
-    return width % 8 == 0 && whole(rows, row, size_of(rows_dt)) && whole(dense, width, size_of(dense_dt));
+// Values of a piece; `rows` and `dense` are the two sides.
+int embedding_piece(const void* rows, int rows_dt, int64_t row, const void* dense, int dense_dt, int64_t width) {
+    const int v = rows_dt == TR_F32 && dense_dt == TR_F32 ? 4 : 8;
+    auto lie = [&](const void* p, int64_t r, int dt) { return (uintptr_t)p % 16 == 0 && r * size_of(dt) % 16 == 0; };
+    return width % v == 0 && lie(rows, row, rows_dt) && lie(dense, width, dense_dt) ? v : 1;
 }
-bool embedding_launchable(int64_t n, int64_t vocab, int64_t width, bool wide, bool backward) {
-    const int64_t pieces = wide ? width / 8 : width, most = 0xffffffffll / kThreads;
+bool embedding_launchable(int64_t n, int64_t vocab, int64_t width, int piece, bool backward) {
+    const int64_t pieces = width / piece, most = 0xffffffffll / kThreads;
     if (!backward) return (n * pieces + 4 * kThreads - 1) / (4 * kThreads) <= most;
     const EmbedPlan P = plan_embed(n, vocab, width);
     return (P.chunks * pieces + kThreads - 1) / kThreads + (vocab * pieces + kThreads - 1) / kThreads <= most &&
@@ -293,7 +337,7 @@ bool embedding_launchable(int64_t n, int64_t vocab, int64_t width, bool wide, bo
 hipError_t launch_embedding(const void* table, int table_dt, int64_t table_row, const int64_t* tokens, int64_t n, int64_t vocab, int64_t width,
                             float scale, void* out, int out_dt, hipStream_t st) {
     if (n == 0) return hipSuccess;
-    const bool wide = embedding_is_wide(table, table_dt, table_row, out, out_dt, width);
+    const bool wide = embedding_piece(table, table_dt, table_row, out, out_dt, width) > 1;
     return by_types(table_dt, out_dt, [&](auto* w, auto* o) {
         using W = std::remove_pointer_t<decltype(w)>;
         using O = std::remove_pointer_t<decltype(o)>;
@@ -306,10 +350,11 @@ hipError_t launch_embedding(const void* table, int table_dt, int64_t table_row, 
         };
         using one = std::integral_constant<int, 1>;
         using four = std::integral_constant<int, 4>;
-        using eight = std::integral_constant<int, 8>;
+        using wide_piece = std::integral_constant<int, kMostPiece<W, O>>;
         // few pieces: a thread each; many: four, whose loads are under way together
-        if (wide) return n * width / 8 <= 1 << 16 ? go(eight{}, one{}) : go(eight{}, four{});
-        return n * width <= 1 << 16 ? go(one{}, one{}) : go(one{}, four{});
+        const bool few = n * (width / (wide ? wide_piece::value : 1)) <= 1 << 16;
+        if (wide) return few ? go(wide_piece{}, one{}) : go(wide_piece{}, four{});
+        return few ? go(one{}, one{}) : go(one{}, four{});
     });
 }
 
@@ -323,7 +368,7 @@ hipError_t launch_embedding_backward(const void* dout, int dout_dt, int64_t dout
     k_embed_sort<<<dim3((unsigned)P.groups), kSortThreads, kSortWaves * P.range * 4, st>>>(tokens, (int)n, (int)vocab, P.range, starts, order);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const bool wide = embedding_is_wide(dout, dout_dt, dout_row, dtable, table_dt, width);
+    const bool wide = embedding_piece(dout, dout_dt, dout_row, dtable, table_dt, width) > 1;
     return by_types(table_dt, dout_dt, [&](auto* w, auto* o) {
         using W = std::remove_pointer_t<decltype(w)>;
         using O = std::remove_pointer_t<decltype(o)>;
@@ -341,7 +386,7 @@ hipError_t launch_embedding_backward(const void* dout, int dout_dt, int64_t dout
                                                                                                order, groups, scale, part, (W*)dtable);
             return hipGetLastError();
         };
-        return wide ? go(std::integral_constant<int, 8>{}) : go(std::integral_constant<int, 1>{});
+        return wide ? go(std::integral_constant<int, kMostPiece<W, O>>{}) : go(std::integral_constant<int, 1>{});
     });
 }
 

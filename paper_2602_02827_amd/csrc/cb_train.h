@@ -78,8 +78,8 @@ size_t clip_workspace_bytes(int64_t n, const int64_t* sizes);
 hipError_t launch_clip(int64_t n, const void* const* grads, void* const* out, const int64_t* sizes, const int32_t* dts,
                        float max_norm, float* norm, void* ws, hipStream_t st);
 
-bool embedding_is_wide(const void* rows, int rows_dt, int64_t row, const void* dense, int dense_dt, int64_t width);
-bool embedding_launchable(int64_t n, int64_t vocab, int64_t width, bool wide, bool backward);
+int embedding_piece(const void* rows, int rows_dt, int64_t row, const void* dense, int dense_dt, int64_t width);      // values of a piece
+bool embedding_launchable(int64_t n, int64_t vocab, int64_t width, int piece, bool backward);
 hipError_t launch_embedding(const void* table, int table_dt, int64_t table_row, const int64_t* tokens, int64_t n, int64_t vocab, int64_t width,
                             float scale, void* out, int out_dt, hipStream_t st);
 size_t embedding_workspace_bytes(int64_t n, int64_t vocab, int64_t width);

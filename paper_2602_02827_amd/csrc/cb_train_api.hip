@@ -403,7 +403,7 @@ int colbandit_embedding(const void* table, colbandit_dtype table_dt, int64_t tab
     const int rc = check_embedding(n, vocab, width, table_row, table_dt, out_dt);
     if (rc) return rc;
     if (!table || (n && (!tokens || !out))) return COLBANDIT_ERR_NULL;
-    if (!embedding_launchable(n, vocab, width, embedding_is_wide(table, table_dt, table_row, out, out_dt, width), false)) return COLBANDIT_ERR_UNSUPPORTED;
+    if (!embedding_launchable(n, vocab, width, embedding_piece(table, table_dt, table_row, out, out_dt, width), false)) return COLBANDIT_ERR_UNSUPPORTED;
     if (misaligned(table, size_of(table_dt)) || misaligned(out, size_of(out_dt)) || misaligned(tokens, 8)) return COLBANDIT_ERR_ALIGNMENT;
     return hip(launch_embedding(table, table_dt, table_row, tokens, n, vocab, width, scale, out, out_dt, (hipStream_t)stream));
 }
@@ -418,7 +418,7 @@ int colbandit_embedding_backward(const void* dout, colbandit_dtype dout_dt, int6
     int rc = check_embedding(n, vocab, width, dout_row, table_dt, dout_dt);
     if (rc) return rc;
     if (!dtable || (n && (!tokens || !dout))) return COLBANDIT_ERR_NULL;
-    if (!embedding_launchable(n, vocab, width, embedding_is_wide(dout, dout_dt, dout_row, dtable, table_dt, width), true))
+    if (!embedding_launchable(n, vocab, width, embedding_piece(dout, dout_dt, dout_row, dtable, table_dt, width), true))
         return COLBANDIT_ERR_UNSUPPORTED;
     if (misaligned(dtable, size_of(table_dt)) || misaligned(dout, size_of(dout_dt)) || misaligned(tokens, 8)) return COLBANDIT_ERR_ALIGNMENT;
     rc = workspace_ok(workspace, workspace_bytes, embedding_workspace_bytes(n, vocab, width));
