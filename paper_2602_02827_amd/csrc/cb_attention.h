@@ -376,6 +376,7 @@ __global__ __launch_bounds__(64 * kWavefronts, (kWaves<E, D>)) void k_attention(
     const typename T::At at_tiles(lds[0], lane);
     int i = first_tile, buf = 0;
     while (true) {
+        settle<E>();
         const int base = at_key.base(i);
         const typename T::At lk = at_tiles + buf * 2 * T::BYTES, lv = lk + T::BYTES;
         const bool last = i + 1 >= end_tile;                     // of the unit
@@ -724,6 +725,7 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
     float weight = 0.f;                                          // sum of a row's probabilities, in a far tile's first pass
     int i = 0, buf = 0;
     while (true) {
+        settle<E>();
         if (i == 0) {                                            // a head unit begins
             int is = 0;
 #pragma unroll
@@ -1035,19 +1037,23 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int s
     // 16 bits: a row's log-sum-exp and delta are what its accumulators start from (in 32 bits that would cost the scores an
     // error of some roundings of the log-sum-exp, which 16-bit results do not show: it is at most kFarRow there)
     constexpr bool START = sizeof(E) == 2;
-    auto place_of_row = [&](int head0, int c0, int r) {           // of a tile's row among all heads'
-        const int row0 = c0 / G, c1 = c0 - row0 * G, row = G == 1 ? r : (int)((uint32_t)(c1 + r) / (uint32_t)G);
-        return (int64_t)head0 * A.total_q + qs.lo + row0 + row + (int64_t)(c1 + r - row * G) * A.total_q;
+    // A tile's first row, and its first column's place in it; what a tile adds to them.  Divisions by the number of heads that share a
+    // tile, at most 16, are products (of fewer than 2^8 columns, exact): they were a quarter of the vector instructions.
+    struct Place { int row, c; };
+    const Place step = {T::ROWS / G, T::ROWS % G}, first_place = {col0 / G, 0};
+    const uint32_t inverse = (65536u + (uint32_t)G - 1u) / (uint32_t)G;
+    auto row_of = [&](int x) { return G == 1 ? x : (int)((uint32_t)x * inverse >> 16); };
+    auto place_of_row = [&](int head0, const Place& p, int r) {   // of a tile's row among all heads'
+        const int row = row_of(p.c + r);
+        return (int64_t)head0 * A.total_q + qs.lo + p.row + row + (int64_t)(p.c + r - row * G) * A.total_q;
     };
-    auto issue = [&](int head0, int c0, char* to) {
-        const int row0 = c0 / G, c1 = c0 - row0 * G;              // the tile's first row, and its first column's place in it
-        auto row_of = [&](int r) { return G == 1 ? r : (int)((uint32_t)(c1 + r) / (uint32_t)G); };
+    auto issue = [&](int head0, int c0, const Place& p, char* to) {
         auto offset = [&](int r, uint32_t per_row, uint32_t per_head) {
-            const int row = row_of(r);
-            return G == 1 ? (uint32_t)row * per_row : (uint32_t)row * per_row + (uint32_t)(c1 + r - row * G) * per_head;
+            const int row = row_of(p.c + r);
+            return G == 1 ? (uint32_t)row * per_row : (uint32_t)row * per_row + (uint32_t)(p.c + r - row * G) * per_head;
         };
-        auto place = [&](int r) { return place_of_row(head0, c0, r); };
-        next.issue(qp + row0 * qrow + head0 * qhead, gp + row0 * grow + head0 * ghead, to, cols - c0, tid,
+        auto place = [&](int r) { return place_of_row(head0, p, r); };
+        next.issue(qp + p.row * qrow + head0 * qhead, gp + p.row * grow + head0 * ghead, to, cols - c0, tid,
                    [&](int r) { return offset(r, (uint32_t)qrow, (uint32_t)qhead); },
                    [&](int r) { return offset(r, (uint32_t)grow, (uint32_t)ghead); },
                    [&](int r) { return (uint8_t)(lse[place(r)] != -INFINITY); });
@@ -1060,7 +1066,7 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int s
             }
         }
     };
-    auto finish = [&](int buf, int head0, int c0) {
+    auto finish = [&](int buf, int head0, const Place& p) {
         next.finish(lds[buf], tid);
         if (tid < T::ROWS) {
             const bool own = is_far(n_lse, scale2), far = __ballot(own) != 0;
@@ -1068,7 +1074,7 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int s
             const float add = n_lse == -INFINITY ? -INFINITY : -n_lse * (START ? LOG2E / scale2 : LOG2E);
             if (far) {
                 row_far[buf][0][tid] = n_lse == -INFINITY ? INFINITY : n_lse;
-                row_far[buf][1][tid] = own ? delta[(int64_t)A.heads * A.total_q + place_of_row(head0, c0, tid)] : 0.f;
+                row_far[buf][1][tid] = own ? delta[(int64_t)A.heads * A.total_q + place_of_row(head0, p, tid)] : 0.f;
             }
             row_lse[buf][tid] = far ? 0.f : add;
             row_delta[buf][tid] = -n_delta;
@@ -1076,9 +1082,10 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int s
         }
     };
     int head0 = kv0 * A.group, c0 = col0;
+    Place at_c0 = first_place;
     const int head_end = kv_end * A.group;
     const bool any = col0 < cols;
-    if (any) issue(head0, c0, lds[0]);
+    if (any) issue(head0, c0, at_c0, lds[0]);
     Column<E, D> k, v;
     auto load_keys = [&](int kv) {
         k.load((const E*)A.k + at * A.k_row + kv * A.k_head, seen, h);
@@ -1096,17 +1103,21 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int s
         __syncthreads();
         fill_bias<E>(A, head0, starts, table, tid, THREADS);
     }
-    if (any) finish(0, head0, c0);
+    if (any) finish(0, head0, at_c0);
     __syncthreads();
     const typename T::At at_tiles(lds[0], lane);
     int buf = 0;
     while (true) {
+        settle<E>();
         const int far_now = tile_far[buf];
         const bool last_tile = c0 + T::ROWS >= cols;
         const int n_head = last_tile ? head0 + G : head0, n_c = last_tile ? col0 : c0 + T::ROWS;
+        Place n_place = {at_c0.row + step.row, at_c0.c + step.c};
+        if (n_place.c >= G) n_place = {n_place.row + 1, n_place.c - G};
+        if (last_tile) n_place = first_place;
         const bool last = last_tile && n_head % A.group == 0;                           // of a key head
         const bool more = kRuns<D> ? n_head < head_end : !last;
-        if (more && any) issue(n_head, n_c, lds[buf ^ 1]);
+        if (more && any) issue(n_head, n_c, n_place, lds[buf ^ 1]);
         const typename T::At lq = at_tiles + buf * 2 * T::BYTES, lg = lq + T::BYTES;
         if (any && busy && c0 + T::ROWS > wfirst && (!WIN || c0 < wend)) {
             bool diagonal;
@@ -1229,7 +1240,7 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int s
                 if constexpr (!APART) acc2[db] = {};
             }
         }
-        if (more && any) finish(buf ^ 1, n_head, n_c);
+        if (more && any) finish(buf ^ 1, n_head, n_place);
         __syncthreads();
         if (BIAS && n_head != head0) {
             fill_bias<E>(A, n_head, starts, table, tid, THREADS);
@@ -1237,6 +1248,7 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int s
         }
         head0 = n_head;
         c0 = n_c;
+        at_c0 = n_place;
         buf ^= 1;
     }
 }

@@ -174,22 +174,6 @@ __device__ __forceinline__ int turn_of(int row) {
 __device__ __forceinline__ f16x8 read_piece(lds_ptr p) { return *(const __attribute__((address_space(3))) f16x8*)(uintptr_t)p; }
 __device__ __forceinline__ void mma(f32x16& acc, const f16x8& a, const f16x8& b) { acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, acc, 0, 0, 0); }
 
-// Sixteen bytes a lane from memory to LDS without registers: lane i's, from base + offset, go to dst + 16 i (base, dst: the same for
-// the wavefront).  The instruction is written out because the compiler, for its own builtin, waits for all copies under way before the
-// next read of any LDS, which it cannot tell from theirs (updates of an encoder's matrices: the third product 186 us so, 160).  Every
-// copy is waited for, and followed by a barrier, before its bytes are read and before the wavefront ends.
-__device__ __forceinline__ void copy_ahead(const char* base, uint32_t offset, char* dst) {
-    const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)dst);      // (LDS begins at a whole multiple of 4 GiB)
-    const uint64_t at = (uint64_t)(uintptr_t)base;
-    const uint64_t from = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32)) << 32 |
-                          (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at);
-    uint32_t before;                                 // m0 is left as it was
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
-                 : "=&s"(before) : "s"(to), "v"(offset), "s"(from) : "memory");
-}
-// All but the last N of the wavefront's copies have arrived.
-template <int N> __device__ __forceinline__ void wait_but() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
-
 // Eight values of a row of the output, which has the input's shape.
 __device__ __forceinline__ void store_row(const OrthoMatrix& M, int row, int col, const f32x8& z) {
     const int rows = M.tall ? M.n : M.m, cols = M.tall ? M.m : M.n;
@@ -255,8 +239,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_ortho_product(const OrthoTable 
         for (int x = 0; x < COPIES / 2; ++x) {
             const int line = x * 32 + wave * 8 + (lane >> 3);
             const uint32_t piece = (uint32_t)((lane & 7) ^ turn_of(line)) * 16;
-            copy_ahead(p, (uint32_t)line * kLine + piece, to + x * 32 * kLine);
-            copy_ahead(q, (STEP == APPLY ? (uint32_t)(line >> 5) * (uint32_t)rows + (uint32_t)(line & 31) : (uint32_t)line) * kLine + piece,
+            copy_to_lds(p, (uint32_t)line * kLine + piece, to + x * 32 * kLine);
+            copy_to_lds(q, (STEP == APPLY ? (uint32_t)(line >> 5) * (uint32_t)rows + (uint32_t)(line & 31) : (uint32_t)line) * kLine + piece,
                        to + (T + x * 32) * kLine);
         }
     };
@@ -284,7 +268,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_ortho_product(const OrthoTable 
     for (int kb = 0; kb < AHEAD && kb < steps; ++kb) issue(kb);
     for (int kb = 0; kb < steps; ++kb) {
         // this tile's copies have arrived: those of AHEAD - 1 later ones may be under way
-        if (kb + AHEAD - 1 < steps) wait_but<(AHEAD - 1) * COPIES>(); else wait_but<0>();
+        if (kb + AHEAD - 1 < steps) wait_for_copies<(AHEAD - 1) * COPIES>(); else wait_for_copies();
         __syncthreads();                             // everyone's, and nobody reads the one before any more
         if (kb + AHEAD < steps) issue(kb + AHEAD);
         const uint32_t from = (uint32_t)(kb % (AHEAD + 1) * BYTES);

@@ -162,13 +162,33 @@ __device__ __forceinline__ int here(int x) {
 // The compiler moves nothing across: operands of the next products are not read while the registers are needed for these.
 __device__ __forceinline__ void phase() { __builtin_amdgcn_sched_barrier(0); }
 
-// Sixteen bytes a lane from memory to LDS without registers: lane i's go to dst + 16 i (dst: the same for the wavefront).
-__device__ __forceinline__ void copy_to_lds(const void* src, char* dst) {
-    using G = const __attribute__((address_space(1))) void;
-    using L = __attribute__((address_space(3))) void;
-    __builtin_amdgcn_global_load_lds((G*)src, (L*)dst, 16, 0, 0);
+// Sixteen bytes a lane from memory to LDS without registers: lane i's, from base + offset, go to dst + 16 i (base, dst: the same for
+// the wavefront).  Every copy is waited for, and followed by a barrier, before its bytes are read and before the wavefront ends.
+// The instruction is written out because the compiler, for its own builtin, waits for all copies under way before the next read of any
+// LDS, which it cannot tell from theirs, so that nothing would be a tile ahead.
+__device__ __forceinline__ void copy_to_lds(const void* base, uint32_t offset, char* dst) {
+    const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)dst);      // (LDS begins at a whole multiple of 4 GiB)
+    const uint64_t at = (uint64_t)(uintptr_t)base;
+    const uint64_t from = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32)) << 32 |
+                          (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at);
+    uint32_t before;                                 // m0 is left as it was
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
+                 : "=&s"(before) : "s"(to), "v"(offset), "s"(from) : "memory");
 }
-__device__ __forceinline__ void wait_for_copies() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// All but the last N of the wavefront's copies and loads have arrived.  By the builtin, which the compiler counts: loads from before a
+// loop, were their wait not known to it, would be waited for in every turn, and the copies under way with them.
+template <int N = 0> __device__ __forceinline__ void wait_for_copies() {
+    static_assert(N < 64, "a count of six bits");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0xf70);       // the other counters: any
+    asm volatile("" ::: "memory");
+}
+
+// Where tiles are copied by the memory unit: said at the top of a loop over tiles, where nothing is under way, for the compiler, which
+// else finds ways around the waits that are never gone, and waits for the copies in the middle of the turn.
+template <class E> __device__ __forceinline__ void settle() {
+    if constexpr (sizeof(E) == 2) wait_for_copies();
+}
 
 // A matrix's rows on their way to a tile in LDS, a tile ahead of its use, rows past the end as the last row again.  16 bits: by the
 // memory unit itself.  32 bits: they wait in registers, and are cut into their pieces as they are written.
@@ -187,10 +207,11 @@ template <class E, int D, int THREADS, int R = Oper<E>::ROWS> struct Rows {
         for (int i = 0; i < N; ++i) {
             if (ALL % THREADS && i * THREADS + wave * 64 >= ALL) break;          // of the wavefront
             const int place = row(i, tid);
-            const char* src = a + (at(place < rows ? place : rows - 1) + piece(i, tid));
+            const uint32_t offset = at(place < rows ? place : rows - 1) + piece(i, tid);
             if constexpr (DIRECT) {
-                copy_to_lds(src, lds + (i * THREADS + wave * 64) * 16);
+                copy_to_lds(a, offset, lds + (i * THREADS + wave * 64) * 16);
             } else {
+                const char* src = a + offset;
                 x[i][0] = *(const f32x4*)src;
                 x[i][1] = *((const f32x4*)src + 1);
             }
