@@ -932,22 +932,23 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
 // In 16 bits wide heads have two wavefronts for the same rows, one for either gradient: the scores are made twice (five products
 // where there were four), but two wavefronts share a SIMD (24 causal pages, forward and backward: 508 us, with one 828).
 template <class E, int D> constexpr bool kApart = sizeof(E) == 2 && D >= 96;
-// With a window the first keys are left to workgroups of their own (from `main` on, `sink_groups` of them), since all of a sequence's
-// rows see them: a key tile's others see some rows only.  Such a workgroup takes kSinkRows rows of a sequence, and leaves its shares of
-// the first keys' gradients to k_attention_join_sinks.
+// With a window the first keys are left to workgroups of their own (the first `sink_groups` ones), since all of a sequence's rows see
+// them: a key tile's others see some rows only.  Such a workgroup takes kSinkRows rows of a sequence, and leaves its shares of the first
+// keys' gradients to k_attention_join_sinks.  They are short, and come first, so that the others begin one after the other and do not
+// leave most CUs idle where their number is a little more than that of the CUs.
 template <class E, int D, bool BIAS, bool MASKED, bool WIN>
 __global__ __launch_bounds__((kApart<E, D> ? 128 : 64) * kWavefronts, (kGradientWaves<E, D>)) void
 k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int sink_groups, int q_slots, const E* dout, const float* lse,
                 const float* delta, const float* bias_part, E* dk, E* dv, E* dbias, float* sink_part) {
     using O = Oper<E>;
-    using T = Tile<E, D>;
+    using T = Tile<E, D, kApart<E, D> ? 128 : Oper<E>::ROWS>;
     constexpr int NB = T::ROWS / 32, DB = D / 32, COLS = 32 * kWavefronts;
     constexpr bool APART = kApart<E, D>;
     constexpr int WAVES = APART ? 2 * kWavefronts : kWavefronts, THREADS = 64 * WAVES;
     const bool keys = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) >= kWavefronts;        // (APART) this wavefront has the keys' gradient
     __shared__ __align__(256) char lds[2][2 * T::BYTES];
     __shared__ __align__(16) float row_lse[2][T::ROWS], row_delta[2][T::ROWS], row_far[2][2][T::ROWS];
-    __shared__ int tile_far[2];                       // some row is far: row_far has log-sum-exps, and what is added to far rows' exponents
+    __shared__ int tile_far[2][(T::ROWS + 63) / 64];  // of 64 rows, some row is far: row_far has log-sum-exps, and what is added to far rows' exponents
     extern __shared__ __align__(16) char dyn[];
     const int tid = threadIdx.x, lane0 = tid & 63, lane = lane0, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     if constexpr (BIAS) {
@@ -963,12 +964,12 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int s
             return;
         }
     }
-    const bool sinks = WIN && (int)blockIdx.x >= main;
+    const bool sinks = WIN && (int)blockIdx.x < sink_groups;
     int slot, kv0, kv_end, seq, key0;
     bool rest = false;
     Range ks, qs;
     if (!sinks) {
-        const Work work = work_of(blockIdx.x, slots, (A.kv_heads + run - 1) / run, A.n_seqs, order, false);
+        const Work work = work_of((int)blockIdx.x - (WIN ? sink_groups : 0), slots, (A.kv_heads + run - 1) / run, A.n_seqs, order, false);
         slot = work.slot;
         kv0 = work.inner * run;
         kv_end = kv0 + run < A.kv_heads ? kv0 + run : A.kv_heads;
@@ -978,7 +979,7 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int s
         key0 = (slot - ks.place) * COLS;
         if (key0 < 0 || key0 >= ks.n) return;
     } else {
-        const int x = (int)blockIdx.x - main, inner = A.kv_heads * ((A.sinks + COLS - 1) / COLS);
+        const int x = (int)blockIdx.x, inner = A.kv_heads * ((A.sinks + COLS - 1) / COLS);
         slot = x / inner;
         kv0 = x % inner % A.kv_heads;
         kv_end = kv0 + 1;
@@ -1078,7 +1079,7 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int s
             }
             row_lse[buf][tid] = far ? 0.f : add;
             row_delta[buf][tid] = -n_delta;
-            if (tid == 0) tile_far[buf] = far;
+            if (lane0 == 0) tile_far[buf][wave] = far;
         }
     };
     int head0 = kv0 * A.group, c0 = col0;
@@ -1109,7 +1110,6 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int s
     int buf = 0;
     while (true) {
         settle<E>();
-        const int far_now = tile_far[buf];
         const bool last_tile = c0 + T::ROWS >= cols;
         const int n_head = last_tile ? head0 + G : head0, n_c = last_tile ? col0 : c0 + T::ROWS;
         Place n_place = {at_c0.row + step.row, at_c0.c + step.c};
@@ -1129,7 +1129,7 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int s
                 if constexpr (WIN)
                     if (c0 + 32 * b + 32 <= wfirst) continue;
                 f32x16 s = {}, dp = {};
-                const bool far = __builtin_amdgcn_readfirstlane(far_now) != 0;
+                const bool far = __builtin_amdgcn_readfirstlane(tile_far[buf][b >> 1]) != 0;
                 if constexpr (START) s = of_rows(row_lse[buf], b, h);
 #pragma unroll
                 for (int c = 0; c < D / 16; ++c) O::template mma<true>(s, T::rows(lq, b, c), k.v[c]);

@@ -54,9 +54,10 @@ AttnPlan plan_attention(const AttnArgs& A, int d, int dt, bool backward) {
         // Few tiles over long keys: their keys are cut into parts of 128 rows or more (on average; the longest sequence's are
         // longer) until there are 2,048 workgroups.  16 tokens over 1 to 16,385 keys, us: 40 so, 46 with 256 rows and 1,024, 42 with
         // 128 and 4,096, 66 with 512 and 1,024.
-        if (groups < 512 && k_rows >= 512) {
+        const int64_t part = A.windowed ? 64 : 128;
+        if (groups < 512 && k_rows >= 4 * part) {
             int64_t s = (2048 - 1 + groups) / groups;
-            s = s < k_rows / 128 ? s : k_rows / 128;
+            s = s < k_rows / part ? s : k_rows / part;
             P.splits = (int)(s < 1 ? 1 : s > 256 ? 256 : s);
         }
         if (P.splits > 1) {

@@ -102,9 +102,9 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _stream():
+def _stream(dev=None):
     # the handle alone: making a Stream object of it costs as much as a small call's kernels (2.8 us)
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if dev is None else dev)
 
 
 def _check(rc, what):
@@ -113,10 +113,12 @@ def _check(rc, what):
 
 
 def _on_device(*tensors):
+    """The current device, on which all of them must live."""
     dev = torch.cuda.current_device()
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise ValueError("tensors must live on the current device")
+    return dev
 
 
 def _offsets(off):
@@ -149,30 +151,34 @@ def colbandit_bias_buckets(n_buckets, max_distance, causal=False) -> np.ndarray:
 def _attn(q, k, v, q_offsets, k_offsets, causal, scale, keep, bias, max_distance):
     if k_offsets is None:
         k_offsets = q_offsets
-    if q.dtype not in _DTYPES or k.dtype != q.dtype or v.dtype != q.dtype:
+    dtype = q.dtype
+    dt = _DTYPES.get(dtype)
+    if dt is None or k.dtype != dtype or v.dtype != dtype:
         raise TypeError("q, k and v must be float32 or bfloat16, all of one type")
-    if q.dim() != 3 or k.dim() != 3 or v.shape != k.shape or q.shape[2] != k.shape[2]:
+    k_shape = k.shape
+    if q.dim() != 3 or len(k_shape) != 3 or v.shape != k_shape or q.shape[2] != k_shape[2]:
         raise ValueError("q is [total_q, heads, d], k and v are [total_k, kv_heads, d]")
-    for t in (q, k, v):
-        if t.stride(2) != 1:
-            raise ValueError("the values of a row and head must be consecutive")
-    if _offsets(q_offsets).shape != _offsets(k_offsets).shape:
+    total_q, heads, d = q.shape
+    total_k, kv_heads, _ = k_shape
+    (q_row, q_head, q_last), (k_row, k_head, k_last), (v_row, v_head, v_last) = q.stride(), k.stride(), v.stride()
+    if q_last != 1 or k_last != 1 or v_last != 1:
+        raise ValueError("the values of a row and head must be consecutive")
+    n = _offsets(q_offsets).shape[0]
+    if k_offsets is not q_offsets and _offsets(k_offsets).shape[0] != n:
         raise ValueError("q_offsets and k_offsets must hold equally many sequences")
     if keep is not None:
-        if keep.dtype not in (torch.bool, torch.uint8) or keep.shape != k.shape[:1] or not keep.is_contiguous():
+        if keep.dtype not in (torch.bool, torch.uint8) or keep.shape != k_shape[:1] or not keep.is_contiguous():
             raise ValueError("keep is a contiguous bool or uint8 vector over the key rows")
     if bias is not None:
-        if bias.dtype != q.dtype:
+        if bias.dtype != dtype:
             raise TypeError("bias must have the type of q")
-        if bias.dim() != 2 or bias.shape[1] != q.shape[1] or not bias.is_contiguous():
+        if bias.dim() != 2 or bias.shape[1] != heads or not bias.is_contiguous():
             raise ValueError("bias is a contiguous [n_buckets, heads]")
     _on_device(q, k, v, q_offsets, k_offsets, keep, bias)
     return ColbanditAttn(
-        _DTYPES[q.dtype], q_offsets.shape[0] - 1, q.shape[1], k.shape[1], q.shape[2], 1 if causal else 0,
-        0 if bias is None else bias.shape[0], int(max_distance),
-        1.0 / math.sqrt(q.shape[2]) if scale is None else scale, q.shape[0], k.shape[0],
-        q_offsets.data_ptr(), k_offsets.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(),
-        q.stride(0), q.stride(1), k.stride(0), k.stride(1), v.stride(0), v.stride(1), _ptr(keep), _ptr(bias))
+        dt, n - 1, heads, kv_heads, d, 1 if causal else 0, 0 if bias is None else bias.shape[0], int(max_distance),
+        1.0 / math.sqrt(d) if scale is None else scale, total_q, total_k, q_offsets.data_ptr(), k_offsets.data_ptr(),
+        q.data_ptr(), k.data_ptr(), v.data_ptr(), q_row, q_head, k_row, k_head, v_row, v_head, _ptr(keep), _ptr(bias))
 
 
 def _window(window, sinks):
@@ -185,8 +191,12 @@ def _window(window, sinks):
     return ColbanditWindow(before, after, sinks)
 
 
+def _like(t):
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
 def _dense(t, shape, dtype, what):
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
+    if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
         raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
     return t
 
@@ -202,16 +212,15 @@ def colbandit_attention(q, k, v, q_offsets, k_offsets=None, *, causal=False, sca
     a = _attn(q, k, v, q_offsets, k_offsets, causal, scale, keep, bias, max_distance)
     L = lib()
     o, lse = (out["out"], out["lse"]) if out else (None, None)
-    o = q.new_empty(q.shape) if o is None else _dense(o, q.shape, q.dtype, "out")
-    lse = q.new_empty((q.shape[1], q.shape[0]), dtype=torch.float32) if lse is None else \
-        _dense(lse, (q.shape[1], q.shape[0]), torch.float32, "lse")
-    _on_device(o, lse)
+    o = _like(q) if o is None else _dense(o, q.shape, q.dtype, "out")
+    lse = q.new_empty((a.heads, a.total_q), dtype=torch.float32) if lse is None else _dense(lse, (a.heads, a.total_q), torch.float32, "lse")
+    dev = _on_device(o, lse)
     if w is not None:
         ws, nb = _workspace(workspace, L.colbandit_attention_window_workspace_bytes(a, w, 0), q.device)
-        _check(L.colbandit_attention_window(a, w, o.data_ptr(), lse.data_ptr(), _ptr(ws), nb, _stream()), "colbandit_attention_window")
+        _check(L.colbandit_attention_window(a, w, o.data_ptr(), lse.data_ptr(), _ptr(ws), nb, _stream(dev)), "colbandit_attention_window")
         return {"out": o, "lse": lse}
     ws, nb = _workspace(workspace, L.colbandit_attention_workspace_bytes(a, 0), q.device)
-    _check(L.colbandit_attention(a, o.data_ptr(), lse.data_ptr(), _ptr(ws), nb, _stream()), "colbandit_attention")
+    _check(L.colbandit_attention(a, o.data_ptr(), lse.data_ptr(), _ptr(ws), nb, _stream(dev)), "colbandit_attention")
     return {"out": o, "lse": lse}
 
 
@@ -226,7 +235,7 @@ def colbandit_attention_backward(dout, q, k, v, out, lse, q_offsets, k_offsets=N
     _dense(lse, (q.shape[1], q.shape[0]), torch.float32, "lse")
     _dense(dout, q.shape, q.dtype, "dout")
     _on_device(out, lse, dout)
-    dq, dk, dv = q.new_empty(q.shape), k.new_empty(k.shape), k.new_empty(k.shape)
+    dq, dk, dv = _like(q), _like(k), _like(k)
     dbias = None if bias is None else torch.empty_like(bias)
     if w is not None:
         ws, nb = _workspace(workspace, L.colbandit_attention_window_workspace_bytes(a, w, 1), q.device)
@@ -242,51 +251,63 @@ def colbandit_attention_backward(dout, q, k, v, out, lse, q_offsets, k_offsets=N
 
 
 def _rows_of(t, what):
-    if t.dtype not in _DTYPES:
+    """Type, shape and distance of the rows of a matrix whose rows may lie apart."""
+    dt, shape = _DTYPES.get(t.dtype), t.shape
+    if dt is None:
         raise TypeError(f"{what} must be float32 or bfloat16")
-    if t.dim() != 2 or t.shape[1] < 1 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
-        raise ValueError(f"{what} is [rows, width] with consecutive values in rows that do not overlap")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    if len(shape) != 2 or shape[1] < 1:
+        raise ValueError(f"{what} is [rows, width]")
+    row, last = t.stride()
+    if shape[0] <= 1:
+        row = shape[1]
+    if (last != 1 and shape[1] > 1) or row < shape[1]:
+        raise ValueError(f"{what} has consecutive values, in rows that do not overlap")
+    return dt, shape[0], shape[1], row
 
 
 def _tokens(tokens):
     if tokens.dtype != torch.int64 or tokens.dim() != 1 or not tokens.is_contiguous():
         raise ValueError("tokens must be a contiguous int64 vector")
+    return tokens.shape[0]
+
+
+def _type_of_rows(dtype):
+    dt = _DTYPES.get(dtype)
+    if dt is None:
+        raise TypeError("rows must be float32 or bfloat16")
+    return dt
 
 
 def colbandit_embedding(table, tokens, *, scale=1.0, dtype=None, out=None):
     """Rows of `table` [vocab, width] for `tokens` int64 [n], times scale; zeros for tokens outside of the table (padding).  `dtype`: of
     the rows, where it is not the table's; `out`: a tensor to write.  Returns dict(out [n, width])."""
-    row = _rows_of(table, "table")
-    _tokens(tokens)
-    n, (vocab, width) = tokens.shape[0], table.shape
-    dtype = table.dtype if dtype is None else dtype
-    if dtype not in _DTYPES:
-        raise TypeError("rows must be float32 or bfloat16")
+    dt, vocab, width, row = _rows_of(table, "table")
+    n = _tokens(tokens)
+    if dtype is None:
+        dtype = table.dtype
+    to = _type_of_rows(dtype)
     out = table.new_empty((n, width), dtype=dtype) if out is None else _dense(out, (n, width), dtype, "out")
-    _on_device(table, tokens, out)
-    _check(lib().colbandit_embedding(table.data_ptr(), _DTYPES[table.dtype], row, tokens.data_ptr(), n, vocab, width, scale,
-                                     out.data_ptr(), _DTYPES[dtype], _stream()), "colbandit_embedding")
+    dev = _on_device(table, tokens, out)
+    _check(lib().colbandit_embedding(table.data_ptr(), dt, row, tokens.data_ptr(), n, vocab, width, scale, out.data_ptr(), to,
+                                     _stream(dev)), "colbandit_embedding")
     return {"out": out}
 
 
 def colbandit_embedding_backward(dout, tokens, vocab, *, scale=1.0, dtype=None, out=None, workspace=None):
     """Gradient of a table of `vocab` rows from that of the rows that were looked up, in the order of the tokens.  `dtype`: of the
     table; `out`: a tensor to write.  Returns dict(dtable [vocab, width])."""
-    row = _rows_of(dout, "dout")
-    _tokens(tokens)
-    n, width = dout.shape
-    if tokens.shape[0] != n:
+    dt, n, width, row = _rows_of(dout, "dout")
+    if _tokens(tokens) != n:
         raise ValueError("dout has a row for each token")
-    dtype = dout.dtype if dtype is None else dtype
-    if dtype not in _DTYPES:
-        raise TypeError("a table is float32 or bfloat16")
+    if dtype is None:
+        dtype = dout.dtype
+    to = _type_of_rows(dtype)
     L = lib()
     out = dout.new_empty((vocab, width), dtype=dtype) if out is None else _dense(out, (vocab, width), dtype, "dtable")
-    _on_device(dout, tokens, out)
+    dev = _on_device(dout, tokens, out)
     ws, nb = _workspace(workspace, L.colbandit_embedding_workspace_bytes(n, vocab, width), dout.device)
-    _check(L.colbandit_embedding_backward(dout.data_ptr(), _DTYPES[dout.dtype], row, tokens.data_ptr(), n, vocab, width, scale,
-                                          out.data_ptr(), _DTYPES[dtype], _ptr(ws), nb, _stream()), "colbandit_embedding_backward")
+    _check(L.colbandit_embedding_backward(dout.data_ptr(), dt, row, tokens.data_ptr(), n, vocab, width, scale, out.data_ptr(), to,
+                                          _ptr(ws), nb, _stream(dev)), "colbandit_embedding_backward")
     return {"dtable": out}
 
 
@@ -298,38 +319,41 @@ def colbandit_rotary_table(n_positions, d, base=10000.0, device=None) -> torch.T
     return table.to(torch.device("cuda", torch.cuda.current_device()) if device is None else device)
 
 
-def _rotation(q, k, positions, table, q_weight, k_weight, eps, interleaved):
-    if q.dtype not in _DTYPES or k.dtype != q.dtype:
+def _rotation(q, k, positions, table, q_weight, k_weight, eps, interleaved, *more):
+    """The library's arguments, and the current device (`more`: tensors that must live there too)."""
+    dt, q_shape, k_shape = _DTYPES.get(q.dtype), q.shape, k.shape
+    if dt is None or k.dtype != q.dtype:
         raise TypeError("q and k must be float32 or bfloat16, both of one type")
-    if q.dim() != 3 or k.dim() != 3 or q.shape[0] != k.shape[0] or q.shape[2] != k.shape[2]:
+    if len(q_shape) != 3 or len(k_shape) != 3 or q_shape[0] != k_shape[0] or q_shape[2] != k_shape[2]:
         raise ValueError("q is [rows, heads, d], k [rows, kv_heads, d]")
-    if q.stride(2) != 1 or k.stride(2) != 1:
+    (q_row, q_head, q_last), (k_row, k_head, k_last) = q.stride(), k.stride()
+    if q_last != 1 or k_last != 1:
         raise ValueError("the values of a row and head must be consecutive")
-    d = q.shape[2]
-    for w in (q_weight, k_weight):
-        if w is not None:
-            _dense(w, (d,), torch.float32, "a weight")
+    rows, heads, d = q_shape
+    n_positions = at = turns = wq = wk = None
+    if q_weight is not None:
+        wq = _dense(q_weight, (d,), torch.float32, "a weight").data_ptr()
+    if k_weight is not None:
+        wk = _dense(k_weight, (d,), torch.float32, "a weight").data_ptr()
     if table is not None:
         if positions is None:
             raise ValueError("a rotation needs positions")
-        _dense(table, (table.shape[0], d // 2, 2), torch.float32, "the table")
-        _dense(positions, q.shape[:1], torch.int64, "positions")
-    _on_device(q, k, positions, table, q_weight, k_weight)
-    return ColbanditRotation(_DTYPES[q.dtype], q.shape[1], k.shape[1], d, 1 if interleaved else 0, eps, q.shape[0],
-                             0 if table is None else table.shape[0], q.data_ptr(), k.data_ptr(), q.stride(0), q.stride(1),
-                             k.stride(0), k.stride(1), _ptr(q_weight), _ptr(k_weight), _ptr(table),
-                             None if table is None else positions.data_ptr())
+        n_positions = table.shape[0]
+        turns = _dense(table, (n_positions, d // 2, 2), torch.float32, "the table").data_ptr()
+        at = _dense(positions, (rows,), torch.int64, "positions").data_ptr()
+    dev = _on_device(q, k, None if table is None else positions, table, q_weight, k_weight, *more)
+    return ColbanditRotation(dt, heads, k_shape[1], d, 1 if interleaved else 0, eps, rows, n_positions or 0, q.data_ptr(), k.data_ptr(),
+                             q_row, q_head, k_row, k_head, wq, wk, turns, at), dev
 
 
 def colbandit_norm_rotate(q, k, *, positions=None, table=None, q_weight=None, k_weight=None, eps=1e-6, interleaved=False, out=None):
     """q [rows, heads, d] and k [rows, kv_heads, d] (any row and head strides), each head divided by its root mean square, times
     the weights float32 [d], and rotated by `table` (colbandit_rotary_table) at `positions` int64 [rows]; rows whose position is none
     of the table's get zeros.  `table` None: no rotation.  `out`: tensors to write, as this returns them.  Returns dict(q, k), dense."""
-    r = _rotation(q, k, positions, table, q_weight, k_weight, eps, interleaved)
-    q_out, k_out = (q.new_empty(q.shape), k.new_empty(k.shape)) if out is None else (
+    q_out, k_out = (_like(q), _like(k)) if out is None else (
         _dense(out["q"], q.shape, q.dtype, "q"), _dense(out["k"], k.shape, k.dtype, "k"))
-    _on_device(q_out, k_out)
-    _check(lib().colbandit_norm_rotate(r, q_out.data_ptr(), k_out.data_ptr(), _stream()), "colbandit_norm_rotate")
+    r, dev = _rotation(q, k, positions, table, q_weight, k_weight, eps, interleaved, q_out, k_out)
+    _check(lib().colbandit_norm_rotate(r, q_out.data_ptr(), k_out.data_ptr(), _stream(dev)), "colbandit_norm_rotate")
     return {"q": q_out, "k": k_out}
 
 
@@ -339,15 +363,14 @@ def colbandit_norm_rotate_backward(dq_out, dk_out, q, k, *, positions=None, tabl
     also where there are no weights."""
     _dense(dq_out, q.shape, q.dtype, "dq_out")
     _dense(dk_out, k.shape, k.dtype, "dk_out")
-    r = _rotation(q, k, positions, table, q_weight, k_weight, eps, interleaved)
-    _on_device(dq_out, dk_out)
+    r, dev = _rotation(q, k, positions, table, q_weight, k_weight, eps, interleaved, dq_out, dk_out)
     L = lib()
-    dq, dk = q.new_empty(q.shape), k.new_empty(k.shape)
-    dw = q.new_empty((2, q.shape[2]), dtype=torch.float32)
+    dq, dk = _like(q), _like(k)
+    dq_weight, dk_weight = q.new_empty(r.d, dtype=torch.float32), q.new_empty(r.d, dtype=torch.float32)
     ws, nb = _workspace(workspace, L.colbandit_norm_rotate_workspace_bytes(r), q.device)
-    _check(L.colbandit_norm_rotate_backward(r, dq_out.data_ptr(), dk_out.data_ptr(), dq.data_ptr(), dk.data_ptr(), dw[0].data_ptr(),
-                                            dw[1].data_ptr(), _ptr(ws), nb, _stream()), "colbandit_norm_rotate_backward")
-    return {"dq": dq, "dk": dk, "dq_weight": dw[0], "dk_weight": dw[1]}
+    _check(L.colbandit_norm_rotate_backward(r, dq_out.data_ptr(), dk_out.data_ptr(), dq.data_ptr(), dk.data_ptr(), dq_weight.data_ptr(),
+                                            dk_weight.data_ptr(), _ptr(ws), nb, _stream(dev)), "colbandit_norm_rotate_backward")
+    return {"dq": dq, "dk": dk, "dq_weight": dq_weight, "dk_weight": dk_weight}
 
 
 def _maxsim(Q, docs, offsets):
