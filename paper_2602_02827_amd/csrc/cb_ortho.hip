@@ -94,7 +94,11 @@ __device__ __forceinline__ double block_total(double x) {
 }
 
 // Sums of squares, in 64 bits, of chunks of each matrix.
-__global__ __launch_bounds__(kThreads) void k_ortho_norm(const OrthoTable t, double* parts) {
+__global__ __launch_bounds__(kThreads) void k_ortho_norm(const OrthoTable t, double* parts, OrthoTable* table) {
+    // the others read the table from memory, where a second one finds it in L2 (the same nine matrices: 139 us from a kernel's arguments,
+    // 131 so)
+    if (blockIdx.x == 0)
+        for (int i = threadIdx.x; i < (int)(sizeof t / 4); i += kThreads) ((uint32_t*)table)[i] = ((const uint32_t*)&t)[i];
     const int i = find_matrix(t, blockIdx.x, [&](int j) { return t.of[j].chunk0; });
     const OrthoMatrix& M = t.of[i];
     const int64_t size = (int64_t)M.m * M.n, first = (int64_t)(blockIdx.x - M.chunk0) * kNormChunk;
@@ -130,7 +134,8 @@ template <class E> __device__ __forceinline__ void load_side(const E* p, const O
         }
     }
 }
-__global__ __launch_bounds__(kThreads) void k_ortho_in(const OrthoTable t, const double* parts, char* ws) {
+__global__ __launch_bounds__(kThreads) void k_ortho_in(const OrthoTable* __restrict__ table, const double* parts, char* ws) {
+    const OrthoTable& t = *table;
     __shared__ float side[kSide][kSide + 1];
     const int i = find_matrix(t, blockIdx.x, [&](int j) { return t.of[j].side0; });
     const OrthoMatrix& M = t.of[i];
@@ -203,13 +208,17 @@ __device__ __forceinline__ void store_piece(char* line, const Piece& p, const f3
     *(f16x8*)(line + 64 + p.col % 32 * 2) = second;
 }
 
-template <int T, int AHEAD, int STEP, bool LAST>
-__global__ __launch_bounds__(kThreads, 2) void k_ortho_product(const OrthoTable t, char* ws, int odd, int back, float a, float b, float c) {
+// DEEP: that many groups of four wavefronts share a tile, each with every DEEP-th tile of k; their sums are added in their order.
+template <int T, int DEEP, int AHEAD, int STEP, bool LAST>
+__global__ __launch_bounds__(DEEP * kThreads, DEEP > 1 ? DEEP : 2) void k_ortho_product(const OrthoTable* __restrict__ table, char* ws, int odd, int back, float a, float b, float c) {
     constexpr int NB = T / 64;                       // blocks of 32 of a wavefront's side
     constexpr int BYTES = 2 * T * kLine, COPIES = T / 16;
-    __shared__ __align__(256) char lds[AHEAD + 1][BYTES];
+    __shared__ __align__(256) char lds[DEEP][AHEAD + 1][BYTES];
     static_assert(T * T * 4 <= (AHEAD + 1) * BYTES, "the tile goes through the same LDS");
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
+    static_assert(DEEP == 1 || AHEAD == 1, "which copies are under way");
+    const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6) % 4, deep = __builtin_amdgcn_readfirstlane(tid >> 6) / 4;
+    const OrthoTable& t = *table;
     const OrthoEnds& ends = STEP == GRAM ? t.gram : STEP == SQUARE ? t.square : t.apply;
     const uint32_t first = ends.of[blockIdx.x % kXcds], behind = ends.of[blockIdx.x % kXcds + 1];
     if (blockIdx.x / kXcds >= behind - first) return;
@@ -231,9 +240,11 @@ __global__ __launch_bounds__(kThreads, 2) void k_ortho_product(const OrthoTable 
     }
     const int i0 = ti * T, j0 = tj * T, rows = M.mp;
     const char* P = STEP == GRAM ? X : ws + (STEP == SQUARE ? M.a : M.b);
-    const int steps = (STEP == GRAM ? M.np : M.mp) / 32;
-    auto issue = [&](int kb) {
-        char* to = lds[kb % (AHEAD + 1)] + wave * 8 * kLine;      // eight lines a wavefront
+    const int tiles = (STEP == GRAM ? M.np : M.mp) / 32, steps = (tiles + DEEP - 1) / DEEP;
+    auto issue = [&](int s) {
+        char* to = lds[deep][s % (AHEAD + 1)] + wave * 8 * kLine;      // eight lines a wavefront
+        const int kb = s * DEEP + deep;
+        if (DEEP > 1 && kb >= tiles) return;
         const char *p = line_at(P, i0, rows, kb), *q = STEP == APPLY ? line_at(X, kb * 32, rows, j0 / 32) : line_at(P, j0, rows, kb);
 #pragma unroll
         for (int x = 0; x < COPIES / 2; ++x) {
@@ -245,20 +256,22 @@ __global__ __launch_bounds__(kThreads, 2) void k_ortho_product(const OrthoTable 
         }
     };
     const int wi = (wave & 1) * (T / 2), wj = (wave >> 1) * (T / 2);
-    const lds_ptr base = in_lds(lds[0]);
+    const lds_ptr base = in_lds(lds[deep]);
     // row operand: line `row`, eight values from 16 c + 8 h on; turned: sixteen lanes read four rows of sixteen values
     const lds_ptr p_place = base + (uint32_t)((wi + n) * kLine), q_place = base + (uint32_t)((T + wj + n) * kLine);
     const int t_row = 8 * h + ((lane & 15) >> 2), t_piece = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
     // what the product is added to: a thread's pieces of eight values, a block's lines one after the other
-    constexpr int PIECES = T * T / 8 / kThreads;
+    constexpr int ALL = T * T / 8, PIECES = (ALL + DEEP * kThreads - 1) / (DEEP * kThreads);
+    const bool has = ALL % (DEEP * kThreads) == 0 || tid < ALL;
     auto piece_of = [&](int x) {
-        const int p = x * kThreads + tid;
+        const int p = x * DEEP * kThreads + tid;
         return Piece{(p >> 2) % T, (p >> 2) / T * 32 + (p & 3) * 8};
     };
-    f16x8 add[STEP == GRAM ? 1 : PIECES][2];
+    f16x8 add[STEP == GRAM ? 1 : PIECES][2] = {};
     if constexpr (STEP != GRAM)
 #pragma unroll
         for (int x = 0; x < PIECES; ++x) {
+            if (!has) break;
             const Piece p = piece_of(x);
             const char* line = line_at(STEP == SQUARE ? P : X, i0 + p.row, rows, (j0 + p.col) / 32) + p.col % 32 * 2;
             add[x][0] = *(const f16x8*)line;
@@ -272,6 +285,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_ortho_product(const OrthoTable 
         __syncthreads();                             // everyone's, and nobody reads the one before any more
         if (kb + AHEAD < steps) issue(kb + AHEAD);
         const uint32_t from = (uint32_t)(kb % (AHEAD + 1) * BYTES);
+        if (DEEP > 1 && kb * DEEP + deep >= tiles) continue;
         // all operands are asked for first: the products begin with the first ones while the others arrive
         f16x8 p[2][NB][2], q[2][NB][2];
 #pragma unroll
@@ -306,7 +320,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_ortho_product(const OrthoTable 
     __syncthreads();
     // The tile goes through LDS once more, in 32 bits, so that lines are read and written whole (from the accumulators a lane would
     // have eight bytes of each: twice as many requests to L2 as the products' operands).  Four values' places are turned by the row.
-    float* tile_of = (float*)lds[0];
+    float* tile_of = (float*)lds;
     auto place = [&](int i, int j) { return i * T + (((j >> 2) ^ (i & (T / 4 - 1))) << 2 | (j & 3)); };
 #pragma unroll
     for (int x = 0; x < NB; ++x)
@@ -314,20 +328,24 @@ __global__ __launch_bounds__(kThreads, 2) void k_ortho_product(const OrthoTable 
         for (int y = 0; y < NB; ++y)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                *(f32x4*)(tile_of + place(wi + 32 * y + n, wj + 32 * x + 8 * r + 4 * h)) =
+                *(f32x4*)(tile_of + deep * T * T + place(wi + 32 * y + n, wj + 32 * x + 8 * r + 4 * h)) =
                     f32x4{acc[x][y][4 * r], acc[x][y][4 * r + 1], acc[x][y][4 * r + 2], acc[x][y][4 * r + 3]};
     char* to = ws + (STEP == GRAM ? M.a : STEP == SQUARE ? M.b : odd ? M.x : M.y);
     const float by = STEP == GRAM ? kScaleA / (kScaleX * kScaleX) : STEP == SQUARE ? c * (kScaleB / (kScaleA * kScaleA)) : 1.f / kScaleB;
     const float more = STEP == SQUARE ? b * (kScaleB / kScaleA) : a;
+    constexpr bool AGAIN = STEP != GRAM || DEEP > 1;              // the transpose is stored from what was stored
     const bool mirrored = STEP != APPLY && ti != tj, again = STEP == APPLY ? LAST && M.tall : mirrored;
     __syncthreads();
 #pragma unroll
     for (int x = 0; x < PIECES; ++x) {
+        if (!has) break;
         const Piece p = piece_of(x);
         f32x8 z;
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
-            const f32x4 v = *(const f32x4*)(tile_of + place(p.row, p.col + 4 * q));
+            f32x4 v = *(const f32x4*)(tile_of + place(p.row, p.col + 4 * q));
+#pragma unroll
+            for (int d = 1; d < DEEP; ++d) v += *(const f32x4*)(tile_of + d * T * T + place(p.row, p.col + 4 * q));
 #pragma unroll
             for (int e = 0; e < 4; ++e) z[4 * q + e] = v[e] * by;
         }
@@ -335,7 +353,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_ortho_product(const OrthoTable 
         if constexpr (LAST) z *= 1.f / kScaleX;
         if constexpr (!LAST) store_piece(line_at(to, i0 + p.row, rows, (j0 + p.col) / 32), p, z);
         else if (!M.tall) store_row(M, i0 + p.row, j0 + p.col, z);
-        if constexpr (STEP != GRAM) {
+        if constexpr (AGAIN) {
             if (again)                               // each thread's own places
 #pragma unroll
                 for (int q = 0; q < 2; ++q)
@@ -343,13 +361,14 @@ __global__ __launch_bounds__(kThreads, 2) void k_ortho_product(const OrthoTable 
         }
     }
     if (!again) return;                              // the tile is also, or only, stored as its transpose
-    if constexpr (STEP != GRAM) __syncthreads();
+    if constexpr (AGAIN) __syncthreads();
 #pragma unroll 2
     for (int x = 0; x < PIECES; ++x) {
+        if (!has) break;
         const Piece p = piece_of(x);                 // of the transpose
         f32x8 z;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) z[e] = tile_of[place(p.col + e, p.row)] * (STEP == GRAM ? by : 1.f);
+        for (int e = 0; e < 8; ++e) z[e] = tile_of[place(p.col + e, p.row)] * (AGAIN ? 1.f : by);
         if constexpr (STEP == APPLY) store_row(M, j0 + p.row, i0 + p.col, z);
         else store_piece(line_at(to, j0 + p.row, rows, (i0 + p.col) / 32), p, z);
     }
@@ -375,7 +394,7 @@ template <class Depth> void share_out(const OrthoTable& t, OrthoEnds& ends, int6
 }
 
 // The matrices from `first` on that one series of launches takes, and what it needs.
-struct OrthoGroup { OrthoTable t; int64_t end, chunks, sides, squares, applies; size_t parts, bytes; int tile; };
+struct OrthoGroup { OrthoTable t; int64_t end, chunks, sides, squares, applies; size_t parts, table, bytes; int tile; };
 OrthoGroup group_from(int64_t first, int64_t n, const int64_t* rows, const int64_t* cols, const void* const* in, void* const* out,
                       const int32_t* dts) {
     OrthoGroup G = {};
@@ -419,6 +438,7 @@ OrthoGroup group_from(int64_t first, int64_t n, const int64_t* rows, const int64
         M.b = take(a);
     }
     G.parts = take(G.chunks * 8);
+    G.table = take(sizeof(OrthoTable));
     G.bytes = at;
     share_out(G.t, G.t.gram, G.squares, &OrthoMatrix::square0, [](const OrthoMatrix& M) { return M.np; });
     share_out(G.t, G.t.square, G.squares, &OrthoMatrix::square0, [](const OrthoMatrix& M) { return M.mp; });
@@ -433,21 +453,24 @@ unsigned groups_of(const OrthoEnds& ends) {
 }
 
 // Tiles of 128 x 128 leave room for two workgroups a CU, one storing while the other multiplies, with copies one k tile ahead; of
-// small matrices, in tiles of 64 x 64, the copies' latency is all there is: three ahead.
+// small matrices, in tiles of 64 x 64, the copies' latency is all there is: three ahead, or, where there is no more than one tile for
+// each CU, four groups of wavefronts at a tile (nine fp32 matrices of up to 640 x 256: 152 us without, 139 so, 155 with them also
+// where tiles are more).
 template <int STEP, bool LAST = false>
 hipError_t launch_product(const OrthoGroup& G, const OrthoEnds& ends, char* ws, int odd, int back, const float* k, hipStream_t st) {
     const dim3 grid(groups_of(ends));
-    if (G.tile == 128) k_ortho_product<128, 1, STEP, LAST><<<grid, kThreads, 0, st>>>(G.t, ws, odd, back, k[0], k[1], k[2]);
-    else k_ortho_product<64, 3, STEP, LAST><<<grid, kThreads, 0, st>>>(G.t, ws, odd, back, k[0], k[1], k[2]);
+    if (G.tile == 128) k_ortho_product<128, 1, 1, STEP, LAST><<<grid, kThreads, 0, st>>>((const OrthoTable*)(ws + G.table), ws, odd, back, k[0], k[1], k[2]);
+    else if (grid.x <= 256) k_ortho_product<64, 4, 1, STEP, LAST><<<grid, 4 * kThreads, 0, st>>>((const OrthoTable*)(ws + G.table), ws, odd, back, k[0], k[1], k[2]);
+    else k_ortho_product<64, 1, 3, STEP, LAST><<<grid, kThreads, 0, st>>>((const OrthoTable*)(ws + G.table), ws, odd, back, k[0], k[1], k[2]);
     return hipGetLastError();
 }
 
 hipError_t launch_group(const OrthoGroup& G, char* ws, int steps, const float* k, hipStream_t st) {
     double* parts = (double*)(ws + G.parts);
-    k_ortho_norm<<<dim3((unsigned)G.chunks), kThreads, 0, st>>>(G.t, parts);
+    k_ortho_norm<<<dim3((unsigned)G.chunks), kThreads, 0, st>>>(G.t, parts, (OrthoTable*)(ws + G.table));
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    k_ortho_in<<<dim3((unsigned)G.sides), kThreads, 0, st>>>(G.t, parts, ws);
+    k_ortho_in<<<dim3((unsigned)G.sides), kThreads, 0, st>>>((const OrthoTable*)(ws + G.table), parts, ws);
     e = hipGetLastError();
     for (int s = 0; s < steps && e == hipSuccess; ++s) {
         const int odd = s & 1;
