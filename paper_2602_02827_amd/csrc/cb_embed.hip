@@ -106,6 +106,10 @@ __global__ __launch_bounds__(kThreads) void k_embed(const W* table, int64_t tabl
 // only goes over its run again where there are more of them than it has room for.
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kMostRange = 960, kNoted = 512;
 
+// A token in 32 bits, which rows are counted in.
+constexpr uint32_t kNoToken = 0xffffffffu;
+__device__ __forceinline__ uint32_t in_32_bits(int64_t token) { return (uint64_t)token >> 32 ? kNoToken : (uint32_t)token; }
+
 __global__ __launch_bounds__(kSortThreads) void k_embed_sort(const int64_t* tokens, int n, int vocab, int range, int* starts, int* order) {
     extern __shared__ int place[];                   // [wavefront][row of the range]: counts, then next places
     __shared__ int below_of[kSortWaves], sums[kSortWaves];
@@ -123,28 +127,27 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(const int64_t* toke
     int below = 0, notes = 0;
     constexpr int AHEAD = 8;
     for (int i0 = begin; i0 < end; i0 += 64 * AHEAD) {
-        int64_t t[AHEAD];
+        int64_t t[AHEAD];                            // past the end: the last token, and none below
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) t[j] = end - i0 > 64 * j + lane ? tokens[(int64_t)i0 + 64 * j + lane] : -1;
+        for (int j = 0; j < AHEAD; ++j) t[j] = tokens[i0 + 64 * j + lane < end ? i0 + 64 * j + lane : end - 1];
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) {
-            below += t[j] >= 0 && t[j] < lo;
-            const bool mine = t[j] >= lo && t[j] < lo + rows;
+            const uint32_t x = i0 + 64 * j + lane < end ? in_32_bits(t[j]) : kNoToken, r = x - (uint32_t)lo;
+            below += __popcll(__ballot(x < (uint32_t)lo));
+            const bool mine = r < (uint32_t)rows;
             const uint64_t all = __ballot(mine);
             if (!all) continue;
             const int at = notes + __popcll(all & before_me);
             if (mine) {
-                atomicAdd(own + (int)(t[j] - lo), 1);
+                atomicAdd(own + r, 1);
                 if (at < kNoted) {
                     noted[wave][at] = i0 + 64 * j + lane;
-                    noted_row[wave][at] = (uint16_t)(t[j] - lo);
+                    noted_row[wave][at] = (uint16_t)r;
                 }
             }
             notes += __popcll(all);
         }
     }
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) below += __shfl_xor(below, m);
     if (lane == 0) below_of[wave] = below;
     __syncthreads();
     // a row's tokens of all wavefronts, then those of the rows before it
@@ -192,8 +195,8 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(const int64_t* toke
         return;
     }
     for (int i = begin; i < end; i += 64) {
-        const int64_t t = end - i > lane ? tokens[i + lane] : -1;
-        put(t >= lo && t < lo + rows ? (int)(t - lo) : -1, i + lane);
+        const uint32_t r = (end - i > lane ? in_32_bits(tokens[i + lane]) : kNoToken) - (uint32_t)lo;
+        put(r < (uint32_t)rows ? (int)r : -1, i + lane);
     }
 }
 
