@@ -201,6 +201,7 @@ size_t colbandit_sizeof_rotation(void);
  */
 int colbandit_rotary_table(int64_t n_positions, int d, double base, float *table);
 
+/* q_out, k_out: may be q and k, where these are dense; otherwise they overlap nothing. */
 int colbandit_norm_rotate(const colbandit_rotation *r, void *q_out, void *k_out, void *stream);
 /*
  * dq, dk from the gradients of the outputs; dq_weight, dk_weight DEVICE float [d], either may be

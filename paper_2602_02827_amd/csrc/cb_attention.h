@@ -926,6 +926,10 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
     }
 }
 
+// Where a sequence's chunk of kSinkRows rows leaves its shares.  Sequences of more than one chunk begin further apart than a chunk is
+// long, so that their first chunks have places of their own, and so have the others, which begin after them.
+__device__ __forceinline__ int64_t sink_place(const Range& rows, int chunk) { return 2 * (int64_t)(rows.lo / kSinkRows + chunk) + (chunk == 0); }
+
 // Gradients of keys and values, `run` key heads one after the other; workgroups from `main` on add up the bias table's shares
 // of all tiles.
 // A wavefront with both gradients of 32 wide rows takes more than half of the registers, so nothing runs beside its waits.
@@ -933,8 +937,8 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
 // where there were four), but two wavefronts share a SIMD (24 causal pages, forward and backward: 508 us, with one 828).
 template <class E, int D> constexpr bool kApart = sizeof(E) == 2 && D >= 96;
 // With a window the first keys are left to workgroups of their own (the first `sink_groups` ones), since all of a sequence's rows see
-// them: a key tile's others see some rows only.  Such a workgroup takes kSinkRows rows of a sequence, and leaves its shares of the first
-// keys' gradients to k_attention_join_sinks.  They are short, and come first, so that the others begin one after the other and do not
+// them: a key tile's others see some rows only.  Such a workgroup takes kSinkRows rows of a sequence, and, where the sequence has more,
+// leaves its shares of the first keys' gradients to k_attention_join_sinks.  They are short, and come first, so that the others begin one after the other and do not
 // leave most CUs idle where their number is a little more than that of the CUs.
 template <class E, int D, bool BIAS, bool MASKED, bool WIN>
 __global__ __launch_bounds__((kApart<E, D> ? 128 : 64) * kWavefronts, (kGradientWaves<E, D>)) void
@@ -1209,8 +1213,8 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int s
                             O::store4(to + dense + 32 * db + 8 * j + 4 * h, seen ? x : f32x4{0.f, 0.f, 0.f, 0.f});
                         }
                 };
-                if (WIN && sinks) {
-                    float* to = sink_part + (((int64_t)slot * A.kv_heads + kv) * A.sinks + key) * 2 * D;
+                if (WIN && sinks && qs.n > kSinkRows) {
+                    float* to = sink_part + ((sink_place(qs, (slot - qs.place)) * A.kv_heads + kv) * A.sinks + key) * 2 * D;
                     auto leave = [&](int which, const f32x16(&a)[DB], float by) {
 #pragma unroll
                         for (int db = 0; db < DB; ++db)
@@ -1253,7 +1257,8 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int s
     }
 }
 
-// Adds up the shares of the first keys' gradients: a wavefront for each of them and key head.
+// Adds up the shares of the first keys' gradients, in the order of the rows: a wavefront for each of them and key head.  Of sequences
+// without rows they are zeros.
 template <class E, int D>
 __global__ __launch_bounds__(256) void k_attention_join_sinks(const AttnArgs A, const float* part, E* dk, E* dv) {
     const int lane = threadIdx.x & 63;
@@ -1264,10 +1269,11 @@ __global__ __launch_bounds__(256) void k_attention_join_sinks(const AttnArgs A, 
     const Range ks = sequence_rows(A.koff, seq, A.total_k), qs = sequence_rows(A.qoff, seq, A.total_q, kSinkRows);
     if (key >= ks.n) return;
     const int parts = (qs.n + kSinkRows - 1) / kSinkRows;
+    if (parts == 1) return;                          // written as they are
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
     for (int p = 0; p < parts; ++p)
-        sum += *(const f32x4*)(part + (((int64_t)(qs.place + p) * A.kv_heads + kv) * A.sinks + key) * 2 * D + 4 * lane);
+        sum += *(const f32x4*)(part + ((sink_place(qs, p) * A.kv_heads + kv) * A.sinks + key) * 2 * D + 4 * lane);
     E* to = lane < D / 4 ? dk : dv;
     Oper<E>::store4(to + ((int64_t)(ks.lo + key) * A.kv_heads + kv) * D + 4 * (lane % (D / 4)), sum);
 }

@@ -71,7 +71,7 @@ AttnPlan plan_attention(const AttnArgs& A, int d, int dt, bool backward) {
         if (A.windowed && A.sinks) {
             const int64_t slots = A.total_q / kSinkRows + A.n_seqs, tile = 32 * kWavefronts;
             P.sink_groups = slots * A.kv_heads * ((A.sinks + tile - 1) / tile);
-            P.sink_part = take(slots * A.kv_heads * A.sinks * 2 * d * 4);
+            P.sink_part = take(2 * (A.total_q / kSinkRows + 1) * (int64_t)A.kv_heads * A.sinks * 2 * d * 4);
         }
     }
     P.bytes = o;

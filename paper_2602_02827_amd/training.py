@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+from operator import index
 
 import numpy as np
 import torch
@@ -188,7 +189,8 @@ def _window(window, sinks):
             raise ValueError("sinks come with a window")
         return None
     before, after = window
-    return ColbanditWindow(before, after, sinks)
+    most = 1 << 62                                   # (ctypes would cut what does not fit)
+    return ColbanditWindow(min(index(before), most), min(index(after), most), min(index(sinks), most))
 
 
 def _like(t):
@@ -349,7 +351,8 @@ def _rotation(q, k, positions, table, q_weight, k_weight, eps, interleaved, *mor
 def colbandit_norm_rotate(q, k, *, positions=None, table=None, q_weight=None, k_weight=None, eps=1e-6, interleaved=False, out=None):
     """q [rows, heads, d] and k [rows, kv_heads, d] (any row and head strides), each head divided by its root mean square, times
     the weights float32 [d], and rotated by `table` (colbandit_rotary_table) at `positions` int64 [rows]; rows whose position is none
-    of the table's get zeros.  `table` None: no rotation.  `out`: tensors to write, as this returns them.  Returns dict(q, k), dense."""
+    of the table's get zeros.  `table` None: no rotation.  `out`: tensors to write, as this returns them (q and k themselves, where
+    they are dense).  Returns dict(q, k), dense."""
     q_out, k_out = (_like(q), _like(k)) if out is None else (
         _dense(out["q"], q.shape, q.dtype, "q"), _dense(out["k"], k.shape, k.dtype, "k"))
     r, dev = _rotation(q, k, positions, table, q_weight, k_weight, eps, interleaved, q_out, k_out)
@@ -605,9 +608,13 @@ def orthogonal_step_(parameters, momenta, rate, momentum=0.95, steps=5, coeffici
     """One step of descent along orthogonalised momenta, for 2-d parameters: of each that has a gradient the momentum becomes
     momentum * itself + gradient, and the parameter goes down `rate` times sqrt(max(1, rows / columns)) times
     colbandit_orthogonalise of gradient + momentum * itself.  `momenta`: a dict of the parameters' momenta, which this fills."""
-    parameters = [p for p in dict.fromkeys(parameters) if p.grad is not None]
+    parameters = [p for p in dict.fromkeys(parameters) if p.grad is not None and p.numel()]
     if not parameters:
         return
+    for p in parameters:                             # before any momentum is changed
+        if p.dim() != 2 or p.dtype not in _DTYPES:
+            raise ValueError("parameters must be two-dimensional, and float32 or bfloat16")
+    _on_device(*parameters)
     updates = []
     with torch.no_grad():
         for p in parameters:

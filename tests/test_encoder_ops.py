@@ -355,6 +355,18 @@ def test_rotation_in_graphs_and_as_part_of_a_program(tr, dev):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_rotation_in_place(tr, dev, dtype, interleaved):
+    p, _, _ = rotation_problem(dev, dtype, 130, 5, 2, 96, seed=12)
+    how = dict(positions=p["positions"], table=tr.colbandit_rotary_table(50, 96), q_weight=p["q_weight"], interleaved=interleaved)
+    q, k = p["q"].contiguous(), p["k"].contiguous()
+    want = tr.colbandit_norm_rotate(q, k, **how)
+    got = tr.colbandit_norm_rotate(q, k, out={"q": q, "k": k}, **how)
+    assert got["q"] is q and torch.equal(q, want["q"]) and torch.equal(k, want["k"])
+
+
+@gpu
 def test_rotation_gradients_against_differences(tr, dev):
     p, dq, dk = rotation_problem(dev, "f32", 9, 2, 1, 32, seed=9)
     table = tr.colbandit_rotary_table(50, 32)
@@ -541,6 +553,16 @@ def test_windows_in_long_sequences(tr, dev, dtype, causal, window, sinks, keep):
 
 @gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("ql", [[513, 512, 514, 511], [1, 600, 2, 1100, 0, 513], [700, 700]])
+def test_first_keys_of_sequences_of_several_chunks(tr, dev, dtype, ql):
+    """Chunks of 512 rows: sequences of one, of two, and of a row more, one after the other."""
+    kl = [n + 3 for n in ql]
+    p = window_problem(dev, dtype, ql, kl, 2, 2, 32, seed=14)
+    check_window(tr, p, ql, kl, dtype, False, (3, 2), 5)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("d,H,Hk,keep", [(128, 8, 2, False), (64, 4, 4, True)])
 @pytest.mark.parametrize("window,sinks", [((1023, 0), 4), ((3, 0), 0), ((100000, 0), 0)])
 def test_single_tokens_through_a_window(tr, dev, dtype, d, H, Hk, keep, window, sinks):
@@ -561,6 +583,9 @@ def test_a_window_over_everything_is_no_window(tr, dev, dtype, causal):
     for window, sinks in (((1 << 62, 1 << 40), 0), ((600, 600), 7), ((0, 0), 600)):
         g, _ = check_window(tr, p, ql, ql, dtype, causal, window, sinks)
         assert float((g["out"].float() - f["out"].float()).abs().max()) <= 2 * U[dtype] * 4 + 1e-4
+    wide = tr.colbandit_attention(p["q"], p["k"], p["v"], off, causal=causal, keep=p["keep"], window=(1 << 70, 1 << 64))
+    whole = tr.colbandit_attention(p["q"], p["k"], p["v"], off, causal=causal, keep=p["keep"], window=(1 << 62, 1 << 62))
+    assert torch.equal(wide["out"], whole["out"]) and torch.equal(wide["lse"], whole["lse"])
 
 
 @gpu
@@ -753,6 +778,15 @@ def test_orthogonalising_in_place_in_graphs_and_steps(tr, dev):
     p = [torch.nn.Parameter(torch.zeros(30, 20, device=dev)), torch.nn.Parameter(torch.zeros(20, 30, device=dev)),
          torch.nn.Parameter(torch.zeros(4, 4, device=dev))]
     momenta = {}
+    with pytest.raises(ValueError, match="two-dimensional"):
+        flat = torch.nn.Parameter(torch.zeros(4, device=dev))
+        flat.grad = torch.ones(4, device=dev)
+        p[0].grad = torch.ones(30, 20, device=dev)
+        tr.orthogonal_step_([p[0], flat], momenta, rate=0.1)
+    assert not momenta and not bool(p[0].any())
+    empty = torch.nn.Parameter(torch.zeros(0, 4, device=dev))
+    empty.grad = torch.zeros(0, 4, device=dev)
+    tr.orthogonal_step_([empty], momenta, rate=0.1)
     grads = updates([(30, 20), (20, 30)], "f32", dev, seed=8)
     for _ in range(2):
         p[0].grad, p[1].grad = grads[0].clone(), grads[1].clone()
