@@ -40,8 +40,10 @@ __device__ __forceinline__ void fill_bias(const AttnArgs& A, int head, const int
         const int i = behind ? b - A.n_dir : b;
         const float z = (float)((const E*)A.bias)[(int64_t)b * A.heads + head];
         const int end = starts[i + 1];
-        for (int j = starts[i] + (tid & 7); j < end; j += 8)
-            if (!behind) table[middle - j] = z; else if (j > 0) table[middle + j] = z;
+        int j = starts[i] + (tid & 7);
+        if (behind && j == 0) j = 8;                  // (distance 0 is not behind)
+        const int step = behind ? 8 : -8;
+        for (float* to = table + middle + (behind ? j : -j); j < end; j += 8, to += step) *to = z;
         if (A.causal && b == 0)                       // no row sees a key behind it: as distance 0
             for (int j = 1 + (tid & 7); j <= middle; j += 8) table[middle + j] = z;
     }
@@ -271,6 +273,29 @@ __device__ __forceinline__ f32x16 of_rows(const float* v, int b, int h) {
         for (int i = 0; i < 4; ++i) x[4 * j + i] = y[i];
     }
     return x;
+}
+
+// Products of a block's rows with the wavefront's columns.  The compiler, which would save registers, asks for an operand before its
+// product, which then waits for it: a third wavefront on the SIMD goes on meanwhile, a second one often waits as well.  EARLY: operands
+// are asked for three products ahead.
+template <class T, bool EARLY, bool TURNED = false, int N>
+__device__ __forceinline__ void add_rows(f32x16& x, const typename T::At& t, int b, const typename T::Frag (&own)[N]) {
+    if constexpr (EARLY) {
+        constexpr int AHEAD = 3;
+        typename T::Frag f[N];
+#pragma unroll
+        for (int c = 0; c < AHEAD && c < N; ++c) f[c] = T::rows(t, b, c);
+        in_turn();
+#pragma unroll
+        for (int c = 0; c < N; ++c) {
+            T::O::template mma<TURNED>(x, f[c], own[c]);
+            if (c + AHEAD < N) f[c + AHEAD] = T::rows(t, b, c + AHEAD);
+            in_turn();
+        }
+    } else {
+#pragma unroll
+        for (int c = 0; c < N; ++c) T::O::template mma<TURNED>(x, T::rows(t, b, c), own[c]);
+    }
 }
 
 // Rows of a block that a lane's column sees under a limit, as bits: a lane's rows lie at 8 (r / 4) + r % 4 from its first one.  One
@@ -625,6 +650,7 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
                float* delta, float* bias_part) {
     using O = Oper<E>;
     using T = Tile<E, D>;
+    constexpr bool EARLY = sizeof(E) == 2 && kQueryWaves<E, D> < 3;
     constexpr int NB = T::ROWS / 32, DB = D / 32, THREADS = 64 * kWavefronts;
     __shared__ __align__(256) char lds[2][2 * T::BYTES];
     __shared__ __align__(16) float hidden[2][T::ROWS];
@@ -759,13 +785,11 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
                 if constexpr (WIN)
                     if (!win.some(base + 32 * b, 32)) continue;
                 f32x16 s = {}, dp;
-#pragma unroll
-                for (int c = 0; c < D / 16; ++c) O::mma(s, T::rows(lk, b, c), q.v[c]);
+                add_rows<T, EARLY>(s, lk, b, q.v);
                 phase();
 #pragma unroll
                 for (int r = 0; r < 16; ++r) dp[r] = -dot;
-#pragma unroll
-                for (int c = 0; c < D / 16; ++c) O::mma(dp, T::rows(lv, b, c), g.v[c]);
+                add_rows<T, EARLY>(dp, lv, b, g.v);
                 phase();
                 const int d0 = base + 32 * b - w.first_lim, side = BIAS ? block_side(d0, A.reach) : 0;
                 if (BIAS && !side) {
@@ -825,11 +849,22 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
 #pragma unroll
                         for (int e = 0; e < 8; ++e) most[e] = __uint_as_float(__float_as_uint(x[e]) & 0xffff0000u);
                         const typename O::Frag p = O::round(most), rest = O::round(x - most);
+                        if constexpr (EARLY) {
+                            typename O::Frag f[DB];
 #pragma unroll
-                        for (int db = 0; db < DB; ++db) {
-                            const typename O::Frag x = T::turned(lk, b, c, db);
-                            O::mma(acc[db], x, rest);
-                            O::mma(acc[db], x, p);
+                            for (int db = 0; db < DB; ++db) f[db] = T::turned(lk, b, c, db);
+                            in_turn();
+#pragma unroll
+                            for (int db = 0; db < DB; ++db) O::mma(acc[db], f[db], rest);
+#pragma unroll
+                            for (int db = 0; db < DB; ++db) O::mma(acc[db], f[db], p);
+                        } else {
+#pragma unroll
+                            for (int db = 0; db < DB; ++db) {
+                                const typename O::Frag x = T::turned(lk, b, c, db);
+                                O::mma(acc[db], x, rest);
+                                O::mma(acc[db], x, p);
+                            }
                         }
                     }
                 } else {
@@ -933,8 +968,10 @@ __device__ __forceinline__ int64_t sink_place(const Range& rows, int chunk) { re
 // Gradients of keys and values, `run` key heads one after the other; workgroups from `main` on add up the bias table's shares
 // of all tiles.
 // A wavefront with both gradients of 32 wide rows takes more than half of the registers, so nothing runs beside its waits.
-// In 16 bits wide heads have two wavefronts for the same rows, one for either gradient: the scores are made twice (five products
-// where there were four), but two wavefronts share a SIMD (24 causal pages, forward and backward: 508 us, with one 828).
+// In 16 bits wide heads have two wavefronts for the same rows, one for either gradient, so that two share a SIMD (24 causal pages,
+// forward and backward: 508 us, with one 828).  The values' one makes the probabilities and hands them over in LDS, in 32 bits; the
+// keys' one is a block of 32 rows behind, which costs a barrier a block and a third tile in LDS (500 us where both make the scores and
+// take their exponentials; so 476, and 456 with operands asked for ahead).
 template <class E, int D> constexpr bool kApart = sizeof(E) == 2 && D >= 96;
 // With a window the first keys are left to workgroups of their own (the first `sink_groups` ones), since all of a sequence's rows see
 // them: a key tile's others see some rows only.  Such a workgroup takes kSinkRows rows of a sequence, and, where the sequence has more,
@@ -945,14 +982,16 @@ __global__ __launch_bounds__((kApart<E, D> ? 128 : 64) * kWavefronts, (kGradient
 k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int sink_groups, int q_slots, const E* dout, const float* lse,
                 const float* delta, const float* bias_part, E* dk, E* dv, E* dbias, float* sink_part) {
     using O = Oper<E>;
-    using T = Tile<E, D, kApart<E, D> ? 128 : Oper<E>::ROWS>;
+    using T = Tile<E, D>;
     constexpr int NB = T::ROWS / 32, DB = D / 32, COLS = 32 * kWavefronts;
     constexpr bool APART = kApart<E, D>;
+    constexpr int BUFS = APART ? 3 : 2;               // tiles in LDS
     constexpr int WAVES = APART ? 2 * kWavefronts : kWavefronts, THREADS = 64 * WAVES;
     const bool keys = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) >= kWavefronts;        // (APART) this wavefront has the keys' gradient
-    __shared__ __align__(256) char lds[2][2 * T::BYTES];
-    __shared__ __align__(16) float row_lse[2][T::ROWS], row_delta[2][T::ROWS], row_far[2][2][T::ROWS];
-    __shared__ int tile_far[2][(T::ROWS + 63) / 64];  // of 64 rows, some row is far: row_far has log-sum-exps, and what is added to far rows' exponents
+    __shared__ __align__(256) char lds[BUFS][2 * T::BYTES];
+    __shared__ __align__(16) float row_lse[BUFS][T::ROWS], row_delta[BUFS][T::ROWS], row_far[BUFS][2][T::ROWS];
+    __shared__ int tile_far[BUFS];                    // some row is far: row_far has log-sum-exps, and what is added to far rows' exponents
+    __shared__ f32x4 handed[APART ? 2 : 1][APART ? kWavefronts : 1][4][64];      // (APART) a block's probabilities
     extern __shared__ __align__(16) char dyn[];
     const int tid = threadIdx.x, lane0 = tid & 63, lane = lane0, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     if constexpr (BIAS) {
@@ -1083,7 +1122,7 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int s
             }
             row_lse[buf][tid] = far ? 0.f : add;
             row_delta[buf][tid] = -n_delta;
-            if (lane0 == 0) tile_far[buf][wave] = far;
+            if (tid == 0) tile_far[buf] = far;
         }
     };
     int head0 = kv0 * A.group, c0 = col0;
@@ -1091,11 +1130,15 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int s
     const int head_end = kv_end * A.group;
     const bool any = col0 < cols;
     if (any) issue(head0, c0, at_c0, lds[0]);
-    Column<E, D> k, v;
+    Column<E, D> k, v;                                // (APART) k: the wavefront's own, of keys or of values
     auto load_keys = [&](int kv) {
-        k.load((const E*)A.k + at * A.k_row + kv * A.k_head, seen, h);
-        k.take_sign(A.scale);
-        if (!APART || keys) v.load((const E*)A.v + at * A.v_row + kv * A.v_head, seen, h);
+        if (APART && keys) {
+            k.load((const E*)A.v + at * A.v_row + kv * A.v_head, seen, h);
+        } else {
+            k.load((const E*)A.k + at * A.k_row + kv * A.k_head, seen, h);
+            k.take_sign(A.scale);
+        }
+        if constexpr (!APART) v.load((const E*)A.v + at * A.v_row + kv * A.v_head, seen, h);
     };
     load_keys(kv0);
     f32x16 acc[DB] = {}, acc2[APART ? 1 : DB] = {};              // of keys and of values, or of the wavefront's own
@@ -1111,92 +1154,132 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int s
     if (any) finish(0, head0, at_c0);
     __syncthreads();
     const typename T::At at_tiles(lds[0], lane);
+    // Of block b of the tile in `buf`, whose rows are the columns from c0 on: scores' probabilities,
+    auto exponentials = [&](f32x16& s, int buf, int b, bool far, bool diagonal) {
+        if constexpr (BIAS) {
+            const int d0 = wkey - (c0 + 32 * b + shift), side = block_side(d0, A.reach);
+            if (!side) {
+                const float* x = table + middle + key - (c0 + 32 * b + shift) - 4 * h - 27;    // of the lane's last row
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], unit_scale, x[27 - 8 * (r >> 2) - (r & 3)]);
+            } else {
+                const float x = table[side < 0 ? 0 : 2 * middle];
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], unit_scale, x);
+            }
+        }
+        if (far) {
+            const f32x16 from = of_rows(row_far[buf][0], b, h), x = of_rows(row_far[buf][1], b, h);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = fmaf((BIAS ? s[r] : rounded_product(s[r], unit_scale)) - from[r], LOG2E, x[r]);
+        } else if constexpr (START) {
+            s *= per_unit;
+        } else {
+            const f32x16 x = of_rows(row_lse[buf], b, h);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], per_unit, x[r]);
+        }
+        if (diagonal) {                               // a lane's key is seen by columns from (key - shift) G on
+            uint32_t own;
+            if constexpr (WIN) {
+                const int from = c0 + 32 * b + 4 * h;
+                own = bits_up_to(see_to - 1 - from) & ~bits_up_to(see_from - 1 - from);
+            } else {
+                own = ~bits_up_to((key - shift) * G - c0 - 32 * b - 4 * h - 1);
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = hidden_unless(s[r], all_if(own, r));
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = exp2_fast(s[r]);
+    };
+    // and what the block adds to a gradient.
+    auto add_up = [&](f32x16(&to)[DB], const typename T::At& t, int b, const f32x16& x) {
+        const typename O::Frag p0 = O::round(eight<0>(x)), p1 = O::round(eight<8>(x));
+        phase();
+#pragma unroll
+        for (int db = 0; db < DB; ++db) O::mma(to[db], T::turned(t, b, 0, db), p0);
+#pragma unroll
+        for (int db = 0; db < DB; ++db) O::mma(to[db], T::turned(t, b, 1, db), p1);
+    };
+    // (APART) The keys' wavefronts are a block behind, whose probabilities have been handed over; held: its tile's buffer and its number,
+    // or none that the wavefront's keys are seen by.
+    int held = -1, turn = 0;
     int buf = 0;
     while (true) {
         settle<E>();
         const bool last_tile = c0 + T::ROWS >= cols;
-        const int n_head = last_tile ? head0 + G : head0, n_c = last_tile ? col0 : c0 + T::ROWS;
+        const int n_head = last_tile ? head0 + G : head0, n_c = last_tile ? col0 : c0 + T::ROWS, n_buf = buf + 1 < BUFS ? buf + 1 : 0;
         Place n_place = {at_c0.row + step.row, at_c0.c + step.c};
         if (n_place.c >= G) n_place = {n_place.row + 1, n_place.c - G};
         if (last_tile) n_place = first_place;
         const bool last = last_tile && n_head % A.group == 0;                           // of a key head
         const bool more = kRuns<D> ? n_head < head_end : !last;
-        if (more && any) issue(n_head, n_c, n_place, lds[buf ^ 1]);
+        if (more && any) issue(n_head, n_c, n_place, lds[n_buf]);
         const typename T::At lq = at_tiles + buf * 2 * T::BYTES, lg = lq + T::BYTES;
-        if (any && busy && c0 + T::ROWS > wfirst && (!WIN || c0 < wend)) {
+        const bool seen_by = busy && c0 + T::ROWS > wfirst && (!WIN || c0 < wend);      // some of the wavefront's keys, by some of the rows
+        if (any && (APART || seen_by)) {
             bool diagonal;
             if constexpr (WIN) diagonal = c0 < all_from || c0 + T::ROWS > all_to;
             else diagonal = A.causal && (wkey + 31 - shift) * G > c0;
-            const typename T::At own = APART && !keys ? lg : lq;           // (own gradient's other operand)
+            const int blocks = WIN && !APART ? (wend - c0 + 31) / 32 : (cols - c0 + 31) / 32, all = blocks < NB ? blocks : NB;
 #pragma unroll 1
-            for (int b = 0; b < NB && c0 + 32 * b < (WIN ? wend : cols); ++b) {
-                if constexpr (WIN)
-                    if (c0 + 32 * b + 32 <= wfirst) continue;
-                f32x16 s = {}, dp = {};
-                const bool far = __builtin_amdgcn_readfirstlane(tile_far[buf][b >> 1]) != 0;
-                if constexpr (START) s = of_rows(row_lse[buf], b, h);
-#pragma unroll
-                for (int c = 0; c < D / 16; ++c) O::template mma<true>(s, T::rows(lq, b, c), k.v[c]);
-                phase();
-                if (!APART || keys) {
-                    if constexpr (START) dp = of_rows(row_delta[buf], b, h);
-#pragma unroll
-                    for (int c = 0; c < D / 16; ++c) O::mma(dp, T::rows(lg, b, c), v.v[c]);
-                    phase();
-                }
-                if constexpr (!START) dp += of_rows(row_delta[buf], b, h);
-                if constexpr (BIAS) {
-                    const int d0 = wkey - (c0 + 32 * b + shift), side = block_side(d0, A.reach);
-                    if (!side) {
-                        const float* x = table + middle + key - (c0 + 32 * b + shift) - 4 * h - 27;    // of the lane's last row
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], unit_scale, x[27 - 8 * (r >> 2) - (r & 3)]);
-                    } else {
-                        const float x = table[side < 0 ? 0 : 2 * middle];
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], unit_scale, x);
-                    }
-                }
-                if (far) {
-                    const f32x16 from = of_rows(row_far[buf][0], b, h), x = of_rows(row_far[buf][1], b, h);
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) s[r] = fmaf((BIAS ? s[r] : rounded_product(s[r], unit_scale)) - from[r], LOG2E, x[r]);
-                } else if constexpr (START) {
-                    s *= per_unit;
-                } else {
-                    const f32x16 x = of_rows(row_lse[buf], b, h);
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], per_unit, x[r]);
-                }
-                if (diagonal) {                       // a lane's key is seen by columns from (key - shift) G on
-                    uint32_t own;
-                    if constexpr (WIN) {
-                        const int from = c0 + 32 * b + 4 * h;
-                        own = bits_up_to(see_to - 1 - from) & ~bits_up_to(see_from - 1 - from);
-                    } else {
-                        own = ~bits_up_to((key - shift) * G - c0 - 32 * b - 4 * h - 1);
-                    }
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) s[r] = hidden_unless(s[r], all_if(own, r));
-                }
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = exp2_fast(s[r]);
+            for (int b = 0; b < all + (APART && last); ++b) {
+                const bool on = !WIN || (c0 + 32 * b + 32 > wfirst && c0 + 32 * b < wend);
                 if constexpr (!APART) {
-                    const typename O::Frag p0 = O::round(eight<0>(s)), p1 = O::round(eight<8>(s));
+                    if (!on) continue;
+                    f32x16 s = {}, dp = {};
+                    const bool far = __builtin_amdgcn_readfirstlane(tile_far[buf]) != 0;
+                    if constexpr (START) s = of_rows(row_lse[buf], b, h);
+                    add_rows<T, false, true>(s, lq, b, k.v);
                     phase();
-#pragma unroll
-                    for (int db = 0; db < DB; ++db) O::mma(acc2[db], T::turned(lg, b, 0, db), p0);
-#pragma unroll
-                    for (int db = 0; db < DB; ++db) O::mma(acc2[db], T::turned(lg, b, 1, db), p1);
+                    if constexpr (START) dp = of_rows(row_delta[buf], b, h);
+                    add_rows<T, false>(dp, lg, b, v.v);
                     phase();
+                    if constexpr (!START) dp += of_rows(row_delta[buf], b, h);
+                    exponentials(s, buf, b, far, diagonal);
+                    add_up(acc2, lg, b, s);
+                    phase();
+                    s *= dp;
+                    add_up(acc, lq, b, s);
+                } else {
+                    if (b) __syncthreads();
+                    const int now = b < all && seen_by && on ? buf * NB + b : -1, own = keys ? held : now;
+                    if (own >= 0) {
+                        const int of = own / NB, block = own % NB;
+                        const typename T::At scored = at_tiles + (2 * of + keys) * T::BYTES, added = at_tiles + (2 * of + !keys) * T::BYTES;
+                        const bool far = __builtin_amdgcn_readfirstlane(tile_far[buf]) != 0;
+                        f32x16 x = of_rows(keys ? row_delta[of] : row_lse[of], block, h);
+                        add_rows<T, true>(x, scored, block, k.v);
+                        phase();
+                        typename O::Frag f[2][DB];
+#pragma unroll
+                        for (int db = 0; db < DB; ++db) f[0][db] = T::turned(added, block, 0, db);
+                        phase();
+                        if (keys) {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const f32x4 p = handed[turn ^ 1][wave % kWavefronts][j][lane0];
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) x[4 * j + i] *= p[i];
+                            }
+                        } else {
+                            exponentials(x, buf, b, far, diagonal);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) handed[turn][wave % kWavefronts][j][lane0] = f32x4{x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]};
+                        }
+                        const typename O::Frag p0 = O::round(eight<0>(x)), p1 = O::round(eight<8>(x));
+#pragma unroll
+                        for (int db = 0; db < DB; ++db) f[1][db] = T::turned(added, block, 1, db);
+                        phase();
+#pragma unroll
+                        for (int db = 0; db < DB; ++db) O::mma(acc[db], f[0][db], p0);
+#pragma unroll
+                        for (int db = 0; db < DB; ++db) O::mma(acc[db], f[1][db], p1);
+                    }
+                    held = now;
+                    turn ^= 1;
                 }
-                if (!APART || keys) s *= dp;
-                const typename O::Frag p0 = O::round(eight<0>(s)), p1 = O::round(eight<8>(s));
-                phase();
-#pragma unroll
-                for (int db = 0; db < DB; ++db) O::mma(acc[db], T::turned(own, b, 0, db), p0);
-#pragma unroll
-                for (int db = 0; db < DB; ++db) O::mma(acc[db], T::turned(own, b, 1, db), p1);
             }
         }
         if (last) {
@@ -1244,7 +1327,7 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int s
                 if constexpr (!APART) acc2[db] = {};
             }
         }
-        if (more && any) finish(buf ^ 1, n_head, n_place);
+        if (more && any) finish(n_buf, n_head, n_place);
         __syncthreads();
         if (BIAS && n_head != head0) {
             fill_bias<E>(A, n_head, starts, table, tid, THREADS);
@@ -1253,7 +1336,7 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int s
         head0 = n_head;
         c0 = n_c;
         at_c0 = n_place;
-        buf ^= 1;
+        buf = n_buf;
     }
 }
 

@@ -113,7 +113,8 @@ __device__ __forceinline__ bf16x8 read_turned(lds_ptr p, lds_ptr q) {
 
 // A tile: one plane, or one of each piece.  R rows of it.
 template <class E, int D, int R = Oper<E>::ROWS> struct Tile {
-    using Frag = typename Oper<E>::Frag;
+    using O = Oper<E>;
+    using Frag = typename O::Frag;
     static constexpr int ROWS = R, PLANES = sizeof(E) == 2 ? 1 : 3;
     using P = Plane<ROWS, D>;
     static constexpr int PIECES = P::PIECES, BYTES = PLANES * P::BYTES;
@@ -161,6 +162,8 @@ __device__ __forceinline__ int here(int x) {
 
 // The compiler moves nothing across: operands of the next products are not read while the registers are needed for these.
 __device__ __forceinline__ void phase() { __builtin_amdgcn_sched_barrier(0); }
+// Matrix instructions and LDS accesses stay on their side, others may move across.
+__device__ __forceinline__ void in_turn() { __builtin_amdgcn_sched_barrier(0x406); }
 
 // Sixteen bytes a lane from memory to LDS without registers: lane i's, from base + offset, go to dst + 16 i (base, dst: the same for
 // the wavefront).  Every copy is waited for, and followed by a barrier, before its bytes are read and before the wavefront ends.
