@@ -127,7 +127,8 @@ int colbandit_attention_backward(const colbandit_attn *a, const void *out, const
  *   seen   : as above, and (p_i - before <= j <= p_i + after or j < sinks)
  * Under a causal limit `after` says nothing.  Keys and values that the mask leaves are finite
  * (also those that no row's window reaches).  Rows: at most 2^28.  The gradients' workgroups for
- * the first keys count towards a launch's, one for 512 rows of a sequence and each key head.
+ * the first keys count towards a launch's, one for 128 to 512 rows of a sequence, each key head and
+ * 64 to 128 first keys.
  */
 #define COLBANDIT_MAX_SINKS 1024
 typedef struct {

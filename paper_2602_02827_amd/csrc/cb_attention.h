@@ -961,9 +961,9 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
     }
 }
 
-// Where a sequence's chunk of kSinkRows rows leaves its shares.  Sequences of more than one chunk begin further apart than a chunk is
+// Where a sequence's chunk of A.sink_rows rows leaves its shares.  Sequences of more than one chunk begin further apart than a chunk is
 // long, so that their first chunks have places of their own, and so have the others, which begin after them.
-__device__ __forceinline__ int64_t sink_place(const Range& rows, int chunk) { return 2 * (int64_t)(rows.lo / kSinkRows + chunk) + (chunk == 0); }
+__device__ __forceinline__ int64_t sink_place(const Range& rows, int chunk, int per) { return 2 * (int64_t)(rows.lo / per + chunk) + (chunk == 0); }
 
 // Gradients of keys and values, `run` key heads one after the other; workgroups from `main` on add up the bias table's shares
 // of all tiles.
@@ -972,26 +972,30 @@ __device__ __forceinline__ int64_t sink_place(const Range& rows, int chunk) { re
 // forward and backward: 508 us, with one 828).  The values' one makes the probabilities and hands them over in LDS, in 32 bits; the
 // keys' one is a block of 32 rows behind, which costs a barrier a block and a third tile in LDS (500 us where both make the scores and
 // take their exponentials; so 476, and 456 with operands asked for ahead).
-template <class E, int D> constexpr bool kApart = sizeof(E) == 2 && D >= 96;
+// Through a window such a workgroup has 64 key rows instead of 128, and tiles of 32 rows: two share a CU, and fewer rows that see only
+// some of its keys are gone over (26 pages of 1,030 tokens, 6 heads of 128, 64 to either side, with gradients: 258 and 241 us; without
+// a window, where each goes over all rows, 24 causal pages 456 and 468, of heads of 96 with a bias 705 and 753).
+template <class E, int D> constexpr bool kApart = two_for_keys(D, sizeof(E));
+template <class E, int D, bool WIN> constexpr int kKeyWaves = kApart<E, D> && !WIN ? 2 * kWavefronts : kWavefronts;
 // With a window the first keys are left to workgroups of their own (the first `sink_groups` ones), since all of a sequence's rows see
-// them: a key tile's others see some rows only.  Such a workgroup takes kSinkRows rows of a sequence, and, where the sequence has more,
-// leaves its shares of the first keys' gradients to k_attention_join_sinks.  They are short, and come first, so that the others begin one after the other and do not
-// leave most CUs idle where their number is a little more than that of the CUs.
+// them: a key tile's others see some rows only.  Such a workgroup takes A.sink_rows rows of a sequence, and, where the sequence has
+// more, leaves its shares of the first keys' gradients to k_attention_join_sinks.  They come first: the others, which are all of about
+// one length, then do not begin at the same time, nor end so.
 template <class E, int D, bool BIAS, bool MASKED, bool WIN>
-__global__ __launch_bounds__((kApart<E, D> ? 128 : 64) * kWavefronts, (kGradientWaves<E, D>)) void
+__global__ __launch_bounds__(64 * (kKeyWaves<E, D, WIN>), (kGradientWaves<E, D>)) void
 k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int sink_groups, int q_slots, const E* dout, const float* lse,
                 const float* delta, const float* bias_part, E* dk, E* dv, E* dbias, float* sink_part) {
     using O = Oper<E>;
-    using T = Tile<E, D>;
-    constexpr int NB = T::ROWS / 32, DB = D / 32, COLS = 32 * kWavefronts;
     constexpr bool APART = kApart<E, D>;
+    using T = Tile<E, D, APART && WIN ? 32 : Oper<E>::ROWS>;
+    constexpr int WAVES = kKeyWaves<E, D, WIN>, GROUPS = APART ? WAVES / 2 : WAVES;      // of 32 key rows
+    constexpr int NB = T::ROWS / 32, DB = D / 32, COLS = 32 * GROUPS, THREADS = 64 * WAVES;
     constexpr int BUFS = APART ? 3 : 2;               // tiles in LDS
-    constexpr int WAVES = APART ? 2 * kWavefronts : kWavefronts, THREADS = 64 * WAVES;
-    const bool keys = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) >= kWavefronts;        // (APART) this wavefront has the keys' gradient
+    const bool keys = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) >= GROUPS;        // (APART) this wavefront has the keys' gradient
     __shared__ __align__(256) char lds[BUFS][2 * T::BYTES];
     __shared__ __align__(16) float row_lse[BUFS][T::ROWS], row_delta[BUFS][T::ROWS], row_far[BUFS][2][T::ROWS];
     __shared__ int tile_far[BUFS];                    // some row is far: row_far has log-sum-exps, and what is added to far rows' exponents
-    __shared__ f32x4 handed[APART ? 2 : 1][APART ? kWavefronts : 1][4][64];      // (APART) a block's probabilities
+    __shared__ f32x4 handed[APART ? 2 : 1][APART ? GROUPS : 1][4][64];      // (APART) a block's probabilities
     extern __shared__ __align__(16) char dyn[];
     const int tid = threadIdx.x, lane0 = tid & 63, lane = lane0, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     if constexpr (BIAS) {
@@ -1027,12 +1031,12 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int s
         kv0 = x % inner % A.kv_heads;
         kv_end = kv0 + 1;
         key0 = x % inner / A.kv_heads * COLS;
-        seq = find_sequence(A.qoff, A.n_seqs, kSinkRows, A.total_q, slot, lane);
-        qs = rows_of_place(A.qoff, seq, A.n_seqs, A.total_q, kSinkRows, slot, rest);
+        seq = find_sequence(A.qoff, A.n_seqs, A.sink_rows, A.total_q, slot, lane);
+        qs = rows_of_place(A.qoff, seq, A.n_seqs, A.total_q, A.sink_rows, slot, rest);
         if (rest) return;
         ks = sequence_rows(A.koff, seq, A.total_k);
     }
-    const int wkey = key0 + wave % kWavefronts * 32, key = wkey + (lane & 31), shift = ks.n - qs.n;
+    const int wkey = key0 + wave % GROUPS * 32, key = wkey + (lane & 31), shift = ks.n - qs.n;
     const int G = A.pack;
     int key_from = 0, key_to = ks.n;                              // keys that are this workgroup's
     int cols = qs.n * G;
@@ -1043,7 +1047,7 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int s
     if constexpr (WIN) {
         auto row = [&](int r) { return r < 0 ? 0 : r > qs.n ? qs.n : r; };      // ends of ranges of rows
         if (sinks) {
-            const int begin = (slot - qs.place) * kSinkRows, end = row(begin + kSinkRows);
+            const int begin = (slot - qs.place) * A.sink_rows, end = row(begin + A.sink_rows);
             key_to = A.sinks < ks.n ? A.sinks : ks.n;
             if (begin < 0 || begin >= qs.n || key0 >= key_to) return;
             const int from = A.causal ? row(key0 - shift) : 0;
@@ -1259,14 +1263,14 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int s
                         if (keys) {
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
-                                const f32x4 p = handed[turn ^ 1][wave % kWavefronts][j][lane0];
+                                const f32x4 p = handed[turn ^ 1][wave % GROUPS][j][lane0];
 #pragma unroll
                                 for (int i = 0; i < 4; ++i) x[4 * j + i] *= p[i];
                             }
                         } else {
                             exponentials(x, buf, b, far, diagonal);
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) handed[turn][wave % kWavefronts][j][lane0] = f32x4{x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]};
+                            for (int j = 0; j < 4; ++j) handed[turn][wave % GROUPS][j][lane0] = f32x4{x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]};
                         }
                         const typename O::Frag p0 = O::round(eight<0>(x)), p1 = O::round(eight<8>(x));
 #pragma unroll
@@ -1296,8 +1300,8 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int s
                             O::store4(to + dense + 32 * db + 8 * j + 4 * h, seen ? x : f32x4{0.f, 0.f, 0.f, 0.f});
                         }
                 };
-                if (WIN && sinks && qs.n > kSinkRows) {
-                    float* to = sink_part + ((sink_place(qs, (slot - qs.place)) * A.kv_heads + kv) * A.sinks + key) * 2 * D;
+                if (WIN && sinks && qs.n > A.sink_rows) {
+                    float* to = sink_part + ((sink_place(qs, slot - qs.place, A.sink_rows) * A.kv_heads + kv) * A.sinks + key) * 2 * D;
                     auto leave = [&](int which, const f32x16(&a)[DB], float by) {
 #pragma unroll
                         for (int db = 0; db < DB; ++db)
@@ -1349,14 +1353,14 @@ __global__ __launch_bounds__(256) void k_attention_join_sinks(const AttnArgs A, 
     const int64_t of = place / A.sinks;
     const int key = (int)(place - of * A.sinks), seq = (int)(of / A.kv_heads), kv = (int)(of % A.kv_heads);
     if (seq >= A.n_seqs || lane >= D / 2) return;
-    const Range ks = sequence_rows(A.koff, seq, A.total_k), qs = sequence_rows(A.qoff, seq, A.total_q, kSinkRows);
+    const Range ks = sequence_rows(A.koff, seq, A.total_k), qs = sequence_rows(A.qoff, seq, A.total_q, A.sink_rows);
     if (key >= ks.n) return;
-    const int parts = (qs.n + kSinkRows - 1) / kSinkRows;
+    const int parts = (qs.n + A.sink_rows - 1) / A.sink_rows;
     if (parts == 1) return;                          // written as they are
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
     for (int p = 0; p < parts; ++p)
-        sum += *(const f32x4*)(part + ((sink_place(qs, p) * A.kv_heads + kv) * A.sinks + key) * 2 * D + 4 * lane);
+        sum += *(const f32x4*)(part + ((sink_place(qs, p, A.sink_rows) * A.kv_heads + kv) * A.sinks + key) * 2 * D + 4 * lane);
     E* to = lane < D / 4 ? dk : dv;
     Oper<E>::store4(to + ((int64_t)(ks.lo + key) * A.kv_heads + kv) * D + 4 * (lane % (D / 4)), sum);
 }
@@ -1420,7 +1424,7 @@ hipError_t launch_attention_backward(const AttnArgs& A, const AttnPlan& P, const
             constexpr bool BIAS = decltype(bias)::value, MASKED = decltype(masked)::value;
             const size_t lds = BIAS ? bias_bytes(A.reach, 1) : 0;
             const int main = A.total_k > 0 ? (int)(P.k_slots * ((A.kv_heads + P.kv_run - 1) / P.kv_run)) : 0;
-            constexpr int WAVES = kApart<E, D> ? 2 * kWavefronts : kWavefronts;
+            constexpr int WAVES = kKeyWaves<E, D, WIN>;
             const int more = BIAS ? (A.n_buckets * A.heads + WAVES - 1) / WAVES : 0;
             const int sinks = WIN && main ? (int)P.sink_groups : 0;
             if (main + more == 0) return hipSuccess;

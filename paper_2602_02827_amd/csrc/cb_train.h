@@ -24,6 +24,7 @@ struct AttnArgs {
     int16_t starts[128];         // first distance of each bucket of one direction
     int windowed;                // rows see `before` keys before them, `after` behind them, and the first `sinks`
     int before, after, sinks;
+    int sink_rows;               // rows of a sequence that one workgroup adds up for the gradients of its first keys
 };
 
 // Wavefronts of a workgroup, 32 columns each.  (Of one, for sequences of up to 32 columns: one query of 32 tokens, forward pass and both
@@ -31,10 +32,9 @@ struct AttnArgs {
 constexpr int kWavefronts = 4;
 // Wide heads take all registers: their workgroups do not go on to the next one.
 constexpr bool goes_on_to_next_head(int d) { return d <= 64; }
+// In 16 bits the gradients of wide heads' keys and values take a wavefront each.
+constexpr bool two_for_keys(int d, int bytes) { return bytes == 2 && d >= 96; }
 constexpr int kMostRun = 2;      // heads that a workgroup takes one after the other (four: the histograms leave half the workgroups no LDS)
-
-// Rows of a sequence that one workgroup adds up for the gradients of its first keys, where all rows see them.
-constexpr int kSinkRows = 512;
 
 enum { AS_THEY_COME, BY_XCD, LONGEST_FIRST };         // order of workgroups
 

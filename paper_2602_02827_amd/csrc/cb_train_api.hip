@@ -24,7 +24,8 @@ AttnPlan plan_attention(const AttnArgs& A, int d, int dt, bool backward) {
         q_rows = span * A.group < q_rows ? span * A.group : q_rows;
     }
     P.q_slots = A.total_q / (32 * kWavefronts / A.pack) + A.n_seqs;
-    P.k_slots = A.total_k / (32 * kWavefronts) + A.n_seqs;
+    const int64_t key_tile = A.windowed && two_for_keys(d, dt == TR_BF16 ? 2 : 4) ? 16 * kWavefronts : 32 * kWavefronts;
+    P.k_slots = A.total_k / key_tile + A.n_seqs;
     auto order_of = [&](int64_t slots, int64_t rows) {
         return rows <= kShortRows ? BY_XCD : A.causal && slots >= 4 * (int64_t)A.n_seqs ? LONGEST_FIRST : AS_THEY_COME;
     };
@@ -69,9 +70,9 @@ AttnPlan plan_attention(const AttnArgs& A, int d, int dt, bool backward) {
         P.delta = take((int64_t)A.heads * A.total_q * 8);        // and a value of rows that are far (is_far)
         if (A.bias) P.bias_part = take(P.q_slots * A.heads * A.n_buckets * 4);
         if (A.windowed && A.sinks) {
-            const int64_t slots = A.total_q / kSinkRows + A.n_seqs, tile = 32 * kWavefronts;
-            P.sink_groups = slots * A.kv_heads * ((A.sinks + tile - 1) / tile);
-            P.sink_part = take(2 * (A.total_q / kSinkRows + 1) * (int64_t)A.kv_heads * A.sinks * 2 * d * 4);
+            const int64_t slots = A.total_q / A.sink_rows + A.n_seqs;
+            P.sink_groups = slots * A.kv_heads * ((A.sinks + key_tile - 1) / key_tile);
+            P.sink_part = take(2 * (A.total_q / A.sink_rows + 1) * (int64_t)A.kv_heads * A.sinks * 2 * d * 4);
         }
     }
     P.bytes = o;
@@ -180,7 +181,8 @@ int attn_args(const colbandit_attn* a, AttnArgs& A) {
 constexpr int64_t kMostWindowRows = 1 << 28;
 constexpr int kWholeWindow = 1 << 29;
 
-int window_args(const colbandit_window* w, AttnArgs& A) {
+int64_t size_of(int dt) { return dt == COLBANDIT_BF16 ? 2 : 4; }
+int window_args(const colbandit_attn* a, const colbandit_window* w, AttnArgs& A) {
     if (!w) return COLBANDIT_ERR_NULL;
     if (w->before < 0 || w->after < 0 || w->sinks < 0) return COLBANDIT_ERR_SHAPE;
     if (w->sinks > COLBANDIT_MAX_SINKS || A.total_q > kMostWindowRows || A.total_k > kMostWindowRows) return COLBANDIT_ERR_UNSUPPORTED;
@@ -188,6 +190,10 @@ int window_args(const colbandit_window* w, AttnArgs& A) {
     A.before = w->before < kWholeWindow ? (int)w->before : kWholeWindow;
     A.after = A.causal ? 0 : w->after < kWholeWindow ? (int)w->after : kWholeWindow;
     A.sinks = (int)w->sinks;
+    // Short enough for an even load, since workgroups of the first keys have little to do at a time, as long as that costs little
+    // workspace.  (8 documents of 2,048 tokens, two key heads of 128 under eight, a window of 256 rows and four first keys, with
+    // gradients: 216 us, with 256 rows 232, with 512 242; of up to 4,095 tokens, heads of 64: 175, 164 and 167.)
+    A.sink_rows = A.sinks > 256 ? 512 : A.sinks > 64 || !two_for_keys(a->d, (int)size_of(a->dt)) ? 256 : 128;
     return COLBANDIT_OK;
 }
 
@@ -246,7 +252,6 @@ int attention_backward(const colbandit_attn* a, AttnArgs& A, const AttnGrads& G,
 }
 
 bool is_type(int dt) { return dt == COLBANDIT_F32 || dt == COLBANDIT_BF16; }
-int64_t size_of(int dt) { return dt == COLBANDIT_BF16 ? 2 : 4; }
 
 constexpr int64_t kMostVocab = 1 << 24, kMostWidth = 1 << 16;
 int check_embedding(int64_t n, int64_t vocab, int64_t width, int64_t row, int dt, int other) {
@@ -379,7 +384,7 @@ size_t colbandit_sizeof_window(void) { return sizeof(colbandit_window); }
 
 size_t colbandit_attention_window_workspace_bytes(const colbandit_attn* a, const colbandit_window* w, int backward) {
     AttnArgs A;
-    if (attn_args(a, A) || window_args(w, A)) return 0;
+    if (attn_args(a, A) || window_args(a, w, A)) return 0;
     return plan_attention(A, a->d, a->dt, backward != 0).bytes;
 }
 
@@ -387,7 +392,7 @@ int colbandit_attention_window(const colbandit_attn* a, const colbandit_window* 
                                size_t workspace_bytes, void* stream) {
     AttnArgs A;
     int rc = attn_args(a, A);
-    if (!rc) rc = window_args(w, A);
+    if (!rc) rc = window_args(a, w, A);
     return rc ? rc : attention(a, A, out, lse, workspace, workspace_bytes, stream);
 }
 
@@ -395,7 +400,7 @@ int colbandit_attention_window_backward(const colbandit_attn* a, const colbandit
                                         void* dq, void* dk, void* dv, void* dbias, void* workspace, size_t workspace_bytes, void* stream) {
     AttnArgs A;
     int rc = attn_args(a, A);
-    if (!rc) rc = window_args(w, A);
+    if (!rc) rc = window_args(a, w, A);
     return rc ? rc : attention_backward(a, A, {out, dout, lse, dq, dk, dv, dbias}, workspace, workspace_bytes, stream);
 }
 

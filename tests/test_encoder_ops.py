@@ -545,7 +545,7 @@ def test_windows_over_queries_and_keys_of_different_lengths(tr, dev, dtype, caus
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("causal,window,sinks,keep", [(True, (255, 0), 4, False), (False, (64, 64), 1, True), (False, (700, 3), 33, False)])
 def test_windows_in_long_sequences(tr, dev, dtype, causal, window, sinks, keep):
-    """More than one workgroup's rows for the first keys (512 each)."""
+    """More than one workgroup's rows for the first keys."""
     ql = [1500, 513, 512]
     p = window_problem(dev, dtype, ql, ql, 2, 1, 64, seed=4, keep=keep)
     check_window(tr, p, ql, ql, dtype, causal, window, sinks)
@@ -555,10 +555,21 @@ def test_windows_in_long_sequences(tr, dev, dtype, causal, window, sinks, keep):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("ql", [[513, 512, 514, 511], [1, 600, 2, 1100, 0, 513], [700, 700]])
 def test_first_keys_of_sequences_of_several_chunks(tr, dev, dtype, ql):
-    """Chunks of 512 rows: sequences of one, of two, and of a row more, one after the other."""
+    """Chunks of 256 rows: sequences of two, of three, and of a row more, one after the other."""
     kl = [n + 3 for n in ql]
     p = window_problem(dev, dtype, ql, kl, 2, 2, 32, seed=14)
     check_window(tr, p, ql, kl, dtype, False, (3, 2), 5)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,d,sinks,rows", [("bf16", 128, 64, 128), ("bf16", 96, 5, 128), ("f32", 128, 5, 256), ("bf16", 64, 3, 256),
+                                                ("bf16", 128, 65, 256), ("bf16", 64, 257, 512), ("f32", 64, 256, 256)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_first_keys_at_the_edges_of_chunks(tr, dev, dtype, d, sinks, rows, causal):
+    """Rows that one workgroup adds up for the first keys: as many, one less and more, twice as many, none and one."""
+    ql = [rows, rows + 1, 0, rows - 1, 2 * rows, 2 * rows + 1, 1, rows]
+    p = window_problem(dev, dtype, ql, ql, 2, 1, d, seed=19)
+    check_window(tr, p, ql, ql, dtype, causal, (7, 5), sinks)
 
 
 @gpu
