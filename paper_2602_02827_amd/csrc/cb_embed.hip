@@ -72,6 +72,9 @@ __device__ __forceinline__ Place place_of_piece(uint64_t first, uint32_t more, u
 
 constexpr int kThreads = 256;
 
+// out[i] = scale * table[tokens[i]], in 32 bits, rounded once.  Bound by memory: 54 thousand rows of 768, a 32-bit table under 16-bit rows,
+// 35 us (83 MB written, and a table's rows read that come again from the last-level cache); one query of 32 tokens 2.5 us, a launch and
+// two dependent loads.
 template <class W, class O, int V, int U>
 __global__ __launch_bounds__(kThreads) void k_embed(const W* table, int64_t table_row, const int64_t* tokens, uint64_t vocab, uint64_t n,
                                                     uint32_t pieces, float scale, O* out) {
@@ -103,7 +106,9 @@ __global__ __launch_bounds__(kThreads) void k_embed(const W* table, int64_t tabl
 // First tokens are sorted, each workgroup having a range of the table's rows: it goes over all tokens, counts those below its range
 // (which is where its part of the sorted list begins) and those of each row, and then puts its own into their places.  A wavefront
 // has a run of consecutive tokens, so that the order of equal ones is that of the list.  It notes its own tokens as it comes by, and
-// only goes over its run again where there are more of them than it has room for.
+// only goes over its run again where there are more of them than it has room for.  All workgroups read all tokens, from L2: 256 of them,
+// so that this is done at once on all CUs; one sort by all of them together would be several dependent launches, of 3.6 us each.  54
+// thousand tokens, 32,000 rows: 17 us; 2,700 tokens, 800 rows: 6 us.
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kMostRange = 960, kNoted = 512;
 
 // A token in 32 bits, which rows are counted in.
@@ -203,6 +208,8 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(const int64_t* toke
 // Then rows are added up.  A row of up to kLong tokens, or of none, is one thread's sum for each piece.  The sorted list is cut into
 // chunks of kLong, and what a chunk has of longer rows (at most of two: one that began before and one that goes on) is a sum of its
 // own, joined by a second launch.
+// Bound by memory, or by the most frequent tokens' rows (a row's additions are one after the other): 54 thousand rows of 768 in 16 bits,
+// 49 us (83 MB read, 98 MB of the table written, 3.7 TB/s) and 6 us to join.  2,700 rows of 256 in 32 bits, 800 tokens: 3.5 and 2 us.
 constexpr int kLong = 64;
 
 // A piece as it is stored, so that many are under way in few registers.

@@ -93,7 +93,8 @@ __device__ __forceinline__ double block_total(double x) {
     return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
-// Sums of squares, in 64 bits, of chunks of each matrix.
+// Sums of squares, in 64 bits (no matrix of finite values overflows or vanishes), of chunks of each matrix.  32 million bf16 values: 16 us,
+// 4 TB/s; the next kernel's sums of a matrix's chunks, and its pieces, 38 us (64 MB read, 128 MB written).
 __global__ __launch_bounds__(kThreads) void k_ortho_norm(const OrthoTable t, double* parts, OrthoTable* table) {
     // the others read the table from memory, where a second one finds it in L2 (the same nine matrices: 139 us from a kernel's arguments,
     // 131 so)
@@ -170,6 +171,11 @@ __global__ __launch_bounds__(kThreads) void k_ortho_in(const OrthoTable* __restr
 // by its row, so that sixteen rows' pieces (256 bytes, what LDS reads a clock) lie in different banks, and so do four rows' halves.
 // Each XCD has tiles that follow one another, of as much work as any other's: a matrix is then read into one L2 and not into eight.
 // Launches go through the matrices there and back: what one wrote last, the next reads first, from the last-level cache.
+// Bound by the matrix units and by memory in turn: of all matrices of six layers of 768 (32 million values, 422 GFLOP in five steps, three
+// times that as products of pieces), one step's launches take 103, 50 and 158 us (815 TFLOP/s of pieces), of which the products alone 72,
+// 22 and 74.  What is left is mostly the way of a finished tile to memory, 64 KB, through LDS and with what it is added to: a workgroup's
+// products are 24 to 96 turns, too few to hide it behind those of the other workgroup on the CU, which ends at about the same time (to
+// delay every second one made no difference).  A 768 x 128 matrix: 97 us for 17 launches that depend on each other, 4 to 9 us each.
 enum { GRAM, SQUARE, APPLY };
 
 __device__ __forceinline__ int turn_of(int row) {
