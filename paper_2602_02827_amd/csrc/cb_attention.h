@@ -420,7 +420,7 @@ __global__ __launch_bounds__(64 * kWavefronts, (kWaves<E, D>)) void k_attention(
         if constexpr (WIN) {
             visit = visit && win.some(base, T::ROWS);
             one = NB > 1 && !win.some(base + 32, 32);
-            diagonal = !win.every(base, T::ROWS);
+            diagonal = false;
         } else {
             visit = visit && base < w.end;
             one = NB > 1 && base + 32 >= w.end;
@@ -454,6 +454,7 @@ __global__ __launch_bounds__(64 * kWavefronts, (kWaves<E, D>)) void k_attention(
                     }
                 }
                 if (part) s[b] += of_rows(hidden[buf], b, h);
+                if constexpr (WIN) diagonal = !win.every(base + 32 * b, 32);
                 if (diagonal) {
                     uint32_t own;
                     if constexpr (WIN) own = win.bits(base + 32 * b + 4 * h);
@@ -782,7 +783,7 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
         const bool part = seen != kAllRows;
         if constexpr (WIN) {
             visit = visit && win.some(base, T::ROWS);
-            diagonal = !win.every(base, T::ROWS);
+            diagonal = false;
         } else {
             visit = visit && base < w.end;
             diagonal = A.causal && base + T::ROWS - 1 > w.first_lim;
@@ -792,6 +793,7 @@ k_attention_dq(const AttnArgs A, int slots, int order, int units, int run, const
             for (int b = 0; b < NB && (WIN || base + 32 * b < w.end); ++b) {
                 if constexpr (WIN)
                     if (!win.some(base + 32 * b, 32)) continue;
+                if constexpr (WIN) diagonal = !win.every(base + 32 * b, 32);
                 f32x16 s = {}, dp;
                 add_rows<T, EARLY>(s, lk, b, q.v);
                 phase();
@@ -999,7 +1001,10 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int s
     constexpr int WAVES = kKeyWaves<E, D, WIN>, GROUPS = APART ? WAVES / 2 : WAVES;      // of 32 key rows
     constexpr int NB = T::ROWS / 32, DB = D / 32, COLS = 32 * GROUPS, THREADS = 64 * WAVES;
     constexpr int BUFS = APART ? 3 : 2;               // tiles in LDS
-    const bool keys = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) >= GROUPS;        // (APART) this wavefront has the keys' gradient
+    // (APART) This wavefront has the keys' gradient.  Of two workgroups on a CU (with a window; the second ones are about 256 on) one has its
+    // values' wavefronts, with the exponentials, on the SIMDs where the other has its keys' (8 documents of up to 4,095 tokens, a window
+    // of 256 rows and four first keys, with gradients: 269 us, so 261).
+    const bool keys = (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) >= GROUPS) != (WIN && (blockIdx.x >> 8 & 1));
     __shared__ __align__(256) char lds[BUFS][2 * T::BYTES];
     __shared__ __align__(16) float row_lse[BUFS][T::ROWS], row_delta[BUFS][T::ROWS], row_far[BUFS][2][T::ROWS];
     __shared__ int tile_far[BUFS];                    // some row is far: row_far has log-sum-exps, and what is added to far rows' exponents
@@ -1232,12 +1237,12 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int s
         const bool seen_by = busy && c0 + T::ROWS > wfirst && (!WIN || c0 < wend);      // some of the wavefront's keys, by some of the rows
         if (any && (APART || seen_by)) {
             bool diagonal;
-            if constexpr (WIN) diagonal = c0 < all_from || c0 + T::ROWS > all_to;
-            else diagonal = A.causal && (wkey + 31 - shift) * G > c0;
+            if constexpr (!WIN) diagonal = A.causal && (wkey + 31 - shift) * G > c0;
             const int blocks = WIN && !APART ? (wend - c0 + 31) / 32 : (cols - c0 + 31) / 32, all = blocks < NB ? blocks : NB;
 #pragma unroll 1
             for (int b = 0; b < all + (APART && last); ++b) {
                 const bool on = !WIN || (c0 + 32 * b + 32 > wfirst && c0 + 32 * b < wend);
+                if constexpr (WIN) diagonal = c0 + 32 * b < all_from || c0 + 32 * b + 32 > all_to;
                 if constexpr (!APART) {
                     if (!on) continue;
                     f32x16 s = {}, dp = {};
