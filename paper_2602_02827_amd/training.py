@@ -607,7 +607,8 @@ def clip_gradients_(parameters, max_norm):
 def orthogonal_step_(parameters, momenta, rate, momentum=0.95, steps=5, coefficients=POLYNOMIAL):
     """One step of descent along orthogonalised momenta, for 2-d parameters: of each that has a gradient the momentum becomes
     momentum * itself + gradient, and the parameter goes down `rate` times sqrt(max(1, rows / columns)) times
-    colbandit_orthogonalise of gradient + momentum * itself.  `momenta`: a dict of the parameters' momenta, which this fills."""
+    colbandit_orthogonalise of gradient + momentum * itself.  `momenta`: a dict of the parameters' momenta, which this fills; they are
+    float32 whatever the parameters' type."""
     parameters = [p for p in dict.fromkeys(parameters) if p.grad is not None and p.numel()]
     if not parameters:
         return
@@ -620,7 +621,7 @@ def orthogonal_step_(parameters, momenta, rate, momentum=0.95, steps=5, coeffici
         for p in parameters:
             m = momenta.get(p)
             if m is None:
-                m = momenta[p] = torch.zeros_like(p, memory_format=torch.contiguous_format)
+                m = momenta[p] = torch.zeros_like(p, dtype=torch.float32, memory_format=torch.contiguous_format)
             m.mul_(momentum).add_(p.grad)
             updates.append(torch.add(p.grad, m, alpha=momentum).contiguous())
         colbandit_orthogonalise(updates, steps=steps, coefficients=coefficients, out=updates)

@@ -810,6 +810,19 @@ def test_orthogonalising_in_place_in_graphs_and_steps(tr, dev):
         assert float((x.detach() - step).norm()) <= 1e-4 * float(step.norm())
 
 
+@gpu
+def test_momenta_of_16_bit_parameters_are_32_bits(tr, dev):
+    """A gradient of 2^-10 of the momentum, which 16 bits would leave out, counts in every step."""
+    p = torch.nn.Parameter(torch.zeros(24, 40, device=dev, dtype=torch.bfloat16))
+    momenta = {}
+    for x in [1.0] + [2.0 ** -10] * 4:
+        p.grad = torch.full_like(p, x)
+        tr.orthogonal_step_([p], momenta, rate=0.1, momentum=1.0)
+    assert momenta[p].dtype == torch.float32 and p.dtype == torch.bfloat16
+    assert torch.equal(momenta[p], torch.full_like(momenta[p], 1.0 + 2.0 ** -8))
+    assert bool((p < 0).all())
+
+
 # ---- together --------------------------------------------------------------------------------------------------
 
 @gpu
