@@ -987,6 +987,10 @@ __device__ __forceinline__ int64_t sink_place(const Range& rows, int chunk, int 
 // a window, where each goes over all rows, 24 causal pages 456 and 468, of heads of 96 with a bias 705 and 753).
 template <class E, int D> constexpr bool kApart = two_for_keys(D, sizeof(E));
 template <class E, int D, bool WIN> constexpr int kKeyWaves = kApart<E, D> && !WIN ? 2 * kWavefronts : kWavefronts;
+// Rows (of all heads that share a key head) that a 32-bit sum through a window takes before it is added to the result.  (11 documents of
+// 1,030 tokens, seven fp32 heads of 64 to a key head, a window of 719 rows: keys' and values' gradients are 7.3e-7 of their norm off, 1.3e-6
+// in one sum, plain 32-bit products 7.3e-7; 1,037 us, in one sum 1,055.  Heads of 128, four to a key head: 967 and 900.)
+constexpr int kMostSum = 1024;
 // With a window the first keys are left to workgroups of their own (the first `sink_groups` ones), since all of a sequence's rows see
 // them: a key tile's others see some rows only.  Such a workgroup takes A.sink_rows rows of a sequence, and, where the sequence has
 // more, leaves its shares of the first keys' gradients to k_attention_join_sinks.  They come first: the others, which are all of about
@@ -1159,6 +1163,8 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int s
     };
     load_keys(kv0);
     f32x16 acc[DB] = {}, acc2[APART ? 1 : DB] = {};              // of keys and of values, or of the wavefront's own
+    int summed = 0;                                   // tiles since they were last added to the result, which holds some: again
+    bool again = false;
     const int middle = bias_middle(A.reach);
     const bool busy = wkey < key_to && wkey + 32 > key_from;
     int16_t* starts = (int16_t*)dyn;
@@ -1299,9 +1305,13 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int s
                 }
             }
         }
-        if (last) {
+        // fp32 through a window: all heads' rows of a wide window are one sum, whose rounding with each of six products of pieces shows, so
+        // every kMostSum rows it is added to what the result holds
+        constexpr bool PARTS = WIN && sizeof(E) == 4;
+        const bool part = PARTS && !last && any && ++summed == kMostSum / T::ROWS;
+        if (last || part) {
             const int kv = head0 / A.group;
-            if (kRuns<D> && more) load_keys(kv + 1);
+            if (kRuns<D> && more && last) load_keys(kv + 1);
             if (real) {
                 const int64_t dense = (at * A.kv_heads + kv) * D;
                 auto store = [&](E* to, const f32x16(&a)[DB], float by) {
@@ -1309,8 +1319,11 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int s
                     for (int db = 0; db < DB; ++db)
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
-                            const f32x4 x = {a[db][4 * j] * by, a[db][4 * j + 1] * by, a[db][4 * j + 2] * by, a[db][4 * j + 3] * by};
-                            O::store4(to + dense + 32 * db + 8 * j + 4 * h, seen ? x : f32x4{0.f, 0.f, 0.f, 0.f});
+                            f32x4 x = {a[db][4 * j] * by, a[db][4 * j + 1] * by, a[db][4 * j + 2] * by, a[db][4 * j + 3] * by};
+                            E* at = to + dense + 32 * db + 8 * j + 4 * h;
+                            if constexpr (PARTS)
+                                if (again) x += *(const f32x4*)at;
+                            O::store4(at, seen ? x : f32x4{0.f, 0.f, 0.f, 0.f});
                         }
                 };
                 if (WIN && sinks && qs.n > A.sink_rows) {
@@ -1320,8 +1333,11 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int s
                         for (int db = 0; db < DB; ++db)
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
-                                const f32x4 x = {a[db][4 * j] * by, a[db][4 * j + 1] * by, a[db][4 * j + 2] * by, a[db][4 * j + 3] * by};
-                                *(f32x4*)(to + which * D + 32 * db + 8 * j + 4 * h) = seen ? x : f32x4{0.f, 0.f, 0.f, 0.f};
+                                f32x4 x = {a[db][4 * j] * by, a[db][4 * j + 1] * by, a[db][4 * j + 2] * by, a[db][4 * j + 3] * by};
+                                float* at = to + which * D + 32 * db + 8 * j + 4 * h;
+                                if constexpr (PARTS)
+                                    if (again) x += *(const f32x4*)at;
+                                *(f32x4*)at = seen ? x : f32x4{0.f, 0.f, 0.f, 0.f};
                             }
                     };
                     if constexpr (!APART) {
@@ -1337,7 +1353,9 @@ k_attention_dkv(const AttnArgs A, int slots, int order, int run, int main, int s
                     store(keys ? dk : dv, acc, keys ? A.scale : 1.f);
                 }
             }
-            if (!more) return;
+            if (last && !more) return;
+            again = part;
+            summed = 0;
 #pragma unroll
             for (int db = 0; db < DB; ++db) {
                 acc[db] = {};

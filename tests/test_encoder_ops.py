@@ -574,6 +574,16 @@ def test_first_keys_at_the_edges_of_chunks(tr, dev, dtype, d, sinks, rows, causa
 
 @gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,sinks,keep", [(32, 0, False), (64, 5, True), (96, 300, False), (128, 3, False)])
+def test_long_sums_of_heads_that_share_keys(tr, dev, dtype, d, sinks, keep):
+    """Keys that more than a thousand rows see, those of all heads together, some of them by a whole multiple of that."""
+    ql = [640, 385, 1, 256, 128]
+    p = window_problem(dev, dtype, ql, ql, 16, 2, d, seed=23, keep=keep)
+    check_window(tr, p, ql, ql, dtype, True, (255, 0), sinks)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("d,H,Hk,keep", [(128, 8, 2, False), (64, 4, 4, True)])
 @pytest.mark.parametrize("window,sinks", [((1023, 0), 4), ((3, 0), 0), ((100000, 0), 0)])
 def test_single_tokens_through_a_window(tr, dev, dtype, d, H, Hk, keep, window, sinks):
