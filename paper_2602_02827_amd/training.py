@@ -194,7 +194,12 @@ def _window(window, sinks):
 
 
 def _like(t):
-    return torch.empty_like(t, memory_format=torch.contiguous_format)
+    return torch.empty_like(t) if t.is_contiguous() else torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
+def _new(t, dtype, *shape):
+    # without a type, and from numbers, it takes 1 us less, which small calls notice
+    return t.new_empty(*shape) if dtype is t.dtype else t.new_empty(shape, dtype=dtype)
 
 
 def _dense(t, shape, dtype, what):
@@ -215,7 +220,7 @@ def colbandit_attention(q, k, v, q_offsets, k_offsets=None, *, causal=False, sca
     L = lib()
     o, lse = (out["out"], out["lse"]) if out else (None, None)
     o = _like(q) if o is None else _dense(o, q.shape, q.dtype, "out")
-    lse = q.new_empty((a.heads, a.total_q), dtype=torch.float32) if lse is None else _dense(lse, (a.heads, a.total_q), torch.float32, "lse")
+    lse = _new(q, torch.float32, a.heads, a.total_q) if lse is None else _dense(lse, (a.heads, a.total_q), torch.float32, "lse")
     dev = _on_device(o, lse)
     if w is not None:
         ws, nb = _workspace(workspace, L.colbandit_attention_window_workspace_bytes(a, w, 0), q.device)
@@ -288,7 +293,7 @@ def colbandit_embedding(table, tokens, *, scale=1.0, dtype=None, out=None):
     if dtype is None:
         dtype = table.dtype
     to = _type_of_rows(dtype)
-    out = table.new_empty((n, width), dtype=dtype) if out is None else _dense(out, (n, width), dtype, "out")
+    out = _new(table, dtype, n, width) if out is None else _dense(out, (n, width), dtype, "out")
     dev = _on_device(table, tokens, out)
     _check(lib().colbandit_embedding(table.data_ptr(), dt, row, tokens.data_ptr(), n, vocab, width, scale, out.data_ptr(), to,
                                      _stream(dev)), "colbandit_embedding")
@@ -305,7 +310,7 @@ def colbandit_embedding_backward(dout, tokens, vocab, *, scale=1.0, dtype=None, 
         dtype = dout.dtype
     to = _type_of_rows(dtype)
     L = lib()
-    out = dout.new_empty((vocab, width), dtype=dtype) if out is None else _dense(out, (vocab, width), dtype, "dtable")
+    out = _new(dout, dtype, vocab, width) if out is None else _dense(out, (vocab, width), dtype, "dtable")
     dev = _on_device(dout, tokens, out)
     ws, nb = _workspace(workspace, L.colbandit_embedding_workspace_bytes(n, vocab, width), dout.device)
     _check(L.colbandit_embedding_backward(dout.data_ptr(), dt, row, tokens.data_ptr(), n, vocab, width, scale, out.data_ptr(), to,
@@ -369,7 +374,7 @@ def colbandit_norm_rotate_backward(dq_out, dk_out, q, k, *, positions=None, tabl
     r, dev = _rotation(q, k, positions, table, q_weight, k_weight, eps, interleaved, dq_out, dk_out)
     L = lib()
     dq, dk = _like(q), _like(k)
-    dq_weight, dk_weight = q.new_empty(r.d, dtype=torch.float32), q.new_empty(r.d, dtype=torch.float32)
+    dq_weight, dk_weight = _new(q, torch.float32, r.d), _new(q, torch.float32, r.d)
     ws, nb = _workspace(workspace, L.colbandit_norm_rotate_workspace_bytes(r), q.device)
     _check(L.colbandit_norm_rotate_backward(r, dq_out.data_ptr(), dk_out.data_ptr(), dq.data_ptr(), dk.data_ptr(), dq_weight.data_ptr(),
                                             dk_weight.data_ptr(), _ptr(ws), nb, _stream(dev)), "colbandit_norm_rotate_backward")
