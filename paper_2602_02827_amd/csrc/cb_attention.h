@@ -335,9 +335,9 @@ constexpr float kLag = 8.f;
 // mask, 141 us.  Single tokens by memory: 16 over 1 to 16,385 keys, two key heads of 128, 134 MB in 29 us and 7.5 us to join their
 // parts.
 // Through a window (WIN) only tiles that some row sees are gone over, and tiles of the first keys; what a row sees of a tile is a bit a key.
-// 6 documents of 500 to 8,191 tokens, 12 heads of 64, 64 keys to either side, one first key: 59 us, 10.3 GFLOP of 161 MB.  A workgroup's
-// 128 rows see 256 keys together and 129 each, so half of the products and exponentials are of hidden keys; vector instructions bound it
-// (1,500 of a wavefront).  16 single tokens that see 1,028 of up to 16,385 keys: 9 us and 4 us to join.
+// 6 documents of 500 to 8,191 tokens, 12 heads of 64, 64 keys to either side, one first key: 58 us, 10.3 GFLOP of 161 MB (38
+// with a window of one key).  A workgroup's 128 rows see 256 keys together and 129 each, so half of the products and exponentials are of
+// hidden keys; vector instructions (1,500 of a wavefront) and what comes before the first product bound it.  16 single tokens that see 1,028 of up to 16,385 keys: 9 us and 4 us to join.
 template <class E, int D, bool BIAS, bool MASKED, bool WIN>
 __global__ __launch_bounds__(64 * kWavefronts, (kWaves<E, D>)) void k_attention(const AttnArgs A, int slots, int order, int units, int run,
                                                                            int splits, E* out, float* lse, float* o_part,
@@ -629,7 +629,7 @@ __device__ __forceinline__ bool is_far(float lse, float scale2) {
 // Bound by the matrix and vector units' turns where sequences are long (24 causal pages, 8 heads of 128 over 2: 169 and 190 us, 510
 // TFLOP/s of the three and four products that each cannot do without), by latency and by what surrounds the products where they are
 // short (the 512 passages: 286 and 262 us).  8 documents of up to 4,095 tokens through a window of 256 rows and four first keys, 8 heads
-// of 128 over 2: forward 51 us, queries 81, keys and values 129, 6.6 to join the first keys'.
+// of 128 over 2: forward 51 us, queries 82, keys and values 127, 6.5 to join the first keys'.
 
 // Sums of a 32 x 32 block along its diagonals, added to a histogram by distance.  The block is in accumulators: a lane has sixteen
 // keys of a column.  Lane p of a half takes key k's value from column (p + k) mod 32: it lies on diagonal -p, or 32 - p where that
