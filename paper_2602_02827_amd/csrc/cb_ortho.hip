@@ -172,7 +172,7 @@ __global__ __launch_bounds__(kThreads) void k_ortho_in(const OrthoTable* __restr
 // Each XCD has tiles that follow one another, of as much work as any other's: a matrix is then read into one L2 and not into eight.
 // Launches go through the matrices there and back: what one wrote last, the next reads first, from the last-level cache.
 // Bound by the matrix units and by memory in turn: of all matrices of six layers of 768 (32 million values, 422 GFLOP in five steps, three
-// times that as products of pieces), one step's launches take 103, 50 and 158 us (815 TFLOP/s of pieces), of which the products alone 72,
+// times that as products of pieces), one step's launches take 104, 46 and 155 us (830 TFLOP/s of pieces), of which the products alone 72,
 // 22 and 74.  What is left is mostly the way of a finished tile to memory, 64 KB, through LDS and with what it is added to: a workgroup's
 // products are 24 to 96 turns, too few to hide it behind those of the other workgroup on the CU, which ends at about the same time (to
 // delay every second one made no difference).  A 768 x 128 matrix: 97 us for 17 launches that depend on each other, 4 to 9 us each.
@@ -273,16 +273,6 @@ __global__ __launch_bounds__(DEEP * kThreads, DEEP > 1 ? DEEP : 2) void k_ortho_
         const int p = x * DEEP * kThreads + tid;
         return Piece{(p >> 2) % T, (p >> 2) / T * 32 + (p & 3) * 8};
     };
-    f16x8 add[STEP == GRAM ? 1 : PIECES][2] = {};
-    if constexpr (STEP != GRAM)
-#pragma unroll
-        for (int x = 0; x < PIECES; ++x) {
-            if (!has) break;
-            const Piece p = piece_of(x);
-            const char* line = line_at(STEP == SQUARE ? P : X, i0 + p.row, rows, (j0 + p.col) / 32) + p.col % 32 * 2;
-            add[x][0] = *(const f16x8*)line;
-            add[x][1] = *(const f16x8*)(line + 64);
-        }
     f32x16 acc[NB][NB] = {};                         // [j][i]
     for (int kb = 0; kb < AHEAD && kb < steps; ++kb) issue(kb);
     for (int kb = 0; kb < steps; ++kb) {
@@ -323,6 +313,17 @@ __global__ __launch_bounds__(DEEP * kThreads, DEEP > 1 ? DEEP : 2) void k_ortho_
 #pragma unroll
                     for (int y = 0; y < NB; ++y) mma(acc[x][y], q[s][x][z == 0], p[s][y][z == 1]);
     }
+    // (before the products the first copies would be waited for together with it: 1,600 us instead of 1,576 for an encoder's matrices)
+    f16x8 add[STEP == GRAM ? 1 : PIECES][2] = {};
+    if constexpr (STEP != GRAM)
+#pragma unroll
+        for (int x = 0; x < PIECES; ++x) {
+            if (!has) break;
+            const Piece p = piece_of(x);
+            const char* line = line_at(STEP == SQUARE ? P : X, i0 + p.row, rows, (j0 + p.col) / 32) + p.col % 32 * 2;
+            add[x][0] = *(const f16x8*)line;
+            add[x][1] = *(const f16x8*)(line + 64);
+        }
     __syncthreads();
     // The tile goes through LDS once more, in 32 bits, so that lines are read and written whole (from the accumulators a lane would
     // have eight bytes of each: twice as many requests to L2 as the products' operands).  Four values' places are turned by the row.
