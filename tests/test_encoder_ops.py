@@ -673,6 +673,148 @@ def test_windows_in_graphs_and_as_part_of_a_program(tr, dev, bias, sinks):
     assert torch.equal(out, want["out"]) and all(torch.equal(t.grad, want["d" + x]) for t, x in zip(leaves, "qkv"))
 
 
+def two_heads_a_workgroup(ql, kl, heads, kv_heads, bias, window, sinks):
+    """Whether the plan's workgroups go on to a second head through a window: units (key heads) in pairs leave 1,536 workgroups or
+    more, and a tile of 128 sees up to 384 rows; for the queries' tiles and for the keys'.  (Heads of up to 64.)"""
+    n, group, span = len(ql), heads // kv_heads, sum(window) + 128
+    pack = 1 if bias or group > 16 else group
+    units, q_slots, k_slots = heads // pack, sum(ql) // (128 // pack) + n, sum(kl) // 128 + n
+    k_rows, q_rows = min(span + sinks, sum(kl) // n), min(span * group, sum(ql) * group // n)
+    return k_rows <= 384 and units > 1 and q_slots * (units // 2) >= 1536, q_rows <= 384 and kv_heads > 1 and k_slots * (kv_heads // 2) >= 1536
+
+
+@gpu
+@pytest.mark.parametrize("dtype,d,H", [("bf16", 64, 25), ("bf16", 32, 24), ("f32", 64, 24), ("f32", 32, 25)])
+@pytest.mark.parametrize("causal,bias,keep,window,sinks", [
+    (False, None, False, (64, 64), 1), (True, None, True, (47, 0), 0), (False, 32, True, (20, 33), 0), (True, 32, False, (90, 0), 130)])
+def test_two_heads_a_workgroup_through_a_window(tr, dev, dtype, d, H, causal, bias, keep, window, sinks):
+    """Sequences of 1 to 180 rows; with an odd number of heads the last workgroup of a tile has one."""
+    lengths = [1 + i * 179 // 127 for i in range(128)]
+    assert two_heads_a_workgroup(lengths, lengths, H, H, bias, window, sinks) == (True, True)
+    p = window_problem(dev, dtype, lengths, lengths, H, H, d, seed=31, bias=bias, keep=keep)
+    check_window(tr, p, lengths, lengths, dtype, causal, window, sinks)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,sinks,keep", [(64, 0, False), (32, 5, True), (64, 5, False)])
+def test_two_heads_a_workgroup_with_long_sums(tr, dev, dtype, d, sinks, keep):
+    """Many short sequences and a long one, whose keys more than a thousand rows of the heads that share them see: the second key
+    head of a workgroup begins its sums anew.  Five heads to a key head: so are the first keys' sums."""
+    lengths = (np.random.default_rng(33).integers(0, 5, 1540).tolist()) + [900]
+    assert two_heads_a_workgroup(lengths, lengths, 10, 2, None, (700, 300), sinks)[1]
+    p = window_problem(dev, dtype, lengths, lengths, 10, 2, d, seed=32, keep=keep)
+    check_window(tr, p, lengths, lengths, dtype, False, (700, 300), sinks)
+
+
+def check_far_window(tr, p, ql, kl, dtype, causal, window, sinks, scale=None, like=None, by=1.0, lse_of=lambda x: x):
+    """All results of rows whose log-sum-exp may be of any size: it has a 32-bit value's own rounding, and as much again for the
+    product that it is the sum of.  The reference's probabilities are exp(S - lse), which in 64 bits lose a sum's logarithm too
+    where lse is that large: it is then given a problem of the same probabilities (`like`: other inputs, q divided by `by`, a power
+    of two, which is what the keys' gradient differs by), and `lse_of` its log-sum-exp.  A scale is its queries' factor."""
+    qo, ko = offsets(ql).to(p["q"].device), offsets(kl).to(p["q"].device)
+    how = dict(causal=causal, keep=p["keep"], bias=p["bias"], window=window, sinks=sinks, scale=scale)
+    f = tr.colbandit_attention(p["q"], p["k"], p["v"], qo, ko, **how)
+    b = tr.colbandit_attention_backward(p["dout"], p["q"], p["k"], p["v"], f["out"], f["lse"], qo, ko, **how)
+    torch.cuda.synchronize()
+    a = dict(p, **(like or {}))
+    factor = 1.0 if scale is None else float(np.float32(scale)) * math.sqrt(p["q"].shape[2])
+    if scale is not None:
+        a["q"] = a["q"].double() * factor
+    r = window_reference(a, ql, kl, dtype, causal, window, sinks)
+    r["dq"], r["dq_tol"] = r["dq"] * factor, r["dq_tol"] * abs(factor)
+    r["dk"], r["dk_tol"] = r["dk"] * by, r["dk_tol"] * by
+    r["lse"] = torch.where(r["lse"] == -math.inf, r["lse"], lse_of(r["lse"]))
+    lse = f["lse"].double().cpu()
+    assert torch.equal(lse == -math.inf, r["lse"] == -math.inf)
+    fine = r["lse"] > -math.inf
+    assert bool(((lse - r["lse"]).abs() <= F * 2 + 2.0 ** -22 * r["lse"].abs())[fine].all())
+    more = lambda t: 1.05 * t + 1e-9  # noqa: E731
+    within(f["out"], r["out"], more(r["out_tol"]), "out")
+    for x in ("dq", "dk", "dv") + (() if p["bias"] is None else ("dbias",)):
+        within(b[x], r[x], more(r[x + "_tol"]), x)
+
+
+LOWEST = {"bf16": torch.finfo(torch.bfloat16).min, "f32": torch.finfo(torch.float32).min}
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [32, 64, 96, 128])
+@pytest.mark.parametrize("causal,window,sinks", [(True, (3, 0), 0), (False, (0, 0), 0), (False, (2, 40), 1), (True, (64, 0), 3)])
+@pytest.mark.parametrize("low", [-1e4, -1e30, "lowest", -math.inf])
+def test_rows_that_see_a_hidden_distance_through_a_window(tr, dev, dtype, d, causal, window, sinks, low):
+    """A bucket of the table hides distance 0: of rows that see only this one, and beside others.  With minus infinity the former see
+    nothing."""
+    lengths = [50, 1, 133, 1]
+    p = window_problem(dev, dtype, lengths, lengths, 2, 2, d, seed=33, bias=8)
+    p["bias"][0] = LOWEST[dtype] if low == "lowest" else low
+    check_far_window(tr, p, lengths, lengths, dtype, causal, window, sinks)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("ql,kl,window,sinks", [([150, 1, 70], [150, 1, 70], (31, 20), 5), ([1, 3], [5000, 700], (1023, 0), 4)])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("value", ["lowest", -1e30, 1e30])
+def test_tables_far_from_zero_through_a_window(tr, dev, dtype, d, ql, kl, window, sinks, causal, value):
+    """Products are below such a bias' rounding in 64 bits as well: all keys that are seen weigh the same, in one part or several."""
+    p = window_problem(dev, dtype, ql, kl, 2, 2, d, seed=34, bias=32, keep=True)
+    p["bias"][:] = LOWEST[dtype] if value == "lowest" else value
+    at, tiny = float(p["bias"][0, 0].double()), 2.0 ** -40
+    check_far_window(tr, p, ql, kl, dtype, causal, window, sinks, like=dict(q=p["q"].double() * tiny, bias=torch.zeros_like(p["bias"])),
+                     by=1 / tiny, lse_of=lambda x: x + at)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,heads,kv_heads", [(64, 4, 4), (128, 4, 2), (96, 3, 1)])
+@pytest.mark.parametrize("ql,kl,window,sinks", [([150, 3, 70], [150, 3, 70], (40, 9), 2), ([40, 1], [1100, 900], (600, 0), 70)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_rows_on_both_sides_of_where_they_are_normalised_again_through_a_window(tr, dev, monkeypatch, dtype, d, heads, kv_heads, ql, kl,
+                                                                                window, sinks, causal):
+    """Ordinary rows with biases that move them to 240 and to 280: log-sum-exps below and above 256 in one call.  Scores of up to 290
+    carry nine times the error of the file's bound, which is for up to 32."""
+    monkeypatch.setitem(globals(), "F", F * 290 / 32)
+    p = window_problem(dev, dtype, ql, kl, heads, kv_heads, d, seed=35, bias=32, keep=True)
+    p["bias"] += torch.tensor([240.0, 280.0], device=dev).repeat(2)[:heads].to(DT[dtype])
+    check_far_window(tr, p, ql, kl, dtype, causal, window, sinks)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("head", [0, 1, 2])
+@pytest.mark.parametrize("d,causal,window,sinks", [(64, True, (2, 0), 0), (32, False, (0, 1), 1)])
+def test_one_head_of_several_is_far_from_zero_through_a_window(tr, dev, dtype, head, d, causal, window, sinks):
+    """Workgroups that go on from a head whose rows see nothing but a hidden distance to one whose do not, and the other way."""
+    lengths = np.random.default_rng(43).integers(0, 4, 1600).tolist()
+    assert two_heads_a_workgroup(lengths, lengths, 3, 3, 8, window, sinks) == (True, True)
+    p = window_problem(dev, dtype, lengths, lengths, 3, 3, d, seed=36, bias=8)
+    p["bias"][0, head] = LOWEST[dtype]
+    check_far_window(tr, p, lengths, lengths, dtype, causal, window, sinks)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bias", [None, 32])
+@pytest.mark.parametrize("scale", [0.0, -0.125, -3e-3])
+@pytest.mark.parametrize("d,heads,kv_heads,ql,kl", [(64, 2, 1, [150, 1, 70], [150, 1, 70]), (128, 4, 2, [90, 33], [90, 33]), (128, 2, 2, [1, 2], [3000, 400])])
+def test_scales_of_zero_and_below_through_a_window(tr, dev, dtype, bias, scale, d, heads, kv_heads, ql, kl):
+    p = window_problem(dev, dtype, ql, kl, heads, kv_heads, d, seed=37, bias=bias)
+    check_far_window(tr, p, ql, kl, dtype, True, (300, 0), 5, scale=scale)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,causal,window,sinks", [(128, True, (1023, 0), 4), (64, False, (2000, 2000), 0)])
+def test_single_tokens_with_a_bias_through_a_window(tr, dev, dtype, d, causal, window, sinks):
+    """Keys in several parts."""
+    ql, kl = [1] * 6, [1, 5000, 1024, 1025, 3, 2600]
+    p = window_problem(dev, dtype, ql, kl, 3, 3, d, seed=38, bias=32, keep=True)
+    check_window(tr, p, ql, kl, dtype, causal, window, sinks)
+
+
 # ---- orthogonalised updates ------------------------------------------------------------------------------------
 
 POLYNOMIAL = (3.4445, -4.7750, 2.0315)
