@@ -218,12 +218,24 @@ int colbandit_norm_rotate_backward(const colbandit_rotation *r, const void *dq_o
  * becomes U p(..p(S)) V^T with p(s) = a s + b s^3 + c s^5, `steps` times: with the usual
  * coefficients singular values come near to one.  Computed by matrix products,
  *   X <- a X + (b A + c A^2) X,  A = X X^T
- * whose sums are 32 bits; X, A and the bracket are held as two 16-bit pieces each, 22 bits of a
- * value.  A matrix of zeros stays zeros, one that holds an infinity or NaN is NaN everywhere.
+ * whose sums are 32 bits.  X, A and the bracket are held as two 16-bit pieces each: 22 bits of a
+ * value, but some 2^-40 of the matrix' norm is lost of what is small beside it, and each step raises
+ * that with the value.  They are held in 32 bits instead, with products to 2^-26 and in up to 2.3
+ * times the time, where that loss could come to 2^-19 of the result, and where |a| < 1: where the
+ * product of all steps' largest factors of a singular value (3.4 for the usual coefficients) and of the
+ * root of rows times columns is beyond 2^22, or up to four times less where steps make singular
+ * values of more than 1.5.  (Usual steps: more than five for 7,500 x 7,500 values, six for 2,200,
+ * seven for 640.  Matrices that follow one another in a list, up to 40, are held alike.)  So a
+ * matrix is about as far off as by plain 32-bit products, whatever its rows' and columns' sizes.  Rows
+ * that are small beside the others at the end are right on their own in 32 bits, in pieces only up to
+ * the loss.  What is below 2^-100 of the norm may be lost.
+ * A matrix of zeros stays zeros, one that holds an infinity or NaN is NaN everywhere.
  *   n_matrices    >= 1
  *   in, out       HOST arrays of DEVICE pointers [rows][cols], dense, each aligned to its type
  *                 (out[i] may be in[i]; no other two overlap)
  *   rows, cols    HOST, >= 0; the smaller of the two at most 2^14, the other 2^26
+ *                 (matrices that follow one another, up to 40: below 2^33 values in all, each side
+ *                 rounded up to 64)
  *   dts           HOST: colbandit_dtype of each matrix and its output
  *   steps         1 .. 64
  *   coefficients  HOST float [3]: a, b, c.  Refused (COLBANDIT_ERR_KNOB) where singular values from

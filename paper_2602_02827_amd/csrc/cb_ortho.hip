@@ -15,13 +15,21 @@ namespace {
 // Here X, A and B are held as two fp16 pieces each, 22 bits, a product is three products of pieces (the fourth is 2^-22 of it), and
 // sums are in 32 bits: the result is as far from 64 bits (1.7e-6) as that of plain 32-bit products, at a third of the 16-bit rate
 // instead of a sixteenth.  fp16 has few exponents: pieces are held times a power of two that puts the largest possible value (the
-// host knows how far the polynomial can take a singular value) just below overflow, so that second pieces are normal numbers.
-constexpr float kScaleX = 8192.f, kScaleA = 2048.f, kScaleB = 1024.f;
+// host knows how far the polynomial can take a singular value) just below overflow.  Second pieces of what is more than 2^11 below that
+// are no normal numbers any more: whatever a value's size, 2^-40 of the matrix' norm is lost of it.  In a matrix whose rows or columns
+// are of very different sizes that is all there is of some, and each step raises it with them.  So that is the rule, by the steps'
+// polynomial and the sizes: WIDE, where what is lost could be raised to more than kLost of the result, or where small values become
+// smaller, X, A and B are held in 32 bits, and cut into three bf16 pieces as they are multiplied (six products of pieces, what is left
+// out is 2^-26).  (128 x 512, rows that fall to 10^-8 of the first, twelve usual steps: 7.7e-5 off in pieces, 7e-7 so, plain 32-bit
+// products 3e-6; five steps: 5e-7, 3e-7 and 1.4e-6.  An encoder's 25 matrices, five steps: 1,610 us in pieces, 3,410 WIDE; one of 768 x 128: 99 and
+// 155.)
+constexpr double kLost = 0x1p-19;
+constexpr double kSmallest = 0x1p-24 / 3.4641016151377544;       // root mean square of a second piece's rounding, of which 2^-24 is the last place
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
-// Pieces lie in lines of 128 bytes: 32 consecutive values of a row, all first pieces and then all second ones.  The lines of a block
+// Values lie in lines of 128 bytes: 32 consecutive ones of a row, all first pieces and then all second ones, or 32 bits each.  The lines of a block
 // of 32 columns follow one another, so that what a tile reads at once lies side by side (with a row's lines side by side the rows of a
 // tile lie a few KB apart, in a quarter of the L2's channels).
 constexpr int kLine = 128;
@@ -35,11 +43,15 @@ __device__ __forceinline__ void split(const f32x4& x, f16x4& first, f16x4& secon
     first = __builtin_convertvector(x, f16x4);
     second = __builtin_convertvector(x - __builtin_convertvector(first, f32x4), f16x4);
 }
-__device__ __forceinline__ void store_line(char* line, int at, const f32x4& x) {
-    f16x4 first, second;
-    split(x, first, second);
-    *(f16x4*)(line + 2 * at) = first;
-    *(f16x4*)(line + 64 + 2 * at) = second;
+template <bool WIDE> __device__ __forceinline__ void store_line(char* line, int at, const f32x4& x) {
+    if constexpr (WIDE) {
+        *(f32x4*)(line + 4 * at) = x;
+    } else {
+        f16x4 first, second;
+        split(x, first, second);
+        *(f16x4*)(line + 2 * at) = first;
+        *(f16x4*)(line + 64 + 2 * at) = second;
+    }
 }
 __device__ __forceinline__ void split(const f32x8& x, f16x8& first, f16x8& second) {
     first = __builtin_convertvector(x, f16x8);
@@ -135,7 +147,8 @@ template <class E> __device__ __forceinline__ void load_side(const E* p, const O
         }
     }
 }
-__global__ __launch_bounds__(kThreads) void k_ortho_in(const OrthoTable* __restrict__ table, const double* parts, char* ws) {
+template <bool WIDE>
+__global__ __launch_bounds__(kThreads) void k_ortho_in(const OrthoTable* __restrict__ table, const double* parts, char* ws, float scale) {
     const OrthoTable& t = *table;
     __shared__ float side[kSide][kSide + 1];
     const int i = find_matrix(t, blockIdx.x, [&](int j) { return t.of[j].side0; });
@@ -145,7 +158,7 @@ __global__ __launch_bounds__(kThreads) void k_ortho_in(const OrthoTable* __restr
     for (int c = threadIdx.x; c < chunks; c += kThreads) sum += parts[M.chunk0 + c];
     sum = block_total(sum);
     // a matrix of zeros stays one; one that is not finite is NaN everywhere, as its products would be
-    const double by = sum == 0.0 ? 0.0 : sum < (double)INFINITY ? (double)kScaleX / sqrt(sum) : (double)NAN;
+    const double by = sum == 0.0 ? 0.0 : sum < (double)INFINITY ? (double)scale / sqrt(sum) : (double)NAN;
     const int across = M.np / kSide, at = blockIdx.x - M.side0;
     const int i0 = at / across * kSide, j0 = at % across * kSide;
     if (M.bf16) load_side((const __bf16*)M.in, M, i0, j0, by, side);
@@ -156,7 +169,7 @@ __global__ __launch_bounds__(kThreads) void k_ortho_in(const OrthoTable* __restr
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         const float* x = &side[r][c + 4 * q];
-        store_line(line, c % 32 + 4 * q, f32x4{x[0], x[1], x[2], x[3]});
+        store_line<WIDE>(line, c % 32 + 4 * q, f32x4{x[0], x[1], x[2], x[3]});
     }
 }
 
@@ -184,6 +197,21 @@ __device__ __forceinline__ int turn_of(int row) {
 }
 __device__ __forceinline__ f16x8 read_piece(lds_ptr p) { return *(const __attribute__((address_space(3))) f16x8*)(uintptr_t)p; }
 __device__ __forceinline__ void mma(f32x16& acc, const f16x8& a, const f16x8& b) { acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, acc, 0, 0, 0); }
+__device__ __forceinline__ f32x4 read_four(lds_ptr p) { return *(const __attribute__((address_space(3))) f32x4*)(uintptr_t)p; }
+__device__ __forceinline__ float read_one(lds_ptr p) { return *(const __attribute__((address_space(3))) float*)(uintptr_t)p; }
+
+// (WIDE) Eight values cut into three pieces, each rounded: what they leave is 2^-27 of a value.
+struct Cut {
+    bf16x8 p[3];
+    __device__ __forceinline__ Cut() {}
+    __device__ __forceinline__ explicit Cut(const f32x8& x) {
+        p[0] = __builtin_convertvector(x, bf16x8);
+        const f32x8 rest = x - __builtin_convertvector(p[0], f32x8);
+        p[1] = __builtin_convertvector(rest, bf16x8);
+        p[2] = __builtin_convertvector(rest - __builtin_convertvector(p[1], f32x8), bf16x8);
+    }
+};
+__device__ __forceinline__ void mma(f32x16& acc, const bf16x8& a, const bf16x8& b) { acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, acc, 0, 0, 0); }
 
 // Eight values of a row of the output, which has the input's shape.
 __device__ __forceinline__ void store_row(const OrthoMatrix& M, int row, int col, const f32x8& z) {
@@ -207,16 +235,40 @@ __device__ __forceinline__ void store_row(const OrthoMatrix& M, int row, int col
 }
 
 struct Piece { int row, col; };                      // of a tile: eight values from here on
-__device__ __forceinline__ void store_piece(char* line, const Piece& p, const f32x8& z) {
-    f16x8 first, second;
-    split(z, first, second);
-    *(f16x8*)(line + p.col % 32 * 2) = first;
-    *(f16x8*)(line + 64 + p.col % 32 * 2) = second;
+template <bool WIDE> __device__ __forceinline__ void store_piece(char* line, const Piece& p, const f32x8& z) {
+    if constexpr (WIDE) {
+        f32x4* to = (f32x4*)(line + p.col % 32 * 4);
+        to[0] = __builtin_shufflevector(z, z, 0, 1, 2, 3);
+        to[1] = __builtin_shufflevector(z, z, 4, 5, 6, 7);
+    } else {
+        f16x8 first, second;
+        split(z, first, second);
+        *(f16x8*)(line + p.col % 32 * 2) = first;
+        *(f16x8*)(line + 64 + p.col % 32 * 2) = second;
+    }
 }
+// One as it is stored.
+template <bool WIDE> struct Stored {
+    f16x8 x[2];
+    __device__ __forceinline__ void load(const char* line, const Piece& p) {
+        x[0] = *(const f16x8*)(line + p.col % 32 * 2);
+        x[1] = *(const f16x8*)(line + p.col % 32 * 2 + 64);
+    }
+    __device__ __forceinline__ f32x8 value() const { return __builtin_convertvector(x[0], f32x8) + __builtin_convertvector(x[1], f32x8); }
+};
+template <> struct Stored<true> {
+    f32x4 x[2];
+    __device__ __forceinline__ void load(const char* line, const Piece& p) {
+        x[0] = *(const f32x4*)(line + p.col % 32 * 4);
+        x[1] = *(const f32x4*)(line + p.col % 32 * 4 + 16);
+    }
+    __device__ __forceinline__ f32x8 value() const { return __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7); }
+};
 
 // DEEP: that many groups of four wavefronts share a tile, each with every DEEP-th tile of k; their sums are added in their order.
-template <int T, int DEEP, int AHEAD, int STEP, bool LAST>
-__global__ __launch_bounds__(DEEP * kThreads, DEEP > 1 ? DEEP : 2) void k_ortho_product(const OrthoTable* __restrict__ table, char* ws, int odd, int back, float a, float b, float c) {
+template <int T, int DEEP, int AHEAD, bool WIDE, int STEP, bool LAST>
+__global__ __launch_bounds__(DEEP * kThreads, DEEP > 1 ? DEEP : 2) void k_ortho_product(const OrthoTable* __restrict__ table, char* ws, int odd,
+                                                                                        int back, float by, float more) {
     constexpr int NB = T / 64;                       // blocks of 32 of a wavefront's side
     constexpr int BYTES = 2 * T * kLine, COPIES = T / 16;
     __shared__ __align__(256) char lds[DEEP][AHEAD + 1][BYTES];
@@ -274,6 +326,9 @@ __global__ __launch_bounds__(DEEP * kThreads, DEEP > 1 ? DEEP : 2) void k_ortho_
         return Piece{(p >> 2) % T, (p >> 2) / T * 32 + (p & 3) * 8};
     };
     f32x16 acc[NB][NB] = {};                         // [j][i]
+    // (WIDE) of all but the first pieces: small sums, which are rounded as such (12 usual steps of graded matrices: with one sum for all
+    // of them 0.6 of plain 32-bit products' error, so 0.4)
+    f32x16 more_acc[WIDE ? NB : 1][WIDE ? NB : 1] = {};
     for (int kb = 0; kb < AHEAD && kb < steps; ++kb) issue(kb);
     for (int kb = 0; kb < steps; ++kb) {
         // this tile's copies have arrived: those of AHEAD - 1 later ones may be under way
@@ -282,6 +337,39 @@ __global__ __launch_bounds__(DEEP * kThreads, DEEP > 1 ? DEEP : 2) void k_ortho_
         if (kb + AHEAD < steps) issue(kb + AHEAD);
         const uint32_t from = (uint32_t)(kb % (AHEAD + 1) * BYTES);
         if (DEEP > 1 && kb * DEEP + deep >= tiles) continue;
+        if constexpr (WIDE) {
+            auto row_operand = [&](lds_ptr line, int s) {
+                const lds_ptr at = line + from + (uint32_t)(((4 * s + 2 * h) ^ turn_of(n)) << 4);
+                return Cut(__builtin_shufflevector(read_four(at), read_four(at ^ 16), 0, 1, 2, 3, 4, 5, 6, 7));
+            };
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                Cut p[NB], q[NB];
+#pragma unroll
+                for (int x = 0; x < NB; ++x) {
+                    p[x] = row_operand(p_place + (uint32_t)(x * 32 * kLine), s);
+                    if constexpr (STEP != APPLY) {
+                        q[x] = row_operand(q_place + (uint32_t)(x * 32 * kLine), s);
+                    } else {                         // column n of eight rows
+                        f32x8 z;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const int row = 16 * s + 8 * h + e;
+                            z[e] = read_one(base + from + (uint32_t)((T + wj + 32 * x + row) * kLine + (((n >> 2) ^ turn_of(row)) << 4) + (n & 3) * 4));
+                        }
+                        q[x] = Cut(z);
+                    }
+                }
+                constexpr int X[6] = {2, 0, 1, 1, 0, 0}, Y[6] = {0, 2, 1, 0, 1, 0};      // the smallest first
+#pragma unroll
+                for (int z = 0; z < 6; ++z)
+#pragma unroll
+                    for (int x = 0; x < NB; ++x)
+#pragma unroll
+                        for (int y = 0; y < NB; ++y) mma(z < 5 ? more_acc[x][y] : acc[x][y], q[x].p[X[z]], p[y].p[Y[z]]);
+            }
+            continue;
+        }
         // all operands are asked for first: the products begin with the first ones while the others arrive
         f16x8 p[2][NB][2], q[2][NB][2];
 #pragma unroll
@@ -313,16 +401,19 @@ __global__ __launch_bounds__(DEEP * kThreads, DEEP > 1 ? DEEP : 2) void k_ortho_
 #pragma unroll
                     for (int y = 0; y < NB; ++y) mma(acc[x][y], q[s][x][z == 0], p[s][y][z == 1]);
     }
+    if constexpr (WIDE)
+#pragma unroll
+        for (int x = 0; x < NB; ++x)
+#pragma unroll
+            for (int y = 0; y < NB; ++y) acc[x][y] += more_acc[x][y];
     // (before the products the first copies would be waited for together with it: 1,600 us instead of 1,576 for an encoder's matrices)
-    f16x8 add[STEP == GRAM ? 1 : PIECES][2] = {};
+    Stored<WIDE> add[STEP == GRAM ? 1 : PIECES] = {};
     if constexpr (STEP != GRAM)
 #pragma unroll
         for (int x = 0; x < PIECES; ++x) {
             if (!has) break;
             const Piece p = piece_of(x);
-            const char* line = line_at(STEP == SQUARE ? P : X, i0 + p.row, rows, (j0 + p.col) / 32) + p.col % 32 * 2;
-            add[x][0] = *(const f16x8*)line;
-            add[x][1] = *(const f16x8*)(line + 64);
+            add[x].load(line_at(STEP == SQUARE ? P : X, i0 + p.row, rows, (j0 + p.col) / 32), p);
         }
     __syncthreads();
     // The tile goes through LDS once more, in 32 bits, so that lines are read and written whole (from the accumulators a lane would
@@ -338,8 +429,6 @@ __global__ __launch_bounds__(DEEP * kThreads, DEEP > 1 ? DEEP : 2) void k_ortho_
                 *(f32x4*)(tile_of + deep * T * T + place(wi + 32 * y + n, wj + 32 * x + 8 * r + 4 * h)) =
                     f32x4{acc[x][y][4 * r], acc[x][y][4 * r + 1], acc[x][y][4 * r + 2], acc[x][y][4 * r + 3]};
     char* to = ws + (STEP == GRAM ? M.a : STEP == SQUARE ? M.b : odd ? M.x : M.y);
-    const float by = STEP == GRAM ? kScaleA / (kScaleX * kScaleX) : STEP == SQUARE ? c * (kScaleB / (kScaleA * kScaleA)) : 1.f / kScaleB;
-    const float more = STEP == SQUARE ? b * (kScaleB / kScaleA) : a;
     constexpr bool AGAIN = STEP != GRAM || DEEP > 1;              // the transpose is stored from what was stored
     const bool mirrored = STEP != APPLY && ti != tj, again = STEP == APPLY ? LAST && M.tall : mirrored;
     __syncthreads();
@@ -356,9 +445,8 @@ __global__ __launch_bounds__(DEEP * kThreads, DEEP > 1 ? DEEP : 2) void k_ortho_
 #pragma unroll
             for (int e = 0; e < 4; ++e) z[4 * q + e] = v[e] * by;
         }
-        if constexpr (STEP != GRAM) z += (__builtin_convertvector(add[x][0], f32x8) + __builtin_convertvector(add[x][1], f32x8)) * more;
-        if constexpr (LAST) z *= 1.f / kScaleX;
-        if constexpr (!LAST) store_piece(line_at(to, i0 + p.row, rows, (j0 + p.col) / 32), p, z);
+        if constexpr (STEP != GRAM) z += add[x].value() * more;
+        if constexpr (!LAST) store_piece<WIDE>(line_at(to, i0 + p.row, rows, (j0 + p.col) / 32), p, z);
         else if (!M.tall) store_row(M, i0 + p.row, j0 + p.col, z);
         if constexpr (AGAIN) {
             if (again)                               // each thread's own places
@@ -377,7 +465,7 @@ __global__ __launch_bounds__(DEEP * kThreads, DEEP > 1 ? DEEP : 2) void k_ortho_
 #pragma unroll
         for (int e = 0; e < 8; ++e) z[e] = tile_of[place(p.col + e, p.row)] * (AGAIN ? 1.f : by);
         if constexpr (STEP == APPLY) store_row(M, j0 + p.row, i0 + p.col, z);
-        else store_piece(line_at(to, j0 + p.row, rows, (i0 + p.col) / 32), p, z);
+        else store_piece<WIDE>(line_at(to, j0 + p.row, rows, (i0 + p.col) / 32), p, z);
     }
 }
 
@@ -463,28 +551,40 @@ unsigned groups_of(const OrthoEnds& ends) {
 // small matrices, in tiles of 64 x 64, the copies' latency is all there is: three ahead, or, where there is no more than one tile for
 // each CU, four groups of wavefronts at a tile (nine fp32 matrices of up to 640 x 256: 152 us without, 139 so, 155 with them also
 // where tiles are more).
-template <int STEP, bool LAST = false>
-hipError_t launch_product(const OrthoGroup& G, const OrthoEnds& ends, char* ws, int odd, int back, const float* k, hipStream_t st) {
+template <bool WIDE, int STEP, bool LAST = false>
+hipError_t launch_product(const OrthoGroup& G, const OrthoEnds& ends, char* ws, int odd, int back, const OrthoPolynomial& K, hipStream_t st) {
     const dim3 grid(groups_of(ends));
-    if (G.tile == 128) k_ortho_product<128, 1, 1, STEP, LAST><<<grid, kThreads, 0, st>>>((const OrthoTable*)(ws + G.table), ws, odd, back, k[0], k[1], k[2]);
-    else if (grid.x <= 256) k_ortho_product<64, 4, 1, STEP, LAST><<<grid, 4 * kThreads, 0, st>>>((const OrthoTable*)(ws + G.table), ws, odd, back, k[0], k[1], k[2]);
-    else k_ortho_product<64, 1, 3, STEP, LAST><<<grid, kThreads, 0, st>>>((const OrthoTable*)(ws + G.table), ws, odd, back, k[0], k[1], k[2]);
+    const OrthoTable* t = (const OrthoTable*)(ws + G.table);
+    // what a tile is multiplied by as it is stored, and what it is added to; the pieces' scales among them (the last step's are taken out)
+    const float last = LAST ? 1.f / K.scale_x : 1.f;
+    const float by = STEP == GRAM ? K.scale_a / (K.scale_x * K.scale_x) : STEP == SQUARE ? K.c * (K.scale_b / (K.scale_a * K.scale_a)) : last / K.scale_b;
+    const float more = STEP == SQUARE ? K.b * (K.scale_b / K.scale_a) : K.a * last;
+    if (G.tile == 128) k_ortho_product<128, 1, 1, WIDE, STEP, LAST><<<grid, kThreads, 0, st>>>(t, ws, odd, back, by, more);
+    else if (grid.x <= 256) k_ortho_product<64, 4, 1, WIDE, STEP, LAST><<<grid, 4 * kThreads, 0, st>>>(t, ws, odd, back, by, more);
+    else k_ortho_product<64, 1, 3, WIDE, STEP, LAST><<<grid, kThreads, 0, st>>>(t, ws, odd, back, by, more);
     return hipGetLastError();
 }
 
-hipError_t launch_group(const OrthoGroup& G, char* ws, int steps, const float* k, hipStream_t st) {
+// Whether two pieces hold all matrices' values well enough for the polynomial's steps.
+bool pieces_hold(const OrthoGroup& G, const OrthoPolynomial& K) {
+    for (int i = 0; i < G.t.n; ++i)
+        if (!(sqrt((double)G.t.of[i].m * G.t.of[i].n) * (kSmallest / K.scale_x) * K.raised <= kLost)) return false;
+    return true;
+}
+
+template <bool WIDE> hipError_t launch_group(const OrthoGroup& G, char* ws, int steps, const OrthoPolynomial& K, hipStream_t st) {
     double* parts = (double*)(ws + G.parts);
     k_ortho_norm<<<dim3((unsigned)G.chunks), kThreads, 0, st>>>(G.t, parts, (OrthoTable*)(ws + G.table));
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    k_ortho_in<<<dim3((unsigned)G.sides), kThreads, 0, st>>>((const OrthoTable*)(ws + G.table), parts, ws);
+    k_ortho_in<WIDE><<<dim3((unsigned)G.sides), kThreads, 0, st>>>((const OrthoTable*)(ws + G.table), parts, ws, K.scale_x);
     e = hipGetLastError();
     for (int s = 0; s < steps && e == hipSuccess; ++s) {
         const int odd = s & 1;
-        if ((e = launch_product<GRAM>(G, G.t.gram, ws, odd, s & 1, k, st)) != hipSuccess) break;
-        if ((e = launch_product<SQUARE>(G, G.t.square, ws, odd, ~s & 1, k, st)) != hipSuccess) break;
-        e = s + 1 < steps ? launch_product<APPLY>(G, G.t.apply, ws, odd, s & 1, k, st)
-                          : launch_product<APPLY, true>(G, G.t.apply, ws, odd, s & 1, k, st);
+        if ((e = launch_product<WIDE, GRAM>(G, G.t.gram, ws, odd, s & 1, K, st)) != hipSuccess) break;
+        if ((e = launch_product<WIDE, SQUARE>(G, G.t.square, ws, odd, ~s & 1, K, st)) != hipSuccess) break;
+        e = s + 1 < steps ? launch_product<WIDE, APPLY>(G, G.t.apply, ws, odd, s & 1, K, st)
+                          : launch_product<WIDE, APPLY, true>(G, G.t.apply, ws, odd, s & 1, K, st);
     }
     return e;
 }
@@ -513,12 +613,14 @@ bool ortho_launchable(int64_t n, const int64_t* rows, const int64_t* cols) {
 
 // Groups use the workspace one after the other.
 hipError_t launch_ortho(int64_t n, const void* const* in, void* const* out, const int64_t* rows, const int64_t* cols, const int32_t* dts,
-                        int steps, const float* coefficients, char* ws, hipStream_t st) {
+                        int steps, const OrthoPolynomial& polynomial, char* ws, hipStream_t st) {
+    OrthoPolynomial whole = polynomial;
+    whole.scale_x = whole.scale_a = whole.scale_b = 1.f;
     for (int64_t i = 0; i < n;) {
         const OrthoGroup G = group_from(i, n, rows, cols, in, out, dts);
         i = G.end;
         if (!G.t.n) continue;
-        const hipError_t e = launch_group(G, ws, steps, coefficients, st);
+        const hipError_t e = pieces_hold(G, polynomial) ? launch_group<false>(G, ws, steps, polynomial, st) : launch_group<true>(G, ws, steps, whole, st);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;

@@ -104,9 +104,15 @@ size_t rotate_workspace_bytes(const RotateArgs& A, int d);
 hipError_t launch_rotate(const RotateArgs& A, int d, int dt, hipStream_t st);
 hipError_t launch_rotate_backward(const RotateArgs& A, int d, int dt, float* dq_weight, float* dk_weight, hipStream_t st);
 
+// A polynomial a s + b s^3 + c s^5 and what is known of its steps from singular values of up to one on.
+struct OrthoPolynomial {
+    float a, b, c;
+    float scale_x, scale_a, scale_b; // powers of two that X, A and B are held times in 16-bit pieces (1 in 32 bits)
+    double raised;                   // factor by which the steps raise small values at most; infinite where they lower them
+};
 size_t ortho_workspace_bytes(int64_t n, const int64_t* rows, const int64_t* cols);
 bool ortho_launchable(int64_t n, const int64_t* rows, const int64_t* cols);
 hipError_t launch_ortho(int64_t n, const void* const* in, void* const* out, const int64_t* rows, const int64_t* cols, const int32_t* dts,
-                        int steps, const float* coefficients, char* ws, hipStream_t st);
+                        int steps, const OrthoPolynomial& polynomial, char* ws, hipStream_t st);
 
 }  // namespace cb

@@ -299,12 +299,16 @@ int rotate_args(const colbandit_rotation* r, bool back, RotateArgs& A) {
     return fits_a_grid(rotate_groups(A, r->d, back), 256) ? COLBANDIT_OK : COLBANDIT_ERR_UNSUPPORTED;
 }
 
+// The largest power of two that takes what is at most `limit` in size to no more than three quarters of what 16 bits hold.
+float scale_for(double limit) { return (float)exp2(floor(log2(49152.0 / fmax(limit, 1.0)))); }
+
 // Whether singular values from 0 to 1 stay within what the pieces of X, A and B can hold (4, 16 and 32 in size) over all steps of
-// s <- a s + b s^3 + c s^5.  A polynomial's extremes are where its derivative is zero, and at the ends.
-bool polynomial_holds(const float* k, int steps) {
+// s <- a s + b s^3 + c s^5, and what the kernels have to know of them.  A polynomial's extremes are where its derivative is zero, and
+// at the ends.
+bool polynomial_holds(const float* k, int steps, OrthoPolynomial& P) {
     const double a = k[0], b = k[1], c = k[2];
     if (!isfinite(a) || !isfinite(b) || !isfinite(c)) return false;
-    double most = 1.0;
+    double most = 1.0, most_x = 1.0, most_b = 0.0, raised = 1.0;
     for (int s = 0; s < steps; ++s) {
         most *= 1.0001;                              // (roundings)
         if (most > 4.0) return false;
@@ -313,6 +317,12 @@ bool polynomial_holds(const float* k, int steps) {
         double side = square(u1);
         if (c != 0.0 && -b / (2 * c) > 0.0 && -b / (2 * c) < u1) side = fmax(side, square(-b / (2 * c)));
         if (side > 32.0) return false;
+        most_x = fmax(most_x, most);
+        most_b = fmax(most_b, side);
+        auto factor = [&](double u) { return fabs(a + b * u + c * u * u); };      // of a singular value sqrt(u)
+        double most_factor = fmax(factor(0.0), factor(u1));
+        if (c != 0.0 && -b / (2 * c) > 0.0 && -b / (2 * c) < u1) most_factor = fmax(most_factor, factor(-b / (2 * c)));
+        raised *= most_factor;
         auto value = [&](double u) { return fabs(sqrt(u) * (a + b * u + c * u * u)); };
         double next = value(u1);
         const double q[3] = {5 * c, 3 * b, a};       // of u = s^2
@@ -331,6 +341,7 @@ bool polynomial_holds(const float* k, int steps) {
             if (roots[i] > 0.0 && roots[i] < u1) next = fmax(next, value(roots[i]));
         most = next;
     }
+    P = {k[0], k[1], k[2], scale_for(most_x), scale_for(most_x * most_x), scale_for(most_b), fabs(a) < 1.0 ? (double)INFINITY : raised};
     return most <= 4.0;
 }
 
@@ -495,7 +506,8 @@ int colbandit_orthogonalise(int64_t n_matrices, const void* const* in, void* con
     int rc = check_matrices(n_matrices, rows, cols);
     if (rc) return rc;
     if (steps < 1) return COLBANDIT_ERR_SHAPE;
-    if (steps > 64 || !polynomial_holds(coefficients, steps)) return COLBANDIT_ERR_KNOB;
+    OrthoPolynomial polynomial;
+    if (steps > 64 || !polynomial_holds(coefficients, steps, polynomial)) return COLBANDIT_ERR_KNOB;
     for (int64_t i = 0; i < n_matrices; ++i) {
         if (!is_type(dts[i])) return COLBANDIT_ERR_SHAPE;
         if (rows[i] && cols[i] && (!in[i] || !out[i])) return COLBANDIT_ERR_NULL;
@@ -503,7 +515,7 @@ int colbandit_orthogonalise(int64_t n_matrices, const void* const* in, void* con
     }
     rc = workspace_ok(workspace, workspace_bytes, ortho_workspace_bytes(n_matrices, rows, cols));
     if (rc) return rc;
-    return hip(launch_ortho(n_matrices, in, out, rows, cols, dts, steps, coefficients, (char*)workspace, (hipStream_t)stream));
+    return hip(launch_ortho(n_matrices, in, out, rows, cols, dts, steps, polynomial, (char*)workspace, (hipStream_t)stream));
 }
 
 int colbandit_maxsim_scores(const void* Q, int n_queries, int T, int d, colbandit_dtype dt, const void* docs, const int64_t* offsets,

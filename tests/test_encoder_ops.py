@@ -914,6 +914,58 @@ def test_matrices_of_low_rank(tr, dev, rank, noise):
     check_orthogonal(m, tr.colbandit_orthogonalise(m)["out"])
 
 
+def graded(kind, by, shape, seed=9):
+    """Rows or columns that fall to 10^-by of the first, or one row and others that are all that small."""
+    x = torch.randn(shape, generator=torch.Generator().manual_seed(seed))
+    if kind == "one":
+        x[1:] *= 10.0 ** -by
+        return x
+    n = shape[0 if kind == "rows" else 1]
+    fall = torch.logspace(0, -by, n)
+    return x * (fall[:, None] if kind == "rows" else fall)
+
+
+@gpu
+@pytest.mark.parametrize("kind,by", [("rows", 6), ("rows", 8), ("rows", 10), ("columns", 6), ("columns", 10), ("one", 4), ("one", 8)])
+@pytest.mark.parametrize("steps,k", [(5, POLYNOMIAL), (6, POLYNOMIAL), (8, POLYNOMIAL), (12, POLYNOMIAL), (20, POLYNOMIAL),
+                                     (12, (1.875, -1.25, 0.375)), (64, (1.5, -0.5, 0.0))])
+def test_graded_matrices(tr, dev, kind, by, steps, k):
+    """What is small beside a matrix' norm counts as much as the rest once enough steps have raised it."""
+    m = [graded(kind, by, shape).to(dev) for shape in ((128, 512), (300, 129), (64, 70))]
+    out = tr.colbandit_orthogonalise(m, steps=steps, coefficients=k)["out"]
+    check_orthogonal(m, out, steps, k)
+
+
+def rows_are_right(g, o, steps, k):
+    """Each row on its own: 32-bit values and sums, whose products lose 2^-26, are off by what plain 32-bit products are off by."""
+    g, o = g.cpu(), o.double().cpu()
+    k32 = [float(np.float32(x)) for x in k]
+    want = polynomial_steps(g.double(), steps, k32, torch.float64)
+    plain = ((polynomial_steps(g.float(), steps, k32, torch.float32).double() - want).norm(dim=1) / want.norm(dim=1)).max()
+    assert float(((o - want).norm(dim=1) / want.norm(dim=1)).max()) <= 4 * float(plain) + 4 * steps * E32
+
+
+@gpu
+@pytest.mark.parametrize("kind,by", [("rows", 8), ("columns", 8), ("one", 8)])
+@pytest.mark.parametrize("steps,k", [(12, POLYNOMIAL), (64, (1.5, -0.5, 0.0)), (5, (0.5, 0.0, 0.0)), (40, (0.6, 0.2, 0.0))])
+def test_rows_of_graded_matrices(tr, dev, kind, by, steps, k):
+    """Where steps raise what is small far, or make all of a matrix small, values are held in 32 bits."""
+    for shape in ((128, 512), (300, 129)):
+        m = graded(kind, by, shape).to(dev)
+        rows_are_right(m, tr.colbandit_orthogonalise([m], steps=steps, coefficients=k)["out"][0], steps, k)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,steps", [("bf16", 5), ("f32", 5), ("f32", 9)])
+def test_matrices_with_long_sides(tr, dev, dtype, steps):
+    """Sides above 1,000, tiles of 64 and, with enough of them, of 128: pieces and, of nine steps, 32 bits."""
+    m = updates([(1030, 1100), (33, 5000), (2100, 70)], dtype, dev, seed=10)
+    check_orthogonal(m, tr.colbandit_orthogonalise(m, steps=steps)["out"], steps)
+    m += updates([(1030, 1029)] * 6, dtype, dev, seed=11)
+    out = tr.colbandit_orthogonalise(m, steps=steps)["out"]
+    check_orthogonal(m[:4], out[:4], steps)
+
+
 @gpu
 def test_extreme_matrices(tr, dev):
     """Zeros stay zeros, any finite size is normalised, what is not finite is NaN, and neither touches the others of the list."""
