@@ -326,16 +326,13 @@ bool polynomial_holds(const float* k, int steps, OrthoPolynomial& P) {
         auto value = [&](double u) { return fabs(sqrt(u) * (a + b * u + c * u * u)); };
         double next = value(u1);
         const double q[3] = {5 * c, 3 * b, a};       // of u = s^2
+        const double under = q[1] * q[1] - 4 * q[0] * q[2];
         double roots[2];
         int n = 0;
-        if (q[0] == 0.0) {
-            if (q[1] != 0.0) roots[n++] = -q[2] / q[1];
-        } else {
-            const double under = q[1] * q[1] - 4 * q[0] * q[2];
-            if (under >= 0.0) {
-                roots[n++] = (-q[1] + sqrt(under)) / (2 * q[0]);
-                roots[n++] = (-q[1] - sqrt(under)) / (2 * q[0]);
-            }
+        if (under >= 0.0) {                          // without a difference, which a small q[0] would leave nothing of
+            const double sum = -0.5 * (q[1] + copysign(sqrt(under), q[1]));
+            if (q[0] != 0.0) roots[n++] = sum / q[0];
+            if (sum != 0.0) roots[n++] = q[2] / sum;
         }
         for (int i = 0; i < n; ++i)
             if (roots[i] > 0.0 && roots[i] < u1) next = fmax(next, value(roots[i]));

@@ -1190,6 +1190,14 @@ def test_orthogonalising_refusals(tr):
     assert call(g=(0x1002, 0x2000)) == -6 and call(o=(0x1000, 0x2001)) == -6 and call(ws=0x10010) == -6 and call(nb=64) == -5
 
 
+def test_polynomials_with_a_small_leading_coefficient_are_refused_too(tr):
+    """An extreme between the ends, where the quadratic formula's own cancellation loses it."""
+    for k in ((30.0, -30.0, 1e-30), (30.0, -30.0, 0.0), (30.0, -30.0, -1e-25), (-30.0, 30.0, 1e-20)):
+        arr = lambda t, *v: (t * len(v))(*v)  # noqa: E731
+        assert tr.lib().colbandit_orthogonalise(1, arr(ctypes.c_void_p, 0x1000), arr(ctypes.c_void_p, 0x1000), arr(ctypes.c_int64, 4),
+                                                arr(ctypes.c_int64, 5), arr(ctypes.c_int32, 0), 1, arr(ctypes.c_float, *k), None, 0, None) == -3
+
+
 def test_python_refusals(tr):
     """Shapes, types and places are checked before the library is called."""
     W, t = torch.zeros(5, 8), torch.zeros(3, dtype=torch.int64)
