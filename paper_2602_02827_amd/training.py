@@ -29,6 +29,7 @@ EXPORTS = [
 ]
 
 _DTYPES = {torch.bfloat16: BF16, torch.float32: F32}
+_ERR_WORKSPACE = -5                                  # COLBANDIT_ERR_WORKSPACE
 
 
 class ColbanditAttn(ctypes.Structure):
@@ -462,6 +463,13 @@ def colbandit_orthogonalise(matrices, *, steps=5, coefficients=POLYNOMIAL, out=N
     """Each of `matrices` (a list of contiguous 2-d float32 or bfloat16 tensors) with its singular values brought near to one by
     `steps` of s <- a s + b s^3 + c s^5, after a division by its Frobenius norm.  Into `out` (a list alike; it may be `matrices`), or
     new tensors.  Returns dict(out)."""
+    to, call = _orthogonalise(matrices, steps, coefficients, out, workspace)
+    _check(call(), "colbandit_orthogonalise")
+    return {"out": to}
+
+
+def _orthogonalise(matrices, steps, coefficients, out, workspace=None):
+    """Outputs, and the library's call: without room for its work, which it asks for last, it checks all else and does nothing."""
     matrices = list(matrices)
     to = [torch.empty_like(m) for m in matrices] if out is None else list(out)
     if not matrices or len(to) != len(matrices):
@@ -477,10 +485,9 @@ def colbandit_orthogonalise(matrices, *, steps=5, coefficients=POLYNOMIAL, out=N
     rows, cols = sizes(*[m.shape[0] for m in matrices]), sizes(*[m.shape[1] for m in matrices])
     L = lib()
     ws, nb = _workspace(workspace, L.colbandit_orthogonalise_workspace_bytes(n, rows, cols), matrices[0].device)
-    _check(L.colbandit_orthogonalise(n, pointers(*[m.data_ptr() for m in matrices]), pointers(*[o.data_ptr() for o in to]), rows, cols,
-                                     (ctypes.c_int32 * n)(*[_DTYPES[m.dtype] for m in matrices]), steps,
-                                     (ctypes.c_float * 3)(*coefficients), _ptr(ws), nb, _stream()), "colbandit_orthogonalise")
-    return {"out": to}
+    args = (n, pointers(*[m.data_ptr() for m in matrices]), pointers(*[o.data_ptr() for o in to]), rows, cols,
+            (ctypes.c_int32 * n)(*[_DTYPES[m.dtype] for m in matrices]), steps, (ctypes.c_float * 3)(*coefficients), _ptr(ws))
+    return to, lambda room=True: L.colbandit_orthogonalise(*args, nb if room else 0, _stream())
 
 
 # ---- as parts of a torch program ---------------------------------------------------------------------
@@ -613,22 +620,35 @@ def orthogonal_step_(parameters, momenta, rate, momentum=0.95, steps=5, coeffici
     """One step of descent along orthogonalised momenta, for 2-d parameters: of each that has a gradient the momentum becomes
     momentum * itself + gradient, and the parameter goes down `rate` times sqrt(max(1, rows / columns)) times
     colbandit_orthogonalise of gradient + momentum * itself.  `momenta`: a dict of the parameters' momenta, which this fills; they are
-    float32 whatever the parameters' type."""
+    float32 whatever the parameters' type.  A step that is refused changes nothing."""
     parameters = [p for p in dict.fromkeys(parameters) if p.grad is not None and p.numel()]
     if not parameters:
         return
-    for p in parameters:                             # before any momentum is changed
+    rate, momentum = float(rate), float(momentum)
+    for p in parameters:
         if p.dim() != 2 or p.dtype not in _DTYPES:
             raise ValueError("parameters must be two-dimensional, and float32 or bfloat16")
-    _on_device(*parameters)
-    updates = []
+        if p.grad.layout != torch.strided:
+            raise ValueError("gradients must be dense")
+        m = momenta.get(p)
+        if m is not None and (m.shape != p.shape or m.layout != torch.strided or not m.is_floating_point()):
+            raise ValueError("momenta must be dense, of floating point and their parameters' shapes")
+    there = [m for m in map(momenta.get, parameters) if m is not None]
+    _on_device(*parameters, *there)
     with torch.no_grad():
-        for p in parameters:
-            m = momenta.get(p)
-            if m is None:
-                m = momenta[p] = torch.zeros_like(p, dtype=torch.float32, memory_format=torch.contiguous_format)
+        # all memory is there, and the library has nothing against the call, before any momentum is changed
+        updates = [torch.empty(p.shape, dtype=torch.float32, device=p.device) for p in parameters]
+        new = {p: torch.zeros_like(p, dtype=torch.float32, memory_format=torch.contiguous_format) for p in parameters
+               if momenta.get(p) is None}
+        _, call = _orthogonalise(updates, steps, coefficients, updates)
+        rc = call(room=False)
+        if rc != _ERR_WORKSPACE:
+            raise ColbanditError(rc, "colbandit_orthogonalise")
+        momenta.update(new)
+        for p, u in zip(parameters, updates):
+            m = momenta[p]
             m.mul_(momentum).add_(p.grad)
-            updates.append(torch.add(p.grad, m, alpha=momentum).contiguous())
-        colbandit_orthogonalise(updates, steps=steps, coefficients=coefficients, out=updates)
+            torch.add(p.grad, m, alpha=momentum, out=u)
+        _check(call(), "colbandit_orthogonalise")
         for p, u in zip(parameters, updates):
             p.sub_(u, alpha=rate * math.sqrt(max(1.0, p.shape[0] / p.shape[1])))

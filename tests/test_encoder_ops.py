@@ -1015,6 +1015,34 @@ def test_orthogonalising_in_place_in_graphs_and_steps(tr, dev):
 
 
 @gpu
+@pytest.mark.parametrize("bad", ["coefficients", "steps", "many", "size", "momentum", "sparse"])
+def test_refused_steps_change_nothing(tr, dev, bad):
+    """Neither momenta nor parameters, nor is a momentum made."""
+    p = [torch.nn.Parameter(torch.randn(30, 20, device=dev)), torch.nn.Parameter(torch.randn(20, 30, device=dev))]
+    for x in p:
+        x.grad = torch.randn_like(x)
+    momenta, how = {}, {}
+    tr.orthogonal_step_(p[:1], momenta, rate=0.1)
+    if bad == "coefficients":
+        how = dict(coefficients=(5.0, 0.0, 0.0))
+    elif bad in ("steps", "many"):
+        how = dict(steps=0 if bad == "steps" else 65)
+    elif bad == "size":
+        p.append(torch.nn.Parameter(torch.zeros(16385, 16385, device=dev, dtype=torch.bfloat16)))
+        p[-1].grad = torch.zeros_like(p[-1])
+    elif bad == "momentum":
+        momenta[p[1]] = torch.ones(30, 20, device=dev)
+    else:
+        p[1].grad = p[1].grad.to_sparse()
+    before = {x: m.clone() for x, m in momenta.items()}
+    values = [x.detach().clone() for x in p]
+    with pytest.raises((ValueError, RuntimeError)):
+        tr.orthogonal_step_(p, momenta, rate=0.1, **how)
+    assert [id(x) for x in momenta] == [id(x) for x in before] and all(torch.equal(momenta[x], m) for x, m in before.items())
+    assert all(torch.equal(x, y) for x, y in zip(p, values))
+
+
+@gpu
 def test_momenta_of_16_bit_parameters_are_32_bits(tr, dev):
     """A gradient of 2^-10 of the momentum, which 16 bits would leave out, counts in every step."""
     p = torch.nn.Parameter(torch.zeros(24, 40, device=dev, dtype=torch.bfloat16))
