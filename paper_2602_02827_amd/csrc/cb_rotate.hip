@@ -213,10 +213,10 @@ int lg_parts_of(const RotateArgs& A, int lanes) {
     while (2 << lg <= A.heads + A.kv_heads && (A.rows * lanes << lg) < 1 << 19) ++lg;
     return lg;
 }
-constexpr int64_t kMostGroups = 1024;                // of the backward pass
+constexpr int64_t kMostGroups = 1024, kMostForward = 0xffffffffll / kThreads;        // of the backward pass; what a launch can have
 int64_t groups_of(const RotateArgs& A, int lg_parts, int lanes, bool back) {
-    const int64_t per = kThreads / lanes, groups = ((A.rows << lg_parts) + per - 1) / per;
-    return back && groups > kMostGroups ? kMostGroups : groups;
+    const int64_t per = kThreads / lanes, groups = ((A.rows << lg_parts) + per - 1) / per, most = back ? kMostGroups : kMostForward;
+    return groups > most ? most : groups;
 }
 int lanes_of(int d) { return d == 96 ? 16 : d / 8; }
 
@@ -245,8 +245,10 @@ template <bool BACK> hipError_t launch(const RotateArgs& A, int d, int dt, hipSt
 
 }  // namespace
 
-int64_t rotate_groups(const RotateArgs& A, int d, bool back) { return groups_of(A, lg_parts_of(A, lanes_of(d)), lanes_of(d), back); }
-size_t rotate_workspace_bytes(const RotateArgs& A, int d) { return (size_t)(rotate_groups(A, d, true) * 2 * d * 4 + 255) / 256 * 256; }
+namespace {
+int64_t parts_of(const RotateArgs& A, int d) { return groups_of(A, lg_parts_of(A, lanes_of(d)), lanes_of(d), true); }
+}
+size_t rotate_workspace_bytes(const RotateArgs& A, int d) { return (size_t)(parts_of(A, d) * 2 * d * 4 + 255) / 256 * 256; }
 
 hipError_t launch_rotate(const RotateArgs& A, int d, int dt, hipStream_t st) {
     return A.rows == 0 ? hipSuccess : launch<false>(A, d, dt, st);
@@ -257,7 +259,7 @@ hipError_t launch_rotate_backward(const RotateArgs& A, int d, int dt, float* dq_
         if (e != hipSuccess) return e;
     }
     if (!dq_weight && !dk_weight) return hipSuccess;
-    k_rotate_join<<<dim3((unsigned)(2 * d / kJoinValues)), kJoinThreads, 0, st>>>(A.part, A.rows ? (int)rotate_groups(A, d, true) : 0, d, dq_weight,
+    k_rotate_join<<<dim3((unsigned)(2 * d / kJoinValues)), kJoinThreads, 0, st>>>(A.part, A.rows ? (int)parts_of(A, d) : 0, d, dq_weight,
                                                                                   dk_weight);
     return hipGetLastError();
 }

@@ -99,7 +99,6 @@ struct RotateArgs {
     void *q_to, *k_to;                               // outputs, or gradients of the inputs
     float* part;                                     // the workgroups' sums for the weights' gradients
 };
-int64_t rotate_groups(const RotateArgs& A, int d, bool back);
 size_t rotate_workspace_bytes(const RotateArgs& A, int d);
 hipError_t launch_rotate(const RotateArgs& A, int d, int dt, hipStream_t st);
 hipError_t launch_rotate_backward(const RotateArgs& A, int d, int dt, float* dq_weight, float* dk_weight, hipStream_t st);

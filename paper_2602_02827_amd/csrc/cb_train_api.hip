@@ -262,7 +262,7 @@ int check_embedding(int64_t n, int64_t vocab, int64_t width, int64_t row, int dt
     return COLBANDIT_OK;
 }
 
-int rotate_args(const colbandit_rotation* r, bool back, RotateArgs& A) {
+int rotate_args(const colbandit_rotation* r, RotateArgs& A) {
     if (!r) return COLBANDIT_ERR_NULL;
     if (!is_type(r->dt) || r->rows < 0 || r->heads < 1 || r->kv_heads < 1 || r->d < 1) return COLBANDIT_ERR_SHAPE;
     if (!(r->eps >= 0.f && r->eps < INFINITY)) return COLBANDIT_ERR_KNOB;
@@ -296,7 +296,7 @@ int rotate_args(const colbandit_rotation* r, bool back, RotateArgs& A) {
     A.kv_heads = r->kv_heads;
     A.near = r->interleaved != 0;
     A.eps = r->eps;
-    return fits_a_grid(rotate_groups(A, r->d, back), 256) ? COLBANDIT_OK : COLBANDIT_ERR_UNSUPPORTED;
+    return COLBANDIT_OK;
 }
 
 // The largest power of two that takes what is at most `limit` in size to no more than three quarters of what 16 bits hold.
@@ -461,7 +461,7 @@ size_t colbandit_sizeof_rotation(void) { return sizeof(colbandit_rotation); }
 
 int colbandit_norm_rotate(const colbandit_rotation* r, void* q_out, void* k_out, void* stream) {
     RotateArgs A;
-    const int rc = rotate_args(r, false, A);
+    const int rc = rotate_args(r, A);
     if (rc) return rc;
     if (A.rows && (!q_out || !k_out)) return COLBANDIT_ERR_NULL;
     if (misaligned(q_out) || misaligned(k_out)) return COLBANDIT_ERR_ALIGNMENT;
@@ -472,13 +472,13 @@ int colbandit_norm_rotate(const colbandit_rotation* r, void* q_out, void* k_out,
 
 size_t colbandit_norm_rotate_workspace_bytes(const colbandit_rotation* r) {
     RotateArgs A;
-    return rotate_args(r, true, A) ? 0 : rotate_workspace_bytes(A, r->d);
+    return rotate_args(r, A) ? 0 : rotate_workspace_bytes(A, r->d);
 }
 
 int colbandit_norm_rotate_backward(const colbandit_rotation* r, const void* dq_out, const void* dk_out, void* dq, void* dk, float* dq_weight,
                                    float* dk_weight, void* workspace, size_t workspace_bytes, void* stream) {
     RotateArgs A;
-    int rc = rotate_args(r, true, A);
+    int rc = rotate_args(r, A);
     if (rc) return rc;
     if (A.rows && (!dq_out || !dk_out || !dq || !dk)) return COLBANDIT_ERR_NULL;
     if (misaligned(dq_out) || misaligned(dk_out) || misaligned(dq) || misaligned(dk) || misaligned(dq_weight, 4) || misaligned(dk_weight, 4))

@@ -1226,6 +1226,14 @@ def test_polynomials_with_a_small_leading_coefficient_are_refused_too(tr):
                                                 arr(ctypes.c_int64, 5), arr(ctypes.c_int32, 0), 1, arr(ctypes.c_float, *k), None, 0, None) == -3
 
 
+def test_rotation_takes_as_many_rows_as_it_says(tr):
+    """More than a launch of a thread for every value would have threads: refused for what is missing and not for their number."""
+    for d in (32, 64, 96, 128):
+        r = tr.ColbanditRotation(1, 1, 1, d, 0, 1e-6, (1 << 31) - (1 << 16) - 1, 1, 0x1000, 0x2000, d, d, d, d, None, None, None, None)
+        assert tr.lib().colbandit_norm_rotate(r, None, None, None) == -1
+        assert tr.lib().colbandit_norm_rotate_backward(r, None, None, None, None, None, None, None, 0, None) == -1
+
+
 def test_python_refusals(tr):
     """Shapes, types and places are checked before the library is called."""
     W, t = torch.zeros(5, 8), torch.zeros(3, dtype=torch.int64)
