@@ -178,9 +178,14 @@ def _attn(q, k, v, q_offsets, k_offsets, causal, scale, keep, bias, max_distance
             raise ValueError("bias is a contiguous [n_buckets, heads]")
     _on_device(q, k, v, q_offsets, k_offsets, keep, bias)
     return ColbanditAttn(
-        dt, n - 1, heads, kv_heads, d, 1 if causal else 0, 0 if bias is None else bias.shape[0], int(max_distance),
+        dt, n - 1, heads, kv_heads, d, 1 if causal else 0, 0 if bias is None else bias.shape[0], _within(int(max_distance), 30),
         1.0 / math.sqrt(d) if scale is None else scale, total_q, total_k, q_offsets.data_ptr(), k_offsets.data_ptr(),
         q.data_ptr(), k.data_ptr(), v.data_ptr(), q_row, q_head, k_row, k_head, v_row, v_head, _ptr(keep), _ptr(bias))
+
+
+def _within(x, bits):
+    """A whole number, cut to what fits (ctypes would leave out its upper bits)."""
+    return max(-1 << bits, min(index(x), 1 << bits))
 
 
 def _window(window, sinks):
@@ -190,8 +195,7 @@ def _window(window, sinks):
             raise ValueError("sinks come with a window")
         return None
     before, after = window
-    most = 1 << 62                                   # (ctypes would cut what does not fit)
-    return ColbanditWindow(min(index(before), most), min(index(after), most), min(index(sinks), most))
+    return ColbanditWindow(*(_within(x, 62) for x in (before, after, sinks)))
 
 
 def _like(t):
@@ -486,7 +490,7 @@ def _orthogonalise(matrices, steps, coefficients, out, workspace=None):
     L = lib()
     ws, nb = _workspace(workspace, L.colbandit_orthogonalise_workspace_bytes(n, rows, cols), matrices[0].device)
     args = (n, pointers(*[m.data_ptr() for m in matrices]), pointers(*[o.data_ptr() for o in to]), rows, cols,
-            (ctypes.c_int32 * n)(*[_DTYPES[m.dtype] for m in matrices]), steps, (ctypes.c_float * 3)(*coefficients), _ptr(ws))
+            (ctypes.c_int32 * n)(*[_DTYPES[m.dtype] for m in matrices]), _within(steps, 30), (ctypes.c_float * 3)(*coefficients), _ptr(ws))
     return to, lambda room=True: L.colbandit_orthogonalise(*args, nb if room else 0, _stream())
 
 

@@ -1234,6 +1234,18 @@ def test_rotation_takes_as_many_rows_as_it_says(tr):
         assert tr.lib().colbandit_norm_rotate_backward(r, None, None, None, None, None, None, None, 0, None) == -1
 
 
+def test_numbers_beyond_the_librarys_types_keep_their_sign(tr, monkeypatch):
+    w = tr._window((-(1 << 64) + 5, 1 << 64), 3)
+    assert w.before < 0 and w.after == 1 << 62
+    assert tr._window((1, 1), -(1 << 64) + 1).sinks < 0
+    monkeypatch.setattr(tr, "_on_device", lambda *t: 0)
+    monkeypatch.setattr(tr, "_workspace", lambda *a: (None, 0))
+    monkeypatch.setattr(tr, "_stream", lambda *a: None)
+    for steps in ((1 << 32) + 5, -(1 << 32) + 5):
+        with pytest.raises(tr.ColbanditError, match="-[23]"):
+            tr.colbandit_orthogonalise([torch.zeros(4, 5)], steps=steps)
+
+
 def test_python_refusals(tr):
     """Shapes, types and places are checked before the library is called."""
     W, t = torch.zeros(5, 8), torch.zeros(3, dtype=torch.int64)
