@@ -1070,6 +1070,41 @@ def test_an_encoder_of_all_of_them(tr, dev, positions):
     assert all(math.isfinite(x) for x in a["losses"] + a["norms"]) and a["losses"] == b["losses"] and a["norms"] == b["norms"]
 
 
+@pytest.mark.parametrize("window", [None, 7])
+@pytest.mark.parametrize("positions", ["bias", "rotary"])
+def test_the_examples_encoder_says_what_it_means(tr, monkeypatch, positions, window):
+    """What the example's encoder asks of the operators, by stand-ins: each row's place in its own sequence, empty ones among them, the
+    window to both sides with the first key, the mask and the bias."""
+    from paper_2602_02827_amd import finetune
+    asked = {}
+
+    def rotate(q, k, **how):
+        asked.update(how)
+        return q, k
+
+    def attend(q, k, v, off, **how):
+        asked.update(how, off=off)
+        return v
+
+    monkeypatch.setattr(tr, "embedding", lambda W, t: W[t])
+    monkeypatch.setattr(tr, "norm_rotate", rotate)
+    monkeypatch.setattr(tr, "attention", attend)
+    encoder = finetune.Encoder(positions, window)
+    lengths = [20, 0, 150, 1, 33]
+    off, tokens = offsets(lengths), torch.randint(0, 2 * finetune.WORDS, (sum(lengths),), generator=torch.Generator().manual_seed(3))
+    out = encoder(tokens, off)
+    assert out.shape == (sum(lengths), finetune.EMBED) and asked["off"] is off
+    assert torch.equal(asked["keep"], tokens >= finetune.PUNCTUATION)
+    assert asked.get("window") == (None if window is None else (window, window)) and asked.get("sinks", 0) == (0 if window is None else 1)
+    if positions == "rotary":
+        assert torch.equal(asked["positions"], torch.cat([torch.arange(n) for n in lengths])) and asked["table"].shape[0] >= max(lengths)
+        assert asked["q_weight"] is encoder.q_weight and asked["k_weight"] is encoder.k_weight and "bias" not in asked
+    else:
+        assert torch.equal(asked["bias"], encoder.bias.bfloat16()) and asked["max_distance"] == finetune.MAX_DISTANCE
+    out.float().square().sum().backward()
+    assert bool(encoder.tokens.grad.any()) and bool(encoder.qkv.weight.grad.any())
+
+
 @gpu
 def test_gradients_through_lookup_rotation_and_window(tr, dev):
     """Token table to attention's output and back, against the same by torch in 64 bits."""
