@@ -21,7 +21,7 @@ namespace {
 // polynomial and the sizes: WIDE, where what is lost could be raised to more than kLost of the result, or where small values become
 // smaller, X, A and B are held in 32 bits, and cut into three bf16 pieces as they are multiplied (six products of pieces, what is left
 // out is 2^-26).  (128 x 512, rows that fall to 10^-8 of the first, twelve usual steps: 7.7e-5 off in pieces, 7e-7 so, plain 32-bit
-// products 3e-6; five steps: 5e-7, 3e-7 and 1.4e-6.  An encoder's 25 matrices, five steps: 1,610 us in pieces, 3,410 WIDE; one of 768 x 128: 99 and
+// products 3e-6; five steps: 5e-7, 3e-7 and 1.4e-6.  An encoder's 25 matrices, five steps: 1,575 us in pieces, 3,280 WIDE; one of 768 x 128: 99 and
 // 155.)
 constexpr double kLost = 0x1p-19;
 constexpr double kSmallest = 0x1p-24 / 3.4641016151377544;       // root mean square of a second piece's rounding, of which 2^-24 is the last place
@@ -268,7 +268,7 @@ template <> struct Stored<true> {
 // DEEP: that many groups of four wavefronts share a tile, each with every DEEP-th tile of k; their sums are added in their order.
 template <int T, int DEEP, int AHEAD, bool WIDE, int STEP, bool LAST>
 __global__ __launch_bounds__(DEEP * kThreads, DEEP > 1 ? DEEP : 2) void k_ortho_product(const OrthoTable* __restrict__ table, char* ws, int odd,
-                                                                                        int back, float by, float more) {
+                                                                                        int back, float scale, float more) {
     constexpr int NB = T / 64;                       // blocks of 32 of a wavefront's side
     constexpr int BYTES = 2 * T * kLine, COPIES = T / 16;
     __shared__ __align__(256) char lds[DEEP][AHEAD + 1][BYTES];
@@ -429,6 +429,7 @@ __global__ __launch_bounds__(DEEP * kThreads, DEEP > 1 ? DEEP : 2) void k_ortho_
                 *(f32x4*)(tile_of + deep * T * T + place(wi + 32 * y + n, wj + 32 * x + 8 * r + 4 * h)) =
                     f32x4{acc[x][y][4 * r], acc[x][y][4 * r + 1], acc[x][y][4 * r + 2], acc[x][y][4 * r + 3]};
     char* to = ws + (STEP == GRAM ? M.a : STEP == SQUARE ? M.b : odd ? M.x : M.y);
+    const float by = STEP == GRAM ? (WIDE ? 1.f : kGramScale) : scale;
     constexpr bool AGAIN = STEP != GRAM || DEEP > 1;              // the transpose is stored from what was stored
     const bool mirrored = STEP != APPLY && ti != tj, again = STEP == APPLY ? LAST && M.tall : mirrored;
     __syncthreads();
@@ -557,7 +558,7 @@ hipError_t launch_product(const OrthoGroup& G, const OrthoEnds& ends, char* ws, 
     const OrthoTable* t = (const OrthoTable*)(ws + G.table);
     // what a tile is multiplied by as it is stored, and what it is added to; the pieces' scales among them (the last step's are taken out)
     const float last = LAST ? 1.f / K.scale_x : 1.f;
-    const float by = STEP == GRAM ? K.scale_a / (K.scale_x * K.scale_x) : STEP == SQUARE ? K.c * (K.scale_b / (K.scale_a * K.scale_a)) : last / K.scale_b;
+    const float by = STEP == SQUARE ? K.c * (K.scale_b / (K.scale_a * K.scale_a)) : last / K.scale_b;       // (GRAM: a constant)
     const float more = STEP == SQUARE ? K.b * (K.scale_b / K.scale_a) : K.a * last;
     if (G.tile == 128) k_ortho_product<128, 1, 1, WIDE, STEP, LAST><<<grid, kThreads, 0, st>>>(t, ws, odd, back, by, more);
     else if (grid.x <= 256) k_ortho_product<64, 4, 1, WIDE, STEP, LAST><<<grid, 4 * kThreads, 0, st>>>(t, ws, odd, back, by, more);

@@ -103,6 +103,9 @@ size_t rotate_workspace_bytes(const RotateArgs& A, int d);
 hipError_t launch_rotate(const RotateArgs& A, int d, int dt, hipStream_t st);
 hipError_t launch_rotate_backward(const RotateArgs& A, int d, int dt, float* dq_weight, float* dk_weight, hipStream_t st);
 
+// A's scale is X's squared times this, so that what the product of its pieces is multiplied by is a constant: X's is at most 2^15, and
+// 49,152 by the largest singular value, which leaves A below 36,864.  (As an argument it cost an encoder's matrices 1,608 us for 1,585.)
+constexpr float kGramScale = 0x1p-16f;
 // A polynomial a s + b s^3 + c s^5 and what is known of its steps from singular values of up to one on.
 struct OrthoPolynomial {
     float a, b, c;

@@ -338,7 +338,8 @@ bool polynomial_holds(const float* k, int steps, OrthoPolynomial& P) {
             if (roots[i] > 0.0 && roots[i] < u1) next = fmax(next, value(roots[i]));
         most = next;
     }
-    P = {k[0], k[1], k[2], scale_for(most_x), scale_for(most_x * most_x), scale_for(most_b), fabs(a) < 1.0 ? (double)INFINITY : raised};
+    const float x = scale_for(most_x);
+    P = {k[0], k[1], k[2], x, x * x * kGramScale, scale_for(most_b), fabs(a) < 1.0 ? (double)INFINITY : raised};
     return most <= 4.0;
 }
 
