@@ -490,8 +490,8 @@ def _orthogonalise(matrices, steps, coefficients, out, workspace=None):
     L = lib()
     ws, nb = _workspace(workspace, L.colbandit_orthogonalise_workspace_bytes(n, rows, cols), matrices[0].device)
     args = (n, pointers(*[m.data_ptr() for m in matrices]), pointers(*[o.data_ptr() for o in to]), rows, cols,
-            (ctypes.c_int32 * n)(*[_DTYPES[m.dtype] for m in matrices]), _within(steps, 30), (ctypes.c_float * 3)(*coefficients), _ptr(ws))
-    return to, lambda room=True: L.colbandit_orthogonalise(*args, nb if room else 0, _stream())
+            (ctypes.c_int32 * n)(*[_DTYPES[m.dtype] for m in matrices]), _within(steps, 30), (ctypes.c_float * 3)(*coefficients))
+    return to, lambda room=True: L.colbandit_orthogonalise(*args, _ptr(ws), nb if room else 0, _stream())      # (and it holds ws)
 
 
 # ---- as parts of a torch program ---------------------------------------------------------------------

@@ -983,6 +983,26 @@ def test_extreme_matrices(tr, dev):
 
 
 @gpu
+def test_extreme_matrices_of_many_steps(tr, dev):
+    """The same of values that are held in 32 bits, and in place, in a graph and on another stream."""
+    base = updates([(40, 50)], "f32", dev, seed=6)[0]
+    bad, nan = base.clone(), base.clone()
+    bad[3, 4], nan[39, 49] = -math.inf, math.nan
+    big, small = base / base.abs().max() * 3e38, base * 1e-38
+    m, how = [base, torch.zeros_like(base), bad, big, nan, small], dict(steps=12)
+    out = tr.colbandit_orthogonalise(m, **how)["out"]
+    assert torch.equal(out[0], tr.colbandit_orthogonalise([base], **how)["out"][0])
+    assert not bool(out[1].any()) and bool(out[2].isnan().all()) and bool(out[4].isnan().all())
+    check_orthogonal([base, big, small], [out[0], out[3], out[5]], 12)
+    m = updates([(50, 90), (200, 64), (700, 720)], "bf16", dev, seed=7)
+    want = tr.colbandit_orthogonalise(m, **how)["out"]
+    copies = [x.clone() for x in m]
+    tr.colbandit_orthogonalise(copies, out=copies, **how)
+    assert all(torch.equal(a, b) for a, b in zip(copies, want))
+    captured(dev, lambda: dict(enumerate(tr.colbandit_orthogonalise(m, **how)["out"])))
+
+
+@gpu
 def test_orthogonalising_in_place_in_graphs_and_steps(tr, dev):
     m = updates([(50, 90), (200, 64), (64, 64)], "bf16", dev, seed=7)
     want = tr.colbandit_orthogonalise(m)["out"]
@@ -1279,6 +1299,34 @@ def test_numbers_beyond_the_librarys_types_keep_their_sign(tr, monkeypatch):
     for steps in ((1 << 32) + 5, -(1 << 32) + 5):
         with pytest.raises(tr.ColbanditError, match="-[23]"):
             tr.colbandit_orthogonalise([torch.zeros(4, 5)], steps=steps)
+
+
+def test_an_orthogonal_steps_workspace_lives_until_it_is_used(tr, monkeypatch):
+    """From the checks, through what is done before the call, to the call."""
+    import gc
+    import types
+    import weakref
+    held, calls = [], []
+
+    def call(*args):
+        gc.collect()
+        calls.append((args[-2], [x() is not None for x in held]))
+        return 0 if args[-2] else -5
+
+    def workspace(ws, need, device):
+        ws = torch.zeros(need, dtype=torch.uint8)
+        held.append(weakref.ref(ws))
+        return ws, need
+
+    monkeypatch.setattr(tr, "_on_device", lambda *t: 0)
+    monkeypatch.setattr(tr, "_stream", lambda *a: None)
+    monkeypatch.setattr(tr, "_workspace", workspace)
+    monkeypatch.setattr(tr, "lib", lambda: types.SimpleNamespace(colbandit_orthogonalise=call, colbandit_orthogonalise_workspace_bytes=lambda *a: 64))
+    p = torch.nn.Parameter(torch.zeros(4, 5))
+    p.grad = torch.ones(4, 5)
+    tr.orthogonal_step_([p], {}, rate=0.1)
+    tr.colbandit_orthogonalise([p.grad])
+    assert [room for room, _ in calls] == [0, 64, 64] and [alive[-1] for _, alive in calls] == [True] * 3
 
 
 def test_python_refusals(tr):
