@@ -336,8 +336,10 @@ constexpr float kLag = 8.f;
 // parts.
 // Through a window (WIN) only tiles that some row sees are gone over, and tiles of the first keys; what a row sees of a tile is a bit a key.
 // 6 documents of 500 to 8,191 tokens, 12 heads of 64, 64 keys to either side, one first key: 58 us, 10.3 GFLOP of 161 MB (38
-// with a window of one key).  A workgroup's 128 rows see 256 keys together and 129 each, so half of the products and exponentials are of
-// hidden keys; vector instructions (1,500 of a wavefront) and what comes before the first product bound it.  16 single tokens that see 1,028 of up to 16,385 keys: 9 us and 4 us to join.
+// with a window of one key).  A workgroup's 128 rows see 256 keys together and 129 each.  A wavefront's 32 rows see 160, and it passes over
+// tiles, and halves of them, that are not among them: it multiplies six and a half blocks of 32 keys, of which 37 % of the scores are hidden,
+// and waits at the nine or ten that the others need.  Vector instructions (1,500 of a wavefront) and what comes before the first product
+// bound it.  16 single tokens that see 1,028 of up to 16,385 keys: 9 us and 4 us to join.
 template <class E, int D, bool BIAS, bool MASKED, bool WIN>
 __global__ __launch_bounds__(64 * kWavefronts, (kWaves<E, D>)) void k_attention(const AttnArgs A, int slots, int order, int units, int run,
                                                                            int splits, E* out, float* lse, float* o_part,

@@ -500,6 +500,9 @@ OrthoGroup group_from(int64_t first, int64_t n, const int64_t* rows, const int64
         const int64_t m = rows[i] < cols[i] ? rows[i] : cols[i], across = (m + 127) / 128;
         half += across * (across + 1) / 2;
     }
+    // Large tiles where they fill the CUs.  (Five steps, us, with 128 and 64: 16 matrices of 768 x 768, 336 such tiles, 705 and 740; 8 of
+    // 1,024, 288, 730 and 834; 4 of 768, 84, 362 and 270; 24 of 384, 144, 266 and 225.  Some long sums gain below that too: 4 of 1,024,
+    // 144, 472 and 505.)
     G.tile = half >= 256 ? 128 : 64;
     size_t at = 0;
     auto take = [&](int64_t bytes) {
@@ -621,7 +624,8 @@ hipError_t launch_ortho(int64_t n, const void* const* in, void* const* out, cons
         const OrthoGroup G = group_from(i, n, rows, cols, in, out, dts);
         i = G.end;
         if (!G.t.n) continue;
-        const hipError_t e = pieces_hold(G, polynomial) ? launch_group<false>(G, ws, steps, polynomial, st) : launch_group<true>(G, ws, steps, whole, st);
+        const hipError_t e = pieces_hold(G, polynomial) ? launch_group<false>(G, ws, steps, polynomial, st)
+                                                        : launch_group<true>(G, ws, steps, whole, st);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;

@@ -207,7 +207,9 @@ __global__ __launch_bounds__(kJoinThreads) void k_rotate_join(const float* part,
     if (to) to[at < d ? at : at - d] = s;
 }
 
-// Heads of a row are dealt to several groups where rows are few.
+// Heads of a row are dealt to several groups where rows are few: until there are 2^19 lanes.  (Forward, bf16, us, with 2^17, 2^19 and 2^21:
+// 11 thousand rows of 10 heads of 128 11.4, 13.7 and 16.0; 20 thousand of 24 heads of 64 22.1, 20.6 and 32.5; 54 thousand 75.6, 68.5 and
+// 77.3; up to 2.7 thousand alike.)
 int lg_parts_of(const RotateArgs& A, int lanes) {
     int lg = 0;
     while (2 << lg <= A.heads + A.kv_heads && (A.rows * lanes << lg) < 1 << 19) ++lg;

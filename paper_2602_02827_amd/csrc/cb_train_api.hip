@@ -193,7 +193,10 @@ int window_args(const colbandit_attn* a, const colbandit_window* w, AttnArgs& A)
     A.sinks = (int)w->sinks;
     // Short enough for an even load, since workgroups of the first keys have little to do at a time, as long as that costs little
     // workspace.  (8 documents of 2,048 tokens, two key heads of 128 under eight, a window of 256 rows and four first keys, with
-    // gradients: 216 us, with 256 rows 232, with 512 242; of up to 4,095 tokens, heads of 64: 175, 164 and 167.)
+    // gradients: 216 us, with 256 rows 232, with 512 242; of up to 4,095 tokens, heads of 64: 175, 164 and 167.
+    // More first keys are more workgroups, and more shares to add up: backward pass of the first documents with 200 of them, in chunks of
+    // 256 and of 512 rows, 231 and 237 us, with 300 266 and 254; 26 pages of 1,030 tokens, six heads of 64, 100 first keys, 142 and 137,
+    // with 300 223 and 198.)
     A.sink_rows = A.sinks > 256 ? 512 : A.sinks > 64 || !two_for_keys(a->d, (int)size_of(a->dt)) ? 256 : 128;
     return COLBANDIT_OK;
 }
